@@ -240,7 +240,9 @@ dsmp_status dsmp_radius_graph_edges(dsmp_handle* h, const dsmp_graph_query* q, v
  * dim in {2, 3}; other values give UNSUPPORTED.
  */
 enum { DSMP_F32 = 0, DSMP_BF16 = 1 };
-enum { DSMP_ACT_IDENTITY = 0, DSMP_ACT_RELU = 1 };
+/* A layer takes the first two activations, a norm (below) all four:
+ * SiLU z / (1 + e^-z), and GELU z Phi(z) with the normal distribution's Phi. */
+enum { DSMP_ACT_IDENTITY = 0, DSMP_ACT_RELU = 1, DSMP_ACT_SILU = 2, DSMP_ACT_GELU = 3 };
 enum { DSMP_ATTR_CONCAT = 0, DSMP_ATTR_DIFF = 1 };
 /* Backward flags: DSMP_GRAD_ACCUMULATE adds parameter gradients to the
  * caller's arrays (parameters shared by several layers or hops);
@@ -374,6 +376,103 @@ dsmp_status dsmp_masked_mse_workspace(int64_t n, size_t* bytes);
 dsmp_status dsmp_masked_mse(dsmp_handle* h, const float* pred, const float* target, const uint8_t* mask,
                             int64_t n, int32_t c, float* loss, float* grad, void* ws, size_t ws_bytes);
 
+/* ------------------------------------------------ checkpoints in 8 bits
+ * An activation kept for the backward pass in 8 bits per value: for each row,
+ * blocks of 64 consecutive channels (the last one shorter) share one float32
+ * scale.  With a = max |x| of the block, in float32:
+ *     scale = a * fl(1/127),  q = rint(x * (127 / a))  (ties to even, |q| <= 127)
+ * and the value that is kept is q * scale, within scale / 2 of x (and a
+ * rounding).  A block with a < 2^-100 is kept as zeros (scale 0); a block that
+ * holds an infinity or a NaN is kept as NaN (scale NaN, q 0), so that an
+ * overflow is not lost.  Channels: 1..512, others give UNSUPPORTED.
+ *
+ * q: device int8 [n, channels]; scale: device float32 [n, ceil(channels/64)].
+ * Both rows are contiguous; the buffers are the caller's. */
+typedef struct dsmp_checkpoint {
+  int8_t* q;
+  float* scale;
+} dsmp_checkpoint;
+
+/* x: device [n, channels] of dtype DSMP_F32 or DSMP_BF16, rows ldx elements
+ * apart (ldx >= channels; any alignment of its type; so for every matrix of
+ * this section and the next).  n == 0 enqueues nothing. */
+dsmp_status dsmp_checkpoint_store(dsmp_handle* h, const void* x, int32_t dtype, int64_t ldx, int64_t n,
+                                  int32_t channels, const dsmp_checkpoint* ck);
+
+/* y = the kept values, rounded to dtype (DSMP_F32: exactly q * scale). */
+dsmp_status dsmp_checkpoint_load(dsmp_handle* h, const dsmp_checkpoint* ck, int64_t n, int32_t channels, void* y,
+                                 int32_t dtype, int64_t ldy);
+
+/* ------------------------------------------- group norm with an activation
+ * Normalisation of node features between layers, channels last.  The n rows
+ * are packed segments (sub-graphs one after another); the channels form
+ * `groups` groups of c = channels / groups.  For each segment s and group g,
+ * over the m = rows(s) * c values t of both (t = x, or the sum with an addend):
+ *     mean = sum t / m,  var = sum (t - mean)^2 / m,  rstd = 1 / sqrt(var + eps)
+ *     xn = (t - mean) * rstd,  z = gamma xn + beta,  y = act(z)
+ * Statistics and sums are float32 or wider whatever the types.  Segments of no
+ * rows get mean 0 and rstd 0.  groups = 1 with one row to a segment is a
+ * normalisation of every row over its channels. */
+typedef struct dsmp_norm_desc {
+  int32_t channels;  /* 1..512, others give UNSUPPORTED */
+  int32_t groups;    /* divides channels */
+  int32_t x_dtype;   /* of x, addend and sum: DSMP_F32 or DSMP_BF16 */
+  int32_t y_dtype;   /* of y */
+  int32_t act;       /* DSMP_ACT_* */
+  float eps;         /* >= 0 */
+} dsmp_norm_desc;
+
+/* n rows in n_seg >= 1 segments.  ptr: device int32 [n_seg + 1], ascending from
+ * 0 to n (segment s has the rows [ptr[s], ptr[s+1])); its values are read on the
+ * device only, and limited to [0, n]: rows past a wrong one go to some segment,
+ * no access leaves the arrays.  ptr NULL: equal segments of n / n_seg rows
+ * (INVALID_ARG if n_seg does not divide n); n_seg == n makes each row a segment. */
+typedef struct dsmp_segments {
+  int64_t n;
+  int64_t n_seg;
+  const int32_t* ptr;
+} dsmp_segments;
+
+/* Workspace bytes of the forward and backward calls on such segments. */
+dsmp_status dsmp_group_norm_workspace(const dsmp_norm_desc* desc, const dsmp_segments* seg, size_t* fwd_ws_bytes,
+                                      size_t* bwd_ws_bytes);
+
+/* Forward.  x: device [n, channels] of x_dtype.  addend: NULL, or device
+ * [n, channels] of x_dtype; then t = x + addend rounded to x_dtype, and `sum`
+ * (required with an addend, else NULL) receives t; sum may be x or addend
+ * itself (with its row distance).  gamma, beta: device float32 [channels], or
+ * both NULL (1 and 0).  y: device [n, channels] of y_dtype.  stats: device
+ * float32 [n_seg, groups, 2], receives mean and rstd, which the calls below
+ * take.  ck: NULL, or a checkpoint of t to write in the same pass.  Apart from
+ * sum, outputs do not overlap inputs.  n == 0 writes the statistics only. */
+dsmp_status dsmp_group_norm_forward(dsmp_handle* h, const dsmp_norm_desc* desc, const dsmp_segments* seg,
+                                    const void* x, int64_t ldx, const void* addend, int64_t lda, void* sum,
+                                    int64_t lds, const float* gamma, const float* beta, void* y, int64_t ldy,
+                                    float* stats, const dsmp_checkpoint* ck, void* ws, size_t ws_bytes);
+
+/* y again from a checkpoint of t and the kept statistics (the operand of a
+ * layer that is run a second time in the backward pass).  x_dtype is not used. */
+dsmp_status dsmp_group_norm_restore(dsmp_handle* h, const dsmp_norm_desc* desc, const dsmp_segments* seg,
+                                    const dsmp_checkpoint* ck, const float* stats, const float* gamma,
+                                    const float* beta, void* y, int64_t ldy);
+
+/* Backward, from t itself (x: device [n, channels] of x_dtype, ck NULL) or from
+ * its checkpoint (x NULL): with w = grad_y act'(z) (ReLU'(0) = 0), sums over a
+ * segment's group and over all rows,
+ *     A = sum gamma w / m,  B = sum gamma w xn / m
+ *     grad_x = grad_addend + rstd (gamma w - A - xn B)
+ *     dbeta = sum w,  dgamma = sum w xn
+ * mean and rstd are those of stats.  grad_y, grad_x: device float32
+ * [n, channels].  grad_addend: NULL, or device float32 [n, channels] (the
+ * gradient that passes by the norm on the residual path); it may be grad_x
+ * itself.  dgamma, dbeta: device float32 [channels] (NULL when gamma and beta
+ * are), overwritten, or added to when flags has DSMP_GRAD_ACCUMULATE. */
+dsmp_status dsmp_group_norm_backward(dsmp_handle* h, const dsmp_norm_desc* desc, const dsmp_segments* seg,
+                                     const void* x, int64_t ldx, const dsmp_checkpoint* ck, const float* stats,
+                                     const float* gamma, const float* beta, const float* grad_y, int64_t ldgy,
+                                     const float* grad_addend, int64_t ldga, float* grad_x, int64_t ldgx,
+                                     float* dgamma, float* dbeta, int32_t flags, void* ws, size_t ws_bytes);
+
 /* How the layer evaluates the edge contraction.  DSMP_EDGE_PER_EDGE forms
  * each message m_e on MFMA (edge tiles against streamed W3 chunks) and sums
  * them per destination.  DSMP_EDGE_AGGREGATE uses the linearity of the mean:
@@ -422,7 +521,9 @@ enum {
   DSMP_K_LOSS = 21,     /* masked mean squared error */
   DSMP_K_DH_U = 22,     /* per-edge feature-gradient terms from U (aggregate form, bf16) */
   DSMP_K_DA1 = 23,      /* da1 from the stored da2 (aggregate form, bf16: d = 128, large d = 64) */
-  DSMP_K_COUNT = 24
+  DSMP_K_NORM = 24,     /* group norms, forward, restored and backward */
+  DSMP_K_CKPT = 25,     /* checkpoints in 8 bits, stored and loaded */
+  DSMP_K_COUNT = 26
 };
 dsmp_status dsmp_profile_enable(dsmp_handle* h, int enable);
 dsmp_status dsmp_profile_reset(dsmp_handle* h);

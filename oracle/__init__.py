@@ -24,10 +24,12 @@ Contents, each following the paper passage named in its module docstring:
                       sub-domain, forward and backward.
 * ``infer``        -- sub-domain inference with reassembly (Sec. 3, testing
                       procedure).
+* ``norm``         -- group norm with an activation over packed segments, its
+                      gradients, and checkpoints in 8 bits.
 
 Floating point: the layer runs in float64.  The radius test runs in float32
 in a fixed evaluation order (no fused multiply-add), because the paper fixes
 no precision and the GPU must reproduce the edge set bit for bit.
 """
 
-from . import rng, sampling, radius_graph, nnconv, hop, infer  # noqa: F401
+from . import rng, sampling, radius_graph, nnconv, hop, infer, norm  # noqa: F401

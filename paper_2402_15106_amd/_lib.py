@@ -23,7 +23,7 @@ STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "CAPACITY", 3: "HIP_ERROR", 4: "UN
                 5: "WORKSPACE_TOO_SMALL"}
 CAP_KNN, CAP_RANDOM = 0, 1
 F32, BF16 = 0, 1
-ACT_IDENTITY, ACT_RELU = 0, 1
+ACT_IDENTITY, ACT_RELU, ACT_SILU, ACT_GELU = range(4)
 ATTR_CONCAT, ATTR_DIFF = 0, 1
 GRAD_ACCUMULATE = 1
 GRAD_X_ACCUMULATE = 2
@@ -38,12 +38,14 @@ EXPORTED = ["dsmp_version", "dsmp_create", "dsmp_destroy", "dsmp_set_stream", "d
             "dsmp_nnconv_packed_bytes", "dsmp_nnconv_pack", "dsmp_nnconv_workspace",
             "dsmp_nnconv_forward", "dsmp_nnconv_backward", "dsmp_profile_enable", "dsmp_profile_reset",
             "dsmp_profile_read", "dsmp_set_edge_algorithm", "dsmp_mlp_workspace", "dsmp_mlp_forward",
-            "dsmp_mlp_backward", "dsmp_masked_mse_workspace", "dsmp_masked_mse"]
+            "dsmp_mlp_backward", "dsmp_masked_mse_workspace", "dsmp_masked_mse",
+            "dsmp_checkpoint_store", "dsmp_checkpoint_load", "dsmp_group_norm_workspace", "dsmp_group_norm_forward",
+            "dsmp_group_norm_restore", "dsmp_group_norm_backward"]
 
 # kernel classes of the opt-in timing (dsmp_profile_*)
 KERNEL_CLASSES = ["sample", "gather", "graph", "edge_fwd", "node_fwd", "node_bwd", "edge_dh", "dh_final",
                   "dz", "dW3", "dW2", "dW1", "reduce", "edge_mlp", "outer_fwd", "gemm_fwd", "outer_dh",
-                  "gemm_dh", "u_gemm", "attr", "mlp", "loss", "dh_u", "da1"]
+                  "gemm_dh", "u_gemm", "attr", "mlp", "loss", "dh_u", "da1", "norm", "ckpt"]
 
 
 class DsmpError(RuntimeError):
@@ -90,7 +92,21 @@ class MlpGrads(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("dW1", "db1", "dW2", "db2", "dW3", "db3")]
 
 
+class NormDesc(ctypes.Structure):
+    _fields_ = [("channels", ctypes.c_int32), ("groups", ctypes.c_int32), ("x_dtype", ctypes.c_int32),
+                ("y_dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class CSegments(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("n_seg", ctypes.c_int64), ("ptr", ctypes.c_void_p)]
+
+
+class CCheckpoint(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+
+
 _P = ctypes.c_void_p
+_I64 = ctypes.c_int64
 _SIG = {
     "dsmp_version": (ctypes.c_int, []),
     "dsmp_create": (ctypes.c_int, [ctypes.POINTER(ctypes.c_void_p), ctypes.c_int]),
@@ -136,6 +152,20 @@ _SIG = {
                                          ctypes.c_size_t]),
     "dsmp_masked_mse_workspace": (ctypes.c_int, [ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t)]),
     "dsmp_masked_mse": (ctypes.c_int, [_P, _P, _P, _P, ctypes.c_int64, ctypes.c_int32, _P, _P, _P, ctypes.c_size_t]),
+    "dsmp_checkpoint_store": (ctypes.c_int, [_P, _P, ctypes.c_int32, _I64, _I64, ctypes.c_int32,
+                                             ctypes.POINTER(CCheckpoint)]),
+    "dsmp_checkpoint_load": (ctypes.c_int, [_P, ctypes.POINTER(CCheckpoint), _I64, ctypes.c_int32, _P, ctypes.c_int32,
+                                            _I64]),
+    "dsmp_group_norm_workspace": (ctypes.c_int, [ctypes.POINTER(NormDesc), ctypes.POINTER(CSegments),
+                                                 ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(ctypes.c_size_t)]),
+    "dsmp_group_norm_forward": (ctypes.c_int, [_P, ctypes.POINTER(NormDesc), ctypes.POINTER(CSegments), _P, _I64, _P,
+                                               _I64, _P, _I64, _P, _P, _P, _I64, _P, ctypes.POINTER(CCheckpoint), _P,
+                                               ctypes.c_size_t]),
+    "dsmp_group_norm_restore": (ctypes.c_int, [_P, ctypes.POINTER(NormDesc), ctypes.POINTER(CSegments),
+                                               ctypes.POINTER(CCheckpoint), _P, _P, _P, _P, _I64]),
+    "dsmp_group_norm_backward": (ctypes.c_int, [_P, ctypes.POINTER(NormDesc), ctypes.POINTER(CSegments), _P, _I64,
+                                                ctypes.POINTER(CCheckpoint), _P, _P, _P, _P, _I64, _P, _I64, _P, _I64,
+                                                _P, _P, ctypes.c_int32, _P, ctypes.c_size_t]),
     "dsmp_profile_enable": (ctypes.c_int, [_P, ctypes.c_int]),
     "dsmp_profile_reset": (ctypes.c_int, [_P]),
     "dsmp_profile_read": (ctypes.c_int, [_P, ctypes.c_int, ctypes.POINTER(ctypes.c_double),
@@ -182,6 +212,27 @@ class Graph:
         return CGraph(self.n_dst, self.n_src, self.n_edges, self.row_ptr.data_ptr(),
                       self.col.data_ptr(), self.dst.data_ptr(), self.csc_ptr.data_ptr(),
                       self.csc_eid.data_ptr())
+
+
+@dataclass
+class Checkpoint:
+    """Rows of values kept in 8 bits: q int8 [n, channels], scale float32
+    [n, ceil(channels / 64)], both contiguous."""
+    q: torch.Tensor
+    scale: torch.Tensor
+
+    @staticmethod
+    def empty(n: int, channels: int, device) -> "Checkpoint":
+        return Checkpoint(torch.empty(n, channels, dtype=torch.int8, device=device),
+                          torch.empty(n, (channels + 63) // 64, dtype=torch.float32, device=device))
+
+
+def norm_desc(channels, groups, x_dtype, y_dtype, act=ACT_IDENTITY, eps=1e-5) -> NormDesc:
+    return NormDesc(channels, groups, x_dtype, y_dtype, act, eps)
+
+
+_TORCH = {F32: torch.float32, BF16: torch.bfloat16}
+_CODE = {torch.float32: F32, torch.bfloat16: BF16}
 
 
 def layer_desc(dim, d, h1, h2, dtype, act=ACT_IDENTITY, residual=1, attr_mode=ATTR_CONCAT) -> LayerDesc:
@@ -480,3 +531,143 @@ class Dsmp:
         self._check(self.lib.dsmp_masked_mse(self.h, _ptr(pred), _ptr(target), _ptr(mask), n, c, _ptr(loss),
                                              _ptr(grad), _ptr(ws), ws.numel()), self.h)
         return loss, grad
+
+    # ------------------------------------------------------------ checkpoints in 8 bits and group norm
+    def _rows(self, t, name, n, channels, dtype):
+        """(address, row distance) of a matrix [n, channels] whose rows are contiguous."""
+        if not (isinstance(t, torch.Tensor) and t.device == self.device and t.dtype == dtype and t.dim() == 2
+                and t.shape[0] == n and t.shape[1] == channels):
+            raise DsmpError(INVALID_ARG, "%s: a %s [%d, %d] on %s is needed" % (name, dtype, n, channels, self.device))
+        ld = t.stride(0) if n > 1 else channels
+        if (channels > 1 and t.stride(1) != 1) or ld < channels:
+            raise DsmpError(INVALID_ARG, "%s: rows must be contiguous and not overlap" % name)
+        return t.data_ptr(), ld
+
+    def _flat(self, t, name, shape, dtype=torch.float32):
+        """Address of a contiguous array of a shape."""
+        if not (isinstance(t, torch.Tensor) and t.device == self.device and t.dtype == dtype
+                and tuple(t.shape) == shape and t.is_contiguous()):
+            raise DsmpError(INVALID_ARG, "%s: a contiguous %s %s on %s is needed" % (name, dtype, list(shape), self.device))
+        return t.data_ptr()
+
+    def _checkpoint(self, ck, n, channels):
+        if not isinstance(ck, Checkpoint):
+            raise DsmpError(INVALID_ARG, "a Checkpoint is needed")
+        return CCheckpoint(self._flat(ck.q, "q", (n, channels), torch.int8),
+                           self._flat(ck.scale, "scale", (n, (channels + 63) // 64)))
+
+    def _segments(self, n, segments):
+        if segments is None:
+            return CSegments(n, 1, None)
+        if isinstance(segments, torch.Tensor):
+            return CSegments(n, segments.numel() - 1, self._flat(segments, "segments", (segments.numel(),), torch.int32))
+        return CSegments(n, int(segments), None)
+
+    def _norm_params(self, C, gamma, beta):
+        return (None if gamma is None else self._flat(gamma, "gamma", (C,)),
+                None if beta is None else self._flat(beta, "beta", (C,)))
+
+    def _norm_ws(self, desc, seg, backward):
+        """Binds the current stream; the scratch buffer that its calls share."""
+        f, b = ctypes.c_size_t(), ctypes.c_size_t()
+        self._check(self.lib.dsmp_group_norm_workspace(ctypes.byref(desc), ctypes.byref(seg), ctypes.byref(f),
+                                                       ctypes.byref(b)), None)
+        s = torch.cuda.current_stream(self.device).cuda_stream
+        self._check(self.lib.dsmp_set_stream(self.h, s), self.h)
+        return self.workspace(("norm", s), b.value if backward else f.value)
+
+    def dsmp_checkpoint_store(self, x: torch.Tensor, out: Optional[Checkpoint] = None) -> Checkpoint:
+        """Keep the rows of x (float32 or bfloat16 [n, channels]) in 8 bits."""
+        if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.dtype not in _CODE:
+            raise DsmpError(INVALID_ARG, "x: a float32 or bfloat16 matrix is needed")
+        n, C = x.shape
+        p, ld = self._rows(x, "x", n, C, x.dtype)
+        out = Checkpoint.empty(n, C, self.device) if out is None else out
+        ck = self._checkpoint(out, n, C)
+        self._bind()
+        self._check(self.lib.dsmp_checkpoint_store(self.h, p, _CODE[x.dtype], ld, n, C, ctypes.byref(ck)), self.h)
+        return out
+
+    def dsmp_checkpoint_load(self, ck: Checkpoint, y: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The kept values (float32, or y's type)."""
+        n, C = ck.q.shape
+        if y is None:
+            y = torch.empty(n, C, dtype=torch.float32, device=self.device)
+        if y.dtype not in _CODE:
+            raise DsmpError(INVALID_ARG, "y: a float32 or bfloat16 matrix is needed")
+        p, ld = self._rows(y, "y", n, C, y.dtype)
+        cck = self._checkpoint(ck, n, C)
+        self._bind()
+        self._check(self.lib.dsmp_checkpoint_load(self.h, ctypes.byref(cck), n, C, p, _CODE[y.dtype], ld), self.h)
+        return y
+
+    def dsmp_group_norm_forward(self, desc: NormDesc, x, gamma, beta, segments=None, addend=None, sum_out=None, y=None,
+                                stats=None, checkpoint: Optional[Checkpoint] = None):
+        """y = act(norm(t) gamma + beta) with t = x (+ addend); returns (y, stats).
+
+        segments: None (all rows), the number of equal segments (x.shape[0]:
+        each row its own), or an int32 tensor of the n_seg + 1 segment bounds.
+        sum_out receives t (needed with an addend; x or addend itself may be
+        given); checkpoint, if given, receives t in 8 bits."""
+        C, n = desc.channels, x.shape[0]
+        seg = self._segments(n, segments)
+        xt, yt = _TORCH.get(desc.x_dtype), _TORCH.get(desc.y_dtype)
+        xp, ldx = self._rows(x, "x", n, C, xt)
+        ap, lda = (None, 0) if addend is None else self._rows(addend, "addend", n, C, xt)
+        sp, lds = (None, 0) if sum_out is None else self._rows(sum_out, "sum_out", n, C, xt)
+        gp, bp = self._norm_params(C, gamma, beta)
+        y = torch.empty(n, C, dtype=yt, device=self.device) if y is None else y
+        yp, ldy = self._rows(y, "y", n, C, yt)
+        shape = (seg.n_seg, desc.groups, 2)
+        stats = torch.empty(shape, dtype=torch.float32, device=self.device) if stats is None else stats
+        stp = self._flat(stats, "stats", shape)
+        ck = None if checkpoint is None else self._checkpoint(checkpoint, n, C)
+        ws = self._norm_ws(desc, seg, False)
+        self._check(self.lib.dsmp_group_norm_forward(self.h, ctypes.byref(desc), ctypes.byref(seg), xp, ldx, ap, lda, sp,
+                                                     lds, gp, bp, yp, ldy, stp, None if ck is None else ctypes.byref(ck),
+                                                     ws.data_ptr(), ws.numel()), self.h)
+        return y, stats
+
+    def dsmp_group_norm_restore(self, desc: NormDesc, checkpoint: Checkpoint, stats, gamma, beta, segments=None, y=None):
+        """The forward's y again, from the checkpoint of t and the kept statistics."""
+        C, n = desc.channels, checkpoint.q.shape[0]
+        seg = self._segments(n, segments)
+        yt = _TORCH.get(desc.y_dtype)
+        ck = self._checkpoint(checkpoint, n, C)
+        stp = self._flat(stats, "stats", (seg.n_seg, desc.groups, 2))
+        gp, bp = self._norm_params(C, gamma, beta)
+        y = torch.empty(n, C, dtype=yt, device=self.device) if y is None else y
+        yp, ldy = self._rows(y, "y", n, C, yt)
+        self._bind()
+        self._check(self.lib.dsmp_group_norm_restore(self.h, ctypes.byref(desc), ctypes.byref(seg), ctypes.byref(ck), stp,
+                                                     gp, bp, yp, ldy), self.h)
+        return y
+
+    def dsmp_group_norm_backward(self, desc: NormDesc, source, stats, gamma, beta, grad_y, segments=None,
+                                 grad_addend=None, grad_x=None, grads: Optional[dict] = None, flags: int = 0):
+        """Gradients of the forward that left stats, from t itself or its
+        Checkpoint (source); returns (grad_x, {"dgamma", "dbeta"}).  grad_addend
+        (which may be grad_x itself) is added to grad_x."""
+        kept = isinstance(source, Checkpoint)
+        C, n = desc.channels, (source.q if kept else source).shape[0]
+        seg = self._segments(n, segments)
+        xp, ldx = (None, 0) if kept else self._rows(source, "x", n, C, _TORCH.get(desc.x_dtype))
+        ck = self._checkpoint(source, n, C) if kept else None
+        stp = self._flat(stats, "stats", (seg.n_seg, desc.groups, 2))
+        gp, bp = self._norm_params(C, gamma, beta)
+        dyp, ldgy = self._rows(grad_y, "grad_y", n, C, torch.float32)
+        gap, ldga = (None, 0) if grad_addend is None else self._rows(grad_addend, "grad_addend", n, C, torch.float32)
+        f32 = dict(dtype=torch.float32, device=self.device)
+        grad_x = torch.empty(n, C, **f32) if grad_x is None else grad_x
+        dxp, ldgx = self._rows(grad_x, "grad_x", n, C, torch.float32)
+        if gamma is None:
+            grads, dg, db = {}, None, None
+        else:
+            grads = {"dgamma": torch.empty(C, **f32), "dbeta": torch.empty(C, **f32)} if grads is None else grads
+            dg, db = self._flat(grads["dgamma"], "dgamma", (C,)), self._flat(grads["dbeta"], "dbeta", (C,))
+        ws = self._norm_ws(desc, seg, True)
+        self._check(self.lib.dsmp_group_norm_backward(self.h, ctypes.byref(desc), ctypes.byref(seg), xp, ldx,
+                                                      None if ck is None else ctypes.byref(ck), stp, gp, bp, dyp, ldgy,
+                                                      gap, ldga, dxp, ldgx, dg, db, flags, ws.data_ptr(), ws.numel()),
+                    self.h)
+        return grad_x, grads

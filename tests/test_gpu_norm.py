@@ -1,0 +1,571 @@
+"""GPU parity of the group norm (forward, restored, backward) and of the 8-bit
+checkpoints against the float64 oracle.
+
+Checkpoints are compared bit for bit.  Floating outputs are held element by
+element to bounds that follow from the operations, with u = 2^-24:
+  xn   16 u (max|t| rstd + |xn|): the joined means and squares, a difference, a product
+  z    |gamma| that, + 4 u (|z| + |beta|)
+  y    1.13 (the largest slope of any activation) times that, + 8 u (1 + |z|) + 3e-7 |z|
+       for the exponentials and the published polynomial of the normal tail
+  w    |dy| (0.8 (the largest second derivative) the bound of z + 1e-6)
+  A, B the mean of the bounds of their terms, + 32 u times the mean magnitude
+  outputs in bfloat16 add 2^-8 |value| (half a unit in the last place), with 1 % to spare
+"""
+
+import numpy as np
+import pytest
+
+from oracle import norm as on
+from tests.helpers import announce, gpu_lib
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+BF = 2.0 ** -8 * 1.01
+
+
+@pytest.fixture(scope="module")
+def env():
+    return gpu_lib()
+
+
+def _np(t):
+    return t.detach().float().cpu().numpy()
+
+
+def bits(t):
+    """Bytes of a tensor's values (NaN included in comparisons)."""
+    import torch
+    return t.contiguous().view(torch.uint8).cpu()
+
+
+class Case:
+    """Inputs on the GPU and as float64, with a slope's kink kept away from."""
+
+    def __init__(self, torch, n, C, G, segments=None, x="f32", y="f32", act=on.SILU, eps=1e-5, seed=0, offset=1.0,
+                 affine=True, addend=False):
+        g = np.random.default_rng(seed + 7 * n + C)
+        self.torch, self.n, self.C, self.G, self.act, self.eps = torch, n, C, G, act, eps
+        self.dt = {"f32": torch.float32, "bf16": torch.bfloat16}
+        self.x_name, self.y_name = x, y
+        self.segments = segments
+        xv = g.normal(size=(n, C)) * np.exp(0.3 * g.normal(size=C)) + offset * g.normal(size=C)
+        self.x = torch.tensor(xv, dtype=torch.float32, device="cuda").to(self.dt[x])
+        self.addend = None
+        t = self.x
+        if addend:
+            self.addend = torch.tensor(g.normal(size=(n, C)), dtype=torch.float32, device="cuda").to(self.dt[x])
+            t = (self.x.float() + self.addend.float()).to(self.dt[x])
+        self.t = t
+        f = lambda v: torch.tensor(v, dtype=torch.float32, device="cuda")  # noqa: E731
+        self.gamma = f(1 + 0.3 * g.normal(size=C)) if affine else None
+        self.beta = f(0.3 * g.normal(size=C)) if affine else None
+        self.ga64 = _np(self.gamma).astype(np.float64) if affine else np.ones(C)
+        self.be64 = _np(self.beta).astype(np.float64) if affine else np.zeros(C)
+        self.t64 = _np(t).astype(np.float64)
+        self.dy = f(g.normal(size=(n, C)))
+        self.grad_addend = f(g.normal(size=(n, C)))
+
+    def desc(self, dm):
+        code = {"f32": dm.F32, "bf16": dm.BF16}
+        return dm.norm_desc(self.C, self.G, code[self.x_name], code[self.y_name], self.act, self.eps)
+
+    def seg(self):
+        return (self.torch.tensor(self.segments, dtype=self.torch.int32, device="cuda")
+                if isinstance(self.segments, list) else self.segments)
+
+    def away_from_kink(self, z):
+        """ReLU's slope has a jump at zero: no gradient enters within 1e-3 of it."""
+        if self.act == on.RELU:
+            self.dy[self.torch.tensor(np.abs(z) < 1e-3, device="cuda")] = 0.0
+
+    def bounds(self, t64, stats):
+        """(xn, z, and their error bounds) of rows t64."""
+        xn = on.normalised(t64, stats, self.segments)
+        z = xn * self.ga64 + self.be64
+        b = on.bounds(self.n, self.segments)
+        row = np.repeat(np.arange(len(b) - 1), np.diff(b))
+        rstd = np.repeat(stats[row, :, 1], self.C // self.G, 1)
+        big = np.abs(t64).max() if t64.size else 0.0
+        exn = 16 * U * (big * rstd + np.abs(xn))
+        ez = np.abs(self.ga64) * exn + 4 * U * (np.abs(z) + np.abs(self.be64))
+        return xn, z, exn, ez, rstd, row
+
+    def check_y(self, y, t64, stats, what="y"):
+        xn, z, exn, ez, _, _ = self.bounds(t64, stats)
+        ref = on.act(z, self.act)
+        tol = 1.13 * ez + 8 * U * (1 + np.abs(z)) + 3e-7 * np.abs(z)
+        tol = tol + (BF * (np.abs(ref) + tol) if self.y_name == "bf16" else U * np.abs(ref))
+        err = np.abs(_np(y).astype(np.float64) - ref)
+        assert (err <= tol).all(), (what, float((err / tol).max()))
+
+    def check_stats(self, got, t64):
+        ref = on.statistics(t64, self.segments, self.G, self.eps)
+        got = _np(got).astype(np.float64)
+        big = np.abs(t64).max() if t64.size else 0.0
+        assert (np.abs(got[:, :, 0] - ref[:, :, 0]) <= 16 * U * big).all()
+        # the squares lose what the means do: twice 16 u max|t| sigma
+        assert (np.abs(got[:, :, 1] - ref[:, :, 1]) <= ref[:, :, 1] * (32 * U + 32 * U * big * ref[:, :, 1])).all()
+        return ref
+
+    def check_backward(self, dx, grads, t64, stats, grad_addend=None, times=1):
+        xn, z, exn, ez, rstd, row = self.bounds(t64, stats)
+        dy = _np(self.dy).astype(np.float64)
+        ref, dgamma, dbeta = on.backward(t64, stats, self.segments, self.ga64, self.be64, self.act, dy)
+        w = dy * on.act_slope(z, self.act)
+        ew = np.abs(dy) * (0.8 * ez + 1e-6) + 4 * U * np.abs(w)
+        ga = np.abs(self.ga64)
+        c, nseg = self.C // self.G, len(stats)
+
+        def group_mean(v):
+            s = np.zeros((nseg, self.G))
+            np.add.at(s, row, v.reshape(self.n, self.G, c).sum(2))
+            m = np.bincount(row, minlength=nseg)[:, None] * c
+            return np.repeat((s / np.maximum(m, 1))[row], c, 1)
+
+        A, B = group_mean(w * self.ga64), group_mean(w * self.ga64 * xn)
+        eA = group_mean(ga * ew) + 32 * U * group_mean(ga * np.abs(w))
+        eB = group_mean(ga * (ew * np.abs(xn) + np.abs(w) * exn)) + 32 * U * group_mean(ga * np.abs(w * xn))
+        tol = rstd * (ga * ew + eA + np.abs(xn) * eB + exn * np.abs(B)
+                      + 8 * U * (ga * np.abs(w) + np.abs(A) + np.abs(xn * B)))
+        tol = tol + 16 * U * np.abs(ref)
+        if grad_addend is not None:
+            ref = ref + _np(grad_addend).astype(np.float64)
+            tol = tol + 2 * U * np.abs(ref)
+        err = np.abs(_np(dx).astype(np.float64) - ref)
+        assert (err <= tol + 1e-30).all(), ("dx", float((err / (tol + 1e-30)).max()))
+        if self.gamma is not None:
+            tg = (ew * np.abs(xn) + np.abs(w) * exn).sum(0) + 32 * U * np.abs(w * xn).sum(0)
+            tb = ew.sum(0) + 32 * U * np.abs(w).sum(0)
+            assert (np.abs(_np(grads["dgamma"]) - times * dgamma) <= times * tg + 1e-30).all(), "dgamma"
+            assert (np.abs(_np(grads["dbeta"]) - times * dbeta) <= times * tb + 1e-30).all(), "dbeta"
+
+
+RAGGED = [0, 0, 1, 1, 71, 400, 400, 699, 700, 700]
+SHAPES = [
+    # n, C, G, segments
+    (1, 32, 4, None), (1, 8, 1, [0, 1]), (2, 16, 2, None), (1000, 32, 8, None), (777, 33, 3, None), (2049, 96, 12, None),
+    (500, 64, 64, None), (300, 512, 2, None), (130, 257, 1, None), (3, 1, 1, None), (640, 7, 7, None),
+    (700, 64, 8, RAGGED), (700, 20, 2, RAGGED), (700, 128, 1, RAGGED), (60, 48, 6, [0, 60, 60, 60]),
+    (1000, 64, 16, 8), (4, 200, 25, 2), (9000, 64, 4, None),
+    # each row a segment
+    (513, 64, 1, 513), (100, 96, 1, 100), (100, 96, 12, 100), (77, 40, 4, 77), (50, 24, 8, 50), (33, 5, 1, 33),
+    (1, 3, 1, 1), (65, 512, 2, 65), (1000, 128, 16, 1000), (40, 320, 5, 40), (30, 257, 1, 30), (20, 100, 4, 20),
+]
+
+
+@pytest.mark.parametrize("n,C,G,segments", SHAPES)
+def test_forward_restore_backward(env, n, C, G, segments):
+    dm, lib, torch = env
+    kinds = [on.SILU, on.GELU, on.RELU, on.IDENTITY]
+    for i, (x, y) in enumerate([("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")]):
+        announce("norm", n, C, G, segments, x, y, kinds[i])
+        c = Case(torch, n, C, G, segments, x, y, kinds[i], addend=i % 2 == 1, seed=i)
+        d, seg = c.desc(dm), c.seg()
+        total = torch.empty_like(c.x) if c.addend is not None else None
+        ck = dm.Checkpoint.empty(n, C, c.x.device)
+        out, st = lib.dsmp_group_norm_forward(d, c.x, c.gamma, c.beta, segments=seg, addend=c.addend, sum_out=total,
+                                              checkpoint=ck)
+        ref = c.check_stats(st, c.t64)
+        if total is not None:
+            assert torch.equal(total, c.t)
+        c.check_y(out, c.t64, ref)
+        q, scale = on.checkpoint(_np(c.t))
+        assert np.array_equal(ck.q.cpu().numpy(), q) and np.array_equal(ck.scale.cpu().numpy(), scale)
+        # without a checkpoint: the same bits
+        again, st2 = lib.dsmp_group_norm_forward(d, c.x, c.gamma, c.beta, segments=seg, addend=c.addend, sum_out=total)
+        assert torch.equal(again, out) and torch.equal(st, st2)
+        kept = on.values(q, scale).astype(np.float64)
+        st64 = _np(st).astype(np.float64)      # the calls below take the statistics as they are
+        c.check_y(lib.dsmp_group_norm_restore(d, ck, st, c.gamma, c.beta, segments=seg), kept, st64, "restored")
+        for source, t64, ga in ((c.t, c.t64, None), (ck, kept, c.grad_addend)):
+            c.away_from_kink(c.bounds(t64, st64)[1])
+            dx, grads = lib.dsmp_group_norm_backward(d, source, st, c.gamma, c.beta, c.dy, segments=seg, grad_addend=ga)
+            c.check_backward(dx, grads, t64, st64, ga)
+
+
+def test_without_affine_parameters(env):
+    dm, lib, torch = env
+    for segments in (None, [0, 100, 300], 300):
+        announce("norm no affine", segments)
+        c = Case(torch, 300, 48, 6, segments, affine=False)
+        d, seg = c.desc(dm), c.seg()
+        y, st = lib.dsmp_group_norm_forward(d, c.x, None, None, segments=seg)
+        c.check_y(y, c.t64, c.check_stats(st, c.t64))
+        dx, grads = lib.dsmp_group_norm_backward(d, c.x, st, None, None, c.dy, segments=seg)
+        assert grads == {}
+        c.check_backward(dx, None, c.t64, _np(st).astype(np.float64))
+
+
+@pytest.mark.parametrize("offset", [1e3, 1e5])
+def test_large_mean_keeps_its_digits(env, offset):
+    """The variance of values far from zero: squares about the mean, not about zero."""
+    dm, lib, torch = env
+    announce("norm offset", offset)
+    for segments in (None, 5000):
+        c = Case(torch, 5000, 32, 2, segments)
+        c.x = c.x + offset
+        c.t64 = _np(c.x).astype(np.float64)
+        _, st = lib.dsmp_group_norm_forward(c.desc(dm), c.x, c.gamma, c.beta, segments=c.seg())
+        c.check_stats(st, c.t64)
+
+
+def test_far_out_value_does_not_disturb_the_variance_of_the_rest(env):
+    """A value of 1e6 in one group: the other groups keep theirs, its own keeps float32 accuracy."""
+    dm, lib, torch = env
+    announce("norm outlier")
+    c = Case(torch, 4096, 64, 8, None)
+    c.x[0, 3] = 1e6
+    t64 = _np(c.x).astype(np.float64)
+    _, st = lib.dsmp_group_norm_forward(c.desc(dm), c.x, c.gamma, c.beta)
+    ref = on.statistics(t64, None, 8, c.eps)
+    got = _np(st).astype(np.float64)
+    np.testing.assert_allclose(got[0, :, 1], ref[0, :, 1], rtol=64 * U)
+    np.testing.assert_allclose(got[0, 1:, 0], ref[0, 1:, 0], atol=64 * U * 10)
+
+
+@pytest.mark.parametrize("segments", [None, [0, 150, 400], 400])
+@pytest.mark.parametrize("C,G", [(64, 8), (33, 3)])
+def test_strided_and_unaligned_rows(env, segments, C, G):
+    """Column slices of wider matrices at odd places: the same values, and nothing written beside them."""
+    dm, lib, torch = env
+    n = 400
+    for x, y in (("f32", "bf16"), ("bf16", "f32")):
+        announce("norm strided", segments, C, x, y)
+        c = Case(torch, n, C, G, segments, x, y, addend=True)
+        d, seg = c.desc(dm), c.seg()
+
+        def wide(v, at, extra, dtype):
+            m = torch.full((n, C + extra), 77.0, dtype=dtype, device="cuda")
+            s = m[:, at:at + C]
+            if v is not None:
+                s.copy_(v)
+            return m, s
+
+        def beside(m, at):
+            assert (m[:, :at] == 77).all() and (m[:, at + C:] == 77).all()
+
+        _, xs = wide(c.x, 3, 8, c.x.dtype)
+        _, ads = wide(c.addend, 1, 2, c.x.dtype)
+        sm, ss = wide(None, 5, 9, c.x.dtype)
+        ym, ys = wide(None, 1, 5, c.dt[y])
+        ck, ck2 = dm.Checkpoint.empty(n, C, "cuda"), dm.Checkpoint.empty(n, C, "cuda")
+        want, st0 = lib.dsmp_group_norm_forward(d, c.x, c.gamma, c.beta, segments=seg, addend=c.addend,
+                                                sum_out=torch.empty_like(c.x), checkpoint=ck2)
+        _, st = lib.dsmp_group_norm_forward(d, xs, c.gamma, c.beta, segments=seg, addend=ads, sum_out=ss, y=ys,
+                                            checkpoint=ck)
+        beside(sm, 5)
+        beside(ym, 1)
+        assert torch.equal(ss, c.t) and torch.equal(ck.q, ck2.q) and torch.equal(ck.scale, ck2.scale)
+        c.check_y(ys, c.t64, c.check_stats(st, c.t64))
+        rm, rs = wide(None, 2, 6, c.dt[y])
+        lib.dsmp_group_norm_restore(d, ck, st, c.gamma, c.beta, segments=seg, y=rs)
+        beside(rm, 2)
+        c.check_y(rs, on.values(ck.q.cpu().numpy(), ck.scale.cpu().numpy()).astype(np.float64),
+                  _np(st).astype(np.float64), "restored")
+        _, dys = wide(c.dy, 3, 4, torch.float32)
+        _, gas = wide(c.grad_addend, 1, 1, torch.float32)
+        dm_, dxs = wide(None, 2, 3, torch.float32)
+        _, grads = lib.dsmp_group_norm_backward(d, ss, st, c.gamma, c.beta, dys, segments=seg, grad_addend=gas,
+                                                grad_x=dxs)
+        beside(dm_, 2)
+        c.check_backward(dxs, grads, c.t64, _np(st).astype(np.float64), c.grad_addend)
+        lm, ls = wide(None, 1, 2, torch.float32)
+        lib.dsmp_checkpoint_load(lib.dsmp_checkpoint_store(xs), ls)
+        beside(lm, 1)
+        assert np.array_equal(_np(ls), on.values(*on.checkpoint(_np(c.x))))
+
+
+def test_sum_and_gradient_in_place(env):
+    dm, lib, torch = env
+    for segments in (None, [0, 10, 500], 500):
+        for target in ("x", "addend"):
+            announce("norm in place", segments, target)
+            c = Case(torch, 500, 64, 8, segments, "bf16", "bf16", addend=True)
+            d, seg = c.desc(dm), c.seg()
+            x, ad = c.x.clone(), c.addend.clone()
+            s = x if target == "x" else ad
+            y, st = lib.dsmp_group_norm_forward(d, x, c.gamma, c.beta, segments=seg, addend=ad, sum_out=s)
+            assert torch.equal(s, c.t)
+            c.check_y(y, c.t64, c.check_stats(st, c.t64))
+            g = c.grad_addend.clone()
+            _, grads = lib.dsmp_group_norm_backward(d, s, st, c.gamma, c.beta, c.dy, segments=seg, grad_addend=g,
+                                                    grad_x=g)
+            c.check_backward(g, grads, c.t64, _np(st).astype(np.float64), c.grad_addend)
+
+
+@pytest.mark.parametrize("n,C", [(1, 1), (3, 5), (100, 64), (257, 65), (64, 96), (33, 250), (9, 512), (1000, 8)])
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+def test_checkpoint_store_and_load(env, n, C, x):
+    dm, lib, torch = env
+    announce("checkpoint", n, C, x)
+    g = np.random.default_rng(n + C)
+    v = g.normal(size=(n, C)) * np.exp(4 * g.normal(size=(n, 1)))
+    t = torch.tensor(v, dtype=torch.float32, device="cuda").to({"f32": torch.float32, "bf16": torch.bfloat16}[x])
+    if n > 8 and C >= 5:
+        t[0] = 0.0
+        t[1, C - 1] = float("inf")
+        t[2, 0] = float("nan")
+        t[3] = t[3] * 1e-38
+        t[4, 0], t[4, 1:5] = 127.0, torch.tensor([0.5, 1.5, -2.5, 126.5], dtype=t.dtype, device="cuda")   # ties
+        t[5] = -t[5].abs()
+        t[6, 0] = float("-inf")
+        t[7] = 3.0e38
+    ck = lib.dsmp_checkpoint_store(t)
+    q, scale = on.checkpoint(_np(t))
+    assert np.array_equal(ck.q.cpu().numpy(), q)
+    assert np.array_equal(ck.scale.cpu().numpy(), scale, equal_nan=True)
+    want = on.values(q, scale)
+    assert np.array_equal(_np(lib.dsmp_checkpoint_load(ck)), want, equal_nan=True)
+    low = lib.dsmp_checkpoint_load(ck, torch.empty(n, C, dtype=torch.bfloat16, device="cuda"))
+    assert np.array_equal(_np(low), _np(torch.tensor(want).to(torch.bfloat16)), equal_nan=True)
+
+
+def test_infinities_and_nan_stay_in_their_segment_and_group(env):
+    dm, lib, torch = env
+    n, C, G = 600, 64, 4
+    for segments in ([0, 200, 200, 450, 600], 600):
+        for bad in (float("nan"), float("inf")):
+            announce("norm non-finite", segments, bad)
+            c = Case(torch, n, C, G, segments)
+            clean, st0 = lib.dsmp_group_norm_forward(c.desc(dm), c.x, c.gamma, c.beta, segments=c.seg())
+            x = c.x.clone()
+            x[300, 20] = bad                       # second non-empty segment, group 1
+            ck = dm.Checkpoint.empty(n, C, "cuda")
+            y, st = lib.dsmp_group_norm_forward(c.desc(dm), x, c.gamma, c.beta, segments=c.seg(), checkpoint=ck)
+            hit = torch.zeros(n, C, dtype=torch.bool, device="cuda")
+            rows = slice(200, 450) if isinstance(segments, list) else slice(300, 301)
+            hit[rows, 16:32] = True
+            assert torch.equal(y[~hit], clean[~hit])
+            assert torch.isnan(y[300, 20]) and not torch.isfinite(y[hit]).all()
+            dx, grads = lib.dsmp_group_norm_backward(c.desc(dm), ck, st, c.gamma, c.beta, c.dy, segments=c.seg())
+            block = hit.clone()
+            block[300, :] = True                   # the row's checkpoint block is one scale
+            rows_ok = ~block
+            if isinstance(segments, list):         # its sums reach every group of the segment
+                rows_ok[200:450] = False
+            assert torch.isfinite(dx[rows_ok]).all() and torch.isnan(dx[300]).all()
+
+
+def test_no_rows_and_empty_segments(env):
+    dm, lib, torch = env
+    announce("norm no rows")
+    C, G = 32, 4
+    d = dm.norm_desc(C, G, dm.F32, dm.F32, dm.ACT_SILU)
+    x, dy = torch.empty(0, C, device="cuda"), torch.empty(0, C, device="cuda")
+    gamma, beta = torch.ones(C, device="cuda"), torch.zeros(C, device="cuda")
+    for seg, k in ((None, 1), (torch.zeros(4, dtype=torch.int32, device="cuda"), 3), (5, 5)):
+        st = torch.full((k, G, 2), 9.0, device="cuda")
+        ck = dm.Checkpoint.empty(0, C, "cuda")
+        y, _ = lib.dsmp_group_norm_forward(d, x, gamma, beta, segments=seg, stats=st, checkpoint=ck)
+        assert y.shape == (0, C) and (st == 0).all()
+        lib.dsmp_group_norm_restore(d, ck, st, gamma, beta, segments=seg)
+        grads = {"dgamma": torch.full((C,), 2.0, device="cuda"), "dbeta": torch.full((C,), 3.0, device="cuda")}
+        lib.dsmp_group_norm_backward(d, ck, st, gamma, beta, dy, segments=seg, grads=grads, flags=dm.GRAD_ACCUMULATE)
+        assert (grads["dgamma"] == 2).all() and (grads["dbeta"] == 3).all()
+        lib.dsmp_group_norm_backward(d, x, st, gamma, beta, dy, segments=seg, grads=grads)
+        assert (grads["dgamma"] == 0).all() and (grads["dbeta"] == 0).all()
+    assert lib.dsmp_checkpoint_load(lib.dsmp_checkpoint_store(x)).shape == (0, C)
+
+
+def test_gradients_accumulate(env):
+    dm, lib, torch = env
+    for segments in (None, 300):
+        announce("norm accumulate", segments)
+        c = Case(torch, 300, 40, 5, segments)
+        d = c.desc(dm)
+        _, st = lib.dsmp_group_norm_forward(d, c.x, c.gamma, c.beta, segments=segments)
+        dx, grads = lib.dsmp_group_norm_backward(d, c.x, st, c.gamma, c.beta, c.dy, segments=segments)
+        lib.dsmp_group_norm_backward(d, c.x, st, c.gamma, c.beta, c.dy, segments=segments, grads=grads,
+                                     flags=dm.GRAD_ACCUMULATE)
+        c.check_backward(dx, grads, c.t64, _np(st).astype(np.float64), times=2)
+
+
+def test_same_bits_on_every_run_and_on_another_stream(env):
+    dm, lib, torch = env
+    for segments in (None, [0, 5000, 5001, 30000], 30000):
+        announce("norm determinism", segments)
+        c = Case(torch, 30000, 64, 8, segments, "bf16", "bf16", on.GELU, addend=True)
+        d, seg = c.desc(dm), c.seg()
+
+        def go():
+            ck = dm.Checkpoint.empty(c.n, c.C, "cuda")
+            y, st = lib.dsmp_group_norm_forward(d, c.x, c.gamma, c.beta, segments=seg, addend=c.addend,
+                                                sum_out=torch.empty_like(c.x), checkpoint=ck)
+            u = lib.dsmp_group_norm_restore(d, ck, st, c.gamma, c.beta, segments=seg)
+            dx, gr = lib.dsmp_group_norm_backward(d, ck, st, c.gamma, c.beta, c.dy, segments=seg,
+                                                  grad_addend=c.grad_addend)
+            return [y, st, ck.q, ck.scale, u, dx, gr["dgamma"], gr["dbeta"]]
+
+        first = go()
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            other = go()
+        second = go()
+        torch.cuda.synchronize()
+        for a, b, e in zip(first, second, other):
+            assert torch.equal(bits(a), bits(b)) and torch.equal(bits(a), bits(e))
+
+
+def test_replayed_from_a_graph(env):
+    """A captured forward, restore and backward, replayed with new inputs and eager work between the replays."""
+    dm, lib, torch = env
+    for segments in (None, [0, 700, 2000], 2000):
+        announce("norm graph", segments)
+        c = Case(torch, 2000, 64, 8, segments, "f32", "bf16", addend=True)
+        d, seg = c.desc(dm), c.seg()
+        ck = dm.Checkpoint.empty(c.n, c.C, "cuda")
+        b = {"sum": torch.empty_like(c.x), "y": torch.empty(c.n, c.C, dtype=torch.bfloat16, device="cuda"),
+             "u": torch.empty(c.n, c.C, dtype=torch.bfloat16, device="cuda"), "dx": torch.empty(c.n, c.C, device="cuda"),
+             "st": torch.empty(len(on.bounds(c.n, segments)) - 1, c.G, 2, device="cuda"),
+             "dgamma": torch.empty(c.C, device="cuda"), "dbeta": torch.empty(c.C, device="cuda")}
+
+        def go():
+            lib.dsmp_group_norm_forward(d, c.x, c.gamma, c.beta, segments=seg, addend=c.addend, sum_out=b["sum"],
+                                        y=b["y"], stats=b["st"], checkpoint=ck)
+            lib.dsmp_group_norm_restore(d, ck, b["st"], c.gamma, c.beta, segments=seg, y=b["u"])
+            lib.dsmp_group_norm_backward(d, ck, b["st"], c.gamma, c.beta, c.dy, segments=seg, grad_x=b["dx"],
+                                         grads={"dgamma": b["dgamma"], "dbeta": b["dbeta"]})
+
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            go()                                     # its scratch buffer exists before the capture
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            go()
+        for k in range(4):
+            c.x.copy_(torch.randn_like(c.x) + k)
+            c.dy.copy_(torch.randn_like(c.dy))
+            graph.replay()
+            torch.cuda.synchronize()
+            got = {n: v.clone() for n, v in b.items()}
+            go()
+            torch.cuda.synchronize()
+            for n, v in b.items():
+                assert torch.equal(bits(got[n]), bits(v)), (k, n)
+
+
+def test_wrong_segment_bounds_write_nothing_outside(env):
+    """Bounds that do not ascend, or leave the rows: limited on the device; the arrays' neighbours stay."""
+    dm, lib, torch = env
+    n, C, G = 500, 64, 8
+    for segments in ([0, 400, 100, 500], [-7, 100, 9000, 20, 500], [500, 500, 0, 0], [0, 3, 2 ** 31 - 1, -2 ** 31, 4]):
+        announce("norm wrong bounds", segments)
+        c = Case(torch, n, C, G)
+        seg = torch.tensor(segments, dtype=torch.int32, device="cuda")
+        k = len(segments) - 1
+        pad = 64
+        y, dx = (torch.full((n + 2 * pad, C), 7.0, device="cuda") for _ in range(2))
+        st = torch.full((k + 2, G, 2), 7.0, device="cuda")
+        lib.dsmp_group_norm_forward(c.desc(dm), c.x, c.gamma, c.beta, segments=seg, y=y[pad:-pad], stats=st[1:-1])
+        lib.dsmp_group_norm_backward(c.desc(dm), c.x, st[1:-1], c.gamma, c.beta, c.dy, segments=seg, grad_x=dx[pad:-pad])
+        for t in (y[:pad], y[-pad:], dx[:pad], dx[-pad:], st[:1], st[-1:]):
+            assert (t == 7).all()
+
+
+def test_offsets_past_32_bits(env):
+    """9.1 million rows of 256 channels: 2.3e9 values; the last segment against the oracle."""
+    dm, lib, torch = env
+    n, C, G, m = 9_100_000, 256, 32, 1000
+    announce("norm large", n, C)
+    if torch.cuda.mem_get_info()[0] < 60e9:
+        pytest.skip("needs 60 GB")
+    x = torch.empty(n, C, dtype=torch.bfloat16, device="cuda").normal_()
+    c = Case(torch, m, C, G, None, "bf16", "bf16")
+    x[n - m:] = c.x
+    dy = torch.ones(n, C, device="cuda")
+    dy[n - m:] = c.dy
+    seg = torch.tensor([0, 5, n - m, n], dtype=torch.int32, device="cuda")
+    ck = dm.Checkpoint.empty(n, C, "cuda")
+    d = c.desc(dm)
+    y, st = lib.dsmp_group_norm_forward(d, x, c.gamma, c.beta, segments=seg, checkpoint=ck)
+    ref = c.check_stats(st[2:], c.t64)
+    c.check_y(y[n - m:], c.t64, ref)
+    q, scale = on.checkpoint(_np(c.x))
+    assert np.array_equal(ck.q[n - m:].cpu().numpy(), q) and np.array_equal(ck.scale[n - m:].cpu().numpy(), scale)
+    lib.dsmp_group_norm_restore(d, ck, st, c.gamma, c.beta, segments=seg, y=y)
+    c.check_y(y[n - m:], on.values(q, scale).astype(np.float64), _np(st[2:]).astype(np.float64), "restored")
+    del y
+    dx, _ = lib.dsmp_group_norm_backward(d, x, st, c.gamma, c.beta, dy, segments=seg)
+    c.gamma = None       # the parameters' gradients cover all rows: dx alone is compared
+    c.check_backward(dx[n - m:], None, c.t64, _np(st[2:]).astype(np.float64))
+
+
+def test_gradient_against_differences(env):
+    """The library's own forward, stepped along random directions: central
+    differences of sum(dy y) in float64.  With steps of 2^-6 on values of order
+    one the third derivative leaves 1e-4 of the sum, rounding 4 u / 2^-6 of
+    the terms' norm."""
+    dm, lib, torch = env
+    for segments in (None, [0, 50, 200], 200):
+        announce("norm differences", segments)
+        c = Case(torch, 200, 64, 8, segments, act=on.SILU, eps=1e-2)
+        d, seg, h = c.desc(dm), c.seg(), 2.0 ** -6
+        _, st = lib.dsmp_group_norm_forward(d, c.x, c.gamma, c.beta, segments=seg)
+        dx, grads = lib.dsmp_group_norm_backward(d, c.x, st, c.gamma, c.beta, c.dy, segments=seg)
+        g = torch.Generator(device="cuda").manual_seed(3)
+
+        def loss(x, gamma, beta):
+            y, _ = lib.dsmp_group_norm_forward(d, x, gamma, beta, segments=seg)
+            return float((y.double() * c.dy.double()).sum())
+
+        for name, v, got in (("x", c.x, dx), ("gamma", c.gamma, grads["dgamma"]), ("beta", c.beta, grads["dbeta"])):
+            e = torch.randn(v.shape, generator=g, device="cuda")
+            args = {"x": c.x, "gamma": c.gamma, "beta": c.beta}
+            up, dn = loss(**{**args, name: v + h * e}), loss(**{**args, name: v - h * e})
+            want = float((got.double() * e.double()).sum())
+            norm = float(got.double().norm()) * float(e.double().norm()) / e.numel() ** 0.5
+            assert abs((up - dn) / (2 * h) - want) <= 5e-3 * norm, (name, (up - dn) / (2 * h), want)
+
+
+def test_refusals(env):
+    dm, lib, torch = env
+    announce("norm refusals")
+    n, C, G = 10, 32, 4
+    x, f = torch.zeros(n, C, device="cuda"), torch.ones(C, device="cuda")
+    ok = dm.norm_desc(C, G, dm.F32, dm.F32, dm.ACT_SILU)
+    _, st = lib.dsmp_group_norm_forward(ok, x, f, f)
+    ck = lib.dsmp_checkpoint_store(x)
+
+    def refused(status, fn, *args, **kw):
+        with pytest.raises(dm.DsmpError) as e:
+            fn(*args, **kw)
+        assert e.value.status == status, str(e.value)
+
+    fwd, bwd, res = lib.dsmp_group_norm_forward, lib.dsmp_group_norm_backward, lib.dsmp_group_norm_restore
+    wide = torch.zeros(n, 513, device="cuda")
+    refused(dm.UNSUPPORTED, fwd, dm.norm_desc(513, 1, dm.F32, dm.F32), wide, None, None)
+    refused(dm.UNSUPPORTED, lib.dsmp_checkpoint_store, wide)
+    for d in (dm.norm_desc(C, 5, dm.F32, dm.F32), dm.norm_desc(C, 0, dm.F32, dm.F32),
+              dm.norm_desc(C, G, dm.F32, dm.F32, 4), dm.norm_desc(C, G, dm.F32, dm.F32, 0, -1.0),
+              dm.norm_desc(C, G, dm.F32, dm.F32, 0, float("nan")), dm.norm_desc(C, G, 2, dm.F32)):
+        refused(dm.INVALID_ARG, fwd, d, x, f, f)
+    refused(dm.INVALID_ARG, fwd, ok, x, f, None)                       # gamma without beta
+    refused(dm.INVALID_ARG, fwd, ok, x, f, f, segments=3)              # 3 does not divide 10
+    refused(dm.INVALID_ARG, fwd, ok, x, f, f, segments=0)
+    refused(dm.INVALID_ARG, fwd, ok, x, f, f, addend=x)                # no place for the sum
+    refused(dm.INVALID_ARG, fwd, ok, x.bfloat16(), f, f)
+    refused(dm.INVALID_ARG, fwd, ok, x.cpu(), f, f)
+    refused(dm.INVALID_ARG, fwd, ok, x.t(), f, f)
+    refused(dm.INVALID_ARG, fwd, ok, torch.zeros(C, n, device="cuda").t(), f, f)
+    refused(dm.INVALID_ARG, fwd, ok, torch.zeros(1, C, device="cuda").expand(n, C), f, f)
+    refused(dm.INVALID_ARG, fwd, ok, x, f[:8], f)
+    refused(dm.INVALID_ARG, fwd, ok, x, f, f, segments=torch.zeros(3, dtype=torch.int64, device="cuda"))
+    refused(dm.INVALID_ARG, fwd, ok, x, f, f, stats=torch.zeros(1, G, 3, device="cuda"))
+    refused(dm.INVALID_ARG, fwd, ok, x, f, f, checkpoint=dm.Checkpoint.empty(n, C + 1, "cuda"))
+    refused(dm.INVALID_ARG, res, ok, dm.Checkpoint(ck.q, ck.scale[:5]), st, f, f)
+    refused(dm.INVALID_ARG, bwd, ok, ck, st, f, f, x.bfloat16())
+    refused(dm.INVALID_ARG, bwd, ok, ck, st[:, :2], f, f, x)
+    refused(dm.INVALID_ARG, bwd, ok, ck, st, f, f, x, flags=dm.GRAD_X_ACCUMULATE)
+    refused(dm.INVALID_ARG, lib.dsmp_checkpoint_store, x.half())
+    refused(dm.INVALID_ARG, lib.dsmp_checkpoint_load, ck, torch.zeros(n, C, dtype=torch.float16, device="cuda"))
+    # the layers take the first two activations alone
+    desc = dm.layer_desc(2, 32, 64, 64, dm.F32, act=dm.ACT_SILU)
+    g = lib.dsmp_radius_graph_build(torch.rand(n, 2, device="cuda"), n, 0.5)
+    with pytest.raises(dm.DsmpError):
+        lib.dsmp_nnconv_workspace(desc, g)
