@@ -35,9 +35,14 @@ constexpr float TINY = 0x1p-100f;
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
+// VEC, in all that follows: rows are whole aligned groups of 8 channels, and no
+// group of the norm ends inside four of them.  Four channels are then a unit with
+// one set of statistics; elsewhere every channel is its own.
+template <bool VEC>
+constexpr int UNIT = VEC ? 4 : 1;
+
 // Rows a lane has in flight in the forward passes, and in the backward ones,
-// which hold twice the values of each (rows that are not whole aligned groups:
-// one and the same, their loads have branches).
+// which hold twice the values of each (fewer where loads have branches).
 template <bool VEC>
 constexpr int FWD_TILE = VEC ? 4 : 2;
 template <bool VEC>
@@ -68,7 +73,7 @@ struct NormArgs {
   float* scale;
   float2* part;                 // sums of the pieces (chunk x segment), [chunk + segment][G]
   float eps;
-  int act, merge;
+  int merge, ck, y_bf16;
   const float* gy;
   int64_t ldgy;
   const float* ga;
@@ -252,15 +257,20 @@ __device__ __forceinline__ void store_q8(int8_t* q, float* scale, int64_t r, int
   if (c0 % BLOCK_C == 0) scale[r * ((C + BLOCK_C - 1) / BLOCK_C) + c0 / BLOCK_C] = s;
 }
 
-// t = x (+ addend, rounded to T and written to sum); its checkpoint.
-template <typename T, bool VEC, bool ADD>
-__device__ __forceinline__ void take_row(const NormArgs& a, int64_t r, int c0, int cnt, float (&v)[8]) {
-  Source<T, VEC>::load(a, r, c0, cnt, v);
-  if (ADD) {
-    float u[8];
-    Row<T, VEC>::load(static_cast<const T*>(a.add) + r * a.lda, c0, cnt, u);
+// t = x, or x + addend rounded to T, of rows i, i + step, ...
+template <typename T, bool VEC, bool ADD, int N>
+__device__ __forceinline__ void take_rows(const NormArgs& a, int64_t i, int step, int c0, int cnt, float (&v)[N][8]) {
+  float u[N][8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = (float)(T)(v[k] + u[k]);
+  for (int t = 0; t < N; ++t) {
+    Source<T, VEC>::load(a, i + t * step, c0, cnt, v[t]);
+    if (ADD) Row<T, VEC>::load(static_cast<const T*>(a.add) + (i + t * step) * a.lda, c0, cnt, u[t]);
+  }
+  if (ADD) {
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[t][k] = (float)(T)(v[t][k] + u[t][k]);
   }
 }
 
@@ -281,42 +291,31 @@ __device__ __forceinline__ float normal_tail(float z, float& e) {
   return 0.5f * p * t * e;
 }
 
-__device__ __forceinline__ void activate8(int act, float (&z)[8]) {
-  if (act == DSMP_ACT_SILU) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) z[k] *= __builtin_amdgcn_rcpf(1.0f + __expf(-z[k]));
-  } else if (act == DSMP_ACT_GELU) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      float e;
-      const float q = normal_tail(z[k], e);
-      z[k] *= z[k] < 0.0f ? q : 1.0f - q;
-    }
-  } else if (act == DSMP_ACT_RELU) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) z[k] = z[k] < 0.0f ? 0.0f : z[k];   // a NaN passes
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+  if (ACT == DSMP_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+  if (ACT == DSMP_ACT_GELU) {
+    float e;
+    const float q = normal_tail(z, e);
+    return z * (z < 0.0f ? q : 1.0f - q);
   }
+  if (ACT == DSMP_ACT_RELU) return z < 0.0f ? 0.0f : z;   // a NaN passes
+  return z;
 }
 
-// w *= act'(z)
-__device__ __forceinline__ void slope8(int act, const float (&z)[8], float (&w)[8]) {
-  if (act == DSMP_ACT_SILU) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float p = __builtin_amdgcn_rcpf(1.0f + __expf(-z[k]));
-      w[k] *= p * __builtin_fmaf(z[k], 1.0f - p, 1.0f);
-    }
-  } else if (act == DSMP_ACT_GELU) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      float e;
-      const float q = normal_tail(z[k], e);
-      w[k] *= __builtin_fmaf(z[k] * 0.39894228f, e, z[k] < 0.0f ? q : 1.0f - q);
-    }
-  } else if (act == DSMP_ACT_RELU) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = z[k] > 0.0f ? w[k] : z[k] <= 0.0f ? 0.0f : z[k];
+template <int ACT>
+__device__ __forceinline__ float slope(float z) {
+  if (ACT == DSMP_ACT_SILU) {
+    const float p = __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+    return p * __builtin_fmaf(z, 1.0f - p, 1.0f);
   }
+  if (ACT == DSMP_ACT_GELU) {
+    float e;
+    const float q = normal_tail(z, e);
+    return __builtin_fmaf(z * 0.39894228f, e, z < 0.0f ? q : 1.0f - q);
+  }
+  if (ACT == DSMP_ACT_RELU) return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;   // a NaN passes
+  return 1.0f;
 }
 
 // ------------------------------------------------------------ segments
@@ -330,18 +329,21 @@ __device__ __forceinline__ int64_t seg_begin(const NormArgs& a, int s) {
 __device__ __forceinline__ int64_t seg_end(const NormArgs& a, int s) {
   return s + 1 >= a.n_seg ? a.n : seg_begin(a, s + 1);
 }
-// The last segment that begins at or before row r.
+// The last segment that begins at or before row r: 64 bounds at a time, one to a
+// lane of each wave (every wave finds the same).
 __device__ __forceinline__ int seg_find(const NormArgs& a, int64_t r) {
-  if (!a.ptr) return a.len > 0 ? (int)std::min<int64_t>(r / a.len, a.n_seg - 1) : 0;
-  int lo = 0, hi = a.n_seg - 1;
-  while (lo < hi) {
-    const int mid = lo + (hi - lo + 1) / 2;
-    if (seg_begin(a, mid) <= r)
-      lo = mid;
-    else
-      hi = mid - 1;
+  if (!a.ptr) return a.len > 0 ? (int)((uint32_t)r / (uint32_t)a.len) : 0;
+  const int lane = threadIdx.x & 63;
+  int lo = 0, count = a.n_seg;   // it is one of lo .. lo + count - 1
+  while (count > 1) {
+    const int step = (count + 63) / 64, i = lo + lane * step;
+    const bool at = lane * step < count && seg_begin(a, i) <= r;
+    // bounds that do not ascend still leave the first lane's true
+    const int k = 63 - __builtin_clzll(__ballot(at) | 1ull);
+    count = std::min(step, count - k * step);
+    lo += k * step;
   }
-  return lo;
+  return __builtin_amdgcn_readfirstlane(lo);
 }
 
 struct Lanes {
@@ -356,8 +358,8 @@ struct Lanes {
   }
 };
 
-// s1, s2: the workgroup's sums per channel (float64 in LDS).  Writes the sums
-// over each group's channels to out(g, sum1, sum2), by one lane each.
+// s1, s2: the workgroup's sums per channel (or unit of channels), float64 in LDS.
+// Gives the sums over each group's gs of them to out(g, sum1, sum2), by one lane each.
 template <typename F>
 __device__ __forceinline__ void group_sums(const double* s1, const double* s2, int G, int gs, F out) {
   int tg = 1;   // lanes of a group
@@ -373,112 +375,180 @@ __device__ __forceinline__ void group_sums(const double* s1, const double* s2, i
   }
 }
 
-// ------------------------------------------------------------ forward, first pass
+// ------------------------------------------------------------ per lane
 
-// Count, mean and sum of squares about the mean of eight channels.  Rows join
-// TILE at a time (mean of the tile, then deviations from it, then the pair rule
-// of Chan, Golub and LeVeque), so a large mean or a far-out row costs no digits.
-struct Moments {
-  float n = 0.0f, mean[8] = {}, m2[8] = {};
+template <bool VEC>
+__device__ __forceinline__ void store_y(const NormArgs& a, int64_t r, const Lanes& L, const float (&v)[8]) {
+  if (a.y_bf16)
+    Row<__bf16, VEC>::store(static_cast<__bf16*>(a.y) + r * a.ldy, L.c0, L.cnt, v);
+  else
+    Row<float, VEC>::store(static_cast<float*>(a.y) + r * a.ldy, L.c0, L.cnt, v);
+}
 
-  template <int N>
-  __device__ __forceinline__ void add(const float (&v)[N][8]) {
-    const float nn = n + N, w = N / nn, f = n * w;
-    n = nn;
+// A value for each of a lane's eight channels that is the same within a unit.
+template <bool VEC>
+struct PerUnit {
+  static constexpr int N = 8 / UNIT<VEC>;
+  float v[N];
+  __device__ __forceinline__ float operator[](int k) const { return v[k / UNIT<VEC>]; }
+};
+
+// The groups of a lane's units.
+template <bool VEC>
+struct Groups {
+  int g[PerUnit<VEC>::N];
+  __device__ __forceinline__ Groups(const NormArgs& a, int c0) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      float s = v[0][k];
-#pragma unroll
-      for (int t = 1; t < N; ++t) s += v[t][k];
-      const float m = s * (1.0f / N);
-      float q = 0.0f;
-#pragma unroll
-      for (int t = 0; t < N; ++t) q = __builtin_fmaf(v[t][k] - m, v[t][k] - m, q);
-      const float d = m - mean[k];
-      mean[k] = __builtin_fmaf(d, w, mean[k]);
-      m2[k] += __builtin_fmaf(d * d, f, q);
-    }
+    for (int j = 0; j < PerUnit<VEC>::N; ++j) g[j] = std::min(c0 + j * UNIT<VEC>, a.C - 1) / a.gs;
   }
-  // joins the lane `o` away
-  __device__ __forceinline__ void join(int o) {
-    const float nb = __shfl_xor(n, o, 64), nn = n + nb, w = nn > 0.0f ? nb / nn : 0.0f, f = n * w;
-    n = nn;
+  // pairs of a segment's groups: (mean, rstd), or the two sums of the backward pass
+  __device__ __forceinline__ void read(const float2* st, PerUnit<VEC>& x, PerUnit<VEC>& y) const {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float mb = __shfl_xor(mean[k], o, 64), qb = __shfl_xor(m2[k], o, 64), d = mb - mean[k];
-      mean[k] = __builtin_fmaf(d, w, mean[k]);
-      m2[k] += __builtin_fmaf(d * d, f, qb);
+    for (int j = 0; j < PerUnit<VEC>::N; ++j) {
+      const float2 t = st[g[j]];
+      x.v[j] = t.x, y.v[j] = t.y;
     }
   }
 };
 
-size_t stats_lds(int lg, int C) { return (size_t)NW * (16 << lg) * 4 + NW * 4 + 8 + 16 * (size_t)C; }
+template <bool VEC>
+__device__ __forceinline__ void params8(const NormArgs& a, const Lanes& L, float (&gamma)[8], float (&beta)[8]) {
+  if (a.gamma) {
+    Row<float, VEC>::load(a.gamma, L.c0, L.cnt, gamma);
+    Row<float, VEC>::load(a.beta, L.c0, L.cnt, beta);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) gamma[k] = 1.0f, beta[k] = 0.0f;
+  }
+}
 
-template <typename T, bool VEC, bool ADD, bool CK>
+__device__ __forceinline__ float2* stats_of(const NormArgs& a, int s) {
+  return reinterpret_cast<float2*>(a.stats) + (int64_t)s * a.G;
+}
+
+// ------------------------------------------------------------ forward, statistics
+
+// Rows, and for each unit the mean and the sum of squares about it.  Rows join
+// a few at a time (mean of the tile, then deviations from it, then the pair rule
+// of Chan, Golub and LeVeque), so a large mean or a far-out row costs no digits.
+template <bool VEC>
+struct Moments {
+  static constexpr int U = UNIT<VEC>, N = 8 / U;
+  float n = 0.0f, mean[N] = {}, m2[N] = {};
+
+  template <int T>
+  __device__ __forceinline__ void add(const float (&v)[T][8]) {
+    const float nn = n + T, w = T / nn, f = n * w * U;
+    n = nn;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      float s = 0.0f, q = 0.0f;
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int k = 0; k < U; ++k) s += v[t][j * U + k];
+      const float m = s * (1.0f / (T * U));
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int k = 0; k < U; ++k) q = __builtin_fmaf(v[t][j * U + k] - m, v[t][j * U + k] - m, q);
+      const float d = m - mean[j];
+      mean[j] = __builtin_fmaf(d, w, mean[j]);
+      m2[j] += __builtin_fmaf(d * d, f, q);
+    }
+  }
+  // joins the lane `o` away
+  __device__ __forceinline__ void join(int o) {
+    const float nb = __shfl_xor(n, o, 64), nn = n + nb, w = nn > 0.0f ? nb / nn : 0.0f, f = n * w * U;
+    n = nn;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float mb = __shfl_xor(mean[j], o, 64), qb = __shfl_xor(m2[j], o, 64), d = mb - mean[j];
+      mean[j] = __builtin_fmaf(d, w, mean[j]);
+      m2[j] += __builtin_fmaf(d * d, f, qb);
+    }
+  }
+};
+
+// Dynamic LDS of the summing passes: two float64 per channel, two floats per
+// wave and channel, a count per wave.
+size_t sums_lds(int lg, int C) { return (size_t)NW * (16 << lg) * 4 + NW * 4 + 16 * (size_t)C; }
+
+// The workgroup's sums over rows [r, e) for every group: the mean-weighted count and
+// the squares about zero in float64, to out(g, u, v).  Adds the addend and
+// writes the sum and the checkpoint on the way.
+template <typename T, bool VEC, bool ADD, typename OUT>
+__device__ __forceinline__ void moments_of(const NormArgs& a, const Lanes& L, int64_t r, int64_t e, double* sh, OUT out) {
+  constexpr int U = UNIT<VEC>, N = 8 / U, TILE = FWD_TILE<VEC>;
+  const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63, wu = L.lpr * N, units = a.C / U;
+  double *s1 = sh, *s2 = sh + units;
+  float *mm = reinterpret_cast<float*>(s2 + units), *qq = mm + NW * wu, *nn = qq + NW * wu;
+  Moments<VEC> m;
+  auto keep = [&](int64_t row, const float(&v)[8]) {
+    if (ADD) Row<T, VEC>::store(static_cast<T*>(a.sum) + row * a.lds, L.c0, L.cnt, v);
+    if (a.ck) store_q8<VEC>(a.q, a.scale, row, a.C, L.c0, L.cnt, std::min(8, L.lpr), v);
+  };
+  int64_t i = r + L.rl;
+  for (; i + (TILE - 1) * L.RL < e; i += TILE * L.RL) {
+    float v[TILE][8];
+    take_rows<T, VEC, ADD, TILE>(a, i, L.RL, L.c0, L.cnt, v);
+#pragma unroll
+    for (int t = 0; t < TILE; ++t) keep(i + t * L.RL, v[t]);
+    m.template add<TILE>(v);
+  }
+  for (; i < e; i += L.RL) {
+    float v[1][8];
+    take_rows<T, VEC, ADD, 1>(a, i, L.RL, L.c0, L.cnt, v);
+    keep(i, v[0]);
+    m.template add<1>(v);
+  }
+  for (int o = L.lpr; o < 64; o <<= 1) m.join(o);
+  if (lane < L.lpr) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) mm[wid * wu + L.lr * N + j] = m.mean[j], qq[wid * wu + L.lr * N + j] = m.m2[j];
+    if (lane == 0) nn[wid] = m.n;
+  }
+  __syncthreads();
+  const int c = threadIdx.x;
+  if (c < units) {
+    double u = 0.0, v = 0.0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const double mw = mm[w * wu + c], nw = (double)(nn[w] * U);
+      u += nw * mw;
+      v += (double)qq[w * wu + c] + nw * mw * mw;
+    }
+    s1[c] = u;
+    s2[c] = v;
+  }
+  __syncthreads();
+  group_sums(s1, s2, a.G, a.gs / U, out);
+}
+
+template <typename T, bool VEC, bool ADD>
 __global__ __launch_bounds__(NT) void k_norm_stats(NormArgs a) {
   extern __shared__ double sh[];
   const Lanes L(a.lg, a.C, NT);
-  const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63, w8 = L.lpr * 8;
-  double *s1 = sh, *s2 = sh + a.C;
-  float *mm = reinterpret_cast<float*>(s2 + a.C), *qq = mm + NW * w8, *nn = qq + NW * w8;
   const int64_t r0 = (int64_t)blockIdx.x * a.R, r1 = std::min<int64_t>(r0 + a.R, a.n);
   int s = seg_find(a, r0);
   for (int64_t r = r0; r < r1; ++s) {
     const int64_t e = std::min<int64_t>(seg_end(a, s), r1);
     if (e <= r) continue;
-    Moments m;
-    constexpr int TILE = FWD_TILE<VEC>;
-    int64_t i = r + L.rl;
-    auto take = [&](int64_t row, float(&v)[8]) {
-      take_row<T, VEC, ADD>(a, row, L.c0, L.cnt, v);
-    };
-    auto keep = [&](int64_t row, const float(&v)[8]) {
-      if (ADD) Row<T, VEC>::store(static_cast<T*>(a.sum) + row * a.lds, L.c0, L.cnt, v);
-      if (CK) store_q8<VEC>(a.q, a.scale, row, a.C, L.c0, L.cnt, std::min(8, L.lpr), v);
-    };
-    for (; i + (TILE - 1) * L.RL < e; i += TILE * L.RL) {
-      float v[TILE][8];
-#pragma unroll
-      for (int t = 0; t < TILE; ++t) take(i + t * L.RL, v[t]);
-#pragma unroll
-      for (int t = 0; t < TILE; ++t) keep(i + t * L.RL, v[t]);
-      m.add<TILE>(v);
-    }
-    for (; i < e; i += L.RL) {
-      float v[1][8];
-      take(i, v[0]);
-      keep(i, v[0]);
-      m.add<1>(v);
-    }
-    for (int o = L.lpr; o < 64; o <<= 1) m.join(o);
-    if (lane < L.lpr) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) mm[wid * w8 + L.c0 + k] = m.mean[k], qq[wid * w8 + L.c0 + k] = m.m2[k];
-      if (lane == 0) nn[wid] = m.n;
-    }
-    __syncthreads();
-    // per channel: sum n_w mean_w, and the squares about zero, in float64
-    const int c = threadIdx.x;
-    if (c < a.C) {
-      double u = 0.0, v = 0.0;
-      for (int w = 0; w < NW; ++w) {
-        const double mw = mm[w * w8 + c], nw = nn[w];
-        u += nw * mw;
-        v += (double)qq[w * w8 + c] + nw * mw * mw;
-      }
-      s1[c] = u;
-      s2[c] = v;
-    }
-    __syncthreads();
-    const double count = (double)(e - r) * a.gs;
+    const double inv = 1.0 / ((double)(e - r) * a.gs);
     float2* part = a.part + ((int64_t)blockIdx.x + s) * a.G;
-    group_sums(s1, s2, a.G, a.gs, [&](int g, double u, double v) {
-      const double mean = u / count;
+    moments_of<T, VEC, ADD>(a, L, r, e, sh, [&](int g, double u, double v) {
+      const double mean = u * inv;
       part[g] = make_float2((float)mean, (float)fmax(v - u * mean, 0.0));
     });
     __syncthreads();
     r = e;
   }
+}
+
+// mean and rstd of a group from its sums about zero
+__device__ __forceinline__ float2 finish(double u, double v, double inv, float eps) {
+  const double m = u * inv;
+  return make_float2((float)m, 1.0f / sqrtf((float)fmax(v * inv - m * m, 0.0) + eps));
 }
 
 // ------------------------------------------------------------ joining the pieces
@@ -489,22 +559,22 @@ __global__ __launch_bounds__(NT) void k_norm_stats(NormArgs a) {
 template <typename TERM, typename DONE>
 __device__ __forceinline__ void join_pieces(const NormArgs& a, int s, int64_t b, int64_t e, double* sh, TERM term,
                                             DONE done) {
-  int gp = 1;
-  while (gp < a.G) gp <<= 1;
-  const int g = threadIdx.x & (gp - 1), p = threadIdx.x / gp, P = NT / gp;
-  const int64_t j0 = b / a.R, j1 = (e - 1) / a.R;
+  int lgp = 0;
+  while ((1 << lgp) < a.G) ++lgp;
+  const int gp = 1 << lgp, g = threadIdx.x & (gp - 1), p = threadIdx.x >> lgp, P = NT >> lgp;
+  const int64_t j0 = (uint32_t)b / (uint32_t)a.R, j1 = (uint32_t)(e - 1) / (uint32_t)a.R;
   double u = 0.0, v = 0.0;
   if (g < a.G) {
+    const float2* part = a.part + s * (int64_t)a.G + g;
 #pragma unroll 4
     for (int64_t j = j0 + p; j <= j1; j += P) {
-      const float2 t = a.part[(j + s) * a.G + g];
       const int64_t rows = std::min<int64_t>(e, (j + 1) * a.R) - std::max<int64_t>(b, j * a.R);
-      term(t, (double)rows, u, v);
+      term(part[j * a.G], (double)(int32_t)rows, u, v);
     }
   }
   for (int o = gp; o < 64; o <<= 1) u += __shfl_xor(u, o, 64), v += __shfl_xor(v, o, 64);
   if (gp >= 64) {
-    // one row of P sums per group
+    // P sums of each group, gp apart
     sh[threadIdx.x] = u;
     sh[NT + threadIdx.x] = v;
     __syncthreads();
@@ -516,7 +586,8 @@ __device__ __forceinline__ void join_pieces(const NormArgs& a, int s, int64_t b,
     const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63;
     if (lane < gp) sh[wid * 64 + lane] = u, sh[NT + wid * 64 + lane] = v;
     __syncthreads();
-    if (threadIdx.x < (unsigned)gp && g < a.G) {
+    if (threadIdx.x < (unsigned)a.G) {
+#pragma unroll
       for (int w = 1; w < NW; ++w) u += sh[w * 64 + g], v += sh[NT + w * 64 + g];
       done(g, u, v);
     }
@@ -524,51 +595,63 @@ __device__ __forceinline__ void join_pieces(const NormArgs& a, int s, int64_t b,
   __syncthreads();
 }
 
-// ------------------------------------------------------------ forward, second pass
+// ------------------------------------------------------------ forward, result
 
-// mean and rstd of eight channels' groups
-__device__ __forceinline__ void spread(const float* st, const NormArgs& a, int c0, float (&mean)[8], float (&rstd)[8]) {
+// y of rows [r, end) from their groups' mean and rstd.
+template <typename T, bool VEC, int ACT>
+__device__ __forceinline__ void apply_rows(const NormArgs& a, const Lanes& L, int64_t r, int64_t end,
+                                           const PerUnit<VEC>& mean, const PerUnit<VEC>& rstd, const float (&gamma)[8],
+                                           const float (&beta)[8]) {
+  constexpr int TILE = FWD_TILE<VEC>;
+  float scale[8];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const int g = std::min(c0 + k, a.C - 1) / a.gs;
-    mean[k] = st[2 * g];
-    rstd[k] = st[2 * g + 1];
+  for (int k = 0; k < 8; ++k) scale[k] = rstd[k] * gamma[k];
+  auto put = [&](int64_t row, float(&v)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = activate<ACT>(__builtin_fmaf(v[k] - mean[k], scale[k], beta[k]));
+    store_y<VEC>(a, row, L, v);
+  };
+  int64_t i = r + L.rl;
+  for (; i + (TILE - 1) * L.RL < end; i += TILE * L.RL) {
+    float v[TILE][8];
+#pragma unroll
+    for (int t = 0; t < TILE; ++t) Source<T, VEC>::load(a, i + t * L.RL, L.c0, L.cnt, v[t]);
+#pragma unroll
+    for (int t = 0; t < TILE; ++t) put(i + t * L.RL, v[t]);
   }
-}
-
-__device__ __forceinline__ void params8(const NormArgs& a, int c0, float (&gamma)[8], float (&beta)[8]) {
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const int c = std::min(c0 + k, a.C - 1);
-    gamma[k] = a.gamma ? a.gamma[c] : 1.0f;
-    beta[k] = a.gamma ? a.beta[c] : 0.0f;
+  for (; i < end; i += L.RL) {
+    float v[8];
+    Source<T, VEC>::load(a, i, L.c0, L.cnt, v);
+    put(i, v);
   }
 }
 
 // y = act((t - mean) * (rstd gamma) + beta) on this workgroup's rows, segment by
 // segment.  a.merge: the statistics come from the first pass's pieces (and are
 // written, by the workgroup that has the segment's first row), else from a.stats.
-template <typename T, typename Y, bool VEC>
+template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(NT) void k_norm_apply(NormArgs a) {
   __shared__ double sh[2 * NT];
-  __shared__ float st[2 * MAX_C];
+  __shared__ float2 st[MAX_C];
   const Lanes L(a.lg, a.C, NT);
   const int64_t r0 = (int64_t)blockIdx.x * a.RA, r1 = std::min<int64_t>(r0 + a.RA, a.n);
   if (a.merge && blockIdx.x == 0) {
     for (int s = threadIdx.x; s < a.n_seg; s += NT)
       if (seg_end(a, s) <= seg_begin(a, s))
-        for (int g = 0; g < 2 * a.G; ++g) a.stats[(int64_t)s * 2 * a.G + g] = 0.0f;
+        for (int g = 0; g < a.G; ++g) stats_of(a, s)[g] = make_float2(0.0f, 0.0f);
   }
   if (r0 >= r1) return;
+  const Groups<VEC> groups(a, L.c0);
   float gamma[8], beta[8];
-  params8(a, L.c0, gamma, beta);
+  params8<VEC>(a, L, gamma, beta);
   int s = seg_find(a, r0);
   for (int64_t r = r0; r < r1; ++s) {
     const int64_t b = seg_begin(a, s), e = seg_end(a, s), end = std::min<int64_t>(e, r1);
     if (end <= r) continue;
-    float mean[8], scale[8];
+    PerUnit<VEC> mean, rstd;
     if (a.merge) {
-      const double count = (double)(e - b) * a.gs;
+      const double inv = 1.0 / ((double)(e - b) * a.gs);
+      const bool first = b >= r0;
       join_pieces(
           a, s, b, e, sh,
           [&](float2 t, double rows, double& u, double& v) {
@@ -577,132 +660,148 @@ __global__ __launch_bounds__(NT) void k_norm_apply(NormArgs a) {
             v += (double)t.y + k * m * m;
           },
           [&](int g, double u, double v) {
-            const double m = u / count;
-            st[2 * g] = (float)m;
-            st[2 * g + 1] = (float)(1.0 / sqrt(fmax(v / count - m * m, 0.0) + (double)a.eps));
+            st[g] = finish(u, v, inv, a.eps);
+            if (first) stats_of(a, s)[g] = st[g];
           });
-      if (b >= r0)
-        for (int g = threadIdx.x; g < 2 * a.G; g += NT) a.stats[(int64_t)s * 2 * a.G + g] = st[g];
-      spread(st, a, L.c0, mean, scale);
+      groups.read(st, mean, rstd);
     } else {
-      spread(a.stats + (int64_t)s * 2 * a.G, a, L.c0, mean, scale);
+      groups.read(stats_of(a, s), mean, rstd);
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) scale[k] *= gamma[k];
-    auto put = [&](int64_t row, float(&v)[8]) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = __builtin_fmaf(v[k] - mean[k], scale[k], beta[k]);
-      activate8(a.act, v);
-      Row<Y, VEC>::store(static_cast<Y*>(a.y) + row * a.ldy, L.c0, L.cnt, v);
-    };
-    constexpr int TILE = FWD_TILE<VEC>;
-    int64_t i = r + L.rl;
-    for (; i + (TILE - 1) * L.RL < end; i += TILE * L.RL) {
-      float v[TILE][8];
-#pragma unroll
-      for (int t = 0; t < TILE; ++t) Source<T, VEC>::load(a, i + t * L.RL, L.c0, L.cnt, v[t]);
-#pragma unroll
-      for (int t = 0; t < TILE; ++t) put(i + t * L.RL, v[t]);
-    }
-    for (; i < end; i += L.RL) {
-      float v[8];
-      Source<T, VEC>::load(a, i, L.c0, L.cnt, v);
-      put(i, v);
-    }
+    apply_rows<T, VEC, ACT>(a, L, r, end, mean, rstd, gamma, beta);
     r = end;
   }
 }
 
-// ------------------------------------------------------------ backward
-
-// Of one row's eight channels: w = grad_y act'(z) and xn.
-template <typename T, bool VEC>
-__device__ __forceinline__ void weigh(const NormArgs& a, const float (&t)[8], const float (&mean)[8],
-                                      const float (&rstd)[8], const float (&gamma)[8], const float (&beta)[8],
-                                      float (&w)[8], float (&xn)[8]) {
-  float z[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    xn[k] = (t[k] - mean[k]) * rstd[k];
-    z[k] = __builtin_fmaf(xn[k], gamma[k], beta[k]);
+// One workgroup to a segment: both passes in one launch.
+template <typename T, bool VEC, bool ADD, int ACT>
+__global__ __launch_bounds__(NT) void k_norm_small(NormArgs a) {
+  extern __shared__ double sh[];
+  __shared__ float2 st[MAX_C];
+  const Lanes L(a.lg, a.C, NT);
+  const int s = blockIdx.x;
+  const int64_t b = seg_begin(a, s), e = seg_end(a, s);
+  if (e <= b) {
+    for (int g = threadIdx.x; g < a.G; g += NT) stats_of(a, s)[g] = make_float2(0.0f, 0.0f);
+    return;
   }
-  slope8(a.act, z, w);
+  const Groups<VEC> groups(a, L.c0);
+  float gamma[8], beta[8];
+  params8<VEC>(a, L, gamma, beta);
+  const double inv = 1.0 / ((double)(e - b) * a.gs);
+  moments_of<T, VEC, ADD>(a, L, b, e, sh, [&](int g, double u, double v) {
+    st[g] = finish(u, v, inv, a.eps);
+    stats_of(a, s)[g] = st[g];
+  });
+  __syncthreads();
+  PerUnit<VEC> mean, rstd;
+  groups.read(st, mean, rstd);
+  if (ADD) a.x = a.sum, a.ldx = a.lds;   // every lane reads back what it wrote itself
+  apply_rows<T, VEC, ACT>(a, L, b, e, mean, rstd, gamma, beta);
 }
 
-// First pass: per chunk and segment the groups' sums of gamma w and gamma w xn,
-// per chunk the channels' sums of w and w xn.
-template <typename T, bool VEC>
-__global__ __launch_bounds__(NT) void k_norm_bwd_sums(NormArgs a) {
-  extern __shared__ double sh[];
-  const Lanes L(a.lg, a.C, NT);
+// ------------------------------------------------------------ backward
+
+// What the backward passes know of a segment.
+template <bool VEC>
+struct Norm {
+  PerUnit<VEC> mean, rstd;
+  float gamma[8], beta[8];
+  // of one row: w = grad_y act'(z) in place of grad_y, xn in place of t
+  template <int ACT>
+  __device__ __forceinline__ void weigh(float (&t)[8], float (&w)[8]) const {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      t[k] = (t[k] - mean[k]) * rstd[k];
+      w[k] *= slope<ACT>(__builtin_fmaf(t[k], gamma[k], beta[k]));
+    }
+  }
+};
+
+// The workgroup's sums over rows [r, e): per channel w and w xn (to chan(c, u, v), by
+// the thread that has the number c), per group gamma times both (to out(g, u, v)).
+template <typename T, bool VEC, int ACT, typename CHAN, typename OUT>
+__device__ __forceinline__ void grad_sums(const NormArgs& a, const Lanes& L, const Norm<VEC>& nm, int64_t r, int64_t e,
+                                          double* sh, CHAN chan, OUT out) {
+  constexpr int TILE = BWD_TILE<VEC>;
   const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63, w8 = L.lpr * 8, c = threadIdx.x;
   double *s1 = sh, *s2 = sh + a.C;
   float *uu = reinterpret_cast<float*>(s2 + a.C), *vv = uu + NW * w8;
+  float u[8] = {}, v[8] = {};
+  auto add = [&](float(&t)[8], float(&w)[8]) {
+    nm.template weigh<ACT>(t, w);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) u[k] += w[k], v[k] = __builtin_fmaf(w[k], t[k], v[k]);
+  };
+  int64_t i = r + L.rl;
+  for (; i + (TILE - 1) * L.RL < e; i += TILE * L.RL) {
+    float t[TILE][8], w[TILE][8];
+#pragma unroll
+    for (int j = 0; j < TILE; ++j) {
+      Source<T, VEC>::load(a, i + j * L.RL, L.c0, L.cnt, t[j]);
+      Row<float, VEC>::load(a.gy + (i + j * L.RL) * a.ldgy, L.c0, L.cnt, w[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < TILE; ++j) add(t[j], w[j]);
+  }
+  for (; i < e; i += L.RL) {
+    float t[8], w[8];
+    Source<T, VEC>::load(a, i, L.c0, L.cnt, t);
+    Row<float, VEC>::load(a.gy + i * a.ldgy, L.c0, L.cnt, w);
+    add(t, w);
+  }
+  for (int o = L.lpr; o < 64; o <<= 1) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) u[k] += __shfl_xor(u[k], o, 64), v[k] += __shfl_xor(v[k], o, 64);
+  }
+  if (lane < L.lpr) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) uu[wid * w8 + L.c0 + k] = u[k], vv[wid * w8 + L.c0 + k] = v[k];
+  }
+  __syncthreads();
+  if (c < a.C) {
+    double x = 0.0, y = 0.0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) x += uu[w * w8 + c], y += vv[w * w8 + c];
+    const double gc = a.gamma ? a.gamma[c] : 1.0f;
+    chan(c, x, y);
+    s1[c] = gc * x;
+    s2[c] = gc * y;
+  }
+  __syncthreads();
+  group_sums(s1, s2, a.G, a.gs, out);
+}
+
+// First pass: per chunk and segment the groups' sums, per chunk the channels'.
+template <typename T, bool VEC, int ACT>
+__global__ __launch_bounds__(NT) void k_norm_bwd_sums(NormArgs a) {
+  extern __shared__ double sh[];
+  const Lanes L(a.lg, a.C, NT);
   const int64_t r0 = (int64_t)blockIdx.x * a.R, r1 = std::min<int64_t>(r0 + a.R, a.n);
-  float gamma[8], beta[8];
-  params8(a, L.c0, gamma, beta);
-  const double gc = c < a.C && a.gamma ? a.gamma[c] : 1.0;
+  const Groups<VEC> groups(a, L.c0);
+  Norm<VEC> nm;
+  params8<VEC>(a, L, nm.gamma, nm.beta);
   double cu = 0.0, cv = 0.0;
   int s = seg_find(a, r0);
   for (int64_t r = r0; r < r1; ++s) {
     const int64_t e = std::min<int64_t>(seg_end(a, s), r1);
     if (e <= r) continue;
-    float mean[8], rstd[8], u[8] = {}, v[8] = {};
-    spread(a.stats + (int64_t)s * 2 * a.G, a, L.c0, mean, rstd);
-    auto add = [&](const float(&t)[8], float(&w)[8]) {
-      float xn[8];
-      weigh<T, VEC>(a, t, mean, rstd, gamma, beta, w, xn);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) u[k] += w[k], v[k] = __builtin_fmaf(w[k], xn[k], v[k]);
-    };
-    constexpr int TILE = BWD_TILE<VEC>;
-    int64_t i = r + L.rl;
-    for (; i + (TILE - 1) * L.RL < e; i += TILE * L.RL) {
-      float t[TILE][8], w[TILE][8];
-#pragma unroll
-      for (int j = 0; j < TILE; ++j) {
-        Source<T, VEC>::load(a, i + j * L.RL, L.c0, L.cnt, t[j]);
-        Row<float, VEC>::load(a.gy + (i + j * L.RL) * a.ldgy, L.c0, L.cnt, w[j]);
-      }
-#pragma unroll
-      for (int j = 0; j < TILE; ++j) add(t[j], w[j]);
-    }
-    for (; i < e; i += L.RL) {
-      float t[8], w[8];
-      Source<T, VEC>::load(a, i, L.c0, L.cnt, t);
-      Row<float, VEC>::load(a.gy + i * a.ldgy, L.c0, L.cnt, w);
-      add(t, w);
-    }
-    for (int o = L.lpr; o < 64; o <<= 1) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) u[k] += __shfl_xor(u[k], o, 64), v[k] += __shfl_xor(v[k], o, 64);
-    }
-    if (lane < L.lpr) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) uu[wid * w8 + L.c0 + k] = u[k], vv[wid * w8 + L.c0 + k] = v[k];
-    }
-    __syncthreads();
-    if (c < a.C) {
-      double x = 0.0, y = 0.0;
-      for (int w = 0; w < NW; ++w) x += uu[w * w8 + c], y += vv[w * w8 + c];
-      cu += x, cv += y;
-      s1[c] = gc * x;
-      s2[c] = gc * y;
-    }
-    __syncthreads();
+    groups.read(stats_of(a, s), nm.mean, nm.rstd);
     float2* part = a.part + ((int64_t)blockIdx.x + s) * a.G;
-    group_sums(s1, s2, a.G, a.gs, [&](int g, double x, double y) { part[g] = make_float2((float)x, (float)y); });
+    grad_sums<T, VEC, ACT>(
+        a, L, nm, r, e, sh, [&](int, double x, double y) { cu += x, cv += y; },
+        [&](int g, double x, double y) { part[g] = make_float2((float)x, (float)y); });
     __syncthreads();
     r = e;
   }
+  const int c = threadIdx.x;
   if (a.part_c && c < a.C) {
     a.part_c[(int64_t)blockIdx.x * 2 * a.C + c] = (float)cu;
     a.part_c[(int64_t)blockIdx.x * 2 * a.C + a.C + c] = (float)cv;
   }
 }
 
-// dbeta and dgamma from the chunks' sums: 64 columns of part_c to a workgroup of
-// `threads`, the chunks dealt to its waves, joined in wave order.
+// dbeta and dgamma from the chunks' sums: 64 columns of part_c to a workgroup,
+// the chunks dealt to its waves, joined in wave order.
 __device__ __forceinline__ void columns(const NormArgs& a, int block, double* sh, int waves) {
   const int col = block * 64 + (threadIdx.x & 63), wid = threadIdx.x >> 6;
   double v = 0.0;
@@ -719,19 +818,49 @@ __device__ __forceinline__ void columns(const NormArgs& a, int block, double* sh
   }
 }
 
-// grad_x of one row from its groups' sums
-__device__ __forceinline__ void grad8(const float (&rstd)[8], const float (&gamma)[8], const float (&A)[8],
-                                      const float (&B)[8], const float (&w)[8], const float (&xn)[8], float (&g)[8]) {
+// grad_x of one row from its groups' sums A and B, added to g
+template <bool VEC>
+__device__ __forceinline__ void grad8(const Norm<VEC>& nm, const PerUnit<VEC>& A, const PerUnit<VEC>& B,
+                                      const float (&w)[8], const float (&xn)[8], float (&g)[8]) {
 #pragma unroll
   for (int k = 0; k < 8; ++k)
-    g[k] = __builtin_fmaf(rstd[k], __builtin_fmaf(-xn[k], B[k], __builtin_fmaf(gamma[k], w[k], -A[k])), g[k]);
+    g[k] = __builtin_fmaf(nm.rstd[k], __builtin_fmaf(-xn[k], B[k], __builtin_fmaf(nm.gamma[k], w[k], -A[k])), g[k]);
+}
+
+template <typename T, bool VEC, int ACT>
+__device__ __forceinline__ void grad_rows(const NormArgs& a, const Lanes& L, const Norm<VEC>& nm, const PerUnit<VEC>& A,
+                                          const PerUnit<VEC>& B, int64_t r, int64_t end) {
+  constexpr int TILE = BWD_TILE<VEC>;
+  auto take = [&](int64_t row, float(&t)[8], float(&w)[8], float(&g)[8]) {
+    Source<T, VEC>::load(a, row, L.c0, L.cnt, t);
+    Row<float, VEC>::load(a.gy + row * a.ldgy, L.c0, L.cnt, w);
+    if (a.ga) Row<float, VEC>::load(a.ga + row * a.ldga, L.c0, L.cnt, g);
+  };
+  auto put = [&](int64_t row, float(&t)[8], float(&w)[8], float(&g)[8]) {
+    nm.template weigh<ACT>(t, w);
+    grad8(nm, A, B, w, t, g);
+    Row<float, VEC>::store(a.gx + row * a.ldgx, L.c0, L.cnt, g);
+  };
+  int64_t i = r + L.rl;
+  for (; i + (TILE - 1) * L.RL < end; i += TILE * L.RL) {
+    float t[TILE][8], w[TILE][8], g[TILE][8] = {};
+#pragma unroll
+    for (int j = 0; j < TILE; ++j) take(i + j * L.RL, t[j], w[j], g[j]);
+#pragma unroll
+    for (int j = 0; j < TILE; ++j) put(i + j * L.RL, t[j], w[j], g[j]);
+  }
+  for (; i < end; i += L.RL) {
+    float t[8], w[8], g[8] = {};
+    take(i, t, w, g);
+    put(i, t, w, g);
+  }
 }
 
 // Second pass.  The first a.nred workgroups form dbeta and dgamma.
-template <typename T, bool VEC>
+template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(NT) void k_norm_bwd_dx(NormArgs a) {
   __shared__ double sh[2 * NT];
-  __shared__ float st[2 * MAX_C];
+  __shared__ float2 st[MAX_C];
   if ((int)blockIdx.x < a.nred) {
     columns(a, blockIdx.x, sh, NW);
     return;
@@ -739,48 +868,48 @@ __global__ __launch_bounds__(NT) void k_norm_bwd_dx(NormArgs a) {
   const Lanes L(a.lg, a.C, NT);
   const int64_t r0 = (int64_t)(blockIdx.x - a.nred) * a.RA, r1 = std::min<int64_t>(r0 + a.RA, a.n);
   if (r0 >= r1) return;
-  float gamma[8], beta[8];
-  params8(a, L.c0, gamma, beta);
+  const Groups<VEC> groups(a, L.c0);
+  Norm<VEC> nm;
+  params8<VEC>(a, L, nm.gamma, nm.beta);
   int s = seg_find(a, r0);
   for (int64_t r = r0; r < r1; ++s) {
     const int64_t b = seg_begin(a, s), e = seg_end(a, s), end = std::min<int64_t>(e, r1);
     if (end <= r) continue;
-    const double count = (double)(e - b) * a.gs;
+    groups.read(stats_of(a, s), nm.mean, nm.rstd);
+    const double inv = 1.0 / ((double)(e - b) * a.gs);
     join_pieces(
         a, s, b, e, sh, [&](float2 t, double, double& u, double& v) { u += t.x, v += t.y; },
-        [&](int g, double u, double v) { st[2 * g] = (float)(u / count), st[2 * g + 1] = (float)(v / count); });
-    float mean[8], rstd[8], A[8], B[8];
-    spread(st, a, L.c0, A, B);
-    spread(a.stats + (int64_t)s * 2 * a.G, a, L.c0, mean, rstd);
-    auto put = [&](int64_t row, const float(&t)[8], float(&w)[8], float(&g)[8]) {
-      float xn[8];
-      weigh<T, VEC>(a, t, mean, rstd, gamma, beta, w, xn);
-      grad8(rstd, gamma, A, B, w, xn, g);
-      Row<float, VEC>::store(a.gx + row * a.ldgx, L.c0, L.cnt, g);
-    };
-    constexpr int TD = BWD_TILE<VEC>;
-    int64_t i = r + L.rl;
-    for (; i + (TD - 1) * L.RL < end; i += TD * L.RL) {
-      float t[TD][8], w[TD][8], g[TD][8] = {};
-#pragma unroll
-      for (int j = 0; j < TD; ++j) {
-        const int64_t row = i + j * L.RL;
-        Source<T, VEC>::load(a, row, L.c0, L.cnt, t[j]);
-        Row<float, VEC>::load(a.gy + row * a.ldgy, L.c0, L.cnt, w[j]);
-        if (a.ga) Row<float, VEC>::load(a.ga + row * a.ldga, L.c0, L.cnt, g[j]);
-      }
-#pragma unroll
-      for (int j = 0; j < TD; ++j) put(i + j * L.RL, t[j], w[j], g[j]);
-    }
-    for (; i < end; i += L.RL) {
-      float t[8], w[8], g[8] = {};
-      Source<T, VEC>::load(a, i, L.c0, L.cnt, t);
-      Row<float, VEC>::load(a.gy + i * a.ldgy, L.c0, L.cnt, w);
-      if (a.ga) Row<float, VEC>::load(a.ga + i * a.ldga, L.c0, L.cnt, g);
-      put(i, t, w, g);
-    }
+        [&](int g, double u, double v) { st[g] = make_float2((float)(u * inv), (float)(v * inv)); });
+    PerUnit<VEC> A, B;
+    groups.read(st, A, B);
+    grad_rows<T, VEC, ACT>(a, L, nm, A, B, r, end);
     r = end;
   }
+}
+
+// One segment, one workgroup: both passes and the parameters' gradients.
+template <typename T, bool VEC, int ACT>
+__global__ __launch_bounds__(NT) void k_norm_bwd_small(NormArgs a) {
+  extern __shared__ double sh[];
+  __shared__ float2 st[MAX_C];
+  const Lanes L(a.lg, a.C, NT);
+  const Groups<VEC> groups(a, L.c0);
+  Norm<VEC> nm;
+  params8<VEC>(a, L, nm.gamma, nm.beta);
+  groups.read(stats_of(a, 0), nm.mean, nm.rstd);
+  const double inv = 1.0 / ((double)a.n * a.gs);
+  grad_sums<T, VEC, ACT>(
+      a, L, nm, 0, a.n, sh,
+      [&](int c, double x, double y) {
+        if (!a.dbeta) return;
+        a.dbeta[c] = a.accumulate ? a.dbeta[c] + (float)x : (float)x;
+        a.dgamma[c] = a.accumulate ? a.dgamma[c] + (float)y : (float)y;
+      },
+      [&](int g, double u, double v) { st[g] = make_float2((float)(u * inv), (float)(v * inv)); });
+  __syncthreads();
+  PerUnit<VEC> A, B;
+  groups.read(st, A, B);
+  grad_rows<T, VEC, ACT>(a, L, nm, A, B, 0, a.n);
 }
 
 // dbeta and dgamma alone (rows as segments, no rows at all)
@@ -791,138 +920,144 @@ __global__ __launch_bounds__(RNT) void k_norm_columns(NormArgs a) {
 
 // ------------------------------------------------------------ each row a segment
 
-// Sums over the groups of a row: p[k] becomes the sum over the group of channel
-// c0 + k.  width: the lanes of a group where it is whole lanes and a power of two
-// of them (or the whole row); 0: any other group, through the wave's LDS.
+// Sums over the groups of a row.  How depends on the group: a unit by itself;
+// whole lanes, a power of two of them (or the whole row), by shuffles; any
+// other through the wave's LDS.
+template <bool VEC>
 struct RowGroups {
-  int width;
-  int at[8];     // first channel of each channel's group
-  float* lds;    // the wave's 512 floats
+  static constexpr int U = UNIT<VEC>, N = 8 / U;
+  int width;     // lanes of a group; 0: a unit; -1: through LDS
+  int at[N];     // first unit of each unit's group
+  float* lds;    // the wave's 64 N floats
 
   __device__ __forceinline__ RowGroups(const NormArgs& a, const Lanes& L, float* wave_lds) : lds(wave_lds) {
-    const int lg = a.gs / 8;
-    width = a.G == 1 ? L.lpr : (a.gs % 8 == 0 && (lg & (lg - 1)) == 0) ? lg : 0;
+    const int lanes = a.gs / 8, gu = a.gs / U;
+    width = gu == 1 ? 0 : a.G == 1 ? L.lpr : (a.gs % 8 == 0 && (lanes & (lanes - 1)) == 0) ? lanes : -1;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) at[k] = std::min(L.c0 + k, a.C - 1) / a.gs * a.gs;
+    for (int j = 0; j < N; ++j) at[j] = std::min(L.lr * N + j, a.C / U - 1) / gu * gu;
   }
-  __device__ __forceinline__ void sum(const NormArgs& a, const Lanes& L, float (&p)[8]) const {
-    if (width) {
-      float s = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-      for (int o = 1; o < width; o <<= 1) s += __shfl_xor(s, o, 64);
+  // p: this lane's eight values; the sum over its group for each unit
+  __device__ __forceinline__ PerUnit<VEC> sum(const NormArgs& a, const Lanes& L, const float (&p)[8]) const {
+    PerUnit<VEC> s;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) p[k] = s;
-      return;
+    for (int j = 0; j < N; ++j) {
+      s.v[j] = p[j * U];
+#pragma unroll
+      for (int k = 1; k < U; ++k) s.v[j] += p[j * U + k];
     }
-    float* row = lds + ((threadIdx.x & 63) - L.lr) * 8;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (width > 0) {
+      float t = s.v[0];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) row[L.c0 + k] = p[k];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+      for (int j = 1; j < N; ++j) t += s.v[j];
+      for (int o = 1; o < width; o <<= 1) t += __shfl_xor(t, o, 64);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      float s = 0.0f;
-      for (int i = 0; i < a.gs; ++i) s += row[at[k] + i];
-      p[k] = s;
+      for (int j = 0; j < N; ++j) s.v[j] = t;
+    } else if (width < 0) {
+      float* row = lds + ((threadIdx.x & 63) - L.lr) * N;
+#pragma unroll
+      for (int j = 0; j < N; ++j) row[L.lr * N + j] = s.v[j];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        float t = 0.0f;
+        for (int i = 0; i < a.gs / U; ++i) t += row[at[j] + i];
+        s.v[j] = t;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
-  // mean and rstd of a row's groups
-  __device__ __forceinline__ void read(const NormArgs& a, const float* st, float (&mean)[8], float (&rstd)[8]) const {
-    if (width) {
-      const float2 t = reinterpret_cast<const float2*>(st)[at[0] / a.gs];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) mean[k] = t.x, rstd[k] = t.y;
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) mean[k] = st[2 * (at[k] / a.gs)], rstd[k] = st[2 * (at[k] / a.gs) + 1];
-    }
+    return s;
   }
 };
 
-template <typename T, typename Y, bool VEC, bool ADD, bool CK>
+template <typename T, bool VEC, bool ADD, int ACT>
 __global__ __launch_bounds__(RNT) void k_norm_rows(NormArgs a) {
-  __shared__ float lds[RNT * 8];
+  constexpr int U = UNIT<VEC>, N = 8 / U;
+  __shared__ float lds[RNT * N];
   const Lanes L(a.lg, a.C, RNT);
-  const RowGroups R(a, L, lds + (threadIdx.x >> 6) * 512);
+  const RowGroups<VEC> R(a, L, lds + (threadIdx.x >> 6) * 64 * N);
+  const Groups<VEC> groups(a, L.c0);
   float gamma[8], beta[8];
-  params8(a, L.c0, gamma, beta);
+  params8<VEC>(a, L, gamma, beta);
   const float f = 1.0f / a.gs;
   for (int64_t i = (int64_t)blockIdx.x * L.RL + L.rl; i < a.n; i += (int64_t)gridDim.x * L.RL) {
-    float v[8], m[8], q[8];
-    take_row<T, VEC, ADD>(a, i, L.c0, L.cnt, v);
+    float t[1][8], q[8];
+    take_rows<T, VEC, ADD, 1>(a, i, 0, L.c0, L.cnt, t);
+    float(&v)[8] = t[0];
     if (ADD) Row<T, VEC>::store(static_cast<T*>(a.sum) + i * a.lds, L.c0, L.cnt, v);
-    if (CK) store_q8<VEC>(a.q, a.scale, i, a.C, L.c0, L.cnt, std::min(8, L.lpr), v);
+    if (a.ck) store_q8<VEC>(a.q, a.scale, i, a.C, L.c0, L.cnt, std::min(8, L.lpr), v);
+    PerUnit<VEC> mean = R.sum(a, L, v), rstd;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) m[k] = v[k];
-    R.sum(a, L, m);
+    for (int j = 0; j < N; ++j) mean.v[j] *= f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      m[k] *= f;
-      const float d = k < L.cnt ? v[k] - m[k] : 0.0f;
+      const float d = k < L.cnt ? v[k] - mean[k] : 0.0f;
       q[k] = d * d;
     }
-    R.sum(a, L, q);
+    rstd = R.sum(a, L, q);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      q[k] = 1.0f / sqrtf(__builtin_fmaf(q[k], f, a.eps));
-      if (k < L.cnt && L.c0 + k == R.at[k]) {
-        const int64_t g = i * a.G + R.at[k] / a.gs;
-        reinterpret_cast<float2*>(a.stats)[g] = make_float2(m[k], q[k]);
-      }
-      v[k] = __builtin_fmaf((v[k] - m[k]) * q[k], gamma[k], beta[k]);
+    for (int j = 0; j < N; ++j) {
+      rstd.v[j] = 1.0f / sqrtf(__builtin_fmaf(rstd.v[j], f, a.eps));
+      // a group's first unit writes for it
+      if (j * U < L.cnt && L.lr * N + j == R.at[j])
+        reinterpret_cast<float2*>(a.stats)[i * a.G + groups.g[j]] = make_float2(mean.v[j], rstd.v[j]);
     }
-    activate8(a.act, v);
-    Row<Y, VEC>::store(static_cast<Y*>(a.y) + i * a.ldy, L.c0, L.cnt, v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      v[k] = activate<ACT>(__builtin_fmaf((v[k] - mean[k]) * rstd[k], gamma[k], beta[k]));
+    store_y<VEC>(a, i, L, v);
   }
 }
 
-template <typename Y, bool VEC>
+template <bool VEC, int ACT>
 __global__ __launch_bounds__(RNT) void k_norm_rows_restore(NormArgs a) {
   const Lanes L(a.lg, a.C, RNT);
-  const RowGroups R(a, L, nullptr);
+  const Groups<VEC> groups(a, L.c0);
   float gamma[8], beta[8];
-  params8(a, L.c0, gamma, beta);
+  params8<VEC>(a, L, gamma, beta);
   for (int64_t i = (int64_t)blockIdx.x * L.RL + L.rl; i < a.n; i += (int64_t)gridDim.x * L.RL) {
-    float v[8], mean[8], rstd[8];
+    float v[8];
+    PerUnit<VEC> mean, rstd;
     Source<Q8, VEC>::load(a, i, L.c0, L.cnt, v);
-    R.read(a, a.stats + i * 2 * a.G, mean, rstd);
+    groups.read(reinterpret_cast<const float2*>(a.stats) + i * a.G, mean, rstd);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = __builtin_fmaf((v[k] - mean[k]) * rstd[k], gamma[k], beta[k]);
-    activate8(a.act, v);
-    Row<Y, VEC>::store(static_cast<Y*>(a.y) + i * a.ldy, L.c0, L.cnt, v);
+    for (int k = 0; k < 8; ++k)
+      v[k] = activate<ACT>(__builtin_fmaf((v[k] - mean[k]) * rstd[k], gamma[k], beta[k]));
+    store_y<VEC>(a, i, L, v);
   }
 }
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(RNT) void k_norm_rows_bwd(NormArgs a) {
+  constexpr int N = 8 / UNIT<VEC>;
   __shared__ float lds[RNT * 16];
   const Lanes L(a.lg, a.C, RNT);
-  const RowGroups R(a, L, lds + (threadIdx.x >> 6) * 512);
-  float gamma[8], beta[8], u[8] = {}, v[8] = {};
-  params8(a, L.c0, gamma, beta);
+  const RowGroups<VEC> R(a, L, lds + (threadIdx.x >> 6) * 64 * N);
+  const Groups<VEC> groups(a, L.c0);
+  Norm<VEC> nm;
+  float u[8] = {}, v[8] = {};
+  params8<VEC>(a, L, nm.gamma, nm.beta);
   const float f = 1.0f / a.gs;
   for (int64_t i = (int64_t)blockIdx.x * L.RL + L.rl; i < a.n; i += (int64_t)gridDim.x * L.RL) {
-    float t[8], w[8], g[8] = {}, mean[8], rstd[8], xn[8], A[8], B[8];
+    float t[8], w[8], g[8] = {}, x[8], y[8];
     Source<T, VEC>::load(a, i, L.c0, L.cnt, t);
     Row<float, VEC>::load(a.gy + i * a.ldgy, L.c0, L.cnt, w);
     if (a.ga) Row<float, VEC>::load(a.ga + i * a.ldga, L.c0, L.cnt, g);
-    R.read(a, a.stats + i * 2 * a.G, mean, rstd);
-    weigh<T, VEC>(a, t, mean, rstd, gamma, beta, w, xn);
+    groups.read(reinterpret_cast<const float2*>(a.stats) + i * a.G, nm.mean, nm.rstd);
+    nm.template weigh<ACT>(t, w);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       if (k >= L.cnt) w[k] = 0.0f;
       u[k] += w[k];
-      v[k] = __builtin_fmaf(w[k], xn[k], v[k]);
-      A[k] = k < L.cnt ? gamma[k] * w[k] : 0.0f;
-      B[k] = k < L.cnt ? A[k] * xn[k] : 0.0f;
+      v[k] = __builtin_fmaf(w[k], t[k], v[k]);
+      x[k] = k < L.cnt ? nm.gamma[k] * w[k] : 0.0f;
+      y[k] = k < L.cnt ? x[k] * t[k] : 0.0f;
     }
-    R.sum(a, L, A);
-    R.sum(a, L, B);
+    PerUnit<VEC> A = R.sum(a, L, x), B = R.sum(a, L, y);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) A[k] *= f, B[k] *= f;
-    grad8(rstd, gamma, A, B, w, xn, g);
+    for (int j = 0; j < N; ++j) A.v[j] *= f, B.v[j] *= f;
+    grad8(nm, A, B, w, t, g);
     Row<float, VEC>::store(a.gx + i * a.ldgx, L.c0, L.cnt, g);
   }
   if (!a.part_c) return;
@@ -1035,7 +1170,6 @@ NormArgs norm_args(const dsmp_norm_desc& d, const dsmp_segments& s) {
   a.ptr = s.ptr;
   a.len = s.ptr ? 0 : s.n / s.n_seg;
   a.eps = d.eps;
-  a.act = d.act;
   int64_t chunks;
   chunking(s.n, a.C, a.R, chunks);
   a.nchunks = (int)chunks;
@@ -1055,6 +1189,18 @@ unsigned row_grid(const dsmp_handle* h, const NormArgs& a, int per_cu) {
   return (unsigned)std::min<int64_t>((a.n + step - 1) / step, (int64_t)h->n_cu * per_cu);
 }
 
+bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7) == 0; }
+
+// the channels, groups and parameters that VEC asks for
+bool whole(const NormArgs& a) {
+  return a.C % 8 == 0 && a.gs % 4 == 0 && aligned(a.gamma, 0, 4) && aligned(a.beta, 0, 4);
+}
+
+// One launch with a workgroup to a segment: where all the rows are at most
+// SMALL_STEPS steps of one workgroup, however they are dealt to the segments.
+constexpr int SMALL_STEPS = 16;
+bool small(const NormArgs& a) { return a.n <= (int64_t)SMALL_STEPS * (NT >> a.lg); }
+
 template <typename F>
 void by_bool(bool b, F f) {
   if (b)
@@ -1068,6 +1214,16 @@ void by_type(int dtype, F f) {
     f(__bf16{});
   else
     f(float{});
+}
+
+template <typename F>
+void by_act(int act, F f) {
+  switch (act) {
+    case DSMP_ACT_RELU: return f(std::integral_constant<int, DSMP_ACT_RELU>{});
+    case DSMP_ACT_SILU: return f(std::integral_constant<int, DSMP_ACT_SILU>{});
+    case DSMP_ACT_GELU: return f(std::integral_constant<int, DSMP_ACT_GELU>{});
+    default: return f(std::integral_constant<int, DSMP_ACT_IDENTITY>{});
+  }
 }
 
 }  // namespace
@@ -1108,33 +1264,34 @@ extern "C" dsmp_status dsmp_group_norm_forward(dsmp_handle* h, const dsmp_norm_d
   if (ck) a.q = ck->q, a.scale = ck->scale;
   a.part = w.part;
   a.merge = 1;
-  const int xs = size_of(desc->x_dtype), ys = size_of(desc->y_dtype);
-  const bool vec = C % 8 == 0 && aligned(x, ldx, xs) && aligned(addend, lda, xs) && aligned(sum, lds, xs) &&
-                   aligned(y, ldy, ys) && (!ck || (reinterpret_cast<uintptr_t>(ck->q) & 7) == 0);
+  a.ck = ck != nullptr;
+  a.y_bf16 = desc->y_dtype == DSMP_BF16;
+  const int xs = size_of(desc->x_dtype);
+  const bool vec = whole(a) && aligned(x, ldx, xs) && aligned(addend, lda, xs) && aligned(sum, lds, xs) &&
+                   aligned(y, ldy, size_of(desc->y_dtype)) && (!ck || aligned8(ck->q));
   ProfScope prof(h, DSMP_K_NORM);
   by_type(desc->x_dtype, [&](auto xt) {
-    by_type(desc->y_dtype, [&](auto yt) {
-      by_bool(vec, [&](auto v) {
+    by_bool(vec, [&](auto v) {
+      by_act(desc->act, [&](auto act) {
         using T = decltype(xt);
-        using Y = decltype(yt);
         constexpr bool V = decltype(v)::value;
+        constexpr int ACT = decltype(act)::value;
         if (rows_are_segments(*seg)) {
-          by_bool(addend != nullptr, [&](auto ad) {
-            by_bool(ck != nullptr, [&](auto c) {
-              DSMP_GO((k_norm_rows<T, Y, V, decltype(ad)::value, decltype(c)::value>), row_grid(h, a, 16), RNT, 0);
-            });
+          by_bool(addend, [&](auto ad) {
+            DSMP_GO((k_norm_rows<T, V, decltype(ad)::value, ACT>), row_grid(h, a, 16), RNT, 0);
           });
-          return;
+        } else if (small(a)) {
+          by_bool(addend, [&](auto ad) {
+            DSMP_GO((k_norm_small<T, V, decltype(ad)::value, ACT>), a.n_seg, NT, sums_lds(a.lg, C));
+          });
+        } else {
+          by_bool(addend, [&](auto ad) {
+            DSMP_GO((k_norm_stats<T, V, decltype(ad)::value>), a.nchunks, NT, sums_lds(a.lg, C));
+          });
+          if (addend) a.x = sum, a.ldx = lds;
+          const unsigned grid = second_grid(h, a);
+          DSMP_GO((k_norm_apply<T, V, ACT>), grid, NT, 0);
         }
-        if (n > 0)
-          by_bool(addend != nullptr, [&](auto ad) {
-            by_bool(ck != nullptr, [&](auto c) {
-              DSMP_GO((k_norm_stats<T, V, decltype(ad)::value, decltype(c)::value>), a.nchunks, NT, stats_lds(a.lg, C));
-            });
-          });
-        if (addend) a.x = sum, a.ldx = lds;
-        const unsigned grid = second_grid(h, a);
-        DSMP_GO((k_norm_apply<T, Y, V>), grid, NT, 0);
       });
     });
   });
@@ -1156,17 +1313,18 @@ extern "C" dsmp_status dsmp_group_norm_restore(dsmp_handle* h, const dsmp_norm_d
   NormArgs a = norm_args(*desc, *seg);
   a.x = ck->q, a.xscale = ck->scale;
   a.gamma = gamma, a.beta = beta, a.y = y, a.ldy = ldy, a.stats = const_cast<float*>(stats);
-  const bool vec = C % 8 == 0 && aligned(y, ldy, size_of(desc->y_dtype)) && (reinterpret_cast<uintptr_t>(ck->q) & 7) == 0;
+  a.y_bf16 = desc->y_dtype == DSMP_BF16;
+  const bool vec = whole(a) && aligned(y, ldy, size_of(desc->y_dtype)) && aligned8(ck->q);
   ProfScope prof(h, DSMP_K_NORM);
-  by_type(desc->y_dtype, [&](auto yt) {
-    by_bool(vec, [&](auto v) {
-      using Y = decltype(yt);
+  by_bool(vec, [&](auto v) {
+    by_act(desc->act, [&](auto act) {
       constexpr bool V = decltype(v)::value;
+      constexpr int ACT = decltype(act)::value;
       if (rows_are_segments(*seg)) {
-        DSMP_GO((k_norm_rows_restore<Y, V>), row_grid(h, a, 16), RNT, 0);
+        DSMP_GO((k_norm_rows_restore<V, ACT>), row_grid(h, a, 16), RNT, 0);
       } else {
         const unsigned grid = second_grid(h, a);
-        DSMP_GO((k_norm_apply<Q8, Y, V>), grid, NT, 0);
+        DSMP_GO((k_norm_apply<Q8, V, ACT>), grid, NT, 0);
       }
     });
   });
@@ -1203,9 +1361,8 @@ extern "C" dsmp_status dsmp_group_norm_backward(dsmp_handle* h, const dsmp_norm_
   a.dgamma = dgamma, a.dbeta = dbeta, a.accumulate = flags & DSMP_GRAD_ACCUMULATE;
   a.part = w.part, a.part_c = gamma ? w.part_c : nullptr;
   const unsigned nred = gamma ? ceil_div(2 * C, 64) : 0;
-  const bool vec = C % 8 == 0 && aligned(x, ldx, size_of(desc->x_dtype)) && aligned(grad_y, ldgy, 4) &&
-                   aligned(grad_addend, ldga, 4) && aligned(grad_x, ldgx, 4) &&
-                   (!ck || (reinterpret_cast<uintptr_t>(ck->q) & 7) == 0);
+  const bool vec = whole(a) && aligned(x, ldx, size_of(desc->x_dtype)) && aligned(grad_y, ldgy, 4) &&
+                   aligned(grad_addend, ldga, 4) && aligned(grad_x, ldgx, 4) && (!ck || aligned8(ck->q));
   ProfScope prof(h, DSMP_K_NORM);
   if (n == 0) {
     if (nred) DSMP_GO(k_norm_columns, nred, RNT, 0);   // sums of no chunk
@@ -1214,19 +1371,24 @@ extern "C" dsmp_status dsmp_group_norm_backward(dsmp_handle* h, const dsmp_norm_
   }
   auto go = [&](auto xt) {
     by_bool(vec, [&](auto v) {
-      using T = decltype(xt);
-      constexpr bool V = decltype(v)::value;
-      if (rows_are_segments(*seg)) {
-        const unsigned grid = std::min<unsigned>(row_grid(h, a, 4), MAX_CHUNKS);
-        a.nchunks = (int)grid;
-        DSMP_GO((k_norm_rows_bwd<T, V>), grid, RNT, 0);
-        if (nred) DSMP_GO(k_norm_columns, nred, RNT, 0);
-        return;
-      }
-      DSMP_GO((k_norm_bwd_sums<T, V>), a.nchunks, NT, stats_lds(a.lg, C));
-      a.nred = (int)nred;
-      const unsigned grid = second_grid(h, a);
-      DSMP_GO((k_norm_bwd_dx<T, V>), grid + nred, NT, 0);
+      by_act(desc->act, [&](auto act) {
+        using T = decltype(xt);
+        constexpr bool V = decltype(v)::value;
+        constexpr int ACT = decltype(act)::value;
+        if (rows_are_segments(*seg)) {
+          const unsigned grid = std::min<unsigned>(row_grid(h, a, 4), MAX_CHUNKS);
+          a.nchunks = (int)grid;
+          DSMP_GO((k_norm_rows_bwd<T, V, ACT>), grid, RNT, 0);
+          if (nred) DSMP_GO(k_norm_columns, nred, RNT, 0);
+        } else if (small(a) && a.n_seg == 1) {
+          DSMP_GO((k_norm_bwd_small<T, V, ACT>), 1, NT, sums_lds(a.lg, C));
+        } else {
+          DSMP_GO((k_norm_bwd_sums<T, V, ACT>), a.nchunks, NT, sums_lds(a.lg, C));
+          a.nred = (int)nred;
+          const unsigned grid = second_grid(h, a);
+          DSMP_GO((k_norm_bwd_dx<T, V, ACT>), grid + nred, NT, 0);
+        }
+      });
     });
   };
   if (ck)
