@@ -394,8 +394,8 @@ typedef struct dsmp_checkpoint {
 } dsmp_checkpoint;
 
 /* x: device [n, channels] of dtype DSMP_F32 or DSMP_BF16, rows ldx elements
- * apart (ldx >= channels; any alignment of its type; so for every matrix of
- * this section and the next).  n == 0 enqueues nothing. */
+ * apart (channels <= ldx <= 2^16; any alignment of its type; so for every matrix
+ * of this section and the next).  n == 0 enqueues nothing. */
 dsmp_status dsmp_checkpoint_store(dsmp_handle* h, const void* x, int32_t dtype, int64_t ldx, int64_t n,
                                   int32_t channels, const dsmp_checkpoint* ck);
 

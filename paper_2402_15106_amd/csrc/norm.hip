@@ -17,6 +17,8 @@
 // every run.  What crosses a chunk is joined in float64.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
+#include <type_traits>
 
 #include "common.hpp"
 
@@ -28,6 +30,8 @@ constexpr int MAX_C = 512;      // 64 lanes of 8 channels: a row stays in one wa
 constexpr int BLOCK_C = 64;     // channels that share a checkpoint scale
 constexpr int NT = 512;         // threads of the passes over segments
 constexpr int NW = NT / 64;
+constexpr int SNT = 1024;       // threads where one workgroup takes a whole segment
+constexpr int SNW = SNT / 64;
 constexpr int RNT = 256;        // threads where each row is a segment, and of the checkpoint passes
 constexpr int MAX_CHUNKS = 512; // chunks of rows that sums are split over
 constexpr float TINY = 0x1p-100f;
@@ -35,18 +39,23 @@ constexpr float TINY = 0x1p-100f;
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-// VEC, in all that follows: rows are whole aligned groups of 8 channels, and no
-// group of the norm ends inside four of them.  Four channels are then a unit with
-// one set of statistics; elsewhere every channel is its own.
+// VEC, in all that follows: rows are whole aligned groups of four channels, up to
+// 256 of them, and no group of the norm ends inside four.  A lane then holds four
+// channels (a load instruction of a wave is one contiguous piece for every type;
+// eight channels of float32 take two that each touch every line: 53 us instead of
+// 44 for the second pass over 262,144 x 128), with one set of statistics.
+// Elsewhere it holds eight, every channel with its own.
 template <bool VEC>
-constexpr int UNIT = VEC ? 4 : 1;
+constexpr int CPL = VEC ? 4 : 8;    // channels per lane
+template <bool VEC>
+constexpr int UNIT = VEC ? 4 : 1;   // channels with the same statistics
 
 // Rows a lane has in flight in the forward passes, and in the backward ones,
 // which hold twice the values of each (fewer where loads have branches).
 template <bool VEC>
-constexpr int FWD_TILE = VEC ? 4 : 2;
+constexpr int FWD_TILE = VEC ? 8 : 2;
 template <bool VEC>
-constexpr int BWD_TILE = VEC ? 2 : 1;
+constexpr int BWD_TILE = VEC ? 4 : 1;
 
 struct Q8 {};   // tag: a checkpoint as the source of values
 
@@ -85,194 +94,280 @@ struct NormArgs {
   int accumulate, nchunks, nred;
 };
 
-// ------------------------------------------------------------ eight channels
+// ------------------------------------------------------------ rows and lanes
 
-// cnt: channels of this lane that exist (8, fewer in a last lane, none past it).
-// VEC: rows are whole aligned groups of 8; a lane past the row reads the
-// row's first group and drops it (a load under a condition would make the
-// compiler wait for everything in flight).
+// The place of a lane: CPL channels from c0 (cnt of them exist) in row rl of the
+// RL rows that a workgroup steps over.
 template <bool VEC>
-__device__ __forceinline__ void words4(const void* p, uint32_t (&w)[4]) {
-  if (VEC) {
+struct Lanes {
+  int lpr, lr, rl, RL, c0, cnt;
+  __device__ __forceinline__ Lanes(int lg, int C, int threads) {
+    lpr = 1 << lg;
+    lr = threadIdx.x & (lpr - 1);
+    rl = threadIdx.x >> lg;
+    RL = threads >> lg;
+    c0 = lr * CPL<VEC>;
+    cnt = std::min(CPL<VEC>, C - c0);
+  }
+  // Where the lane reads.  With whole groups a lane past the row takes the row's
+  // last channels once more (no sum counts them, and a block's largest is the
+  // same): a condition would become a branch around the load, and a wait.
+  __device__ __forceinline__ int at(int C) const { return VEC ? std::min(c0, C - CPL<VEC>) : c0; }
+};
+
+// Rows of a matrix.  Row i + at, where i is the same for all lanes (scalar
+// registers) and `at` the lane's own, small enough for 24-bit products and
+// 32-bit offsets.
+template <typename T>
+struct Mat {
+  const char* p;
+  int64_t pitch;
+  uint32_t off;
+  __device__ __forceinline__ Mat(const void* base, int64_t ld, int c)
+      : p(static_cast<const char*>(base)), pitch(ld * (int64_t)sizeof(T)), off((uint32_t)c * (uint32_t)sizeof(T)) {}
+  __device__ __forceinline__ T* row(int64_t i, int at) const {
+    return reinterpret_cast<T*>(const_cast<char*>(p + i * pitch) + (__umul24((uint32_t)at, (uint32_t)pitch) + off));
+  }
+};
+
+// The rows of a tile: N steps of RL rows, of which the first `left` exist.  Reads
+// take the last row again past it (all loads of a tile go out together, whatever
+// exists); what they bring is not used.
+template <int N>
+struct Tile {
+  int left, at[N];
+  bool ok[N];
+  template <typename LANES>
+  __device__ __forceinline__ Tile(const LANES& L, int left_) : left(left_) {
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+      const int r = L.rl + t * L.RL;
+      ok[t] = r < left;
+      at[t] = std::min(r, left - 1);
+    }
+  }
+};
+
+// tile(i, rows of it) over the rows [r, e)
+template <int N, typename LANES, typename F>
+__device__ __forceinline__ void over_rows(const LANES& L, int64_t r, int64_t e, F tile) {
+  for (int64_t i = r; i < e; i += N * L.RL) tile(i, Tile<N>(L, (int)std::min<int64_t>(e - i, N * L.RL)));
+}
+
+// N four-byte words from or to any address, or whole aligned ones (VEC)
+template <bool VEC, int N>
+__device__ __forceinline__ void get_words(const void* p, uint32_t (&w)[N]) {
+  if (VEC && N == 4) {
     const uint4 u = *static_cast<const uint4*>(p);
-    w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+    w[0] = u.x, w[1] = u.y, w[2 % N] = u.z, w[3 % N] = u.w;
+  } else if (VEC && N == 2) {
+    const uint2 u = *static_cast<const uint2*>(p);
+    w[0] = u.x, w[1 % N] = u.y;
+  } else if (VEC) {
+    w[0] = *static_cast<const uint32_t*>(p);
   } else {
-    __builtin_memcpy(w, p, 16);   // one load of any alignment
+    __builtin_memcpy(w, p, 4 * N);
   }
 }
+template <bool VEC, int N>
+__device__ __forceinline__ void put_words(void* p, const uint32_t (&w)[N]) {
+  if (VEC && N == 4)
+    *static_cast<uint4*>(p) = make_uint4(w[0], w[1 % N], w[2 % N], w[3 % N]);
+  else if (VEC && N == 2)
+    *static_cast<uint2*>(p) = make_uint2(w[0], w[1 % N]);
+  else if (VEC)
+    *static_cast<uint32_t*>(p) = w[0];
+  else
+    __builtin_memcpy(p, w, 4 * N);
+}
 
-template <typename T, bool VEC>
-struct Row;
-
+// cnt: how many of a lane's channels exist (all, fewer in a last lane, none or
+// less past it); not looked at in loads where VEC.
 template <bool VEC>
-struct Row<float, VEC> {
-  static __device__ __forceinline__ void load(const float* row, int c0, int cnt, float (&v)[8]) {
-    if (VEC || cnt == 8) {
-      const float* p = row + (cnt > 0 ? c0 : 0);
-      uint32_t w[4], u[4];
-      words4<VEC>(p, w);
-      words4<VEC>(p + 4, u);
+__device__ __forceinline__ void load_row(const float* p, int cnt, float (&v)[CPL<VEC>]) {
+  if (VEC || cnt == CPL<VEC>) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        v[k] = cnt > 0 ? __builtin_bit_cast(float, w[k]) : 0.0f;
-        v[4 + k] = cnt > 0 ? __builtin_bit_cast(float, u[k]) : 0.0f;
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = k < cnt ? row[c0 + k] : 0.0f;
-    }
-  }
-  static __device__ __forceinline__ void store(float* row, int c0, int cnt, const float (&v)[8]) {
-    if (VEC || cnt == 8) {
-      if (cnt <= 0) return;
-      float* p = row + c0;
-      if (VEC) {
-        reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-      } else {
-        __builtin_memcpy(p, &v[0], 16);
-        __builtin_memcpy(p + 4, &v[4], 16);
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (k < cnt) row[c0 + k] = v[k];
-    }
-  }
-};
-
-template <bool VEC>
-struct Row<__bf16, VEC> {
-  static __device__ __forceinline__ void load(const __bf16* row, int c0, int cnt, float (&v)[8]) {
-    if (VEC || cnt == 8) {
+    for (int j = 0; j < CPL<VEC>; j += 4) {
       uint32_t w[4];
-      const __bf16* p = row + (cnt > 0 ? c0 : 0);
-      words4<VEC>(p, w);
+      get_words<VEC>(p + j, w);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        v[2 * k] = cnt > 0 ? __builtin_bit_cast(float, w[k] << 16) : 0.0f;
-        v[2 * k + 1] = cnt > 0 ? __builtin_bit_cast(float, w[k] & 0xffff0000u) : 0.0f;
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = k < cnt ? (float)row[c0 + k] : 0.0f;
-    }
-  }
-  static __device__ __forceinline__ void store(__bf16* row, int c0, int cnt, const float (&v)[8]) {
-    if (VEC || cnt == 8) {
-      if (cnt <= 0) return;
-      uint32_t w[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){v[2 * k], v[2 * k + 1]}, bf16x2));
-      __bf16* p = row + c0;
-      if (VEC)
-        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-      else
-        __builtin_memcpy(p, w, 16);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (k < cnt) row[c0 + k] = (__bf16)v[k];
-    }
-  }
-};
-
-// The eight bytes of a checkpoint row, times their block's scale.
-template <bool VEC>
-__device__ __forceinline__ void load_q8(const int8_t* row, const float* scale_row, int c0, int cnt, float (&v)[8]) {
-  const int at = cnt > 0 ? c0 : 0;
-  const float s = scale_row[at / BLOCK_C];
-  if (VEC || cnt == 8) {
-    uint32_t w[2];
-    if (VEC) {
-      const uint2 u = *reinterpret_cast<const uint2*>(row + at);
-      w[0] = u.x, w[1] = u.y;
-    } else {
-      __builtin_memcpy(w, row + at, 8);
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int32_t b = (int32_t)(w[k / 4] << (24 - 8 * (k % 4))) >> 24;
-      v[k] = cnt > 0 ? (float)b * s : 0.0f;
+      for (int k = 0; k < 4; ++k) v[j + k] = __builtin_bit_cast(float, w[k]);
     }
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = k < cnt ? (float)row[c0 + k] * s : 0.0f;
+    for (int k = 0; k < CPL<VEC>; ++k) v[k] = k < cnt ? p[k] : 0.0f;
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void load_row(const __bf16* p, int cnt, float (&v)[CPL<VEC>]) {
+  if (VEC || cnt == CPL<VEC>) {
+    uint32_t w[CPL<VEC> / 2];
+    get_words<VEC>(p, w);
+#pragma unroll
+    for (int k = 0; k < CPL<VEC> / 2; ++k) {
+      v[2 * k] = __builtin_bit_cast(float, w[k] << 16);
+      v[2 * k + 1] = __builtin_bit_cast(float, w[k] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < CPL<VEC>; ++k) v[k] = k < cnt ? (float)p[k] : 0.0f;
+  }
+}
+// bytes of a checkpoint times their block's scale
+template <bool VEC>
+__device__ __forceinline__ void load_row(const int8_t* p, float scale, int cnt, float (&v)[CPL<VEC>]) {
+  if (VEC || cnt == CPL<VEC>) {
+    uint32_t w[CPL<VEC> / 4];
+    get_words<VEC>(p, w);
+#pragma unroll
+    for (int k = 0; k < CPL<VEC>; ++k) v[k] = (float)((int32_t)(w[k / 4] << (24 - 8 * (k % 4))) >> 24) * scale;
+  } else {
+#pragma unroll
+    for (int k = 0; k < CPL<VEC>; ++k) v[k] = k < cnt ? (float)p[k] * scale : 0.0f;
   }
 }
 
-// Row r of the source, whatever it is.
+template <bool VEC>
+__device__ __forceinline__ void store_row(float* p, int cnt, const float (&v)[CPL<VEC>]) {
+  if (cnt == CPL<VEC>) {
+#pragma unroll
+    for (int j = 0; j < CPL<VEC>; j += 4) {
+      uint32_t w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = __builtin_bit_cast(uint32_t, v[j + k]);
+      put_words<VEC>(p + j, w);
+    }
+  } else if (!VEC) {
+#pragma unroll
+    for (int k = 0; k < CPL<VEC>; ++k)
+      if (k < cnt) p[k] = v[k];
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void store_row(__bf16* p, int cnt, const float (&v)[CPL<VEC>]) {
+  if (cnt == CPL<VEC>) {
+    uint32_t w[CPL<VEC> / 2];
+#pragma unroll
+    for (int k = 0; k < CPL<VEC> / 2; ++k)
+      w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){v[2 * k], v[2 * k + 1]}, bf16x2));
+    put_words<VEC>(p, w);
+  } else if (!VEC) {
+#pragma unroll
+    for (int k = 0; k < CPL<VEC>; ++k)
+      if (k < cnt) p[k] = (__bf16)v[k];
+  }
+}
+
+__host__ __device__ __forceinline__ int blocks_of(int C) { return (C + BLOCK_C - 1) / BLOCK_C; }
+
+// The values that are normalised: rows of T, or of a checkpoint.
 template <typename T, bool VEC>
 struct Source {
-  static __device__ __forceinline__ void load(const NormArgs& a, int64_t r, int c0, int cnt, float (&v)[8]) {
-    Row<T, VEC>::load(static_cast<const T*>(a.x) + r * a.ldx, c0, cnt, v);
+  Mat<T> m;
+  int cnt;
+  __device__ __forceinline__ Source(const NormArgs& a, const Lanes<VEC>& L) : m(a.x, a.ldx, L.at(a.C)), cnt(L.cnt) {}
+  __device__ __forceinline__ void load(int64_t i, int at, float (&v)[CPL<VEC>]) const {
+    load_row<VEC>(m.row(i, at), cnt, v);
   }
 };
 template <bool VEC>
 struct Source<Q8, VEC> {
-  static __device__ __forceinline__ void load(const NormArgs& a, int64_t r, int c0, int cnt, float (&v)[8]) {
-    load_q8<VEC>(static_cast<const int8_t*>(a.x) + r * a.C, a.xscale + r * ((a.C + BLOCK_C - 1) / BLOCK_C), c0, cnt,
-                 v);
+  Mat<int8_t> m;
+  Mat<float> s;
+  int cnt;
+  __device__ __forceinline__ Source(const NormArgs& a, const Lanes<VEC>& L)
+      : m(a.x, a.C, L.at(a.C)),
+        s(a.xscale, blocks_of(a.C), std::min(L.at(a.C), a.C - 1) / BLOCK_C), cnt(L.cnt) {}
+  __device__ __forceinline__ void load(int64_t i, int at, float (&v)[CPL<VEC>]) const {
+    load_row<VEC>(m.row(i, at), *s.row(i, at), cnt, v);
   }
 };
 
-// Quantises a lane's eight values of a block of 64 channels (8 lanes; `width`
-// of them where the row has fewer) and writes them and the block's scale.  The
-// largest magnitude is found on the bits without the sign, which order as the
-// values do and put a NaN above everything.
-template <bool VEC>
-__device__ __forceinline__ void store_q8(int8_t* q, float* scale, int64_t r, int C, int c0, int cnt, int width,
-                                         const float (&v)[8]) {
-  uint32_t m = 0;
+// t = x, or x + addend rounded to T, which is then written to sum.
+template <typename T, bool VEC, bool ADD>
+struct Stream {
+  Source<T, VEC> x;
+  Mat<T> add, sum;
+  int cnt;
+  __device__ __forceinline__ Stream(const NormArgs& a, const Lanes<VEC>& L)
+      : x(a, L), add(a.add, a.lda, L.at(a.C)), sum(a.sum, a.lds, L.c0), cnt(L.cnt) {}
+  template <int N>
+  __device__ __forceinline__ void load(int64_t i, const Tile<N>& rows, float (&v)[N][CPL<VEC>]) const {
+    float u[N][CPL<VEC>];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) m = max(m, __builtin_bit_cast(uint32_t, v[k]) & 0x7fffffffu);
-  for (int o = 1; o < width; o <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
-  const float big = __builtin_bit_cast(float, m);
-  const bool some = m >= __builtin_bit_cast(uint32_t, TINY), odd = m >= 0x7f800000u;
-  const float inv = some && !odd ? 127.0f / big : 0.0f;
-  const float s = odd ? __builtin_bit_cast(float, 0x7fc00000u) : some ? big * (1.0f / 127.0f) : 0.0f;
-  if (cnt <= 0) return;
-  int b[8];
+    for (int t = 0; t < N; ++t) {
+      x.load(i, rows.at[t], v[t]);
+      if (ADD) load_row<VEC>(add.row(i, rows.at[t]), cnt, u[t]);
+    }
+    if (ADD) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const float t = odd ? 0.0f : __builtin_rintf(v[k] * inv);
-    b[k] = (int)fminf(fmaxf(t, -127.0f), 127.0f);
+      for (int t = 0; t < N; ++t) {
+#pragma unroll
+        for (int k = 0; k < CPL<VEC>; ++k) v[t][k] = (float)(T)(v[t][k] + u[t][k]);
+        if (rows.ok[t]) store_row<VEC>(sum.row(i, rows.at[t]), cnt, v[t]);
+      }
+    }
   }
-  int8_t* p = q + r * C + c0;
-  if (VEC || cnt == 8) {
-    uint32_t w[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      w[i] = (b[4 * i] & 255) | (b[4 * i + 1] & 255) << 8 | (b[4 * i + 2] & 255) << 16 | (uint32_t)b[4 * i + 3] << 24;
-    if (VEC)
-      *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-    else
-      __builtin_memcpy(p, w, 8);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (k < cnt) p[k] = (int8_t)b[k];
-  }
-  if (c0 % BLOCK_C == 0) scale[r * ((C + BLOCK_C - 1) / BLOCK_C) + c0 / BLOCK_C] = s;
-}
+};
 
-// t = x, or x + addend rounded to T, of rows i, i + step, ...
-template <typename T, bool VEC, bool ADD, int N>
-__device__ __forceinline__ void take_rows(const NormArgs& a, int64_t i, int step, int c0, int cnt, float (&v)[N][8]) {
-  float u[N][8];
-#pragma unroll
-  for (int t = 0; t < N; ++t) {
-    Source<T, VEC>::load(a, i + t * step, c0, cnt, v[t]);
-    if (ADD) Row<T, VEC>::load(static_cast<const T*>(a.add) + (i + t * step) * a.lda, c0, cnt, u[t]);
+// Where y goes, of either type.
+template <bool VEC>
+struct Result {
+  Mat<float> f;
+  Mat<__bf16> b;
+  int cnt, bf16;
+  __device__ __forceinline__ Result(const NormArgs& a, const Lanes<VEC>& L)
+      : f(a.y, a.ldy, L.c0), b(a.y, a.ldy, L.c0), cnt(L.cnt), bf16(a.y_bf16) {}
+  __device__ __forceinline__ void store(int64_t i, int at, const float (&v)[CPL<VEC>]) const {
+    if (bf16)
+      store_row<VEC>(b.row(i, at), cnt, v);
+    else
+      store_row<VEC>(f.row(i, at), cnt, v);
   }
-  if (ADD) {
+};
+
+// Writes rows in 8 bits.  64 / CPL lanes (fewer where a row has fewer) hold a block
+// of 64 channels.  Its largest magnitude is found on the bits without the sign,
+// which order as the values do and put a NaN above everything.
+template <bool VEC>
+struct Keep {
+  Mat<int8_t> q;
+  Mat<float> s;
+  int cnt, width, first;
+  __device__ __forceinline__ Keep(const NormArgs& a, const Lanes<VEC>& L)
+      : q(a.q, a.C, L.c0), s(a.scale, blocks_of(a.C), L.c0 / BLOCK_C), cnt(L.cnt),
+        width(std::min(BLOCK_C / CPL<VEC>, L.lpr)), first(L.c0 % BLOCK_C == 0) {}
+  __device__ __forceinline__ void store(int64_t i, int at, bool ok, const float (&v)[CPL<VEC>]) const {
+    uint32_t m = 0;
 #pragma unroll
-    for (int t = 0; t < N; ++t)
+    for (int k = 0; k < CPL<VEC>; ++k) m = max(m, __builtin_bit_cast(uint32_t, v[k]) & 0x7fffffffu);
+    for (int o = 1; o < width; o <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+    const float big = __builtin_bit_cast(float, m);
+    const bool some = m >= __builtin_bit_cast(uint32_t, TINY), odd = m >= 0x7f800000u;
+    const float inv = some && !odd ? 127.0f / big : 0.0f;
+    const float scale = odd ? __builtin_bit_cast(float, 0x7fc00000u) : some ? big * (1.0f / 127.0f) : 0.0f;
+    if (cnt <= 0 || !ok) return;
+    int b[CPL<VEC>];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[t][k] = (float)(T)(v[t][k] + u[t][k]);
+    for (int k = 0; k < CPL<VEC>; ++k) {
+      const float t = odd ? 0.0f : __builtin_rintf(v[k] * inv);
+      b[k] = (int)fminf(fmaxf(t, -127.0f), 127.0f);
+    }
+    int8_t* p = q.row(i, at);
+    if (cnt == CPL<VEC>) {
+      uint32_t w[CPL<VEC> / 4];
+#pragma unroll
+      for (int j = 0; j < CPL<VEC> / 4; ++j)
+        w[j] = (b[4 * j] & 255) | (b[4 * j + 1] & 255) << 8 | (b[4 * j + 2] & 255) << 16 | (uint32_t)b[4 * j + 3] << 24;
+      put_words<VEC>(p, w);
+    } else if (!VEC) {
+#pragma unroll
+      for (int k = 0; k < CPL<VEC>; ++k)
+        if (k < cnt) p[k] = (int8_t)b[k];
+    }
+    if (first) *s.row(i, at) = scale;
   }
-}
+};
 
 // ------------------------------------------------------------ activations
 
@@ -346,25 +441,13 @@ __device__ __forceinline__ int seg_find(const NormArgs& a, int64_t r) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
-struct Lanes {
-  int lpr, lr, rl, RL, c0, cnt;
-  __device__ __forceinline__ Lanes(int lg, int C, int threads) {
-    lpr = 1 << lg;
-    lr = threadIdx.x & (lpr - 1);
-    rl = threadIdx.x >> lg;
-    RL = threads >> lg;
-    c0 = lr * 8;
-    cnt = std::min(8, C - c0);
-  }
-};
-
 // s1, s2: the workgroup's sums per channel (or unit of channels), float64 in LDS.
 // Gives the sums over each group's gs of them to out(g, sum1, sum2), by one lane each.
-template <typename F>
+template <int W, typename F>
 __device__ __forceinline__ void group_sums(const double* s1, const double* s2, int G, int gs, F out) {
   int tg = 1;   // lanes of a group
-  while (tg < 64 && tg * 2 * G <= NT && tg < gs) tg <<= 1;
-  const int per = NT / tg;
+  while (tg < 64 && tg * 2 * G <= W * 64 && tg < gs) tg <<= 1;
+  const int per = W * 64 / tg;
   for (int gb = 0; gb < G; gb += per) {
     const int g = gb + (int)threadIdx.x / tg, l = threadIdx.x % tg;
     double u = 0.0, v = 0.0;
@@ -377,18 +460,10 @@ __device__ __forceinline__ void group_sums(const double* s1, const double* s2, i
 
 // ------------------------------------------------------------ per lane
 
-template <bool VEC>
-__device__ __forceinline__ void store_y(const NormArgs& a, int64_t r, const Lanes& L, const float (&v)[8]) {
-  if (a.y_bf16)
-    Row<__bf16, VEC>::store(static_cast<__bf16*>(a.y) + r * a.ldy, L.c0, L.cnt, v);
-  else
-    Row<float, VEC>::store(static_cast<float*>(a.y) + r * a.ldy, L.c0, L.cnt, v);
-}
-
-// A value for each of a lane's eight channels that is the same within a unit.
+// A value for each of a lane's channels that is the same within a unit.
 template <bool VEC>
 struct PerUnit {
-  static constexpr int N = 8 / UNIT<VEC>;
+  static constexpr int N = CPL<VEC> / UNIT<VEC>;
   float v[N];
   __device__ __forceinline__ float operator[](int k) const { return v[k / UNIT<VEC>]; }
 };
@@ -412,13 +487,13 @@ struct Groups {
 };
 
 template <bool VEC>
-__device__ __forceinline__ void params8(const NormArgs& a, const Lanes& L, float (&gamma)[8], float (&beta)[8]) {
+__device__ __forceinline__ void params(const NormArgs& a, const Lanes<VEC>& L, float (&gamma)[CPL<VEC>], float (&beta)[CPL<VEC>]) {
   if (a.gamma) {
-    Row<float, VEC>::load(a.gamma, L.c0, L.cnt, gamma);
-    Row<float, VEC>::load(a.beta, L.c0, L.cnt, beta);
+    load_row<VEC>(a.gamma + L.at(a.C), L.cnt, gamma);
+    load_row<VEC>(a.beta + L.at(a.C), L.cnt, beta);
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) gamma[k] = 1.0f, beta[k] = 0.0f;
+    for (int k = 0; k < CPL<VEC>; ++k) gamma[k] = 1.0f, beta[k] = 0.0f;
   }
 }
 
@@ -433,11 +508,11 @@ __device__ __forceinline__ float2* stats_of(const NormArgs& a, int s) {
 // of Chan, Golub and LeVeque), so a large mean or a far-out row costs no digits.
 template <bool VEC>
 struct Moments {
-  static constexpr int U = UNIT<VEC>, N = 8 / U;
+  static constexpr int U = UNIT<VEC>, N = CPL<VEC> / U;
   float n = 0.0f, mean[N] = {}, m2[N] = {};
 
   template <int T>
-  __device__ __forceinline__ void add(const float (&v)[T][8]) {
+  __device__ __forceinline__ void add(const float (&v)[T][CPL<VEC>]) {
     const float nn = n + T, w = T / nn, f = n * w * U;
     n = nn;
 #pragma unroll
@@ -457,6 +532,35 @@ struct Moments {
       m2[j] += __builtin_fmaf(d * d, f, q);
     }
   }
+  // the same where a lane has fewer than T rows
+  template <int T>
+  __device__ __forceinline__ void add(const float (&v)[T][CPL<VEC>], const bool (&ok)[T]) {
+    float c = 0.0f;
+#pragma unroll
+    for (int t = 0; t < T; ++t) c += ok[t] ? 1.0f : 0.0f;
+    if (c == 0.0f) return;
+    const float nn = n + c, w = c / nn, f = n * w * U, inv = 1.0f / (c * U);
+    n = nn;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      float s = 0.0f, q = 0.0f;
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int k = 0; k < U; ++k) s += ok[t] ? v[t][j * U + k] : 0.0f;
+      const float m = s * inv;
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          const float d = ok[t] ? v[t][j * U + k] - m : 0.0f;
+          q = __builtin_fmaf(d, d, q);
+        }
+      const float d = m - mean[j];
+      mean[j] = __builtin_fmaf(d, w, mean[j]);
+      m2[j] += __builtin_fmaf(d * d, f, q);
+    }
+  }
   // joins the lane `o` away
   __device__ __forceinline__ void join(int o) {
     const float nb = __shfl_xor(n, o, 64), nn = n + nb, w = nn > 0.0f ? nb / nn : 0.0f, f = n * w * U;
@@ -470,65 +574,67 @@ struct Moments {
   }
 };
 
-// Dynamic LDS of the summing passes: two float64 per channel, two floats per
-// wave and channel, a count per wave.
-size_t sums_lds(int lg, int C) { return (size_t)NW * (16 << lg) * 4 + NW * 4 + 16 * (size_t)C; }
+// LDS of the summing passes on W waves: two float64 per channel, two floats per
+// wave and channel, a count per wave.  Sixteen waves take rows of at most 256
+// channels.  (Row distances known to the compiler: as variables they cost 16
+// addresses, kept in registers throughout.)
+template <int W>
+struct SumsLds {
+  static constexpr int C = W == NW ? MAX_C : MAX_C / 2;
+  double s1[C], s2[C];
+  float u[W * C], v[W * C], n[W];
+};
 
 // The workgroup's sums over rows [r, e) for every group: the mean-weighted count and
 // the squares about zero in float64, to out(g, u, v).  Adds the addend and
 // writes the sum and the checkpoint on the way.
-template <typename T, bool VEC, bool ADD, typename OUT>
-__device__ __forceinline__ void moments_of(const NormArgs& a, const Lanes& L, int64_t r, int64_t e, double* sh, OUT out) {
-  constexpr int U = UNIT<VEC>, N = 8 / U, TILE = FWD_TILE<VEC>;
-  const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63, wu = L.lpr * N, units = a.C / U;
-  double *s1 = sh, *s2 = sh + units;
-  float *mm = reinterpret_cast<float*>(s2 + units), *qq = mm + NW * wu, *nn = qq + NW * wu;
+template <int W, typename T, bool VEC, bool ADD, typename OUT>
+__device__ __forceinline__ void moments_of(const NormArgs& a, const Lanes<VEC>& L, int64_t r, int64_t e, SumsLds<W>& sh, OUT out) {
+  constexpr int U = UNIT<VEC>, N = CPL<VEC> / U, TILE = FWD_TILE<VEC>, wu = SumsLds<W>::C / U;
+  const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63, units = a.C / U;
   Moments<VEC> m;
-  auto keep = [&](int64_t row, const float(&v)[8]) {
-    if (ADD) Row<T, VEC>::store(static_cast<T*>(a.sum) + row * a.lds, L.c0, L.cnt, v);
-    if (a.ck) store_q8<VEC>(a.q, a.scale, row, a.C, L.c0, L.cnt, std::min(8, L.lpr), v);
-  };
-  int64_t i = r + L.rl;
-  for (; i + (TILE - 1) * L.RL < e; i += TILE * L.RL) {
-    float v[TILE][8];
-    take_rows<T, VEC, ADD, TILE>(a, i, L.RL, L.c0, L.cnt, v);
+  const Stream<T, VEC, ADD> in(a, L);
+  const Keep<VEC> keep(a, L);
+  over_rows<TILE>(L, r, e, [&](int64_t i, const Tile<TILE>& rows) {
+    float v[TILE][CPL<VEC>];
+    in.load(i, rows, v);
+    if (a.ck) {
 #pragma unroll
-    for (int t = 0; t < TILE; ++t) keep(i + t * L.RL, v[t]);
-    m.template add<TILE>(v);
-  }
-  for (; i < e; i += L.RL) {
-    float v[1][8];
-    take_rows<T, VEC, ADD, 1>(a, i, L.RL, L.c0, L.cnt, v);
-    keep(i, v[0]);
-    m.template add<1>(v);
-  }
+      for (int t = 0; t < TILE; ++t)
+        if (t * L.RL < rows.left) keep.store(i, rows.at[t], rows.ok[t], v[t]);
+    }
+    if (rows.left == TILE * L.RL)
+      m.add(v);
+    else
+      m.add(v, rows.ok);
+  });
   for (int o = L.lpr; o < 64; o <<= 1) m.join(o);
   if (lane < L.lpr) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) mm[wid * wu + L.lr * N + j] = m.mean[j], qq[wid * wu + L.lr * N + j] = m.m2[j];
-    if (lane == 0) nn[wid] = m.n;
+    for (int j = 0; j < N; ++j) sh.u[wid * wu + L.lr * N + j] = m.mean[j], sh.v[wid * wu + L.lr * N + j] = m.m2[j];
+    if (lane == 0) sh.n[wid] = m.n;
   }
   __syncthreads();
   const int c = threadIdx.x;
   if (c < units) {
     double u = 0.0, v = 0.0;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const double mw = mm[w * wu + c], nw = (double)(nn[w] * U);
+    for (int w = 0; w < W; ++w) {
+      const double mw = sh.u[w * wu + c], nw = (double)(sh.n[w] * U);
       u += nw * mw;
-      v += (double)qq[w * wu + c] + nw * mw * mw;
+      v += (double)sh.v[w * wu + c] + nw * mw * mw;
     }
-    s1[c] = u;
-    s2[c] = v;
+    sh.s1[c] = u;
+    sh.s2[c] = v;
   }
   __syncthreads();
-  group_sums(s1, s2, a.G, a.gs / U, out);
+  group_sums<W>(sh.s1, sh.s2, a.G, a.gs / U, out);
 }
 
 template <typename T, bool VEC, bool ADD>
-__global__ __launch_bounds__(NT) void k_norm_stats(NormArgs a) {
-  extern __shared__ double sh[];
-  const Lanes L(a.lg, a.C, NT);
+__global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_stats(NormArgs a) {
+  __shared__ SumsLds<NW> sh;
+  const Lanes<VEC> L(a.lg, a.C, NT);
   const int64_t r0 = (int64_t)blockIdx.x * a.R, r1 = std::min<int64_t>(r0 + a.R, a.n);
   int s = seg_find(a, r0);
   for (int64_t r = r0; r < r1; ++s) {
@@ -536,7 +642,7 @@ __global__ __launch_bounds__(NT) void k_norm_stats(NormArgs a) {
     if (e <= r) continue;
     const double inv = 1.0 / ((double)(e - r) * a.gs);
     float2* part = a.part + ((int64_t)blockIdx.x + s) * a.G;
-    moments_of<T, VEC, ADD>(a, L, r, e, sh, [&](int g, double u, double v) {
+    moments_of<NW, T, VEC, ADD>(a, L, r, e, sh, [&](int g, double u, double v) {
       const double mean = u * inv;
       part[g] = make_float2((float)mean, (float)fmax(v - u * mean, 0.0));
     });
@@ -599,41 +705,37 @@ __device__ __forceinline__ void join_pieces(const NormArgs& a, int s, int64_t b,
 
 // y of rows [r, end) from their groups' mean and rstd.
 template <typename T, bool VEC, int ACT>
-__device__ __forceinline__ void apply_rows(const NormArgs& a, const Lanes& L, int64_t r, int64_t end,
-                                           const PerUnit<VEC>& mean, const PerUnit<VEC>& rstd, const float (&gamma)[8],
-                                           const float (&beta)[8]) {
+__device__ __forceinline__ void apply_rows(const NormArgs& a, const Lanes<VEC>& L, int64_t r, int64_t end,
+                                           const PerUnit<VEC>& mean, const PerUnit<VEC>& rstd, const float (&gamma)[CPL<VEC>],
+                                           const float (&beta)[CPL<VEC>]) {
   constexpr int TILE = FWD_TILE<VEC>;
-  float scale[8];
+  const Source<T, VEC> in(a, L);
+  const Result<VEC> out(a, L);
+  float scale[CPL<VEC>];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) scale[k] = rstd[k] * gamma[k];
-  auto put = [&](int64_t row, float(&v)[8]) {
+  for (int k = 0; k < CPL<VEC>; ++k) scale[k] = rstd[k] * gamma[k];
+  over_rows<TILE>(L, r, end, [&](int64_t i, const Tile<TILE>& rows) {
+    float v[TILE][CPL<VEC>];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = activate<ACT>(__builtin_fmaf(v[k] - mean[k], scale[k], beta[k]));
-    store_y<VEC>(a, row, L, v);
-  };
-  int64_t i = r + L.rl;
-  for (; i + (TILE - 1) * L.RL < end; i += TILE * L.RL) {
-    float v[TILE][8];
+    for (int t = 0; t < TILE; ++t) in.load(i, rows.at[t], v[t]);
 #pragma unroll
-    for (int t = 0; t < TILE; ++t) Source<T, VEC>::load(a, i + t * L.RL, L.c0, L.cnt, v[t]);
+    for (int t = 0; t < TILE; ++t) {
+      if (t * L.RL >= rows.left) break;
 #pragma unroll
-    for (int t = 0; t < TILE; ++t) put(i + t * L.RL, v[t]);
-  }
-  for (; i < end; i += L.RL) {
-    float v[8];
-    Source<T, VEC>::load(a, i, L.c0, L.cnt, v);
-    put(i, v);
-  }
+      for (int k = 0; k < CPL<VEC>; ++k) v[t][k] = activate<ACT>(__builtin_fmaf(v[t][k] - mean[k], scale[k], beta[k]));
+      if (rows.ok[t]) out.store(i, rows.at[t], v[t]);
+    }
+  });
 }
 
 // y = act((t - mean) * (rstd gamma) + beta) on this workgroup's rows, segment by
 // segment.  a.merge: the statistics come from the first pass's pieces (and are
 // written, by the workgroup that has the segment's first row), else from a.stats.
 template <typename T, bool VEC, int ACT>
-__global__ __launch_bounds__(NT) void k_norm_apply(NormArgs a) {
+__global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_apply(NormArgs a) {
   __shared__ double sh[2 * NT];
   __shared__ float2 st[MAX_C];
-  const Lanes L(a.lg, a.C, NT);
+  const Lanes<VEC> L(a.lg, a.C, NT);
   const int64_t r0 = (int64_t)blockIdx.x * a.RA, r1 = std::min<int64_t>(r0 + a.RA, a.n);
   if (a.merge && blockIdx.x == 0) {
     for (int s = threadIdx.x; s < a.n_seg; s += NT)
@@ -642,8 +744,8 @@ __global__ __launch_bounds__(NT) void k_norm_apply(NormArgs a) {
   }
   if (r0 >= r1) return;
   const Groups<VEC> groups(a, L.c0);
-  float gamma[8], beta[8];
-  params8<VEC>(a, L, gamma, beta);
+  float gamma[CPL<VEC>], beta[CPL<VEC>];
+  params<VEC>(a, L, gamma, beta);
   int s = seg_find(a, r0);
   for (int64_t r = r0; r < r1; ++s) {
     const int64_t b = seg_begin(a, s), e = seg_end(a, s), end = std::min<int64_t>(e, r1);
@@ -674,21 +776,21 @@ __global__ __launch_bounds__(NT) void k_norm_apply(NormArgs a) {
 
 // One workgroup to a segment: both passes in one launch.
 template <typename T, bool VEC, bool ADD, int ACT>
-__global__ __launch_bounds__(NT) void k_norm_small(NormArgs a) {
-  extern __shared__ double sh[];
+__global__ __launch_bounds__(SNT) void k_norm_small(NormArgs a) {
+  __shared__ SumsLds<SNW> sh;
   __shared__ float2 st[MAX_C];
-  const Lanes L(a.lg, a.C, NT);
+  const Lanes<VEC> L(a.lg, a.C, SNT);
   const int s = blockIdx.x;
   const int64_t b = seg_begin(a, s), e = seg_end(a, s);
   if (e <= b) {
-    for (int g = threadIdx.x; g < a.G; g += NT) stats_of(a, s)[g] = make_float2(0.0f, 0.0f);
+    for (int g = threadIdx.x; g < a.G; g += SNT) stats_of(a, s)[g] = make_float2(0.0f, 0.0f);
     return;
   }
   const Groups<VEC> groups(a, L.c0);
-  float gamma[8], beta[8];
-  params8<VEC>(a, L, gamma, beta);
+  float gamma[CPL<VEC>], beta[CPL<VEC>];
+  params<VEC>(a, L, gamma, beta);
   const double inv = 1.0 / ((double)(e - b) * a.gs);
-  moments_of<T, VEC, ADD>(a, L, b, e, sh, [&](int g, double u, double v) {
+  moments_of<SNW, T, VEC, ADD>(a, L, b, e, sh, [&](int g, double u, double v) {
     st[g] = finish(u, v, inv, a.eps);
     stats_of(a, s)[g] = st[g];
   });
@@ -705,12 +807,12 @@ __global__ __launch_bounds__(NT) void k_norm_small(NormArgs a) {
 template <bool VEC>
 struct Norm {
   PerUnit<VEC> mean, rstd;
-  float gamma[8], beta[8];
+  float gamma[CPL<VEC>], beta[CPL<VEC>];
   // of one row: w = grad_y act'(z) in place of grad_y, xn in place of t
   template <int ACT>
-  __device__ __forceinline__ void weigh(float (&t)[8], float (&w)[8]) const {
+  __device__ __forceinline__ void weigh(float (&t)[CPL<VEC>], float (&w)[CPL<VEC>]) const {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < CPL<VEC>; ++k) {
       t[k] = (t[k] - mean[k]) * rstd[k];
       w[k] *= slope<ACT>(__builtin_fmaf(t[k], gamma[k], beta[k]));
     }
@@ -719,67 +821,62 @@ struct Norm {
 
 // The workgroup's sums over rows [r, e): per channel w and w xn (to chan(c, u, v), by
 // the thread that has the number c), per group gamma times both (to out(g, u, v)).
-template <typename T, bool VEC, int ACT, typename CHAN, typename OUT>
-__device__ __forceinline__ void grad_sums(const NormArgs& a, const Lanes& L, const Norm<VEC>& nm, int64_t r, int64_t e,
-                                          double* sh, CHAN chan, OUT out) {
-  constexpr int TILE = BWD_TILE<VEC>;
-  const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63, w8 = L.lpr * 8, c = threadIdx.x;
-  double *s1 = sh, *s2 = sh + a.C;
-  float *uu = reinterpret_cast<float*>(s2 + a.C), *vv = uu + NW * w8;
-  float u[8] = {}, v[8] = {};
-  auto add = [&](float(&t)[8], float(&w)[8]) {
-    nm.template weigh<ACT>(t, w);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) u[k] += w[k], v[k] = __builtin_fmaf(w[k], t[k], v[k]);
-  };
-  int64_t i = r + L.rl;
-  for (; i + (TILE - 1) * L.RL < e; i += TILE * L.RL) {
-    float t[TILE][8], w[TILE][8];
+template <int W, typename T, bool VEC, int ACT, typename CHAN, typename OUT>
+__device__ __forceinline__ void grad_sums(const NormArgs& a, const Lanes<VEC>& L, const Norm<VEC>& nm, int64_t r, int64_t e,
+                                          SumsLds<W>& sh, CHAN chan, OUT out) {
+  constexpr int TILE = BWD_TILE<VEC>, w8 = SumsLds<W>::C;
+  const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63, c = threadIdx.x;
+  float u[CPL<VEC>] = {}, v[CPL<VEC>] = {};
+  const Source<T, VEC> in(a, L);
+  const Mat<float> gy(a.gy, a.ldgy, L.at(a.C));
+  over_rows<TILE>(L, r, e, [&](int64_t i, const Tile<TILE>& rows) {
+    float t[TILE][CPL<VEC>], w[TILE][CPL<VEC>];
 #pragma unroll
     for (int j = 0; j < TILE; ++j) {
-      Source<T, VEC>::load(a, i + j * L.RL, L.c0, L.cnt, t[j]);
-      Row<float, VEC>::load(a.gy + (i + j * L.RL) * a.ldgy, L.c0, L.cnt, w[j]);
+      in.load(i, rows.at[j], t[j]);
+      load_row<VEC>(gy.row(i, rows.at[j]), L.cnt, w[j]);
     }
 #pragma unroll
-    for (int j = 0; j < TILE; ++j) add(t[j], w[j]);
-  }
-  for (; i < e; i += L.RL) {
-    float t[8], w[8];
-    Source<T, VEC>::load(a, i, L.c0, L.cnt, t);
-    Row<float, VEC>::load(a.gy + i * a.ldgy, L.c0, L.cnt, w);
-    add(t, w);
-  }
+    for (int j = 0; j < TILE; ++j) {
+      if (j * L.RL >= rows.left) break;
+      nm.template weigh<ACT>(t[j], w[j]);
+      if (rows.ok[j]) {
+#pragma unroll
+        for (int k = 0; k < CPL<VEC>; ++k) u[k] += w[j][k], v[k] = __builtin_fmaf(w[j][k], t[j][k], v[k]);
+      }
+    }
+  });
   for (int o = L.lpr; o < 64; o <<= 1) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) u[k] += __shfl_xor(u[k], o, 64), v[k] += __shfl_xor(v[k], o, 64);
+    for (int k = 0; k < CPL<VEC>; ++k) u[k] += __shfl_xor(u[k], o, 64), v[k] += __shfl_xor(v[k], o, 64);
   }
   if (lane < L.lpr) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) uu[wid * w8 + L.c0 + k] = u[k], vv[wid * w8 + L.c0 + k] = v[k];
+    for (int k = 0; k < CPL<VEC>; ++k) sh.u[wid * w8 + L.c0 + k] = u[k], sh.v[wid * w8 + L.c0 + k] = v[k];
   }
   __syncthreads();
   if (c < a.C) {
     double x = 0.0, y = 0.0;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) x += uu[w * w8 + c], y += vv[w * w8 + c];
+    for (int w = 0; w < W; ++w) x += sh.u[w * w8 + c], y += sh.v[w * w8 + c];
     const double gc = a.gamma ? a.gamma[c] : 1.0f;
     chan(c, x, y);
-    s1[c] = gc * x;
-    s2[c] = gc * y;
+    sh.s1[c] = gc * x;
+    sh.s2[c] = gc * y;
   }
   __syncthreads();
-  group_sums(s1, s2, a.G, a.gs, out);
+  group_sums<W>(sh.s1, sh.s2, a.G, a.gs, out);
 }
 
 // First pass: per chunk and segment the groups' sums, per chunk the channels'.
 template <typename T, bool VEC, int ACT>
-__global__ __launch_bounds__(NT) void k_norm_bwd_sums(NormArgs a) {
-  extern __shared__ double sh[];
-  const Lanes L(a.lg, a.C, NT);
+__global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_sums(NormArgs a) {
+  __shared__ SumsLds<NW> sh;
+  const Lanes<VEC> L(a.lg, a.C, NT);
   const int64_t r0 = (int64_t)blockIdx.x * a.R, r1 = std::min<int64_t>(r0 + a.R, a.n);
   const Groups<VEC> groups(a, L.c0);
   Norm<VEC> nm;
-  params8<VEC>(a, L, nm.gamma, nm.beta);
+  params<VEC>(a, L, nm.gamma, nm.beta);
   double cu = 0.0, cv = 0.0;
   int s = seg_find(a, r0);
   for (int64_t r = r0; r < r1; ++s) {
@@ -787,7 +884,7 @@ __global__ __launch_bounds__(NT) void k_norm_bwd_sums(NormArgs a) {
     if (e <= r) continue;
     groups.read(stats_of(a, s), nm.mean, nm.rstd);
     float2* part = a.part + ((int64_t)blockIdx.x + s) * a.G;
-    grad_sums<T, VEC, ACT>(
+    grad_sums<NW, T, VEC, ACT>(
         a, L, nm, r, e, sh, [&](int, double x, double y) { cu += x, cv += y; },
         [&](int g, double x, double y) { part[g] = make_float2((float)x, (float)y); });
     __syncthreads();
@@ -802,17 +899,18 @@ __global__ __launch_bounds__(NT) void k_norm_bwd_sums(NormArgs a) {
 
 // dbeta and dgamma from the chunks' sums: 64 columns of part_c to a workgroup,
 // the chunks dealt to its waves, joined in wave order.
-__device__ __forceinline__ void columns(const NormArgs& a, int block, double* sh, int waves) {
+template <int W>
+__device__ __forceinline__ void columns(const NormArgs& a, int block, double* sh) {
   const int col = block * 64 + (threadIdx.x & 63), wid = threadIdx.x >> 6;
   double v = 0.0;
   if (col < 2 * a.C) {
 #pragma unroll 8
-    for (int j = wid; j < a.nchunks; j += waves) v += a.part_c[(int64_t)j * 2 * a.C + col];
+    for (int j = wid; j < a.nchunks; j += W) v += a.part_c[(int64_t)j * 2 * a.C + col];
   }
   sh[threadIdx.x] = v;
   __syncthreads();
   if (wid == 0 && col < 2 * a.C) {
-    for (int w = 1; w < waves; ++w) v += sh[w * 64 + threadIdx.x];
+    for (int w = 1; w < W; ++w) v += sh[w * 64 + threadIdx.x];
     float* p = col < a.C ? a.dbeta + col : a.dgamma + (col - a.C);
     *p = a.accumulate ? *p + (float)v : (float)v;
   }
@@ -820,57 +918,52 @@ __device__ __forceinline__ void columns(const NormArgs& a, int block, double* sh
 
 // grad_x of one row from its groups' sums A and B, added to g
 template <bool VEC>
-__device__ __forceinline__ void grad8(const Norm<VEC>& nm, const PerUnit<VEC>& A, const PerUnit<VEC>& B,
-                                      const float (&w)[8], const float (&xn)[8], float (&g)[8]) {
+__device__ __forceinline__ void grad_row(const Norm<VEC>& nm, const PerUnit<VEC>& A, const PerUnit<VEC>& B,
+                                      const float (&w)[CPL<VEC>], const float (&xn)[CPL<VEC>], float (&g)[CPL<VEC>]) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
+  for (int k = 0; k < CPL<VEC>; ++k)
     g[k] = __builtin_fmaf(nm.rstd[k], __builtin_fmaf(-xn[k], B[k], __builtin_fmaf(nm.gamma[k], w[k], -A[k])), g[k]);
 }
 
 template <typename T, bool VEC, int ACT>
-__device__ __forceinline__ void grad_rows(const NormArgs& a, const Lanes& L, const Norm<VEC>& nm, const PerUnit<VEC>& A,
+__device__ __forceinline__ void grad_rows(const NormArgs& a, const Lanes<VEC>& L, const Norm<VEC>& nm, const PerUnit<VEC>& A,
                                           const PerUnit<VEC>& B, int64_t r, int64_t end) {
   constexpr int TILE = BWD_TILE<VEC>;
-  auto take = [&](int64_t row, float(&t)[8], float(&w)[8], float(&g)[8]) {
-    Source<T, VEC>::load(a, row, L.c0, L.cnt, t);
-    Row<float, VEC>::load(a.gy + row * a.ldgy, L.c0, L.cnt, w);
-    if (a.ga) Row<float, VEC>::load(a.ga + row * a.ldga, L.c0, L.cnt, g);
-  };
-  auto put = [&](int64_t row, float(&t)[8], float(&w)[8], float(&g)[8]) {
-    nm.template weigh<ACT>(t, w);
-    grad8(nm, A, B, w, t, g);
-    Row<float, VEC>::store(a.gx + row * a.ldgx, L.c0, L.cnt, g);
-  };
-  int64_t i = r + L.rl;
-  for (; i + (TILE - 1) * L.RL < end; i += TILE * L.RL) {
-    float t[TILE][8], w[TILE][8], g[TILE][8] = {};
+  const Source<T, VEC> in(a, L);
+  const Mat<float> gy(a.gy, a.ldgy, L.at(a.C)), ga(a.ga, a.ldga, L.at(a.C)), gx(a.gx, a.ldgx, L.c0);
+  over_rows<TILE>(L, r, end, [&](int64_t i, const Tile<TILE>& rows) {
+    float t[TILE][CPL<VEC>], w[TILE][CPL<VEC>], g[TILE][CPL<VEC>] = {};
 #pragma unroll
-    for (int j = 0; j < TILE; ++j) take(i + j * L.RL, t[j], w[j], g[j]);
+    for (int j = 0; j < TILE; ++j) {
+      in.load(i, rows.at[j], t[j]);
+      load_row<VEC>(gy.row(i, rows.at[j]), L.cnt, w[j]);
+      if (a.ga) load_row<VEC>(ga.row(i, rows.at[j]), L.cnt, g[j]);
+    }
 #pragma unroll
-    for (int j = 0; j < TILE; ++j) put(i + j * L.RL, t[j], w[j], g[j]);
-  }
-  for (; i < end; i += L.RL) {
-    float t[8], w[8], g[8] = {};
-    take(i, t, w, g);
-    put(i, t, w, g);
-  }
+    for (int j = 0; j < TILE; ++j) {
+      if (j * L.RL >= rows.left) break;
+      nm.template weigh<ACT>(t[j], w[j]);
+      grad_row(nm, A, B, w[j], t[j], g[j]);
+      if (rows.ok[j]) store_row<VEC>(gx.row(i, rows.at[j]), L.cnt, g[j]);
+    }
+  });
 }
 
 // Second pass.  The first a.nred workgroups form dbeta and dgamma.
 template <typename T, bool VEC, int ACT>
-__global__ __launch_bounds__(NT) void k_norm_bwd_dx(NormArgs a) {
+__global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_dx(NormArgs a) {
   __shared__ double sh[2 * NT];
   __shared__ float2 st[MAX_C];
   if ((int)blockIdx.x < a.nred) {
-    columns(a, blockIdx.x, sh, NW);
+    columns<NW>(a, blockIdx.x, sh);
     return;
   }
-  const Lanes L(a.lg, a.C, NT);
+  const Lanes<VEC> L(a.lg, a.C, NT);
   const int64_t r0 = (int64_t)(blockIdx.x - a.nred) * a.RA, r1 = std::min<int64_t>(r0 + a.RA, a.n);
   if (r0 >= r1) return;
   const Groups<VEC> groups(a, L.c0);
   Norm<VEC> nm;
-  params8<VEC>(a, L, nm.gamma, nm.beta);
+  params<VEC>(a, L, nm.gamma, nm.beta);
   int s = seg_find(a, r0);
   for (int64_t r = r0; r < r1; ++s) {
     const int64_t b = seg_begin(a, s), e = seg_end(a, s), end = std::min<int64_t>(e, r1);
@@ -889,16 +982,16 @@ __global__ __launch_bounds__(NT) void k_norm_bwd_dx(NormArgs a) {
 
 // One segment, one workgroup: both passes and the parameters' gradients.
 template <typename T, bool VEC, int ACT>
-__global__ __launch_bounds__(NT) void k_norm_bwd_small(NormArgs a) {
-  extern __shared__ double sh[];
+__global__ __launch_bounds__(SNT) void k_norm_bwd_small(NormArgs a) {
+  __shared__ SumsLds<SNW> sh;
   __shared__ float2 st[MAX_C];
-  const Lanes L(a.lg, a.C, NT);
+  const Lanes<VEC> L(a.lg, a.C, SNT);
   const Groups<VEC> groups(a, L.c0);
   Norm<VEC> nm;
-  params8<VEC>(a, L, nm.gamma, nm.beta);
+  params<VEC>(a, L, nm.gamma, nm.beta);
   groups.read(stats_of(a, 0), nm.mean, nm.rstd);
   const double inv = 1.0 / ((double)a.n * a.gs);
-  grad_sums<T, VEC, ACT>(
+  grad_sums<SNW, T, VEC, ACT>(
       a, L, nm, 0, a.n, sh,
       [&](int c, double x, double y) {
         if (!a.dbeta) return;
@@ -913,9 +1006,9 @@ __global__ __launch_bounds__(NT) void k_norm_bwd_small(NormArgs a) {
 }
 
 // dbeta and dgamma alone (rows as segments, no rows at all)
-__global__ __launch_bounds__(RNT) void k_norm_columns(NormArgs a) {
-  __shared__ double sh[RNT];
-  columns(a, blockIdx.x, sh, RNT / 64);
+__global__ __launch_bounds__(SNT) void k_norm_columns(NormArgs a) {
+  __shared__ double sh[SNT];
+  columns<SNW>(a, blockIdx.x, sh);
 }
 
 // ------------------------------------------------------------ each row a segment
@@ -925,19 +1018,19 @@ __global__ __launch_bounds__(RNT) void k_norm_columns(NormArgs a) {
 // other through the wave's LDS.
 template <bool VEC>
 struct RowGroups {
-  static constexpr int U = UNIT<VEC>, N = 8 / U;
+  static constexpr int U = UNIT<VEC>, N = CPL<VEC> / U;
   int width;     // lanes of a group; 0: a unit; -1: through LDS
   int at[N];     // first unit of each unit's group
   float* lds;    // the wave's 64 N floats
 
-  __device__ __forceinline__ RowGroups(const NormArgs& a, const Lanes& L, float* wave_lds) : lds(wave_lds) {
-    const int lanes = a.gs / 8, gu = a.gs / U;
-    width = gu == 1 ? 0 : a.G == 1 ? L.lpr : (a.gs % 8 == 0 && (lanes & (lanes - 1)) == 0) ? lanes : -1;
+  __device__ __forceinline__ RowGroups(const NormArgs& a, const Lanes<VEC>& L, float* wave_lds) : lds(wave_lds) {
+    const int lanes = a.gs / CPL<VEC>, gu = a.gs / U;
+    width = gu == 1 ? 0 : a.G == 1 ? L.lpr : (a.gs % CPL<VEC> == 0 && (lanes & (lanes - 1)) == 0) ? lanes : -1;
 #pragma unroll
     for (int j = 0; j < N; ++j) at[j] = std::min(L.lr * N + j, a.C / U - 1) / gu * gu;
   }
-  // p: this lane's eight values; the sum over its group for each unit
-  __device__ __forceinline__ PerUnit<VEC> sum(const NormArgs& a, const Lanes& L, const float (&p)[8]) const {
+  // p: this lane's values; the sum over its group for each unit
+  __device__ __forceinline__ PerUnit<VEC> sum(const NormArgs& a, const Lanes<VEC>& L, const float (&p)[CPL<VEC>]) const {
     PerUnit<VEC> s;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
@@ -949,6 +1042,7 @@ struct RowGroups {
       float t = s.v[0];
 #pragma unroll
       for (int j = 1; j < N; ++j) t += s.v[j];
+      t = L.cnt > 0 ? t : 0.0f;
       for (int o = 1; o < width; o <<= 1) t += __shfl_xor(t, o, 64);
 #pragma unroll
       for (int j = 0; j < N; ++j) s.v[j] = t;
@@ -973,25 +1067,29 @@ struct RowGroups {
 
 template <typename T, bool VEC, bool ADD, int ACT>
 __global__ __launch_bounds__(RNT) void k_norm_rows(NormArgs a) {
-  constexpr int U = UNIT<VEC>, N = 8 / U;
+  constexpr int U = UNIT<VEC>, N = CPL<VEC> / U;
   __shared__ float lds[RNT * N];
-  const Lanes L(a.lg, a.C, RNT);
+  const Lanes<VEC> L(a.lg, a.C, RNT);
   const RowGroups<VEC> R(a, L, lds + (threadIdx.x >> 6) * 64 * N);
   const Groups<VEC> groups(a, L.c0);
-  float gamma[8], beta[8];
-  params8<VEC>(a, L, gamma, beta);
+  float gamma[CPL<VEC>], beta[CPL<VEC>];
+  params<VEC>(a, L, gamma, beta);
   const float f = 1.0f / a.gs;
-  for (int64_t i = (int64_t)blockIdx.x * L.RL + L.rl; i < a.n; i += (int64_t)gridDim.x * L.RL) {
-    float t[1][8], q[8];
-    take_rows<T, VEC, ADD, 1>(a, i, 0, L.c0, L.cnt, t);
-    float(&v)[8] = t[0];
-    if (ADD) Row<T, VEC>::store(static_cast<T*>(a.sum) + i * a.lds, L.c0, L.cnt, v);
-    if (a.ck) store_q8<VEC>(a.q, a.scale, i, a.C, L.c0, L.cnt, std::min(8, L.lpr), v);
+  const Stream<T, VEC, ADD> in(a, L);
+  const Keep<VEC> keep(a, L);
+  const Result<VEC> out(a, L);
+  const Mat<float2> st(a.stats, a.G, 0);
+  for (int64_t i = (int64_t)blockIdx.x * L.RL; i < a.n; i += (int64_t)gridDim.x * L.RL) {
+    if (i + L.rl >= a.n) return;
+    float t[1][CPL<VEC>], q[CPL<VEC>];
+    in.load(i, Tile<1>(L, L.RL), t);
+    float(&v)[CPL<VEC>] = t[0];
+    if (a.ck) keep.store(i, L.rl, true, v);
     PerUnit<VEC> mean = R.sum(a, L, v), rstd;
 #pragma unroll
     for (int j = 0; j < N; ++j) mean.v[j] *= f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < CPL<VEC>; ++k) {
       const float d = k < L.cnt ? v[k] - mean[k] : 0.0f;
       q[k] = d * d;
     }
@@ -1001,53 +1099,61 @@ __global__ __launch_bounds__(RNT) void k_norm_rows(NormArgs a) {
       rstd.v[j] = 1.0f / sqrtf(__builtin_fmaf(rstd.v[j], f, a.eps));
       // a group's first unit writes for it
       if (j * U < L.cnt && L.lr * N + j == R.at[j])
-        reinterpret_cast<float2*>(a.stats)[i * a.G + groups.g[j]] = make_float2(mean.v[j], rstd.v[j]);
+        st.row(i, L.rl)[groups.g[j]] = make_float2(mean.v[j], rstd.v[j]);
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
+    for (int k = 0; k < CPL<VEC>; ++k)
       v[k] = activate<ACT>(__builtin_fmaf((v[k] - mean[k]) * rstd[k], gamma[k], beta[k]));
-    store_y<VEC>(a, i, L, v);
+    out.store(i, L.rl, v);
   }
 }
 
 template <bool VEC, int ACT>
 __global__ __launch_bounds__(RNT) void k_norm_rows_restore(NormArgs a) {
-  const Lanes L(a.lg, a.C, RNT);
+  const Lanes<VEC> L(a.lg, a.C, RNT);
   const Groups<VEC> groups(a, L.c0);
-  float gamma[8], beta[8];
-  params8<VEC>(a, L, gamma, beta);
-  for (int64_t i = (int64_t)blockIdx.x * L.RL + L.rl; i < a.n; i += (int64_t)gridDim.x * L.RL) {
-    float v[8];
+  float gamma[CPL<VEC>], beta[CPL<VEC>];
+  params<VEC>(a, L, gamma, beta);
+  const Source<Q8, VEC> in(a, L);
+  const Result<VEC> out(a, L);
+  const Mat<float2> st(a.stats, a.G, 0);
+  for (int64_t i = (int64_t)blockIdx.x * L.RL; i < a.n; i += (int64_t)gridDim.x * L.RL) {
+    if (i + L.rl >= a.n) return;
+    float v[CPL<VEC>];
     PerUnit<VEC> mean, rstd;
-    Source<Q8, VEC>::load(a, i, L.c0, L.cnt, v);
-    groups.read(reinterpret_cast<const float2*>(a.stats) + i * a.G, mean, rstd);
+    in.load(i, L.rl, v);
+    groups.read(st.row(i, L.rl), mean, rstd);
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
+    for (int k = 0; k < CPL<VEC>; ++k)
       v[k] = activate<ACT>(__builtin_fmaf((v[k] - mean[k]) * rstd[k], gamma[k], beta[k]));
-    store_y<VEC>(a, i, L, v);
+    out.store(i, L.rl, v);
   }
 }
 
 template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(RNT) void k_norm_rows_bwd(NormArgs a) {
-  constexpr int N = 8 / UNIT<VEC>;
+  constexpr int N = CPL<VEC> / UNIT<VEC>;
   __shared__ float lds[RNT * 16];
-  const Lanes L(a.lg, a.C, RNT);
+  const Lanes<VEC> L(a.lg, a.C, RNT);
   const RowGroups<VEC> R(a, L, lds + (threadIdx.x >> 6) * 64 * N);
   const Groups<VEC> groups(a, L.c0);
   Norm<VEC> nm;
-  float u[8] = {}, v[8] = {};
-  params8<VEC>(a, L, nm.gamma, nm.beta);
+  float u[CPL<VEC>] = {}, v[CPL<VEC>] = {};
+  params<VEC>(a, L, nm.gamma, nm.beta);
   const float f = 1.0f / a.gs;
-  for (int64_t i = (int64_t)blockIdx.x * L.RL + L.rl; i < a.n; i += (int64_t)gridDim.x * L.RL) {
-    float t[8], w[8], g[8] = {}, x[8], y[8];
-    Source<T, VEC>::load(a, i, L.c0, L.cnt, t);
-    Row<float, VEC>::load(a.gy + i * a.ldgy, L.c0, L.cnt, w);
-    if (a.ga) Row<float, VEC>::load(a.ga + i * a.ldga, L.c0, L.cnt, g);
-    groups.read(reinterpret_cast<const float2*>(a.stats) + i * a.G, nm.mean, nm.rstd);
+  const Source<T, VEC> in(a, L);
+  const Mat<float> gy(a.gy, a.ldgy, L.at(a.C)), ga(a.ga, a.ldga, L.at(a.C)), gx(a.gx, a.ldgx, L.c0);
+  const Mat<float2> st(a.stats, a.G, 0);
+  for (int64_t i = (int64_t)blockIdx.x * L.RL; i < a.n; i += (int64_t)gridDim.x * L.RL) {
+    if (i + L.rl >= a.n) break;
+    float t[CPL<VEC>], w[CPL<VEC>], g[CPL<VEC>] = {}, x[CPL<VEC>], y[CPL<VEC>];
+    in.load(i, L.rl, t);
+    load_row<VEC>(gy.row(i, L.rl), L.cnt, w);
+    if (a.ga) load_row<VEC>(ga.row(i, L.rl), L.cnt, g);
+    groups.read(st.row(i, L.rl), nm.mean, nm.rstd);
     nm.template weigh<ACT>(t, w);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < CPL<VEC>; ++k) {
       if (k >= L.cnt) w[k] = 0.0f;
       u[k] += w[k];
       v[k] = __builtin_fmaf(w[k], t[k], v[k]);
@@ -1057,19 +1163,19 @@ __global__ __launch_bounds__(RNT) void k_norm_rows_bwd(NormArgs a) {
     PerUnit<VEC> A = R.sum(a, L, x), B = R.sum(a, L, y);
 #pragma unroll
     for (int j = 0; j < N; ++j) A.v[j] *= f, B.v[j] *= f;
-    grad8(nm, A, B, w, t, g);
-    Row<float, VEC>::store(a.gx + i * a.ldgx, L.c0, L.cnt, g);
+    grad_row(nm, A, B, w, t, g);
+    store_row<VEC>(gx.row(i, L.rl), L.cnt, g);
   }
   if (!a.part_c) return;
   for (int o = L.lpr; o < 64; o <<= 1) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) u[k] += __shfl_xor(u[k], o, 64), v[k] += __shfl_xor(v[k], o, 64);
+    for (int k = 0; k < CPL<VEC>; ++k) u[k] += __shfl_xor(u[k], o, 64), v[k] += __shfl_xor(v[k], o, 64);
   }
   __syncthreads();
-  const int w8 = L.lpr * 8, wid = threadIdx.x >> 6;
+  const int w8 = L.lpr * CPL<VEC>, wid = threadIdx.x >> 6;
   if ((threadIdx.x & 63) < (unsigned)L.lpr) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) lds[wid * 2 * w8 + L.c0 + k] = u[k], lds[wid * 2 * w8 + w8 + L.c0 + k] = v[k];
+    for (int k = 0; k < CPL<VEC>; ++k) lds[wid * 2 * w8 + L.c0 + k] = u[k], lds[wid * 2 * w8 + w8 + L.c0 + k] = v[k];
   }
   __syncthreads();
   for (int c = threadIdx.x; c < a.C; c += RNT) {
@@ -1084,46 +1190,63 @@ __global__ __launch_bounds__(RNT) void k_norm_rows_bwd(NormArgs a) {
 
 template <typename T, bool VEC>
 __global__ __launch_bounds__(RNT) void k_ckpt_store(NormArgs a) {
-  const Lanes L(a.lg, a.C, RNT);
-  for (int64_t i = (int64_t)blockIdx.x * L.RL + L.rl; i < a.n; i += (int64_t)gridDim.x * L.RL) {
-    float v[8];
-    Source<T, VEC>::load(a, i, L.c0, L.cnt, v);
-    store_q8<VEC>(a.q, a.scale, i, a.C, L.c0, L.cnt, std::min(8, L.lpr), v);
+  const Lanes<VEC> L(a.lg, a.C, RNT);
+  const Source<T, VEC> in(a, L);
+  const Keep<VEC> keep(a, L);
+  for (int64_t i = (int64_t)blockIdx.x * L.RL; i < a.n; i += (int64_t)gridDim.x * L.RL) {
+    if (i + L.rl >= a.n) return;
+    float v[CPL<VEC>];
+    in.load(i, L.rl, v);
+    keep.store(i, L.rl, true, v);
   }
 }
 
-template <typename Y, bool VEC>
+template <bool VEC>
 __global__ __launch_bounds__(RNT) void k_ckpt_load(NormArgs a) {
-  const Lanes L(a.lg, a.C, RNT);
-  for (int64_t i = (int64_t)blockIdx.x * L.RL + L.rl; i < a.n; i += (int64_t)gridDim.x * L.RL) {
-    float v[8];
-    Source<Q8, VEC>::load(a, i, L.c0, L.cnt, v);
-    Row<Y, VEC>::store(static_cast<Y*>(a.y) + i * a.ldy, L.c0, L.cnt, v);
+  const Lanes<VEC> L(a.lg, a.C, RNT);
+  const Source<Q8, VEC> in(a, L);
+  const Result<VEC> out(a, L);
+  for (int64_t i = (int64_t)blockIdx.x * L.RL; i < a.n; i += (int64_t)gridDim.x * L.RL) {
+    if (i + L.rl >= a.n) return;
+    float v[CPL<VEC>];
+    in.load(i, L.rl, v);
+    out.store(i, L.rl, v);
   }
 }
 
 // ------------------------------------------------------------ host side
 
-int lanes_log2(int C) {
+int lanes_log2(int C, bool vec) {
   int lg = 0;
-  while ((8 << lg) < C) ++lg;
+  while (((vec ? CPL<true> : CPL<false>) << lg) < C) ++lg;
   return lg;
 }
 
 // Chunks of the summing pass: whole steps of the workgroup's rows, at most MAX_CHUNKS.
-void chunking(int64_t n, int C, int64_t& rows, int64_t& chunks) {
-  const int64_t step = NT >> lanes_log2(C);
+void chunking(int64_t n, int lg, int64_t& rows, int64_t& chunks) {
+  const int64_t step = NT >> lg;
   const int64_t steps = (n + step - 1) / step;
   rows = std::max<int64_t>(1, (steps + MAX_CHUNKS - 1) / MAX_CHUNKS) * step;
   chunks = (n + rows - 1) / rows;
 }
 
-// whole aligned groups of eight in every row
+// whole aligned groups of four values in every row
 bool aligned(const void* p, int64_t ld, int size) {
-  return !p || ((reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld * size & 15) == 0);
+  return !p || (reinterpret_cast<uintptr_t>(p) % (4 * size) == 0 && ld % 4 == 0);
 }
 
 int size_of(int dtype) { return dtype == DSMP_BF16 ? 2 : 4; }
+
+// Row distances: at least the channels, and small enough that the rows of a tile
+// of a workgroup (8 steps of at most 1,024 rows) lie within 32 bits.
+constexpr int64_t MAX_LD = (int64_t)1 << 16;
+dsmp_status check_ld(dsmp_handle* h, int C, std::initializer_list<int64_t> lds) {
+  for (const int64_t ld : lds) {
+    DSMP_CHECK(h, ld >= C, DSMP_INVALID_ARG, "rows are closer than their channels");
+    DSMP_CHECK(h, ld <= MAX_LD, DSMP_UNSUPPORTED, "rows more than %lld elements apart", (long long)MAX_LD);
+  }
+  return DSMP_OK;
+}
 
 bool rows_are_segments(const dsmp_segments& s) { return !s.ptr && s.n_seg == s.n; }
 
@@ -1149,8 +1272,10 @@ struct NormWs {
 };
 
 NormWs norm_ws(const dsmp_norm_desc& d, const dsmp_segments& s, bool backward, void* ws) {
-  int64_t rows, chunks;
-  chunking(s.n, d.channels, rows, chunks);
+  int64_t rows, chunks, wide;
+  chunking(s.n, lanes_log2(d.channels, false), rows, chunks);
+  chunking(s.n, lanes_log2(d.channels, true), rows, wide);
+  chunks = std::max(chunks, wide);
   Carve cv(ws);
   NormWs w{};
   w.part = cv.take<float2>(rows_are_segments(s) ? 0 : (size_t)(chunks + s.n_seg) * d.groups);
@@ -1165,21 +1290,25 @@ NormArgs norm_args(const dsmp_norm_desc& d, const dsmp_segments& s) {
   a.C = d.channels;
   a.G = d.groups;
   a.gs = d.channels / d.groups;
-  a.lg = lanes_log2(a.C);
   a.n_seg = (int)s.n_seg;
   a.ptr = s.ptr;
   a.len = s.ptr ? 0 : s.n / s.n_seg;
   a.eps = d.eps;
-  int64_t chunks;
-  chunking(s.n, a.C, a.R, chunks);
-  a.nchunks = (int)chunks;
   return a;
+}
+
+// Lanes and chunks.
+void place(NormArgs& a, bool vec) {
+  int64_t chunks;
+  a.lg = lanes_log2(a.C, vec);
+  chunking(a.n, a.lg, a.R, chunks);
+  a.nchunks = (int)chunks;
 }
 
 // workgroups of the second pass and their rows
 unsigned second_grid(const dsmp_handle* h, NormArgs& a) {
   const int64_t step = NT >> a.lg, steps = (a.n + step - 1) / step;
-  const int64_t most = (int64_t)h->n_cu * 4;
+  const int64_t most = (int64_t)h->n_cu * 2;
   a.RA = std::max<int64_t>(1, (steps + most - 1) / most) * step;
   return (unsigned)std::max<int64_t>(1, (a.n + a.RA - 1) / a.RA);
 }
@@ -1189,17 +1318,18 @@ unsigned row_grid(const dsmp_handle* h, const NormArgs& a, int per_cu) {
   return (unsigned)std::min<int64_t>((a.n + step - 1) / step, (int64_t)h->n_cu * per_cu);
 }
 
-bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7) == 0; }
-
 // the channels, groups and parameters that VEC asks for
 bool whole(const NormArgs& a) {
-  return a.C % 8 == 0 && a.gs % 4 == 0 && aligned(a.gamma, 0, 4) && aligned(a.beta, 0, 4);
+  return a.C <= MAX_C / 2 && a.gs % 4 == 0 && aligned(a.gamma, 0, 4) && aligned(a.beta, 0, 4);
 }
 
 // One launch with a workgroup to a segment: where all the rows are at most
-// SMALL_STEPS steps of one workgroup, however they are dealt to the segments.
-constexpr int SMALL_STEPS = 16;
-bool small(const NormArgs& a) { return a.n <= (int64_t)SMALL_STEPS * (NT >> a.lg); }
+// SMALL_STEPS steps of one workgroup, however they are dealt to the segments (and
+// its LDS stays within 64 KB).
+#ifndef SMALL_STEPS
+constexpr int SMALL_STEPS = 8;
+#endif
+bool small(const NormArgs& a) { return a.C <= MAX_C / 2 && a.n <= (int64_t)SMALL_STEPS * (SNT >> a.lg); }
 
 template <typename F>
 void by_bool(bool b, F f) {
@@ -1246,7 +1376,7 @@ extern "C" dsmp_status dsmp_group_norm_forward(dsmp_handle* h, const dsmp_norm_d
                                                int64_t ldy, float* stats, const dsmp_checkpoint* ck, void* ws,
                                                size_t ws_bytes) {
   if (!h) return DSMP_INVALID_ARG;
-  const dsmp_status st = check_norm(h, desc, seg);
+  dsmp_status st = check_norm(h, desc, seg);
   if (st != DSMP_OK) return st;
   const int64_t n = seg->n;
   const int C = desc->channels;
@@ -1254,8 +1384,8 @@ extern "C" dsmp_status dsmp_group_norm_forward(dsmp_handle* h, const dsmp_norm_d
   DSMP_CHECK(h, !gamma == !beta, DSMP_INVALID_ARG, "gamma and beta go together");
   DSMP_CHECK(h, !addend == !sum, DSMP_INVALID_ARG, "an addend and the sum go together");
   DSMP_CHECK(h, !ck || n == 0 || (ck->q && ck->scale), DSMP_INVALID_ARG, "a checkpoint pointer is NULL");
-  DSMP_CHECK(h, ldx >= C && ldy >= C && (!addend || (lda >= C && lds >= C)), DSMP_INVALID_ARG,
-             "rows are closer than their channels");
+  st = check_ld(h, C, {ldx, ldy, addend ? lda : C, addend ? lds : C});
+  if (st != DSMP_OK) return st;
   const NormWs w = norm_ws(*desc, *seg, false, ws);
   DSMP_CHECK(h, ws_bytes >= w.total && (ws || w.total == 0), DSMP_WORKSPACE_TOO_SMALL, "workspace needs %zu bytes", w.total);
   NormArgs a = norm_args(*desc, *seg);
@@ -1268,7 +1398,8 @@ extern "C" dsmp_status dsmp_group_norm_forward(dsmp_handle* h, const dsmp_norm_d
   a.y_bf16 = desc->y_dtype == DSMP_BF16;
   const int xs = size_of(desc->x_dtype);
   const bool vec = whole(a) && aligned(x, ldx, xs) && aligned(addend, lda, xs) && aligned(sum, lds, xs) &&
-                   aligned(y, ldy, size_of(desc->y_dtype)) && (!ck || aligned8(ck->q));
+                   aligned(y, ldy, size_of(desc->y_dtype)) && (!ck || aligned(ck->q, C, 1));
+  place(a, vec);
   ProfScope prof(h, DSMP_K_NORM);
   by_type(desc->x_dtype, [&](auto xt) {
     by_bool(vec, [&](auto v) {
@@ -1282,11 +1413,11 @@ extern "C" dsmp_status dsmp_group_norm_forward(dsmp_handle* h, const dsmp_norm_d
           });
         } else if (small(a)) {
           by_bool(addend, [&](auto ad) {
-            DSMP_GO((k_norm_small<T, V, decltype(ad)::value, ACT>), a.n_seg, NT, sums_lds(a.lg, C));
+            DSMP_GO((k_norm_small<T, V, decltype(ad)::value, ACT>), a.n_seg, SNT, 0);
           });
         } else {
           by_bool(addend, [&](auto ad) {
-            DSMP_GO((k_norm_stats<T, V, decltype(ad)::value>), a.nchunks, NT, sums_lds(a.lg, C));
+            DSMP_GO((k_norm_stats<T, V, decltype(ad)::value>), a.nchunks, NT, 0);
           });
           if (addend) a.x = sum, a.ldx = lds;
           const unsigned grid = second_grid(h, a);
@@ -1303,18 +1434,19 @@ extern "C" dsmp_status dsmp_group_norm_restore(dsmp_handle* h, const dsmp_norm_d
                                                const dsmp_checkpoint* ck, const float* stats, const float* gamma,
                                                const float* beta, void* y, int64_t ldy) {
   if (!h) return DSMP_INVALID_ARG;
-  const dsmp_status st = check_norm(h, desc, seg);
+  dsmp_status st = check_norm(h, desc, seg);
   if (st != DSMP_OK) return st;
   const int C = desc->channels;
   DSMP_CHECK(h, seg->n == 0 || (ck && ck->q && ck->scale && stats && y), DSMP_INVALID_ARG, "a data pointer is NULL");
   DSMP_CHECK(h, !gamma == !beta, DSMP_INVALID_ARG, "gamma and beta go together");
-  DSMP_CHECK(h, ldy >= C, DSMP_INVALID_ARG, "rows are closer than their channels");
-  if (seg->n == 0) return DSMP_OK;
+  st = check_ld(h, C, {ldy});
+  if (st != DSMP_OK || seg->n == 0) return st;
   NormArgs a = norm_args(*desc, *seg);
   a.x = ck->q, a.xscale = ck->scale;
   a.gamma = gamma, a.beta = beta, a.y = y, a.ldy = ldy, a.stats = const_cast<float*>(stats);
   a.y_bf16 = desc->y_dtype == DSMP_BF16;
-  const bool vec = whole(a) && aligned(y, ldy, size_of(desc->y_dtype)) && aligned8(ck->q);
+  const bool vec = whole(a) && aligned(y, ldy, size_of(desc->y_dtype)) && aligned(ck->q, C, 1);
+  place(a, vec);
   ProfScope prof(h, DSMP_K_NORM);
   by_bool(vec, [&](auto v) {
     by_act(desc->act, [&](auto act) {
@@ -1339,7 +1471,7 @@ extern "C" dsmp_status dsmp_group_norm_backward(dsmp_handle* h, const dsmp_norm_
                                                 int64_t ldga, float* grad_x, int64_t ldgx, float* dgamma, float* dbeta,
                                                 int32_t flags, void* ws, size_t ws_bytes) {
   if (!h) return DSMP_INVALID_ARG;
-  const dsmp_status st = check_norm(h, desc, seg);
+  dsmp_status st = check_norm(h, desc, seg);
   if (st != DSMP_OK) return st;
   const int64_t n = seg->n;
   const int C = desc->channels;
@@ -1349,8 +1481,8 @@ extern "C" dsmp_status dsmp_group_norm_backward(dsmp_handle* h, const dsmp_norm_
              "a data pointer is NULL");
   DSMP_CHECK(h, !gamma == !beta && !gamma == !dgamma && !gamma == !dbeta, DSMP_INVALID_ARG,
              "gamma, beta and their gradients go together");
-  DSMP_CHECK(h, (!x || ldx >= C) && ldgy >= C && ldgx >= C && (!grad_addend || ldga >= C), DSMP_INVALID_ARG,
-             "rows are closer than their channels");
+  st = check_ld(h, C, {x ? ldx : C, ldgy, ldgx, grad_addend ? ldga : C});
+  if (st != DSMP_OK) return st;
   const NormWs w = norm_ws(*desc, *seg, true, ws);
   DSMP_CHECK(h, ws && ws_bytes >= w.total, DSMP_WORKSPACE_TOO_SMALL, "workspace needs %zu bytes", w.total);
   NormArgs a = norm_args(*desc, *seg);
@@ -1362,10 +1494,11 @@ extern "C" dsmp_status dsmp_group_norm_backward(dsmp_handle* h, const dsmp_norm_
   a.part = w.part, a.part_c = gamma ? w.part_c : nullptr;
   const unsigned nred = gamma ? ceil_div(2 * C, 64) : 0;
   const bool vec = whole(a) && aligned(x, ldx, size_of(desc->x_dtype)) && aligned(grad_y, ldgy, 4) &&
-                   aligned(grad_addend, ldga, 4) && aligned(grad_x, ldgx, 4) && (!ck || aligned8(ck->q));
+                   aligned(grad_addend, ldga, 4) && aligned(grad_x, ldgx, 4) && (!ck || aligned(ck->q, C, 1));
+  place(a, vec);
   ProfScope prof(h, DSMP_K_NORM);
   if (n == 0) {
-    if (nred) DSMP_GO(k_norm_columns, nred, RNT, 0);   // sums of no chunk
+    if (nred) DSMP_GO(k_norm_columns, nred, SNT, 0);   // sums of no chunk
     DSMP_LAUNCHED(h, "group norm backward");
     return DSMP_OK;
   }
@@ -1379,11 +1512,11 @@ extern "C" dsmp_status dsmp_group_norm_backward(dsmp_handle* h, const dsmp_norm_
           const unsigned grid = std::min<unsigned>(row_grid(h, a, 4), MAX_CHUNKS);
           a.nchunks = (int)grid;
           DSMP_GO((k_norm_rows_bwd<T, V, ACT>), grid, RNT, 0);
-          if (nred) DSMP_GO(k_norm_columns, nred, RNT, 0);
+          if (nred) DSMP_GO(k_norm_columns, nred, SNT, 0);
         } else if (small(a) && a.n_seg == 1) {
-          DSMP_GO((k_norm_bwd_small<T, V, ACT>), 1, NT, sums_lds(a.lg, C));
+          DSMP_GO((k_norm_bwd_small<T, V, ACT>), 1, SNT, 0);
         } else {
-          DSMP_GO((k_norm_bwd_sums<T, V, ACT>), a.nchunks, NT, sums_lds(a.lg, C));
+          DSMP_GO((k_norm_bwd_sums<T, V, ACT>), a.nchunks, NT, 0);
           a.nred = (int)nred;
           const unsigned grid = second_grid(h, a);
           DSMP_GO((k_norm_bwd_dx<T, V, ACT>), grid + nred, NT, 0);
@@ -1408,8 +1541,7 @@ dsmp_status check_ckpt(dsmp_handle* h, const dsmp_checkpoint* ck, const void* p,
   DSMP_CHECK(h, n < (int64_t)1 << 31, DSMP_UNSUPPORTED, "2^31 rows and more");
   DSMP_CHECK(h, C <= MAX_C, DSMP_UNSUPPORTED, "more than %d channels", MAX_C);
   DSMP_CHECK(h, n == 0 || (ck && ck->q && ck->scale && p), DSMP_INVALID_ARG, "a data pointer is NULL");
-  DSMP_CHECK(h, ld >= C, DSMP_INVALID_ARG, "rows are closer than their channels");
-  return DSMP_OK;
+  return check_ld(h, C, {ld});
 }
 
 }  // namespace
@@ -1420,9 +1552,10 @@ extern "C" dsmp_status dsmp_checkpoint_store(dsmp_handle* h, const void* x, int3
   const dsmp_status st = check_ckpt(h, ck, x, dtype, ldx, n, channels);
   if (st != DSMP_OK || n == 0) return st;
   NormArgs a{};
-  a.n = n, a.C = channels, a.lg = lanes_log2(channels);
+  a.n = n, a.C = channels;
   a.x = x, a.ldx = ldx, a.q = ck->q, a.scale = ck->scale;
-  const bool vec = channels % 8 == 0 && aligned(x, ldx, size_of(dtype)) && (reinterpret_cast<uintptr_t>(ck->q) & 7) == 0;
+  const bool vec = channels % 4 == 0 && channels <= MAX_C / 2 && aligned(x, ldx, size_of(dtype)) && aligned(ck->q, channels, 1);
+  place(a, vec);
   ProfScope prof(h, DSMP_K_CKPT);
   by_type(dtype, [&](auto t) {
     by_bool(vec, [&](auto v) { DSMP_GO((k_ckpt_store<decltype(t), decltype(v)::value>), row_grid(h, a, 16), RNT, 0); });
@@ -1437,13 +1570,12 @@ extern "C" dsmp_status dsmp_checkpoint_load(dsmp_handle* h, const dsmp_checkpoin
   const dsmp_status st = check_ckpt(h, ck, y, dtype, ldy, n, channels);
   if (st != DSMP_OK || n == 0) return st;
   NormArgs a{};
-  a.n = n, a.C = channels, a.lg = lanes_log2(channels);
-  a.x = ck->q, a.xscale = ck->scale, a.y = y, a.ldy = ldy;
-  const bool vec = channels % 8 == 0 && aligned(y, ldy, size_of(dtype)) && (reinterpret_cast<uintptr_t>(ck->q) & 7) == 0;
+  a.n = n, a.C = channels;
+  a.x = ck->q, a.xscale = ck->scale, a.y = y, a.ldy = ldy, a.y_bf16 = dtype == DSMP_BF16;
+  const bool vec = channels % 4 == 0 && channels <= MAX_C / 2 && aligned(y, ldy, size_of(dtype)) && aligned(ck->q, channels, 1);
+  place(a, vec);
   ProfScope prof(h, DSMP_K_CKPT);
-  by_type(dtype, [&](auto t) {
-    by_bool(vec, [&](auto v) { DSMP_GO((k_ckpt_load<decltype(t), decltype(v)::value>), row_grid(h, a, 16), RNT, 0); });
-  });
+  by_bool(vec, [&](auto v) { DSMP_GO((k_ckpt_load<decltype(v)::value>), row_grid(h, a, 16), RNT, 0); });
   DSMP_LAUNCHED(h, "checkpoint load");
   return DSMP_OK;
 }

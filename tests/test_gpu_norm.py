@@ -569,3 +569,31 @@ def test_refusals(env):
     g = lib.dsmp_radius_graph_build(torch.rand(n, 2, device="cuda"), n, 0.5)
     with pytest.raises(dm.DsmpError):
         lib.dsmp_nnconv_workspace(desc, g)
+
+
+@pytest.mark.parametrize("C,G", [(96, 12), (40, 5), (33, 3), (512, 4)])
+@pytest.mark.parametrize("segments", [None, [0, 10, 3000], 3000])
+def test_sum_in_place_with_a_checkpoint(env, segments, C, G):
+    """Widths at which a row's last lanes have no channels of their own, the sum written over x."""
+    dm, lib, torch = env
+    announce("norm in place, kept", segments, C)
+    c = Case(torch, 3000, C, G, segments, "f32", "bf16", addend=True)
+    x, ck = c.x.clone(), dm.Checkpoint.empty(3000, C, "cuda")
+    y, st = lib.dsmp_group_norm_forward(c.desc(dm), x, c.gamma, c.beta, segments=c.seg(), addend=c.addend, sum_out=x,
+                                        checkpoint=ck)
+    assert torch.equal(x, c.t)
+    c.check_y(y, c.t64, c.check_stats(st, c.t64))
+    q, scale = on.checkpoint(_np(c.t))
+    assert np.array_equal(ck.q.cpu().numpy(), q) and np.array_equal(ck.scale.cpu().numpy(), scale)
+
+
+def test_refuses_rows_too_far_apart(env):
+    dm, lib, torch = env
+    announce("norm row distance")
+    far = torch.zeros(2, (1 << 16) + 1, device="cuda")[:, :32]
+    f = torch.ones(32, device="cuda")
+    for call in (lambda: lib.dsmp_group_norm_forward(dm.norm_desc(32, 4, dm.F32, dm.F32), far, f, f),
+                 lambda: lib.dsmp_checkpoint_store(far)):
+        with pytest.raises(dm.DsmpError) as e:
+            call()
+        assert e.value.status == dm.UNSUPPORTED
