@@ -56,6 +56,8 @@ template <bool VEC>
 constexpr int FWD_TILE = VEC ? 8 : 2;
 template <bool VEC>
 constexpr int BWD_TILE = VEC ? 4 : 1;
+template <bool VEC>
+constexpr int SMALL_TILE = VEC ? 8 : 2;
 
 struct Q8 {};   // tag: a checkpoint as the source of values
 
@@ -93,6 +95,94 @@ struct NormArgs {
   float *dgamma, *dbeta;
   int accumulate, nchunks, nred;
 };
+
+// ------------------------------------------------------------ across lanes
+
+// Sums over lanes by data-parallel moves (a shuffle through LDS takes tens of
+// cycles more, and these come in chains).
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, false);
+}
+template <int CTRL>
+__device__ __forceinline__ float moved(float x) {
+  return __builtin_bit_cast(float, moved<CTRL>(__builtin_bit_cast(uint32_t, x)));
+}
+template <int CTRL>
+__device__ __forceinline__ double moved(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  return __builtin_bit_cast(double, (uint64_t)moved<CTRL>((uint32_t)(u >> 32)) << 32 | moved<CTRL>((uint32_t)u));
+}
+
+// A lane's value and that of a lane O away: rotated within 16 lanes, or the two
+// sides of an exchange of 16 or 32.  Repeated with O = o, 2 o, ... 32 it meets every
+// lane of the same place modulo o once.
+template <typename T>
+struct Two {
+  T a, b;
+};
+template <int O>
+__device__ __forceinline__ Two<uint32_t> across(uint32_t x) {
+  if (O == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return {r[0], r[1]};
+  }
+  if (O == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return {r[0], r[1]};
+  }
+  return {x, moved<0x120 + (O < 16 ? O : 1)>(x)};
+}
+template <int O>
+__device__ __forceinline__ Two<float> across(float x) {
+  const Two<uint32_t> r = across<O>(__builtin_bit_cast(uint32_t, x));
+  return {__builtin_bit_cast(float, r.a), __builtin_bit_cast(float, r.b)};
+}
+template <int O>
+__device__ __forceinline__ Two<double> across(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const Two<uint32_t> l = across<O>((uint32_t)u), h = across<O>((uint32_t)(u >> 32));
+  return {__builtin_bit_cast(double, (uint64_t)h.a << 32 | l.a), __builtin_bit_cast(double, (uint64_t)h.b << 32 | l.b)};
+}
+
+// f(O) for O = first, 2 first, ... 32
+template <typename F>
+__device__ __forceinline__ void levels(int first, F f) {
+  if (first <= 1) f(std::integral_constant<int, 1>{});
+  if (first <= 2) f(std::integral_constant<int, 2>{});
+  if (first <= 4) f(std::integral_constant<int, 4>{});
+  if (first <= 8) f(std::integral_constant<int, 8>{});
+  if (first <= 16) f(std::integral_constant<int, 16>{});
+  if (first <= 32) f(std::integral_constant<int, 32>{});
+}
+template <int O, typename T>
+__device__ __forceinline__ void add_across(T& x) {
+  const Two<T> r = across<O>(x);
+  x = r.a + r.b;
+}
+
+// op over `width` neighbouring lanes (a power of two), in all of them: pairs, fours,
+// then mirrored halves of eight and sixteen, then exchanges.
+template <typename T, typename OP>
+__device__ __forceinline__ T over_lanes(T x, int width, OP op) {
+  if (width > 1) x = op(x, moved<0xb1>(x));
+  if (width > 2) x = op(x, moved<0x4e>(x));
+  if (width > 4) x = op(x, moved<0x141>(x));
+  if (width > 8) x = op(x, moved<0x140>(x));
+  if (width > 16) {
+    const Two<T> r = across<16>(x);
+    x = op(r.a, r.b);
+  }
+  if (width > 32) {
+    const Two<T> r = across<32>(x);
+    x = op(r.a, r.b);
+  }
+  return x;
+}
+template <typename T>
+__device__ __forceinline__ T sum_lanes(T x, int width) {
+  return over_lanes(x, width, [](T a, T b) { return a + b; });
+}
 
 // ------------------------------------------------------------ rows and lanes
 
@@ -337,11 +427,23 @@ struct Keep {
   __device__ __forceinline__ Keep(const NormArgs& a, const Lanes<VEC>& L)
       : q(a.q, a.C, L.c0), s(a.scale, blocks_of(a.C), L.c0 / BLOCK_C), cnt(L.cnt),
         width(std::min(BLOCK_C / CPL<VEC>, L.lpr)), first(L.c0 % BLOCK_C == 0) {}
-  __device__ __forceinline__ void store(int64_t i, int at, bool ok, const float (&v)[CPL<VEC>]) const {
-    uint32_t m = 0;
+  template <int N>
+  __device__ __forceinline__ void store(int64_t i, const Tile<N>& rows, int RL, const float (&v)[N][CPL<VEC>]) const {
+    uint32_t m[N];
 #pragma unroll
-    for (int k = 0; k < CPL<VEC>; ++k) m = max(m, __builtin_bit_cast(uint32_t, v[k]) & 0x7fffffffu);
-    for (int o = 1; o < width; o <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+    for (int t = 0; t < N; ++t) {
+      m[t] = 0;
+#pragma unroll
+      for (int k = 0; k < CPL<VEC>; ++k) m[t] = max(m[t], __builtin_bit_cast(uint32_t, v[t][k]) & 0x7fffffffu);
+      m[t] = over_lanes(m[t], width, [](uint32_t a, uint32_t b) { return max(a, b); });
+    }
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+      if (t * RL >= rows.left) break;
+      one(i, rows.at[t], rows.ok[t], m[t], v[t]);
+    }
+  }
+  __device__ __forceinline__ void one(int64_t i, int at, bool ok, uint32_t m, const float (&v)[CPL<VEC>]) const {
     const float big = __builtin_bit_cast(float, m);
     const bool some = m >= __builtin_bit_cast(uint32_t, TINY), odd = m >= 0x7f800000u;
     const float inv = some && !odd ? 127.0f / big : 0.0f;
@@ -453,7 +555,8 @@ __device__ __forceinline__ void group_sums(const double* s1, const double* s2, i
     double u = 0.0, v = 0.0;
     if (g < G)
       for (int i = l; i < gs; i += tg) u += s1[g * gs + i], v += s2[g * gs + i];
-    for (int o = 1; o < tg; o <<= 1) u += __shfl_xor(u, o, 64), v += __shfl_xor(v, o, 64);
+    u = sum_lanes(u, tg);
+    v = sum_lanes(v, tg);
     if (g < G && l == 0) out(g, u, v);
   }
 }
@@ -532,7 +635,14 @@ struct Moments {
       m2[j] += __builtin_fmaf(d * d, f, q);
     }
   }
-  // the same where a lane has fewer than T rows
+  template <int T>
+  __device__ __forceinline__ void add(const float (&v)[T][CPL<VEC>], const Tile<T>& rows, int RL) {
+    if (rows.left == T * RL)
+      add(v);
+    else
+      add(v, rows.ok);
+  }
+  // where a lane has fewer than T rows
   template <int T>
   __device__ __forceinline__ void add(const float (&v)[T][CPL<VEC>], const bool (&ok)[T]) {
     float c = 0.0f;
@@ -561,15 +671,18 @@ struct Moments {
       m2[j] += __builtin_fmaf(d * d, f, q);
     }
   }
-  // joins the lane `o` away
-  __device__ __forceinline__ void join(int o) {
-    const float nb = __shfl_xor(n, o, 64), nn = n + nb, w = nn > 0.0f ? nb / nn : 0.0f, f = n * w * U;
+  // joins the lane O away
+  template <int O>
+  __device__ __forceinline__ void join() {
+    const Two<float> c = across<O>(n);
+    const float nn = c.a + c.b, w = nn > 0.0f ? c.b / nn : 0.0f, f = c.a * w * U;
     n = nn;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const float mb = __shfl_xor(mean[j], o, 64), qb = __shfl_xor(m2[j], o, 64), d = mb - mean[j];
-      mean[j] = __builtin_fmaf(d, w, mean[j]);
-      m2[j] += __builtin_fmaf(d * d, f, qb);
+      const Two<float> m = across<O>(mean[j]), q = across<O>(m2[j]);
+      const float d = m.b - m.a;
+      mean[j] = __builtin_fmaf(d, w, m.a);
+      m2[j] = q.a + __builtin_fmaf(d * d, f, q.b);
     }
   }
 };
@@ -585,44 +698,27 @@ struct SumsLds {
   float u[W * C], v[W * C], n[W];
 };
 
-// The workgroup's sums over rows [r, e) for every group: the mean-weighted count and
-// the squares about zero in float64, to out(g, u, v).  Adds the addend and
-// writes the sum and the checkpoint on the way.
-template <int W, typename T, bool VEC, bool ADD, typename OUT>
-__device__ __forceinline__ void moments_of(const NormArgs& a, const Lanes<VEC>& L, int64_t r, int64_t e, SumsLds<W>& sh, OUT out) {
-  constexpr int U = UNIT<VEC>, N = CPL<VEC> / U, TILE = FWD_TILE<VEC>, wu = SumsLds<W>::C / U;
-  const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63, units = a.C / U;
-  Moments<VEC> m;
-  const Stream<T, VEC, ADD> in(a, L);
-  const Keep<VEC> keep(a, L);
-  over_rows<TILE>(L, r, e, [&](int64_t i, const Tile<TILE>& rows) {
-    float v[TILE][CPL<VEC>];
-    in.load(i, rows, v);
-    if (a.ck) {
-#pragma unroll
-      for (int t = 0; t < TILE; ++t)
-        if (t * L.RL < rows.left) keep.store(i, rows.at[t], rows.ok[t], v[t]);
-    }
-    if (rows.left == TILE * L.RL)
-      m.add(v);
-    else
-      m.add(v, rows.ok);
-  });
-  for (int o = L.lpr; o < 64; o <<= 1) m.join(o);
+// The workgroup's moments joined: for every group the sum of all values and of
+// their squares about zero, in float64, to out(g, u, v).
+template <int W, bool VEC, typename OUT>
+__device__ __forceinline__ void join_moments(const NormArgs& a, const Lanes<VEC>& L, Moments<VEC>& m, SumsLds<W>& sh,
+                                             OUT out) {
+  constexpr int U = UNIT<VEC>, N = CPL<VEC> / U, wu = SumsLds<W>::C / U;
+  const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63, c = threadIdx.x, units = a.C / U;
+  levels(L.lpr, [&](auto o) { m.template join<decltype(o)::value>(); });
   if (lane < L.lpr) {
 #pragma unroll
     for (int j = 0; j < N; ++j) sh.u[wid * wu + L.lr * N + j] = m.mean[j], sh.v[wid * wu + L.lr * N + j] = m.m2[j];
     if (lane == 0) sh.n[wid] = m.n;
   }
   __syncthreads();
-  const int c = threadIdx.x;
   if (c < units) {
     double u = 0.0, v = 0.0;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      const double mw = sh.u[w * wu + c], nw = (double)(sh.n[w] * U);
-      u += nw * mw;
-      v += (double)sh.v[w * wu + c] + nw * mw * mw;
+      const double mw = sh.u[w * wu + c], nw = (double)(sh.n[w] * U), t = nw * mw;
+      u += t;
+      v += __builtin_fma(t, mw, (double)sh.v[w * wu + c]);
     }
     sh.s1[c] = u;
     sh.s2[c] = v;
@@ -635,6 +731,9 @@ template <typename T, bool VEC, bool ADD>
 __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_stats(NormArgs a) {
   __shared__ SumsLds<NW> sh;
   const Lanes<VEC> L(a.lg, a.C, NT);
+  const Stream<T, VEC, ADD> in(a, L);
+  const Keep<VEC> keep(a, L);
+  constexpr int TILE = FWD_TILE<VEC>;
   const int64_t r0 = (int64_t)blockIdx.x * a.R, r1 = std::min<int64_t>(r0 + a.R, a.n);
   int s = seg_find(a, r0);
   for (int64_t r = r0; r < r1; ++s) {
@@ -642,7 +741,14 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_stats(NormArgs a) {
     if (e <= r) continue;
     const double inv = 1.0 / ((double)(e - r) * a.gs);
     float2* part = a.part + ((int64_t)blockIdx.x + s) * a.G;
-    moments_of<NW, T, VEC, ADD>(a, L, r, e, sh, [&](int g, double u, double v) {
+    Moments<VEC> m;
+    over_rows<TILE>(L, r, e, [&](int64_t i, const Tile<TILE>& rows) {
+      float v[TILE][CPL<VEC>];
+      in.load(i, rows, v);
+      if (a.ck) keep.store(i, rows, L.RL, v);
+      m.add(v, rows, L.RL);
+    });
+    join_moments(a, L, m, sh, [&](int g, double u, double v) {
       const double mean = u * inv;
       part[g] = make_float2((float)mean, (float)fmax(v - u * mean, 0.0));
     });
@@ -678,7 +784,10 @@ __device__ __forceinline__ void join_pieces(const NormArgs& a, int s, int64_t b,
       term(part[j * a.G], (double)(int32_t)rows, u, v);
     }
   }
-  for (int o = gp; o < 64; o <<= 1) u += __shfl_xor(u, o, 64), v += __shfl_xor(v, o, 64);
+  levels(gp, [&](auto o) {
+    add_across<decltype(o)::value>(u);
+    add_across<decltype(o)::value>(v);
+  });
   if (gp >= 64) {
     // P sums of each group, gp apart
     sh[threadIdx.x] = u;
@@ -774,9 +883,11 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_apply(NormArgs a) {
   }
 }
 
-// One workgroup to a segment: both passes in one launch.
+// One workgroup to a segment whose rows are one tile: they stay in registers
+// between the statistics and the result.
 template <typename T, bool VEC, bool ADD, int ACT>
 __global__ __launch_bounds__(SNT) void k_norm_small(NormArgs a) {
+  constexpr int TILE = SMALL_TILE<VEC>;
   __shared__ SumsLds<SNW> sh;
   __shared__ float2 st[MAX_C];
   const Lanes<VEC> L(a.lg, a.C, SNT);
@@ -786,19 +897,31 @@ __global__ __launch_bounds__(SNT) void k_norm_small(NormArgs a) {
     for (int g = threadIdx.x; g < a.G; g += SNT) stats_of(a, s)[g] = make_float2(0.0f, 0.0f);
     return;
   }
-  const Groups<VEC> groups(a, L.c0);
-  float gamma[CPL<VEC>], beta[CPL<VEC>];
+  const Tile<TILE> rows(L, (int)(e - b));
+  float v[TILE][CPL<VEC>], gamma[CPL<VEC>], beta[CPL<VEC>];
+  Stream<T, VEC, ADD>(a, L).load(b, rows, v);
   params<VEC>(a, L, gamma, beta);
+  const Groups<VEC> groups(a, L.c0);
   const double inv = 1.0 / ((double)(e - b) * a.gs);
-  moments_of<SNW, T, VEC, ADD>(a, L, b, e, sh, [&](int g, double u, double v) {
-    st[g] = finish(u, v, inv, a.eps);
+  Moments<VEC> m;
+  m.add(v, rows, L.RL);
+  if (a.ck) Keep<VEC>(a, L).store(b, rows, L.RL, v);
+  join_moments(a, L, m, sh, [&](int g, double u, double q) {
+    st[g] = finish(u, q, inv, a.eps);
     stats_of(a, s)[g] = st[g];
   });
   __syncthreads();
   PerUnit<VEC> mean, rstd;
   groups.read(st, mean, rstd);
-  if (ADD) a.x = a.sum, a.ldx = a.lds;   // every lane reads back what it wrote itself
-  apply_rows<T, VEC, ACT>(a, L, b, e, mean, rstd, gamma, beta);
+  const Result<VEC> out(a, L);
+#pragma unroll
+  for (int t = 0; t < TILE; ++t) {
+    if (t * L.RL >= rows.left) break;
+#pragma unroll
+    for (int k = 0; k < CPL<VEC>; ++k)
+      v[t][k] = activate<ACT>(__builtin_fmaf(v[t][k] - mean[k], rstd[k] * gamma[k], beta[k]));
+    if (rows.ok[t]) out.store(b, rows.at[t], v[t]);
+  }
 }
 
 // ------------------------------------------------------------ backward
@@ -819,37 +942,19 @@ struct Norm {
   }
 };
 
-// The workgroup's sums over rows [r, e): per channel w and w xn (to chan(c, u, v), by
-// the thread that has the number c), per group gamma times both (to out(g, u, v)).
-template <int W, typename T, bool VEC, int ACT, typename CHAN, typename OUT>
-__device__ __forceinline__ void grad_sums(const NormArgs& a, const Lanes<VEC>& L, const Norm<VEC>& nm, int64_t r, int64_t e,
-                                          SumsLds<W>& sh, CHAN chan, OUT out) {
-  constexpr int TILE = BWD_TILE<VEC>, w8 = SumsLds<W>::C;
+// The lanes' sums u of w and v of w xn joined over the workgroup: per channel to
+// chan(c, u, v), by the thread that has the number c; per group, times gamma, to
+// out(g, u, v).
+template <int W, bool VEC, typename CHAN, typename OUT>
+__device__ __forceinline__ void join_sums(const NormArgs& a, const Lanes<VEC>& L, float (&u)[CPL<VEC>],
+                                          float (&v)[CPL<VEC>], SumsLds<W>& sh, CHAN chan, OUT out) {
+  constexpr int w8 = SumsLds<W>::C;
   const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63, c = threadIdx.x;
-  float u[CPL<VEC>] = {}, v[CPL<VEC>] = {};
-  const Source<T, VEC> in(a, L);
-  const Mat<float> gy(a.gy, a.ldgy, L.at(a.C));
-  over_rows<TILE>(L, r, e, [&](int64_t i, const Tile<TILE>& rows) {
-    float t[TILE][CPL<VEC>], w[TILE][CPL<VEC>];
+  levels(L.lpr, [&](auto o) {
 #pragma unroll
-    for (int j = 0; j < TILE; ++j) {
-      in.load(i, rows.at[j], t[j]);
-      load_row<VEC>(gy.row(i, rows.at[j]), L.cnt, w[j]);
-    }
-#pragma unroll
-    for (int j = 0; j < TILE; ++j) {
-      if (j * L.RL >= rows.left) break;
-      nm.template weigh<ACT>(t[j], w[j]);
-      if (rows.ok[j]) {
-#pragma unroll
-        for (int k = 0; k < CPL<VEC>; ++k) u[k] += w[j][k], v[k] = __builtin_fmaf(w[j][k], t[j][k], v[k]);
-      }
-    }
+    for (int k = 0; k < CPL<VEC>; ++k) add_across<decltype(o)::value>(u[k]), add_across<decltype(o)::value>(v[k]);
   });
-  for (int o = L.lpr; o < 64; o <<= 1) {
-#pragma unroll
-    for (int k = 0; k < CPL<VEC>; ++k) u[k] += __shfl_xor(u[k], o, 64), v[k] += __shfl_xor(v[k], o, 64);
-  }
+  const double gc = c < a.C && a.gamma ? a.gamma[c] : 1.0f;
   if (lane < L.lpr) {
 #pragma unroll
     for (int k = 0; k < CPL<VEC>; ++k) sh.u[wid * w8 + L.c0 + k] = u[k], sh.v[wid * w8 + L.c0 + k] = v[k];
@@ -859,13 +964,27 @@ __device__ __forceinline__ void grad_sums(const NormArgs& a, const Lanes<VEC>& L
     double x = 0.0, y = 0.0;
 #pragma unroll
     for (int w = 0; w < W; ++w) x += sh.u[w * w8 + c], y += sh.v[w * w8 + c];
-    const double gc = a.gamma ? a.gamma[c] : 1.0f;
     chan(c, x, y);
     sh.s1[c] = gc * x;
     sh.s2[c] = gc * y;
   }
   __syncthreads();
   group_sums<W>(sh.s1, sh.s2, a.G, a.gs, out);
+}
+
+// w and xn of a tile in place of grad_y and t, added to the lane's sums
+template <int ACT, bool VEC, int N>
+__device__ __forceinline__ void weigh_tile(const Norm<VEC>& nm, const Tile<N>& rows, int RL, float (&t)[N][CPL<VEC>],
+                                           float (&w)[N][CPL<VEC>], float (&u)[CPL<VEC>], float (&v)[CPL<VEC>]) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    if (j * RL >= rows.left) break;
+    nm.template weigh<ACT>(t[j], w[j]);
+    if (rows.ok[j]) {
+#pragma unroll
+      for (int k = 0; k < CPL<VEC>; ++k) u[k] += w[j][k], v[k] = __builtin_fmaf(w[j][k], t[j][k], v[k]);
+    }
+  }
 }
 
 // First pass: per chunk and segment the groups' sums, per chunk the channels'.
@@ -877,6 +996,9 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_sums(NormArgs a) {
   const Groups<VEC> groups(a, L.c0);
   Norm<VEC> nm;
   params<VEC>(a, L, nm.gamma, nm.beta);
+  const Source<T, VEC> in(a, L);
+  const Mat<float> gy(a.gy, a.ldgy, L.at(a.C));
+  constexpr int TILE = BWD_TILE<VEC>;
   double cu = 0.0, cv = 0.0;
   int s = seg_find(a, r0);
   for (int64_t r = r0; r < r1; ++s) {
@@ -884,8 +1006,18 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_sums(NormArgs a) {
     if (e <= r) continue;
     groups.read(stats_of(a, s), nm.mean, nm.rstd);
     float2* part = a.part + ((int64_t)blockIdx.x + s) * a.G;
-    grad_sums<NW, T, VEC, ACT>(
-        a, L, nm, r, e, sh, [&](int, double x, double y) { cu += x, cv += y; },
+    float u[CPL<VEC>] = {}, v[CPL<VEC>] = {};
+    over_rows<TILE>(L, r, e, [&](int64_t i, const Tile<TILE>& rows) {
+      float t[TILE][CPL<VEC>], w[TILE][CPL<VEC>];
+#pragma unroll
+      for (int j = 0; j < TILE; ++j) {
+        in.load(i, rows.at[j], t[j]);
+        load_row<VEC>(gy.row(i, rows.at[j]), L.cnt, w[j]);
+      }
+      weigh_tile<ACT>(nm, rows, L.RL, t, w, u, v);
+    });
+    join_sums(
+        a, L, u, v, sh, [&](int, double x, double y) { cu += x, cv += y; },
         [&](int g, double x, double y) { part[g] = make_float2((float)x, (float)y); });
     __syncthreads();
     r = e;
@@ -980,29 +1112,47 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_dx(NormArgs a) {
   }
 }
 
-// One segment, one workgroup: both passes and the parameters' gradients.
+// One segment of one tile of rows, one workgroup: w and xn stay in registers.
 template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(SNT) void k_norm_bwd_small(NormArgs a) {
+  constexpr int TILE = SMALL_TILE<VEC>;
   __shared__ SumsLds<SNW> sh;
   __shared__ float2 st[MAX_C];
   const Lanes<VEC> L(a.lg, a.C, SNT);
+  const Tile<TILE> rows(L, (int)a.n);
+  const Source<T, VEC> in(a, L);
+  const Mat<float> gy(a.gy, a.ldgy, L.at(a.C)), ga(a.ga, a.ldga, L.at(a.C)), gx(a.gx, a.ldgx, L.c0);
+  float t[TILE][CPL<VEC>], w[TILE][CPL<VEC>], u[CPL<VEC>] = {}, v[CPL<VEC>] = {};
+#pragma unroll
+  for (int j = 0; j < TILE; ++j) {
+    in.load(0, rows.at[j], t[j]);
+    load_row<VEC>(gy.row(0, rows.at[j]), L.cnt, w[j]);
+  }
   const Groups<VEC> groups(a, L.c0);
   Norm<VEC> nm;
   params<VEC>(a, L, nm.gamma, nm.beta);
   groups.read(stats_of(a, 0), nm.mean, nm.rstd);
+  weigh_tile<ACT>(nm, rows, L.RL, t, w, u, v);
   const double inv = 1.0 / ((double)a.n * a.gs);
-  grad_sums<SNW, T, VEC, ACT>(
-      a, L, nm, 0, a.n, sh,
+  join_sums(
+      a, L, u, v, sh,
       [&](int c, double x, double y) {
         if (!a.dbeta) return;
         a.dbeta[c] = a.accumulate ? a.dbeta[c] + (float)x : (float)x;
         a.dgamma[c] = a.accumulate ? a.dgamma[c] + (float)y : (float)y;
       },
-      [&](int g, double u, double v) { st[g] = make_float2((float)(u * inv), (float)(v * inv)); });
+      [&](int g, double x, double y) { st[g] = make_float2((float)(x * inv), (float)(y * inv)); });
   __syncthreads();
   PerUnit<VEC> A, B;
   groups.read(st, A, B);
-  grad_rows<T, VEC, ACT>(a, L, nm, A, B, 0, a.n);
+#pragma unroll
+  for (int j = 0; j < TILE; ++j) {
+    if (j * L.RL >= rows.left) break;
+    float g[CPL<VEC>] = {};
+    if (a.ga) load_row<VEC>(ga.row(0, rows.at[j]), L.cnt, g);
+    grad_row(nm, A, B, w[j], t[j], g);
+    if (rows.ok[j]) store_row<VEC>(gx.row(0, rows.at[j]), L.cnt, g);
+  }
 }
 
 // dbeta and dgamma alone (rows as segments, no rows at all)
@@ -1043,7 +1193,7 @@ struct RowGroups {
 #pragma unroll
       for (int j = 1; j < N; ++j) t += s.v[j];
       t = L.cnt > 0 ? t : 0.0f;
-      for (int o = 1; o < width; o <<= 1) t += __shfl_xor(t, o, 64);
+      t = sum_lanes(t, width);
 #pragma unroll
       for (int j = 0; j < N; ++j) s.v[j] = t;
     } else if (width < 0) {
@@ -1082,9 +1232,10 @@ __global__ __launch_bounds__(RNT) void k_norm_rows(NormArgs a) {
   for (int64_t i = (int64_t)blockIdx.x * L.RL; i < a.n; i += (int64_t)gridDim.x * L.RL) {
     if (i + L.rl >= a.n) return;
     float t[1][CPL<VEC>], q[CPL<VEC>];
-    in.load(i, Tile<1>(L, L.RL), t);
+    const Tile<1> row(L, L.RL);
+    in.load(i, row, t);
     float(&v)[CPL<VEC>] = t[0];
-    if (a.ck) keep.store(i, L.rl, true, v);
+    if (a.ck) keep.store(i, row, L.RL, t);
     PerUnit<VEC> mean = R.sum(a, L, v), rstd;
 #pragma unroll
     for (int j = 0; j < N; ++j) mean.v[j] *= f;
@@ -1167,10 +1318,10 @@ __global__ __launch_bounds__(RNT) void k_norm_rows_bwd(NormArgs a) {
     store_row<VEC>(gx.row(i, L.rl), L.cnt, g);
   }
   if (!a.part_c) return;
-  for (int o = L.lpr; o < 64; o <<= 1) {
+  levels(L.lpr, [&](auto o) {
 #pragma unroll
-    for (int k = 0; k < CPL<VEC>; ++k) u[k] += __shfl_xor(u[k], o, 64), v[k] += __shfl_xor(v[k], o, 64);
-  }
+    for (int k = 0; k < CPL<VEC>; ++k) add_across<decltype(o)::value>(u[k]), add_across<decltype(o)::value>(v[k]);
+  });
   __syncthreads();
   const int w8 = L.lpr * CPL<VEC>, wid = threadIdx.x >> 6;
   if ((threadIdx.x & 63) < (unsigned)L.lpr) {
@@ -1195,9 +1346,9 @@ __global__ __launch_bounds__(RNT) void k_ckpt_store(NormArgs a) {
   const Keep<VEC> keep(a, L);
   for (int64_t i = (int64_t)blockIdx.x * L.RL; i < a.n; i += (int64_t)gridDim.x * L.RL) {
     if (i + L.rl >= a.n) return;
-    float v[CPL<VEC>];
-    in.load(i, L.rl, v);
-    keep.store(i, L.rl, true, v);
+    float v[1][CPL<VEC>];
+    in.load(i, L.rl, v[0]);
+    keep.store(i, Tile<1>(L, L.RL), L.RL, v);
   }
 }
 
@@ -1323,13 +1474,12 @@ bool whole(const NormArgs& a) {
   return a.C <= MAX_C / 2 && a.gs % 4 == 0 && aligned(a.gamma, 0, 4) && aligned(a.beta, 0, 4);
 }
 
-// One launch with a workgroup to a segment: where all the rows are at most
-// SMALL_STEPS steps of one workgroup, however they are dealt to the segments (and
-// its LDS stays within 64 KB).
-#ifndef SMALL_STEPS
-constexpr int SMALL_STEPS = 8;
-#endif
-bool small(const NormArgs& a) { return a.C <= MAX_C / 2 && a.n <= (int64_t)SMALL_STEPS * (SNT >> a.lg); }
+// One launch with a workgroup to a segment: where all the rows are at most one
+// tile of a workgroup, however they are dealt to the segments (and its LDS
+// stays within 64 KB).
+bool small(const NormArgs& a, bool vec) {
+  return a.C <= MAX_C / 2 && a.n <= (int64_t)(vec ? SMALL_TILE<true> : SMALL_TILE<false>) * (SNT >> a.lg);
+}
 
 template <typename F>
 void by_bool(bool b, F f) {
@@ -1411,7 +1561,7 @@ extern "C" dsmp_status dsmp_group_norm_forward(dsmp_handle* h, const dsmp_norm_d
           by_bool(addend, [&](auto ad) {
             DSMP_GO((k_norm_rows<T, V, decltype(ad)::value, ACT>), row_grid(h, a, 16), RNT, 0);
           });
-        } else if (small(a)) {
+        } else if (small(a, vec)) {
           by_bool(addend, [&](auto ad) {
             DSMP_GO((k_norm_small<T, V, decltype(ad)::value, ACT>), a.n_seg, SNT, 0);
           });
@@ -1513,7 +1663,7 @@ extern "C" dsmp_status dsmp_group_norm_backward(dsmp_handle* h, const dsmp_norm_
           a.nchunks = (int)grid;
           DSMP_GO((k_norm_rows_bwd<T, V, ACT>), grid, RNT, 0);
           if (nred) DSMP_GO(k_norm_columns, nred, SNT, 0);
-        } else if (small(a) && a.n_seg == 1) {
+        } else if (small(a, vec) && a.n_seg == 1) {
           DSMP_GO((k_norm_bwd_small<T, V, ACT>), 1, SNT, 0);
         } else {
           DSMP_GO((k_norm_bwd_sums<T, V, ACT>), a.nchunks, NT, 0);
