@@ -172,6 +172,14 @@ _SIG = {
                                          ctypes.POINTER(ctypes.c_int64)]),
 }
 
+# address of the current stream of a device, without a Stream object around it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _current_stream(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream if _raw_stream is None else _raw_stream(index)
+
+
 _lib = None
 
 
@@ -253,6 +261,8 @@ class Dsmp:
         self._check(self.lib.dsmp_create(ctypes.byref(h), device), None)
         self.h = h
         self._ws = {}
+        self._index = device
+        self._norm_sizes = {}
 
     def close(self):
         if getattr(self, "h", None) is not None:
@@ -533,28 +543,32 @@ class Dsmp:
         return loss, grad
 
     # ------------------------------------------------------------ checkpoints in 8 bits and group norm
-    def _rows(self, t, name, n, channels, dtype):
-        """(address, row distance) of a matrix [n, channels] whose rows are contiguous."""
-        if not (isinstance(t, torch.Tensor) and t.device == self.device and t.dtype == dtype and t.dim() == 2
-                and t.shape[0] == n and t.shape[1] == channels):
-            raise DsmpError(INVALID_ARG, "%s: a %s [%d, %d] on %s is needed" % (name, dtype, n, channels, self.device))
-        ld = t.stride(0) if n > 1 else channels
-        if (channels > 1 and t.stride(1) != 1) or ld < channels:
+    # Small inputs take less time on the GPU than a call takes here: the checks
+    # look at each tensor once, sizes are asked for once.
+    def _rows(self, t, name, shape, dtype):
+        """(address, row distance) of a matrix whose rows are contiguous."""
+        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape
+                and t.get_device() == self._index):
+            raise DsmpError(INVALID_ARG, "%s: a %s %s on %s is needed" % (name, dtype, list(shape), self.device))
+        ld, one = t.stride()
+        if shape[0] <= 1:
+            ld = shape[1]
+        if ld < shape[1] or (one != 1 and shape[1] > 1):
             raise DsmpError(INVALID_ARG, "%s: rows must be contiguous and not overlap" % name)
         return t.data_ptr(), ld
 
     def _flat(self, t, name, shape, dtype=torch.float32):
         """Address of a contiguous array of a shape."""
-        if not (isinstance(t, torch.Tensor) and t.device == self.device and t.dtype == dtype
-                and tuple(t.shape) == shape and t.is_contiguous()):
+        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.is_contiguous()
+                and t.get_device() == self._index):
             raise DsmpError(INVALID_ARG, "%s: a contiguous %s %s on %s is needed" % (name, dtype, list(shape), self.device))
         return t.data_ptr()
 
-    def _checkpoint(self, ck, n, channels):
+    def _checkpoint(self, ck, shape):
         if not isinstance(ck, Checkpoint):
             raise DsmpError(INVALID_ARG, "a Checkpoint is needed")
-        return CCheckpoint(self._flat(ck.q, "q", (n, channels), torch.int8),
-                           self._flat(ck.scale, "scale", (n, (channels + 63) // 64)))
+        return CCheckpoint(self._flat(ck.q, "q", shape, torch.int8),
+                           self._flat(ck.scale, "scale", (shape[0], (shape[1] + 63) // 64)))
 
     def _segments(self, n, segments):
         if segments is None:
@@ -567,37 +581,47 @@ class Dsmp:
         return (None if gamma is None else self._flat(gamma, "gamma", (C,)),
                 None if beta is None else self._flat(beta, "beta", (C,)))
 
-    def _norm_ws(self, desc, seg, backward):
-        """Binds the current stream; the scratch buffer that its calls share."""
-        f, b = ctypes.c_size_t(), ctypes.c_size_t()
-        self._check(self.lib.dsmp_group_norm_workspace(ctypes.byref(desc), ctypes.byref(seg), ctypes.byref(f),
-                                                       ctypes.byref(b)), None)
-        s = torch.cuda.current_stream(self.device).cuda_stream
+    def _bind_current(self):
+        s = _current_stream(self._index)
         self._check(self.lib.dsmp_set_stream(self.h, s), self.h)
-        return self.workspace(("norm", s), b.value if backward else f.value)
+        return s
+
+    def _norm_ws(self, desc, seg, backward):
+        """Binds the current stream; address and size of the scratch buffer that its calls share."""
+        key = (desc.channels, desc.groups, seg.n, seg.n_seg, seg.ptr is None)
+        sizes = self._norm_sizes.get(key)
+        if sizes is None:
+            f, b = ctypes.c_size_t(), ctypes.c_size_t()
+            self._check(self.lib.dsmp_group_norm_workspace(ctypes.byref(desc), ctypes.byref(seg), ctypes.byref(f),
+                                                           ctypes.byref(b)), None)
+            if len(self._norm_sizes) >= 1024:
+                self._norm_sizes.clear()
+            sizes = self._norm_sizes[key] = (f.value, b.value)
+        ws = self.workspace(("norm", self._bind_current()), sizes[backward])
+        return ws.data_ptr(), ws.numel()
 
     def dsmp_checkpoint_store(self, x: torch.Tensor, out: Optional[Checkpoint] = None) -> Checkpoint:
         """Keep the rows of x (float32 or bfloat16 [n, channels]) in 8 bits."""
         if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.dtype not in _CODE:
             raise DsmpError(INVALID_ARG, "x: a float32 or bfloat16 matrix is needed")
-        n, C = x.shape
-        p, ld = self._rows(x, "x", n, C, x.dtype)
+        n, C = shape = x.shape
+        p, ld = self._rows(x, "x", shape, x.dtype)
         out = Checkpoint.empty(n, C, self.device) if out is None else out
-        ck = self._checkpoint(out, n, C)
-        self._bind()
+        ck = self._checkpoint(out, shape)
+        self._bind_current()
         self._check(self.lib.dsmp_checkpoint_store(self.h, p, _CODE[x.dtype], ld, n, C, ctypes.byref(ck)), self.h)
         return out
 
     def dsmp_checkpoint_load(self, ck: Checkpoint, y: Optional[torch.Tensor] = None) -> torch.Tensor:
         """The kept values (float32, or y's type)."""
-        n, C = ck.q.shape
+        n, C = shape = ck.q.shape
         if y is None:
             y = torch.empty(n, C, dtype=torch.float32, device=self.device)
         if y.dtype not in _CODE:
             raise DsmpError(INVALID_ARG, "y: a float32 or bfloat16 matrix is needed")
-        p, ld = self._rows(y, "y", n, C, y.dtype)
-        cck = self._checkpoint(ck, n, C)
-        self._bind()
+        p, ld = self._rows(y, "y", shape, y.dtype)
+        cck = self._checkpoint(ck, shape)
+        self._bind_current()
         self._check(self.lib.dsmp_checkpoint_load(self.h, ctypes.byref(cck), n, C, p, _CODE[y.dtype], ld), self.h)
         return y
 
@@ -610,35 +634,37 @@ class Dsmp:
         sum_out receives t (needed with an addend; x or addend itself may be
         given); checkpoint, if given, receives t in 8 bits."""
         C, n = desc.channels, x.shape[0]
+        rows = (n, C)
         seg = self._segments(n, segments)
         xt, yt = _TORCH.get(desc.x_dtype), _TORCH.get(desc.y_dtype)
-        xp, ldx = self._rows(x, "x", n, C, xt)
-        ap, lda = (None, 0) if addend is None else self._rows(addend, "addend", n, C, xt)
-        sp, lds = (None, 0) if sum_out is None else self._rows(sum_out, "sum_out", n, C, xt)
+        xp, ldx = self._rows(x, "x", rows, xt)
+        ap, lda = (None, 0) if addend is None else self._rows(addend, "addend", rows, xt)
+        sp, lds = (None, 0) if sum_out is None else self._rows(sum_out, "sum_out", rows, xt)
         gp, bp = self._norm_params(C, gamma, beta)
         y = torch.empty(n, C, dtype=yt, device=self.device) if y is None else y
-        yp, ldy = self._rows(y, "y", n, C, yt)
+        yp, ldy = self._rows(y, "y", rows, yt)
         shape = (seg.n_seg, desc.groups, 2)
         stats = torch.empty(shape, dtype=torch.float32, device=self.device) if stats is None else stats
         stp = self._flat(stats, "stats", shape)
-        ck = None if checkpoint is None else self._checkpoint(checkpoint, n, C)
-        ws = self._norm_ws(desc, seg, False)
+        ck = None if checkpoint is None else self._checkpoint(checkpoint, rows)
+        ws, ws_bytes = self._norm_ws(desc, seg, False)
         self._check(self.lib.dsmp_group_norm_forward(self.h, ctypes.byref(desc), ctypes.byref(seg), xp, ldx, ap, lda, sp,
                                                      lds, gp, bp, yp, ldy, stp, None if ck is None else ctypes.byref(ck),
-                                                     ws.data_ptr(), ws.numel()), self.h)
+                                                     ws, ws_bytes), self.h)
         return y, stats
 
     def dsmp_group_norm_restore(self, desc: NormDesc, checkpoint: Checkpoint, stats, gamma, beta, segments=None, y=None):
         """The forward's y again, from the checkpoint of t and the kept statistics."""
         C, n = desc.channels, checkpoint.q.shape[0]
+        rows = (n, C)
         seg = self._segments(n, segments)
         yt = _TORCH.get(desc.y_dtype)
-        ck = self._checkpoint(checkpoint, n, C)
+        ck = self._checkpoint(checkpoint, rows)
         stp = self._flat(stats, "stats", (seg.n_seg, desc.groups, 2))
         gp, bp = self._norm_params(C, gamma, beta)
         y = torch.empty(n, C, dtype=yt, device=self.device) if y is None else y
-        yp, ldy = self._rows(y, "y", n, C, yt)
-        self._bind()
+        yp, ldy = self._rows(y, "y", rows, yt)
+        self._bind_current()
         self._check(self.lib.dsmp_group_norm_restore(self.h, ctypes.byref(desc), ctypes.byref(seg), ctypes.byref(ck), stp,
                                                      gp, bp, yp, ldy), self.h)
         return y
@@ -650,24 +676,25 @@ class Dsmp:
         (which may be grad_x itself) is added to grad_x."""
         kept = isinstance(source, Checkpoint)
         C, n = desc.channels, (source.q if kept else source).shape[0]
+        rows = (n, C)
         seg = self._segments(n, segments)
-        xp, ldx = (None, 0) if kept else self._rows(source, "x", n, C, _TORCH.get(desc.x_dtype))
-        ck = self._checkpoint(source, n, C) if kept else None
+        xp, ldx = (None, 0) if kept else self._rows(source, "x", rows, _TORCH.get(desc.x_dtype))
+        ck = self._checkpoint(source, rows) if kept else None
         stp = self._flat(stats, "stats", (seg.n_seg, desc.groups, 2))
         gp, bp = self._norm_params(C, gamma, beta)
-        dyp, ldgy = self._rows(grad_y, "grad_y", n, C, torch.float32)
-        gap, ldga = (None, 0) if grad_addend is None else self._rows(grad_addend, "grad_addend", n, C, torch.float32)
+        dyp, ldgy = self._rows(grad_y, "grad_y", rows, torch.float32)
+        gap, ldga = (None, 0) if grad_addend is None else self._rows(grad_addend, "grad_addend", rows, torch.float32)
         f32 = dict(dtype=torch.float32, device=self.device)
         grad_x = torch.empty(n, C, **f32) if grad_x is None else grad_x
-        dxp, ldgx = self._rows(grad_x, "grad_x", n, C, torch.float32)
+        dxp, ldgx = self._rows(grad_x, "grad_x", rows, torch.float32)
         if gamma is None:
             grads, dg, db = {}, None, None
         else:
             grads = {"dgamma": torch.empty(C, **f32), "dbeta": torch.empty(C, **f32)} if grads is None else grads
             dg, db = self._flat(grads["dgamma"], "dgamma", (C,)), self._flat(grads["dbeta"], "dbeta", (C,))
-        ws = self._norm_ws(desc, seg, True)
+        ws, ws_bytes = self._norm_ws(desc, seg, True)
         self._check(self.lib.dsmp_group_norm_backward(self.h, ctypes.byref(desc), ctypes.byref(seg), xp, ldx,
                                                       None if ck is None else ctypes.byref(ck), stp, gp, bp, dyp, ldgy,
-                                                      gap, ldga, dxp, ldgx, dg, db, flags, ws.data_ptr(), ws.numel()),
+                                                      gap, ldga, dxp, ldgx, dg, db, flags, ws, ws_bytes),
                     self.h)
         return grad_x, grads

@@ -184,6 +184,20 @@ __device__ __forceinline__ T sum_lanes(T x, int width) {
   return over_lanes(x, width, [](T a, T b) { return a + b; });
 }
 
+// to[t] = x of lane t of the 16 lanes (`wide`) or 8 lanes that a lane is one of
+template <int T>
+__device__ __forceinline__ float from_lane(float x, bool wide) {
+  const float low = moved<0x150 + T>(x);
+  if (wide) return low;
+  const float high = moved<0x158 + T>(x);
+  return threadIdx.x & 8 ? high : low;
+}
+__device__ __forceinline__ void from_lanes(float x, float (&to)[8], bool wide) {
+  to[0] = from_lane<0>(x, wide), to[1] = from_lane<1>(x, wide), to[2] = from_lane<2>(x, wide);
+  to[3] = from_lane<3>(x, wide), to[4] = from_lane<4>(x, wide), to[5] = from_lane<5>(x, wide);
+  to[6] = from_lane<6>(x, wide), to[7] = from_lane<7>(x, wide);
+}
+
 // ------------------------------------------------------------ rows and lanes
 
 // The place of a lane: CPL channels from c0 (cnt of them exist) in row rl of the
@@ -418,15 +432,26 @@ struct Result {
 
 // Writes rows in 8 bits.  64 / CPL lanes (fewer where a row has fewer) hold a block
 // of 64 channels.  Its largest magnitude is found on the bits without the sign,
-// which order as the values do and put a NaN above everything.
+// which order as the values do and put a NaN above everything.  The division of a
+// block is done for all rows of a tile at once, each by another lane of the block.
 template <bool VEC>
 struct Keep {
   Mat<int8_t> q;
   Mat<float> s;
-  int cnt, width, first;
+  int cnt, width;
+  bool first;
   __device__ __forceinline__ Keep(const NormArgs& a, const Lanes<VEC>& L)
       : q(a.q, a.C, L.c0), s(a.scale, blocks_of(a.C), L.c0 / BLOCK_C), cnt(L.cnt),
-        width(std::min(BLOCK_C / CPL<VEC>, L.lpr)), first(L.c0 % BLOCK_C == 0) {}
+        width(std::min(BLOCK_C / CPL<VEC>, L.lpr)), first(L.c0 % BLOCK_C == 0 && L.cnt > 0) {}
+
+  // 127 / big, and the scale, of a block
+  static __device__ __forceinline__ void factors(uint32_t m, float& inv, float& scale) {
+    const float big = __builtin_bit_cast(float, m);
+    const bool some = m >= __builtin_bit_cast(uint32_t, TINY), odd = m >= 0x7f800000u;
+    inv = some && !odd ? 127.0f / big : 0.0f;
+    scale = odd ? __builtin_bit_cast(float, 0x7fc00000u) : some ? big * (1.0f / 127.0f) : 0.0f;
+  }
+
   template <int N>
   __device__ __forceinline__ void store(int64_t i, const Tile<N>& rows, int RL, const float (&v)[N][CPL<VEC>]) const {
     uint32_t m[N];
@@ -437,35 +462,56 @@ struct Keep {
       for (int k = 0; k < CPL<VEC>; ++k) m[t] = max(m[t], __builtin_bit_cast(uint32_t, v[t][k]) & 0x7fffffffu);
       m[t] = over_lanes(m[t], width, [](uint32_t a, uint32_t b) { return max(a, b); });
     }
+    float inv[N], scale[N];
+    bool done = false;
+    if constexpr (N == 8) {
+      done = width >= 8;
+      if (done) {
+        const int l = threadIdx.x & 7;
+        uint32_t mine = m[0];
+#pragma unroll
+        for (int t = 1; t < N; ++t) mine = l == t ? m[t] : mine;
+        float fi, fs;
+        factors(mine, fi, fs);
+        from_lanes(fi, inv, width > 8);
+        from_lanes(fs, scale, width > 8);
+      }
+    }
+    if (!done) {
+#pragma unroll
+      for (int t = 0; t < N; ++t) factors(m[t], inv[t], scale[t]);
+    }
 #pragma unroll
     for (int t = 0; t < N; ++t) {
       if (t * RL >= rows.left) break;
-      one(i, rows.at[t], rows.ok[t], m[t], v[t]);
+      if (rows.ok[t]) one(i, rows.at[t], m[t], inv[t], scale[t], v[t]);
     }
   }
-  __device__ __forceinline__ void one(int64_t i, int at, bool ok, uint32_t m, const float (&v)[CPL<VEC>]) const {
-    const float big = __builtin_bit_cast(float, m);
-    const bool some = m >= __builtin_bit_cast(uint32_t, TINY), odd = m >= 0x7f800000u;
-    const float inv = some && !odd ? 127.0f / big : 0.0f;
-    const float scale = odd ? __builtin_bit_cast(float, 0x7fc00000u) : some ? big * (1.0f / 127.0f) : 0.0f;
-    if (cnt <= 0 || !ok) return;
-    int b[CPL<VEC>];
+
+  // x inv rounded to whole numbers: 1.5 2^23 is added, and the sum's last byte is the
+  // number (a magnitude of at most 127; product and sum are rounded apart)
+  static __device__ __forceinline__ uint32_t whole_number(float x, float inv) {
+#pragma clang fp contract(off)
+    const float p = x * inv;
+    return __builtin_bit_cast(uint32_t, p + 12582912.0f) & 255u;
+  }
+
+  __device__ __forceinline__ void one(int64_t i, int at, uint32_t m, float inv, float scale,
+                                      const float (&v)[CPL<VEC>]) const {
+    uint32_t w[CPL<VEC> / 4];
 #pragma unroll
-    for (int k = 0; k < CPL<VEC>; ++k) {
-      const float t = odd ? 0.0f : __builtin_rintf(v[k] * inv);
-      b[k] = (int)fminf(fmaxf(t, -127.0f), 127.0f);
+    for (int j = 0; j < CPL<VEC> / 4; ++j) {
+      w[j] = whole_number(v[4 * j], inv) | whole_number(v[4 * j + 1], inv) << 8 | whole_number(v[4 * j + 2], inv) << 16 |
+             whole_number(v[4 * j + 3], inv) << 24;
+      w[j] = m >= 0x7f800000u ? 0u : w[j];
     }
     int8_t* p = q.row(i, at);
     if (cnt == CPL<VEC>) {
-      uint32_t w[CPL<VEC> / 4];
-#pragma unroll
-      for (int j = 0; j < CPL<VEC> / 4; ++j)
-        w[j] = (b[4 * j] & 255) | (b[4 * j + 1] & 255) << 8 | (b[4 * j + 2] & 255) << 16 | (uint32_t)b[4 * j + 3] << 24;
       put_words<VEC>(p, w);
     } else if (!VEC) {
 #pragma unroll
       for (int k = 0; k < CPL<VEC>; ++k)
-        if (k < cnt) p[k] = (int8_t)b[k];
+        if (k < cnt) p[k] = (int8_t)(w[k / 4] >> (8 * (k % 4)));
     }
     if (first) *s.row(i, at) = scale;
   }
