@@ -33,11 +33,15 @@ constexpr int NW = NT / 64;
 constexpr int SNT = 1024;       // threads where one workgroup takes a whole segment
 constexpr int SNW = SNT / 64;
 constexpr int RNT = 256;        // threads where each row is a segment, and of the checkpoint passes
-constexpr int MAX_CHUNKS = 512; // chunks of rows that sums are split over
+constexpr int MAX_CHUNKS = 256; // chunks of rows that sums are split over: one for each CU
+constexpr int MAX_PARTS = 512;  // and where there are no sums
+constexpr int ROW_PARTS = 1024; // workgroups whose channel sums are kept where each row is a segment
 constexpr float TINY = 0x1p-100f;
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // VEC, in all that follows: rows are whole aligned groups of four channels, up to
 // 256 of them, and no group of the norm ends inside four.  A lane then holds four
@@ -50,10 +54,11 @@ constexpr int CPL = VEC ? 4 : 8;    // channels per lane
 template <bool VEC>
 constexpr int UNIT = VEC ? 4 : 1;   // channels with the same statistics
 
-// Rows a lane has in flight in the forward passes, and in the backward ones,
-// which hold twice the values of each (fewer where loads have branches).
-template <bool VEC>
-constexpr int FWD_TILE = VEC ? 8 : 2;
+// Steps of rows that a lane has in flight: of the forward passes (eight of a
+// checkpoint, whose loads are a quarter as wide), of the backward ones, and
+// where a whole segment is one tile.  Fewer where loads have branches.
+template <bool VEC, bool Q = false>
+constexpr int FWD_TILE = VEC ? (Q ? 8 : 4) : 2;
 template <bool VEC>
 constexpr int BWD_TILE = VEC ? 4 : 1;
 template <bool VEC>
@@ -68,7 +73,6 @@ struct NormArgs {
   int64_t len;                  // rows of a segment where ptr is null
   const int32_t* ptr;
   int64_t R;                    // rows of a chunk of the summing pass
-  int64_t RA;                   // rows of a workgroup of the second pass
   const void* x;                // T, or int8 of a checkpoint
   int64_t ldx;
   const float* xscale;
@@ -93,7 +97,7 @@ struct NormArgs {
   int64_t ldgx;
   float* part_c;                // [chunk][2][C]: chunk sums of w and w xn
   float *dgamma, *dbeta;
-  int accumulate, nchunks, nred;
+  int accumulate, nchunks;
 };
 
 // ------------------------------------------------------------ across lanes
@@ -234,66 +238,94 @@ struct Mat {
   }
 };
 
-// The rows of a tile: N steps of RL rows, of which the first `left` exist.  Reads
-// take the last row again past it (all loads of a tile go out together, whatever
-// exists); what they bring is not used.
-template <int N>
+// The rows of a tile: N steps of RL rows, all of which exist (FULL) or the first
+// `left`.  Reads then take the last row again past it, and what they bring is not
+// used: all loads of a tile go out together, whatever exists.
+template <int N_, bool FULL_>
 struct Tile {
-  int left, at[N];
-  bool ok[N];
+  static constexpr int N = N_;
+  static constexpr bool FULL = FULL_;
+  int rl, RL, left;
   template <typename LANES>
-  __device__ __forceinline__ Tile(const LANES& L, int left_) : left(left_) {
-#pragma unroll
-    for (int t = 0; t < N; ++t) {
-      const int r = L.rl + t * L.RL;
-      ok[t] = r < left;
-      at[t] = std::min(r, left - 1);
-    }
-  }
+  __device__ __forceinline__ Tile(const LANES& L, int left_) : rl(L.rl), RL(L.RL), left(left_) {}
+  // step t's rows: the lane's is at(t) past first(i, t)
+  __device__ __forceinline__ int64_t first(int64_t i, int t) const { return FULL ? i + t * RL : i; }
+  __device__ __forceinline__ int at(int t) const { return FULL ? rl : std::min(rl + t * RL, left - 1); }
+  __device__ __forceinline__ bool ok(int t) const { return FULL || rl + t * RL < left; }
+  __device__ __forceinline__ bool end(int t) const { return !FULL && t * RL >= left; }   // no lane has it
 };
 
-// tile(i, rows of it) over the rows [r, e)
-template <int N, typename LANES, typename F>
-__device__ __forceinline__ void over_rows(const LANES& L, int64_t r, int64_t e, F tile) {
-  for (int64_t i = r; i < e; i += N * L.RL) tile(i, Tile<N>(L, (int)std::min<int64_t>(e - i, N * L.RL)));
+// Keeps loads ahead of the conditions that their values are used under: sunk into
+// them, each would be waited for by itself.
+template <int N, int M>
+__device__ __forceinline__ void arrived(float (&v)[N][M]) {
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int k = 0; k < M; ++k) asm volatile("" : "+v"(v[t][k]));
 }
 
-// N four-byte words from or to any address, or whole aligned ones (VEC)
-template <bool VEC, int N>
+// tile(i, rows of it) over the rows [r, e): whole tiles of N steps, the rest in
+// tiles of half as many
+template <int N, typename LANES, typename F>
+__device__ __forceinline__ void over_rows(const LANES& L, int64_t r, int64_t e, F tile) {
+  constexpr int H = N > 1 ? N / 2 : 1;
+  int64_t i = r;
+  for (; i + N * L.RL <= e; i += N * L.RL) tile(i, Tile<N, true>(L, N * L.RL));
+  for (; i < e; i += H * L.RL) tile(i, Tile<H, false>(L, (int)std::min<int64_t>(e - i, H * L.RL)));
+}
+
+// N four-byte words from or to any address, or whole aligned ones (VEC).  STREAM:
+// with the non-temporal hint, for what is not used again soon.
+template <bool STREAM, typename W>
+__device__ __forceinline__ W get(const void* p) {
+  if constexpr (STREAM)
+    return __builtin_nontemporal_load(static_cast<const W*>(p));
+  else
+    return *static_cast<const W*>(p);
+}
+template <bool STREAM, typename W>
+__device__ __forceinline__ void put(void* p, W w) {
+  if constexpr (STREAM)
+    __builtin_nontemporal_store(w, static_cast<W*>(p));
+  else
+    *static_cast<W*>(p) = w;
+}
+template <bool VEC, bool STREAM, int N>
 __device__ __forceinline__ void get_words(const void* p, uint32_t (&w)[N]) {
-  if (VEC && N == 4) {
-    const uint4 u = *static_cast<const uint4*>(p);
-    w[0] = u.x, w[1] = u.y, w[2 % N] = u.z, w[3 % N] = u.w;
-  } else if (VEC && N == 2) {
-    const uint2 u = *static_cast<const uint2*>(p);
-    w[0] = u.x, w[1 % N] = u.y;
-  } else if (VEC) {
-    w[0] = *static_cast<const uint32_t*>(p);
+  if constexpr (VEC && N == 4) {
+    const u32x4 u = get<STREAM, u32x4>(p);
+    w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+  } else if constexpr (VEC && N == 2) {
+    const u32x2 u = get<STREAM, u32x2>(p);
+    w[0] = u.x, w[1] = u.y;
+  } else if constexpr (VEC) {
+    w[0] = get<STREAM, uint32_t>(p);
   } else {
     __builtin_memcpy(w, p, 4 * N);
   }
 }
-template <bool VEC, int N>
+template <bool VEC, bool STREAM, int N>
 __device__ __forceinline__ void put_words(void* p, const uint32_t (&w)[N]) {
-  if (VEC && N == 4)
-    *static_cast<uint4*>(p) = make_uint4(w[0], w[1 % N], w[2 % N], w[3 % N]);
-  else if (VEC && N == 2)
-    *static_cast<uint2*>(p) = make_uint2(w[0], w[1 % N]);
-  else if (VEC)
-    *static_cast<uint32_t*>(p) = w[0];
+  if constexpr (VEC && N == 4)
+    put<STREAM>(p, (u32x4){w[0], w[1], w[2], w[3]});
+  else if constexpr (VEC && N == 2)
+    put<STREAM>(p, (u32x2){w[0], w[1]});
+  else if constexpr (VEC)
+    put<STREAM>(p, w[0]);
   else
     __builtin_memcpy(p, w, 4 * N);
 }
 
 // cnt: how many of a lane's channels exist (all, fewer in a last lane, none or
 // less past it); not looked at in loads where VEC.
-template <bool VEC>
+template <bool VEC, bool STREAM>
 __device__ __forceinline__ void load_row(const float* p, int cnt, float (&v)[CPL<VEC>]) {
   if (VEC || cnt == CPL<VEC>) {
 #pragma unroll
     for (int j = 0; j < CPL<VEC>; j += 4) {
       uint32_t w[4];
-      get_words<VEC>(p + j, w);
+      get_words<VEC, STREAM>(p + j, w);
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[j + k] = __builtin_bit_cast(float, w[k]);
     }
@@ -302,11 +334,11 @@ __device__ __forceinline__ void load_row(const float* p, int cnt, float (&v)[CPL
     for (int k = 0; k < CPL<VEC>; ++k) v[k] = k < cnt ? p[k] : 0.0f;
   }
 }
-template <bool VEC>
+template <bool VEC, bool STREAM>
 __device__ __forceinline__ void load_row(const __bf16* p, int cnt, float (&v)[CPL<VEC>]) {
   if (VEC || cnt == CPL<VEC>) {
     uint32_t w[CPL<VEC> / 2];
-    get_words<VEC>(p, w);
+    get_words<VEC, STREAM>(p, w);
 #pragma unroll
     for (int k = 0; k < CPL<VEC> / 2; ++k) {
       v[2 * k] = __builtin_bit_cast(float, w[k] << 16);
@@ -318,11 +350,11 @@ __device__ __forceinline__ void load_row(const __bf16* p, int cnt, float (&v)[CP
   }
 }
 // bytes of a checkpoint times their block's scale
-template <bool VEC>
+template <bool VEC, bool STREAM>
 __device__ __forceinline__ void load_row(const int8_t* p, float scale, int cnt, float (&v)[CPL<VEC>]) {
   if (VEC || cnt == CPL<VEC>) {
     uint32_t w[CPL<VEC> / 4];
-    get_words<VEC>(p, w);
+    get_words<VEC, STREAM>(p, w);
 #pragma unroll
     for (int k = 0; k < CPL<VEC>; ++k) v[k] = (float)((int32_t)(w[k / 4] << (24 - 8 * (k % 4))) >> 24) * scale;
   } else {
@@ -331,7 +363,7 @@ __device__ __forceinline__ void load_row(const int8_t* p, float scale, int cnt, 
   }
 }
 
-template <bool VEC>
+template <bool VEC, bool STREAM>
 __device__ __forceinline__ void store_row(float* p, int cnt, const float (&v)[CPL<VEC>]) {
   if (cnt == CPL<VEC>) {
 #pragma unroll
@@ -339,7 +371,7 @@ __device__ __forceinline__ void store_row(float* p, int cnt, const float (&v)[CP
       uint32_t w[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[k] = __builtin_bit_cast(uint32_t, v[j + k]);
-      put_words<VEC>(p + j, w);
+      put_words<VEC, STREAM>(p + j, w);
     }
   } else if (!VEC) {
 #pragma unroll
@@ -347,14 +379,14 @@ __device__ __forceinline__ void store_row(float* p, int cnt, const float (&v)[CP
       if (k < cnt) p[k] = v[k];
   }
 }
-template <bool VEC>
+template <bool VEC, bool STREAM>
 __device__ __forceinline__ void store_row(__bf16* p, int cnt, const float (&v)[CPL<VEC>]) {
   if (cnt == CPL<VEC>) {
     uint32_t w[CPL<VEC> / 2];
 #pragma unroll
     for (int k = 0; k < CPL<VEC> / 2; ++k)
       w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){v[2 * k], v[2 * k + 1]}, bf16x2));
-    put_words<VEC>(p, w);
+    put_words<VEC, STREAM>(p, w);
   } else if (!VEC) {
 #pragma unroll
     for (int k = 0; k < CPL<VEC>; ++k)
@@ -365,17 +397,17 @@ __device__ __forceinline__ void store_row(__bf16* p, int cnt, const float (&v)[C
 __host__ __device__ __forceinline__ int blocks_of(int C) { return (C + BLOCK_C - 1) / BLOCK_C; }
 
 // The values that are normalised: rows of T, or of a checkpoint.
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool STREAM = false>
 struct Source {
   Mat<T> m;
   int cnt;
   __device__ __forceinline__ Source(const NormArgs& a, const Lanes<VEC>& L) : m(a.x, a.ldx, L.at(a.C)), cnt(L.cnt) {}
   __device__ __forceinline__ void load(int64_t i, int at, float (&v)[CPL<VEC>]) const {
-    load_row<VEC>(m.row(i, at), cnt, v);
+    load_row<VEC, STREAM>(m.row(i, at), cnt, v);
   }
 };
-template <bool VEC>
-struct Source<Q8, VEC> {
+template <bool VEC, bool STREAM>
+struct Source<Q8, VEC, STREAM> {
   Mat<int8_t> m;
   Mat<float> s;
   int cnt;
@@ -383,32 +415,36 @@ struct Source<Q8, VEC> {
       : m(a.x, a.C, L.at(a.C)),
         s(a.xscale, blocks_of(a.C), std::min(L.at(a.C), a.C - 1) / BLOCK_C), cnt(L.cnt) {}
   __device__ __forceinline__ void load(int64_t i, int at, float (&v)[CPL<VEC>]) const {
-    load_row<VEC>(m.row(i, at), *s.row(i, at), cnt, v);
+    load_row<VEC, STREAM>(m.row(i, at), *s.row(i, at), cnt, v);
   }
 };
 
 // t = x, or x + addend rounded to T, which is then written to sum.
 template <typename T, bool VEC, bool ADD>
 struct Stream {
-  Source<T, VEC> x;
+  Source<T, VEC, ADD> x;   // with an addend it is the sum that is read again
   Mat<T> add, sum;
   int cnt;
   __device__ __forceinline__ Stream(const NormArgs& a, const Lanes<VEC>& L)
       : x(a, L), add(a.add, a.lda, L.at(a.C)), sum(a.sum, a.lds, L.c0), cnt(L.cnt) {}
-  template <int N>
-  __device__ __forceinline__ void load(int64_t i, const Tile<N>& rows, float (&v)[N][CPL<VEC>]) const {
+  template <int N, bool FULL>
+  __device__ __forceinline__ void load(int64_t i, const Tile<N, FULL>& rows, float (&v)[N][CPL<VEC>]) const {
     float u[N][CPL<VEC>];
 #pragma unroll
     for (int t = 0; t < N; ++t) {
-      x.load(i, rows.at[t], v[t]);
-      if (ADD) load_row<VEC>(add.row(i, rows.at[t]), cnt, u[t]);
+      x.load(rows.first(i, t), rows.at(t), v[t]);
+      if (ADD) load_row<VEC, true>(add.row(rows.first(i, t), rows.at(t)), cnt, u[t]);
+    }
+    if (!FULL) {
+      arrived(v);
+      if (ADD) arrived(u);
     }
     if (ADD) {
 #pragma unroll
       for (int t = 0; t < N; ++t) {
 #pragma unroll
         for (int k = 0; k < CPL<VEC>; ++k) v[t][k] = (float)(T)(v[t][k] + u[t][k]);
-        if (rows.ok[t]) store_row<VEC>(sum.row(i, rows.at[t]), cnt, v[t]);
+        if (rows.ok(t)) store_row<VEC, false>(sum.row(rows.first(i, t), rows.at(t)), cnt, v[t]);   // read again at once
       }
     }
   }
@@ -424,9 +460,9 @@ struct Result {
       : f(a.y, a.ldy, L.c0), b(a.y, a.ldy, L.c0), cnt(L.cnt), bf16(a.y_bf16) {}
   __device__ __forceinline__ void store(int64_t i, int at, const float (&v)[CPL<VEC>]) const {
     if (bf16)
-      store_row<VEC>(b.row(i, at), cnt, v);
+      store_row<VEC, true>(b.row(i, at), cnt, v);
     else
-      store_row<VEC>(f.row(i, at), cnt, v);
+      store_row<VEC, true>(f.row(i, at), cnt, v);
   }
 };
 
@@ -452,8 +488,8 @@ struct Keep {
     scale = odd ? __builtin_bit_cast(float, 0x7fc00000u) : some ? big * (1.0f / 127.0f) : 0.0f;
   }
 
-  template <int N>
-  __device__ __forceinline__ void store(int64_t i, const Tile<N>& rows, int RL, const float (&v)[N][CPL<VEC>]) const {
+  template <int N, bool FULL>
+  __device__ __forceinline__ void store(int64_t i, const Tile<N, FULL>& rows, const float (&v)[N][CPL<VEC>]) const {
     uint32_t m[N];
 #pragma unroll
     for (int t = 0; t < N; ++t) {
@@ -483,8 +519,8 @@ struct Keep {
     }
 #pragma unroll
     for (int t = 0; t < N; ++t) {
-      if (t * RL >= rows.left) break;
-      if (rows.ok[t]) one(i, rows.at[t], m[t], inv[t], scale[t], v[t]);
+      if (rows.end(t)) break;
+      if (rows.ok(t)) one(rows.first(i, t), rows.at(t), m[t], inv[t], scale[t], v[t]);
     }
   }
 
@@ -507,7 +543,7 @@ struct Keep {
     }
     int8_t* p = q.row(i, at);
     if (cnt == CPL<VEC>) {
-      put_words<VEC>(p, w);
+      put_words<VEC, true>(p, w);
     } else if (!VEC) {
 #pragma unroll
       for (int k = 0; k < CPL<VEC>; ++k)
@@ -589,6 +625,20 @@ __device__ __forceinline__ int seg_find(const NormArgs& a, int64_t r) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// f(s, b, e, r, end) for the segments s = [b, e) that have rows among [r0, r1), with
+// those rows [r, end).  Ends with r1 whatever ptr holds, and [r, end) is in [b, e).
+template <typename F>
+__device__ __forceinline__ void over_segments(const NormArgs& a, int64_t r0, int64_t r1, F f) {
+  if (r0 >= r1) return;
+  int s = seg_find(a, r0);
+  for (int64_t r = r0; r < r1; ++s) {
+    const int64_t e = seg_end(a, s), end = std::min<int64_t>(e, r1);
+    if (end <= r) continue;
+    f(s, std::min<int64_t>(seg_begin(a, s), r), e, r, end);
+    r = end;
+  }
+}
+
 // s1, s2: the workgroup's sums per channel (or unit of channels), float64 in LDS.
 // Gives the sums over each group's gs of them to out(g, sum1, sum2), by one lane each.
 template <int W, typename F>
@@ -638,8 +688,8 @@ struct Groups {
 template <bool VEC>
 __device__ __forceinline__ void params(const NormArgs& a, const Lanes<VEC>& L, float (&gamma)[CPL<VEC>], float (&beta)[CPL<VEC>]) {
   if (a.gamma) {
-    load_row<VEC>(a.gamma + L.at(a.C), L.cnt, gamma);
-    load_row<VEC>(a.beta + L.at(a.C), L.cnt, beta);
+    load_row<VEC, false>(a.gamma + L.at(a.C), L.cnt, gamma);
+    load_row<VEC, false>(a.beta + L.at(a.C), L.cnt, beta);
   } else {
 #pragma unroll
     for (int k = 0; k < CPL<VEC>; ++k) gamma[k] = 1.0f, beta[k] = 0.0f;
@@ -681,19 +731,20 @@ struct Moments {
       m2[j] += __builtin_fmaf(d * d, f, q);
     }
   }
-  template <int T>
-  __device__ __forceinline__ void add(const float (&v)[T][CPL<VEC>], const Tile<T>& rows, int RL) {
-    if (rows.left == T * RL)
+  template <int T, bool FULL>
+  __device__ __forceinline__ void add(const float (&v)[T][CPL<VEC>], const Tile<T, FULL>& rows) {
+    if (FULL)
       add(v);
     else
-      add(v, rows.ok);
+      add_some(v, rows);
   }
   // where a lane has fewer than T rows
-  template <int T>
-  __device__ __forceinline__ void add(const float (&v)[T][CPL<VEC>], const bool (&ok)[T]) {
+  template <int T, bool FULL>
+  __device__ __forceinline__ void add_some(const float (&v)[T][CPL<VEC>], const Tile<T, FULL>& rows) {
+    bool ok[T];
     float c = 0.0f;
 #pragma unroll
-    for (int t = 0; t < T; ++t) c += ok[t] ? 1.0f : 0.0f;
+    for (int t = 0; t < T; ++t) ok[t] = rows.ok(t), c += ok[t] ? 1.0f : 0.0f;
     if (c == 0.0f) return;
     const float nn = n + c, w = c / nn, f = n * w * U, inv = 1.0f / (c * U);
     n = nn;
@@ -779,28 +830,23 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_stats(NormArgs a) {
   const Lanes<VEC> L(a.lg, a.C, NT);
   const Stream<T, VEC, ADD> in(a, L);
   const Keep<VEC> keep(a, L);
-  constexpr int TILE = FWD_TILE<VEC>;
-  const int64_t r0 = (int64_t)blockIdx.x * a.R, r1 = std::min<int64_t>(r0 + a.R, a.n);
-  int s = seg_find(a, r0);
-  for (int64_t r = r0; r < r1; ++s) {
-    const int64_t e = std::min<int64_t>(seg_end(a, s), r1);
-    if (e <= r) continue;
+  const int64_t r0 = (int64_t)blockIdx.x * a.R;
+  over_segments(a, r0, std::min<int64_t>(r0 + a.R, a.n), [&](int s, int64_t, int64_t, int64_t r, int64_t e) {
     const double inv = 1.0 / ((double)(e - r) * a.gs);
     float2* part = a.part + ((int64_t)blockIdx.x + s) * a.G;
     Moments<VEC> m;
-    over_rows<TILE>(L, r, e, [&](int64_t i, const Tile<TILE>& rows) {
-      float v[TILE][CPL<VEC>];
+    over_rows<FWD_TILE<VEC>>(L, r, e, [&](int64_t i, const auto& rows) {
+      float v[std::decay_t<decltype(rows)>::N][CPL<VEC>];
       in.load(i, rows, v);
-      if (a.ck) keep.store(i, rows, L.RL, v);
-      m.add(v, rows, L.RL);
+      if (a.ck) keep.store(i, rows, v);
+      m.add(v, rows);
     });
     join_moments(a, L, m, sh, [&](int g, double u, double v) {
       const double mean = u * inv;
       part[g] = make_float2((float)mean, (float)fmax(v - u * mean, 0.0));
     });
     __syncthreads();
-    r = e;
-  }
+  });
 }
 
 // mean and rstd of a group from its sums about zero
@@ -814,12 +860,12 @@ __device__ __forceinline__ float2 finish(double u, double v, double inv, float e
 // Sums over the pieces of segment s (rows [b, e)) for every group: term(piece
 // value, rows of the piece, u, v) adds to two float64 sums; done(g, u, v) is called
 // by one lane of each group.  Consecutive lanes take consecutive groups.
-template <typename TERM, typename DONE>
+template <int W, typename TERM, typename DONE>
 __device__ __forceinline__ void join_pieces(const NormArgs& a, int s, int64_t b, int64_t e, double* sh, TERM term,
                                             DONE done) {
   int lgp = 0;
   while ((1 << lgp) < a.G) ++lgp;
-  const int gp = 1 << lgp, g = threadIdx.x & (gp - 1), p = threadIdx.x >> lgp, P = NT >> lgp;
+  const int gp = 1 << lgp, g = threadIdx.x & (gp - 1), p = threadIdx.x >> lgp, P = (W * 64) >> lgp;
   const int64_t j0 = (uint32_t)b / (uint32_t)a.R, j1 = (uint32_t)(e - 1) / (uint32_t)a.R;
   double u = 0.0, v = 0.0;
   if (g < a.G) {
@@ -837,19 +883,19 @@ __device__ __forceinline__ void join_pieces(const NormArgs& a, int s, int64_t b,
   if (gp >= 64) {
     // P sums of each group, gp apart
     sh[threadIdx.x] = u;
-    sh[NT + threadIdx.x] = v;
+    sh[W * 64 + threadIdx.x] = v;
     __syncthreads();
     if (p == 0 && g < a.G) {
-      for (int i = 1; i < P; ++i) u += sh[i * gp + g], v += sh[NT + i * gp + g];
+      for (int i = 1; i < P; ++i) u += sh[i * gp + g], v += sh[W * 64 + i * gp + g];
       done(g, u, v);
     }
   } else {
     const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    if (lane < gp) sh[wid * 64 + lane] = u, sh[NT + wid * 64 + lane] = v;
+    if (lane < gp) sh[wid * 64 + lane] = u, sh[W * 64 + wid * 64 + lane] = v;
     __syncthreads();
     if (threadIdx.x < (unsigned)a.G) {
 #pragma unroll
-      for (int w = 1; w < NW; ++w) u += sh[w * 64 + g], v += sh[NT + w * 64 + g];
+      for (int w = 1; w < W; ++w) u += sh[w * 64 + g], v += sh[W * 64 + w * 64 + g];
       done(g, u, v);
     }
   }
@@ -863,22 +909,23 @@ template <typename T, bool VEC, int ACT>
 __device__ __forceinline__ void apply_rows(const NormArgs& a, const Lanes<VEC>& L, int64_t r, int64_t end,
                                            const PerUnit<VEC>& mean, const PerUnit<VEC>& rstd, const float (&gamma)[CPL<VEC>],
                                            const float (&beta)[CPL<VEC>]) {
-  constexpr int TILE = FWD_TILE<VEC>;
-  const Source<T, VEC> in(a, L);
+  const Source<T, VEC, !std::is_same<T, Q8>::value> in(a, L);   // their last use, but for a checkpoint
   const Result<VEC> out(a, L);
   float scale[CPL<VEC>];
 #pragma unroll
   for (int k = 0; k < CPL<VEC>; ++k) scale[k] = rstd[k] * gamma[k];
-  over_rows<TILE>(L, r, end, [&](int64_t i, const Tile<TILE>& rows) {
-    float v[TILE][CPL<VEC>];
+  over_rows<FWD_TILE<VEC, std::is_same<T, Q8>::value>>(L, r, end, [&](int64_t i, const auto& rows) {
+    using TL = std::decay_t<decltype(rows)>;
+    float v[TL::N][CPL<VEC>];
 #pragma unroll
-    for (int t = 0; t < TILE; ++t) in.load(i, rows.at[t], v[t]);
+    for (int t = 0; t < TL::N; ++t) in.load(rows.first(i, t), rows.at(t), v[t]);
+    if (!TL::FULL) arrived(v);
 #pragma unroll
-    for (int t = 0; t < TILE; ++t) {
-      if (t * L.RL >= rows.left) break;
+    for (int t = 0; t < TL::N; ++t) {
+      if (rows.end(t)) break;
 #pragma unroll
       for (int k = 0; k < CPL<VEC>; ++k) v[t][k] = activate<ACT>(__builtin_fmaf(v[t][k] - mean[k], scale[k], beta[k]));
-      if (rows.ok[t]) out.store(i, rows.at[t], v[t]);
+      if (rows.ok(t)) out.store(rows.first(i, t), rows.at(t), v[t]);
     }
   });
 }
@@ -891,25 +938,21 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_apply(NormArgs a) {
   __shared__ double sh[2 * NT];
   __shared__ float2 st[MAX_C];
   const Lanes<VEC> L(a.lg, a.C, NT);
-  const int64_t r0 = (int64_t)blockIdx.x * a.RA, r1 = std::min<int64_t>(r0 + a.RA, a.n);
+  const int64_t r0 = (int64_t)blockIdx.x * a.R;
   if (a.merge && blockIdx.x == 0) {
     for (int s = threadIdx.x; s < a.n_seg; s += NT)
       if (seg_end(a, s) <= seg_begin(a, s))
         for (int g = 0; g < a.G; ++g) stats_of(a, s)[g] = make_float2(0.0f, 0.0f);
   }
-  if (r0 >= r1) return;
   const Groups<VEC> groups(a, L.c0);
   float gamma[CPL<VEC>], beta[CPL<VEC>];
   params<VEC>(a, L, gamma, beta);
-  int s = seg_find(a, r0);
-  for (int64_t r = r0; r < r1; ++s) {
-    const int64_t b = seg_begin(a, s), e = seg_end(a, s), end = std::min<int64_t>(e, r1);
-    if (end <= r) continue;
+  over_segments(a, r0, std::min<int64_t>(r0 + a.R, a.n), [&](int s, int64_t b, int64_t e, int64_t r, int64_t end) {
     PerUnit<VEC> mean, rstd;
     if (a.merge) {
       const double inv = 1.0 / ((double)(e - b) * a.gs);
       const bool first = b >= r0;
-      join_pieces(
+      join_pieces<NW>(
           a, s, b, e, sh,
           [&](float2 t, double rows, double& u, double& v) {
             const double m = t.x, k = rows * a.gs;
@@ -925,8 +968,7 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_apply(NormArgs a) {
       groups.read(stats_of(a, s), mean, rstd);
     }
     apply_rows<T, VEC, ACT>(a, L, r, end, mean, rstd, gamma, beta);
-    r = end;
-  }
+  });
 }
 
 // One workgroup to a segment whose rows are one tile: they stay in registers
@@ -943,15 +985,15 @@ __global__ __launch_bounds__(SNT) void k_norm_small(NormArgs a) {
     for (int g = threadIdx.x; g < a.G; g += SNT) stats_of(a, s)[g] = make_float2(0.0f, 0.0f);
     return;
   }
-  const Tile<TILE> rows(L, (int)(e - b));
+  const Tile<TILE, false> rows(L, (int)(e - b));
   float v[TILE][CPL<VEC>], gamma[CPL<VEC>], beta[CPL<VEC>];
   Stream<T, VEC, ADD>(a, L).load(b, rows, v);
   params<VEC>(a, L, gamma, beta);
   const Groups<VEC> groups(a, L.c0);
   const double inv = 1.0 / ((double)(e - b) * a.gs);
   Moments<VEC> m;
-  m.add(v, rows, L.RL);
-  if (a.ck) Keep<VEC>(a, L).store(b, rows, L.RL, v);
+  m.add(v, rows);
+  if (a.ck) Keep<VEC>(a, L).store(b, rows, v);
   join_moments(a, L, m, sh, [&](int g, double u, double q) {
     st[g] = finish(u, q, inv, a.eps);
     stats_of(a, s)[g] = st[g];
@@ -962,11 +1004,11 @@ __global__ __launch_bounds__(SNT) void k_norm_small(NormArgs a) {
   const Result<VEC> out(a, L);
 #pragma unroll
   for (int t = 0; t < TILE; ++t) {
-    if (t * L.RL >= rows.left) break;
+    if (rows.end(t)) break;
 #pragma unroll
     for (int k = 0; k < CPL<VEC>; ++k)
       v[t][k] = activate<ACT>(__builtin_fmaf(v[t][k] - mean[k], rstd[k] * gamma[k], beta[k]));
-    if (rows.ok[t]) out.store(b, rows.at[t], v[t]);
+    if (rows.ok(t)) out.store(b, rows.at(t), v[t]);
   }
 }
 
@@ -1019,14 +1061,18 @@ __device__ __forceinline__ void join_sums(const NormArgs& a, const Lanes<VEC>& L
 }
 
 // w and xn of a tile in place of grad_y and t, added to the lane's sums
-template <int ACT, bool VEC, int N>
-__device__ __forceinline__ void weigh_tile(const Norm<VEC>& nm, const Tile<N>& rows, int RL, float (&t)[N][CPL<VEC>],
+template <int ACT, bool VEC, int N, bool FULL>
+__device__ __forceinline__ void weigh_tile(const Norm<VEC>& nm, const Tile<N, FULL>& rows, float (&t)[N][CPL<VEC>],
                                            float (&w)[N][CPL<VEC>], float (&u)[CPL<VEC>], float (&v)[CPL<VEC>]) {
+  if (!FULL) {
+    arrived(t);
+    arrived(w);
+  }
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    if (j * RL >= rows.left) break;
+    if (rows.end(j)) break;
     nm.template weigh<ACT>(t[j], w[j]);
-    if (rows.ok[j]) {
+    if (rows.ok(j)) {
 #pragma unroll
       for (int k = 0; k < CPL<VEC>; ++k) u[k] += w[j][k], v[k] = __builtin_fmaf(w[j][k], t[j][k], v[k]);
     }
@@ -1044,30 +1090,26 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_sums(NormArgs a) {
   params<VEC>(a, L, nm.gamma, nm.beta);
   const Source<T, VEC> in(a, L);
   const Mat<float> gy(a.gy, a.ldgy, L.at(a.C));
-  constexpr int TILE = BWD_TILE<VEC>;
   double cu = 0.0, cv = 0.0;
-  int s = seg_find(a, r0);
-  for (int64_t r = r0; r < r1; ++s) {
-    const int64_t e = std::min<int64_t>(seg_end(a, s), r1);
-    if (e <= r) continue;
+  over_segments(a, r0, r1, [&](int s, int64_t, int64_t, int64_t r, int64_t e) {
     groups.read(stats_of(a, s), nm.mean, nm.rstd);
     float2* part = a.part + ((int64_t)blockIdx.x + s) * a.G;
     float u[CPL<VEC>] = {}, v[CPL<VEC>] = {};
-    over_rows<TILE>(L, r, e, [&](int64_t i, const Tile<TILE>& rows) {
-      float t[TILE][CPL<VEC>], w[TILE][CPL<VEC>];
+    over_rows<BWD_TILE<VEC>>(L, r, e, [&](int64_t i, const auto& rows) {
+      constexpr int N = std::decay_t<decltype(rows)>::N;
+      float t[N][CPL<VEC>], w[N][CPL<VEC>];
 #pragma unroll
-      for (int j = 0; j < TILE; ++j) {
-        in.load(i, rows.at[j], t[j]);
-        load_row<VEC>(gy.row(i, rows.at[j]), L.cnt, w[j]);
+      for (int j = 0; j < N; ++j) {
+        in.load(rows.first(i, j), rows.at(j), t[j]);
+        load_row<VEC, false>(gy.row(rows.first(i, j), rows.at(j)), L.cnt, w[j]);
       }
-      weigh_tile<ACT>(nm, rows, L.RL, t, w, u, v);
+      weigh_tile<ACT>(nm, rows, t, w, u, v);
     });
     join_sums(
         a, L, u, v, sh, [&](int, double x, double y) { cu += x, cv += y; },
         [&](int g, double x, double y) { part[g] = make_float2((float)x, (float)y); });
     __syncthreads();
-    r = e;
-  }
+  });
   const int c = threadIdx.x;
   if (a.part_c && c < a.C) {
     a.part_c[(int64_t)blockIdx.x * 2 * a.C + c] = (float)cu;
@@ -1106,56 +1148,56 @@ __device__ __forceinline__ void grad_row(const Norm<VEC>& nm, const PerUnit<VEC>
 template <typename T, bool VEC, int ACT>
 __device__ __forceinline__ void grad_rows(const NormArgs& a, const Lanes<VEC>& L, const Norm<VEC>& nm, const PerUnit<VEC>& A,
                                           const PerUnit<VEC>& B, int64_t r, int64_t end) {
-  constexpr int TILE = BWD_TILE<VEC>;
-  const Source<T, VEC> in(a, L);
+  const Source<T, VEC, true> in(a, L);
   const Mat<float> gy(a.gy, a.ldgy, L.at(a.C)), ga(a.ga, a.ldga, L.at(a.C)), gx(a.gx, a.ldgx, L.c0);
-  over_rows<TILE>(L, r, end, [&](int64_t i, const Tile<TILE>& rows) {
-    float t[TILE][CPL<VEC>], w[TILE][CPL<VEC>], g[TILE][CPL<VEC>] = {};
+  over_rows<BWD_TILE<VEC>>(L, r, end, [&](int64_t i, const auto& rows) {
+    using TL = std::decay_t<decltype(rows)>;
+    float t[TL::N][CPL<VEC>], w[TL::N][CPL<VEC>], g[TL::N][CPL<VEC>] = {};
 #pragma unroll
-    for (int j = 0; j < TILE; ++j) {
-      in.load(i, rows.at[j], t[j]);
-      load_row<VEC>(gy.row(i, rows.at[j]), L.cnt, w[j]);
-      if (a.ga) load_row<VEC>(ga.row(i, rows.at[j]), L.cnt, g[j]);
+    for (int j = 0; j < TL::N; ++j) {
+      in.load(rows.first(i, j), rows.at(j), t[j]);
+      load_row<VEC, true>(gy.row(rows.first(i, j), rows.at(j)), L.cnt, w[j]);
+      if (a.ga) load_row<VEC, true>(ga.row(rows.first(i, j), rows.at(j)), L.cnt, g[j]);
+    }
+    if (!TL::FULL) {
+      arrived(t);
+      arrived(w);
+      arrived(g);
     }
 #pragma unroll
-    for (int j = 0; j < TILE; ++j) {
-      if (j * L.RL >= rows.left) break;
+    for (int j = 0; j < TL::N; ++j) {
+      if (rows.end(j)) break;
       nm.template weigh<ACT>(t[j], w[j]);
       grad_row(nm, A, B, w[j], t[j], g[j]);
-      if (rows.ok[j]) store_row<VEC>(gx.row(i, rows.at[j]), L.cnt, g[j]);
+      if (rows.ok(j)) store_row<VEC, true>(gx.row(rows.first(i, j), rows.at(j)), L.cnt, g[j]);
     }
   });
 }
 
-// Second pass.  The first a.nred workgroups form dbeta and dgamma.
+// Second pass.  The workgroups past the chunks form dbeta and dgamma.
 template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_dx(NormArgs a) {
   __shared__ double sh[2 * NT];
   __shared__ float2 st[MAX_C];
-  if ((int)blockIdx.x < a.nred) {
-    columns<NW>(a, blockIdx.x, sh);
+  if ((int)blockIdx.x >= a.nchunks) {
+    columns<NW>(a, blockIdx.x - a.nchunks, sh);
     return;
   }
   const Lanes<VEC> L(a.lg, a.C, NT);
-  const int64_t r0 = (int64_t)(blockIdx.x - a.nred) * a.RA, r1 = std::min<int64_t>(r0 + a.RA, a.n);
-  if (r0 >= r1) return;
+  const int64_t r0 = (int64_t)blockIdx.x * a.R;
   const Groups<VEC> groups(a, L.c0);
   Norm<VEC> nm;
   params<VEC>(a, L, nm.gamma, nm.beta);
-  int s = seg_find(a, r0);
-  for (int64_t r = r0; r < r1; ++s) {
-    const int64_t b = seg_begin(a, s), e = seg_end(a, s), end = std::min<int64_t>(e, r1);
-    if (end <= r) continue;
+  over_segments(a, r0, std::min<int64_t>(r0 + a.R, a.n), [&](int s, int64_t b, int64_t e, int64_t r, int64_t end) {
     groups.read(stats_of(a, s), nm.mean, nm.rstd);
     const double inv = 1.0 / ((double)(e - b) * a.gs);
-    join_pieces(
+    join_pieces<NW>(
         a, s, b, e, sh, [&](float2 t, double, double& u, double& v) { u += t.x, v += t.y; },
         [&](int g, double u, double v) { st[g] = make_float2((float)(u * inv), (float)(v * inv)); });
     PerUnit<VEC> A, B;
     groups.read(st, A, B);
     grad_rows<T, VEC, ACT>(a, L, nm, A, B, r, end);
-    r = end;
-  }
+  });
 }
 
 // One segment of one tile of rows, one workgroup: w and xn stay in registers.
@@ -1165,20 +1207,20 @@ __global__ __launch_bounds__(SNT) void k_norm_bwd_small(NormArgs a) {
   __shared__ SumsLds<SNW> sh;
   __shared__ float2 st[MAX_C];
   const Lanes<VEC> L(a.lg, a.C, SNT);
-  const Tile<TILE> rows(L, (int)a.n);
+  const Tile<TILE, false> rows(L, (int)a.n);
   const Source<T, VEC> in(a, L);
   const Mat<float> gy(a.gy, a.ldgy, L.at(a.C)), ga(a.ga, a.ldga, L.at(a.C)), gx(a.gx, a.ldgx, L.c0);
   float t[TILE][CPL<VEC>], w[TILE][CPL<VEC>], u[CPL<VEC>] = {}, v[CPL<VEC>] = {};
 #pragma unroll
   for (int j = 0; j < TILE; ++j) {
-    in.load(0, rows.at[j], t[j]);
-    load_row<VEC>(gy.row(0, rows.at[j]), L.cnt, w[j]);
+    in.load(0, rows.at(j), t[j]);
+    load_row<VEC, false>(gy.row(0, rows.at(j)), L.cnt, w[j]);
   }
   const Groups<VEC> groups(a, L.c0);
   Norm<VEC> nm;
   params<VEC>(a, L, nm.gamma, nm.beta);
   groups.read(stats_of(a, 0), nm.mean, nm.rstd);
-  weigh_tile<ACT>(nm, rows, L.RL, t, w, u, v);
+  weigh_tile<ACT>(nm, rows, t, w, u, v);
   const double inv = 1.0 / ((double)a.n * a.gs);
   join_sums(
       a, L, u, v, sh,
@@ -1193,11 +1235,11 @@ __global__ __launch_bounds__(SNT) void k_norm_bwd_small(NormArgs a) {
   groups.read(st, A, B);
 #pragma unroll
   for (int j = 0; j < TILE; ++j) {
-    if (j * L.RL >= rows.left) break;
+    if (rows.end(j)) break;
     float g[CPL<VEC>] = {};
-    if (a.ga) load_row<VEC>(ga.row(0, rows.at[j]), L.cnt, g);
+    if (a.ga) load_row<VEC, false>(ga.row(0, rows.at(j)), L.cnt, g);
     grad_row(nm, A, B, w[j], t[j], g);
-    if (rows.ok[j]) store_row<VEC>(gx.row(0, rows.at[j]), L.cnt, g);
+    if (rows.ok(j)) store_row<VEC, true>(gx.row(0, rows.at(j)), L.cnt, g);
   }
 }
 
@@ -1278,10 +1320,10 @@ __global__ __launch_bounds__(RNT) void k_norm_rows(NormArgs a) {
   for (int64_t i = (int64_t)blockIdx.x * L.RL; i < a.n; i += (int64_t)gridDim.x * L.RL) {
     if (i + L.rl >= a.n) return;
     float t[1][CPL<VEC>], q[CPL<VEC>];
-    const Tile<1> row(L, L.RL);
+    const Tile<1, true> row(L, L.RL);
     in.load(i, row, t);
     float(&v)[CPL<VEC>] = t[0];
-    if (a.ck) keep.store(i, row, L.RL, t);
+    if (a.ck) keep.store(i, row, t);
     PerUnit<VEC> mean = R.sum(a, L, v), rstd;
 #pragma unroll
     for (int j = 0; j < N; ++j) mean.v[j] *= f;
@@ -1345,8 +1387,8 @@ __global__ __launch_bounds__(RNT) void k_norm_rows_bwd(NormArgs a) {
     if (i + L.rl >= a.n) break;
     float t[CPL<VEC>], w[CPL<VEC>], g[CPL<VEC>] = {}, x[CPL<VEC>], y[CPL<VEC>];
     in.load(i, L.rl, t);
-    load_row<VEC>(gy.row(i, L.rl), L.cnt, w);
-    if (a.ga) load_row<VEC>(ga.row(i, L.rl), L.cnt, g);
+    load_row<VEC, false>(gy.row(i, L.rl), L.cnt, w);
+    if (a.ga) load_row<VEC, false>(ga.row(i, L.rl), L.cnt, g);
     groups.read(st.row(i, L.rl), nm.mean, nm.rstd);
     nm.template weigh<ACT>(t, w);
 #pragma unroll
@@ -1361,7 +1403,7 @@ __global__ __launch_bounds__(RNT) void k_norm_rows_bwd(NormArgs a) {
 #pragma unroll
     for (int j = 0; j < N; ++j) A.v[j] *= f, B.v[j] *= f;
     grad_row(nm, A, B, w, t, g);
-    store_row<VEC>(gx.row(i, L.rl), L.cnt, g);
+    store_row<VEC, true>(gx.row(i, L.rl), L.cnt, g);
   }
   if (!a.part_c) return;
   levels(L.lpr, [&](auto o) {
@@ -1394,7 +1436,7 @@ __global__ __launch_bounds__(RNT) void k_ckpt_store(NormArgs a) {
     if (i + L.rl >= a.n) return;
     float v[1][CPL<VEC>];
     in.load(i, L.rl, v[0]);
-    keep.store(i, Tile<1>(L, L.RL), L.RL, v);
+    keep.store(i, Tile<1, true>(L, L.RL), v);
   }
 }
 
@@ -1419,11 +1461,11 @@ int lanes_log2(int C, bool vec) {
   return lg;
 }
 
-// Chunks of the summing pass: whole steps of the workgroup's rows, at most MAX_CHUNKS.
-void chunking(int64_t n, int lg, int64_t& rows, int64_t& chunks) {
+// Chunks of rows: whole steps of a workgroup, at most `most` of them.
+void chunking(int64_t n, int lg, int64_t& rows, int64_t& chunks, int most = MAX_CHUNKS) {
   const int64_t step = NT >> lg;
   const int64_t steps = (n + step - 1) / step;
-  rows = std::max<int64_t>(1, (steps + MAX_CHUNKS - 1) / MAX_CHUNKS) * step;
+  rows = std::max<int64_t>(1, (steps + most - 1) / most) * step;
   chunks = (n + rows - 1) / rows;
 }
 
@@ -1476,7 +1518,7 @@ NormWs norm_ws(const dsmp_norm_desc& d, const dsmp_segments& s, bool backward, v
   Carve cv(ws);
   NormWs w{};
   w.part = cv.take<float2>(rows_are_segments(s) ? 0 : (size_t)(chunks + s.n_seg) * d.groups);
-  if (backward) w.part_c = cv.take<float>((size_t)std::max<int64_t>(chunks, MAX_CHUNKS) * 2 * d.channels);
+  if (backward) w.part_c = cv.take<float>((size_t)(rows_are_segments(s) ? ROW_PARTS : chunks) * 2 * d.channels);
   w.total = cv.used();
   return w;
 }
@@ -1495,19 +1537,11 @@ NormArgs norm_args(const dsmp_norm_desc& d, const dsmp_segments& s) {
 }
 
 // Lanes and chunks.
-void place(NormArgs& a, bool vec) {
+void place(NormArgs& a, bool vec, int most = MAX_CHUNKS) {
   int64_t chunks;
   a.lg = lanes_log2(a.C, vec);
-  chunking(a.n, a.lg, a.R, chunks);
+  chunking(a.n, a.lg, a.R, chunks, most);
   a.nchunks = (int)chunks;
-}
-
-// workgroups of the second pass and their rows
-unsigned second_grid(const dsmp_handle* h, NormArgs& a) {
-  const int64_t step = NT >> a.lg, steps = (a.n + step - 1) / step;
-  const int64_t most = (int64_t)h->n_cu * 2;
-  a.RA = std::max<int64_t>(1, (steps + most - 1) / most) * step;
-  return (unsigned)std::max<int64_t>(1, (a.n + a.RA - 1) / a.RA);
 }
 
 unsigned row_grid(const dsmp_handle* h, const NormArgs& a, int per_cu) {
@@ -1616,8 +1650,7 @@ extern "C" dsmp_status dsmp_group_norm_forward(dsmp_handle* h, const dsmp_norm_d
             DSMP_GO((k_norm_stats<T, V, decltype(ad)::value>), a.nchunks, NT, 0);
           });
           if (addend) a.x = sum, a.ldx = lds;
-          const unsigned grid = second_grid(h, a);
-          DSMP_GO((k_norm_apply<T, V, ACT>), grid, NT, 0);
+          DSMP_GO((k_norm_apply<T, V, ACT>), std::max(a.nchunks, 1), NT, 0);
         }
       });
     });
@@ -1642,7 +1675,7 @@ extern "C" dsmp_status dsmp_group_norm_restore(dsmp_handle* h, const dsmp_norm_d
   a.gamma = gamma, a.beta = beta, a.y = y, a.ldy = ldy, a.stats = const_cast<float*>(stats);
   a.y_bf16 = desc->y_dtype == DSMP_BF16;
   const bool vec = whole(a) && aligned(y, ldy, size_of(desc->y_dtype)) && aligned(ck->q, C, 1);
-  place(a, vec);
+  place(a, vec, MAX_PARTS);
   ProfScope prof(h, DSMP_K_NORM);
   by_bool(vec, [&](auto v) {
     by_act(desc->act, [&](auto act) {
@@ -1651,8 +1684,7 @@ extern "C" dsmp_status dsmp_group_norm_restore(dsmp_handle* h, const dsmp_norm_d
       if (rows_are_segments(*seg)) {
         DSMP_GO((k_norm_rows_restore<V, ACT>), row_grid(h, a, 16), RNT, 0);
       } else {
-        const unsigned grid = second_grid(h, a);
-        DSMP_GO((k_norm_apply<Q8, V, ACT>), grid, NT, 0);
+        DSMP_GO((k_norm_apply<Q8, V, ACT>), a.nchunks, NT, 0);
       }
     });
   });
@@ -1705,7 +1737,7 @@ extern "C" dsmp_status dsmp_group_norm_backward(dsmp_handle* h, const dsmp_norm_
         constexpr bool V = decltype(v)::value;
         constexpr int ACT = decltype(act)::value;
         if (rows_are_segments(*seg)) {
-          const unsigned grid = std::min<unsigned>(row_grid(h, a, 4), MAX_CHUNKS);
+          const unsigned grid = std::min<unsigned>(row_grid(h, a, 4), ROW_PARTS);
           a.nchunks = (int)grid;
           DSMP_GO((k_norm_rows_bwd<T, V, ACT>), grid, RNT, 0);
           if (nred) DSMP_GO(k_norm_columns, nred, SNT, 0);
@@ -1713,9 +1745,7 @@ extern "C" dsmp_status dsmp_group_norm_backward(dsmp_handle* h, const dsmp_norm_
           DSMP_GO((k_norm_bwd_small<T, V, ACT>), 1, SNT, 0);
         } else {
           DSMP_GO((k_norm_bwd_sums<T, V, ACT>), a.nchunks, NT, 0);
-          a.nred = (int)nred;
-          const unsigned grid = second_grid(h, a);
-          DSMP_GO((k_norm_bwd_dx<T, V, ACT>), grid + nred, NT, 0);
+          DSMP_GO((k_norm_bwd_dx<T, V, ACT>), a.nchunks + nred, NT, 0);
         }
       });
     });
