@@ -1,9 +1,9 @@
 """MI355X (gfx950) hot path of DS-MPNN (arXiv 2402.15106).
 
 Node sampling, radius-graph construction, the edge-conditioned
-message-passing layer (forward and backward) and the encoder, decoder and
-loss of the hop loop as hand-written HIP kernels behind a C ABI
-(include/dsmpnn.h); this package is the thin Python binding.
+message-passing layer (forward and backward), the encoder, decoder and loss of
+the hop loop, group norms and 8-bit activation checkpoints as hand-written HIP
+kernels behind a C ABI (include/dsmpnn.h); this package is the thin Python binding.
 """
 
 from ._lib import (  # noqa: F401
@@ -13,3 +13,4 @@ from ._lib import (  # noqa: F401
 )
 from .hop import HopShapes, HopStep  # noqa: F401,E402
 from .infer import SubdomainInference  # noqa: F401,E402
+from .stack import CheckpointedStack, StackShapes  # noqa: F401,E402
