@@ -424,8 +424,8 @@ typedef struct dsmp_norm_desc {
 
 /* n rows in n_seg >= 1 segments.  ptr: device int32 [n_seg + 1], ascending from
  * 0 to n (segment s has the rows [ptr[s], ptr[s+1])); its values are read on the
- * device only, and limited to [0, n]: rows past a wrong one go to some segment,
- * no access leaves the arrays.  ptr NULL: equal segments of n / n_seg rows
+ * device only, and limited to [0, n]: with wrong ones the results are undefined,
+ * but no access leaves the arrays.  ptr NULL: equal segments of n / n_seg rows
  * (INVALID_ARG if n_seg does not divide n); n_seg == n makes each row a segment. */
 typedef struct dsmp_segments {
   int64_t n;

@@ -35,7 +35,8 @@ constexpr int SNW = SNT / 64;
 constexpr int RNT = 256;        // threads where each row is a segment, and of the checkpoint passes
 constexpr int MAX_CHUNKS = 256; // chunks of rows that sums are split over: one for each CU
 constexpr int MAX_PARTS = 512;  // and where there are no sums
-constexpr int ROW_PARTS = 1024; // workgroups whose channel sums are kept where each row is a segment
+constexpr int MAX_GRID = 1024;  // workgroups that pieces are dealt to
+constexpr int ROW_PARTS = 512; // workgroups whose channel sums are kept where each row is a segment
 constexpr float TINY = 0x1p-100f;
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -54,11 +55,10 @@ constexpr int CPL = VEC ? 4 : 8;    // channels per lane
 template <bool VEC>
 constexpr int UNIT = VEC ? 4 : 1;   // channels with the same statistics
 
-// Steps of rows that a lane has in flight: of the forward passes (eight of a
-// checkpoint, whose loads are a quarter as wide), of the backward ones, and
-// where a whole segment is one tile.  Fewer where loads have branches.
-template <bool VEC, bool Q = false>
-constexpr int FWD_TILE = VEC ? (Q ? 8 : 4) : 2;
+// Steps of rows that a lane has in flight in the forward and in the backward passes,
+// and where a whole segment is one tile.  Fewer where loads have branches.
+template <bool VEC>
+constexpr int FWD_TILE = VEC ? 4 : 2;
 template <bool VEC>
 constexpr int BWD_TILE = VEC ? 4 : 1;
 template <bool VEC>
@@ -95,9 +95,10 @@ struct NormArgs {
   int64_t ldga;
   float* gx;
   int64_t ldgx;
-  float* part_c;                // [chunk][2][C]: chunk sums of w and w xn
+  float* part_c;                // [parts][2][C]: a workgroup's sums of w and w xn
   float *dgamma, *dbeta;
-  int accumulate, nchunks;
+  int accumulate, parts, grid;
+  int64_t pieces;
 };
 
 // ------------------------------------------------------------ across lanes
@@ -273,6 +274,39 @@ __device__ __forceinline__ void over_rows(const LANES& L, int64_t r, int64_t e, 
   int64_t i = r;
   for (; i + N * L.RL <= e; i += N * L.RL) tile(i, Tile<N, true>(L, N * L.RL));
   for (; i < e; i += H * L.RL) tile(i, Tile<H, false>(L, (int)std::min<int64_t>(e - i, H * L.RL)));
+}
+
+// The same in two steps: take(i, rows, v) loads a tile into v, give(i, rows, v) uses
+// it.  The next whole tile is on its way while one is used (stores count among the
+// memory operations that a load's wait looks at: a tile loaded after them would
+// wait for them).
+template <int N, int M, typename LANES, typename TAKE, typename GIVE>
+__device__ __forceinline__ void pass_rows(const LANES& L, int64_t r, int64_t e, TAKE take, GIVE give) {
+  constexpr int H = N > 1 ? N / 2 : 1;
+  const int64_t S = N * L.RL;
+  int64_t i = r;
+  if (i + S <= e) {
+    const Tile<N, true> rows(L, N * L.RL);
+    float v[N][M], w[N][M];
+    take(i, rows, v);
+    for (; i + 2 * S <= e; i += S) {
+      take(i + S, rows, w);
+      give(i, rows, v);
+#pragma unroll
+      for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int k = 0; k < M; ++k) v[t][k] = w[t][k];
+    }
+    give(i, rows, v);
+    i += S;
+  }
+  for (; i < e; i += H * L.RL) {
+    const Tile<H, false> rows(L, (int)std::min<int64_t>(e - i, H * L.RL));
+    float v[H][M];
+    take(i, rows, v);
+    arrived(v);
+    give(i, rows, v);
+  }
 }
 
 // N four-byte words from or to any address, or whole aligned ones (VEC).  STREAM:
@@ -608,36 +642,46 @@ __device__ __forceinline__ int64_t seg_begin(const NormArgs& a, int s) {
 __device__ __forceinline__ int64_t seg_end(const NormArgs& a, int s) {
   return s + 1 >= a.n_seg ? a.n : seg_begin(a, s + 1);
 }
-// The last segment that begins at or before row r: 64 bounds at a time, one to a
-// lane of each wave (every wave finds the same).
-__device__ __forceinline__ int seg_find(const NormArgs& a, int64_t r) {
-  if (!a.ptr) return a.len > 0 ? (int)((uint32_t)r / (uint32_t)a.len) : 0;
-  const int lane = threadIdx.x & 63;
-  int lo = 0, count = a.n_seg;   // it is one of lo .. lo + count - 1
-  while (count > 1) {
-    const int step = (count + 63) / 64, i = lo + lane * step;
-    const bool at = lane * step < count && seg_begin(a, i) <= r;
-    // bounds that do not ascend still leave the first lane's true
-    const int k = 63 - __builtin_clzll(__ballot(at) | 1ull);
-    count = std::min(step, count - k * step);
-    lo += k * step;
+// The passes' units of work are pieces: the rows that a segment s has in a chunk j of R
+// rows.  Piece j + s: as rows go on, either the chunk or the segment is the next one,
+// so the numbers of a segment's pieces follow each other, and every number up to
+// chunks + segments is one piece or none.
+struct Piece {
+  int s;
+  int64_t b, e;    // the segment's rows
+  int64_t r, end;  // the piece's
+  bool first;      // the segment begins with it
+  __device__ __forceinline__ Piece(const NormArgs& a, int64_t p) {
+    s = 0, b = 0, e = a.n;
+    if (a.n_seg > 1) find(a, p);
+    const int64_t j = p - s;
+    r = std::max<int64_t>(b, j * a.R);
+    end = std::min<int64_t>(e, (j + 1) * a.R);
+    first = r == b;
   }
-  return __builtin_amdgcn_readfirstlane(lo);
-}
-
-// f(s, b, e, r, end) for the segments s = [b, e) that have rows among [r0, r1), with
-// those rows [r, end).  Ends with r1 whatever ptr holds, and [r, end) is in [b, e).
-template <typename F>
-__device__ __forceinline__ void over_segments(const NormArgs& a, int64_t r0, int64_t r1, F f) {
-  if (r0 >= r1) return;
-  int s = seg_find(a, r0);
-  for (int64_t r = r0; r < r1; ++s) {
-    const int64_t e = seg_end(a, s), end = std::min<int64_t>(e, r1);
-    if (end <= r) continue;
-    f(s, std::min<int64_t>(seg_begin(a, s), r), e, r, end);
-    r = end;
+  // Of the segments whose first number, b / R + s, is at most p, the last: 64 at a time,
+  // one to a lane of each wave (every wave finds the same).
+  __device__ __forceinline__ void find(const NormArgs& a, int64_t p) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, count = a.n_seg, k, mine;   // it is one of lo .. lo + count - 1
+    for (;;) {
+      const int step = (int)(((int64_t)count + 63) / 64);
+      const int64_t off = (int64_t)lane * step, i = lo + off;
+      mine = (int)seg_begin(a, (int)std::min<int64_t>(i, a.n_seg - 1));
+      const bool at = off < count && (int64_t)((uint32_t)mine / (uint32_t)a.R) + i <= p;
+      // bounds that do not ascend still leave the first lane's true
+      k = 63 - __builtin_clzll(__ballot(at) | 1ull);
+      lo += k * step;
+      if (step == 1) break;
+      count = std::min(step, count - k * step);
+    }
+    s = __builtin_amdgcn_readfirstlane(lo);
+    k = __builtin_amdgcn_readfirstlane(k);
+    b = __builtin_amdgcn_readlane(mine, k);
+    // the last round's next lane has the next segment's begin, if it is not the last lane
+    e = s + 1 >= a.n_seg ? a.n : k < 63 ? (int64_t)__builtin_amdgcn_readlane(mine, k + 1) : seg_begin(a, s + 1);
   }
-}
+};
 
 // s1, s2: the workgroup's sums per channel (or unit of channels), float64 in LDS.
 // Gives the sums over each group's gs of them to out(g, sum1, sum2), by one lane each.
@@ -830,12 +874,13 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_stats(NormArgs a) {
   const Lanes<VEC> L(a.lg, a.C, NT);
   const Stream<T, VEC, ADD> in(a, L);
   const Keep<VEC> keep(a, L);
-  const int64_t r0 = (int64_t)blockIdx.x * a.R;
-  over_segments(a, r0, std::min<int64_t>(r0 + a.R, a.n), [&](int s, int64_t, int64_t, int64_t r, int64_t e) {
-    const double inv = 1.0 / ((double)(e - r) * a.gs);
-    float2* part = a.part + ((int64_t)blockIdx.x + s) * a.G;
+  for (int64_t p = blockIdx.x; p < a.pieces; p += gridDim.x) {
+    const Piece pc(a, p);
+    if (pc.end <= pc.r) continue;
+    const double inv = 1.0 / ((double)(pc.end - pc.r) * a.gs);
+    float2* part = a.part + p * a.G;
     Moments<VEC> m;
-    over_rows<FWD_TILE<VEC>>(L, r, e, [&](int64_t i, const auto& rows) {
+    over_rows<FWD_TILE<VEC>>(L, pc.r, pc.end, [&](int64_t i, const auto& rows) {
       float v[std::decay_t<decltype(rows)>::N][CPL<VEC>];
       in.load(i, rows, v);
       if (a.ck) keep.store(i, rows, v);
@@ -846,7 +891,7 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_stats(NormArgs a) {
       part[g] = make_float2((float)mean, (float)fmax(v - u * mean, 0.0));
     });
     __syncthreads();
-  });
+  }
 }
 
 // mean and rstd of a group from its sums about zero
@@ -857,19 +902,19 @@ __device__ __forceinline__ float2 finish(double u, double v, double inv, float e
 
 // ------------------------------------------------------------ joining the pieces
 
-// Sums over the pieces of segment s (rows [b, e)) for every group: term(piece
+// Sums over the pieces of a segment for every group: term(piece
 // value, rows of the piece, u, v) adds to two float64 sums; done(g, u, v) is called
 // by one lane of each group.  Consecutive lanes take consecutive groups.
 template <int W, typename TERM, typename DONE>
-__device__ __forceinline__ void join_pieces(const NormArgs& a, int s, int64_t b, int64_t e, double* sh, TERM term,
+__device__ __forceinline__ void join_pieces(const NormArgs& a, const Piece& pc, double* sh, TERM term,
                                             DONE done) {
   int lgp = 0;
   while ((1 << lgp) < a.G) ++lgp;
   const int gp = 1 << lgp, g = threadIdx.x & (gp - 1), p = threadIdx.x >> lgp, P = (W * 64) >> lgp;
-  const int64_t j0 = (uint32_t)b / (uint32_t)a.R, j1 = (uint32_t)(e - 1) / (uint32_t)a.R;
+  const int64_t b = pc.b, e = pc.e, j0 = (uint32_t)b / (uint32_t)a.R, j1 = (uint32_t)(e - 1) / (uint32_t)a.R;
   double u = 0.0, v = 0.0;
   if (g < a.G) {
-    const float2* part = a.part + s * (int64_t)a.G + g;
+    const float2* part = a.part + pc.s * (int64_t)a.G + g;
 #pragma unroll 4
     for (int64_t j = j0 + p; j <= j1; j += P) {
       const int64_t rows = std::min<int64_t>(e, (j + 1) * a.R) - std::max<int64_t>(b, j * a.R);
@@ -914,46 +959,47 @@ __device__ __forceinline__ void apply_rows(const NormArgs& a, const Lanes<VEC>& 
   float scale[CPL<VEC>];
 #pragma unroll
   for (int k = 0; k < CPL<VEC>; ++k) scale[k] = rstd[k] * gamma[k];
-  over_rows<FWD_TILE<VEC, std::is_same<T, Q8>::value>>(L, r, end, [&](int64_t i, const auto& rows) {
-    using TL = std::decay_t<decltype(rows)>;
-    float v[TL::N][CPL<VEC>];
+  pass_rows<FWD_TILE<VEC>, CPL<VEC>>(
+      L, r, end,
+      [&](int64_t i, const auto& rows, auto& v) {
 #pragma unroll
-    for (int t = 0; t < TL::N; ++t) in.load(rows.first(i, t), rows.at(t), v[t]);
-    if (!TL::FULL) arrived(v);
+        for (int t = 0; t < std::decay_t<decltype(rows)>::N; ++t) in.load(rows.first(i, t), rows.at(t), v[t]);
+      },
+      [&](int64_t i, const auto& rows, auto& v) {
 #pragma unroll
-    for (int t = 0; t < TL::N; ++t) {
-      if (rows.end(t)) break;
+        for (int t = 0; t < std::decay_t<decltype(rows)>::N; ++t) {
+          if (rows.end(t)) break;
 #pragma unroll
-      for (int k = 0; k < CPL<VEC>; ++k) v[t][k] = activate<ACT>(__builtin_fmaf(v[t][k] - mean[k], scale[k], beta[k]));
-      if (rows.ok(t)) out.store(rows.first(i, t), rows.at(t), v[t]);
-    }
-  });
+          for (int k = 0; k < CPL<VEC>; ++k)
+            v[t][k] = activate<ACT>(__builtin_fmaf(v[t][k] - mean[k], scale[k], beta[k]));
+          if (rows.ok(t)) out.store(rows.first(i, t), rows.at(t), v[t]);
+        }
+      });
 }
 
-// y = act((t - mean) * (rstd gamma) + beta) on this workgroup's rows, segment by
-// segment.  a.merge: the statistics come from the first pass's pieces (and are
-// written, by the workgroup that has the segment's first row), else from a.stats.
+// y = act((t - mean) * (rstd gamma) + beta), piece by piece.  a.merge: the statistics
+// come from the first pass's pieces (and are written with the segment's first one),
+// else from a.stats.
 template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_apply(NormArgs a) {
   __shared__ double sh[2 * NT];
   __shared__ float2 st[MAX_C];
   const Lanes<VEC> L(a.lg, a.C, NT);
-  const int64_t r0 = (int64_t)blockIdx.x * a.R;
-  if (a.merge && blockIdx.x == 0) {
-    for (int s = threadIdx.x; s < a.n_seg; s += NT)
-      if (seg_end(a, s) <= seg_begin(a, s))
-        for (int g = 0; g < a.G; ++g) stats_of(a, s)[g] = make_float2(0.0f, 0.0f);
-  }
   const Groups<VEC> groups(a, L.c0);
   float gamma[CPL<VEC>], beta[CPL<VEC>];
   params<VEC>(a, L, gamma, beta);
-  over_segments(a, r0, std::min<int64_t>(r0 + a.R, a.n), [&](int s, int64_t b, int64_t e, int64_t r, int64_t end) {
+  for (int64_t p = blockIdx.x; p < a.pieces; p += gridDim.x) {
+    const Piece pc(a, p);
+    if (pc.end <= pc.r) {
+      if (a.merge && pc.e <= pc.b)   // a segment of no rows has one number
+        for (int g = threadIdx.x; g < a.G; g += NT) stats_of(a, pc.s)[g] = make_float2(0.0f, 0.0f);
+      continue;
+    }
     PerUnit<VEC> mean, rstd;
     if (a.merge) {
-      const double inv = 1.0 / ((double)(e - b) * a.gs);
-      const bool first = b >= r0;
+      const double inv = 1.0 / ((double)(pc.e - pc.b) * a.gs);
       join_pieces<NW>(
-          a, s, b, e, sh,
+          a, pc, sh,
           [&](float2 t, double rows, double& u, double& v) {
             const double m = t.x, k = rows * a.gs;
             u += k * m;
@@ -961,14 +1007,14 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_apply(NormArgs a) {
           },
           [&](int g, double u, double v) {
             st[g] = finish(u, v, inv, a.eps);
-            if (first) stats_of(a, s)[g] = st[g];
+            if (pc.first) stats_of(a, pc.s)[g] = st[g];
           });
       groups.read(st, mean, rstd);
     } else {
-      groups.read(stats_of(a, s), mean, rstd);
+      groups.read(stats_of(a, pc.s), mean, rstd);
     }
-    apply_rows<T, VEC, ACT>(a, L, r, end, mean, rstd, gamma, beta);
-  });
+    apply_rows<T, VEC, ACT>(a, L, pc.r, pc.end, mean, rstd, gamma, beta);
+  }
 }
 
 // One workgroup to a segment whose rows are one tile: they stay in registers
@@ -1084,18 +1130,19 @@ template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_sums(NormArgs a) {
   __shared__ SumsLds<NW> sh;
   const Lanes<VEC> L(a.lg, a.C, NT);
-  const int64_t r0 = (int64_t)blockIdx.x * a.R, r1 = std::min<int64_t>(r0 + a.R, a.n);
   const Groups<VEC> groups(a, L.c0);
   Norm<VEC> nm;
   params<VEC>(a, L, nm.gamma, nm.beta);
   const Source<T, VEC> in(a, L);
   const Mat<float> gy(a.gy, a.ldgy, L.at(a.C));
   double cu = 0.0, cv = 0.0;
-  over_segments(a, r0, r1, [&](int s, int64_t, int64_t, int64_t r, int64_t e) {
-    groups.read(stats_of(a, s), nm.mean, nm.rstd);
-    float2* part = a.part + ((int64_t)blockIdx.x + s) * a.G;
+  for (int64_t p = blockIdx.x; p < a.pieces; p += gridDim.x) {
+    const Piece pc(a, p);
+    if (pc.end <= pc.r) continue;
+    groups.read(stats_of(a, pc.s), nm.mean, nm.rstd);
+    float2* part = a.part + p * a.G;
     float u[CPL<VEC>] = {}, v[CPL<VEC>] = {};
-    over_rows<BWD_TILE<VEC>>(L, r, e, [&](int64_t i, const auto& rows) {
+    over_rows<BWD_TILE<VEC>>(L, pc.r, pc.end, [&](int64_t i, const auto& rows) {
       constexpr int N = std::decay_t<decltype(rows)>::N;
       float t[N][CPL<VEC>], w[N][CPL<VEC>];
 #pragma unroll
@@ -1109,7 +1156,7 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_sums(NormArgs a) {
         a, L, u, v, sh, [&](int, double x, double y) { cu += x, cv += y; },
         [&](int g, double x, double y) { part[g] = make_float2((float)x, (float)y); });
     __syncthreads();
-  });
+  }
   const int c = threadIdx.x;
   if (a.part_c && c < a.C) {
     a.part_c[(int64_t)blockIdx.x * 2 * a.C + c] = (float)cu;
@@ -1125,7 +1172,7 @@ __device__ __forceinline__ void columns(const NormArgs& a, int block, double* sh
   double v = 0.0;
   if (col < 2 * a.C) {
 #pragma unroll 8
-    for (int j = wid; j < a.nchunks; j += W) v += a.part_c[(int64_t)j * 2 * a.C + col];
+    for (int j = wid; j < a.parts; j += W) v += a.part_c[(int64_t)j * 2 * a.C + col];
   }
   sh[threadIdx.x] = v;
   __syncthreads();
@@ -1174,30 +1221,31 @@ __device__ __forceinline__ void grad_rows(const NormArgs& a, const Lanes<VEC>& L
   });
 }
 
-// Second pass.  The workgroups past the chunks form dbeta and dgamma.
+// Second pass.  The last workgroups, past a.grid, form dbeta and dgamma.
 template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_dx(NormArgs a) {
   __shared__ double sh[2 * NT];
   __shared__ float2 st[MAX_C];
-  if ((int)blockIdx.x >= a.nchunks) {
-    columns<NW>(a, blockIdx.x - a.nchunks, sh);
+  if ((int)blockIdx.x >= a.grid) {
+    columns<NW>(a, blockIdx.x - a.grid, sh);
     return;
   }
   const Lanes<VEC> L(a.lg, a.C, NT);
-  const int64_t r0 = (int64_t)blockIdx.x * a.R;
   const Groups<VEC> groups(a, L.c0);
   Norm<VEC> nm;
   params<VEC>(a, L, nm.gamma, nm.beta);
-  over_segments(a, r0, std::min<int64_t>(r0 + a.R, a.n), [&](int s, int64_t b, int64_t e, int64_t r, int64_t end) {
-    groups.read(stats_of(a, s), nm.mean, nm.rstd);
-    const double inv = 1.0 / ((double)(e - b) * a.gs);
+  for (int64_t p = blockIdx.x; p < a.pieces; p += a.grid) {
+    const Piece pc(a, p);
+    if (pc.end <= pc.r) continue;
+    groups.read(stats_of(a, pc.s), nm.mean, nm.rstd);
+    const double inv = 1.0 / ((double)(pc.e - pc.b) * a.gs);
     join_pieces<NW>(
-        a, s, b, e, sh, [&](float2 t, double, double& u, double& v) { u += t.x, v += t.y; },
+        a, pc, sh, [&](float2 t, double, double& u, double& v) { u += t.x, v += t.y; },
         [&](int g, double u, double v) { st[g] = make_float2((float)(u * inv), (float)(v * inv)); });
     PerUnit<VEC> A, B;
     groups.read(st, A, B);
-    grad_rows<T, VEC, ACT>(a, L, nm, A, B, r, end);
-  });
+    grad_rows<T, VEC, ACT>(a, L, nm, A, B, pc.r, pc.end);
+  }
 }
 
 // One segment of one tile of rows, one workgroup: w and xn stay in registers.
@@ -1461,8 +1509,12 @@ int lanes_log2(int C, bool vec) {
   return lg;
 }
 
-// Chunks of rows: whole steps of a workgroup, at most `most` of them.
-void chunking(int64_t n, int lg, int64_t& rows, int64_t& chunks, int most = MAX_CHUNKS) {
+// Chunks of rows: whole steps of a workgroup, at most `most` of them.  most_chunks:
+// so many that the pieces are not more than the CUs (a few more would leave most
+// CUs idle while some have two), unless the segments alone are half as many.
+int most_chunks(int64_t n_seg, int most) { return (int)std::max<int64_t>(most / 2, most + 1 - n_seg); }
+
+void chunking(int64_t n, int lg, int64_t& rows, int64_t& chunks, int most) {
   const int64_t step = NT >> lg;
   const int64_t steps = (n + step - 1) / step;
   rows = std::max<int64_t>(1, (steps + most - 1) / most) * step;
@@ -1512,13 +1564,14 @@ struct NormWs {
 
 NormWs norm_ws(const dsmp_norm_desc& d, const dsmp_segments& s, bool backward, void* ws) {
   int64_t rows, chunks, wide;
-  chunking(s.n, lanes_log2(d.channels, false), rows, chunks);
-  chunking(s.n, lanes_log2(d.channels, true), rows, wide);
+  const int most = most_chunks(s.n_seg, MAX_CHUNKS);
+  chunking(s.n, lanes_log2(d.channels, false), rows, chunks, most);
+  chunking(s.n, lanes_log2(d.channels, true), rows, wide, most);
   chunks = std::max(chunks, wide);
   Carve cv(ws);
   NormWs w{};
   w.part = cv.take<float2>(rows_are_segments(s) ? 0 : (size_t)(chunks + s.n_seg) * d.groups);
-  if (backward) w.part_c = cv.take<float>((size_t)(rows_are_segments(s) ? ROW_PARTS : chunks) * 2 * d.channels);
+  if (backward) w.part_c = cv.take<float>((size_t)(rows_are_segments(s) ? ROW_PARTS : std::min<int64_t>(chunks + s.n_seg, MAX_GRID)) * 2 * d.channels);
   w.total = cv.used();
   return w;
 }
@@ -1540,8 +1593,9 @@ NormArgs norm_args(const dsmp_norm_desc& d, const dsmp_segments& s) {
 void place(NormArgs& a, bool vec, int most = MAX_CHUNKS) {
   int64_t chunks;
   a.lg = lanes_log2(a.C, vec);
-  chunking(a.n, a.lg, a.R, chunks, most);
-  a.nchunks = (int)chunks;
+  chunking(a.n, a.lg, a.R, chunks, most_chunks(a.n_seg, most));
+  a.pieces = chunks + a.n_seg;
+  a.grid = (int)std::min<int64_t>(a.pieces, MAX_GRID);
 }
 
 unsigned row_grid(const dsmp_handle* h, const NormArgs& a, int per_cu) {
@@ -1647,10 +1701,10 @@ extern "C" dsmp_status dsmp_group_norm_forward(dsmp_handle* h, const dsmp_norm_d
           });
         } else {
           by_bool(addend, [&](auto ad) {
-            DSMP_GO((k_norm_stats<T, V, decltype(ad)::value>), a.nchunks, NT, 0);
+            DSMP_GO((k_norm_stats<T, V, decltype(ad)::value>), a.grid, NT, 0);
           });
           if (addend) a.x = sum, a.ldx = lds;
-          DSMP_GO((k_norm_apply<T, V, ACT>), std::max(a.nchunks, 1), NT, 0);
+          DSMP_GO((k_norm_apply<T, V, ACT>), a.grid, NT, 0);
         }
       });
     });
@@ -1684,7 +1738,7 @@ extern "C" dsmp_status dsmp_group_norm_restore(dsmp_handle* h, const dsmp_norm_d
       if (rows_are_segments(*seg)) {
         DSMP_GO((k_norm_rows_restore<V, ACT>), row_grid(h, a, 16), RNT, 0);
       } else {
-        DSMP_GO((k_norm_apply<Q8, V, ACT>), a.nchunks, NT, 0);
+        DSMP_GO((k_norm_apply<Q8, V, ACT>), a.grid, NT, 0);
       }
     });
   });
@@ -1738,14 +1792,15 @@ extern "C" dsmp_status dsmp_group_norm_backward(dsmp_handle* h, const dsmp_norm_
         constexpr int ACT = decltype(act)::value;
         if (rows_are_segments(*seg)) {
           const unsigned grid = std::min<unsigned>(row_grid(h, a, 4), ROW_PARTS);
-          a.nchunks = (int)grid;
+          a.parts = (int)grid;
           DSMP_GO((k_norm_rows_bwd<T, V, ACT>), grid, RNT, 0);
           if (nred) DSMP_GO(k_norm_columns, nred, SNT, 0);
         } else if (small(a, vec) && a.n_seg == 1) {
           DSMP_GO((k_norm_bwd_small<T, V, ACT>), 1, SNT, 0);
         } else {
-          DSMP_GO((k_norm_bwd_sums<T, V, ACT>), a.nchunks, NT, 0);
-          DSMP_GO((k_norm_bwd_dx<T, V, ACT>), a.nchunks + nred, NT, 0);
+          a.parts = a.grid;
+          DSMP_GO((k_norm_bwd_sums<T, V, ACT>), a.grid, NT, 0);
+          DSMP_GO((k_norm_bwd_dx<T, V, ACT>), a.grid + nred, NT, 0);
         }
       });
     });

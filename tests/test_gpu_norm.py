@@ -597,3 +597,31 @@ def test_refuses_rows_too_far_apart(env):
         with pytest.raises(dm.DsmpError) as e:
             call()
         assert e.value.status == dm.UNSUPPORTED
+
+
+def _many(n, count, seed):
+    """count + 1 bounds of unequal segments, a fifth of them empty."""
+    g = np.random.default_rng(seed)
+    w = np.where(g.random(count) < 0.2, 0.0, g.exponential(size=count))
+    return [0] + [int(v) for v in np.minimum(n, np.round(np.cumsum(w) / w.sum() * n))][:-1] + [n]
+
+
+@pytest.mark.parametrize("n,C,G,segments", [(20000, 32, 4, 1000), (20000, 32, 4, _many(20000, 3001, 1)),
+                                            (6001, 40, 5, _many(6001, 4200, 2)), (30000, 64, 8, _many(30000, 64, 3)),
+                                            (30000, 64, 8, _many(30000, 65, 4)), (9999, 24, 2, 3333)])
+def test_many_segments(env, n, C, G, segments):
+    """More segments than a wave has lanes, and more pieces than there are workgroups."""
+    dm, lib, torch = env
+    announce("norm segments", n, C, len(segments) if isinstance(segments, list) else segments)
+    c = Case(torch, n, C, G, segments, "f32", "f32", addend=True)
+    d, seg = c.desc(dm), c.seg()
+    ck, total = dm.Checkpoint.empty(n, C, "cuda"), torch.empty_like(c.x)
+    y, st = lib.dsmp_group_norm_forward(d, c.x, c.gamma, c.beta, segments=seg, addend=c.addend, sum_out=total,
+                                        checkpoint=ck)
+    c.check_y(y, c.t64, c.check_stats(st, c.t64))
+    q, scale = on.checkpoint(_np(c.t))
+    assert np.array_equal(ck.q.cpu().numpy(), q) and np.array_equal(ck.scale.cpu().numpy(), scale)
+    st64, kept = _np(st).astype(np.float64), on.values(q, scale).astype(np.float64)
+    c.check_y(lib.dsmp_group_norm_restore(d, ck, st, c.gamma, c.beta, segments=seg), kept, st64, "restored")
+    dx, grads = lib.dsmp_group_norm_backward(d, ck, st, c.gamma, c.beta, c.dy, segments=seg, grad_addend=c.grad_addend)
+    c.check_backward(dx, grads, kept, st64, c.grad_addend)
