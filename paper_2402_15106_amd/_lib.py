@@ -550,6 +550,8 @@ class Dsmp:
         if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape
                 and t.get_device() == self._index):
             raise DsmpError(INVALID_ARG, "%s: a %s %s on %s is needed" % (name, dtype, list(shape), self.device))
+        if t.is_contiguous():
+            return t.data_ptr(), shape[1]
         ld, one = t.stride()
         if shape[0] <= 1:
             ld = shape[1]
@@ -583,12 +585,14 @@ class Dsmp:
 
     def _bind_current(self):
         s = _current_stream(self._index)
-        self._check(self.lib.dsmp_set_stream(self.h, s), self.h)
+        st = self.lib.dsmp_set_stream(self.h, s)
+        if st:
+            self._check(st, self.h)
         return s
 
-    def _norm_ws(self, desc, seg, backward):
+    def _norm_ws(self, desc, C, seg, n, backward):
         """Binds the current stream; address and size of the scratch buffer that its calls share."""
-        key = (desc.channels, desc.groups, seg.n, seg.n_seg, seg.ptr is None)
+        key = (C, desc.groups, n, seg.n_seg, seg.ptr is None)
         sizes = self._norm_sizes.get(key)
         if sizes is None:
             f, b = ctypes.c_size_t(), ctypes.c_size_t()
@@ -609,7 +613,9 @@ class Dsmp:
         out = Checkpoint.empty(n, C, self.device) if out is None else out
         ck = self._checkpoint(out, shape)
         self._bind_current()
-        self._check(self.lib.dsmp_checkpoint_store(self.h, p, _CODE[x.dtype], ld, n, C, ctypes.byref(ck)), self.h)
+        st = self.lib.dsmp_checkpoint_store(self.h, p, _CODE[x.dtype], ld, n, C, ck)
+        if st:
+            self._check(st, self.h)
         return out
 
     def dsmp_checkpoint_load(self, ck: Checkpoint, y: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -622,7 +628,9 @@ class Dsmp:
         p, ld = self._rows(y, "y", shape, y.dtype)
         cck = self._checkpoint(ck, shape)
         self._bind_current()
-        self._check(self.lib.dsmp_checkpoint_load(self.h, ctypes.byref(cck), n, C, p, _CODE[y.dtype], ld), self.h)
+        st = self.lib.dsmp_checkpoint_load(self.h, cck, n, C, p, _CODE[y.dtype], ld)
+        if st:
+            self._check(st, self.h)
         return y
 
     def dsmp_group_norm_forward(self, desc: NormDesc, x, gamma, beta, segments=None, addend=None, sum_out=None, y=None,
@@ -647,10 +655,11 @@ class Dsmp:
         stats = torch.empty(shape, dtype=torch.float32, device=self.device) if stats is None else stats
         stp = self._flat(stats, "stats", shape)
         ck = None if checkpoint is None else self._checkpoint(checkpoint, rows)
-        ws, ws_bytes = self._norm_ws(desc, seg, False)
-        self._check(self.lib.dsmp_group_norm_forward(self.h, ctypes.byref(desc), ctypes.byref(seg), xp, ldx, ap, lda, sp,
-                                                     lds, gp, bp, yp, ldy, stp, None if ck is None else ctypes.byref(ck),
-                                                     ws, ws_bytes), self.h)
+        ws, ws_bytes = self._norm_ws(desc, C, seg, n, False)
+        st = self.lib.dsmp_group_norm_forward(self.h, desc, seg, xp, ldx, ap, lda, sp, lds, gp, bp, yp, ldy, stp, ck, ws,
+                                              ws_bytes)
+        if st:
+            self._check(st, self.h)
         return y, stats
 
     def dsmp_group_norm_restore(self, desc: NormDesc, checkpoint: Checkpoint, stats, gamma, beta, segments=None, y=None):
@@ -665,8 +674,9 @@ class Dsmp:
         y = torch.empty(n, C, dtype=yt, device=self.device) if y is None else y
         yp, ldy = self._rows(y, "y", rows, yt)
         self._bind_current()
-        self._check(self.lib.dsmp_group_norm_restore(self.h, ctypes.byref(desc), ctypes.byref(seg), ctypes.byref(ck), stp,
-                                                     gp, bp, yp, ldy), self.h)
+        st = self.lib.dsmp_group_norm_restore(self.h, desc, seg, ck, stp, gp, bp, yp, ldy)
+        if st:
+            self._check(st, self.h)
         return y
 
     def dsmp_group_norm_backward(self, desc: NormDesc, source, stats, gamma, beta, grad_y, segments=None,
@@ -692,9 +702,9 @@ class Dsmp:
         else:
             grads = {"dgamma": torch.empty(C, **f32), "dbeta": torch.empty(C, **f32)} if grads is None else grads
             dg, db = self._flat(grads["dgamma"], "dgamma", (C,)), self._flat(grads["dbeta"], "dbeta", (C,))
-        ws, ws_bytes = self._norm_ws(desc, seg, True)
-        self._check(self.lib.dsmp_group_norm_backward(self.h, ctypes.byref(desc), ctypes.byref(seg), xp, ldx,
-                                                      None if ck is None else ctypes.byref(ck), stp, gp, bp, dyp, ldgy,
-                                                      gap, ldga, dxp, ldgx, dg, db, flags, ws, ws_bytes),
-                    self.h)
+        ws, ws_bytes = self._norm_ws(desc, C, seg, n, True)
+        st = self.lib.dsmp_group_norm_backward(self.h, desc, seg, xp, ldx, ck, stp, gp, bp, dyp, ldgy, gap, ldga, dxp,
+                                               ldgx, dg, db, flags, ws, ws_bytes)
+        if st:
+            self._check(st, self.h)
         return grad_x, grads
