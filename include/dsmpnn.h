@@ -442,8 +442,8 @@ dsmp_status dsmp_group_norm_workspace(const dsmp_norm_desc* desc, const dsmp_seg
  * (required with an addend, else NULL) receives t; sum may be x or addend
  * itself (with its row distance).  gamma, beta: device float32 [channels], or
  * both NULL (1 and 0).  y: device [n, channels] of y_dtype.  stats: device
- * float32 [n_seg, groups, 2], receives mean and rstd, which the calls below
- * take.  ck: NULL, or a checkpoint of t to write in the same pass.  Apart from
+ * float32 [n_seg, groups, 2], 8-byte aligned, receives mean and rstd, which the
+ * calls below take.  ck: NULL, or a checkpoint of t to write in the same pass.  Apart from
  * sum, outputs do not overlap inputs.  n == 0 writes the statistics only. */
 dsmp_status dsmp_group_norm_forward(dsmp_handle* h, const dsmp_norm_desc* desc, const dsmp_segments* seg,
                                     const void* x, int64_t ldx, const void* addend, int64_t lda, void* sum,

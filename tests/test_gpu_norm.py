@@ -625,3 +625,33 @@ def test_many_segments(env, n, C, G, segments):
     c.check_y(lib.dsmp_group_norm_restore(d, ck, st, c.gamma, c.beta, segments=seg), kept, st64, "restored")
     dx, grads = lib.dsmp_group_norm_backward(d, ck, st, c.gamma, c.beta, c.dy, segments=seg, grad_addend=c.grad_addend)
     c.check_backward(dx, grads, kept, st64, c.grad_addend)
+
+
+def test_refuses_statistics_between_pairs(env):
+    dm, lib, torch = env
+    announce("norm stats alignment")
+    x, f = torch.zeros(10, 32, device="cuda"), torch.ones(32, device="cuda")
+    d, st = dm.norm_desc(32, 4, dm.F32, dm.F32), torch.zeros(9, device="cuda")[1:].view(1, 4, 2)
+    ck = lib.dsmp_checkpoint_store(x)
+    for call in (lambda: lib.dsmp_group_norm_forward(d, x, f, f, stats=st),
+                 lambda: lib.dsmp_group_norm_restore(d, ck, st, f, f),
+                 lambda: lib.dsmp_group_norm_backward(d, ck, st, f, f, x)):
+        with pytest.raises(dm.DsmpError) as e:
+            call()
+        assert e.value.status == dm.INVALID_ARG
+
+
+@pytest.mark.parametrize("n", [511, 512, 513, 1024, 1025])
+@pytest.mark.parametrize("segments", [None, 1, "two"])
+def test_sizes_at_which_one_launch_becomes_two(env, n, segments):
+    dm, lib, torch = env
+    announce("norm one launch", n, segments)
+    for add in (False, True):
+        c = Case(torch, n, 32, 4, [0, n // 3, n] if segments == "two" else segments, addend=add)
+        total, ck = (torch.empty_like(c.x), dm.Checkpoint.empty(n, 32, "cuda")) if add else (None, None)
+        d, seg = c.desc(dm), c.seg()
+        y, st = lib.dsmp_group_norm_forward(d, c.x, c.gamma, c.beta, segments=seg, addend=c.addend, sum_out=total,
+                                            checkpoint=ck)
+        c.check_y(y, c.t64, c.check_stats(st, c.t64))
+        dx, grads = lib.dsmp_group_norm_backward(d, c.t, st, c.gamma, c.beta, c.dy, segments=seg)
+        c.check_backward(dx, grads, c.t64, _np(st).astype(np.float64))
