@@ -1,20 +1,30 @@
 // Group norm with an activation over packed segments (channels last), forward,
 // restored and backward, and activation checkpoints in 8 bits.
 //
+// t = x (+ addend).  Over the rows of a segment and the gs channels of a group:
+// mean, var = mean of (t - mean)^2, rstd = 1 / sqrt(var + eps), xn = (t - mean) rstd,
+// y = act(gamma xn + beta).  Backward with w = grad_y act'(gamma xn + beta): dbeta and
+// dgamma are the sums of w and w xn over all rows; A and B the means of gamma w and
+// gamma w xn over a segment's group; grad_x = rstd (gamma w - A - xn B) + grad_addend.
+//
 // All of it is bound by memory: about 10 operations per value forward and 30
 // backward, against 4 to 16 bytes.  A segment's statistics need all its rows
 // before any of them can be written, so the long form is two passes: one that
-// sums over chunks of rows (and adds the addend and writes the checkpoint on
-// the way), one that joins the chunks' sums and writes the result.  The second
-// reads what the first just touched.  Where each row is a segment, one pass.
+// sums over pieces of the segments (and adds the addend and writes the checkpoint on
+// the way), one that joins the sums of the pieces and writes the result.  The second
+// reads what the first just touched, as far as that is still in the last-level
+// cache (256 MB).  Where each row is a segment, one pass.
 //
-// Every lane holds 8 consecutive channels of a row: 16 bytes of bfloat16, 32 of
-// float32, 8 of a checkpoint.  A row takes `lpr` lanes, the next power of two,
-// so sums over the rows of a wave are shuffles by lpr, 2 lpr, ..., and a
-// checkpoint's block of 64 channels is 8 neighbouring lanes.
+// A lane holds 4 consecutive channels of a row (8 where a row is not whole aligned
+// groups of 4, VEC below), 4 or 8 rows at a time.  A row takes `lpr` lanes, the next
+// power of two, so sums over the rows of a wave are exchanges lpr, 2 lpr, ... lanes
+// apart, and a checkpoint's block of 64 channels is 16 (8) neighbouring lanes.
 //
-// Sums run in a fixed order (lane, wave, chunk): no atomics, the same bits on
-// every run.  What crosses a chunk is joined in float64.
+// Sums run in a fixed order (lane, wave, piece): no atomics, the same bits on
+// every run.  A lane sums in float32; across waves, and across pieces, in float64.
+//
+// The times below are kernel times on one MI355X, whose large copy runs at 5,144 GB/s
+// (read and written bytes together).
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>
@@ -28,13 +38,18 @@ namespace {
 
 constexpr int MAX_C = 512;      // 64 lanes of 8 channels: a row stays in one wave
 constexpr int BLOCK_C = 64;     // channels that share a checkpoint scale
-constexpr int NT = 512;         // threads of the passes over segments
+// Threads of the passes over segments: two workgroups to a CU.  256: 53 instead of 47 us
+// for the second pass over 285,564 x 128 float32; 1,024: 7.3 instead of 5.3 us for that
+// of the backward over 8,192 x 64.
+constexpr int NT = 512;
 constexpr int NW = NT / 64;
 constexpr int SNT = 1024;       // threads where one workgroup takes a whole segment
 constexpr int SNW = SNT / 64;
 constexpr int RNT = 256;        // threads where each row is a segment, and of the checkpoint passes
-constexpr int MAX_CHUNKS = 256; // chunks of rows that sums are split over: one for each CU
-constexpr int MAX_PARTS = 512;  // and where there are no sums
+// Chunks of rows that sums are split over: one for each CU.  With 512 the second pass
+// over 285,564 x 128 takes 54 us instead of 44: every workgroup joins all the sums.
+constexpr int MAX_CHUNKS = 256;
+constexpr int MAX_PARTS = 512;  // and where there are no sums to join (restore)
 constexpr int MAX_GRID = 1024;  // workgroups that pieces are dealt to
 constexpr int ROW_PARTS = 512;  // workgroups whose channel sums are kept where each row is a segment
 constexpr float TINY = 0x1p-100f;
@@ -44,7 +59,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// VEC, in all that follows: rows are whole aligned groups of four channels, up to
+// VEC, in all that follows, a rule on sizes and alignment alone: rows are whole aligned groups of four channels, up to
 // 256 of them, and no group of the norm ends inside four.  A lane then holds four
 // channels (a load instruction of a wave is one contiguous piece for every type;
 // eight channels of float32 take two that each touch every line: 53 us instead of
@@ -56,7 +71,10 @@ template <bool VEC>
 constexpr int UNIT = VEC ? 4 : 1;   // channels with the same statistics
 
 // Steps of rows that a lane has in flight in the forward and in the backward passes,
-// and where a whole segment is one tile.  Fewer where loads have branches.
+// and where a whole segment is one tile.  Twice the forward's: 14 instead of 11 us for
+// the statistics of 32,768 x 64 bfloat16 in 8 segments (registers: fewer waves); the
+// backward's 6 or 8: 56 instead of 33 us for the sums over 285,564 x 128.  Fewer where
+// a lane holds eight channels (VEC false), each with statistics of its own.
 template <bool VEC>
 constexpr int FWD_TILE = VEC ? 4 : 2;
 template <bool VEC>
@@ -315,7 +333,19 @@ __device__ __forceinline__ void pass_rows(const LANES& L, int64_t r, int64_t e, 
 }
 
 // N four-byte words from or to any address, or whole aligned ones (VEC).  STREAM:
-// with the non-temporal hint, for what is not used again soon.
+// with the non-temporal hint, for what is not used again soon.  It keeps what the
+// second pass reads again in the last-level cache:
+// - results (y, q, grad_x): forward, restore and backward of 285,564 x 128 float32 with
+//   addend and checkpoint 306 us without the hint, 290 with.  A kernel that reads the
+//   result next, timed with it, gains or loses little: 161.5 / 149.5 after the
+//   backward, 112.2 / 109.9 after the forward, 54.4 / 55.6 after restore; 52.9 / 54.4,
+//   42.8 / 42.8, 22.1 / 22.4 at 100,000 x 128.
+// - inputs where they are used for the last time: 290 / 271 us; forward of
+//   262,144 x 128 with an addend 121 / 107.
+// Not where it costs: the sum (read again at once: the second pass 54 us with the hint,
+// 44 without) and a checkpoint in restore (26 with, 20 without: the backward reads it).
+// One rule for all sizes: chosen when compiled (of two stores in one kernel the
+// compiler keeps one, without the hint), and at small sizes the two differ by 0.3 us.
 template <bool STREAM, typename W>
 __device__ __forceinline__ W get(const void* p) {
   if constexpr (STREAM)
@@ -873,6 +903,12 @@ __device__ __forceinline__ void join_moments(const NormArgs& a, const Lanes<VEC>
   group_sums<W>(sh.s1, sh.s2, a.G, a.gs / U, out);
 }
 
+// First pass.  Per piece and group the mean and the sum of squares about it; adds and
+// writes checkpoints on the way.  Bound by memory: 262,144 x 128 float32 with addend
+// and sum 67 us (403 MB, 6.0 TB/s; the second pass's 37 us then reads from the cache in
+// part); 285,564 x 128 with a checkpoint too 85 us (477 MB, 5.6 TB/s).  At 99,991 x 64
+// bfloat16 in 37 segments 8.9 us for 12.8 MB: two tiles to a workgroup, so its launch,
+// one load's way and the joining over lanes and waves are what it takes.
 template <typename T, bool VEC, bool ADD>
 __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_stats(NormArgs a) {
   __shared__ SumsLds<NW> sh;
@@ -907,9 +943,9 @@ __device__ __forceinline__ float2 finish(double u, double v, double inv, float e
 
 // ------------------------------------------------------------ joining the pieces
 
-// Sums over the pieces of a segment for every group: term(piece
-// value, rows of the piece, u, v) adds to two float64 sums; done(g, u, v) is called
-// by one lane of each group.  Consecutive lanes take consecutive groups.
+// Sums over the pieces of a segment for every group: term(piece's value, its rows,
+// u, v) adds to two float64 sums; done(g, u, v) is called by one lane of each group.
+// Consecutive lanes take consecutive groups.
 template <int W, typename TERM, typename DONE>
 __device__ __forceinline__ void join_pieces(const NormArgs& a, const Piece& pc, double* sh, TERM term,
                                             DONE done) {
@@ -984,7 +1020,12 @@ __device__ __forceinline__ void apply_rows(const NormArgs& a, const Lanes<VEC>& 
 
 // y = act((t - mean) * (rstd gamma) + beta), piece by piece.  a.merge: the statistics
 // come from the first pass's pieces (and are written with the segment's first one),
-// else from a.stats.
+// else from a.stats.  Every workgroup joins the sums of its segment's pieces itself, which
+// costs it 2 to 3 us and saves a launch between the passes.  The next tile is loaded while
+// one is written (pass_rows); the first one ahead of the joining too gave 1 to 2 us at
+// 99,991 x 64 and took 4 at 285,564 x 128.  262,144 x 128 float32 to bfloat16 37 us
+// (201 MB, 5.5 TB/s, part of it from the cache), restored from a checkpoint 19 us
+// (103 MB, 5.4 TB/s); 99,991 x 64 bfloat16 in 37 segments 10.4 us (25.6 MB).
 template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_apply(NormArgs a) {
   __shared__ double sh[2 * NT];
@@ -1023,7 +1064,8 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_apply(NormArgs a) {
 }
 
 // One workgroup to a segment whose rows are one tile: they stay in registers
-// between the statistics and the result.
+// between the statistics and the result.  1,024 x 32 float32 7.6 us, all of it latency
+// (launch, one load's way, joining over lanes and waves, the store).
 template <typename T, bool VEC, bool ADD, int ACT>
 __global__ __launch_bounds__(SNT) void k_norm_small(NormArgs a) {
   constexpr int TILE = SMALL_TILE<VEC>;
@@ -1130,7 +1172,9 @@ __device__ __forceinline__ void weigh_tile(const Norm<VEC>& nm, const Tile<N, FU
   }
 }
 
-// First pass: per chunk and segment the groups' sums, per chunk the channels'.
+// First pass: per piece the groups' sums, per workgroup the channels'.  285,564 x 128
+// from a checkpoint 34 us (185 MB, 5.4 TB/s); 8,192 x 64 bfloat16 5.3 us (3.1 MB,
+// latency).
 template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_sums(NormArgs a) {
   __shared__ SumsLds<NW> sh;
@@ -1169,8 +1213,8 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_sums(NormArgs a) {
   }
 }
 
-// dbeta and dgamma from the chunks' sums: 64 columns of part_c to a workgroup,
-// the chunks dealt to its waves, joined in wave order.
+// dbeta and dgamma from the workgroups' sums: 64 columns of part_c to a workgroup,
+// the sums dealt to its waves, joined in wave order.
 template <int W>
 __device__ __forceinline__ void columns(const NormArgs& a, int block, double* sh) {
   const int col = block * 64 + (threadIdx.x & 63), wid = threadIdx.x >> 6;
@@ -1226,7 +1270,10 @@ __device__ __forceinline__ void grad_rows(const NormArgs& a, const Lanes<VEC>& L
   });
 }
 
-// Second pass.  The last workgroups, past a.grid, form dbeta and dgamma.
+// Second pass.  The last workgroups, past a.grid, form dbeta and dgamma (4 us as a launch
+// of their own).  285,564 x 128 from a checkpoint with grad_addend 77 us (477 MB,
+// 6.2 TB/s, part of it from the cache); 8,192 x 64 bfloat16 5.3 us (5.2 MB, latency).
+// Pieces in the opposite order (last read, first used) made no difference.
 template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_dx(NormArgs a) {
   __shared__ double sh[2 * NT];
@@ -1254,6 +1301,7 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_dx(NormArgs a) {
 }
 
 // One segment of one tile of rows, one workgroup: w and xn stay in registers.
+// 1,000 x 32 from a checkpoint 9.8 us.
 template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(SNT) void k_norm_bwd_small(NormArgs a) {
   constexpr int TILE = SMALL_TILE<VEC>;
@@ -1356,6 +1404,9 @@ struct RowGroups {
   }
 };
 
+// A row's statistics need only its own lanes: one pass, mean and then deviations from
+// it in registers.  No tiles: many small workgroups (16 to a CU) hide the loads.
+// 8,192 x 64 bfloat16 3.4 us (2.1 MB).
 template <typename T, bool VEC, bool ADD, int ACT>
 __global__ __launch_bounds__(RNT) void k_norm_rows(NormArgs a) {
   constexpr int U = UNIT<VEC>, N = CPL<VEC> / U;
@@ -1422,6 +1473,9 @@ __global__ __launch_bounds__(RNT) void k_norm_rows_restore(NormArgs a) {
   }
 }
 
+// The channels' sums stay in registers over all rows of a workgroup (4 to a CU, at most
+// ROW_PARTS: so many sums are joined by k_norm_columns).  100,000 x 128 float32 with
+// grad_addend 39 us (211 MB, 5.4 TB/s) and 4.6 us for the columns.
 template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(RNT) void k_norm_rows_bwd(NormArgs a) {
   constexpr int N = CPL<VEC> / UNIT<VEC>;
@@ -1480,6 +1534,11 @@ __global__ __launch_bounds__(RNT) void k_norm_rows_bwd(NormArgs a) {
 
 // ------------------------------------------------------------ checkpoints alone
 
+// One read, one write; as in the norm's passes, with no statistics to wait for.  A
+// bfloat16 or float32 value is kept as an 8-bit multiple of its block's scale,
+// rounded to nearest: off by at most half a scale, 1 / 254 of the block's largest.
+// 100,000 x 256 float32 stored and loaded as bfloat16: 42 us for both (208 MB,
+// 4.9 TB/s); 8,191 x 96 bfloat16 7 us for both.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(RNT) void k_ckpt_store(NormArgs a) {
   const Lanes<VEC> L(a.lg, a.C, RNT);
@@ -1516,7 +1575,8 @@ int lanes_log2(int C, bool vec) {
 
 // Chunks of rows: whole steps of a workgroup, at most `most` of them.  most_chunks:
 // so many that the pieces are not more than the CUs (a few more would leave most
-// CUs idle while some have two), unless the segments alone are half as many.
+// CUs idle while some have two: 37 segments on 256 chunks 14.5 us instead of 11.5 for
+// the second pass over 99,991 x 64), unless the segments alone are half as many.
 int most_chunks(int64_t n_seg, int most) { return (int)std::max<int64_t>(most / 2, most + 1 - n_seg); }
 
 void chunking(int64_t n, int lg, int64_t& rows, int64_t& chunks, int most) {
