@@ -1682,9 +1682,11 @@ bool whole(const NormArgs& a) {
 // forward 7.6 / 4.7 + 4.2 us, backward 9.6 / 4.7 + 5.2.  With an addend and a
 // checkpoint 13.9 / 6.2 + 3.6, where one CU does all the work, but the calls are
 // bound by the host: forward, restore and backward in a row take 29.1 us with one
-// launch for it, 31.0 with two.
+// launch for it, 31.0 with two.  Not for more segments than the pieces are dealt to
+// (most are empty then): a launch has fewer than 2^32 threads.
 bool small(const NormArgs& a, bool vec) {
-  return a.C <= MAX_C / 2 && a.n <= (int64_t)(vec ? SMALL_TILE<true> : SMALL_TILE<false>) * (SNT >> a.lg);
+  return a.C <= MAX_C / 2 && a.n_seg <= MAX_GRID &&
+         a.n <= (int64_t)(vec ? SMALL_TILE<true> : SMALL_TILE<false>) * (SNT >> a.lg);
 }
 
 template <typename F>

@@ -655,3 +655,25 @@ def test_sizes_at_which_one_launch_becomes_two(env, n, segments):
         c.check_y(y, c.t64, c.check_stats(st, c.t64))
         dx, grads = lib.dsmp_group_norm_backward(d, c.t, st, c.gamma, c.beta, c.dy, segments=seg)
         c.check_backward(dx, grads, c.t64, _np(st).astype(np.float64))
+
+
+def test_few_rows_in_millions_of_segments(env):
+    dm, lib, torch = env
+    announce("norm millions of segments")
+    n, C, G, nseg = 10, 8, 2, (1 << 22) + 1   # 1,024 threads for each of them would be past 2^32
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, dy = (torch.randn(n, C, device="cuda", generator=g) for _ in range(2))
+    f = torch.full((C,), 1.5, device="cuda")
+    ptr = torch.full((nseg + 1,), 3, dtype=torch.int32, device="cuda")   # rows 0..2 in the first, 3..9 in the last
+    ptr[0], ptr[nseg] = 0, n
+    two = torch.tensor([0, 3, n], dtype=torch.int32, device="cuda")
+    d = dm.norm_desc(C, G, dm.F32, dm.F32, dm.ACT_SILU)
+    y, st = lib.dsmp_group_norm_forward(d, x, f, f, segments=ptr)
+    y2, st2 = lib.dsmp_group_norm_forward(d, x, f, f, segments=two)
+    # the same formulas in another order of sums: a few units in the last place
+    assert torch.allclose(st[[0, nseg - 1]], st2, rtol=32 * U, atol=32 * U) and torch.allclose(y, y2, rtol=0, atol=256 * U)
+    assert not st[1:nseg - 1].any()
+    dx, gr = lib.dsmp_group_norm_backward(d, x, st, f, f, dy, segments=ptr)
+    dx2, gr2 = lib.dsmp_group_norm_backward(d, x, st2, f, f, dy, segments=two)
+    assert torch.allclose(dx, dx2, rtol=0, atol=1024 * U)
+    assert all(torch.allclose(gr[k], gr2[k], rtol=0, atol=1024 * U) for k in gr)
