@@ -395,7 +395,8 @@ typedef struct dsmp_checkpoint {
 
 /* x: device [n, channels] of dtype DSMP_F32 or DSMP_BF16, rows ldx elements
  * apart (channels <= ldx <= 2^16; any alignment of its type; so for every matrix
- * of this section and the next).  n == 0 enqueues nothing. */
+ * of this section and the next).  What lies between two rows may be read, and is
+ * neither used nor written.  n == 0 enqueues nothing. */
 dsmp_status dsmp_checkpoint_store(dsmp_handle* h, const void* x, int32_t dtype, int64_t ldx, int64_t n,
                                   int32_t channels, const dsmp_checkpoint* ck);
 

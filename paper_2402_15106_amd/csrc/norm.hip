@@ -58,25 +58,37 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// the same at any address: one instruction, as for aligned ones
+typedef uint32_t any_u32 __attribute__((aligned(1)));
+typedef u32x2 any_x2 __attribute__((aligned(1)));
+typedef u32x4 any_x4 __attribute__((aligned(1)));
 
 // VEC, in all that follows, a rule on sizes and alignment alone: rows are whole aligned groups of four channels, up to
 // 256 of them, and no group of the norm ends inside four.  A lane then holds four
 // channels (a load instruction of a wave is one contiguous piece for every type;
 // eight channels of float32 take two that each touch every line: 53 us instead of
 // 44 for the second pass over 262,144 x 128), with one set of statistics.
-// Elsewhere it holds eight, every channel with its own.
+// Elsewhere it holds eight, every channel with its own, read in one go from any address,
+// past the row's end too where the matrix goes on (WIDE).  Reading a row's end value by
+// value instead takes a branch and a wait for each: forward, restore and backward of
+// 120,000 x 147 bfloat16 in 7 groups 382 us instead of 200, x 100 in 10 groups 179 / 103,
+// x 105 float32 186 / 150.
 template <bool VEC>
 constexpr int CPL = VEC ? 4 : 8;    // channels per lane
 template <bool VEC>
 constexpr int UNIT = VEC ? 4 : 1;   // channels with the same statistics
 
-// Steps of rows that a lane has in flight in the forward and in the backward passes,
+// Steps of rows that a lane has in flight in the forward passes, in the two of the backward,
 // and where a whole segment is one tile.  Twice the forward's: 14 instead of 11 us for
 // the statistics of 32,768 x 64 bfloat16 in 8 segments (registers: fewer waves); the
 // backward's 6 or 8: 56 instead of 33 us for the sums over 285,564 x 128.  Fewer where
-// a lane holds eight channels (VEC false), each with statistics of its own.
+// a lane holds eight channels (VEC false), each with statistics of its own: 4 forward
+// 53 instead of 51 us for the statistics of 120,000 x 147, 1 for the sums 35 instead of
+// 31, 2 in the last pass 25 instead of 22.7 at 120,000 x 77 and 100.
 template <bool VEC>
 constexpr int FWD_TILE = VEC ? 4 : 2;
+template <bool VEC>
+constexpr int SUMS_TILE = VEC ? 4 : 2;
 template <bool VEC>
 constexpr int BWD_TILE = VEC ? 4 : 1;
 template <bool VEC>
@@ -244,7 +256,7 @@ struct Lanes {
   // Where the lane reads.  With whole groups a lane past the row takes the row's
   // last channels once more (no sum counts them, and a block's largest is the
   // same): a condition would become a branch around the load, and a wait.
-  __device__ __forceinline__ int at(int C) const { return VEC ? std::min(c0, C - CPL<VEC>) : c0; }
+  __device__ __forceinline__ int at(int C) const { return std::min(c0, VEC ? C - CPL<VEC> : C - 1); }
 };
 
 // Rows of a matrix.  Row i + at, where i is the same for all lanes (scalar
@@ -264,7 +276,9 @@ struct Mat {
 
 // The rows of a tile: N steps of RL rows, all of which exist (FULL) or the first
 // `left`.  Reads then take the last row again past it, and what they bring is not
-// used: all loads of a tile go out together, whatever exists.
+// used: all loads of a tile go out together, whatever exists.  Where rows are not whole
+// groups, the matrix has 7 more rows after a FULL tile: its lanes may read 8 channels
+// from any of a row's, whatever the row distance.
 template <int N_, bool FULL_>
 struct Tile {
   static constexpr int N = N_;
@@ -290,29 +304,46 @@ __device__ __forceinline__ void arrived(float (&v)[N][M]) {
 }
 
 // tile(i, rows of it) over the rows [r, e): whole tiles of N steps, the rest in
-// tiles of half as many
-template <int N, typename LANES, typename F>
-__device__ __forceinline__ void over_rows(const LANES& L, int64_t r, int64_t e, F tile) {
+// tiles of half as many.  n: the matrix's rows.
+template <bool VEC>
+__device__ __forceinline__ int64_t full_end(int64_t e, int64_t n) {
+  return VEC ? e : std::min<int64_t>(e, n - (CPL<VEC> - 1));
+}
+template <int N, bool VEC, typename F>
+__device__ __forceinline__ void over_rows(const Lanes<VEC>& L, int64_t r, int64_t e, int64_t n, F tile) {
   constexpr int H = N > 1 ? N / 2 : 1;
+  const int64_t f = full_end<VEC>(e, n);
   int64_t i = r;
-  for (; i + N * L.RL <= e; i += N * L.RL) tile(i, Tile<N, true>(L, N * L.RL));
+  for (; i + N * L.RL <= f; i += N * L.RL) tile(i, Tile<N, true>(L, N * L.RL));
   for (; i < e; i += H * L.RL) tile(i, Tile<H, false>(L, (int)std::min<int64_t>(e - i, H * L.RL)));
 }
 
-// The same in two steps: take(i, rows, v) loads a tile into v, give(i, rows, v) uses
+// row(i, whole) where a workgroup's rows are i + rl, all workgroups together go over all
+// rows, and only the row's own lanes work together.  whole: as a FULL tile, or only
+// the lanes whose row exists.
+template <bool VEC, typename F>
+__device__ __forceinline__ void each_row(const Lanes<VEC>& L, int64_t n, F row) {
+  const int64_t f = full_end<VEC>(n, n), step = (int64_t)gridDim.x * L.RL;
+  int64_t i = (int64_t)blockIdx.x * L.RL;
+  for (; i + L.RL <= f; i += step) row(i, std::true_type{});
+  for (; i < n; i += step)
+    if (i + L.rl < n) row(i, std::false_type{});
+}
+
+// over_rows in two steps: take(i, rows, v) loads a tile into v, give(i, rows, v) uses
 // it.  The next whole tile is on its way while one is used (stores count among the
 // memory operations that a load's wait looks at: a tile loaded after them would
 // wait for them).
-template <int N, int M, typename LANES, typename TAKE, typename GIVE>
-__device__ __forceinline__ void pass_rows(const LANES& L, int64_t r, int64_t e, TAKE take, GIVE give) {
-  constexpr int H = N > 1 ? N / 2 : 1;
-  const int64_t S = N * L.RL;
+template <int N, bool VEC, typename TAKE, typename GIVE>
+__device__ __forceinline__ void pass_rows(const Lanes<VEC>& L, int64_t r, int64_t e, int64_t n, TAKE take, GIVE give) {
+  constexpr int H = N > 1 ? N / 2 : 1, M = CPL<VEC>;
+  const int64_t S = N * L.RL, f = full_end<VEC>(e, n);
   int64_t i = r;
-  if (i + S <= e) {
+  if (i + S <= f) {
     const Tile<N, true> rows(L, N * L.RL);
     float v[N][M], w[N][M];
     take(i, rows, v);
-    for (; i + 2 * S <= e; i += S) {
+    for (; i + 2 * S <= f; i += S) {
       take(i + S, rows, w);
       give(i, rows, v);
 #pragma unroll
@@ -344,6 +375,10 @@ __device__ __forceinline__ void pass_rows(const LANES& L, int64_t r, int64_t e, 
 //   262,144 x 128 with an addend 121 / 107.
 // Not where it costs: the sum (read again at once: the second pass 54 us with the hint,
 // 44 without) and a checkpoint in restore (26 with, 20 without: the backward reads it).
+// Not where rows are not whole aligned groups (VEC false): pieces of cache lines past the
+// caches cost more than they save.  120,000 rows, forward, restore and backward with it /
+// without: 105 channels of float32 155 / 149 us, 147 of bfloat16 204 / 200, 100 in ten groups
+// 99 / 103; a checkpoint of 60,000 x 226 stored and loaded 27 / 25.
 // One rule for all sizes: chosen when compiled (of two stores in one kernel the
 // compiler keeps one, without the hint), and at small sizes the two differ by 0.3 us.
 template <bool STREAM, typename W>
@@ -362,35 +397,45 @@ __device__ __forceinline__ void put(void* p, W w) {
 }
 template <bool VEC, bool STREAM, int N>
 __device__ __forceinline__ void get_words(const void* p, uint32_t (&w)[N]) {
-  if constexpr (VEC && N == 4) {
-    const u32x4 u = get<STREAM, u32x4>(p);
+  if constexpr (N == 4) {
+    const u32x4 u = get<STREAM && VEC, std::conditional_t<VEC, u32x4, any_x4>>(p);
     w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
-  } else if constexpr (VEC && N == 2) {
-    const u32x2 u = get<STREAM, u32x2>(p);
+  } else if constexpr (N == 2) {
+    const u32x2 u = get<STREAM && VEC, std::conditional_t<VEC, u32x2, any_x2>>(p);
     w[0] = u.x, w[1] = u.y;
-  } else if constexpr (VEC) {
-    w[0] = get<STREAM, uint32_t>(p);
   } else {
-    __builtin_memcpy(w, p, 4 * N);
+    w[0] = get<STREAM && VEC, std::conditional_t<VEC, uint32_t, any_u32>>(p);
   }
 }
 template <bool VEC, bool STREAM, int N>
 __device__ __forceinline__ void put_words(void* p, const uint32_t (&w)[N]) {
-  if constexpr (VEC && N == 4)
-    put<STREAM>(p, (u32x4){w[0], w[1], w[2], w[3]});
-  else if constexpr (VEC && N == 2)
-    put<STREAM>(p, (u32x2){w[0], w[1]});
-  else if constexpr (VEC)
-    put<STREAM>(p, w[0]);
+  if constexpr (N == 4)
+    put<STREAM && VEC, std::conditional_t<VEC, u32x4, any_x4>>(p, (u32x4){w[0], w[1], w[2], w[3]});
+  else if constexpr (N == 2)
+    put<STREAM && VEC, std::conditional_t<VEC, u32x2, any_x2>>(p, (u32x2){w[0], w[1]});
   else
-    __builtin_memcpy(p, w, 4 * N);
+    put<STREAM && VEC, std::conditional_t<VEC, uint32_t, any_u32>>(p, w[0]);
+}
+
+// by value: of two array elements the compiler would choose the address
+template <typename T>
+__device__ __forceinline__ T either(bool c, T a, T b) {
+  return c ? a : b;
 }
 
 // cnt: how many of a lane's channels exist (all, fewer in a last lane, none or
-// less past it); not looked at in loads where VEC.
-template <bool VEC, bool STREAM>
+// less past it); not looked at in loads where VEC.  WIDE: the lane reads all of its
+// places in one go, past the row's end too (see Tile), and puts 0 in the place of what
+// isn't the row's.
+template <bool VEC>
+__device__ __forceinline__ void only(int cnt, float (&v)[CPL<VEC>]) {
+  if (VEC) return;
+#pragma unroll
+  for (int k = 0; k < CPL<VEC>; ++k) v[k] = k < cnt ? v[k] : 0.0f;
+}
+template <bool VEC, bool STREAM, bool WIDE = false>
 __device__ __forceinline__ void load_row(const float* p, int cnt, float (&v)[CPL<VEC>]) {
-  if (VEC || cnt == CPL<VEC>) {
+  if (VEC || WIDE || cnt == CPL<VEC>) {
 #pragma unroll
     for (int j = 0; j < CPL<VEC>; j += 4) {
       uint32_t w[4];
@@ -398,14 +443,15 @@ __device__ __forceinline__ void load_row(const float* p, int cnt, float (&v)[CPL
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[j + k] = __builtin_bit_cast(float, w[k]);
     }
+    if (WIDE) only<VEC>(cnt, v);
   } else {
 #pragma unroll
     for (int k = 0; k < CPL<VEC>; ++k) v[k] = k < cnt ? p[k] : 0.0f;
   }
 }
-template <bool VEC, bool STREAM>
+template <bool VEC, bool STREAM, bool WIDE = false>
 __device__ __forceinline__ void load_row(const __bf16* p, int cnt, float (&v)[CPL<VEC>]) {
-  if (VEC || cnt == CPL<VEC>) {
+  if (VEC || WIDE || cnt == CPL<VEC>) {
     uint32_t w[CPL<VEC> / 2];
     get_words<VEC, STREAM>(p, w);
 #pragma unroll
@@ -413,19 +459,21 @@ __device__ __forceinline__ void load_row(const __bf16* p, int cnt, float (&v)[CP
       v[2 * k] = __builtin_bit_cast(float, w[k] << 16);
       v[2 * k + 1] = __builtin_bit_cast(float, w[k] & 0xffff0000u);
     }
+    if (WIDE) only<VEC>(cnt, v);
   } else {
 #pragma unroll
     for (int k = 0; k < CPL<VEC>; ++k) v[k] = k < cnt ? (float)p[k] : 0.0f;
   }
 }
 // bytes of a checkpoint times their block's scale
-template <bool VEC, bool STREAM>
+template <bool VEC, bool STREAM, bool WIDE = false>
 __device__ __forceinline__ void load_row(const int8_t* p, float scale, int cnt, float (&v)[CPL<VEC>]) {
-  if (VEC || cnt == CPL<VEC>) {
+  if (VEC || WIDE || cnt == CPL<VEC>) {
     uint32_t w[CPL<VEC> / 4];
     get_words<VEC, STREAM>(p, w);
 #pragma unroll
     for (int k = 0; k < CPL<VEC>; ++k) v[k] = (float)((int32_t)(w[k / 4] << (24 - 8 * (k % 4))) >> 24) * scale;
+    if (WIDE) only<VEC>(cnt, v);
   } else {
 #pragma unroll
     for (int k = 0; k < CPL<VEC>; ++k) v[k] = k < cnt ? (float)p[k] * scale : 0.0f;
@@ -442,24 +490,32 @@ __device__ __forceinline__ void store_row(float* p, int cnt, const float (&v)[CP
       for (int k = 0; k < 4; ++k) w[k] = __builtin_bit_cast(uint32_t, v[j + k]);
       put_words<VEC, STREAM>(p + j, w);
     }
-  } else if (!VEC) {
+  } else if constexpr (!VEC) {   // a row's end in fours, twos and ones
+    uint32_t w[4], u[2];
 #pragma unroll
-    for (int k = 0; k < CPL<VEC>; ++k)
-      if (k < cnt) p[k] = v[k];
+    for (int k = 0; k < 4; ++k) w[k] = __builtin_bit_cast(uint32_t, v[k]);
+    if (cnt <= 0) return;
+    if (cnt & 4) put_words<VEC, STREAM>(p, w);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) u[k] = __builtin_bit_cast(uint32_t, either(cnt & 4, v[4 + k], v[k]));
+    if (cnt & 2) put_words<VEC, STREAM>(p + (cnt & 4), u);
+    if (cnt & 1) p[cnt - 1] = either(cnt & 4, either(cnt & 2, v[6], v[4]), either(cnt & 2, v[2], v[0]));
   }
 }
 template <bool VEC, bool STREAM>
 __device__ __forceinline__ void store_row(__bf16* p, int cnt, const float (&v)[CPL<VEC>]) {
+  uint32_t w[CPL<VEC> / 2];
+#pragma unroll
+  for (int k = 0; k < CPL<VEC> / 2; ++k)
+    w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){v[2 * k], v[2 * k + 1]}, bf16x2));
   if (cnt == CPL<VEC>) {
-    uint32_t w[CPL<VEC> / 2];
-#pragma unroll
-    for (int k = 0; k < CPL<VEC> / 2; ++k)
-      w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){v[2 * k], v[2 * k + 1]}, bf16x2));
     put_words<VEC, STREAM>(p, w);
-  } else if (!VEC) {
-#pragma unroll
-    for (int k = 0; k < CPL<VEC>; ++k)
-      if (k < cnt) p[k] = (__bf16)v[k];
+  } else if constexpr (!VEC) {
+    if (cnt <= 0) return;
+    const uint32_t two[2] = {w[0], w[1]}, one[1] = {either(cnt & 4, w[2], w[0])};
+    if (cnt & 4) put_words<VEC, STREAM>(p, two);
+    if (cnt & 2) put_words<VEC, STREAM>(p + (cnt & 4), one);
+    if (cnt & 1) p[cnt - 1] = (__bf16)either(cnt & 4, either(cnt & 2, v[6], v[4]), either(cnt & 2, v[2], v[0]));
   }
 }
 
@@ -471,8 +527,9 @@ struct Source {
   Mat<T> m;
   int cnt;
   __device__ __forceinline__ Source(const NormArgs& a, const Lanes<VEC>& L) : m(a.x, a.ldx, L.at(a.C)), cnt(L.cnt) {}
+  template <bool WIDE>
   __device__ __forceinline__ void load(int64_t i, int at, float (&v)[CPL<VEC>]) const {
-    load_row<VEC, STREAM>(m.row(i, at), cnt, v);
+    load_row<VEC, STREAM, WIDE>(m.row(i, at), cnt, v);
   }
 };
 template <bool VEC, bool STREAM>
@@ -483,8 +540,9 @@ struct Source<Q8, VEC, STREAM> {
   __device__ __forceinline__ Source(const NormArgs& a, const Lanes<VEC>& L)
       : m(a.x, a.C, L.at(a.C)),
         s(a.xscale, blocks_of(a.C), std::min(L.at(a.C), a.C - 1) / BLOCK_C), cnt(L.cnt) {}
+  template <bool WIDE>
   __device__ __forceinline__ void load(int64_t i, int at, float (&v)[CPL<VEC>]) const {
-    load_row<VEC, STREAM>(m.row(i, at), *s.row(i, at), cnt, v);
+    load_row<VEC, STREAM, WIDE>(m.row(i, at), *s.row(i, at), cnt, v);
   }
 };
 
@@ -501,8 +559,8 @@ struct Stream {
     float u[N][CPL<VEC>];
 #pragma unroll
     for (int t = 0; t < N; ++t) {
-      x.load(rows.first(i, t), rows.at(t), v[t]);
-      if (ADD) load_row<VEC, true>(add.row(rows.first(i, t), rows.at(t)), cnt, u[t]);
+      x.template load<FULL>(rows.first(i, t), rows.at(t), v[t]);
+      if (ADD) load_row<VEC, true, FULL>(add.row(rows.first(i, t), rows.at(t)), cnt, u[t]);
     }
     if (!FULL) {
       arrived(v);
@@ -613,10 +671,14 @@ struct Keep {
     int8_t* p = q.row(i, at);
     if (cnt == CPL<VEC>) {
       put_words<VEC, true>(p, w);
-    } else if (!VEC) {
-#pragma unroll
-      for (int k = 0; k < CPL<VEC>; ++k)
-        if (k < cnt) p[k] = (int8_t)(w[k / 4] >> (8 * (k % 4)));
+    } else if constexpr (!VEC) {
+      if (cnt > 0) {
+        const uint32_t four[1] = {w[0]}, u = either(cnt & 4, w[1], w[0]);
+        const uint16_t two = (uint16_t)u;
+        if (cnt & 4) put_words<VEC, true>(p, four);
+        if (cnt & 2) __builtin_memcpy(p + (cnt & 4), &two, 2);
+        if (cnt & 1) p[cnt - 1] = (int8_t)(cnt & 2 ? u >> 16 : u);
+      }
     }
     if (first) *s.row(i, at) = scale;
   }
@@ -921,7 +983,7 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_stats(NormArgs a) {
     const double inv = 1.0 / ((double)(pc.end - pc.r) * a.gs);
     float2* part = a.part + p * a.G;
     Moments<VEC> m;
-    over_rows<FWD_TILE<VEC>>(L, pc.r, pc.end, [&](int64_t i, const auto& rows) {
+    over_rows<FWD_TILE<VEC>>(L, pc.r, pc.end, a.n, [&](int64_t i, const auto& rows) {
       float v[std::decay_t<decltype(rows)>::N][CPL<VEC>];
       in.load(i, rows, v);
       if (a.ck) keep.store(i, rows, v);
@@ -1000,11 +1062,12 @@ __device__ __forceinline__ void apply_rows(const NormArgs& a, const Lanes<VEC>& 
   float scale[CPL<VEC>];
 #pragma unroll
   for (int k = 0; k < CPL<VEC>; ++k) scale[k] = rstd[k] * gamma[k];
-  pass_rows<FWD_TILE<VEC>, CPL<VEC>>(
-      L, r, end,
+  pass_rows<FWD_TILE<VEC>>(
+      L, r, end, a.n,
       [&](int64_t i, const auto& rows, auto& v) {
 #pragma unroll
-        for (int t = 0; t < std::decay_t<decltype(rows)>::N; ++t) in.load(rows.first(i, t), rows.at(t), v[t]);
+        for (int t = 0; t < std::decay_t<decltype(rows)>::N; ++t)
+          in.template load<std::decay_t<decltype(rows)>::FULL>(rows.first(i, t), rows.at(t), v[t]);
       },
       [&](int64_t i, const auto& rows, auto& v) {
 #pragma unroll
@@ -1191,13 +1254,14 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_sums(NormArgs a) {
     groups.read(stats_of(a, pc.s), nm.mean, nm.rstd);
     float2* part = a.part + p * a.G;
     float u[CPL<VEC>] = {}, v[CPL<VEC>] = {};
-    over_rows<BWD_TILE<VEC>>(L, pc.r, pc.end, [&](int64_t i, const auto& rows) {
+    over_rows<SUMS_TILE<VEC>>(L, pc.r, pc.end, a.n, [&](int64_t i, const auto& rows) {
       constexpr int N = std::decay_t<decltype(rows)>::N;
+      constexpr bool FULL = std::decay_t<decltype(rows)>::FULL;
       float t[N][CPL<VEC>], w[N][CPL<VEC>];
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        in.load(rows.first(i, j), rows.at(j), t[j]);
-        load_row<VEC, false>(gy.row(rows.first(i, j), rows.at(j)), L.cnt, w[j]);
+        in.template load<FULL>(rows.first(i, j), rows.at(j), t[j]);
+        load_row<VEC, false, FULL>(gy.row(rows.first(i, j), rows.at(j)), L.cnt, w[j]);
       }
       weigh_tile<ACT>(nm, rows, t, w, u, v);
     });
@@ -1246,14 +1310,14 @@ __device__ __forceinline__ void grad_rows(const NormArgs& a, const Lanes<VEC>& L
                                           const PerUnit<VEC>& B, int64_t r, int64_t end) {
   const Source<T, VEC, true> in(a, L);
   const Mat<float> gy(a.gy, a.ldgy, L.at(a.C)), ga(a.ga, a.ldga, L.at(a.C)), gx(a.gx, a.ldgx, L.c0);
-  over_rows<BWD_TILE<VEC>>(L, r, end, [&](int64_t i, const auto& rows) {
+  over_rows<BWD_TILE<VEC>>(L, r, end, a.n, [&](int64_t i, const auto& rows) {
     using TL = std::decay_t<decltype(rows)>;
     float t[TL::N][CPL<VEC>], w[TL::N][CPL<VEC>], g[TL::N][CPL<VEC>] = {};
 #pragma unroll
     for (int j = 0; j < TL::N; ++j) {
-      in.load(rows.first(i, j), rows.at(j), t[j]);
-      load_row<VEC, true>(gy.row(rows.first(i, j), rows.at(j)), L.cnt, w[j]);
-      if (a.ga) load_row<VEC, true>(ga.row(rows.first(i, j), rows.at(j)), L.cnt, g[j]);
+      in.template load<TL::FULL>(rows.first(i, j), rows.at(j), t[j]);
+      load_row<VEC, true, TL::FULL>(gy.row(rows.first(i, j), rows.at(j)), L.cnt, w[j]);
+      if (a.ga) load_row<VEC, true, TL::FULL>(ga.row(rows.first(i, j), rows.at(j)), L.cnt, g[j]);
     }
     if (!TL::FULL) {
       arrived(t);
@@ -1314,7 +1378,7 @@ __global__ __launch_bounds__(SNT) void k_norm_bwd_small(NormArgs a) {
   float t[TILE][CPL<VEC>], w[TILE][CPL<VEC>], u[CPL<VEC>] = {}, v[CPL<VEC>] = {};
 #pragma unroll
   for (int j = 0; j < TILE; ++j) {
-    in.load(0, rows.at(j), t[j]);
+    in.template load<false>(0, rows.at(j), t[j]);
     load_row<VEC, false>(gy.row(0, rows.at(j)), L.cnt, w[j]);
   }
   const Groups<VEC> groups(a, L.c0);
@@ -1421,10 +1485,10 @@ __global__ __launch_bounds__(RNT) void k_norm_rows(NormArgs a) {
   const Keep<VEC> keep(a, L);
   const Result<VEC> out(a, L);
   const Mat<float2> st(a.stats, a.G, 0);
-  for (int64_t i = (int64_t)blockIdx.x * L.RL; i < a.n; i += (int64_t)gridDim.x * L.RL) {
-    if (i + L.rl >= a.n) return;
+  each_row(L, a.n, [&](int64_t i, auto whole) {
+    constexpr bool WIDE = decltype(whole)::value;
     float t[1][CPL<VEC>], q[CPL<VEC>];
-    const Tile<1, true> row(L, L.RL);
+    const Tile<1, WIDE> row(L, L.RL);
     in.load(i, row, t);
     float(&v)[CPL<VEC>] = t[0];
     if (a.ck) keep.store(i, row, t);
@@ -1448,7 +1512,7 @@ __global__ __launch_bounds__(RNT) void k_norm_rows(NormArgs a) {
     for (int k = 0; k < CPL<VEC>; ++k)
       v[k] = activate<ACT>(__builtin_fmaf((v[k] - mean[k]) * rstd[k], gamma[k], beta[k]));
     out.store(i, L.rl, v);
-  }
+  });
 }
 
 template <bool VEC, int ACT>
@@ -1460,17 +1524,17 @@ __global__ __launch_bounds__(RNT) void k_norm_rows_restore(NormArgs a) {
   const Source<Q8, VEC> in(a, L);
   const Result<VEC> out(a, L);
   const Mat<float2> st(a.stats, a.G, 0);
-  for (int64_t i = (int64_t)blockIdx.x * L.RL; i < a.n; i += (int64_t)gridDim.x * L.RL) {
-    if (i + L.rl >= a.n) return;
+  each_row(L, a.n, [&](int64_t i, auto whole) {
+    constexpr bool WIDE = decltype(whole)::value;
     float v[CPL<VEC>];
     PerUnit<VEC> mean, rstd;
-    in.load(i, L.rl, v);
+    in.template load<WIDE>(i, L.rl, v);
     groups.read(st.row(i, L.rl), mean, rstd);
 #pragma unroll
     for (int k = 0; k < CPL<VEC>; ++k)
       v[k] = activate<ACT>(__builtin_fmaf((v[k] - mean[k]) * rstd[k], gamma[k], beta[k]));
     out.store(i, L.rl, v);
-  }
+  });
 }
 
 // The channels' sums stay in registers over all rows of a workgroup (4 to a CU, at most
@@ -1490,12 +1554,12 @@ __global__ __launch_bounds__(RNT) void k_norm_rows_bwd(NormArgs a) {
   const Source<T, VEC> in(a, L);
   const Mat<float> gy(a.gy, a.ldgy, L.at(a.C)), ga(a.ga, a.ldga, L.at(a.C)), gx(a.gx, a.ldgx, L.c0);
   const Mat<float2> st(a.stats, a.G, 0);
-  for (int64_t i = (int64_t)blockIdx.x * L.RL; i < a.n; i += (int64_t)gridDim.x * L.RL) {
-    if (i + L.rl >= a.n) break;
+  each_row(L, a.n, [&](int64_t i, auto whole) {
+    constexpr bool WIDE = decltype(whole)::value;
     float t[CPL<VEC>], w[CPL<VEC>], g[CPL<VEC>] = {}, x[CPL<VEC>], y[CPL<VEC>];
-    in.load(i, L.rl, t);
-    load_row<VEC, false>(gy.row(i, L.rl), L.cnt, w);
-    if (a.ga) load_row<VEC, false>(ga.row(i, L.rl), L.cnt, g);
+    in.template load<WIDE>(i, L.rl, t);
+    load_row<VEC, false, WIDE>(gy.row(i, L.rl), L.cnt, w);
+    if (a.ga) load_row<VEC, false, WIDE>(ga.row(i, L.rl), L.cnt, g);
     groups.read(st.row(i, L.rl), nm.mean, nm.rstd);
     nm.template weigh<ACT>(t, w);
 #pragma unroll
@@ -1511,7 +1575,7 @@ __global__ __launch_bounds__(RNT) void k_norm_rows_bwd(NormArgs a) {
     for (int j = 0; j < N; ++j) A.v[j] *= f, B.v[j] *= f;
     grad_row(nm, A, B, w, t, g);
     store_row<VEC, true>(gx.row(i, L.rl), L.cnt, g);
-  }
+  });
   if (!a.part_c) return;
   levels(L.lpr, [&](auto o) {
 #pragma unroll
@@ -1544,12 +1608,12 @@ __global__ __launch_bounds__(RNT) void k_ckpt_store(NormArgs a) {
   const Lanes<VEC> L(a.lg, a.C, RNT);
   const Source<T, VEC> in(a, L);
   const Keep<VEC> keep(a, L);
-  for (int64_t i = (int64_t)blockIdx.x * L.RL; i < a.n; i += (int64_t)gridDim.x * L.RL) {
-    if (i + L.rl >= a.n) return;
+  each_row(L, a.n, [&](int64_t i, auto whole) {
+    constexpr bool WIDE = decltype(whole)::value;
     float v[1][CPL<VEC>];
-    in.load(i, L.rl, v[0]);
-    keep.store(i, Tile<1, true>(L, L.RL), v);
-  }
+    in.template load<WIDE>(i, L.rl, v[0]);
+    keep.store(i, Tile<1, WIDE>(L, L.RL), v);
+  });
 }
 
 template <bool VEC>
@@ -1557,12 +1621,12 @@ __global__ __launch_bounds__(RNT) void k_ckpt_load(NormArgs a) {
   const Lanes<VEC> L(a.lg, a.C, RNT);
   const Source<Q8, VEC> in(a, L);
   const Result<VEC> out(a, L);
-  for (int64_t i = (int64_t)blockIdx.x * L.RL; i < a.n; i += (int64_t)gridDim.x * L.RL) {
-    if (i + L.rl >= a.n) return;
+  each_row(L, a.n, [&](int64_t i, auto whole) {
+    constexpr bool WIDE = decltype(whole)::value;
     float v[CPL<VEC>];
-    in.load(i, L.rl, v);
+    in.template load<WIDE>(i, L.rl, v);
     out.store(i, L.rl, v);
-  }
+  });
 }
 
 // ------------------------------------------------------------ host side

@@ -677,3 +677,39 @@ def test_few_rows_in_millions_of_segments(env):
     dx2, gr2 = lib.dsmp_group_norm_backward(d, x, st2, f, f, dy, segments=two)
     assert torch.allclose(dx, dx2, rtol=0, atol=1024 * U)
     assert all(torch.allclose(gr[k], gr2[k], rtol=0, atol=1024 * U) for k in gr)
+
+
+@pytest.mark.parametrize("n", [1, 7, 8, 9, 71, 72, 73, 700])
+@pytest.mark.parametrize("C,G", [(1, 1), (3, 3), (5, 1), (9, 3), (13, 1), (30, 5), (66, 6), (129, 3), (263, 1)])
+@pytest.mark.parametrize("rows", [False, True])
+def test_rows_are_read_no_further_than_the_matrix(env, n, C, G, rows):
+    # reads past a row's end stay in the matrix and never count: NaN between its rows, and it ends where
+    # its buffer does
+    dm, lib, torch = env
+    announce("norm row ends", n, C, G, rows)
+    for i, x in enumerate(("f32", "bf16")):
+        c = Case(torch, n, C, G, n if rows else [0, n // 2, n], x, ("bf16", "f32")[i], on.SILU, addend=True, seed=i)
+        d, seg = c.desc(dm), c.seg()
+
+        def apart(t, gap):
+            buf = torch.full(((n - 1) * (C + gap) + C,), float("nan"), dtype=t.dtype, device=t.device)
+            m = buf.as_strided((n, C), (C + gap, 1))
+            m.copy_(t)
+            return m
+
+        for gap in (0, 5):
+            total, ck = apart(c.x, gap), dm.Checkpoint.empty(n, C, c.x.device)
+            out, st = lib.dsmp_group_norm_forward(d, apart(c.x, gap), c.gamma, c.beta, segments=seg,
+                                                  addend=apart(c.addend, gap), sum_out=total, checkpoint=ck)
+            ref = c.check_stats(st, c.t64)
+            assert torch.equal(total, c.t)
+            c.check_y(out, c.t64, ref)
+            q, scale = on.checkpoint(_np(c.t))
+            assert np.array_equal(ck.q.cpu().numpy(), q) and np.array_equal(ck.scale.cpu().numpy(), scale)
+            kept, st64 = on.values(q, scale), _np(st).astype(np.float64)
+            c.check_y(lib.dsmp_group_norm_restore(d, ck, st, c.gamma, c.beta, segments=seg), kept, st64, "restored")
+            dx, grads = lib.dsmp_group_norm_backward(d, total, st, c.gamma, c.beta, apart(c.dy, gap), segments=seg,
+                                                     grad_addend=apart(c.grad_addend, gap))
+            c.check_backward(dx, grads, c.t64, st64, c.grad_addend)
+            again = lib.dsmp_checkpoint_store(apart(c.t, gap))
+            assert torch.equal(again.q, ck.q) and torch.equal(again.scale, ck.scale)
