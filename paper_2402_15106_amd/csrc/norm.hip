@@ -965,6 +965,11 @@ __device__ __forceinline__ void join_moments(const NormArgs& a, const Lanes<VEC>
   group_sums<W>(sh.s1, sh.s2, a.G, a.gs / U, out);
 }
 
+// A sum of squares about the mean that rounding has left below zero.  A NaN stays: an
+// infinity among the values makes one of it while the mean may be infinite, and a finite
+// rstd would then turn the group's other values into infinities, which ReLU hides.
+__device__ __forceinline__ double not_negative(double x) { return x < 0.0 ? 0.0 : x; }
+
 // First pass.  Per piece and group the mean and the sum of squares about it; adds and
 // writes checkpoints on the way.  Bound by memory: 262,144 x 128 float32 with addend
 // and sum 67 us (403 MB, 6.0 TB/s; the second pass's 37 us then reads from the cache in
@@ -991,7 +996,7 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_stats(NormArgs a) {
     });
     join_moments(a, L, m, sh, [&](int g, double u, double v) {
       const double mean = u * inv;
-      part[g] = make_float2((float)mean, (float)fmax(v - u * mean, 0.0));
+      part[g] = make_float2((float)mean, (float)not_negative(v - u * mean));
     });
     __syncthreads();
   }
@@ -1000,7 +1005,7 @@ __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_stats(NormArgs a) {
 // mean and rstd of a group from its sums about zero
 __device__ __forceinline__ float2 finish(double u, double v, double inv, float eps) {
   const double m = u * inv;
-  return make_float2((float)m, 1.0f / sqrtf((float)fmax(v * inv - m * m, 0.0) + eps));
+  return make_float2((float)m, 1.0f / sqrtf((float)not_negative(v * inv - m * m) + eps));
 }
 
 // ------------------------------------------------------------ joining the pieces

@@ -713,3 +713,30 @@ def test_rows_are_read_no_further_than_the_matrix(env, n, C, G, rows):
             c.check_backward(dx, grads, c.t64, st64, c.grad_addend)
             again = lib.dsmp_checkpoint_store(apart(c.t, gap))
             assert torch.equal(again.q, ck.q) and torch.equal(again.scale, ck.scale)
+
+
+@pytest.mark.parametrize("act", [on.RELU, on.IDENTITY])
+@pytest.mark.parametrize("n,C,G", [(300, 64, 4), (3000, 64, 4), (100, 160, 5), (3000, 160, 5), (3000, 33, 3), (200, 33, 3)])
+def test_an_infinity_leaves_no_number_in_its_group(env, n, C, G, act):
+    """x - mean and the variance of a group with an infinity are no numbers: neither is its rstd, nor any of its
+    results, whatever the place of the infinity and however its rows are joined."""
+    dm, lib, torch = env
+    c = C // G
+    for segments in (None, [0, n // 3, n // 3, n], n):
+        for bad in (float("inf"), -float("inf")):
+            k = Case(torch, n, C, G, segments, act=act)
+            clean, st0 = lib.dsmp_group_norm_forward(k.desc(dm), k.x, k.gamma, k.beta, segments=k.seg())
+            b = on.bounds(n, segments)
+            for i in (0, n // 3, n // 2, n - 1):
+                announce("norm infinity", n, C, G, act, segments, bad, i)
+                x = k.x.clone()
+                x[i, c + 1] = bad                                        # group 1
+                y, st = lib.dsmp_group_norm_forward(k.desc(dm), x, k.gamma, k.beta, segments=k.seg())
+                s = int(np.searchsorted(b, i, side="right")) - 1         # the segment that has the row
+                assert not torch.isfinite(st[s, 1, 0]) and torch.isnan(st[s, 1, 1])
+                hit = torch.zeros(n, C, dtype=torch.bool, device="cuda")
+                hit[b[s]:b[s + 1], c:2 * c] = True
+                assert torch.isnan(y[hit]).all() and torch.equal(y[~hit], clean[~hit])
+                other = torch.ones(st.shape[:2], dtype=torch.bool, device="cuda")
+                other[s, 1] = False
+                assert torch.equal(st[other], st0[other])
