@@ -70,6 +70,7 @@ class CheckpointedStack:
         self.gu = torch.empty(n, d, **f32)
         self.fws = torch.empty(max(fb, 256), dtype=torch.uint8, device=dev)
         self.bws = torch.empty(max(bb, 256), dtype=torch.uint8, device=dev)
+        self._holds = None      # with checkpoints: the layer whose operand and `saved` the buffers hold
 
     def kept_bytes(self) -> int:
         """Bytes held from the forward to the backward pass."""
@@ -97,11 +98,14 @@ class CheckpointedStack:
             if not end:
                 lib.dsmp_nnconv_forward(self.conv, packed[l], self.g, attr, self._at(self.u, l), h_out=self.f,
                                         saved=self._at(self.saved, l), ws=self.fws)
+                self._holds = l
         return self.y
 
     def backward(self, grad_y: torch.Tensor):
         """(grad_x, layer gradients, norm gradients) of sum(grad_y * y) for the
-        forward pass that came last, with its arguments as they were."""
+        forward pass that came last, with its arguments as they were.  It may be called
+        again, with another grad_y; with checkpoints the last layer's operand, which the
+        first call still has as it was, then comes from its checkpoint, as the others' do."""
         lib, s, seg = self.lib, self.s, self.segments
 
         def source(l):
@@ -112,11 +116,13 @@ class CheckpointedStack:
                                                            *self.norms[s.layers], grad_y, segments=seg)
         for l in reversed(range(s.layers)):
             u, saved = self._at(self.u, l), self._at(self.saved, l)
-            # the last layer's operand and what it saved are still there
-            if self.checkpoints and l < s.layers - 1:
+            # after the forward pass the last layer's operand and what it saved are still there
+            if self.checkpoints and l != self._holds:
+                self._holds = None
                 lib.dsmp_group_norm_restore(self.norm, self.kept[l], self.stats[l], *self.norms[l], segments=seg, y=u)
                 lib.dsmp_nnconv_forward(self.conv, self.packed[l], self.g, self.attr, u, h_out=self.f, saved=saved,
                                         ws=self.fws)
+                self._holds = l
             _, conv_g[l] = lib.dsmp_nnconv_backward(self.conv, self.packed[l], self.g, self.attr, u, saved, G,
                                                     grad_h=self.gu, ws=self.bws)
             _, norm_g[l] = lib.dsmp_group_norm_backward(self.norm, source(l), self.stats[l], *self.norms[l], self.gu,

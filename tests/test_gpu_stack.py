@@ -169,3 +169,41 @@ def test_refuses_graphs_with_halo_rows(env):
         with pytest.raises(dm.DsmpError) as e:
             dm.CheckpointedStack(lib, g, shapes)
         assert e.value.status == dm.INVALID_ARG
+
+
+@pytest.mark.parametrize("checkpoints", [True, False])
+@pytest.mark.parametrize("n,d,h,dtype,segments", [CASES[1], CASES[2]])
+def test_backward_again_with_another_gradient(env, n, d, h, dtype, segments, checkpoints):
+    """A second and a third backward of one forward pass: the gradients of the new grad_y, and the
+    same bits where it is the same."""
+    dm, lib, torch = env
+    announce("stack backward again", n, d, dtype, segments, checkpoints)
+    c = Setup(env, n, d, h, dtype, segments, checkpoints)
+    st = c.stack
+    bar = TOL["f32"] if dtype == "f32" else LAYERS * TOL["bf16"]
+    st.forward(*c.args)
+    stats = [_np(t) for t in st.stats]
+    last_u = st._at(st.u, LAYERS - 1).clone()
+    if checkpoints:
+        t = [on.values(k.q.cpu().numpy(), k.scale.cpu().numpy()).astype(np.float64) for k in st.kept]
+        last_u = lib.dsmp_group_norm_restore(st.norm, st.kept[LAYERS - 1], st.stats[LAYERS - 1], *c.args[1][LAYERS - 1],
+                                             segments=st.segments)
+    else:
+        t = [c.x.astype(np.float64)] + [_np(v) for v in st.stream]
+    st.backward(c.gyc)
+    c.gy = np.random.default_rng(99).normal(size=c.gy.shape).astype(np.float32)
+    gyc = torch.from_numpy(c.gy).cuda()
+    runs = []
+    for _ in range(2):
+        gx, conv, norm = st.backward(gyc)
+        runs.append([gx.clone()] + [v.clone() for m in conv + norm for v in m.values()])
+    for u, v in zip(*runs):
+        assert np.array_equal(_np(u), _np(v))
+    rgx, rconv, rnorm = c.reference_grads(t, stats, _np(last_u))
+    assert rel_err(_np(gx), rgx) <= bar, "grad_x"
+    for l in range(LAYERS):
+        for k in ("dW3", "db3", "dWr", "dbr"):
+            assert rel_err(_np(conv[l][k]), rconv[l][k]) <= bar, (l, k)
+    for l in range(LAYERS + 1):
+        assert rel_err(_np(norm[l]["dgamma"]), rnorm[l][0]) <= bar, (l, "dgamma")
+        assert rel_err(_np(norm[l]["dbeta"]), rnorm[l][1]) <= bar, (l, "dbeta")
