@@ -1594,10 +1594,10 @@ __global__ __launch_bounds__(RNT) void k_norm_rows_bwd(NormArgs a) {
   }
   __syncthreads();
   for (int c = threadIdx.x; c < a.C; c += RNT) {
-    float x = 0.0f, y = 0.0f;
+    double x = 0.0, y = 0.0;
     for (int w = 0; w < RNT / 64; ++w) x += lds[w * 2 * w8 + c], y += lds[w * 2 * w8 + w8 + c];
-    a.part_c[(int64_t)blockIdx.x * 2 * a.C + c] = x;
-    a.part_c[(int64_t)blockIdx.x * 2 * a.C + a.C + c] = y;
+    a.part_c[(int64_t)blockIdx.x * 2 * a.C + c] = (float)x;
+    a.part_c[(int64_t)blockIdx.x * 2 * a.C + a.C + c] = (float)y;
   }
 }
 

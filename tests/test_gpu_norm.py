@@ -740,3 +740,23 @@ def test_an_infinity_leaves_no_number_in_its_group(env, n, C, G, act):
                 other = torch.ones(st.shape[:2], dtype=torch.bool, device="cuda")
                 other[s, 1] = False
                 assert torch.equal(st[other], st0[other])
+
+
+def test_rows_gradients_of_the_parameters_join_in_more_than_32_bits(env):
+    """Each row a segment: the sums of a workgroup's four waves, 2^26, 1, 1 and -2^26, give 2 (in float32, 0)."""
+    dm, lib, torch = env
+    announce("norm rows, joined sums")
+    n, C = 32, 32                                   # eight rows to a wave
+    g = np.random.default_rng(1)
+    x = torch.tensor(g.normal(size=(n, C)), dtype=torch.float32, device="cuda")
+    x[24] = x[0]
+    f, dy = torch.ones(C, device="cuda"), torch.zeros(n, C, device="cuda")
+    for row, v in ((0, 2.0 ** 26), (8, 1.0), (16, 1.0), (24, -2.0 ** 26)):
+        dy[row] = v
+    d = dm.norm_desc(C, 4, dm.F32, dm.F32, dm.ACT_IDENTITY)
+    _, st = lib.dsmp_group_norm_forward(d, x, f, 0 * f, segments=n)
+    _, grads = lib.dsmp_group_norm_backward(d, x, st, f, 0 * f, dy, segments=n)
+    assert (grads["dbeta"] == 2).all()
+    xn = on.normalised(_np(x), _np(st).astype(np.float64), n)
+    # the two large terms are equal and opposite; what is left is two values' own roundings
+    assert (np.abs(_np(grads["dgamma"]) - (xn[8] + xn[16])) <= 16 * U * (1 + np.abs(xn[8]) + np.abs(xn[16]))).all()
