@@ -12,6 +12,8 @@ element to bounds that follow from the operations, with u = 2^-24:
   outputs in bfloat16 add 2^-8 |value| (half a unit in the last place), with 1 % to spare
 """
 
+import math
+
 import numpy as np
 import pytest
 
@@ -760,3 +762,49 @@ def test_rows_gradients_of_the_parameters_join_in_more_than_32_bits(env):
     xn = on.normalised(_np(x), _np(st).astype(np.float64), n)
     # the two large terms are equal and opposite; what is left is two values' own roundings
     assert (np.abs(_np(grads["dgamma"]) - (xn[8] + xn[16])) <= 16 * U * (1 + np.abs(xn[8]) + np.abs(xn[16]))).all()
+
+
+def _gelu(z):
+    """GELU and its slope, with the tail's own digits."""
+    z = np.asarray(z, np.float64)
+    tail = np.array([0.5 * math.erfc(abs(v) / math.sqrt(2.0)) for v in z.ravel()]).reshape(z.shape)
+    phi = np.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+    return np.where(z < 0, z * tail, z * (1 - tail)), np.where(z < 0, tail, 1 - tail) + z * phi, tail, phi
+
+
+def test_gelu_keeps_the_digits_of_its_tail(env):
+    """GELU and its slope at chosen arguments (mean 0, rstd 1), relative to their size.
+
+    The tail: 3 u of the polynomial, 1 of its coefficients, 3 of its argument times at most 2.6 (how much
+    faster than the argument it changes), 6 of the evaluation, products and the exponential, and 1.2 z^2 u of
+    the exponent's roundings; with 10 % to spare below (20 + 1.5 z^2) u."""
+    dm, lib, torch = env
+    announce("norm GELU tail")
+    n, C = 50, 256
+    q = torch.arange(n * C, device="cuda").view(n, C) % 255 - 127
+    scale = torch.linspace(0.001, 12.4 / 127, n * 4, device="cuda").view(n, 4)
+    ck = dm.Checkpoint(q.to(torch.int8), scale)
+    z = _np(ck.q.float() * scale.repeat_interleave(64, 1)).astype(np.float64)
+    want, slope, tail, phi = _gelu(z)
+    rel = (20 + 1.5 * z * z) * U
+    for segments in (None, n):
+        for C2, G in ((C, 4), (250, 5)):           # whole groups of four channels, and others
+            part = dm.Checkpoint(ck.q[:, :C2].contiguous(), scale)
+            st = torch.zeros(n if segments else 1, G, 2, device="cuda")
+            st[:, :, 1] = 1.0
+            y = lib.dsmp_group_norm_restore(dm.norm_desc(C2, G, dm.F32, dm.F32, dm.ACT_GELU), part, st, None, None,
+                                            segments=segments)
+            ref, zz = want[:, :C2], z[:, :C2]
+            tol = np.abs(zz) * tail[:, :C2] * rel[:, :C2] + 3 * U * np.abs(ref) + 1e-37
+            err = np.abs(_np(y).astype(np.float64) - ref)
+            assert (err <= tol).all(), float((err / tol).max())
+    # a row by itself: dbeta is the slope at each of its arguments
+    f = torch.ones(C, device="cuda")
+    st = torch.tensor([0.0, 1.0], device="cuda").expand(1, 4, 2).contiguous()
+    d = dm.norm_desc(C, 4, dm.F32, dm.F32, dm.ACT_GELU)
+    for i in range(n):
+        row = dm.Checkpoint(ck.q[i:i + 1].contiguous(), scale[i:i + 1].contiguous())
+        _, grads = lib.dsmp_group_norm_backward(d, row, st, f, 0 * f, torch.ones(1, C, device="cuda"))
+        tol = (tail[i] + np.abs(z[i]) * phi[i]) * rel[i] + 3 * U * np.abs(slope[i]) + 1e-36
+        err = np.abs(_np(grads["dbeta"]).astype(np.float64) - slope[i])
+        assert (err <= tol).all(), (i, float((err / tol).max()))
