@@ -180,6 +180,10 @@ def _current_stream(index: int) -> int:
     return torch.cuda.current_stream(index).cuda_stream if _raw_stream is None else _raw_stream(index)
 
 
+# whether the current stream is being captured, without the function around it
+_capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", torch.cuda.is_current_stream_capturing)
+
+
 _lib = None
 
 
@@ -590,8 +594,8 @@ class Dsmp:
             self._check(st, self.h)
         return s
 
-    def _norm_ws(self, desc, C, seg, n, backward):
-        """Binds the current stream; address and size of the scratch buffer that its calls share."""
+    def _norm_size(self, desc, C, seg, n):
+        """Workspace bytes of the forward and the backward call."""
         key = (C, desc.groups, n, seg.n_seg, seg.ptr is None)
         sizes = self._norm_sizes.get(key)
         if sizes is None:
@@ -601,8 +605,26 @@ class Dsmp:
             if len(self._norm_sizes) >= 1024:
                 self._norm_sizes.clear()
             sizes = self._norm_sizes[key] = (f.value, b.value)
-        ws = self.workspace(("norm", self._bind_current()), sizes[backward])
+        return sizes
+
+    def _norm_ws(self, desc, C, seg, n, backward, ws):
+        """Binds the current stream; address and size of the scratch buffer: the caller's, or the one
+        that the stream's calls share.  A captured call gets one from the graph's own memory: its address
+        stays in the graph, while the shared one is replaced when a larger call comes, and is used by the
+        stream's other calls while the graph may be replayed on another."""
+        size = self._norm_size(desc, C, seg, n)[backward]
+        stream = self._bind_current()
+        if ws is not None:
+            return self._flat(ws, "ws", (ws.numel(),) if isinstance(ws, torch.Tensor) else (), torch.uint8), ws.numel()
+        if _capturing():
+            ws = torch.empty(max(size, 256), dtype=torch.uint8, device=self.device)
+        else:
+            ws = self.workspace(("norm", stream), size)
         return ws.data_ptr(), ws.numel()
+
+    def dsmp_group_norm_workspace(self, desc: NormDesc, n: int, segments=None):
+        """Bytes of scratch that dsmp_group_norm_forward and _backward need for n rows (their ws): (forward, backward)."""
+        return self._norm_size(desc, desc.channels, self._segments(n, segments), n)
 
     def dsmp_checkpoint_store(self, x: torch.Tensor, out: Optional[Checkpoint] = None) -> Checkpoint:
         """Keep the rows of x (float32 or bfloat16 [n, channels]) in 8 bits."""
@@ -634,13 +656,15 @@ class Dsmp:
         return y
 
     def dsmp_group_norm_forward(self, desc: NormDesc, x, gamma, beta, segments=None, addend=None, sum_out=None, y=None,
-                                stats=None, checkpoint: Optional[Checkpoint] = None):
+                                stats=None, checkpoint: Optional[Checkpoint] = None, ws=None):
         """y = act(norm(t) gamma + beta) with t = x (+ addend); returns (y, stats).
 
         segments: None (all rows), the number of equal segments (x.shape[0]:
         each row its own), or an int32 tensor of the n_seg + 1 segment bounds.
         sum_out receives t (needed with an addend; x or addend itself may be
-        given); checkpoint, if given, receives t in 8 bits."""
+        given); checkpoint, if given, receives t in 8 bits.  ws: scratch of the caller's
+        own (uint8, dsmp_group_norm_workspace), in place of the library's; needed in a capture
+        that torch.cuda.graph does not make."""
         C, n = desc.channels, x.shape[0]
         rows = (n, C)
         seg = self._segments(n, segments)
@@ -655,7 +679,7 @@ class Dsmp:
         stats = torch.empty(shape, dtype=torch.float32, device=self.device) if stats is None else stats
         stp = self._flat(stats, "stats", shape)
         ck = None if checkpoint is None else self._checkpoint(checkpoint, rows)
-        ws, ws_bytes = self._norm_ws(desc, C, seg, n, False)
+        ws, ws_bytes = self._norm_ws(desc, C, seg, n, False, ws)
         st = self.lib.dsmp_group_norm_forward(self.h, desc, seg, xp, ldx, ap, lda, sp, lds, gp, bp, yp, ldy, stp, ck, ws,
                                               ws_bytes)
         if st:
@@ -680,10 +704,10 @@ class Dsmp:
         return y
 
     def dsmp_group_norm_backward(self, desc: NormDesc, source, stats, gamma, beta, grad_y, segments=None,
-                                 grad_addend=None, grad_x=None, grads: Optional[dict] = None, flags: int = 0):
+                                 grad_addend=None, grad_x=None, grads: Optional[dict] = None, flags: int = 0, ws=None):
         """Gradients of the forward that left stats, from t itself or its
         Checkpoint (source); returns (grad_x, {"dgamma", "dbeta"}).  grad_addend
-        (which may be grad_x itself) is added to grad_x."""
+        (which may be grad_x itself) is added to grad_x.  ws: as for the forward."""
         kept = isinstance(source, Checkpoint)
         C, n = desc.channels, (source.q if kept else source).shape[0]
         rows = (n, C)
@@ -702,7 +726,7 @@ class Dsmp:
         else:
             grads = {"dgamma": torch.empty(C, **f32), "dbeta": torch.empty(C, **f32)} if grads is None else grads
             dg, db = self._flat(grads["dgamma"], "dgamma", (C,)), self._flat(grads["dbeta"], "dbeta", (C,))
-        ws, ws_bytes = self._norm_ws(desc, C, seg, n, True)
+        ws, ws_bytes = self._norm_ws(desc, C, seg, n, True, ws)
         st = self.lib.dsmp_group_norm_backward(self.h, desc, seg, xp, ldx, ck, stp, gp, bp, dyp, ldgy, gap, ldga, dxp,
                                                ldgx, dg, db, flags, ws, ws_bytes)
         if st:

@@ -808,3 +808,53 @@ def test_gelu_keeps_the_digits_of_its_tail(env):
         tol = (tail[i] + np.abs(z[i]) * phi[i]) * rel[i] + 3 * U * np.abs(slope[i]) + 1e-36
         err = np.abs(_np(grads["dbeta"]).astype(np.float64) - slope[i])
         assert (err <= tol).all(), (i, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("own", [False, True])
+def test_a_graph_keeps_its_scratch_to_itself(env, own):
+    """Captured calls, then a larger eager call on the capturing stream and new tensors there, then replays: the graph
+    writes nothing of theirs and gives what eager calls do, beside eager work on the capturing stream too."""
+    dm, lib, torch = env
+    announce("norm graph scratch", own)
+    n, C, G = 30000, 64, 8
+    c = Case(torch, n, C, G, [0, 9000, n], "f32", "f32")
+    d, seg = c.desc(dm), c.seg()
+    big = Case(torch, 80000, 256, 64)
+    b = {"y": torch.empty_like(c.x), "st": torch.empty(2, G, 2, device="cuda"), "dx": torch.empty_like(c.x),
+         "dgamma": torch.empty(C, device="cuda"), "dbeta": torch.empty(C, device="cuda")}
+    ws = torch.empty(max(lib.dsmp_group_norm_workspace(d, n, seg)), dtype=torch.uint8, device="cuda") if own else None
+
+    def go(out, ws=None):
+        lib.dsmp_group_norm_forward(d, c.x, c.gamma, c.beta, segments=seg, y=out["y"], stats=out["st"], ws=ws)
+        lib.dsmp_group_norm_backward(d, c.x, out["st"], c.gamma, c.beta, c.dy, segments=seg, grad_x=out["dx"],
+                                     grads={"dgamma": out["dgamma"], "dbeta": out["dbeta"]}, ws=ws)
+
+    want = {k: torch.empty_like(v) for k, v in b.items()}
+    go(want)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        go({k: torch.empty_like(v) for k, v in b.items()})        # the stream has a scratch buffer
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        go(b, ws)
+    big_desc = big.desc(dm)
+    big_y, big_st = lib.dsmp_group_norm_forward(big_desc, big.x, big.gamma, big.beta)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        lib.dsmp_group_norm_forward(big_desc, big.x, big.gamma, big.beta)     # needs a larger one
+        new = [torch.full((size,), 7, dtype=torch.uint8, device="cuda")
+               for size in (1 << 9, 1 << 12, 1 << 16, 1 << 18, 1 << 20, 1 << 21) for _ in range(8)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for v in b.values():
+            v.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            y, st = lib.dsmp_group_norm_forward(big_desc, big.x, big.gamma, big.beta)
+        graph.replay()                                            # on the current stream, beside that call
+        torch.cuda.synchronize()
+        assert torch.equal(y, big_y) and torch.equal(st, big_st)
+        for k in b:
+            assert torch.equal(bits(b[k]), bits(want[k])), k
+        assert all((t == 7).all() for t in new)
