@@ -858,3 +858,80 @@ def test_a_graph_keeps_its_scratch_to_itself(env, own):
         for k in b:
             assert torch.equal(bits(b[k]), bits(want[k])), k
         assert all((t == 7).all() for t in new)
+
+
+@pytest.mark.parametrize("C,G", [(32, 4), (128, 32), (100, 10), (147, 7), (512, 512), (1, 1)])
+@pytest.mark.parametrize("n,segments", [(1, None), (37, 37), (700, [0, 0, 71, 700, 700]), (40000, None), (40000, 4000),
+                                        (5000, "many")])
+def test_calls_stay_within_a_workspace_of_the_reported_size(env, n, segments, C, G):
+    dm, lib, torch = env
+    announce("norm workspace", n, C, G, segments)
+    segments = _many(n, 2500, 7) if segments == "many" else segments
+    guard = 4096
+    for x in ("f32", "bf16"):
+        c = Case(torch, n, C, G, segments, x, "f32")
+        d, seg = c.desc(dm), c.seg()
+        sizes = lib.dsmp_group_norm_workspace(d, n, seg)
+        y0, st0 = lib.dsmp_group_norm_forward(d, c.x, c.gamma, c.beta, segments=seg)
+        dx0, g0 = lib.dsmp_group_norm_backward(d, c.x, st0, c.gamma, c.beta, c.dy, segments=seg)
+
+        def within(size, call):
+            buf = torch.full((size + 2 * guard,), 0xAB, dtype=torch.uint8, device="cuda")
+            out = call(buf[guard:guard + size])
+            assert (buf[:guard] == 0xAB).all() and (buf[guard + size:] == 0xAB).all()
+            return out
+
+        y, st = within(sizes[0], lambda ws: lib.dsmp_group_norm_forward(d, c.x, c.gamma, c.beta, segments=seg, ws=ws))
+        dx, g = within(sizes[1], lambda ws: lib.dsmp_group_norm_backward(d, c.x, st, c.gamma, c.beta, c.dy,
+                                                                         segments=seg, ws=ws))
+        for u, v in ((y, y0), (st, st0), (dx, dx0), (g["dgamma"], g0["dgamma"]), (g["dbeta"], g0["dbeta"])):
+            assert torch.equal(bits(u), bits(v))
+        for size, call in ((sizes[0], lambda ws: lib.dsmp_group_norm_forward(d, c.x, c.gamma, c.beta, segments=seg, ws=ws)),
+                           (sizes[1], lambda ws: lib.dsmp_group_norm_backward(d, c.x, st, c.gamma, c.beta, c.dy,
+                                                                              segments=seg, ws=ws))):
+            if size:
+                with pytest.raises(dm.DsmpError) as e:
+                    call(torch.empty(size - 1, dtype=torch.uint8, device="cuda"))
+                assert e.value.status == dm.WORKSPACE_TOO_SMALL
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("n,C,G", [(300, 32, 2), (20000, 32, 2), (20000, 33, 3), (60000, 64, 1)])
+def test_statistics_and_results_far_from_zero(env, n, C, G, x):
+    """Values at 1e3 and 1e5 times their deviation, whose means are float32 values.
+
+    Mean: 8 u |mean|.  A tile adds 16 values one by one, 1.4 u |mean| rms, before that averages out over
+    tiles; a row's 64 channels give 0.6 u rms; six times that, a join and the kept mean's own rounding.
+    rstd: squares are taken about the means of tiles, so an error `off` of a mean, in deviations, adds
+    off^2; it also meets the tile's own distance from the mean, a quarter of a deviation for 16 values,
+    which averages out over the N tiles: six deviations of that, off / 4 * 6 / sqrt N, at most off / 4.  Its
+    own sums: 32 u."""
+    dm, lib, torch = env
+    for offset in (1e3, 1e5):
+        for segments in (None, [0, n // 3, n], n):
+            announce("norm far from zero", n, C, G, x, offset, segments)
+            c = Case(torch, n, C, G, segments, x, "f32", on.IDENTITY, offset=0.0, affine=False)
+            if x == "bf16":       # whole steps of bfloat16's spacing there
+                step = 2.0 ** (math.floor(math.log2(offset)) - 7)
+                c.x = (c.x.float().clamp(-20, 20).round() * step + math.floor(offset / step) * step).bfloat16()
+            else:
+                c.x = c.x + offset
+            t64, per = _np(c.x).astype(np.float64), C // G
+            y, st = lib.dsmp_group_norm_forward(c.desc(dm), c.x, None, None, segments=c.seg())
+            if segments == n:
+                v = t64.reshape(n, G, per)
+                mean, tiles = v.mean(2), 1
+                ref = np.stack([mean, 1 / np.sqrt(((v - mean[:, :, None]) ** 2).mean(2) + c.eps)], -1)
+            else:
+                ref, tiles = on.statistics(t64, segments, G, c.eps), n // 3 * per / 16
+            got = _np(st).astype(np.float64)
+            emean = 8 * U * np.abs(t64).max()
+            assert (np.abs(got[:, :, 0] - ref[:, :, 0]) <= emean).all()
+            off = emean * ref[:, :, 1]
+            tol = off * off + off / 4 * min(1.0, 6 / math.sqrt(tiles)) + 32 * U
+            far = np.abs(got[:, :, 1] / ref[:, :, 1] - 1)
+            assert (far <= tol).all(), float((far / tol).max())
+            xn = on.normalised(t64, ref, segments)
+            row = np.repeat(np.arange(len(ref)), np.diff(on.bounds(n, segments)))
+            most = np.repeat(off[row], per, 1) + np.abs(xn) * (np.repeat(tol[row], per, 1) + 8 * U) + 2 * U
+            assert (np.abs(_np(y).astype(np.float64) - xn) <= most).all()
