@@ -70,6 +70,7 @@ class CheckpointedStack:
         self.gu = torch.empty(n, d, **f32)
         self.fws = torch.empty(max(fb, 256), dtype=torch.uint8, device=dev)
         self.bws = torch.empty(max(bb, 256), dtype=torch.uint8, device=dev)
+        self._whole = False     # a forward pass has ended
         self._holds = None      # with checkpoints: the layer whose operand and `saved` the buffers hold
 
     def kept_bytes(self) -> int:
@@ -87,6 +88,7 @@ class CheckpointedStack:
         """y [n, d] of the stack on x (float32 [n, d], left as it is).  packed: each
         layer's parameters (dsmp_nnconv_pack); norms: layers + 1 pairs (gamma, beta)."""
         lib, s = self.lib, self.s
+        self._whole, self._holds = False, None
         self.attr, self.packed, self.norms, self.x = attr, packed, norms, x
         for l in range(s.layers + 1):
             end = l == s.layers
@@ -99,6 +101,7 @@ class CheckpointedStack:
                 lib.dsmp_nnconv_forward(self.conv, packed[l], self.g, attr, self._at(self.u, l), h_out=self.f,
                                         saved=self._at(self.saved, l), ws=self.fws)
                 self._holds = l
+        self._whole = True
         return self.y
 
     def backward(self, grad_y: torch.Tensor):
@@ -106,6 +109,8 @@ class CheckpointedStack:
         forward pass that came last, with its arguments as they were.  It may be called
         again, with another grad_y; with checkpoints the last layer's operand, which the
         first call still has as it was, then comes from its checkpoint, as the others' do."""
+        if not self._whole:
+            raise L.DsmpError(L.INVALID_ARG, "no forward pass that came to its end")
         lib, s, seg = self.lib, self.s, self.segments
 
         def source(l):

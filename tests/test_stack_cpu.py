@@ -68,3 +68,23 @@ def test_every_backward_runs_on_its_own_layers_operand(checkpoints, layers):
             lib.seen.clear()
             s.backward(torch.zeros(N, D))
             assert lib.seen == want
+
+
+@pytest.mark.parametrize("checkpoints", [True, False])
+def test_no_backward_of_a_forward_that_did_not_end(checkpoints):
+    """Before any forward pass, and after one that raised on its way over an earlier one's buffers."""
+    lib, s, args = stack(checkpoints)
+    with pytest.raises(dm.DsmpError) as e:
+        s.backward(torch.zeros(N, D))
+    assert e.value.status == dm.INVALID_ARG
+    s.forward(*args)
+    s.backward(torch.zeros(N, D))
+    with pytest.raises(IndexError):
+        s.forward(args[0][:2], *args[1:])
+    lib.seen.clear()
+    with pytest.raises(dm.DsmpError):
+        s.backward(torch.zeros(N, D))
+    assert not lib.seen
+    s.forward(*args)
+    s.backward(torch.zeros(N, D))
+    assert len(lib.seen) == LAYERS
