@@ -9,6 +9,7 @@ the import fails: there is no fallback.
 """
 
 import ctypes
+import operator
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -580,8 +581,17 @@ class Dsmp:
         if segments is None:
             return CSegments(n, 1, None)
         if isinstance(segments, torch.Tensor):
-            return CSegments(n, segments.numel() - 1, self._flat(segments, "segments", (segments.numel(),), torch.int32))
-        return CSegments(n, int(segments), None)
+            k = segments.numel() - 1
+            if k < 1:
+                raise DsmpError(INVALID_ARG, "segments: bounds of one segment at least are needed")
+            return CSegments(n, k, self._flat(segments, "segments", (k + 1,), torch.int32))
+        try:
+            k = operator.index(segments)
+        except TypeError:
+            raise DsmpError(INVALID_ARG, "segments: a whole number or a tensor of bounds is needed") from None
+        if k < 1 or n % k:
+            raise DsmpError(INVALID_ARG, "segments: %d do not divide %d rows" % (k, n))
+        return CSegments(n, k, None)
 
     def _norm_params(self, C, gamma, beta):
         return (None if gamma is None else self._flat(gamma, "gamma", (C,)),
