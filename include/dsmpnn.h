@@ -412,7 +412,8 @@ dsmp_status dsmp_checkpoint_load(dsmp_handle* h, const dsmp_checkpoint* ck, int6
  *     mean = sum t / m,  var = sum (t - mean)^2 / m,  rstd = 1 / sqrt(var + eps)
  *     xn = (t - mean) * rstd,  z = gamma xn + beta,  y = act(z)
  * Statistics and sums are float32 or wider whatever the types.  Segments of no
- * rows get mean 0 and rstd 0.  groups = 1 with one row to a segment is a
+ * rows get mean 0 and rstd 0; a group that holds an infinity or a NaN has a rstd
+ * of NaN, and no number among its results.  groups = 1 with one row to a segment is a
  * normalisation of every row over its channels. */
 typedef struct dsmp_norm_desc {
   int32_t channels;  /* 1..512, others give UNSUPPORTED */

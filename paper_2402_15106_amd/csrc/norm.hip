@@ -21,7 +21,9 @@
 // apart, and a checkpoint's block of 64 channels is 16 (8) neighbouring lanes.
 //
 // Sums run in a fixed order (lane, wave, piece): no atomics, the same bits on
-// every run.  A lane sums in float32; across waves, and across pieces, in float64.
+// every run.  A lane sums its rows and a wave its lanes in float32, so a lane's number of
+// roundings grows with the rows: it has about rows x lanes of a row / 131,072 of them.  Across
+// waves, and across pieces, sums are in float64.
 //
 // The times below are kernel times on one MI355X, whose large copy runs at 5,144 GB/s
 // (read and written bytes together).
@@ -746,7 +748,10 @@ __device__ __forceinline__ int64_t seg_end(const NormArgs& a, int s) {
 // The passes' units of work are pieces: the rows that a segment s has in a chunk j of R
 // rows.  Piece j + s: as rows go on, either the chunk or the segment is the next one,
 // so the numbers of a segment's pieces follow each other, and every number up to
-// chunks + segments is one piece or none.
+// chunks + segments is one piece or none.  A piece takes a workgroup through all
+// barriers of the joining, however few rows it has: 65,536 x 64 bfloat16 in 4,096 segments
+// of 16 rows takes 33 + 28 us forward and 32 + 30 backward, in one segment 5.6 + 7.4 and
+// 8.5 + 7.9.
 struct Piece {
   int s;
   int64_t b, e;    // the segment's rows
@@ -849,7 +854,10 @@ __device__ __forceinline__ float2* stats_of(const NormArgs& a, int s) {
 
 // Rows, and for each unit the mean and the sum of squares about it.  Rows join
 // a few at a time (mean of the tile, then deviations from it, then the pair rule
-// of Chan, Golub and LeVeque), so a large mean or a far-out row costs no digits.
+// of Chan, Golub and LeVeque), so a large mean or a far-out row costs the variance no
+// digits.  The means themselves are float32 values, of a lane, a piece and in stats: off by
+// a few units in the last place at most, which xn has times rstd (at a mean of 10^4
+// deviations half a unit is 5e-4 of one).
 template <bool VEC>
 struct Moments {
   static constexpr int U = UNIT<VEC>, N = CPL<VEC> / U;
@@ -978,8 +986,9 @@ __device__ __forceinline__ double not_negative(double x) { return x < 0.0 ? 0.0 
 // writes checkpoints on the way.  Bound by memory: 262,144 x 128 float32 with addend
 // and sum 67 us (403 MB, 6.0 TB/s; the second pass's 37 us then reads from the cache in
 // part); 285,564 x 128 with a checkpoint too 85 us (477 MB, 5.6 TB/s).  At 99,991 x 64
-// bfloat16 in 37 segments 8.9 us for 12.8 MB: two tiles to a workgroup, so its launch,
-// one load's way and the joining over lanes and waves are what it takes.
+// bfloat16 in 37 segments 8.6 us for 12.8 MB: its chunks are 15 steps of rows, three whole
+// tiles and then two halves, each waited for by itself, so that its launch, these loads'
+// way and the joining over lanes and waves are what it takes.
 template <typename T, bool VEC, bool ADD>
 __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_stats(NormArgs a) {
   __shared__ SumsLds<NW> sh;
@@ -1097,7 +1106,7 @@ __device__ __forceinline__ void apply_rows(const NormArgs& a, const Lanes<VEC>& 
 // one is written (pass_rows); the first one ahead of the joining too gave 1 to 2 us at
 // 99,991 x 64 and took 4 at 285,564 x 128.  262,144 x 128 float32 to bfloat16 37 us
 // (201 MB, 5.5 TB/s, part of it from the cache), restored from a checkpoint 19 us
-// (103 MB, 5.4 TB/s); 99,991 x 64 bfloat16 in 37 segments 10.4 us (25.6 MB).
+// (103 MB, 5.4 TB/s); 99,991 x 64 bfloat16 in 37 segments 11 us (25.6 MB).
 template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_apply(NormArgs a) {
   __shared__ double sh[2 * NT];
@@ -1245,8 +1254,8 @@ __device__ __forceinline__ void weigh_tile(const Norm<VEC>& nm, const Tile<N, FU
 }
 
 // First pass: per piece the groups' sums, per workgroup the channels'.  285,564 x 128
-// from a checkpoint 34 us (185 MB, 5.4 TB/s); 8,192 x 64 bfloat16 5.3 us (3.1 MB,
-// latency).
+// from a checkpoint 34 us (185 MB, 5.4 TB/s); 262,144 x 128 from float32 values 47 us
+// (268 MB, 5.7 TB/s); 8,192 x 64 bfloat16 5.4 us (3.1 MB, latency).
 template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_sums(NormArgs a) {
   __shared__ SumsLds<NW> sh;
@@ -1345,7 +1354,8 @@ __device__ __forceinline__ void grad_rows(const NormArgs& a, const Lanes<VEC>& L
 
 // Second pass.  The last workgroups, past a.grid, form dbeta and dgamma (4 us as a launch
 // of their own).  285,564 x 128 from a checkpoint with grad_addend 77 us (477 MB,
-// 6.2 TB/s, part of it from the cache); 8,192 x 64 bfloat16 5.3 us (5.2 MB, latency).
+// 6.2 TB/s, part of it from the cache); 262,144 x 128 from float32 values 82 us (537 MB,
+// 6.5 TB/s); 8,192 x 64 bfloat16 5.4 us (5.2 MB, latency).
 // Pieces in the opposite order (last read, first used) made no difference.
 template <typename T, bool VEC, int ACT>
 __global__ __launch_bounds__(NT, VEC ? 4 : 2) void k_norm_bwd_dx(NormArgs a) {
@@ -1479,7 +1489,8 @@ struct RowGroups {
 
 // A row's statistics need only its own lanes: one pass, mean and then deviations from
 // it in registers.  No tiles: many small workgroups (16 to a CU) hide the loads.
-// 8,192 x 64 bfloat16 3.4 us (2.1 MB).
+// 8,192 x 64 bfloat16 3.6 us (2.1 MB); 262,144 x 128 float32 to bfloat16 41 us (218 MB,
+// 5.3 TB/s).
 template <typename T, bool VEC, bool ADD, int ACT>
 __global__ __launch_bounds__(RNT) void k_norm_rows(NormArgs a) {
   constexpr int U = UNIT<VEC>, N = CPL<VEC> / U;
@@ -1524,6 +1535,7 @@ __global__ __launch_bounds__(RNT) void k_norm_rows(NormArgs a) {
   });
 }
 
+// 262,144 x 128 to bfloat16 21 us (119 MB, 5.6 TB/s).
 template <bool VEC, int ACT>
 __global__ __launch_bounds__(RNT) void k_norm_rows_restore(NormArgs a) {
   const Lanes<VEC> L(a.lg, a.C, RNT);
