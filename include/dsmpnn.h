@@ -475,6 +475,108 @@ dsmp_status dsmp_group_norm_backward(dsmp_handle* h, const dsmp_norm_desc* desc,
                                      const float* grad_addend, int64_t ldga, float* grad_x, int64_t ldgx,
                                      float* dgamma, float* dbeta, int32_t flags, void* ws, size_t ws_bytes);
 
+/* ---------------------------------------- queries and keys, normed and rotated
+ * What a projection hands to attention: rows of heads side by side (element e of
+ * head a at a * head_dim + e), each head normed over its head_dim values (norm = 1)
+ * and its first `rot` values rotated in pairs by the node's coordinates, in one pass:
+ *     u = gamma x / sqrt(mean x^2 + eps)                     (norm = 0: u = x)
+ *     t_p = pos[row][axis(p)] * freq[p],  axis(p) = p * axes / (rot / 2)
+ *     y_a = amplitude (u_a cos t_p - u_b sin t_p),  y_b = amplitude (u_a sin t_p + u_b cos t_p)
+ * for the pairs p < rot / 2; DSMP_ROTATE_HALF: (a, b) = (p, p + rot / 2),
+ * DSMP_ROTATE_INTERLEAVED: (a, b) = (2 p, 2 p + 1).  The values from rot on are u.
+ * The angle is formed and brought into one turn in float64, so far positions keep
+ * their digits; norms and products are float32.
+ *
+ * Matrices: device [n, heads * head_dim] of dtype, rows ld elements apart
+ * (heads * head_dim <= ld <= 2^16), 16-byte aligned, as every one of their rows:
+ * columns of a wider matrix (one projection for all) may be given. */
+enum { DSMP_ROTATE_HALF = 0, DSMP_ROTATE_INTERLEAVED = 1 };
+
+typedef struct dsmp_rotate_desc {
+  int32_t heads;     /* of the queries, 1..256 */
+  int32_t kv_heads;  /* of the keys, 1..256 */
+  int32_t head_dim;  /* a multiple of 8, at most 128; others give UNSUPPORTED */
+  int32_t dtype;     /* of all matrices: DSMP_F32 or DSMP_BF16 */
+  int32_t rot;       /* rotated values of each head: 0, or a multiple of 2 * axes up to head_dim */
+  int32_t axes;      /* coordinates, 1..3 */
+  int32_t layout;    /* DSMP_ROTATE_* */
+  int32_t norm;      /* 0 or 1 */
+  float eps;         /* >= 0 */
+  float amplitude;   /* of the rotated values, finite */
+} dsmp_rotate_desc;
+
+/* q and k of the same n rows; either may be NULL with its output (one of them
+ * alone).  gamma_q, gamma_k: device float32 [head_dim], NULL for 1 (and with norm = 0).
+ * pos: device float32 [n, axes]; freq: device float32 [rot / 2]; neither is read
+ * when rot == 0.  An output may be its own input (with its row distance); otherwise
+ * outputs overlap nothing.  n == 0 enqueues nothing. */
+dsmp_status dsmp_qk_rotate_forward(dsmp_handle* h, const dsmp_rotate_desc* desc, int64_t n, const void* q, int64_t ldq,
+                                   const void* k, int64_t ldk, const float* gamma_q, const float* gamma_k,
+                                   const float* pos, const float* freq, void* q_out, int64_t ldqo, void* k_out,
+                                   int64_t ldko);
+
+/* Backward from the forward's inputs: grad_q, grad_k (of dtype, as the gradients
+ * that come in: operands of the projection's own gradients) receive the gradients
+ * with respect to q and k, and may be grad_q_out, grad_k_out themselves.  dgamma_q, dgamma_k: device float32 [head_dim]
+ * (NULL when the gamma is), summed over rows and heads, overwritten, or added to when
+ * flags has DSMP_GRAD_ACCUMULATE.  Coordinates and frequencies get no gradient. */
+dsmp_status dsmp_qk_rotate_workspace(const dsmp_rotate_desc* desc, int64_t n, size_t* bwd_ws_bytes);
+dsmp_status dsmp_qk_rotate_backward(dsmp_handle* h, const dsmp_rotate_desc* desc, int64_t n, const void* q, int64_t ldq,
+                                    const void* k, int64_t ldk, const float* gamma_q, const float* gamma_k,
+                                    const float* pos, const float* freq, const void* grad_q_out, int64_t ldgqo,
+                                    const void* grad_k_out, int64_t ldgko, void* grad_q, int64_t ldgq, void* grad_k,
+                                    int64_t ldgk, float* dgamma_q, float* dgamma_k, int32_t flags, void* ws,
+                                    size_t ws_bytes);
+
+/* -------------------------------------------- attention within packed segments
+ * Every query of a segment (sub-graph) attends to all keys of the same segment:
+ * for query i and key j of segment s, head a, key head b = a / (heads / kv_heads),
+ *     x = scale q_i.k_j,  c = cap tanh(x / cap)  (cap = 0: c = x)
+ *     z = c - slope_a |p_i - p_j|                (dim = 0: z = c)
+ *     P = softmax of z over the keys of s,  out_i = sum_j P v_j,  lse_i = log sum_j e^z
+ * A query whose segment has no keys gets out 0 and lse -infinity.  Scores, sums and
+ * the softmax are float32; with DSMP_BF16 the operands of the products are bfloat16
+ * (P and the scores' gradients are rounded to it), accumulated in float32.
+ *
+ * Matrices as above: q, out [nq, heads * head_dim], k, v [nk, kv_heads * head_dim].
+ * Coordinates: device float32 [rows, dim], slopes: device float32 [heads]; both
+ * constants (no gradient), NULL when dim == 0; the squares of the differences have to
+ * be finite in float32. */
+typedef struct dsmp_attention_desc {
+  int32_t heads;     /* 1..256 */
+  int32_t kv_heads;  /* divides heads */
+  int32_t head_dim;  /* a multiple of 8, at most 128; others give UNSUPPORTED */
+  int32_t dtype;     /* of all matrices: DSMP_F32 or DSMP_BF16 */
+  int32_t dim;       /* coordinates of the distance, 0..3; 0: none */
+  float scale;       /* finite */
+  float cap;         /* >= 0, finite; 0: none */
+} dsmp_attention_desc;
+
+/* Segments: queries and keys have the same number of segments.  The bounds of
+ * dsmp_segments ascend from any ptr[0] >= 0 to any ptr[n_seg] <= n here: rows that
+ * belong to no segment are neither read nor written (room behind the last
+ * sub-graph).  With wrong bounds results are undefined, but no access leaves the arrays.
+ * Workspace bytes of the forward and the backward call: */
+dsmp_status dsmp_attention_workspace(const dsmp_attention_desc* desc, const dsmp_segments* qs, const dsmp_segments* ks,
+                                     size_t* fwd_ws_bytes, size_t* bwd_ws_bytes);
+
+/* Forward.  lse: device float32 [nq, heads], or NULL (no backward call follows).
+ * Few queries over many keys are cut over the keys too, and joined in a fixed order. */
+dsmp_status dsmp_attention_forward(dsmp_handle* h, const dsmp_attention_desc* desc, const dsmp_segments* qs,
+                                   const dsmp_segments* ks, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                   const void* v, int64_t ldv, const float* pos_q, const float* pos_k,
+                                   const float* slopes, void* out, int64_t ldo, float* lse, void* ws, size_t ws_bytes);
+
+/* Backward of the forward call that left out and lse, with its arguments as they
+ * were: the gradients with respect to q, k and v of sum(grad_out * out), of dtype;
+ * those of shared key heads are summed over their queries' heads in float32. */
+dsmp_status dsmp_attention_backward(dsmp_handle* h, const dsmp_attention_desc* desc, const dsmp_segments* qs,
+                                    const dsmp_segments* ks, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                    const void* v, int64_t ldv, const float* pos_q, const float* pos_k,
+                                    const float* slopes, const void* out, int64_t ldo, const float* lse,
+                                    const void* grad_out, int64_t ldgo, void* grad_q, int64_t ldgq, void* grad_k,
+                                    int64_t ldgk, void* grad_v, int64_t ldgv, void* ws, size_t ws_bytes);
+
 /* How the layer evaluates the edge contraction.  DSMP_EDGE_PER_EDGE forms
  * each message m_e on MFMA (edge tiles against streamed W3 chunks) and sums
  * them per destination.  DSMP_EDGE_AGGREGATE uses the linearity of the mean:
@@ -525,7 +627,10 @@ enum {
   DSMP_K_DA1 = 23,      /* da1 from the stored da2 (aggregate form, bf16: d = 128, large d = 64) */
   DSMP_K_NORM = 24,     /* group norms, forward, restored and backward */
   DSMP_K_CKPT = 25,     /* checkpoints in 8 bits, stored and loaded */
-  DSMP_K_COUNT = 26
+  DSMP_K_ROTATE = 26,   /* queries and keys normed and rotated, forward and backward */
+  DSMP_K_ATTN_FWD = 27, /* attention forward */
+  DSMP_K_ATTN_BWD = 28, /* attention backward */
+  DSMP_K_COUNT = 29
 };
 dsmp_status dsmp_profile_enable(dsmp_handle* h, int enable);
 dsmp_status dsmp_profile_reset(dsmp_handle* h);

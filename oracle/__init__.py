@@ -26,10 +26,12 @@ Contents, each following the paper passage named in its module docstring:
                       procedure).
 * ``norm``         -- group norm with an activation over packed segments, its
                       gradients, and checkpoints in 8 bits.
+* ``attention``    -- queries and keys normed and rotated, attention within
+                      packed segments, and their gradients.
 
 Floating point: the layer runs in float64.  The radius test runs in float32
 in a fixed evaluation order (no fused multiply-add), because the paper fixes
 no precision and the GPU must reproduce the edge set bit for bit.
 """
 
-from . import rng, sampling, radius_graph, nnconv, hop, infer, norm  # noqa: F401
+from . import rng, sampling, radius_graph, nnconv, hop, infer, norm, attention  # noqa: F401

@@ -9,6 +9,7 @@ the import fails: there is no fallback.
 """
 
 import ctypes
+import math
 import operator
 import os
 from dataclasses import dataclass
@@ -26,6 +27,7 @@ CAP_KNN, CAP_RANDOM = 0, 1
 F32, BF16 = 0, 1
 ACT_IDENTITY, ACT_RELU, ACT_SILU, ACT_GELU = range(4)
 ATTR_CONCAT, ATTR_DIFF = 0, 1
+ROTATE_HALF, ROTATE_INTERLEAVED = 0, 1
 GRAD_ACCUMULATE = 1
 GRAD_X_ACCUMULATE = 2
 EDGE_AUTO, EDGE_PER_EDGE, EDGE_AGGREGATE = 0, 1, 2
@@ -41,12 +43,15 @@ EXPORTED = ["dsmp_version", "dsmp_create", "dsmp_destroy", "dsmp_set_stream", "d
             "dsmp_profile_read", "dsmp_set_edge_algorithm", "dsmp_mlp_workspace", "dsmp_mlp_forward",
             "dsmp_mlp_backward", "dsmp_masked_mse_workspace", "dsmp_masked_mse",
             "dsmp_checkpoint_store", "dsmp_checkpoint_load", "dsmp_group_norm_workspace", "dsmp_group_norm_forward",
-            "dsmp_group_norm_restore", "dsmp_group_norm_backward"]
+            "dsmp_group_norm_restore", "dsmp_group_norm_backward",
+            "dsmp_qk_rotate_forward", "dsmp_qk_rotate_workspace", "dsmp_qk_rotate_backward",
+            "dsmp_attention_workspace", "dsmp_attention_forward", "dsmp_attention_backward"]
 
 # kernel classes of the opt-in timing (dsmp_profile_*)
 KERNEL_CLASSES = ["sample", "gather", "graph", "edge_fwd", "node_fwd", "node_bwd", "edge_dh", "dh_final",
                   "dz", "dW3", "dW2", "dW1", "reduce", "edge_mlp", "outer_fwd", "gemm_fwd", "outer_dh",
-                  "gemm_dh", "u_gemm", "attr", "mlp", "loss", "dh_u", "da1", "norm", "ckpt"]
+                  "gemm_dh", "u_gemm", "attr", "mlp", "loss", "dh_u", "da1", "norm", "ckpt", "rotate",
+                  "attn_fwd", "attn_bwd"]
 
 
 class DsmpError(RuntimeError):
@@ -98,6 +103,16 @@ class NormDesc(ctypes.Structure):
                 ("y_dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
+class RotateDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("heads", "kv_heads", "head_dim", "dtype", "rot", "axes", "layout",
+                                              "norm")] + [("eps", ctypes.c_float), ("amplitude", ctypes.c_float)]
+
+
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("heads", "kv_heads", "head_dim", "dtype", "dim")] + [
+        ("scale", ctypes.c_float), ("cap", ctypes.c_float)]
+
+
 class CSegments(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int64), ("n_seg", ctypes.c_int64), ("ptr", ctypes.c_void_p)]
 
@@ -108,6 +123,9 @@ class CCheckpoint(ctypes.Structure):
 
 _P = ctypes.c_void_p
 _I64 = ctypes.c_int64
+_SIZE = ctypes.POINTER(ctypes.c_size_t)
+_ATTN = [_P, ctypes.POINTER(AttentionDesc), ctypes.POINTER(CSegments), ctypes.POINTER(CSegments)]
+_MAT = [_P, _I64]
 _SIG = {
     "dsmp_version": (ctypes.c_int, []),
     "dsmp_create": (ctypes.c_int, [ctypes.POINTER(ctypes.c_void_p), ctypes.c_int]),
@@ -167,6 +185,14 @@ _SIG = {
     "dsmp_group_norm_backward": (ctypes.c_int, [_P, ctypes.POINTER(NormDesc), ctypes.POINTER(CSegments), _P, _I64,
                                                 ctypes.POINTER(CCheckpoint), _P, _P, _P, _P, _I64, _P, _I64, _P, _I64,
                                                 _P, _P, ctypes.c_int32, _P, ctypes.c_size_t]),
+    "dsmp_qk_rotate_forward": (ctypes.c_int, [_P, ctypes.POINTER(RotateDesc), _I64] + 2 * _MAT + 4 * [_P] + 2 * _MAT),
+    "dsmp_qk_rotate_workspace": (ctypes.c_int, [ctypes.POINTER(RotateDesc), _I64, _SIZE]),
+    "dsmp_qk_rotate_backward": (ctypes.c_int, [_P, ctypes.POINTER(RotateDesc), _I64] + 2 * _MAT + 4 * [_P] + 4 * _MAT
+                                + [_P, _P, ctypes.c_int32, _P, ctypes.c_size_t]),
+    "dsmp_attention_workspace": (ctypes.c_int, _ATTN[1:] + [_SIZE, _SIZE]),
+    "dsmp_attention_forward": (ctypes.c_int, _ATTN + 3 * _MAT + 3 * [_P] + _MAT + [_P, _P, ctypes.c_size_t]),
+    "dsmp_attention_backward": (ctypes.c_int, _ATTN + 3 * _MAT + 3 * [_P] + _MAT + [_P] + 4 * _MAT
+                                + [_P, ctypes.c_size_t]),
     "dsmp_profile_enable": (ctypes.c_int, [_P, ctypes.c_int]),
     "dsmp_profile_reset": (ctypes.c_int, [_P]),
     "dsmp_profile_read": (ctypes.c_int, [_P, ctypes.c_int, ctypes.POINTER(ctypes.c_double),
@@ -244,6 +270,38 @@ def norm_desc(channels, groups, x_dtype, y_dtype, act=ACT_IDENTITY, eps=1e-5) ->
     return NormDesc(channels, groups, x_dtype, y_dtype, act, eps)
 
 
+def rotate_desc(heads, kv_heads, head_dim, dtype, rot, axes=1, layout=ROTATE_HALF, norm=True, eps=1e-6,
+                amplitude=1.0) -> RotateDesc:
+    return RotateDesc(heads, kv_heads, head_dim, dtype, rot, axes, layout, int(norm), eps, amplitude)
+
+
+def attention_desc(heads, kv_heads, head_dim, dtype, dim=0, scale=None, cap=0.0) -> AttentionDesc:
+    """scale: 1 / sqrt(head_dim) if not given."""
+    return AttentionDesc(heads, kv_heads, head_dim, dtype, dim, head_dim ** -0.5 if scale is None else scale, cap)
+
+
+def rotary_frequencies(rot, axes=1, base=10000.0, factor=1.0, extent=None, slow=1.0, fast=32.0, device=None):
+    """Frequencies (float32 [rot / 2], radians per unit of a coordinate) of
+    dsmp_qk_rotate_*: base^(-i / m) for the m = rot / 2 / axes pairs i of each axis.
+
+    factor > 1 scales them for coordinates that reach `factor` times further than those a
+    model was trained on: all by 1 / factor; or, with `extent` (the trained range), pairs
+    that turn fewer than `slow` times over it by 1 / factor, those that turn more than
+    `fast` times not at all, and those between by a linear mixture of both."""
+    if axes < 1 or rot < 0 or rot % (2 * axes):
+        raise DsmpError(INVALID_ARG, "rot must be a multiple of 2 axes")
+    if not (base > 0 and factor > 0 and (extent is None or (extent > 0 and fast > slow))):
+        raise DsmpError(INVALID_ARG, "base, factor and extent must be positive, and fast more than slow")
+    m = rot // 2 // axes
+    f = torch.pow(torch.tensor(float(base), dtype=torch.float64), -torch.arange(m, dtype=torch.float64) / max(m, 1))
+    if extent is None:
+        f = f / factor
+    else:
+        keep = ((f * extent / (2 * math.pi) - slow) / (fast - slow)).clamp(0, 1)
+        f = f * (keep + (1 - keep) / factor)
+    return f.repeat(axes).to(dtype=torch.float32, device=device)
+
+
 _TORCH = {F32: torch.float32, BF16: torch.bfloat16}
 _CODE = {torch.float32: F32, torch.bfloat16: BF16}
 
@@ -268,6 +326,7 @@ class Dsmp:
         self._ws = {}
         self._index = device
         self._norm_sizes = {}
+        self._attn_sizes = {}
 
     def close(self):
         if getattr(self, "h", None) is not None:
@@ -742,3 +801,145 @@ class Dsmp:
         if st:
             self._check(st, self.h)
         return grad_x, grads
+
+    # ------------------------------------------------------------ attention
+    def _scratch(self, key, size, ws):
+        """Binds the current stream; address and size of the scratch buffer, as for the norms."""
+        stream = self._bind_current()
+        if ws is not None:
+            return self._flat(ws, "ws", (ws.numel(),) if isinstance(ws, torch.Tensor) else (), torch.uint8), ws.numel()
+        if size == 0:
+            return None, 0
+        if _capturing():
+            ws = torch.empty(size, dtype=torch.uint8, device=self.device)
+        else:
+            ws = self.workspace((key, stream), size)
+        return ws.data_ptr(), ws.numel()
+
+    def _out(self, t, name, shape, dtype):
+        """(tensor, address, row distance) of an output, made if it is not given."""
+        if t is None:
+            t = torch.empty(shape, dtype=dtype, device=self.device)
+        return (t,) + self._rows(t, name, shape, dtype)
+
+    def _rotate_inputs(self, desc, q, k, gamma_q, gamma_k, pos, freq):
+        if q is None and k is None:
+            raise DsmpError(INVALID_ARG, "queries or keys are needed")
+        n, dt, hd = (k if q is None else q).shape[0], _TORCH.get(desc.dtype), desc.head_dim
+        qs, ks = (n, desc.heads * hd), (n, desc.kv_heads * hd)
+        qp = (None, 0) if q is None else self._rows(q, "q", qs, dt)
+        kp = (None, 0) if k is None else self._rows(k, "k", ks, dt)
+        rest = [None if gamma_q is None else self._flat(gamma_q, "gamma_q", (hd,)),
+                None if gamma_k is None else self._flat(gamma_k, "gamma_k", (hd,)),
+                None if not desc.rot else self._flat(pos, "pos", (n, desc.axes)),
+                None if not desc.rot else self._flat(freq, "freq", (desc.rot // 2,))]
+        return n, dt, qs, ks, [*qp, *kp, *rest]
+
+    def dsmp_qk_rotate_forward(self, desc: RotateDesc, q, k, gamma_q=None, gamma_k=None, pos=None, freq=None,
+                               q_out=None, k_out=None):
+        """Queries [n, heads * head_dim] and keys [n, kv_heads * head_dim], each head normed and its pairs
+        rotated by pos (float32 [n, axes]) times freq (float32 [rot / 2], see rotary_frequencies); returns
+        (q_out, k_out).  q or k may be None; an output may be its own input."""
+        n, dt, qs, ks, args = self._rotate_inputs(desc, q, k, gamma_q, gamma_k, pos, freq)
+        q_out, qo, ldqo = (None, None, 0) if q is None else self._out(q_out, "q_out", qs, dt)
+        k_out, ko, ldko = (None, None, 0) if k is None else self._out(k_out, "k_out", ks, dt)
+        self._bind_current()
+        st = self.lib.dsmp_qk_rotate_forward(self.h, desc, n, *args, qo, ldqo, ko, ldko)
+        if st:
+            self._check(st, self.h)
+        return q_out, k_out
+
+    def dsmp_qk_rotate_workspace(self, desc: RotateDesc, n: int) -> int:
+        """Bytes of scratch that dsmp_qk_rotate_backward needs (its ws)."""
+        nb = ctypes.c_size_t()
+        self._check(self.lib.dsmp_qk_rotate_workspace(desc, n, ctypes.byref(nb)), None)
+        return nb.value
+
+    def dsmp_qk_rotate_backward(self, desc: RotateDesc, q, k, gamma_q, gamma_k, pos, freq, grad_q_out, grad_k_out,
+                                grad_q=None, grad_k=None, grads: Optional[dict] = None, flags: int = 0, ws=None):
+        """Gradients of the forward call with these inputs; returns (grad_q, grad_k, {"dgamma_q", "dgamma_k"}
+        for the gammas given).  grad_q and grad_k may be the gradients that come in.  ws: scratch of the
+        caller's own (uint8), needed in a capture that torch.cuda.graph does not make."""
+        n, dt, qs, ks, args = self._rotate_inputs(desc, q, k, gamma_q, gamma_k, pos, freq)
+        gqo = (None, 0) if q is None else self._rows(grad_q_out, "grad_q_out", qs, dt)
+        gko = (None, 0) if k is None else self._rows(grad_k_out, "grad_k_out", ks, dt)
+        grad_q, gq, ldgq = (None, None, 0) if q is None else self._out(grad_q, "grad_q", qs, dt)
+        grad_k, gk, ldgk = (None, None, 0) if k is None else self._out(grad_k, "grad_k", ks, dt)
+        out, dg = {}, []
+        for name, gamma in (("dgamma_q", gamma_q), ("dgamma_k", gamma_k)):
+            if gamma is None:
+                dg.append(None)
+                continue
+            out[name] = torch.empty_like(gamma) if grads is None else grads[name]
+            dg.append(self._flat(out[name], name, (desc.head_dim,)))
+        size = self.dsmp_qk_rotate_workspace(desc, n) if out else 0
+        wp, wb = self._scratch("rotate", size, ws)
+        st = self.lib.dsmp_qk_rotate_backward(self.h, desc, n, *args, *gqo, *gko, gq, ldgq, gk, ldgk, *dg, flags, wp, wb)
+        if st:
+            self._check(st, self.h)
+        return grad_q, grad_k, out
+
+    def _attn_size(self, desc, qs, ks):
+        key = (desc.heads, desc.kv_heads, desc.head_dim, qs.n, qs.n_seg, ks.n, ks.n_seg)
+        sizes = self._attn_sizes.get(key)
+        if sizes is None:
+            f, b = ctypes.c_size_t(), ctypes.c_size_t()
+            self._check(self.lib.dsmp_attention_workspace(desc, qs, ks, ctypes.byref(f), ctypes.byref(b)), None)
+            if len(self._attn_sizes) >= 1024:
+                self._attn_sizes.clear()
+            sizes = self._attn_sizes[key] = (f.value, b.value)
+        return sizes
+
+    def _attn_inputs(self, desc, q, k, v, segments, k_segments, pos, k_pos, slopes):
+        nq, nk, dt, hd = q.shape[0], k.shape[0], _TORCH.get(desc.dtype), desc.head_dim
+        qshape, kshape = (nq, desc.heads * hd), (nk, desc.kv_heads * hd)
+        args = [*self._rows(q, "q", qshape, dt), *self._rows(k, "k", kshape, dt), *self._rows(v, "v", kshape, dt)]
+        if desc.dim > 0:
+            k_pos = pos if k_pos is None else k_pos
+            args += [self._flat(pos, "pos", (nq, desc.dim)), self._flat(k_pos, "k_pos", (nk, desc.dim)),
+                     self._flat(slopes, "slopes", (desc.heads,))]
+        else:
+            args += [None, None, None]
+        qs = self._segments(nq, segments)
+        return nq, dt, qshape, kshape, qs, self._segments(nk, segments if k_segments is None else k_segments), args
+
+    def dsmp_attention_workspace(self, desc: AttentionDesc, n: int, n_keys: int, segments=None, k_segments=None):
+        """Bytes of scratch that dsmp_attention_forward and _backward need (their ws): (forward, backward)."""
+        return self._attn_size(desc, self._segments(n, segments),
+                               self._segments(n_keys, segments if k_segments is None else k_segments))
+
+    def dsmp_attention_forward(self, desc: AttentionDesc, q, k, v, segments=None, k_segments=None, pos=None, k_pos=None,
+                               slopes=None, out=None, lse=None, ws=None):
+        """Attention of the queries q [n, heads * head_dim] to the keys and values k, v [n_keys, kv_heads *
+        head_dim] of their own segment; returns (out, lse).
+
+        segments, k_segments: of the queries and of the keys, as for the norms (k_segments None: the
+        queries'), with rows in front of the first and behind the last bound left alone.  pos, k_pos: float32
+        [n, dim], [n_keys, dim] (k_pos None: pos), slopes float32 [heads], where the descriptor's dim is not
+        0.  ws: scratch of the caller's own (uint8, dsmp_attention_workspace), needed in a capture that
+        torch.cuda.graph does not make."""
+        nq, dt, qshape, _, qs, ks, args = self._attn_inputs(desc, q, k, v, segments, k_segments, pos, k_pos, slopes)
+        out, op, ldo = self._out(out, "out", qshape, dt)
+        lse = torch.empty(nq, desc.heads, dtype=torch.float32, device=self.device) if lse is None else lse
+        lp = self._flat(lse, "lse", (nq, desc.heads))
+        wp, wb = self._scratch("attention", self._attn_size(desc, qs, ks)[0], ws)
+        st = self.lib.dsmp_attention_forward(self.h, desc, qs, ks, *args, op, ldo, lp, wp, wb)
+        if st:
+            self._check(st, self.h)
+        return out, lse
+
+    def dsmp_attention_backward(self, desc: AttentionDesc, q, k, v, out, lse, grad_out, segments=None, k_segments=None,
+                                pos=None, k_pos=None, slopes=None, grad_q=None, grad_k=None, grad_v=None, ws=None):
+        """Gradients with respect to q, k and v of the forward call that returned out and lse; returns
+        (grad_q, grad_k, grad_v), of the matrices' own type."""
+        nq, dt, qshape, kshape, qs, ks, args = self._attn_inputs(desc, q, k, v, segments, k_segments, pos, k_pos, slopes)
+        args += [*self._rows(out, "out", qshape, dt), self._flat(lse, "lse", (nq, desc.heads)),
+                 *self._rows(grad_out, "grad_out", qshape, dt)]
+        grad_q, gq, ldgq = self._out(grad_q, "grad_q", qshape, dt)
+        grad_k, gk, ldgk = self._out(grad_k, "grad_k", kshape, dt)
+        grad_v, gv, ldgv = self._out(grad_v, "grad_v", kshape, dt)
+        wp, wb = self._scratch("attention", self._attn_size(desc, qs, ks)[1], ws)
+        st = self.lib.dsmp_attention_backward(self.h, desc, qs, ks, *args, gq, ldgq, gk, ldgk, gv, ldgv, wp, wb)
+        if st:
+            self._check(st, self.h)
+        return grad_q, grad_k, grad_v

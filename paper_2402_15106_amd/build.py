@@ -23,7 +23,7 @@ LIB = os.path.join(OUT_DIR, "libdsmpnn.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 
 SOURCES = ["core.hip", "graph.hip", "nnconv_fwd.hip", "nnconv_bwd.hip", "nnconv_agg.hip", "hop.hip",
-           "norm.hip"]
+           "norm.hip", "rotate.hip", "attn_fwd.hip", "attn_dq.hip", "attn_dkv.hip"]
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 PER_FILE = {"graph.hip": ["-ffp-contract=off"]}
@@ -68,7 +68,7 @@ def build(verbose: bool = False) -> str:
             sys.stderr.write("".join(l + "\n" for l in r.stderr.splitlines() if "remark" not in l))
         return obj
 
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
         objs = list(ex.map(compile_one, SOURCES))
     tmp = LIB + ".tmp"
     cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs

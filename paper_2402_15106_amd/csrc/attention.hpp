@@ -1,0 +1,319 @@
+// What the attention kernels and the rotation of their operands share: argument
+// checks, product fragments, the mapping of workgroups to packed segments, and the
+// score of a query and a key.
+#pragma once
+
+#include "nnconv.hpp"
+
+#include <cmath>
+#include <initializer_list>
+#include <type_traits>
+
+namespace dsmp {
+
+constexpr int MAX_HEADS = 256, MAX_HEAD_DIM = 128;
+constexpr int64_t MAX_ROW = (int64_t)1 << 16;   // elements between rows: a tile's rows lie within 32 bits
+
+// Makes the handle's device current for a call's launches.
+struct DeviceScope {
+  int before = -1;
+  explicit DeviceScope(const dsmp_handle* h) {
+    int now = -1;
+    if (hipGetDevice(&now) == hipSuccess && now != h->device && hipSetDevice(h->device) == hipSuccess) before = now;
+  }
+  ~DeviceScope() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+struct Matrix {
+  const void* p;   // NULL: not there
+  int64_t ld, width;
+  const char* name;
+};
+
+inline dsmp_status check_matrices(dsmp_handle* h, int size, std::initializer_list<Matrix> all) {
+  for (const Matrix& m : all) {
+    if (!m.p) continue;
+    DSMP_CHECK(h, m.ld >= m.width, DSMP_INVALID_ARG, "%s: rows are closer than their values", m.name);
+    DSMP_CHECK(h, m.ld <= MAX_ROW, DSMP_UNSUPPORTED, "%s: rows more than %lld elements apart", m.name, (long long)MAX_ROW);
+    DSMP_CHECK(h, reinterpret_cast<uintptr_t>(m.p) % 16 == 0 && m.ld * size % 16 == 0, DSMP_INVALID_ARG,
+               "%s: rows must be 16-byte aligned", m.name);
+  }
+  return DSMP_OK;
+}
+
+// ------------------------------------------------------------------ fragments
+// Eight values of a lane: A[row = l % 32][8 h + e], B[8 h + e][col = l % 32] with h = l / 32,
+// 16 deep; the result as in nnconv.hpp.  In float32 eight products 2 deep take element e of
+// both halves each, so both types have the same layout.
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+template <typename T>
+struct Frag;
+template <>
+struct Frag<__bf16> {
+  typedef bf16x8 type;
+};
+template <>
+struct Frag<float> {
+  typedef f32x8 type;
+};
+
+__device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+  return c;
+}
+
+// Eight float32 values rounded to the type of the products (to nearest even).
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type to_frag(const float* v);
+template <>
+__device__ __forceinline__ bf16x8 to_frag<__bf16>(const float* v) { return pack_frag<__bf16>(v); }
+template <>
+__device__ __forceinline__ f32x8 to_frag<float>(const float* v) {
+  f32x8 f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = v[e];
+  return f;
+}
+
+typedef __attribute__((address_space(3))) unsigned char lds_u8;
+
+// A operand from row-major LDS: row r0 + l % 32, values c0 + 8 h + e.
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type lds_rows(lds_u8* X, int pitch, int r0, int c0) {
+  const int l = threadIdx.x & 63;
+  lds_u8* p = X + (r0 + (l & 31)) * pitch + (c0 + 8 * (l >> 5)) * (int)sizeof(T);
+  if (sizeof(T) == 4) {
+    uint32_t at = (uint32_t)(uintptr_t)p;
+    asm volatile("" : "+v"(at));   // formed here: not kept over a loop for each of many calls
+    p = (lds_u8*)(uintptr_t)at;
+  }
+  return *(__attribute__((address_space(3))) typename Frag<T>::type*)p;
+}
+
+// A operand from row-major LDS, transposed: A row = column c0 + l % 32, contraction index
+// (h, e) = LDS row r0 + 8 (e / 4) + 4 h + e % 4 -- the order in which a lane's eight
+// consecutive result registers hold the rows of a 32-row result, which so become the B
+// operand as they are.
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type lds_columns(lds_u8* X, int pitch, int r0, int c0);
+template <>
+__device__ __forceinline__ bf16x8 lds_columns<__bf16>(lds_u8* X, int pitch, int r0, int c0) {
+  const int l = threadIdx.x & 63, g = l >> 4, j = (l >> 2) & 3, q = l & 3;
+  lds_u8* p = X + (r0 + 4 * (g >> 1) + j) * pitch + (c0 + 16 * (g & 1) + 4 * q) * 2;
+  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * pitch));
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+template <>
+__device__ __forceinline__ f32x8 lds_columns<float>(lds_u8* X, int pitch, int r0, int c0) {
+  const int l = threadIdx.x & 63;
+  uint32_t at = (uint32_t)(uintptr_t)(X + (r0 + 4 * (l >> 5)) * pitch + (c0 + (l & 31)) * 4);
+  asm volatile("" : "+v"(at));   // as above
+  lds_u8* p = (lds_u8*)(uintptr_t)at;
+  f32x8 f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    f[e] = *(__attribute__((address_space(3))) float*)(p + (8 * (e / 4) + e % 4) * pitch);
+  return f;
+}
+
+// Row of register i of a 32-row result.
+__device__ __forceinline__ int result_row(int i) { return 8 * (i >> 2) + 4 * ((threadIdx.x & 63) >> 5) + (i & 3); }
+
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+
+// LDS pitch of a tile with D values to a row: rows read 16 bytes at a time (ROWS), or in
+// transposing reads.
+template <typename T, int D, bool ROWS>
+constexpr int pitch_of() {
+  return D * (int)sizeof(T) + (ROWS || sizeof(T) == 4 ? 16 : 16 * tr_pad_units(D * (int)sizeof(T)));
+}
+
+// ------------------------------------------------------------- guarded global reads
+// Buffer reads of 16 bytes: what begins at or behind `bytes` comes back as zero.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+constexpr uint32_t NOWHERE = 0x80000000u;   // an offset behind every tile
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* base, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00020000);
+}
+__device__ __forceinline__ u32x4 buffer_read(__amdgpu_buffer_rsrc_t r, uint32_t offset) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)offset, 0, 0));
+}
+
+// A lane's eight values at p (16-byte aligned), or zeros.
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type read_frag(const T* p, bool there) {
+  typename Frag<T>::type f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = (T)0.0f;
+  if (there) f = *(const typename Frag<T>::type*)p;
+  return f;
+}
+
+// Four values of a row of results, rounded.
+template <typename T>
+__device__ __forceinline__ void store4(T* p, float a, float b, float c, float d) {
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  t4 v;
+  v[0] = (T)a, v[1] = (T)b, v[2] = (T)c, v[3] = (T)d;
+  *(t4*)p = v;
+}
+
+// ------------------------------------------------------------------ segments
+struct Bounds {
+  const int32_t* ptr;   // NULL: equal segments of `len` rows
+  int64_t n, len;
+  __device__ __forceinline__ int64_t at(int s) const {
+    if (!ptr) return s * len;
+    const int64_t v = ptr[s];
+    return v < 0 ? 0 : v > n ? n : v;
+  }
+};
+
+// The segment of tile t, and that segment's first tile.  A segment whose bounds are b
+// and e has the tiles from floor(b M / size) + s on, ceil((e - b) M / size) of them, which ends
+// at or ahead of the next one's: nothing has to be counted up.  M rows of work stand
+// behind each row; sixty-four bounds are looked at at once.
+__device__ __forceinline__ int find_segment(const Bounds& b, int n_seg, int M, int size, int64_t t, int64_t* first) {
+  const int l = threadIdx.x & 63;
+  int lo = 0, count = n_seg;   // the segment is in [lo, lo + count)
+  while (count > 1) {
+    const int step = (count + 63) / 64, s = lo + l * step;
+    const bool le = l * step < count && b.at(s) * M / size + s <= t;
+    const int hit = (int)__popcll(__ballot(le));
+    lo += (hit > 0 ? hit - 1 : 0) * step;
+    count = min(step, n_seg - lo);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  *first = b.at(lo) * M / size + lo;
+  return lo;
+}
+
+inline int64_t tiles_of(int64_t n, int64_t n_seg, int M, int size) { return n * M / size + n_seg; }
+
+// ------------------------------------------------------------------ arguments
+struct AttnArgs {
+  const void *q, *k, *v, *go, *o;
+  int64_t ldq, ldk, ldv, ldgo, ldo;
+  void *out, *gq, *gk, *gv;
+  int64_t ldout, ldgq, ldgk, ldgv;
+  const float *pos_q, *pos_k, *slopes;
+  const float* lse_in;
+  float *lse, *delta, *part;
+  Bounds qb, kb;
+  int n_seg, H, Hk, G, hd, dim, splits;
+  uint32_t g_inv;        // ceil(2^20 / G): x / G = x g_inv >> 20 for x < 512
+  float scale, cap;      // of the scores as they are
+  int64_t nq;
+};
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// How a kernel scores: bfloat16 kernels have the cap and the coordinates compiled in,
+// float32 ones (CAP < 0), whose products take sixteen times as long, look at the arguments.
+template <int CAP_, int DIM_>
+struct Mode {
+  static constexpr int CAP = CAP_, DIM = DIM_;
+  static __device__ __forceinline__ bool cap(const AttnArgs& a) { return CAP < 0 ? a.cap > 0.0f : CAP > 0; }
+  static __device__ __forceinline__ int dim(const AttnArgs& a) { return CAP < 0 ? a.dim : DIM; }
+};
+
+struct Place {
+  float x, y, z;
+};
+
+// Coordinates of a row (those that there are).
+__device__ __forceinline__ Place place_of(const float* pos, int dim, int64_t row) {
+  Place p{0.0f, 0.0f, 0.0f};
+  const float* at = pos + row * dim;
+  p.x = at[0];
+  if (dim > 1) p.y = at[1];
+  if (dim > 2) p.z = at[2];
+  return p;
+}
+
+__device__ __forceinline__ float distance(int dim, const Place& a, float x, float y, float z) {
+  const float dx = a.x - x, dy = a.y - y;
+  float d = fmaf(dy, dy, dx * dx);
+  if (dim > 2) {
+    const float dz = a.z - z;
+    d = fmaf(dz, dz, d);
+  }
+  return __builtin_amdgcn_sqrtf(d);
+}
+
+// Constants of the score in powers of two.
+struct ScoreConst {
+  float scale2;   // scale log2(e)
+  float turn;     // 2 log2(e) scale / cap
+  float cap2;     // cap log2(e)
+};
+__device__ __forceinline__ ScoreConst score_const(const AttnArgs& a) {
+  return {a.scale * LOG2E, a.cap > 0.0f ? 2.0f * LOG2E * a.scale / a.cap : 0.0f, a.cap * LOG2E};
+}
+
+// log2(e) times the score without its bias; `fall` receives 1 - tanh^2.
+// tanh x = 1 - 2 r with r = 1 / (1 + e^2x); 1 - tanh^2 x = 4 r (1 - r).  The difference from 1 leaves an
+// absolute error of about 2^-23 in tanh; float32 scores take tanhf.
+template <typename T, bool SLOPE>
+__device__ __forceinline__ float capped(float s, bool cap, const ScoreConst& c, float* fall) {
+  if (!cap) {
+    if (SLOPE) *fall = 1.0f;
+    return s * c.scale2;
+  }
+  if (sizeof(T) == 4) {
+    const float t = tanhf(s * c.turn * (0.5f * LN2));
+    if (SLOPE) *fall = 1.0f - t * t;
+    return c.cap2 * t;
+  }
+  const float r = __builtin_amdgcn_rcpf(1.0f + exp2_of(s * c.turn));
+  if (SLOPE) *fall = 4.0f * r * (1.0f - r);
+  return fmaf(-2.0f * c.cap2, r, c.cap2);
+}
+
+inline AttnArgs attn_args(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks) {
+  AttnArgs a{};
+  a.qb = {qs.ptr, qs.n, qs.ptr ? 0 : qs.n / qs.n_seg};
+  a.kb = {ks.ptr, ks.n, ks.ptr ? 0 : ks.n / ks.n_seg};
+  a.n_seg = (int)qs.n_seg;
+  a.H = d.heads, a.Hk = d.kv_heads, a.G = d.heads / d.kv_heads, a.hd = d.head_dim, a.dim = d.dim;
+  a.g_inv = ((1u << 20) + a.G - 1) / a.G;
+  a.scale = d.scale, a.cap = d.cap;
+  a.nq = qs.n;
+  a.splits = 1;
+  return a;
+}
+
+// Calls f with the element type, the padded head width and the mode of a call.
+template <typename F>
+void by_attention(const dsmp_attention_desc& d, F f) {
+  auto width = [&](auto t, auto mode) {
+    if (d.head_dim <= 32) f(t, std::integral_constant<int, 32>{}, mode);
+    else if (d.head_dim <= 64) f(t, std::integral_constant<int, 64>{}, mode);
+    else f(t, std::integral_constant<int, 128>{}, mode);
+  };
+  if (d.dtype == DSMP_F32) width(float{}, Mode<-1, 3>{});
+  else if (d.dim == 0 && d.cap == 0.0f) width(__bf16{}, Mode<0, 0>{});
+  else if (d.dim == 0) width(__bf16{}, Mode<1, 0>{});
+  else if (d.cap != 0.0f) width(__bf16{}, Mode<1, 3>{});
+  else if (d.dim <= 2) width(__bf16{}, Mode<0, 2>{});
+  else width(__bf16{}, Mode<0, 3>{});
+}
+
+// Workgroups of 256 threads that fill the card (256 CUs) twice; a launch has fewer than 2^32 threads.
+constexpr int64_t FILL = 512, MAX_GROUPS = ((int64_t)1 << 24) - 1;
+
+dsmp_status check_attention(dsmp_handle* h, const dsmp_attention_desc* d, const dsmp_segments* qs, const dsmp_segments* ks);
+dsmp_status launch_attention_dq(dsmp_handle* h, const dsmp_attention_desc& d, AttnArgs a);
+dsmp_status launch_attention_dkv(dsmp_handle* h, const dsmp_attention_desc& d, AttnArgs a, int64_t nk);
+
+}  // namespace dsmp

@@ -1,0 +1,428 @@
+// Attention within packed segments, forward, and the argument checks of both passes.
+//
+//   z_ij = c(scale q_i.k_j) - slope |p_i - p_j|,  out_i = sum_j e^(z_ij - m_i) v_j / l_i
+//   m_i = max_j z_ij, l_i = sum_j e^(z_ij - m_i), lse_i = m_i + log l_i
+//
+// One pass over the keys with the running maximum m and sum l of each row.  The rows
+// of a key head are its segment's queries times the G query heads that share it (row
+// = query G + head), so one query with eight heads fills eight rows and reads the keys once.
+#include "attention.hpp"
+
+using namespace dsmp;
+
+namespace {
+
+constexpr int NT = 256, NW = 4;   // threads and waves of a workgroup
+
+// WIDE: 32 rows to a wave, 128 to a workgroup, every wave takes every key of a tile.
+// FEW: all waves have the same 32 rows and a quarter of a tile's keys each; they are joined at the end.
+template <typename T, int D, bool FEW>
+struct Fwd {
+  static constexpr int ROWS = FEW ? 32 : 32 * NW;
+  static constexpr int BN = FEW ? 32 * NW : sizeof(T) == 2 ? 64 : 32;
+  static constexpr int SUB = FEW ? 1 : BN / 32;   // blocks of 32 keys that a wave takes of a tile
+  static constexpr int PK = pitch_of<T, D, true>(), PV = pitch_of<T, D, false>();
+  static constexpr int PER = BN * D * (int)sizeof(T) / 16 / NT, STEP = NT * 16 / (D * (int)sizeof(T));
+  // the next tile waits in registers, but for FEW's large ones in float32: those come four units at a time
+  static constexpr bool AHEAD = !(FEW && sizeof(T) == 4);
+  static constexpr int HELD = AHEAD || PER < 4 ? PER : 4;
+  static constexpr int TILE = BN * (PK + PV) + 3 * BN * 4;
+  static constexpr int JOIN = FEW ? NW * 32 * (D + 2) * 4 : 0;
+  static constexpr int LDS = TILE > JOIN ? TILE : JOIN;
+  static_assert(PER >= 1 && PER * NT * 16 == BN * D * (int)sizeof(T), "whole units for every thread");
+};
+
+template <typename T, int D, bool FEW, typename M>
+__global__ __launch_bounds__(NT, D == 128 && (FEW || sizeof(T) == 4 || M::DIM > 2) ? 1 : 2) void k_attn_fwd(AttnArgs a) {
+  using C = Fwd<T, D, FEW>;
+  constexpr int ES = sizeof(T), KS = D / 16, DB = D / 32;
+  typedef typename Frag<T>::type frag;
+  __shared__ __align__(16) unsigned char smem[C::LDS];
+  lds_u8* ldsK = (lds_u8*)smem;
+  lds_u8* ldsV = ldsK + C::BN * C::PK;
+  float* places = (float*)(smem + C::BN * (C::PK + C::PV));   // x, y, z of the tile's keys
+
+  const int tid = (int)threadIdx.x, l = tid & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kvh = (int)(blockIdx.x % (unsigned)a.Hk);
+  const unsigned rest = blockIdx.x / (unsigned)a.Hk;
+  const int split = (int)(rest % (unsigned)a.splits);
+  const int64_t tile = rest / (unsigned)a.splits;
+  int64_t first;
+  const int seg = find_segment(a.qb, a.n_seg, a.G, C::ROWS, tile, &first);
+  const int64_t q0 = a.qb.at(seg), R = (a.qb.at(seg + 1) - q0) * a.G, r0 = (tile - first) * C::ROWS;
+  if (tile < first || r0 >= R) return;
+  const int64_t k0 = a.kb.at(seg), klen = a.kb.at(seg + 1) - k0;
+  const int tiles = klen > 0 ? (int)((klen + C::BN - 1) / C::BN) : 0;
+  const int per = (tiles + a.splits - 1) / a.splits;
+  const int t_begin = min(split * per, tiles), t_end = min(t_begin + per, tiles);
+
+  // this lane's row
+  const bool cap = M::cap(a);
+  const int dim = M::dim(a);
+  const ScoreConst sc = score_const(a);
+  const int64_t r = r0 + (FEW ? 0 : 32 * w) + (l & 31);
+  const bool there = r < R;
+  const unsigned rq = there ? (unsigned)r / (unsigned)a.G : 0u, rg = there ? (unsigned)r - rq * a.G : 0u;
+  const int64_t query = q0 + rq;
+  const int head = kvh * a.G + (int)rg;
+  frag qf[KS];
+#pragma unroll
+  for (int t = 0; t < KS; ++t)
+    qf[t] = read_frag<T>((const T*)a.q + query * a.ldq + head * a.hd + 16 * t + 8 * h, there && 16 * t + 8 * h < a.hd);
+  Place me{0.0f, 0.0f, 0.0f};
+  float slope2 = 0.0f;
+  if (dim && a.dim && there) me = place_of(a.pos_q, a.dim, query), slope2 = a.slopes[head] * LOG2E;
+
+  // a thread's 16-byte units of a tile: one place in every STEP-th row
+  const int row0 = tid / (D * ES / 16), c0 = tid % (D * ES / 16) * 16;
+  const bool in = c0 < a.hd * ES;
+  const uint32_t offK = in ? (uint32_t)(row0 * a.ldk * ES + c0) : NOWHERE, stepK = (uint32_t)(C::STEP * a.ldk * ES);
+  const uint32_t offV = in ? (uint32_t)(row0 * a.ldv * ES + c0) : NOWHERE, stepV = (uint32_t)(C::STEP * a.ldv * ES);
+  u32x4 regK[C::HELD], regV[C::HELD];
+  Place key{0.0f, 0.0f, 0.0f};
+  auto fetch = [&](int t, int i0) {
+    const int64_t j0 = k0 + (int64_t)t * C::BN;
+    const int rem = (int)min((int64_t)C::BN, klen - (int64_t)t * C::BN);
+    const auto bk = buffer_of((const T*)a.k + j0 * a.ldk + kvh * a.hd, (uint32_t)(rem * a.ldk * ES));
+    const auto bv = buffer_of((const T*)a.v + j0 * a.ldv + kvh * a.hd, (uint32_t)(rem * a.ldv * ES));
+#pragma unroll
+    for (int i = 0; i < C::HELD; ++i)
+      regK[i] = buffer_read(bk, offK + (i0 + i) * stepK), regV[i] = buffer_read(bv, offV + (i0 + i) * stepV);
+    if (dim && a.dim && i0 == 0 && tid < rem) key = place_of(a.pos_k, a.dim, j0 + tid);
+  };
+  auto put = [&](int i0) {
+#pragma unroll
+    for (int i = 0; i < C::HELD; ++i) {
+      const int row = row0 + (i0 + i) * C::STEP;
+      *(__attribute__((address_space(3))) u32x4*)(ldsK + row * C::PK + c0) = regK[i];
+      *(__attribute__((address_space(3))) u32x4*)(ldsV + row * C::PV + c0) = regV[i];
+    }
+    if (dim && i0 == 0 && tid < C::BN) places[tid] = key.x, places[C::BN + tid] = key.y, places[2 * C::BN + tid] = key.z;
+  };
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+  float m = -INFINITY, sum = 0.0f;   // of this lane's row; the sum over this half's keys
+
+  if (C::AHEAD && t_begin < t_end) fetch(t_begin, 0);
+  for (int t = t_begin; t < t_end; ++t) {
+    __syncthreads();
+    if (C::AHEAD) {
+      put(0);
+    } else {
+#pragma unroll 1
+      for (int i0 = 0; i0 < C::PER; i0 += C::HELD) fetch(t, i0), put(i0);
+    }
+    __syncthreads();
+    if (C::AHEAD && t + 1 < t_end) fetch(t + 1, 0);
+    const int rem = (int)min((int64_t)C::BN, klen - (int64_t)t * C::BN);
+    const int sub0 = FEW ? w : 0;
+    if (FEW && 32 * w >= rem) continue;
+    float s[C::SUB][16], top = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < C::SUB; ++b) {
+      const int at = 32 * (sub0 + b);
+      f32x16 x;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+#pragma unroll
+      for (int t2 = 0; t2 < KS; ++t2) x = mma(lds_rows<T>(ldsK, C::PK, at, 16 * t2), qf[t2], x);
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        float4 px{}, py{}, pz{};
+        if (dim) {
+          const float* p = places + at + 8 * i4 + 4 * h;
+          px = *(const float4*)p, py = *(const float4*)(p + C::BN);
+          if (dim > 2) pz = *(const float4*)(p + 2 * C::BN);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float z = capped<T, false>(x[4 * i4 + e], cap, sc, nullptr);
+          if (dim) z = fmaf(-slope2, distance(dim, me, (&px.x)[e], (&py.x)[e], (&pz.x)[e]), z);
+          s[b][4 * i4 + e] = z;
+        }
+      }
+      if (at + 32 > rem) {   // behind the last key
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (at + result_row(i) >= rem) s[b][i] = -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+    }
+    top = fmaxf(top, other_half(top));
+    const float now = fmaxf(m, top), base = now == -INFINITY ? 0.0f : now, shrink = exp2_of(m - base);
+    m = now;
+    float add = 0.0f;
+#pragma unroll
+    for (int b = 0; b < C::SUB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[b][i] = exp2_of(s[b][i] - base), add += s[b][i];
+    sum = fmaf(sum, shrink, add);
+    if (__any(shrink != 1.0f)) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= shrink;
+    }
+#pragma unroll
+    for (int b = 0; b < C::SUB; ++b)
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2) {
+        const frag p = to_frag<T>(&s[b][8 * t2]);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] = mma(lds_columns<T>(ldsV, C::PV, 32 * (sub0 + b) + 16 * t2, 32 * d), p, o[d]);
+      }
+  }
+  sum += other_half(sum);
+
+  const int64_t slot = query * a.H + head;   // this row's among all queries and heads
+  if (!FEW) {
+    if (!there) return;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    if (a.lse && h == 0) a.lse[slot] = (m + __log2f(sum)) * LN2;
+    T* out = (T*)a.out + query * a.ldout + head * a.hd;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const int c = 32 * d + 8 * i4 + 4 * h;
+        if (c < a.hd)
+          store4(out + c, o[d][4 * i4] * inv, o[d][4 * i4 + 1] * inv, o[d][4 * i4 + 2] * inv, o[d][4 * i4 + 3] * inv);
+      }
+    return;
+  }
+  // the waves' parts, [wave][value][row], joined by 256 threads: a row and four values in 32 each
+  float *jo = (float*)smem, *jm = jo + NW * D * 32, *js = jm + NW * 32;
+  __syncthreads();
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) jo[(w * D + 32 * d + result_row(i)) * 32 + (l & 31)] = o[d][i];
+  if (h == 0) jm[w * 32 + l] = m, js[w * 32 + l] = sum;
+  __syncthreads();
+  if (!there) return;
+  float top = -INFINITY, weight[NW], total = 0.0f;
+#pragma unroll
+  for (int k = 0; k < NW; ++k) top = fmaxf(top, jm[k * 32 + (l & 31)]);
+#pragma unroll
+  for (int k = 0; k < NW; ++k) {
+    weight[k] = exp2_of(jm[k * 32 + (l & 31)] - (top == -INFINITY ? 0.0f : top));
+    total = fmaf(weight[k], js[k * 32 + (l & 31)], total);
+  }
+  const int g4 = 4 * (tid >> 5);
+  const bool whole = a.splits == 1;
+  const float inv = !whole ? 1.0f : total == 0.0f ? 0.0f : 1.0f / total;
+  const int64_t part = (int64_t)split * a.nq * a.H + slot;
+  if (tid < 32) {
+    if (!whole) {
+      float* ml = a.part + (int64_t)a.splits * a.nq * a.H * a.hd + 2 * part;
+      ml[0] = top, ml[1] = total;
+    } else if (a.lse) {
+      a.lse[slot] = (top + __log2f(total)) * LN2;
+    }
+  }
+#pragma unroll
+  for (int d = 0; d < DB; ++d) {
+    const int c = 32 * d + g4;
+    if (c >= a.hd) continue;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < NW; ++k) v[e] = fmaf(weight[k], jo[(k * D + c + e) * 32 + (l & 31)], v[e]);
+      v[e] *= inv;
+    }
+    if (whole) store4((T*)a.out + query * a.ldout + head * a.hd + c, v[0], v[1], v[2], v[3]);
+    else *(float4*)(a.part + part * a.hd + c) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+}
+
+// The splits of a query's head, joined in their order: a workgroup to each; eight
+// slices of the splits, four values to a thread.
+template <typename T>
+__global__ __launch_bounds__(NT) void k_attn_join(AttnArgs a) {
+  __shared__ float red[8][MAX_HEAD_DIM + 4];
+  __shared__ float reds[8];
+  const int64_t slot = blockIdx.x, query = slot / a.H;
+  const int head = (int)(slot - query * a.H);
+  if (query < a.qb.at(0) || query >= a.qb.at(a.n_seg)) return;
+  const int64_t all = a.nq * a.H;
+  const float2* ml = (const float2*)(a.part + (int64_t)a.splits * all * a.hd);
+  const int c = 4 * ((int)threadIdx.x & 31), slice = (int)threadIdx.x >> 5;
+  float top = -INFINITY;
+  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[s * all + slot].x);
+  const float base = top == -INFINITY ? 0.0f : top;
+  float total = 0.0f, v[4] = {};
+  for (int s = slice; s < a.splits; s += 8) {
+    const float2 x = ml[s * all + slot];
+    if (x.y == 0.0f) continue;   // no keys
+    const float weight = exp2_of(x.x - base);
+    total = fmaf(weight, x.y, total);
+    if (c < a.hd) {
+      const float4 p = *(const float4*)(a.part + (s * all + slot) * a.hd + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(weight, (&p.x)[e], v[e]);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) red[slice][c + e] = v[e];
+  if (c == 0) reds[slice] = total;
+  __syncthreads();
+  if (slice) return;
+  total = 0.0f;
+  for (int s = 0; s < 8; ++s) total += reds[s];
+  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  if (c < a.hd) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = 0.0f;
+      for (int s = 0; s < 8; ++s) v[e] += red[s][c + e];
+    }
+    store4((T*)a.out + query * a.ldout + head * a.hd + c, v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+  }
+  if (c == 0 && a.lse) a.lse[slot] = (top + __log2f(total)) * LN2;
+}
+
+struct FwdPlan {
+  bool few;
+  int splits;
+  int64_t grid;
+};
+
+// Rows in tiles of 128 where these fill the card, else of 32, whose keys are dealt to
+// the waves, and where these are few as well to several workgroups of 512 keys at least.
+FwdPlan fwd_plan(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks) {
+  const int G = d.heads / d.kv_heads;
+  FwdPlan p{false, 1, tiles_of(qs.n, qs.n_seg, G, 32 * NW) * d.kv_heads};
+  if (p.grid >= FILL) return p;
+  p.few = true;
+  p.grid = tiles_of(qs.n, qs.n_seg, G, 32) * d.kv_heads;
+  const int64_t keys = ks.n / ks.n_seg;
+  if (p.grid < FILL) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(2 * FILL / p.grid, keys / 512));
+  p.grid *= p.splits;
+  return p;
+}
+
+size_t fwd_bytes(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks) {
+  const FwdPlan p = fwd_plan(d, qs, ks);
+  return p.splits == 1 ? 0 : (size_t)p.splits * qs.n * d.heads * (d.head_dim + 2) * sizeof(float);
+}
+
+size_t bwd_bytes(const dsmp_attention_desc& d, const dsmp_segments& qs) { return (size_t)qs.n * d.heads * sizeof(float); }
+
+}  // namespace
+
+namespace dsmp {
+
+dsmp_status check_attention(dsmp_handle* h, const dsmp_attention_desc* d, const dsmp_segments* qs, const dsmp_segments* ks) {
+  DSMP_CHECK(h, d && qs && ks, DSMP_INVALID_ARG, "the descriptor or the segments are NULL");
+  DSMP_CHECK(h, d->heads >= 1 && d->kv_heads >= 1 && d->head_dim >= 1, DSMP_INVALID_ARG, "no heads or no values in them");
+  DSMP_CHECK(h, d->heads % d->kv_heads == 0, DSMP_INVALID_ARG, "kv_heads must divide heads");
+  DSMP_CHECK(h, d->heads <= MAX_HEADS, DSMP_UNSUPPORTED, "more than %d heads", MAX_HEADS);
+  DSMP_CHECK(h, d->head_dim % 8 == 0 && d->head_dim <= MAX_HEAD_DIM, DSMP_UNSUPPORTED,
+             "head_dim must be a multiple of 8 up to %d", MAX_HEAD_DIM);
+  DSMP_CHECK(h, d->dtype == DSMP_F32 || d->dtype == DSMP_BF16, DSMP_INVALID_ARG, "unknown dtype");
+  DSMP_CHECK(h, d->dim >= 0 && d->dim <= 3, DSMP_INVALID_ARG, "0 to 3 coordinates");
+  DSMP_CHECK(h, std::isfinite(d->scale), DSMP_INVALID_ARG, "the scale must be finite");
+  DSMP_CHECK(h, std::isfinite(d->cap) && d->cap >= 0.0f, DSMP_INVALID_ARG, "the cap must be finite and not negative");
+  const int G = d->heads / d->kv_heads;
+  for (const dsmp_segments* s : {qs, ks}) {
+    DSMP_CHECK(h, s->n >= 0 && s->n_seg >= 1, DSMP_INVALID_ARG, "negative rows or no segment");
+    DSMP_CHECK(h, s->n < (int64_t)1 << 31 && s->n_seg < (int64_t)1 << 24, DSMP_UNSUPPORTED,
+               "2^31 rows or 2^24 segments and more");
+    DSMP_CHECK(h, s->ptr || s->n % s->n_seg == 0, DSMP_INVALID_ARG, "segments without ptr must divide the rows");
+    DSMP_CHECK(h, tiles_of(s->n, s->n_seg, G, 32) * d->kv_heads <= MAX_GROUPS && s->n * G < (int64_t)1 << 31,
+               DSMP_UNSUPPORTED, "too many rows, segments and heads for one call");
+  }
+  DSMP_CHECK(h, qs->n_seg == ks->n_seg, DSMP_INVALID_ARG, "queries and keys must have the same number of segments");
+  return DSMP_OK;
+}
+
+}  // namespace dsmp
+
+extern "C" dsmp_status dsmp_attention_workspace(const dsmp_attention_desc* desc, const dsmp_segments* qs,
+                                                const dsmp_segments* ks, size_t* fwd_ws_bytes, size_t* bwd_ws_bytes) {
+  const dsmp_status st = check_attention(nullptr, desc, qs, ks);
+  if (st != DSMP_OK) return st;
+  if (!fwd_ws_bytes || !bwd_ws_bytes) return DSMP_INVALID_ARG;
+  *fwd_ws_bytes = fwd_bytes(*desc, *qs, *ks);
+  *bwd_ws_bytes = bwd_bytes(*desc, *qs);
+  return DSMP_OK;
+}
+
+extern "C" dsmp_status dsmp_attention_forward(dsmp_handle* h, const dsmp_attention_desc* desc, const dsmp_segments* qs,
+                                              const dsmp_segments* ks, const void* q, int64_t ldq, const void* k,
+                                              int64_t ldk, const void* v, int64_t ldv, const float* pos_q,
+                                              const float* pos_k, const float* slopes, void* out, int64_t ldo,
+                                              float* lse, void* ws, size_t ws_bytes) {
+  if (!h) return DSMP_INVALID_ARG;
+  dsmp_status st = check_attention(h, desc, qs, ks);
+  if (st != DSMP_OK || qs->n == 0) return st;
+  DSMP_CHECK(h, q && out && (ks->n == 0 || (k && v)), DSMP_INVALID_ARG, "a data pointer is NULL");
+  DSMP_CHECK(h, desc->dim == 0 || (pos_q && slopes && (ks->n == 0 || pos_k)), DSMP_INVALID_ARG,
+             "coordinates and slopes are needed");
+  const int es = desc->dtype == DSMP_BF16 ? 2 : 4, wq = desc->heads * desc->head_dim, wk = desc->kv_heads * desc->head_dim;
+  st = check_matrices(h, es, {{q, ldq, wq, "q"}, {k, ldk, wk, "k"}, {v, ldv, wk, "v"}, {out, ldo, wq, "out"}});
+  if (st != DSMP_OK) return st;
+  const size_t need = fwd_bytes(*desc, *qs, *ks);
+  DSMP_CHECK(h, !need || (ws && ws_bytes >= need), DSMP_WORKSPACE_TOO_SMALL, "workspace needs %zu bytes", need);
+  DSMP_CHECK(h, !need || reinterpret_cast<uintptr_t>(ws) % 16 == 0, DSMP_INVALID_ARG, "the workspace must be 16-byte aligned");
+  const FwdPlan plan = fwd_plan(*desc, *qs, *ks);
+  AttnArgs a = attn_args(*desc, *qs, *ks);
+  a.q = q, a.ldq = ldq, a.k = k, a.ldk = ldk, a.v = v, a.ldv = ldv, a.out = out, a.ldout = ldo, a.lse = lse;
+  a.pos_q = pos_q, a.pos_k = pos_k, a.slopes = slopes;
+  a.splits = plan.splits, a.part = (float*)ws;
+  DeviceScope dev(h);
+  ProfScope prof(h, DSMP_K_ATTN_FWD);
+  by_attention(*desc, [&](auto t, auto width, auto mode) {
+    using T = decltype(t);
+    constexpr int D = decltype(width)::value;
+    using M = decltype(mode);
+    if (plan.few) hipLaunchKernelGGL((k_attn_fwd<T, D, true, M>), dim3((unsigned)plan.grid), dim3(NT), 0, h->stream, a);
+    else hipLaunchKernelGGL((k_attn_fwd<T, D, false, M>), dim3((unsigned)plan.grid), dim3(NT), 0, h->stream, a);
+    if (plan.splits > 1)
+      hipLaunchKernelGGL((k_attn_join<T>), dim3((unsigned)(qs->n * desc->heads)), dim3(NT), 0, h->stream, a);
+  });
+  DSMP_LAUNCHED(h, "attention forward");
+  return DSMP_OK;
+}
+
+extern "C" dsmp_status dsmp_attention_backward(dsmp_handle* h, const dsmp_attention_desc* desc, const dsmp_segments* qs,
+                                               const dsmp_segments* ks, const void* q, int64_t ldq, const void* k,
+                                               int64_t ldk, const void* v, int64_t ldv, const float* pos_q,
+                                               const float* pos_k, const float* slopes, const void* out, int64_t ldo,
+                                               const float* lse, const void* grad_out, int64_t ldgo, void* grad_q,
+                                               int64_t ldgq, void* grad_k, int64_t ldgk, void* grad_v, int64_t ldgv,
+                                               void* ws, size_t ws_bytes) {
+  if (!h) return DSMP_INVALID_ARG;
+  dsmp_status st = check_attention(h, desc, qs, ks);
+  if (st != DSMP_OK) return st;
+  DSMP_CHECK(h, (qs->n == 0 || (q && out && lse && grad_out && grad_q)) && (ks->n == 0 || (k && v && grad_k && grad_v)),
+             DSMP_INVALID_ARG, "a data pointer is NULL");
+  DSMP_CHECK(h, desc->dim == 0 || (slopes && (qs->n == 0 || pos_q) && (ks->n == 0 || pos_k)), DSMP_INVALID_ARG,
+             "coordinates and slopes are needed");
+  const int es = desc->dtype == DSMP_BF16 ? 2 : 4, wq = desc->heads * desc->head_dim, wk = desc->kv_heads * desc->head_dim;
+  st = check_matrices(h, es, {{q, ldq, wq, "q"}, {k, ldk, wk, "k"}, {v, ldv, wk, "v"}, {out, ldo, wq, "out"},
+                              {grad_out, ldgo, wq, "grad_out"}, {grad_q, ldgq, wq, "grad_q"},
+                              {grad_k, ldgk, wk, "grad_k"}, {grad_v, ldgv, wk, "grad_v"}});
+  if (st != DSMP_OK) return st;
+  const size_t need = bwd_bytes(*desc, *qs);
+  DSMP_CHECK(h, !need || (ws && ws_bytes >= need), DSMP_WORKSPACE_TOO_SMALL, "workspace needs %zu bytes", need);
+  DSMP_CHECK(h, !need || reinterpret_cast<uintptr_t>(ws) % 16 == 0, DSMP_INVALID_ARG, "the workspace must be 16-byte aligned");
+  AttnArgs a = attn_args(*desc, *qs, *ks);
+  a.q = q, a.ldq = ldq, a.k = k, a.ldk = ldk, a.v = v, a.ldv = ldv, a.o = out, a.ldo = ldo, a.go = grad_out, a.ldgo = ldgo;
+  a.gq = grad_q, a.ldgq = ldgq, a.gk = grad_k, a.ldgk = ldgk, a.gv = grad_v, a.ldgv = ldgv;
+  a.lse_in = lse, a.delta = (float*)ws;
+  a.pos_q = pos_q, a.pos_k = pos_k, a.slopes = slopes;
+  DeviceScope dev(h);
+  ProfScope prof(h, DSMP_K_ATTN_BWD);
+  if (qs->n > 0) launch_attention_dq(h, *desc, a);
+  if (ks->n > 0) launch_attention_dkv(h, *desc, a, ks->n);
+  DSMP_LAUNCHED(h, "attention backward");
+  return DSMP_OK;
+}
