@@ -261,9 +261,20 @@ __device__ __forceinline__ ScoreConst score_const(const AttnArgs& a) {
   return {a.scale * LOG2E, a.cap > 0.0f ? 2.0f * LOG2E * a.scale / a.cap : 0.0f, a.cap * LOG2E};
 }
 
+// tanh for float32 scores, within about 3 u of it: 1 - 2 / (1 + e^2x), whose difference costs
+// digits near zero, where the series to x^11 takes its place (its next term is 2^-26 of x at 0.35).
+__device__ __forceinline__ float tanh_of(float x) {
+  const float far = 1.0f - 2.0f / (1.0f + exp2_of(x * (2.0f * LOG2E))), s = x * x;
+  float p = fmaf(s, -1382.0f / 155925.0f, 62.0f / 2835.0f);
+  p = fmaf(s, p, -17.0f / 315.0f);
+  p = fmaf(s, p, 2.0f / 15.0f);
+  p = fmaf(s, p, -1.0f / 3.0f);
+  return fabsf(x) < 0.35f ? fmaf(x * s, p, x) : far;
+}
+
 // log2(e) times the score without its bias; `fall` receives 1 - tanh^2.
 // tanh x = 1 - 2 r with r = 1 / (1 + e^2x); 1 - tanh^2 x = 4 r (1 - r).  The difference from 1 leaves an
-// absolute error of about 2^-23 in tanh; float32 scores take tanhf.
+// absolute error of about 2^-23 in tanh, which bfloat16 operands hide.
 template <typename T, bool SLOPE>
 __device__ __forceinline__ float capped(float s, bool cap, const ScoreConst& c, float* fall) {
   if (!cap) {
@@ -271,7 +282,7 @@ __device__ __forceinline__ float capped(float s, bool cap, const ScoreConst& c, 
     return s * c.scale2;
   }
   if (sizeof(T) == 4) {
-    const float t = tanhf(s * c.turn * (0.5f * LN2));
+    const float t = tanh_of(s * c.turn * (0.5f * LN2));
     if (SLOPE) *fall = 1.0f - t * t;
     return c.cap2 * t;
   }

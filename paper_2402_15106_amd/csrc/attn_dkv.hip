@@ -21,7 +21,7 @@ struct Dkv {
   static constexpr int SUB = FEW ? 1 : BQ / 32;
   static constexpr int P = pitch_of<T, D, false>();   // both matrices are read both ways
   static constexpr int PER = BQ * D * (int)sizeof(T) / 16 / NT, STEP = NT * 16 / (D * (int)sizeof(T));
-  static constexpr bool AHEAD = !(FEW && sizeof(T) == 4);
+  static constexpr bool AHEAD = !(FEW && sizeof(T) == 4 && D == 128);
   static constexpr int HELD = AHEAD ? PER : PER < 4 ? PER : 2;
   static constexpr int TILE = 2 * BQ * P + 6 * BQ * 4;
   static constexpr int JOIN = FEW ? NW * 32 * D * 4 : 0;

@@ -22,7 +22,7 @@ struct Dq {
   static constexpr int PK = pitch_of<T, D, false>(), PV = pitch_of<T, D, true>();   // K is read both ways
   static constexpr int PER = BN * D * (int)sizeof(T) / 16 / NT, STEP = NT * 16 / (D * (int)sizeof(T));
   // the next tile waits in registers, but for FEW's large ones in float32: those come four units at a time
-  static constexpr bool AHEAD = !(FEW && sizeof(T) == 4);
+  static constexpr bool AHEAD = !(FEW && sizeof(T) == 4 && D == 128);
   static constexpr int HELD = AHEAD || PER < 4 ? PER : 4;
   static constexpr int TILE = BN * (PK + PV) + 3 * BN * 4;
   static constexpr int JOIN = FEW ? NW * 32 * D * 4 : 0;
@@ -30,7 +30,7 @@ struct Dq {
 };
 
 template <typename T, int D, bool FEW, typename M>
-__global__ __launch_bounds__(NT, D == 128 && (FEW || sizeof(T) == 4) ? 1 : 2) void k_attn_dq(AttnArgs a) {
+__global__ __launch_bounds__(NT, (D == 128 && (FEW || sizeof(T) == 4)) || (D == 64 && FEW && sizeof(T) == 4) ? 1 : 2) void k_attn_dq(AttnArgs a) {
   using C = Dq<T, D, FEW>;
   constexpr int ES = sizeof(T), KS = D / 16, DB = D / 32;
   typedef typename Frag<T>::type frag;

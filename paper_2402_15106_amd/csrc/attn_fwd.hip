@@ -24,7 +24,7 @@ struct Fwd {
   static constexpr int PK = pitch_of<T, D, true>(), PV = pitch_of<T, D, false>();
   static constexpr int PER = BN * D * (int)sizeof(T) / 16 / NT, STEP = NT * 16 / (D * (int)sizeof(T));
   // the next tile waits in registers, but for FEW's large ones in float32: those come four units at a time
-  static constexpr bool AHEAD = !(FEW && sizeof(T) == 4);
+  static constexpr bool AHEAD = !(FEW && sizeof(T) == 4 && D == 128);
   static constexpr int HELD = AHEAD || PER < 4 ? PER : 4;
   static constexpr int TILE = BN * (PK + PV) + 3 * BN * 4;
   static constexpr int JOIN = FEW ? NW * 32 * (D + 2) * 4 : 0;
@@ -242,50 +242,103 @@ __global__ __launch_bounds__(NT, D == 128 && (FEW || sizeof(T) == 4 || M::DIM > 
   }
 }
 
-// The splits of a query's head, joined in their order: a workgroup to each; eight
-// slices of the splits, four values to a thread.
+// The splits of a query's head, joined in their order.  A split without keys has the sum 0
+// and has written no values.  FEW_SPLITS: 32 lanes to each; otherwise a workgroup of 1,024, whose
+// 32 slices of the splits are added up.
+constexpr int FEW_SPLITS = 8, MAX_SPLITS = 1024;
+
+__device__ __forceinline__ bool in_segments(const AttnArgs& a, int64_t query) {
+  return query >= a.qb.at(0) && query < a.qb.at(a.n_seg);
+}
+
 template <typename T>
-__global__ __launch_bounds__(NT) void k_attn_join(AttnArgs a) {
-  __shared__ float red[8][MAX_HEAD_DIM + 4];
-  __shared__ float reds[8];
-  const int64_t slot = blockIdx.x, query = slot / a.H;
-  const int head = (int)(slot - query * a.H);
-  if (query < a.qb.at(0) || query >= a.qb.at(a.n_seg)) return;
-  const int64_t all = a.nq * a.H;
+__device__ __forceinline__ void write_joined(const AttnArgs& a, int64_t slot, int64_t query, int c, const float* v, float top,
+                                             float total) {
+  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  if (c < a.hd)
+    store4((T*)a.out + query * a.ldout + (slot - query * a.H) * a.hd + c, v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+  if (c == 0 && a.lse) a.lse[slot] = (top + __log2f(total)) * LN2;
+}
+
+template <typename T>
+__global__ __launch_bounds__(NT) void k_attn_join_few(AttnArgs a) {
+  const int64_t all = a.nq * a.H, slot = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (slot >= all) return;
+  const int64_t query = slot / a.H;
+  if (!in_segments(a, query)) return;
   const float2* ml = (const float2*)(a.part + (int64_t)a.splits * all * a.hd);
-  const int c = 4 * ((int)threadIdx.x & 31), slice = (int)threadIdx.x >> 5;
+  const int c = 4 * ((int)threadIdx.x & 31);
+  float2 x[FEW_SPLITS];
+  float4 p[FEW_SPLITS];
   float top = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[s * all + slot].x);
+#pragma unroll
+  for (int s = 0; s < FEW_SPLITS; ++s) x[s] = s < a.splits ? ml[s * all + slot] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+  for (int s = 0; s < FEW_SPLITS; ++s)
+    if (s < a.splits && c < a.hd) p[s] = *(const float4*)(a.part + (s * all + slot) * a.hd + c);
+#pragma unroll
+  for (int s = 0; s < FEW_SPLITS; ++s) top = fmaxf(top, x[s].x);
   const float base = top == -INFINITY ? 0.0f : top;
   float total = 0.0f, v[4] = {};
-  for (int s = slice; s < a.splits; s += 8) {
-    const float2 x = ml[s * all + slot];
-    if (x.y == 0.0f) continue;   // no keys
-    const float weight = exp2_of(x.x - base);
-    total = fmaf(weight, x.y, total);
-    if (c < a.hd) {
-      const float4 p = *(const float4*)(a.part + (s * all + slot) * a.hd + c);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = fmaf(weight, (&p.x)[e], v[e]);
+  for (int s = 0; s < FEW_SPLITS; ++s) {
+    if (s >= a.splits || x[s].y == 0.0f) continue;
+    const float weight = exp2_of(x[s].x - base);
+    total = fmaf(weight, x[s].y, total);
+    if (c < a.hd) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(weight, (&p[s].x)[e], v[e]);
+    }
+  }
+  write_joined<T>(a, slot, query, c, v, top, total);
+}
+
+template <typename T>
+__global__ __launch_bounds__(1024) void k_attn_join(AttnArgs a) {
+  __shared__ float red[32][MAX_HEAD_DIM + 4];
+  __shared__ float weight[MAX_SPLITS];
+  __shared__ float wave[2][16];
+  const int64_t slot = blockIdx.x, query = slot / a.H, all = a.nq * a.H;
+  if (!in_segments(a, query)) return;
+  const int tid = (int)threadIdx.x, c = 4 * (tid & 31), slice = tid >> 5;
+  const float2 x = tid < a.splits ? ((const float2*)(a.part + (int64_t)a.splits * all * a.hd))[tid * all + slot]
+                                  : make_float2(-INFINITY, 0.0f);
+  float top = x.x;
+  for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  if ((tid & 63) == 0) wave[0][tid >> 6] = top;
+  __syncthreads();
+  top = wave[0][0];
+  for (int k = 1; k < 16; ++k) top = fmaxf(top, wave[0][k]);
+  const float mine = x.y == 0.0f ? 0.0f : exp2_of(x.x - (top == -INFINITY ? 0.0f : top));
+  weight[tid] = mine;
+  float total = mine * x.y;
+  for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
+  if ((tid & 63) == 0) wave[1][tid >> 6] = total;
+  __syncthreads();
+  total = 0.0f;
+  for (int k = 0; k < 16; ++k) total += wave[1][k];
+  float v[4] = {};
+  if (c < a.hd) {
+    const float* from = a.part + slot * a.hd + c;
+    const int64_t step = all * a.hd;
+#pragma unroll 8
+    for (int s = slice; s < a.splits; s += 32) {
+      const float w = weight[s];
+      const float4 p = *(const float4*)(from + s * step);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = w == 0.0f ? v[e] : fmaf(w, (&p.x)[e], v[e]);
     }
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) red[slice][c + e] = v[e];
-  if (c == 0) reds[slice] = total;
   __syncthreads();
   if (slice) return;
-  total = 0.0f;
-  for (int s = 0; s < 8; ++s) total += reds[s];
-  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-  if (c < a.hd) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[e] = 0.0f;
-      for (int s = 0; s < 8; ++s) v[e] += red[s][c + e];
-    }
-    store4((T*)a.out + query * a.ldout + head * a.hd + c, v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+  for (int e = 0; e < 4; ++e) {
+    v[e] = 0.0f;
+    for (int s = 0; s < 32; ++s) v[e] += red[s][c + e];
   }
-  if (c == 0 && a.lse) a.lse[slot] = (top + __log2f(total)) * LN2;
+  write_joined<T>(a, slot, query, c, v, top, total);
 }
 
 struct FwdPlan {
@@ -303,7 +356,7 @@ FwdPlan fwd_plan(const dsmp_attention_desc& d, const dsmp_segments& qs, const ds
   p.few = true;
   p.grid = tiles_of(qs.n, qs.n_seg, G, 32) * d.kv_heads;
   const int64_t keys = ks.n / ks.n_seg;
-  if (p.grid < FILL) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(2 * FILL / p.grid, keys / 512));
+  if (p.grid < FILL) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({2 * FILL / p.grid, keys / 512, MAX_SPLITS}));
   p.grid *= p.splits;
   return p;
 }
@@ -385,8 +438,11 @@ extern "C" dsmp_status dsmp_attention_forward(dsmp_handle* h, const dsmp_attenti
     using M = decltype(mode);
     if (plan.few) hipLaunchKernelGGL((k_attn_fwd<T, D, true, M>), dim3((unsigned)plan.grid), dim3(NT), 0, h->stream, a);
     else hipLaunchKernelGGL((k_attn_fwd<T, D, false, M>), dim3((unsigned)plan.grid), dim3(NT), 0, h->stream, a);
-    if (plan.splits > 1)
-      hipLaunchKernelGGL((k_attn_join<T>), dim3((unsigned)(qs->n * desc->heads)), dim3(NT), 0, h->stream, a);
+    const int64_t slots = qs->n * desc->heads;
+    if (plan.splits > FEW_SPLITS)
+      hipLaunchKernelGGL((k_attn_join<T>), dim3((unsigned)slots), dim3(1024), 0, h->stream, a);
+    else if (plan.splits > 1)
+      hipLaunchKernelGGL((k_attn_join_few<T>), dim3(ceil_div(slots, 8)), dim3(NT), 0, h->stream, a);
   });
   DSMP_LAUNCHED(h, "attention forward");
   return DSMP_OK;

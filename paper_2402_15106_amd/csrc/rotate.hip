@@ -6,9 +6,10 @@
 //   backward: g = amp times the pairs of dy turned by -t,  w = g gamma
 //             dx = r (w - x r mean(w x r)),  dgamma = sum g x r
 //
-// A head is taken by LP = 2^lg >= head_dim / 8 lanes with eight values each; which
-// eight is chosen so that both values of a pair are a lane's own, and a row's sines
-// and cosines (four pairs to a lane) serve all of its heads.
+// A lane has 16 bytes of a head (VE = 4 or 8 values) and 2^lg lanes a head; a row's sines and
+// cosines serve all of its heads.  The other value of a pair is the lane's own neighbour
+// (interleaved pairs) or comes through LDS (half layout), so that every access to memory is
+// of whole 16-byte pieces in a row.  Bound by memory.
 #include "attention.hpp"
 
 #include <cmath>
@@ -17,16 +18,17 @@ using namespace dsmp;
 
 namespace {
 
-constexpr int RT = 256;        // threads of a workgroup
-constexpr int RU = 4;          // heads of a lane's row that are on their way at once
+constexpr int RT = 256;         // threads of a workgroup
+constexpr int RU = 4;           // heads of a row that are on their way at once (forward)
+constexpr int RUB = 2;          // the same, backward (twice the inputs)
 constexpr int MAX_PARTS = 1024; // workgroups of a backward pass (their sums of dgamma are kept)
 
 struct RotArgs {
   int64_t n;
-  int heads[2], hd, rot, axes, lg, lanes;   // lanes: head_dim / 8
-  int per_axis;                             // pairs to a coordinate
+  int heads[2], hd, rot, axes, lg, lanes;   // lanes: of a head, that have values
+  int per_axis, interleaved;                // per_axis: pairs to a coordinate
   int chunks, per;                          // a row's heads (both sets, one after the other) in chunks of `per`
-  float eps, amp;
+  float eps, amp;                           // eps < 0: no norm
   const void* x[2];
   const void* dy[2];
   void* y[2];
@@ -38,75 +40,66 @@ struct RotArgs {
   int parts, accumulate;
 };
 
-// Where a lane's eight values are.  EIGHT: eight in a row (interleaved pairs, or no
-// pairs).  SPLIT: four and their four partners rot / 2 further on, behind the rotated
-// part eight in a row (half layout, rot a multiple of 8).  PAIRS: four pairs, each
-// value addressed by itself (half layout, any other rot).
-enum { EIGHT = 0, SPLIT = 1, PAIRS = 2 };
+template <typename T>
+constexpr int VE = 16 / (int)sizeof(T);
 
-template <int FORM>
-__device__ __forceinline__ int value_at(const RotArgs& a, int lane, int i) {
-  if (FORM == EIGHT) return 8 * lane + i;
-  const int half = a.rot >> 1;
-  if (FORM == SPLIT) {
-    if (8 * lane >= a.rot) return 8 * lane + i;
-    return i < 4 ? 4 * lane + i : half + 4 * lane + i - 4;
-  }
-  const int p = 4 * lane + (i & 3);      // pairs behind rot / 2: values from rot on, two by two
-  if (p >= half) return 2 * p + (i >> 2);
-  return i < 4 ? p : p + half;
+// The other value of element e's pair (e itself where it is not rotated).
+__device__ __forceinline__ int partner(const RotArgs& a, int e) {
+  if (e >= a.rot) return e;
+  if (a.interleaved) return e ^ 1;
+  return e < (a.rot >> 1) ? e + (a.rot >> 1) : e - (a.rot >> 1);
 }
 
-template <typename T, int FORM>
-__device__ __forceinline__ void load8(float* v, const T* head, const RotArgs& a, int lane) {
-  if (FORM == PAIRS) {
+// The pair's other values of a lane's own (0 for a value that is not rotated).  PIECE > 0 (half layout): through LDS, PIECE values at
+// a time, which divides rot / 2 and VE, so that no piece has partners in two places; `sh` is the
+// wave's own, 16 bytes to a lane, and a wave's LDS accesses stay in order.
+template <typename T, int PIECE>
+__device__ __forceinline__ void exchange(const RotArgs& a, const T* own, T* other, T* sh, int lane) {
+  constexpr int N = VE<T>;
+  if (PIECE == 0) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)head[value_at<FORM>(a, lane, i)];
+    for (int i = 0; i < N; ++i) other[i] = lane * N + i < a.rot ? own[i ^ 1] : (T)0.0f;
     return;
   }
-  if (FORM == EIGHT && sizeof(T) == 2) {
-    typedef T t8 __attribute__((ext_vector_type(8)));
-    const t8 w = *(const t8*)(head + 8 * lane);
+  typedef T whole __attribute__((ext_vector_type(N)));
+  constexpr int P = PIECE ? PIECE : 1;
+  const int wl = (int)threadIdx.x & 63, group = (wl >> a.lg) << a.lg;
+  whole w;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)w[i];
-    return;
+  for (int i = 0; i < N; ++i) w[i] = own[i];
+  *(whole*)(sh + wl * N) = w;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int i = 0; i < N; i += P) {
+    const T* from = sh + group * N + partner(a, lane * N + i);
+    const bool turns = lane * N + i < a.rot;
+    if constexpr (P == 1) {
+      other[i] = turns ? from[0] : (T)0.0f;
+    } else {
+      typedef T piece __attribute__((ext_vector_type(P)));
+      const piece p = *(const piece*)from;
+#pragma unroll
+      for (int k = 0; k < P; ++k) other[i + k] = turns ? p[k] : (T)0.0f;
+    }
   }
-  const T* lo = head + value_at<FORM>(a, lane, 0);
-  const T* hi = head + value_at<FORM>(a, lane, 4);
-  typedef T t4 __attribute__((ext_vector_type(4)));
-  const t4 l = *(const t4*)lo, u = *(const t4*)hi;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = (float)l[i], v[4 + i] = (float)u[i];
 }
 
-template <typename T, int FORM>
-__device__ __forceinline__ void store8(const float* v, T* head, const RotArgs& a, int lane) {
-  if (FORM == PAIRS) {
+template <typename T>
+__device__ __forceinline__ void load_piece(T* v, const T* p) {
+  typedef T whole __attribute__((ext_vector_type(VE<T>)));
+  const whole w = *(const whole*)p;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) head[value_at<FORM>(a, lane, i)] = (T)v[i];
-    return;
-  }
-  if (FORM == EIGHT && sizeof(T) == 2) {
-    typedef T t8 __attribute__((ext_vector_type(8)));
-    t8 w;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = (T)v[i];
-    *(t8*)(head + 8 * lane) = w;
-    return;
-  }
-  typedef T t4 __attribute__((ext_vector_type(4)));
-  t4 l, u;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) l[i] = (T)v[i], u[i] = (T)v[4 + i];
-  *(t4*)(head + value_at<FORM>(a, lane, 0)) = l;
-  *(t4*)(head + value_at<FORM>(a, lane, 4)) = u;
+  for (int i = 0; i < VE<T>; ++i) v[i] = w[i];
 }
-
-// the two registers of a lane's pair k (0..3), the row's pair 4 lane + k
-template <int FORM>
-__device__ __forceinline__ constexpr int first_of(int k) { return FORM == EIGHT ? 2 * k : k; }
-template <int FORM>
-__device__ __forceinline__ constexpr int second_of(int k) { return FORM == EIGHT ? 2 * k + 1 : k + 4; }
+template <typename T>
+__device__ __forceinline__ void store_piece(T* p, const float* v) {
+  typedef T whole __attribute__((ext_vector_type(VE<T>)));
+  whole w;
+#pragma unroll
+  for (int i = 0; i < VE<T>; ++i) w[i] = (T)v[i];
+  *(whole*)p = w;
+}
 
 // sum over the lanes of a head (2^lg of them, side by side)
 __device__ __forceinline__ float sum_lanes(float v, int lg) {
@@ -114,88 +107,114 @@ __device__ __forceinline__ float sum_lanes(float v, int lg) {
   return v;
 }
 
-// amp cos and amp sin of a lane's four pairs; pairs that are not rotated get 1 and 0
+// For each value of a lane: what its own and its partner's count in the turned one
+// (amp cos, and amp sin with its sign); 1 and 0 where nothing is turned.
+template <typename T, int PIECE>
 __device__ __forceinline__ void angles(const RotArgs& a, int64_t row, int lane, float* c, float* s) {
+  constexpr int STEP = PIECE == 0 ? 2 : 1;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int p = 4 * lane + k;
-    c[k] = 1.0f, s[k] = 0.0f;
-    if (p < (a.rot >> 1)) {
+  for (int i = 0; i < VE<T>; i += STEP) {
+    const int e = lane * VE<T> + i, half = a.rot >> 1;
+    c[i] = 1.0f, s[i] = 0.0f;
+    if (STEP == 2) c[i + STEP - 1] = 1.0f, s[i + STEP - 1] = 0.0f;
+    if (e < a.rot) {
+      const int p = STEP == 2 ? e >> 1 : e < half ? e : e - half;
       const int axis = p >= 2 * a.per_axis ? 2 : p >= a.per_axis ? 1 : 0;
-      // turns in float64: the product of two float32 is exact, and so is what is left of it in one turn, but for 2^-53 of it
+      // turns in float64: the product of two float32 is exact, and what is left of it in one turn is within 2^-52 of it
       const double turns = (double)a.pos[row * a.axes + axis] * (double)a.freq[p] * 0.15915494309189533577;
       float sn, cs;
       sincospif(2.0f * (float)(turns - __builtin_rint(turns)), &sn, &cs);
-      c[k] = a.amp * cs, s[k] = a.amp * sn;
+      c[i] = a.amp * cs, s[i] = a.amp * (STEP == 2 || e < half ? -sn : sn);
+      if (STEP == 2) c[i + STEP - 1] = c[i], s[i + STEP - 1] = -s[i];
     }
   }
 }
 
-// One row and chunk of heads to a group of lanes.  Bound by memory: values read and
-// written once.
-template <typename T, int FORM>
+// A row's chunk of heads to a group of lanes.
+template <typename T, int PIECE>
 __global__ __launch_bounds__(RT) void k_rotate(RotArgs a) {
+  constexpr int N = VE<T>;
+  __shared__ __align__(16) T sh[PIECE ? RU * RT * N : N];
   const int group = (int)threadIdx.x >> a.lg, lane = (int)threadIdx.x & ((1 << a.lg) - 1);
+  T* mine = sh + (PIECE ? ((int)threadIdx.x & ~63) * N * RU : 0);
   const int64_t items = a.n * a.chunks, item = (int64_t)blockIdx.x * (RT >> a.lg) + group;
   const bool on = item < items && lane < a.lanes;
   const int64_t row = on ? item / a.chunks : 0;
   const int c0 = on ? (int)(item - row * a.chunks) * a.per : 0;
   const int all = a.heads[0] + a.heads[1], c1 = min(c0 + a.per, all);
-  float cs[4], sn[4], gam[2][8];
-  if (on) angles(a, row, lane, cs, sn);
+  T x[RU][N];
+  auto fetch = [&](int j0) {
+#pragma unroll
+    for (int j = 0; j < RU; ++j) {
+      const int hh = c0 + j0 + j, t = hh >= a.heads[0];
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[j][i] = (T)0.0f;
+      if (on && hh < c1)
+        load_piece(x[j], (const T*)a.x[t] + row * a.ldx[t] + (int64_t)(hh - (t ? a.heads[0] : 0)) * a.hd + lane * N);
+    }
+  };
+  fetch(0);
+  // gamma goes into the angles' factors, one set for the queries and one for the keys
+  float c[N], s[N], own[2][N], oth[2][N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) c[i] = 1.0f, s[i] = 0.0f;
+  if (on) angles<T, PIECE>(a, row, lane, c, s);
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) gam[t][i] = on && a.gamma[t] ? a.gamma[t][value_at<FORM>(a, lane, i)] : 1.0f;
+    for (int i = 0; i < N; ++i) {
+      const int e = lane * N + i;
+      const bool g = on && a.gamma[t];
+      own[t][i] = (g ? a.gamma[t][e] : 1.0f) * c[i], oth[t][i] = (g ? a.gamma[t][partner(a, e)] : 1.0f) * s[i];
+    }
   const float mean = 1.0f / (float)a.hd;
   for (int j0 = 0; j0 < a.per; j0 += RU) {
-    float v[RU][8];
+    T now[RU][N];
+#pragma unroll
+    for (int j = 0; j < RU; ++j)
+#pragma unroll
+      for (int i = 0; i < N; ++i) now[j][i] = x[j][i];
+    if (j0 + RU < a.per) fetch(j0 + RU);
 #pragma unroll
     for (int j = 0; j < RU; ++j) {
       const int hh = c0 + j0 + j, t = hh >= a.heads[0];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[j][i] = 0.0f;
-      if (on && hh < c1)
-        load8<T, FORM>(v[j], (const T*)a.x[t] + row * a.ldx[t] + (int64_t)(hh - (t ? a.heads[0] : 0)) * a.hd, a, lane);
-    }
-#pragma unroll
-    for (int j = 0; j < RU; ++j) {
-      const int hh = c0 + j0 + j, t = hh >= a.heads[0];
-      float r = 1.0f;
+      T other[N];
+      exchange<T, PIECE>(a, now[j], other, mine + (PIECE ? j * 64 * N : 0), lane);
+      float r = 1.0f, v[N];
       if (a.eps >= 0.0f) {
         float q = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q = fmaf(v[j][i], v[j][i], q);
+        for (int i = 0; i < N; ++i) q = fmaf((float)now[j][i], (float)now[j][i], q);
         r = 1.0f / sqrtf(fmaf(sum_lanes(q, a.lg), mean, a.eps));
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[j][i] *= r * (t ? gam[1][i] : gam[0][i]);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float p = v[j][first_of<FORM>(k)], q = v[j][second_of<FORM>(k)];
-        v[j][first_of<FORM>(k)] = p * cs[k] - q * sn[k];
-        v[j][second_of<FORM>(k)] = p * sn[k] + q * cs[k];
+      for (int i = 0; i < N; ++i) {
+        const float ow = t ? own[1][i] : own[0][i], ot = t ? oth[1][i] : oth[0][i];
+        v[i] = r * fmaf((float)now[j][i], ow, (float)other[i] * ot);
       }
       if (on && hh < c1)
-        store8<T, FORM>(v[j], (T*)a.y[t] + row * a.ldy[t] + (int64_t)(hh - (t ? a.heads[0] : 0)) * a.hd, a, lane);
+        store_piece((T*)a.y[t] + row * a.ldy[t] + (int64_t)(hh - (t ? a.heads[0] : 0)) * a.hd + lane * N, v);
     }
   }
 }
 
 // Backward; workgroups step over the items, so that a lane's sums of dgamma stay in
 // its registers; a workgroup's are added up in a fixed order and kept, [part][2][hd].
-template <typename T, int FORM>
+template <typename T, int PIECE>
 __global__ __launch_bounds__(RT) void k_rotate_bwd(RotArgs a) {
-  __shared__ float sh[RT * 8];
+  constexpr int N = VE<T>;
+  constexpr int WORDS = RT * N > RUB * RT * N * (int)sizeof(T) / 4 ? RT * N : RUB * RT * N * (int)sizeof(T) / 4;
+  __shared__ __align__(16) float shf[WORDS];
+  T* mine = (T*)shf + ((int)threadIdx.x & ~63) * N * RUB;
   const int groups = RT >> a.lg, group = (int)threadIdx.x >> a.lg, lane = (int)threadIdx.x & ((1 << a.lg) - 1);
   const int64_t items = a.n * a.chunks;
   const int all = a.heads[0] + a.heads[1];
-  float gam[2][8], dg[2][8];
+  float gam[2][N], dg[2][N];
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      gam[t][i] = lane < a.lanes && a.gamma[t] ? a.gamma[t][value_at<FORM>(a, lane, i)] : 1.0f;
+    for (int i = 0; i < N; ++i) {
+      gam[t][i] = lane < a.lanes && a.gamma[t] ? a.gamma[t][lane * N + i] : 1.0f;
       dg[t][i] = 0.0f;
     }
   const float mean = 1.0f / (float)a.hd;
@@ -204,53 +223,62 @@ __global__ __launch_bounds__(RT) void k_rotate_bwd(RotArgs a) {
     const bool on = item < items && lane < a.lanes;
     const int64_t row = on ? item / a.chunks : 0;
     const int c0 = on ? (int)(item - row * a.chunks) * a.per : 0, c1 = min(c0 + a.per, all);
-    float cs[4], sn[4];
-    if (on) angles(a, row, lane, cs, sn);
-    constexpr int U = 2;
-    for (int j0 = 0; j0 < a.per; j0 += U) {
-      float x[U][8], g[U][8];
+    T xs[RUB][N], gs[RUB][N];
+    auto fetch = [&](int j0) {
 #pragma unroll
-      for (int j = 0; j < U; ++j) {
+      for (int j = 0; j < RUB; ++j) {
         const int hh = c0 + j0 + j, t = hh >= a.heads[0];
-        const int64_t at = (int64_t)(hh - (t ? a.heads[0] : 0)) * a.hd;
+        const int64_t at = (int64_t)(hh - (t ? a.heads[0] : 0)) * a.hd + lane * N;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[j][i] = g[j][i] = 0.0f;
+        for (int i = 0; i < N; ++i) xs[j][i] = gs[j][i] = (T)0.0f;
         if (on && hh < c1) {
-          load8<T, FORM>(x[j], (const T*)a.x[t] + row * a.ldx[t] + at, a, lane);
-          load8<T, FORM>(g[j], (const T*)a.dy[t] + row * a.lddy[t] + at, a, lane);
+          load_piece(xs[j], (const T*)a.x[t] + row * a.ldx[t] + at);
+          load_piece(gs[j], (const T*)a.dy[t] + row * a.lddy[t] + at);
         }
       }
+    };
+    fetch(0);
+    float c[N], s[N];
 #pragma unroll
-      for (int j = 0; j < U; ++j) {
+    for (int i = 0; i < N; ++i) c[i] = 1.0f, s[i] = 0.0f;
+    if (on) angles<T, PIECE>(a, row, lane, c, s);
+    for (int j0 = 0; j0 < a.per; j0 += RUB) {
+      T xn[RUB][N], gn[RUB][N];
+#pragma unroll
+      for (int j = 0; j < RUB; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) xn[j][i] = xs[j][i], gn[j][i] = gs[j][i];
+      if (j0 + RUB < a.per) fetch(j0 + RUB);
+#pragma unroll
+      for (int j = 0; j < RUB; ++j) {
         const int hh = c0 + j0 + j, t = hh >= a.heads[0];
-        const bool here = on && hh < c1;
-        const int64_t at = (int64_t)(hh - (t ? a.heads[0] : 0)) * a.hd;
-        if (here) {
+        T other[N];
+        exchange<T, PIECE>(a, gn[j], other, mine + j * 64 * N, lane);
+        float x[N], g[N];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float p = g[j][first_of<FORM>(k)], q = g[j][second_of<FORM>(k)];
-            g[j][first_of<FORM>(k)] = p * cs[k] + q * sn[k];
-            g[j][second_of<FORM>(k)] = q * cs[k] - p * sn[k];
-          }
+        for (int i = 0; i < N; ++i) {
+          x[i] = (float)xn[j][i];
+          g[i] = fmaf((float)gn[j][i], c[i], -(float)other[i] * s[i]);
         }
         if (a.eps >= 0.0f) {
           float q = 0.0f, m = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) q = fmaf(x[j][i], x[j][i], q);
+          for (int i = 0; i < N; ++i) q = fmaf(x[i], x[i], q);
           const float r = 1.0f / sqrtf(fmaf(sum_lanes(q, a.lg), mean, a.eps));
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            x[j][i] *= r;
-            const float d = g[j][i] * x[j][i];
-            if (here) dg[0][i] += t ? 0.0f : d, dg[1][i] += t ? d : 0.0f;
-            g[j][i] *= t ? gam[1][i] : gam[0][i];
-            m = fmaf(g[j][i], x[j][i], m);
+          for (int i = 0; i < N; ++i) {
+            x[i] *= r;
+            const float d = g[i] * x[i];
+            dg[0][i] += t ? 0.0f : d, dg[1][i] += t ? d : 0.0f;
+            g[i] *= t ? gam[1][i] : gam[0][i];
+            m = fmaf(g[i], x[i], m);
           }
           m = sum_lanes(m, a.lg) * mean;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) g[j][i] = r * (g[j][i] - x[j][i] * m);
+          for (int i = 0; i < N; ++i) g[i] = r * (g[i] - x[i] * m);
         }
-        if (here) store8<T, FORM>(g[j], (T*)a.y[t] + row * a.ldy[t] + at, a, lane);
+        if (on && hh < c1)
+          store_piece((T*)a.y[t] + row * a.ldy[t] + (int64_t)(hh - (t ? a.heads[0] : 0)) * a.hd + lane * N, g);
       }
     }
   }
@@ -259,24 +287,33 @@ __global__ __launch_bounds__(RT) void k_rotate_bwd(RotArgs a) {
   for (int t = 0; t < 2; ++t) {
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sh[(int)threadIdx.x * 8 + i] = dg[t][i];
+    for (int i = 0; i < N; ++i) shf[(int)threadIdx.x * N + i] = dg[t][i];
     __syncthreads();
-    for (int e = (int)threadIdx.x; e < 8 * a.lanes; e += RT) {
+    for (int e = (int)threadIdx.x; e < a.hd; e += RT) {
       float sum = 0.0f;
-      for (int g = 0; g < groups; ++g) sum += sh[(g << a.lg) * 8 + e];
-      a.part[((int64_t)blockIdx.x * 2 + t) * a.hd + value_at<FORM>(a, e >> 3, e & 7)] = sum;
+      for (int g = 0; g < groups; ++g) sum += shf[(g << a.lg) * N + e];
+      a.part[((int64_t)blockIdx.x * 2 + t) * a.hd + e] = sum;
     }
   }
 }
 
-// dgamma: a wave to a value; the parts are added up in a fixed order, in float64
-__global__ __launch_bounds__(64) void k_rotate_columns(RotArgs a) {
-  const int t = (int)blockIdx.x / a.hd, e = (int)blockIdx.x % a.hd;
-  if (!a.dgamma[t]) return;
+// dgamma: sixteen values to a workgroup, each from sixteen slices of the parts, which are
+// added up in a fixed order, in float64.
+__global__ __launch_bounds__(RT) void k_rotate_columns(RotArgs a) {
+  __shared__ double sh[RT];
+  const int e = (int)blockIdx.x * 16 + ((int)threadIdx.x & 15), slice = (int)threadIdx.x >> 4, columns = 2 * a.hd;
   double sum = 0.0;
-  for (int p = (int)threadIdx.x; p < a.parts; p += 64) sum += (double)a.part[((int64_t)p * 2 + t) * a.hd + e];
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-  if (threadIdx.x == 0) a.dgamma[t][e] = (float)(sum + (a.accumulate ? (double)a.dgamma[t][e] : 0.0));
+#pragma unroll 8
+  for (int p = slice; p < a.parts; p += 16) sum += (double)a.part[(int64_t)p * columns + e];
+  sh[threadIdx.x] = sum;
+  __syncthreads();
+  if (slice) return;
+  sum = 0.0;
+  for (int k = 0; k < 16; ++k) sum += sh[16 * k + threadIdx.x];
+  float* out = a.dgamma[e >= a.hd];
+  if (!out) return;
+  out += e >= a.hd ? e - a.hd : e;
+  *out = (float)(sum + (a.accumulate ? (double)*out : 0.0));
 }
 
 dsmp_status check_rotate(dsmp_handle* h, const dsmp_rotate_desc* d, int64_t n) {
@@ -306,7 +343,8 @@ void place(RotArgs& a, const dsmp_rotate_desc& d, int64_t n) {
   a.n = n;
   a.hd = d.head_dim, a.rot = d.rot, a.axes = d.axes;
   a.per_axis = d.rot ? d.rot / 2 / d.axes : 1;
-  a.lanes = d.head_dim / 8;
+  a.lanes = d.head_dim * (d.dtype == DSMP_BF16 ? 2 : 4) / 16;
+  a.interleaved = d.layout == DSMP_ROTATE_INTERLEAVED;
   a.lg = 0;
   while ((1 << a.lg) < a.lanes) ++a.lg;
   a.eps = d.norm ? d.eps : -1.0f, a.amp = d.amplitude;
@@ -317,23 +355,22 @@ void place(RotArgs& a, const dsmp_rotate_desc& d, int64_t n) {
   a.chunks = (int)ceil_div(all, a.per);
 }
 
-int form_of(const dsmp_rotate_desc& d) {
-  if (d.layout == DSMP_ROTATE_INTERLEAVED || d.rot == 0) return EIGHT;
-  return d.rot % 8 == 0 ? SPLIT : PAIRS;
-}
-
 int bwd_parts(const RotArgs& a) {
   return (int)std::min<int64_t>(MAX_PARTS, ceil_div(a.n * a.chunks, rot_items_per_wg(a)));
 }
 
+// Calls f with the type and the largest piece whose partners are together.
 template <typename F>
-void by_form(int dtype, int form, F f) {
+void by_form(const dsmp_rotate_desc& d, F f) {
+  const int half = d.layout == DSMP_ROTATE_INTERLEAVED || d.rot == 0 ? 0 : d.rot / 2;
   auto go = [&](auto t) {
-    if (form == EIGHT) f(t, std::integral_constant<int, EIGHT>{});
-    else if (form == SPLIT) f(t, std::integral_constant<int, SPLIT>{});
-    else f(t, std::integral_constant<int, PAIRS>{});
+    if (half == 0) f(t, std::integral_constant<int, 0>{});
+    else if (sizeof(t) == 2 && half % 8 == 0) f(t, std::integral_constant<int, sizeof(t) == 2 ? 8 : 4>{});
+    else if (half % 4 == 0) f(t, std::integral_constant<int, 4>{});
+    else if (half % 2 == 0) f(t, std::integral_constant<int, 2>{});
+    else f(t, std::integral_constant<int, 1>{});
   };
-  if (dtype == DSMP_BF16) go(__bf16{});
+  if (d.dtype == DSMP_BF16) go(__bf16{});
   else go(float{});
 }
 
@@ -364,7 +401,7 @@ extern "C" dsmp_status dsmp_qk_rotate_forward(dsmp_handle* h, const dsmp_rotate_
   DSMP_CHECK(h, grid < (int64_t)1 << 24, DSMP_UNSUPPORTED, "too many rows for one call");
   DeviceScope dev(h);
   ProfScope prof(h, DSMP_K_ROTATE);
-  by_form(desc->dtype, form_of(*desc), [&](auto t, auto form) {
+  by_form(*desc, [&](auto t, auto form) {
     hipLaunchKernelGGL((k_rotate<decltype(t), decltype(form)::value>), dim3((unsigned)grid), dim3(RT), 0, h->stream, a);
   });
   DSMP_LAUNCHED(h, "rotation");
@@ -422,11 +459,11 @@ extern "C" dsmp_status dsmp_qk_rotate_backward(dsmp_handle* h, const dsmp_rotate
   ProfScope prof(h, DSMP_K_ROTATE);
   if (n > 0) {
     a.parts = bwd_parts(a);
-    by_form(desc->dtype, form_of(*desc), [&](auto t, auto form) {
+    by_form(*desc, [&](auto t, auto form) {
       hipLaunchKernelGGL((k_rotate_bwd<decltype(t), decltype(form)::value>), dim3(a.parts), dim3(RT), 0, h->stream, a);
     });
   }
-  if (sums) hipLaunchKernelGGL(k_rotate_columns, dim3(2 * a.hd), dim3(64), 0, h->stream, a);
+  if (sums) hipLaunchKernelGGL(k_rotate_columns, dim3(a.hd / 8), dim3(RT), 0, h->stream, a);
   DSMP_LAUNCHED(h, "rotation backward");
   return DSMP_OK;
 }
