@@ -115,7 +115,7 @@ template <>
 __device__ __forceinline__ f32x8 lds_columns<float>(lds_u8* X, int pitch, int r0, int c0) {
   const int l = threadIdx.x & 63;
   uint32_t at = (uint32_t)(uintptr_t)(X + (r0 + 4 * (l >> 5)) * pitch + (c0 + (l & 31)) * 4);
-  asm volatile("" : "+v"(at));   // as above
+  asm volatile("" : "+v"(at));   // as in lds_rows
   lds_u8* p = (lds_u8*)(uintptr_t)at;
   f32x8 f;
 #pragma unroll
@@ -207,13 +207,28 @@ struct AttnArgs {
   int64_t ldout, ldgq, ldgk, ldgv;
   const float *pos_q, *pos_k, *slopes;
   const float* lse_in;
-  float *lse, *delta, *part;
+  float *lse, *delta, *part;   // part: of out, or of dq
   Bounds qb, kb;
-  int n_seg, H, Hk, G, hd, dim, splits;
+  int n_seg, H, Hk, G, hd, dim, splits, splits_k;
+  unsigned dq_groups;    // of a launch for both gradients: the first ones are for dq
+  float *part_k, *part_v;
   uint32_t g_inv;        // ceil(2^20 / G): x / G = x g_inv >> 20 for x < 512
   float scale, cap;      // of the scores as they are
-  int64_t nq;
+  int64_t nq, nk;
 };
+
+// A lane's row of a workgroup's tile: row = query G + head of the key head's group.
+struct RowOf {
+  int64_t query;
+  int head;
+  bool there;
+};
+__device__ __forceinline__ RowOf row_of(const AttnArgs& a, int64_t q0, int64_t r0, int64_t R, int kvh, bool few, int tid) {
+  const int64_t r = r0 + (few ? 0 : 32 * (tid >> 6)) + (tid & 31);
+  const bool there = r < R;
+  const unsigned q = there ? (unsigned)r / (unsigned)a.G : 0u, g = there ? (unsigned)r - q * a.G : 0u;
+  return {q0 + q, kvh * a.G + (int)g, there};
+}
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -251,16 +266,6 @@ __device__ __forceinline__ float distance(int dim, const Place& a, float x, floa
   return __builtin_amdgcn_sqrtf(d);
 }
 
-// Constants of the score in powers of two.
-struct ScoreConst {
-  float scale2;   // scale log2(e)
-  float turn;     // 2 log2(e) scale / cap
-  float cap2;     // cap log2(e)
-};
-__device__ __forceinline__ ScoreConst score_const(const AttnArgs& a) {
-  return {a.scale * LOG2E, a.cap > 0.0f ? 2.0f * LOG2E * a.scale / a.cap : 0.0f, a.cap * LOG2E};
-}
-
 // tanh for float32 scores, within about 3 u of it: 1 - 2 / (1 + e^2x), whose difference costs
 // digits near zero, where the series to x^11 takes its place (its next term is 2^-26 of x at 0.35).
 __device__ __forceinline__ float tanh_of(float x) {
@@ -272,23 +277,46 @@ __device__ __forceinline__ float tanh_of(float x) {
   return fabsf(x) < 0.35f ? fmaf(x * s, p, x) : far;
 }
 
-// log2(e) times the score without its bias; `fall` receives 1 - tanh^2.
-// tanh x = 1 - 2 r with r = 1 / (1 + e^2x); 1 - tanh^2 x = 4 r (1 - r).  The difference from 1 leaves an
-// absolute error of about 2^-23 in tanh, which bfloat16 operands hide.
-template <typename T, bool SLOPE>
-__device__ __forceinline__ float capped(float s, bool cap, const ScoreConst& c, float* fall) {
-  if (!cap) {
-    if (SLOPE) *fall = 1.0f;
-    return s * c.scale2;
+// A score is formed as u with z log2(e) = A u + C, so that e^(z - b) is one fma and one power:
+//   no cap              u = x - (slope / scale) d,      A = scale log2(e),    C = 0
+//   cap, bfloat16       u = -r - (slope / 2 cap) d,     A = 2 cap log2(e),    C = cap log2(e)
+//   cap, float32        u = tanh - (slope / cap) d,     A = cap log2(e),      C = 0
+// x = q.k, d the distance, r = 1 / (1 + e^(2 scale x / cap)): tanh = 1 - 2 r, whose absolute error of about
+// 2^-23 bfloat16 operands hide, and 1 - tanh^2 = 4 r (1 - r).  A is positive: a negative scale goes into
+// the sign of one operand of x, and a scale of 0 makes that operand 0 (`sign`).
+template <typename T>
+struct Score {
+  float A, C, turn, per_slope, sign;
+  __device__ __forceinline__ Score(const AttnArgs& a, bool cap) {
+    sign = a.scale > 0.0f ? 1.0f : a.scale < 0.0f ? -1.0f : 0.0f;
+    const float scale = a.scale == 0.0f ? 1.0f : fabsf(a.scale);
+    const float unit = !cap ? scale : sizeof(T) == 4 ? a.cap : 2.0f * a.cap;
+    A = unit * LOG2E;
+    per_slope = 1.0f / unit;
+    C = cap && sizeof(T) == 2 ? a.cap * LOG2E : 0.0f;
+    turn = !cap ? 0.0f : sizeof(T) == 4 ? scale / a.cap : 2.0f * LOG2E * scale / a.cap;
   }
-  if (sizeof(T) == 4) {
-    const float t = tanh_of(s * c.turn * (0.5f * LN2));
-    if (SLOPE) *fall = 1.0f - t * t;
-    return c.cap2 * t;
+  // u without its bias; `fall` receives 1 - tanh^2
+  template <bool SLOPE>
+  __device__ __forceinline__ float u(float x, bool cap, float* fall) const {
+    if (!cap) return x;
+    if (sizeof(T) == 4) {
+      const float t = tanh_of(x * turn);
+      if (SLOPE) *fall = 1.0f - t * t;
+      return t;
+    }
+    const float r = __builtin_amdgcn_rcpf(1.0f + exp2_of(x * turn));
+    if (SLOPE) *fall = 4.0f * r * (1.0f - r);
+    return -r;
   }
-  const float r = __builtin_amdgcn_rcpf(1.0f + exp2_of(s * c.turn));
-  if (SLOPE) *fall = 4.0f * r * (1.0f - r);
-  return fmaf(-2.0f * c.cap2, r, c.cap2);
+};
+
+// An operand of x with the score's sign.
+template <typename F>
+__device__ __forceinline__ void apply_sign(F& f, float sign) {
+  if (sign == 1.0f) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = sign == 0.0f ? 0.0f : -(float)f[e];
 }
 
 inline AttnArgs attn_args(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks) {
@@ -299,8 +327,8 @@ inline AttnArgs attn_args(const dsmp_attention_desc& d, const dsmp_segments& qs,
   a.H = d.heads, a.Hk = d.kv_heads, a.G = d.heads / d.kv_heads, a.hd = d.head_dim, a.dim = d.dim;
   a.g_inv = ((1u << 20) + a.G - 1) / a.G;
   a.scale = d.scale, a.cap = d.cap;
-  a.nq = qs.n;
-  a.splits = 1;
+  a.nq = qs.n, a.nk = ks.n;
+  a.splits = a.splits_k = 1;
   return a;
 }
 
@@ -323,8 +351,9 @@ void by_attention(const dsmp_attention_desc& d, F f) {
 // Workgroups of 256 threads that fill the card (256 CUs) twice; a launch has fewer than 2^32 threads.
 constexpr int64_t FILL = 512, MAX_GROUPS = ((int64_t)1 << 24) - 1;
 
+size_t attention_bwd_bytes(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks);
 dsmp_status check_attention(dsmp_handle* h, const dsmp_attention_desc* d, const dsmp_segments* qs, const dsmp_segments* ks);
-dsmp_status launch_attention_dq(dsmp_handle* h, const dsmp_attention_desc& d, AttnArgs a);
-dsmp_status launch_attention_dkv(dsmp_handle* h, const dsmp_attention_desc& d, AttnArgs a, int64_t nk);
+void launch_attention_dq(dsmp_handle* h, const dsmp_attention_desc& d, const AttnArgs& a, int64_t grid);
+void launch_attention_dkv(dsmp_handle* h, const dsmp_attention_desc& d, const AttnArgs& a, int64_t grid);
 
 }  // namespace dsmp

@@ -1,0 +1,141 @@
+// Attention backward: the call, and its kernels for few rows and keys.
+#include "attn_bwd.hpp"
+
+using namespace dsmp;
+
+namespace {
+
+// Both gradients in one launch, for tiles of 32 rows or keys: the first dq_groups workgroups
+// take those of the queries, the others those of the keys, which form D_i of their rows
+// themselves and so wait for nobody.
+template <typename T, int D, typename M>
+__global__ __launch_bounds__(BT, D == 128 || (D == 64 && sizeof(T) == 4) ? 1 : 2) void k_attn_bwd_few(AttnArgs a) {
+  constexpr int LQ = Bwd<T, D, true, false>::LDS, LK = Bwd<T, D, true, true>::LDS;
+  __shared__ __align__(16) unsigned char smem[LQ > LK ? LQ : LK];
+  if (blockIdx.x < a.dq_groups) dq_tile<T, D, true, M>(a, smem, blockIdx.x);
+  else dkv_tile<T, D, true, M>(a, smem, blockIdx.x - a.dq_groups);
+}
+
+// The splits of the gradients added up in their order, four values to a thread: those of dq, then
+// of dk, then of dv (where there is more than one of each).
+template <typename T>
+__global__ __launch_bounds__(BT) void k_attn_bwd_join(AttnArgs a) {
+  const int64_t nq = a.splits > 1 ? a.nq * a.H * a.hd / 4 : 0, nk = a.splits_k > 1 ? a.nk * a.Hk * a.hd / 4 : 0;
+  int64_t i = (int64_t)blockIdx.x * BT + threadIdx.x;
+  const int which = i < nq ? 0 : i < nq + nk ? 1 : 2;
+  i -= which == 0 ? 0 : which == 1 ? nq : nq + nk;
+  if (which == 2 && i >= nk) return;
+  const int width = (which ? a.Hk : a.H) * a.hd, splits = which ? a.splits_k : a.splits;
+  const int64_t row = 4 * i / width, step = 4 * (which ? nk : nq);
+  const Bounds& b = which ? a.kb : a.qb;
+  if (row < b.at(0) || row >= b.at(a.n_seg)) return;
+  const float* from = (which == 0 ? a.part : which == 1 ? a.part_k : a.part_v) + 4 * i;
+  float4 v = *(const float4*)from;
+#pragma unroll 4
+  for (int s = 1; s < splits; ++s) {
+    const float4 x = *(const float4*)(from + s * step);
+    v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+  }
+  T* out = (T*)(which == 0 ? a.gq : which == 1 ? a.gk : a.gv) + row * (which == 0 ? a.ldgq : which == 1 ? a.ldgk : a.ldgv);
+  store4(out + (4 * i - row * width), v.x, v.y, v.z, v.w);
+}
+
+struct BwdPlan {
+  bool wide_q, wide_k;
+  int splits_q, splits_k;
+  int64_t grid_q, grid_k;
+};
+
+// Rows and keys each in tiles of 128 where these fill the card, else of 32, and where these are
+// few as well cut over the other side, 256 of it to a workgroup at least.
+BwdPlan bwd_plan(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks) {
+  const int G = d.heads / d.kv_heads;
+  BwdPlan p{false, false, 1, 1, tiles_of(qs.n, qs.n_seg, G, 32 * BW) * d.kv_heads, tiles_of(ks.n, ks.n_seg, 1, 32 * BW) * d.kv_heads};
+  p.wide_q = p.grid_q >= FILL, p.wide_k = p.grid_k >= FILL;
+  if (!p.wide_q) p.grid_q = tiles_of(qs.n, qs.n_seg, G, 32) * d.kv_heads;
+  if (!p.wide_k) p.grid_k = tiles_of(ks.n, ks.n_seg, 1, 32) * d.kv_heads;
+  auto splits = [](int64_t grid, int64_t along) {
+    return grid >= FILL ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(FILL / grid, along / 256));
+  };
+  if (!p.wide_q) p.splits_q = splits(p.grid_q, ks.n / ks.n_seg);
+  if (!p.wide_k) p.splits_k = splits(p.grid_k, qs.n / qs.n_seg * G);
+  p.grid_q *= p.splits_q, p.grid_k *= p.splits_k;
+  if (qs.n == 0) p.grid_q = 0;
+  if (ks.n == 0) p.grid_k = 0;
+  return p;
+}
+
+struct BwdWs {
+  float *delta, *q, *k, *v;
+  size_t total;
+};
+
+BwdWs bwd_ws(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks, void* ws) {
+  const BwdPlan p = bwd_plan(d, qs, ks);
+  Carve cv(ws);
+  BwdWs w{};
+  w.delta = cv.take<float>((size_t)qs.n * d.heads);
+  const size_t of_q = p.splits_q > 1 ? (size_t)p.splits_q * qs.n * d.heads * d.head_dim : 0;
+  const size_t of_k = p.splits_k > 1 ? (size_t)p.splits_k * ks.n * d.kv_heads * d.head_dim : 0;
+  w.q = cv.take<float>(of_q), w.k = cv.take<float>(of_k), w.v = cv.take<float>(of_k);
+  w.total = cv.used();
+  return w;
+}
+
+}  // namespace
+
+namespace dsmp {
+
+size_t attention_bwd_bytes(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks) {
+  return bwd_ws(d, qs, ks, nullptr).total;
+}
+
+}  // namespace dsmp
+
+extern "C" dsmp_status dsmp_attention_backward(dsmp_handle* h, const dsmp_attention_desc* desc, const dsmp_segments* qs,
+                                               const dsmp_segments* ks, const void* q, int64_t ldq, const void* k,
+                                               int64_t ldk, const void* v, int64_t ldv, const float* pos_q,
+                                               const float* pos_k, const float* slopes, const void* out, int64_t ldo,
+                                               const float* lse, const void* grad_out, int64_t ldgo, void* grad_q,
+                                               int64_t ldgq, void* grad_k, int64_t ldgk, void* grad_v, int64_t ldgv,
+                                               void* ws, size_t ws_bytes) {
+  if (!h) return DSMP_INVALID_ARG;
+  dsmp_status st = check_attention(h, desc, qs, ks);
+  if (st != DSMP_OK) return st;
+  DSMP_CHECK(h, (qs->n == 0 || (q && out && lse && grad_out && grad_q)) && (ks->n == 0 || (k && v && grad_k && grad_v)),
+             DSMP_INVALID_ARG, "a data pointer is NULL");
+  DSMP_CHECK(h, desc->dim == 0 || (slopes && (qs->n == 0 || pos_q) && (ks->n == 0 || pos_k)), DSMP_INVALID_ARG,
+             "coordinates and slopes are needed");
+  const int es = desc->dtype == DSMP_BF16 ? 2 : 4, wq = desc->heads * desc->head_dim, wk = desc->kv_heads * desc->head_dim;
+  st = check_matrices(h, es, {{q, ldq, wq, "q"}, {k, ldk, wk, "k"}, {v, ldv, wk, "v"}, {out, ldo, wq, "out"},
+                              {grad_out, ldgo, wq, "grad_out"}, {grad_q, ldgq, wq, "grad_q"},
+                              {grad_k, ldgk, wk, "grad_k"}, {grad_v, ldgv, wk, "grad_v"}});
+  if (st != DSMP_OK) return st;
+  const BwdWs w = bwd_ws(*desc, *qs, *ks, ws);
+  DSMP_CHECK(h, !w.total || (ws && ws_bytes >= w.total), DSMP_WORKSPACE_TOO_SMALL, "workspace needs %zu bytes", w.total);
+  DSMP_CHECK(h, reinterpret_cast<uintptr_t>(ws) % 16 == 0, DSMP_INVALID_ARG, "the workspace must be 16-byte aligned");
+  const BwdPlan p = bwd_plan(*desc, *qs, *ks);
+  AttnArgs a = attn_args(*desc, *qs, *ks);
+  a.q = q, a.ldq = ldq, a.k = k, a.ldk = ldk, a.v = v, a.ldv = ldv, a.o = out, a.ldo = ldo, a.go = grad_out, a.ldgo = ldgo;
+  a.gq = grad_q, a.ldgq = ldgq, a.gk = grad_k, a.ldgk = ldgk, a.gv = grad_v, a.ldgv = ldgv;
+  a.lse_in = lse, a.delta = w.delta, a.part = w.q, a.part_k = w.k, a.part_v = w.v;
+  a.splits = p.splits_q, a.splits_k = p.splits_k;
+  a.pos_q = pos_q, a.pos_k = pos_k, a.slopes = slopes;
+  DeviceScope dev(h);
+  ProfScope prof(h, DSMP_K_ATTN_BWD);
+  // a launch for keys in wide tiles reads what the queries' has written
+  if (p.wide_q && p.grid_q) launch_attention_dq(h, *desc, a, p.grid_q);
+  const int64_t few_q = p.wide_q ? 0 : p.grid_q, few_k = p.wide_k ? 0 : p.grid_k;
+  a.dq_groups = (unsigned)few_q;
+  const int64_t joined = ((p.splits_q > 1 ? qs->n * wq : 0) + (p.splits_k > 1 ? 2 * ks->n * wk : 0)) / 4;
+  by_attention(*desc, [&](auto t, auto width, auto mode) {
+    using T = decltype(t);
+    if (few_q + few_k)
+      hipLaunchKernelGGL((k_attn_bwd_few<T, decltype(width)::value, decltype(mode)>), dim3((unsigned)(few_q + few_k)), dim3(BT), 0,
+                         h->stream, a);
+    if (joined) hipLaunchKernelGGL((k_attn_bwd_join<T>), dim3(ceil_div(joined, BT)), dim3(BT), 0, h->stream, a);
+  });
+  if (p.wide_k && p.grid_k) launch_attention_dkv(h, *desc, a, p.grid_k);
+  DSMP_LAUNCHED(h, "attention backward");
+  return DSMP_OK;
+}

@@ -1,0 +1,446 @@
+// Attention within packed segments, backward: what a workgroup does for the gradients of the
+// queries (dq_tile) and for those of the keys and values (dkv_tile).
+//
+//   P_ij = e^(z_ij - lse_i),  D_i = dO_i . o_i,  dS_ij = P_ij (dO_i . v_j - D_i) (1 - tanh^2)
+//   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dO_i
+//
+// Neither has atomics: a workgroup owns its rows or its keys and keeps their sums in registers.
+// P and dS are so formed in both (two products of seven), which sums over workgroups in a
+// fixed order would cost in memory instead.  The gradients of shared key heads add up in the
+// accumulators: the rows of a key head are the queries times the G heads that share it.
+#pragma once
+
+#include "attention.hpp"
+
+namespace dsmp {
+
+constexpr int BT = 256, BW = 4;   // threads and waves of a workgroup
+
+// WIDE: 32 rows (or keys) to a wave, 128 to a workgroup, all keys (rows) of a tile to every wave.
+// FEW: 32 to a workgroup, a quarter of a tile's keys (rows) to each wave; joined at the end.
+// KEYS_OWNED: dkv_tile, whose two streamed matrices are both read both ways.
+template <typename T, int D, bool FEW, bool KEYS_OWNED>
+struct Bwd {
+  static constexpr int OWN = FEW ? 32 : 32 * BW;
+  static constexpr int BN = FEW ? 32 * BW : sizeof(T) == 2 ? 64 : 32;
+  static constexpr int SUB = FEW ? 1 : BN / 32;
+  static constexpr int P0 = pitch_of<T, D, false>(), P1 = pitch_of<T, D, !KEYS_OWNED>();
+  static constexpr int PER = BN * D * (int)sizeof(T) / 16 / BT, STEP = BT * 16 / (D * (int)sizeof(T));
+  // the next tile waits in registers, but for FEW's large ones in float32: those come two units at a time
+  static constexpr bool AHEAD = !(FEW && sizeof(T) == 4 && D == 128);
+  static constexpr int HELD = AHEAD || PER < 2 ? PER : 2;
+  static constexpr int EXTRA = KEYS_OWNED ? 6 : 3;   // float32 of a row that go along
+  static constexpr int TILE = BN * (P0 + P1) + EXTRA * BN * 4;
+  static constexpr int JOIN = FEW ? BW * 32 * D * 4 : 0;
+  static constexpr int LDS = TILE > JOIN ? TILE : JOIN;
+  static_assert(PER >= 1 && PER * BT * 16 == BN * D * (int)sizeof(T), "whole units for every thread");
+};
+
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+
+// A wave's 32 rows of results (D values each, a lane's column), scaled: to `out`, or in float32 to `part`.
+template <typename T, int D>
+__device__ __forceinline__ void write_rows(const f32x16* acc, float scale, T* out, float* part, int hd) {
+  const int h = ((int)threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      const int c = 32 * d + 8 * i4 + 4 * h;
+      if (c >= hd) continue;
+      const float v[4] = {acc[d][4 * i4] * scale, acc[d][4 * i4 + 1] * scale, acc[d][4 * i4 + 2] * scale, acc[d][4 * i4 + 3] * scale};
+      if (part) *(float4*)(part + c) = make_float4(v[0], v[1], v[2], v[3]);
+      else store4(out + c, v[0], v[1], v[2], v[3]);
+    }
+}
+
+// The four waves' results of the same 32 rows added up in LDS ([wave][value][row]) and written:
+// 256 threads with a row and four values in 32 each.
+template <typename T, int D>
+__device__ __forceinline__ void join_rows(const f32x16* acc, float* join, float scale, T* out, float* part, int hd, bool there) {
+  const int tid = (int)threadIdx.x, l = tid & 63, w = tid >> 6;
+  __syncthreads();
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) join[(w * D + 32 * d + result_row(i)) * 32 + (l & 31)] = acc[d][i];
+  __syncthreads();
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) {
+    const int c = 32 * d + 4 * (tid >> 5);
+    if (c >= hd || !there) continue;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < BW; ++k) v[e] += join[(k * D + c + e) * 32 + (l & 31)];
+      v[e] *= scale;
+    }
+    if (part) *(float4*)(part + c) = make_float4(v[0], v[1], v[2], v[3]);
+    else store4(out + c, v[0], v[1], v[2], v[3]);
+  }
+}
+
+template <typename T, int D, bool FEW, typename M>
+__device__ __forceinline__ void dq_tile(const AttnArgs& a, unsigned char* smem, unsigned group) {
+  using C = Bwd<T, D, FEW, false>;
+  constexpr int ES = sizeof(T), KS = D / 16, DB = D / 32;
+  typedef typename Frag<T>::type frag;
+  lds_u8* ldsK = (lds_u8*)smem;
+  lds_u8* ldsV = ldsK + C::BN * C::P0;
+  float* places = (float*)(smem + C::BN * (C::P0 + C::P1));
+
+  const int tid = (int)threadIdx.x, l = tid & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kvh = (int)(group % (unsigned)a.Hk);
+  const unsigned rest = group / (unsigned)a.Hk;
+  const int split = FEW ? (int)(rest % (unsigned)a.splits) : 0;
+  const int64_t tile = FEW ? rest / (unsigned)a.splits : rest;
+  int64_t first;
+  const int seg = find_segment(a.qb, a.n_seg, a.G, C::OWN, tile, &first);
+  const int64_t q0 = a.qb.at(seg), R = (a.qb.at(seg + 1) - q0) * a.G, r0 = (tile - first) * C::OWN;
+  if (tile < first || r0 >= R) return;
+  const int64_t k0 = a.kb.at(seg), klen = a.kb.at(seg + 1) - k0;
+  const int tiles = klen > 0 ? (int)((klen + C::BN - 1) / C::BN) : 0;
+  const int per = FEW ? (tiles + a.splits - 1) / a.splits : tiles;
+  const int t_begin = min(split * per, tiles), t_end = min(t_begin + per, tiles);
+
+  const bool cap = M::cap(a);
+  const int dim = M::dim(a);
+  const Score<T> sc(a, cap);
+  const RowOf row = row_of(a, q0, r0, R, kvh, FEW, tid);
+  const int64_t slot = row.query * a.H + row.head;
+  frag qf[KS], gf[KS];
+  float delta = 0.0f;
+#pragma unroll
+  for (int t = 0; t < KS; ++t) {
+    const int c = 16 * t + 8 * h;
+    const bool in = row.there && c < a.hd;
+    qf[t] = read_frag<T>((const T*)a.q + row.query * a.ldq + row.head * a.hd + c, in);
+    gf[t] = read_frag<T>((const T*)a.go + row.query * a.ldgo + row.head * a.hd + c, in);
+    const frag of = read_frag<T>((const T*)a.o + row.query * a.ldo + row.head * a.hd + c, in);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[t][e], (float)of[e], delta);
+    apply_sign(qf[t], sc.sign);
+  }
+  delta += other_half(delta);
+  if (row.there && h == 0 && split == 0 && (!FEW || w == 0)) a.delta[slot] = delta;
+  // the exponent of a weight is A u + shift; a row without keys has the weights 0
+  const float lse = row.there ? a.lse_in[slot] : INFINITY, shift = lse == -INFINITY ? -INFINITY : sc.C - lse * LOG2E;
+  Place me{0.0f, 0.0f, 0.0f};
+  float slope = 0.0f;
+  if (dim && a.dim && row.there) me = place_of(a.pos_q, a.dim, row.query), slope = a.slopes[row.head] * sc.per_slope;
+
+  const int row0 = tid / (D * ES / 16), c0 = tid % (D * ES / 16) * 16;
+  const bool in = c0 < a.hd * ES;
+  const uint32_t offK = in ? (uint32_t)(row0 * a.ldk * ES + c0) : NOWHERE, stepK = (uint32_t)(C::STEP * a.ldk * ES);
+  const uint32_t offV = in ? (uint32_t)(row0 * a.ldv * ES + c0) : NOWHERE, stepV = (uint32_t)(C::STEP * a.ldv * ES);
+  u32x4 regK[C::HELD], regV[C::HELD];
+  Place key{0.0f, 0.0f, 0.0f};
+  auto fetch = [&](int t, int i0) {
+    const int64_t j0 = k0 + (int64_t)t * C::BN;
+    const int rem = (int)min((int64_t)C::BN, klen - (int64_t)t * C::BN);
+    const auto bk = buffer_of((const T*)a.k + j0 * a.ldk + kvh * a.hd, (uint32_t)(rem * a.ldk * ES));
+    const auto bv = buffer_of((const T*)a.v + j0 * a.ldv + kvh * a.hd, (uint32_t)(rem * a.ldv * ES));
+#pragma unroll
+    for (int i = 0; i < C::HELD; ++i)
+      regK[i] = buffer_read(bk, offK + (i0 + i) * stepK), regV[i] = buffer_read(bv, offV + (i0 + i) * stepV);
+    if (dim && a.dim && i0 == 0 && tid < rem) key = place_of(a.pos_k, a.dim, j0 + tid);
+  };
+  auto put = [&](int i0) {
+#pragma unroll
+    for (int i = 0; i < C::HELD; ++i) {
+      const int r = row0 + (i0 + i) * C::STEP;
+      *(lds_u32x4*)(ldsK + r * C::P0 + c0) = regK[i];
+      *(lds_u32x4*)(ldsV + r * C::P1 + c0) = regV[i];
+    }
+    if (dim && i0 == 0 && tid < C::BN) places[tid] = key.x, places[C::BN + tid] = key.y, places[2 * C::BN + tid] = key.z;
+  };
+
+  f32x16 acc[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) acc[d] = f32x16{};
+
+  if (C::AHEAD && t_begin < t_end) fetch(t_begin, 0);
+  for (int t = t_begin; t < t_end; ++t) {
+    __syncthreads();
+    if (C::AHEAD) {
+      put(0);
+    } else {
+#pragma unroll 1
+      for (int i0 = 0; i0 < C::PER; i0 += C::HELD) fetch(t, i0), put(i0);
+    }
+    __syncthreads();
+    if (C::AHEAD && t + 1 < t_end) fetch(t + 1, 0);
+    const int rem = (int)min((int64_t)C::BN, klen - (int64_t)t * C::BN);
+    if (FEW && 32 * w >= rem) continue;
+#pragma unroll
+    for (int b = 0; b < C::SUB; ++b) {
+      const int at = 32 * ((FEW ? w : 0) + b);
+      // fragments one step ahead of their products, as in the forward pass
+      f32x16 x{}, dp;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) dp[i] = -delta;
+      frag kf[2], vf[2];
+      kf[0] = lds_rows<T>(ldsK, C::P0, at, 0), vf[0] = lds_rows<T>(ldsV, C::P1, at, 0);
+#pragma unroll
+      for (int t2 = 0; t2 < KS; ++t2) {
+        if (t2 + 1 < KS)
+          kf[(t2 + 1) & 1] = lds_rows<T>(ldsK, C::P0, at, 16 * (t2 + 1)), vf[(t2 + 1) & 1] = lds_rows<T>(ldsV, C::P1, at, 16 * (t2 + 1));
+        x = mma(kf[t2 & 1], qf[t2], x);
+        dp = mma(vf[t2 & 1], gf[t2], dp);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        float4 px{}, py{}, pz{};
+        if (dim) {
+          const float* p = places + at + 8 * i4 + 4 * h;
+          px = *(const float4*)p, py = *(const float4*)(p + C::BN);
+          if (dim > 2) pz = *(const float4*)(p + 2 * C::BN);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = 4 * i4 + e;
+          float fall;
+          float u = sc.template u<true>(x[i], cap, &fall);
+          if (dim) u = fmaf(-slope, distance(dim, me, (&px.x)[e], (&py.x)[e], (&pz.x)[e]), u);
+          x[i] = exp2_of(fmaf(u, sc.A, shift)) * dp[i];
+          if (cap) x[i] *= fall;
+        }
+      }
+      if (at + 32 > rem) {   // behind the last key
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (at + result_row(i) >= rem) x[i] = 0.0f;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      frag cf[2][DB];
+#pragma unroll
+      for (int d = 0; d < DB; ++d) cf[0][d] = lds_columns<T>(ldsK, C::P0, at, 32 * d);
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = x[8 * t2 + i];
+        const frag f = to_frag<T>(v);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          if (t2 == 0) cf[1][d] = lds_columns<T>(ldsK, C::P0, at + 16, 32 * d);
+          acc[d] = mma(cf[t2][d], f, acc[d]);
+        }
+      }
+    }
+  }
+
+  int again = tid;   // the row once more: formed here, not kept in registers over the loop
+  asm volatile("" : "+v"(again));
+  const RowOf mine = row_of(a, q0, r0, R, kvh, FEW, again);
+  T* out = (T*)a.gq + mine.query * a.ldgq + mine.head * a.hd;
+  float* part = FEW && a.splits > 1 ? a.part + ((int64_t)split * a.nq * a.H + mine.query * a.H + mine.head) * a.hd : nullptr;
+  if (FEW) join_rows<T, D>(acc, (float*)smem, a.scale, out, part, a.hd, mine.there);
+  else if (mine.there) write_rows<T, D>(acc, a.scale, out, nullptr, a.hd);
+}
+
+template <typename T, int D, bool FEW, typename M>
+__device__ __forceinline__ void dkv_tile(const AttnArgs& a, unsigned char* smem, unsigned group) {
+  using C = Bwd<T, D, FEW, true>;
+  constexpr int ES = sizeof(T), KS = D / 16, DB = D / 32, UNITS = D * ES / 16;
+  typedef typename Frag<T>::type frag;
+  lds_u8* ldsQ = (lds_u8*)smem;
+  lds_u8* ldsG = ldsQ + C::BN * C::P0;
+  float* rows = (float*)(smem + C::BN * (C::P0 + C::P1));   // shift, -D, slope, x, y, z of the tile's rows
+
+  const int tid = (int)threadIdx.x, l = tid & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kvh = (int)(group % (unsigned)a.Hk);
+  const unsigned rest = group / (unsigned)a.Hk;
+  const int split = FEW ? (int)(rest % (unsigned)a.splits_k) : 0;
+  const int64_t tile = FEW ? rest / (unsigned)a.splits_k : rest;
+  int64_t first;
+  const int seg = find_segment(a.kb, a.n_seg, 1, C::OWN, tile, &first);
+  const int64_t k0 = a.kb.at(seg), klen = a.kb.at(seg + 1) - k0, j0 = (tile - first) * C::OWN;
+  if (tile < first || j0 >= klen) return;
+  const int64_t q0 = a.qb.at(seg), queries = a.qb.at(seg + 1) - q0, R = queries > 0 ? queries * a.G : 0;
+  const int tiles = (int)((R + C::BN - 1) / C::BN);
+  const int per = FEW ? (tiles + a.splits_k - 1) / a.splits_k : tiles;
+  const int t_begin = min(split * per, tiles), t_end = min(t_begin + per, tiles);
+
+  const bool cap = M::cap(a);
+  const int dim = M::dim(a);
+  const Score<T> sc(a, cap);
+  frag kf[KS], vf[KS];
+  Place me{0.0f, 0.0f, 0.0f};
+  {
+    const int64_t j = j0 + (FEW ? 0 : 32 * w) + (l & 31);
+    const bool there = j < klen;
+    const int64_t key = k0 + (there ? j : 0);
+#pragma unroll
+    for (int t = 0; t < KS; ++t) {
+      const int c = 16 * t + 8 * h;
+      kf[t] = read_frag<T>((const T*)a.k + key * a.ldk + kvh * a.hd + c, there && c < a.hd);
+      vf[t] = read_frag<T>((const T*)a.v + key * a.ldv + kvh * a.hd + c, there && c < a.hd);
+      apply_sign(kf[t], sc.sign);
+    }
+    if (dim && a.dim && there) me = place_of(a.pos_k, a.dim, key);
+  }
+
+  const int row0 = tid / UNITS, c0 = tid % UNITS * 16;
+  const bool in = c0 < a.hd * ES;
+  u32x4 regQ[C::HELD], regG[C::HELD];
+  float dots[C::HELD];   // FEW: this unit's part of dO . o
+  float rl = -INFINITY, rd = 0.0f, rs = 0.0f;
+  Place rp{0.0f, 0.0f, 0.0f};
+  auto fetch = [&](int t, int i0) {
+    const unsigned base = (unsigned)t * C::BN;   // rows before this tile
+    const unsigned f0 = base / (unsigned)a.G, g0 = base - f0 * a.G;
+    const int64_t left = queries - f0, at = q0 + f0;
+    const int rem = (int)min((int64_t)C::BN + 1, left);
+    const int64_t side = (int64_t)kvh * a.G * a.hd;
+    const auto bq = buffer_of((const T*)a.q + at * a.ldq + side, (uint32_t)(rem * a.ldq * ES));
+    const auto bg = buffer_of((const T*)a.go + at * a.ldgo + side, (uint32_t)(rem * a.ldgo * ES));
+    const auto bo = buffer_of((const T*)a.o + at * a.ldo + side, (uint32_t)(rem * a.ldo * ES));
+#pragma unroll
+    for (int i = 0; i < C::HELD; ++i) {
+      const uint32_t x = g0 + row0 + (i0 + i) * C::STEP, qi = (x * a.g_inv) >> 20, g = x - qi * a.G;
+      const uint32_t off = g * (uint32_t)(a.hd * ES) + c0;
+      const bool got = in && (int)qi < rem;
+      regQ[i] = buffer_read(bq, got ? qi * (uint32_t)(a.ldq * ES) + off : NOWHERE);
+      regG[i] = buffer_read(bg, got ? qi * (uint32_t)(a.ldgo * ES) + off : NOWHERE);
+      if (FEW) {
+        const u32x4 regO = buffer_read(bo, got ? qi * (uint32_t)(a.ldo * ES) + off : NOWHERE);
+        typedef T unit __attribute__((ext_vector_type(16 / ES)));
+        const unit gv = __builtin_bit_cast(unit, regG[i]), ov = __builtin_bit_cast(unit, regO);
+        dots[i] = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16 / ES; ++e) dots[i] = fmaf((float)gv[e], (float)ov[e], dots[i]);
+      }
+    }
+    if (i0 == 0 && tid < C::BN) {
+      const uint32_t x = g0 + tid, qi = (x * a.g_inv) >> 20, g = x - qi * a.G;
+      rl = -INFINITY, rd = 0.0f, rs = 0.0f, rp = Place{0.0f, 0.0f, 0.0f};
+      if ((int64_t)qi < left) {
+        const int64_t query = at + qi, slot = query * a.H + kvh * a.G + g;
+        const float lse = a.lse_in[slot];
+        rl = lse == -INFINITY ? -INFINITY : sc.C - lse * LOG2E;
+        if (!FEW) rd = -a.delta[slot];
+        if (dim && a.dim) rp = place_of(a.pos_q, a.dim, query), rs = a.slopes[kvh * a.G + g] * sc.per_slope;
+      }
+    }
+  };
+  auto put = [&](int i0) {
+#pragma unroll
+    for (int i = 0; i < C::HELD; ++i) {
+      const int r = row0 + (i0 + i) * C::STEP;
+      *(lds_u32x4*)(ldsQ + r * C::P0 + c0) = regQ[i];
+      *(lds_u32x4*)(ldsG + r * C::P1 + c0) = regG[i];
+      if (FEW) {   // the units of a row are a row of lanes
+        float d = dots[i];
+#pragma unroll
+        for (int o = 1; o < UNITS; o <<= 1) d += __shfl_xor(d, o, 64);
+        if (c0 == 0) rows[C::BN + r] = -d;
+      }
+    }
+    if (i0 == 0 && tid < C::BN) {
+      rows[tid] = rl;
+      if (!FEW) rows[C::BN + tid] = rd;
+      if (dim) rows[2 * C::BN + tid] = rs, rows[3 * C::BN + tid] = rp.x, rows[4 * C::BN + tid] = rp.y, rows[5 * C::BN + tid] = rp.z;
+    }
+  };
+
+  f32x16 dk[DB], dv[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) dk[d] = f32x16{}, dv[d] = f32x16{};
+
+  if (C::AHEAD && t_begin < t_end) fetch(t_begin, 0);
+  for (int t = t_begin; t < t_end; ++t) {
+    __syncthreads();
+    if (C::AHEAD) {
+      put(0);
+    } else {
+#pragma unroll 1
+      for (int i0 = 0; i0 < C::PER; i0 += C::HELD) fetch(t, i0), put(i0);
+    }
+    __syncthreads();
+    if (C::AHEAD && t + 1 < t_end) fetch(t + 1, 0);
+    if (FEW && (int64_t)t * C::BN + 32 * w >= R) continue;
+#pragma unroll
+    for (int b = 0; b < C::SUB; ++b) {
+      const int at = 32 * ((FEW ? w : 0) + b);
+      f32x16 x{}, dp;
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const float4 d = *(const float4*)(rows + C::BN + at + 8 * i4 + 4 * h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dp[4 * i4 + e] = (&d.x)[e];
+      }
+      frag rq[2], rg[2];
+      rq[0] = lds_rows<T>(ldsQ, C::P0, at, 0), rg[0] = lds_rows<T>(ldsG, C::P1, at, 0);
+#pragma unroll
+      for (int t2 = 0; t2 < KS; ++t2) {
+        if (t2 + 1 < KS)
+          rq[(t2 + 1) & 1] = lds_rows<T>(ldsQ, C::P0, at, 16 * (t2 + 1)), rg[(t2 + 1) & 1] = lds_rows<T>(ldsG, C::P1, at, 16 * (t2 + 1));
+        x = mma(rq[t2 & 1], kf[t2], x);
+        dp = mma(rg[t2 & 1], vf[t2], dp);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const float* row = rows + at + 8 * i4 + 4 * h;
+        const float4 shift = *(const float4*)row;
+        float4 sl{}, px{}, py{}, pz{};
+        if (dim) {
+          sl = *(const float4*)(row + 2 * C::BN), px = *(const float4*)(row + 3 * C::BN), py = *(const float4*)(row + 4 * C::BN);
+          if (dim > 2) pz = *(const float4*)(row + 5 * C::BN);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = 4 * i4 + e;
+          float fall;
+          float u = sc.template u<true>(x[i], cap, &fall);
+          if (dim) u = fmaf(-(&sl.x)[e], distance(dim, me, (&px.x)[e], (&py.x)[e], (&pz.x)[e]), u);
+          x[i] = exp2_of(fmaf(u, sc.A, (&shift.x)[e]));
+          dp[i] *= x[i];
+          if (cap) dp[i] *= fall;
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2) {
+        float p[8], ds[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = x[8 * t2 + i], ds[i] = dp[8 * t2 + i];
+        const frag pf = to_frag<T>(p), sf = to_frag<T>(ds);
+        frag cg[DB], cq[DB];
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          cg[d] = lds_columns<T>(ldsG, C::P1, at + 16 * t2, 32 * d), cq[d] = lds_columns<T>(ldsQ, C::P0, at + 16 * t2, 32 * d);
+          if (ES == 4) {   // float32 fragments are large: not all of them at once
+            dv[d] = mma(cg[d], pf, dv[d]), dk[d] = mma(cq[d], sf, dk[d]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        if (ES != 4) {
+#pragma unroll
+          for (int d = 0; d < DB; ++d) dv[d] = mma(cg[d], pf, dv[d]), dk[d] = mma(cq[d], sf, dk[d]);
+        }
+      }
+    }
+  }
+
+  int again = tid;   // the lane's key once more: formed here, not kept in registers over the loop
+  asm volatile("" : "+v"(again));
+  const int64_t j = j0 + (FEW ? again & 31 : 32 * (again >> 6) + (again & 31)), key = k0 + j;
+  const bool there = j < klen;
+  T* gk = (T*)a.gk + key * a.ldgk + kvh * a.hd;
+  T* gv = (T*)a.gv + key * a.ldgv + kvh * a.hd;
+  if (FEW) {
+    const int64_t at = (((int64_t)split * a.nk + key) * a.Hk + kvh) * a.hd;
+    join_rows<T, D>(dk, (float*)smem, a.scale, gk, a.splits_k > 1 ? a.part_k + at : nullptr, a.hd, there);
+    join_rows<T, D>(dv, (float*)smem, 1.0f, gv, a.splits_k > 1 ? a.part_v + at : nullptr, a.hd, there);
+  } else if (there) {
+    write_rows<T, D>(dk, a.scale, gk, nullptr, a.hd);
+    write_rows<T, D>(dv, 1.0f, gv, nullptr, a.hd);
+  }
+}
+
+}  // namespace dsmp

@@ -27,20 +27,29 @@ struct Fwd {
   static constexpr bool AHEAD = !(FEW && sizeof(T) == 4 && D == 128);
   static constexpr int HELD = AHEAD || PER < 4 ? PER : 4;
   static constexpr int TILE = BN * (PK + PV) + 3 * BN * 4;
+  static constexpr int BUFS = AHEAD && !FEW && D <= 64 ? 2 : 1;   // two tiles in LDS: one barrier to a tile
   static constexpr int JOIN = FEW ? NW * 32 * (D + 2) * 4 : 0;
-  static constexpr int LDS = TILE > JOIN ? TILE : JOIN;
+  static constexpr int LDS = BUFS * TILE > JOIN ? BUFS * TILE : JOIN;
+  // waves to a SIMD that the registers are cut to
+  static constexpr int waves(int cap, int dim) {
+    if (D == 128) return FEW || sizeof(T) == 4 || dim > 2 ? 1 : 2;
+    if (FEW || sizeof(T) == 4) return 2;
+    return (D == 64 ? 3 : 4) - (cap || dim);
+  }
   static_assert(PER >= 1 && PER * NT * 16 == BN * D * (int)sizeof(T), "whole units for every thread");
 };
 
+// How far the scores of a tile may pass the maximum that a row's sums refer to, in powers of two,
+// before the sums are brought to a new one: weights then reach 2^8, which costs neither
+// float32 sums nor the rounded weights a digit.
+constexpr float SLACK = 8.0f;
+
 template <typename T, int D, bool FEW, typename M>
-__global__ __launch_bounds__(NT, D == 128 && (FEW || sizeof(T) == 4 || M::DIM > 2) ? 1 : 2) void k_attn_fwd(AttnArgs a) {
+__global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::waves(M::CAP, M::DIM))) void k_attn_fwd(AttnArgs a) {
   using C = Fwd<T, D, FEW>;
   constexpr int ES = sizeof(T), KS = D / 16, DB = D / 32;
   typedef typename Frag<T>::type frag;
   __shared__ __align__(16) unsigned char smem[C::LDS];
-  lds_u8* ldsK = (lds_u8*)smem;
-  lds_u8* ldsV = ldsK + C::BN * C::PK;
-  float* places = (float*)(smem + C::BN * (C::PK + C::PV));   // x, y, z of the tile's keys
 
   const int tid = (int)threadIdx.x, l = tid & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = (int)(blockIdx.x % (unsigned)a.Hk);
@@ -59,19 +68,20 @@ __global__ __launch_bounds__(NT, D == 128 && (FEW || sizeof(T) == 4 || M::DIM > 
   // this lane's row
   const bool cap = M::cap(a);
   const int dim = M::dim(a);
-  const ScoreConst sc = score_const(a);
-  const int64_t r = r0 + (FEW ? 0 : 32 * w) + (l & 31);
-  const bool there = r < R;
-  const unsigned rq = there ? (unsigned)r / (unsigned)a.G : 0u, rg = there ? (unsigned)r - rq * a.G : 0u;
-  const int64_t query = q0 + rq;
-  const int head = kvh * a.G + (int)rg;
+  const Score<T> sc(a, cap);
+  const RowOf row = row_of(a, q0, r0, R, kvh, FEW, tid);
+  const bool there = row.there;
+  const int64_t query = row.query;
+  const int head = row.head;
   frag qf[KS];
 #pragma unroll
-  for (int t = 0; t < KS; ++t)
+  for (int t = 0; t < KS; ++t) {
     qf[t] = read_frag<T>((const T*)a.q + query * a.ldq + head * a.hd + 16 * t + 8 * h, there && 16 * t + 8 * h < a.hd);
+    apply_sign(qf[t], sc.sign);
+  }
   Place me{0.0f, 0.0f, 0.0f};
-  float slope2 = 0.0f;
-  if (dim && a.dim && there) me = place_of(a.pos_q, a.dim, query), slope2 = a.slopes[head] * LOG2E;
+  float slope = 0.0f;
+  if (dim && a.dim && there) me = place_of(a.pos_q, a.dim, query), slope = a.slopes[head] * sc.per_slope;
 
   // a thread's 16-byte units of a tile: one place in every STEP-th row
   const int row0 = tid / (D * ES / 16), c0 = tid % (D * ES / 16) * 16;
@@ -90,14 +100,18 @@ __global__ __launch_bounds__(NT, D == 128 && (FEW || sizeof(T) == 4 || M::DIM > 
       regK[i] = buffer_read(bk, offK + (i0 + i) * stepK), regV[i] = buffer_read(bv, offV + (i0 + i) * stepV);
     if (dim && a.dim && i0 == 0 && tid < rem) key = place_of(a.pos_k, a.dim, j0 + tid);
   };
-  auto put = [&](int i0) {
+  auto put = [&](int buf, int i0) {
+    lds_u8* to = (lds_u8*)smem + buf * C::TILE;
 #pragma unroll
     for (int i = 0; i < C::HELD; ++i) {
       const int row = row0 + (i0 + i) * C::STEP;
-      *(__attribute__((address_space(3))) u32x4*)(ldsK + row * C::PK + c0) = regK[i];
-      *(__attribute__((address_space(3))) u32x4*)(ldsV + row * C::PV + c0) = regV[i];
+      *(__attribute__((address_space(3))) u32x4*)(to + row * C::PK + c0) = regK[i];
+      *(__attribute__((address_space(3))) u32x4*)(to + C::BN * C::PK + row * C::PV + c0) = regV[i];
     }
-    if (dim && i0 == 0 && tid < C::BN) places[tid] = key.x, places[C::BN + tid] = key.y, places[2 * C::BN + tid] = key.z;
+    if (dim && i0 == 0 && tid < C::BN) {
+      float* places = (float*)(smem + buf * C::TILE + C::BN * (C::PK + C::PV));
+      places[tid] = key.x, places[C::BN + tid] = key.y, places[2 * C::BN + tid] = key.z;
+    }
   };
 
   f32x16 o[DB];
@@ -105,31 +119,34 @@ __global__ __launch_bounds__(NT, D == 128 && (FEW || sizeof(T) == 4 || M::DIM > 
   for (int d = 0; d < DB; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-  float m = -INFINITY, sum = 0.0f;   // of this lane's row; the sum over this half's keys
+  float m = -INFINITY, sum = 0.0f;   // the u that this lane's row refers to; the sum over this half's keys
 
-  if (C::AHEAD && t_begin < t_end) fetch(t_begin, 0);
-  for (int t = t_begin; t < t_end; ++t) {
-    __syncthreads();
-    if (C::AHEAD) {
-      put(0);
-    } else {
-#pragma unroll 1
-      for (int i0 = 0; i0 < C::PER; i0 += C::HELD) fetch(t, i0), put(i0);
-    }
-    __syncthreads();
-    if (C::AHEAD && t + 1 < t_end) fetch(t + 1, 0);
-    const int rem = (int)min((int64_t)C::BN, klen - (int64_t)t * C::BN);
+  // one tile: scores, then weights and their products with the values
+  auto step = [&](int buf, int rem) {
+    lds_u8* ldsK = (lds_u8*)smem + buf * C::TILE;
+    lds_u8* ldsV = ldsK + C::BN * C::PK;
+    const float* places = (const float*)(smem + buf * C::TILE + C::BN * (C::PK + C::PV));
     const int sub0 = FEW ? w : 0;
-    if (FEW && 32 * w >= rem) continue;
-    float s[C::SUB][16], top = -INFINITY;
+    // Fragments are read one step ahead of their products and no further (the scheduler would
+    // read all of them at once and run out of registers); the products run while the
+    // next step's powers are formed.
+    f32x16 x[C::SUB];
+    frag kf[2][C::SUB];
+#pragma unroll
+    for (int b = 0; b < C::SUB; ++b) kf[0][b] = lds_rows<T>(ldsK, C::PK, 32 * (sub0 + b), 0), x[b] = f32x16{};
+#pragma unroll
+    for (int t2 = 0; t2 < KS; ++t2) {
+#pragma unroll
+      for (int b = 0; b < C::SUB; ++b)
+        if (t2 + 1 < KS) kf[(t2 + 1) & 1][b] = lds_rows<T>(ldsK, C::PK, 32 * (sub0 + b), 16 * (t2 + 1));
+#pragma unroll
+      for (int b = 0; b < C::SUB; ++b) x[b] = mma(kf[t2 & 1][b], qf[t2], x[b]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    float top = -INFINITY;
 #pragma unroll
     for (int b = 0; b < C::SUB; ++b) {
       const int at = 32 * (sub0 + b);
-      f32x16 x;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = 0.0f;
-#pragma unroll
-      for (int t2 = 0; t2 < KS; ++t2) x = mma(lds_rows<T>(ldsK, C::PK, at, 16 * t2), qf[t2], x);
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) {
         float4 px{}, py{}, pz{};
@@ -140,51 +157,96 @@ __global__ __launch_bounds__(NT, D == 128 && (FEW || sizeof(T) == 4 || M::DIM > 
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float z = capped<T, false>(x[4 * i4 + e], cap, sc, nullptr);
-          if (dim) z = fmaf(-slope2, distance(dim, me, (&px.x)[e], (&py.x)[e], (&pz.x)[e]), z);
-          s[b][4 * i4 + e] = z;
+          const int i = 4 * i4 + e;
+          float u = sc.template u<false>(x[b][i], cap, nullptr);
+          if (dim) u = fmaf(-slope, distance(dim, me, (&px.x)[e], (&py.x)[e], (&pz.x)[e]), u);
+          x[b][i] = u;
         }
       }
       if (at + 32 > rem) {   // behind the last key
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (at + result_row(i) >= rem) s[b][i] = -INFINITY;
+          if (at + result_row(i) >= rem) x[b][i] = -INFINITY;
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, x[b][i]);
+      if (dim) __builtin_amdgcn_sched_barrier(0);
     }
+    frag vf[2][DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) vf[0][d] = lds_columns<T>(ldsV, C::PV, 32 * sub0, 32 * d);
     top = fmaxf(top, other_half(top));
-    const float now = fmaxf(m, top), base = now == -INFINITY ? 0.0f : now, shrink = exp2_of(m - base);
-    m = now;
-    float add = 0.0f;
-#pragma unroll
-    for (int b = 0; b < C::SUB; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[b][i] = exp2_of(s[b][i] - base), add += s[b][i];
-    sum = fmaf(sum, shrink, add);
-    if (__any(shrink != 1.0f)) {
+    if (__any((top - m) * sc.A > SLACK)) {   // also where m is -infinity
+      const float now = fmaxf(m, top), shrink = m == -INFINITY ? 0.0f : exp2_of((m - now) * sc.A);
+      m = now;
+      sum *= shrink;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] *= shrink;
     }
+    const float base = m == -INFINITY ? 0.0f : -m * sc.A;
+    float add = 0.0f;
 #pragma unroll
-    for (int b = 0; b < C::SUB; ++b)
+    for (int k = 0; k < 2 * C::SUB; ++k) {
+      const int b = k >> 1, t2 = k & 1;
+      float p[8];
 #pragma unroll
-      for (int t2 = 0; t2 < 2; ++t2) {
-        const frag p = to_frag<T>(&s[b][8 * t2]);
+      for (int i = 0; i < 8; ++i) p[i] = exp2_of(fmaf(x[b][8 * t2 + i], sc.A, base)), add += p[i];
+      const frag pf = to_frag<T>(p);
 #pragma unroll
-        for (int d = 0; d < DB; ++d) o[d] = mma(lds_columns<T>(ldsV, C::PV, 32 * (sub0 + b) + 16 * t2, 32 * d), p, o[d]);
+      for (int d = 0; d < DB; ++d)
+        if (k + 1 < 2 * C::SUB) vf[(k + 1) & 1][d] = lds_columns<T>(ldsV, C::PV, 32 * sub0 + 16 * (k + 1), 32 * d);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[d] = mma(vf[k & 1][d], pf, o[d]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    sum += add;
+  };
+  auto rem_of = [&](int t) { return (int)min((int64_t)C::BN, klen - (int64_t)t * C::BN); };
+  auto take = [&](int buf, int t) {
+    const int rem = rem_of(t);
+    if (FEW && 32 * w >= rem) return;
+    step(buf, rem);
+  };
+
+  if (C::BUFS == 2) {
+    if (t_begin < t_end) fetch(t_begin, 0), put(0, 0);
+    if (t_begin + 1 < t_end) fetch(t_begin + 1, 0);
+    __syncthreads();
+    for (int t = t_begin; t < t_end; ++t) {
+      const int buf = (t - t_begin) & 1;
+      take(buf, t);
+      if (t + 1 < t_end) put(buf ^ 1, 0);   // all waves have left that tile at the barrier before
+      if (t + 2 < t_end) fetch(t + 2, 0);
+      __syncthreads();
+    }
+  } else {
+    if (C::AHEAD && t_begin < t_end) fetch(t_begin, 0);
+    for (int t = t_begin; t < t_end; ++t) {
+      __syncthreads();
+      if (C::AHEAD) {
+        put(0, 0);
+      } else {
+#pragma unroll 1
+        for (int i0 = 0; i0 < C::PER; i0 += C::HELD) fetch(t, i0), put(0, i0);
       }
+      __syncthreads();
+      if (C::AHEAD && t + 1 < t_end) fetch(t + 1, 0);
+      take(0, t);
+    }
   }
   sum += other_half(sum);
 
-  const int64_t slot = query * a.H + head;   // this row's among all queries and heads
+  int again = tid;   // the row once more: formed here, not kept in registers over the loop
+  asm volatile("" : "+v"(again));
+  const RowOf mine = row_of(a, q0, r0, R, kvh, FEW, again);
+  const int64_t slot = mine.query * a.H + mine.head;   // this row's among all queries and heads
   if (!FEW) {
-    if (!there) return;
+    if (!mine.there) return;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    if (a.lse && h == 0) a.lse[slot] = (m + __log2f(sum)) * LN2;
-    T* out = (T*)a.out + query * a.ldout + head * a.hd;
+    if (a.lse && h == 0) a.lse[slot] = (fmaf(m, sc.A, sc.C) + __log2f(sum)) * LN2;
+    T* out = (T*)a.out + mine.query * a.ldout + mine.head * a.hd;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -196,6 +258,7 @@ __global__ __launch_bounds__(NT, D == 128 && (FEW || sizeof(T) == 4 || M::DIM > 
     return;
   }
   // the waves' parts, [wave][value][row], joined by 256 threads: a row and four values in 32 each
+  m = fmaf(m, sc.A, sc.C);   // in powers of two from here on
   float *jo = (float*)smem, *jm = jo + NW * D * 32, *js = jm + NW * 32;
   __syncthreads();
 #pragma unroll
@@ -204,7 +267,7 @@ __global__ __launch_bounds__(NT, D == 128 && (FEW || sizeof(T) == 4 || M::DIM > 
     for (int i = 0; i < 16; ++i) jo[(w * D + 32 * d + result_row(i)) * 32 + (l & 31)] = o[d][i];
   if (h == 0) jm[w * 32 + l] = m, js[w * 32 + l] = sum;
   __syncthreads();
-  if (!there) return;
+  if (!mine.there) return;
   float top = -INFINITY, weight[NW], total = 0.0f;
 #pragma unroll
   for (int k = 0; k < NW; ++k) top = fmaxf(top, jm[k * 32 + (l & 31)]);
@@ -237,7 +300,7 @@ __global__ __launch_bounds__(NT, D == 128 && (FEW || sizeof(T) == 4 || M::DIM > 
       for (int k = 0; k < NW; ++k) v[e] = fmaf(weight[k], jo[(k * D + c + e) * 32 + (l & 31)], v[e]);
       v[e] *= inv;
     }
-    if (whole) store4((T*)a.out + query * a.ldout + head * a.hd + c, v[0], v[1], v[2], v[3]);
+    if (whole) store4((T*)a.out + mine.query * a.ldout + mine.head * a.hd + c, v[0], v[1], v[2], v[3]);
     else *(float4*)(a.part + part * a.hd + c) = make_float4(v[0], v[1], v[2], v[3]);
   }
 }
@@ -366,8 +429,6 @@ size_t fwd_bytes(const dsmp_attention_desc& d, const dsmp_segments& qs, const ds
   return p.splits == 1 ? 0 : (size_t)p.splits * qs.n * d.heads * (d.head_dim + 2) * sizeof(float);
 }
 
-size_t bwd_bytes(const dsmp_attention_desc& d, const dsmp_segments& qs) { return (size_t)qs.n * d.heads * sizeof(float); }
-
 }  // namespace
 
 namespace dsmp {
@@ -383,6 +444,11 @@ dsmp_status check_attention(dsmp_handle* h, const dsmp_attention_desc* d, const 
   DSMP_CHECK(h, d->dim >= 0 && d->dim <= 3, DSMP_INVALID_ARG, "0 to 3 coordinates");
   DSMP_CHECK(h, std::isfinite(d->scale), DSMP_INVALID_ARG, "the scale must be finite");
   DSMP_CHECK(h, std::isfinite(d->cap) && d->cap >= 0.0f, DSMP_INVALID_ARG, "the cap must be finite and not negative");
+  const float least = 0x1p-64f, most = 0x1p64f;   // slopes are divided by them
+  DSMP_CHECK(h, d->scale == 0.0f || (std::fabs(d->scale) >= least && std::fabs(d->scale) <= most), DSMP_UNSUPPORTED,
+             "a scale must be 0 or within 2^-64 and 2^64");
+  DSMP_CHECK(h, d->cap == 0.0f || (d->cap >= least && d->cap <= most), DSMP_UNSUPPORTED,
+             "a cap must be 0 or within 2^-64 and 2^64");
   const int G = d->heads / d->kv_heads;
   for (const dsmp_segments* s : {qs, ks}) {
     DSMP_CHECK(h, s->n >= 0 && s->n_seg >= 1, DSMP_INVALID_ARG, "negative rows or no segment");
@@ -404,7 +470,7 @@ extern "C" dsmp_status dsmp_attention_workspace(const dsmp_attention_desc* desc,
   if (st != DSMP_OK) return st;
   if (!fwd_ws_bytes || !bwd_ws_bytes) return DSMP_INVALID_ARG;
   *fwd_ws_bytes = fwd_bytes(*desc, *qs, *ks);
-  *bwd_ws_bytes = bwd_bytes(*desc, *qs);
+  *bwd_ws_bytes = attention_bwd_bytes(*desc, *qs, *ks);
   return DSMP_OK;
 }
 
@@ -445,40 +511,5 @@ extern "C" dsmp_status dsmp_attention_forward(dsmp_handle* h, const dsmp_attenti
       hipLaunchKernelGGL((k_attn_join_few<T>), dim3(ceil_div(slots, 8)), dim3(NT), 0, h->stream, a);
   });
   DSMP_LAUNCHED(h, "attention forward");
-  return DSMP_OK;
-}
-
-extern "C" dsmp_status dsmp_attention_backward(dsmp_handle* h, const dsmp_attention_desc* desc, const dsmp_segments* qs,
-                                               const dsmp_segments* ks, const void* q, int64_t ldq, const void* k,
-                                               int64_t ldk, const void* v, int64_t ldv, const float* pos_q,
-                                               const float* pos_k, const float* slopes, const void* out, int64_t ldo,
-                                               const float* lse, const void* grad_out, int64_t ldgo, void* grad_q,
-                                               int64_t ldgq, void* grad_k, int64_t ldgk, void* grad_v, int64_t ldgv,
-                                               void* ws, size_t ws_bytes) {
-  if (!h) return DSMP_INVALID_ARG;
-  dsmp_status st = check_attention(h, desc, qs, ks);
-  if (st != DSMP_OK) return st;
-  DSMP_CHECK(h, (qs->n == 0 || (q && out && lse && grad_out && grad_q)) && (ks->n == 0 || (k && v && grad_k && grad_v)),
-             DSMP_INVALID_ARG, "a data pointer is NULL");
-  DSMP_CHECK(h, desc->dim == 0 || (slopes && (qs->n == 0 || pos_q) && (ks->n == 0 || pos_k)), DSMP_INVALID_ARG,
-             "coordinates and slopes are needed");
-  const int es = desc->dtype == DSMP_BF16 ? 2 : 4, wq = desc->heads * desc->head_dim, wk = desc->kv_heads * desc->head_dim;
-  st = check_matrices(h, es, {{q, ldq, wq, "q"}, {k, ldk, wk, "k"}, {v, ldv, wk, "v"}, {out, ldo, wq, "out"},
-                              {grad_out, ldgo, wq, "grad_out"}, {grad_q, ldgq, wq, "grad_q"},
-                              {grad_k, ldgk, wk, "grad_k"}, {grad_v, ldgv, wk, "grad_v"}});
-  if (st != DSMP_OK) return st;
-  const size_t need = bwd_bytes(*desc, *qs);
-  DSMP_CHECK(h, !need || (ws && ws_bytes >= need), DSMP_WORKSPACE_TOO_SMALL, "workspace needs %zu bytes", need);
-  DSMP_CHECK(h, !need || reinterpret_cast<uintptr_t>(ws) % 16 == 0, DSMP_INVALID_ARG, "the workspace must be 16-byte aligned");
-  AttnArgs a = attn_args(*desc, *qs, *ks);
-  a.q = q, a.ldq = ldq, a.k = k, a.ldk = ldk, a.v = v, a.ldv = ldv, a.o = out, a.ldo = ldo, a.go = grad_out, a.ldgo = ldgo;
-  a.gq = grad_q, a.ldgq = ldgq, a.gk = grad_k, a.ldgk = ldgk, a.gv = grad_v, a.ldgv = ldgv;
-  a.lse_in = lse, a.delta = (float*)ws;
-  a.pos_q = pos_q, a.pos_k = pos_k, a.slopes = slopes;
-  DeviceScope dev(h);
-  ProfScope prof(h, DSMP_K_ATTN_BWD);
-  if (qs->n > 0) launch_attention_dq(h, *desc, a);
-  if (ks->n > 0) launch_attention_dkv(h, *desc, a, ks->n);
-  DSMP_LAUNCHED(h, "attention backward");
   return DSMP_OK;
 }

@@ -27,8 +27,9 @@ def test_attention_workspace(lib):
     st, f, b = attention_ws(lib, d, (16384, 1, None), (16384, 1, None))
     assert st == dm.OK and f == 0 and b == 16384 * 8 * 4                 # the tiles fill the card: no parts to join
     st, f, b = attention_ws(lib, d, (5, 1, None), (262144, 1, None))
-    assert st == dm.OK and f >= 2 * 5 * 8 * 66 * 4 and b == 5 * 8 * 4    # two parts at least
-    assert attention_ws(lib, d, (5, 1, None), (100, 1, None))[1] == 0
+    assert st == dm.OK and f >= 2 * 5 * 8 * 66 * 4 and b >= 2 * 5 * 8 * 64 * 4    # two parts at least
+    st, f, b = attention_ws(lib, d, (5, 1, None), (100, 1, None))
+    assert st == dm.OK and f == 0 and 5 * 8 * 4 <= b <= 256
     assert attention_ws(lib, d, (0, 3, None), (0, 3, None)) == (dm.OK, 0, 0)
 
 
@@ -36,7 +37,8 @@ def test_attention_workspace(lib):
     (dict(heads=0), dm.INVALID_ARG), (dict(heads=3), dm.INVALID_ARG), (dict(heads=512, kv_heads=512), dm.UNSUPPORTED),
     (dict(head_dim=12), dm.UNSUPPORTED), (dict(head_dim=136), dm.UNSUPPORTED), (dict(head_dim=0), dm.INVALID_ARG),
     (dict(dtype=2), dm.INVALID_ARG), (dict(dim=4), dm.INVALID_ARG), (dict(dim=-1), dm.INVALID_ARG),
-    (dict(scale=float("nan")), dm.INVALID_ARG), (dict(cap=-1.0), dm.INVALID_ARG), (dict(cap=float("inf")), dm.INVALID_ARG)])
+    (dict(scale=float("nan")), dm.INVALID_ARG), (dict(scale=1e-30), dm.UNSUPPORTED), (dict(scale=-1e30), dm.UNSUPPORTED),
+    (dict(cap=1e-30), dm.UNSUPPORTED), (dict(scale=0.0), dm.OK), (dict(scale=-0.1), dm.OK), (dict(cap=-1.0), dm.INVALID_ARG), (dict(cap=float("inf")), dm.INVALID_ARG)])
 def test_attention_refuses_descriptors(lib, change, status):
     args = {**dict(heads=4, kv_heads=2, head_dim=64, dtype=dm.BF16, dim=2, scale=0.1, cap=0.0), **change}
     assert attention_ws(lib, dm.attention_desc(**args), (10, 1, None), (10, 1, None))[0] == status

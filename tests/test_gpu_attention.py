@@ -163,6 +163,24 @@ def test_few_queries_over_many_keys(env, H, Hk, qb, kb, dim, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("nq,nk,H", [(700, 20, 128), (20, 700, 128)])
+def test_many_rows_and_few_keys_and_the_other_way(env, nq, nk, H, dtype):
+    """Tiles of 128 on one side of the backward pass and of 32 on the other."""
+    announce(dtype, nq, nk)
+    Case(env, [0, nq], [0, nk], H, H, 16, dtype, dim=1).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scores_that_rise_from_tile_to_tile(env, dtype):
+    """Each later key scores higher: the running maximum is passed by more than its slack again and again."""
+    c = Case(env, [0, 40], [0, 1000], 2, 2, 16, dtype, scale=1.0)
+    c.k.copy_((c.torch.arange(1000, device="cuda")[:, None] * 0.06).expand(1000, 32))
+    c.q.copy_(c.torch.rand(40, 32, device="cuda") * 0.2)
+    announce(dtype)
+    c.check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_many_segments(env, dtype):
     """Segments found from their bounds 64 at a time, over three rounds."""
     g = np.random.default_rng(5)
@@ -191,6 +209,14 @@ def test_sharp_and_large_scores(env, dtype):
     c = Case(env, [0, 64], [0, 200], 2, 1, 64, dtype, scale=2.0, spread=2.0)
     announce(dtype)
     c.check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [-0.4, 0.0])
+@pytest.mark.parametrize("dim,cap", [(0, 0.0), (2, 0.0), (2, 3.0)])
+def test_scales_of_any_sign(env, scale, dim, cap, dtype):
+    announce(dtype, scale, dim, cap)
+    Case(env, [0, 70], [0, 150], 2, 1, 32, dtype, dim=dim, cap=cap, scale=scale).check()
 
 
 def test_nan_and_infinity_stay_in_their_segment(env):
