@@ -210,7 +210,7 @@ struct AttnArgs {
   float *lse, *delta, *part;   // part: of out, or of dq
   Bounds qb, kb;
   int n_seg, H, Hk, G, hd, dim, splits, splits_k;
-  unsigned dq_groups;    // of a launch for both gradients: the first ones are for dq
+  unsigned dkv_groups;   // of a launch for both gradients: the first ones are for dk and dv
   float *part_k, *part_v;
   uint32_t g_inv;        // ceil(2^20 / G): x / G = x g_inv >> 20 for x < 512
   float scale, cap;      // of the scores as they are
@@ -269,7 +269,7 @@ __device__ __forceinline__ float distance(int dim, const Place& a, float x, floa
 // tanh for float32 scores, within about 3 u of it: 1 - 2 / (1 + e^2x), whose difference costs
 // digits near zero, where the series to x^11 takes its place (its next term is 2^-26 of x at 0.35).
 __device__ __forceinline__ float tanh_of(float x) {
-  const float far = 1.0f - 2.0f / (1.0f + exp2_of(x * (2.0f * LOG2E))), s = x * x;
+  const float far = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + exp2_of(x * (2.0f * LOG2E))), 1.0f), s = x * x;
   float p = fmaf(s, -1382.0f / 155925.0f, 62.0f / 2835.0f);
   p = fmaf(s, p, -17.0f / 315.0f);
   p = fmaf(s, p, 2.0f / 15.0f);
@@ -350,6 +350,42 @@ void by_attention(const dsmp_attention_desc& d, F f) {
 
 // Workgroups of 256 threads that fill the card (256 CUs) twice; a launch has fewer than 2^32 threads.
 constexpr int64_t FILL = 512, MAX_GROUPS = ((int64_t)1 << 24) - 1;
+
+// How far FEW's workgroups are cut over the other side.  Each of one or two kinds of them, `groups`
+// with `steps` tiles to go over, is cut so that a workgroup has about the same amount of work, and as
+// far as the shortest estimated time asks: the tiles dealt to the card's `slots`, half of
+// a workgroup's for the uneven end, and the launch that adds up the parts (3 us, and their
+// bytes written and read at 4 TB/s).  1,000 nodes, 4 heads of 32 in float32: forward uncut
+// 31 us, now 18; backward 51, now 39; bfloat16 heads gain less (backward 22, now 17).
+struct Cut {
+  int64_t groups, steps;
+  double us, bytes;   // of a tile; of the parts of one split
+  int splits;
+};
+inline void cut_evenly(Cut* c, int n, int64_t slots, int most) {
+  double total = 0, best = 0;
+  for (int i = 0; i < n; ++i) total += c[i].groups * c[i].steps * c[i].us;
+  int now[2] = {1, 1};
+  for (int k = 0; k <= 4; ++k) {   // k = 0: uncut
+    double sum = 0, longest = 0, join = 0;
+    int64_t groups = 0;
+    for (int i = 0; i < n; ++i) {
+      const int64_t per = k ? std::max<int64_t>(1, (int64_t)std::ceil(total / (k * slots * c[i].us))) : std::max<int64_t>(1, c[i].steps);
+      now[i] = (int)std::min<int64_t>(most, std::max<int64_t>(1, (c[i].steps + per - 1) / per));
+      const double time = c[i].groups ? (double)((c[i].steps + now[i] - 1) / now[i]) * c[i].us : 0.0;
+      sum += c[i].groups * now[i] * time;
+      longest = std::max(longest, time);
+      groups += c[i].groups * now[i];
+      if (now[i] > 1) join += 2 * now[i] * c[i].bytes / 4e6;
+    }
+    if (now[0] > 1 || (n > 1 && now[1] > 1)) join += 3.0;
+    const double time = (groups <= slots ? longest : sum / slots + 0.5 * longest) + join;
+    if (k == 0 || time < best) {
+      best = time;
+      for (int i = 0; i < n; ++i) c[i].splits = now[i];
+    }
+  }
+}
 
 size_t attention_bwd_bytes(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks);
 dsmp_status check_attention(dsmp_handle* h, const dsmp_attention_desc* d, const dsmp_segments* qs, const dsmp_segments* ks);

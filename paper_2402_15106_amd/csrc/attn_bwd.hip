@@ -5,15 +5,15 @@ using namespace dsmp;
 
 namespace {
 
-// Both gradients in one launch, for tiles of 32 rows or keys: the first dq_groups workgroups
-// take those of the queries, the others those of the keys, which form D_i of their rows
-// themselves and so wait for nobody.
+// Both gradients in one launch, for tiles of 32 rows or keys: the first dkv_groups workgroups
+// take those of the keys, which are the longer ones and form D_i of their rows
+// themselves and so wait for nobody; the others those of the queries.
 template <typename T, int D, typename M>
 __global__ __launch_bounds__(BT, D == 128 || (D == 64 && sizeof(T) == 4) ? 1 : 2) void k_attn_bwd_few(AttnArgs a) {
   constexpr int LQ = Bwd<T, D, true, false>::LDS, LK = Bwd<T, D, true, true>::LDS;
   __shared__ __align__(16) unsigned char smem[LQ > LK ? LQ : LK];
-  if (blockIdx.x < a.dq_groups) dq_tile<T, D, true, M>(a, smem, blockIdx.x);
-  else dkv_tile<T, D, true, M>(a, smem, blockIdx.x - a.dq_groups);
+  if (blockIdx.x < a.dkv_groups) dkv_tile<T, D, true, M>(a, smem, blockIdx.x);
+  else dq_tile<T, D, true, M>(a, smem, blockIdx.x - a.dkv_groups);
 }
 
 // The splits of the gradients added up in their order, four values to a thread: those of dq, then
@@ -47,18 +47,22 @@ struct BwdPlan {
 };
 
 // Rows and keys each in tiles of 128 where these fill the card, else of 32, and where these are
-// few as well cut over the other side, 256 of it to a workgroup at least.
+// few as well cut over the other side.
 BwdPlan bwd_plan(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks) {
   const int G = d.heads / d.kv_heads;
   BwdPlan p{false, false, 1, 1, tiles_of(qs.n, qs.n_seg, G, 32 * BW) * d.kv_heads, tiles_of(ks.n, ks.n_seg, 1, 32 * BW) * d.kv_heads};
   p.wide_q = p.grid_q >= FILL, p.wide_k = p.grid_k >= FILL;
   if (!p.wide_q) p.grid_q = tiles_of(qs.n, qs.n_seg, G, 32) * d.kv_heads;
   if (!p.wide_k) p.grid_k = tiles_of(ks.n, ks.n_seg, 1, 32) * d.kv_heads;
-  auto splits = [](int64_t grid, int64_t along) {
-    return grid >= FILL ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(FILL / grid, along / 256));
-  };
-  if (!p.wide_q) p.splits_q = splits(p.grid_q, ks.n / ks.n_seg);
-  if (!p.wide_k) p.splits_k = splits(p.grid_k, qs.n / qs.n_seg * G);
+  // microseconds of a tile, as measured: three products against four; float32 heads over 32 and
+  // bfloat16 ones over 64 leave a SIMD's registers to one wave
+  const bool f32 = d.dtype == DSMP_F32, one = d.head_dim > (f32 ? 32 : 64);
+  const double tile = (f32 ? 6.0 : 1.2) * (d.head_dim <= 32 ? 1 : d.head_dim <= 64 ? (f32 ? 1.2 : 2) : (f32 ? 2.5 : 4));
+  Cut c[2] = {{p.wide_q || !qs.n ? 0 : p.grid_q, (ks.n / ks.n_seg + 127) / 128, 0.75 * tile, 4.0 * qs.n * d.heads * d.head_dim, 1},
+              {p.wide_k || !ks.n ? 0 : p.grid_k, (qs.n / qs.n_seg * G + 127) / 128, tile, 8.0 * ks.n * d.kv_heads * d.head_dim, 1}};
+  cut_evenly(c, 2, one ? FILL / 2 : FILL, 64);
+  if (c[0].groups) p.splits_q = c[0].splits;
+  if (c[1].groups) p.splits_k = c[1].splits;
   p.grid_q *= p.splits_q, p.grid_k *= p.splits_k;
   if (qs.n == 0) p.grid_q = 0;
   if (ks.n == 0) p.grid_k = 0;
@@ -126,7 +130,7 @@ extern "C" dsmp_status dsmp_attention_backward(dsmp_handle* h, const dsmp_attent
   // a launch for keys in wide tiles reads what the queries' has written
   if (p.wide_q && p.grid_q) launch_attention_dq(h, *desc, a, p.grid_q);
   const int64_t few_q = p.wide_q ? 0 : p.grid_q, few_k = p.wide_k ? 0 : p.grid_k;
-  a.dq_groups = (unsigned)few_q;
+  a.dkv_groups = (unsigned)few_k;
   const int64_t joined = ((p.splits_q > 1 ? qs->n * wq : 0) + (p.splits_k > 1 ? 2 * ks->n * wk : 0)) / 4;
   by_attention(*desc, [&](auto t, auto width, auto mode) {
     using T = decltype(t);

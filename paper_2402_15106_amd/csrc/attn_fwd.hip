@@ -411,15 +411,18 @@ struct FwdPlan {
 };
 
 // Rows in tiles of 128 where these fill the card, else of 32, whose keys are dealt to
-// the waves, and where these are few as well to several workgroups of 512 keys at least.
+// the waves, and where these are few as well to several workgroups.
 FwdPlan fwd_plan(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks) {
   const int G = d.heads / d.kv_heads;
   FwdPlan p{false, 1, tiles_of(qs.n, qs.n_seg, G, 32 * NW) * d.kv_heads};
   if (p.grid >= FILL) return p;
   p.few = true;
   p.grid = tiles_of(qs.n, qs.n_seg, G, 32) * d.kv_heads;
-  const int64_t keys = ks.n / ks.n_seg;
-  if (p.grid < FILL) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({2 * FILL / p.grid, keys / 512, MAX_SPLITS}));
+  // microseconds of a tile, as measured; heads over 64 leave a SIMD's registers to one wave
+  const double tile = (d.dtype == DSMP_F32 ? 3.5 : 0.5) * (d.head_dim <= 32 ? 1 : d.head_dim <= 64 ? 2 : 4);
+  Cut c{p.grid, (ks.n / ks.n_seg + 127) / 128, tile, 4.0 * qs.n * d.heads * d.head_dim, 1};
+  cut_evenly(&c, 1, d.head_dim > 64 ? FILL / 2 : FILL, MAX_SPLITS);
+  p.splits = c.splits;
   p.grid *= p.splits;
   return p;
 }
