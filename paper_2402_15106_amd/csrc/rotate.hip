@@ -19,8 +19,6 @@ using namespace dsmp;
 namespace {
 
 constexpr int RT = 256;         // threads of a workgroup
-constexpr int RU = 4;           // heads of a row that are on their way at once (forward)
-constexpr int RUB = 2;          // the same, backward (twice the inputs)
 // Workgroups of a backward pass (their sums of dgamma are kept): as many as the card holds at
 // once; 99,991 x 10 heads of 64: 1,024 of them 103 us, 768 of them 86.
 constexpr int MAX_PARTS = 768;
@@ -131,16 +129,17 @@ __device__ __forceinline__ void angles(const RotArgs& a, int64_t row, int lane, 
       const int axis = p >= 2 * a.per_axis ? 2 : p >= a.per_axis ? 1 : 0;
       // turns in float64: the product of two float32 is exact, and what is left of it in one turn is within 2^-52 of it
       const double turns = (double)a.pos[row * a.axes + axis] * (double)a.freq[p] * 0.15915494309189533577;
-      float sn, cs;
-      sincospif(2.0f * (float)(turns - __builtin_rint(turns)), &sn, &cs);
+      // the hardware's sine and cosine take turns; within 1.3e-7 over one turn (all 2^24 multiples of 2^-24 compared)
+      const float rest = (float)(turns - __builtin_rint(turns));
+      const float sn = __builtin_amdgcn_sinf(rest), cs = __builtin_amdgcn_cosf(rest);
       c[i] = a.amp * cs, s[i] = a.amp * (STEP == 2 || e < half ? -sn : sn);
       if (STEP == 2) c[i + STEP - 1] = c[i], s[i + STEP - 1] = -s[i];
     }
   }
 }
 
-// A row's chunk of heads to a group of lanes.
-template <typename T, int PIECE>
+// A row's chunk of heads to a group of lanes, RU of them on their way at once (1 where the chunks are of one head).
+template <typename T, int PIECE, int RU>
 __global__ __launch_bounds__(RT) void k_rotate(RotArgs a) {
   constexpr int N = VE<T>;
   __shared__ __align__(16) T sh[PIECE ? RU * RT * N : N];
@@ -213,10 +212,10 @@ __global__ __launch_bounds__(RT) void k_rotate(RotArgs a) {
 
 // Backward; workgroups step over the items, so that a lane's sums of dgamma stay in
 // its registers; a workgroup's are added up in a fixed order and kept, [part][2][hd].
-template <typename T, int PIECE>
+template <typename T, int PIECE, int RUB>
 __global__ __launch_bounds__(RT) void k_rotate_bwd(RotArgs a) {
   constexpr int N = VE<T>;
-  constexpr int WORDS = RT * N > RUB * RT * N * (int)sizeof(T) / 4 ? RT * N : RUB * RT * N * (int)sizeof(T) / 4;
+  constexpr int WORDS = std::max(RT / 64 * 2 * MAX_HEAD_DIM, RUB * RT * N * (int)sizeof(T) / 4);
   __shared__ __align__(16) float shf[WORDS];
   T* mine = (T*)shf + ((int)threadIdx.x & ~63) * N * RUB;
   const int groups = RT >> a.lg, group = (int)threadIdx.x >> a.lg, lane = (int)threadIdx.x & ((1 << a.lg) - 1);
@@ -296,17 +295,26 @@ __global__ __launch_bounds__(RT) void k_rotate_bwd(RotArgs a) {
     }
   }
   if (!a.part) return;
+  // the groups of a wave across its lanes, then the waves
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    __syncthreads();
+  for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int i = 0; i < N; ++i) shf[(int)threadIdx.x * N + i] = dg[t][i];
-    __syncthreads();
-    for (int e = (int)threadIdx.x; e < a.hd; e += RT) {
-      float sum = 0.0f;
-      for (int g = 0; g < groups; ++g) sum += shf[(g << a.lg) * N + e];
-      a.part[((int64_t)blockIdx.x * 2 + t) * a.hd + e] = sum;
-    }
+    for (int i = 0; i < N; ++i)
+      for (int o = 1 << a.lg; o < 64; o <<= 1) dg[t][i] += __shfl_xor(dg[t][i], o, 64);
+  __syncthreads();
+  const int wl = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+  if (wl < a.lanes) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < N; ++i) shf[(wave * 2 + t) * a.hd + wl * N + i] = dg[t][i];
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < 2 * a.hd) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < RT / 64; ++k) sum += shf[k * 2 * a.hd + threadIdx.x];
+    a.part[(int64_t)blockIdx.x * 2 * a.hd + threadIdx.x] = sum;
   }
 }
 
@@ -415,7 +423,9 @@ extern "C" dsmp_status dsmp_qk_rotate_forward(dsmp_handle* h, const dsmp_rotate_
   DeviceScope dev(h);
   ProfScope prof(h, DSMP_K_ROTATE);
   by_form(*desc, [&](auto t, auto form) {
-    hipLaunchKernelGGL((k_rotate<decltype(t), decltype(form)::value>), dim3((unsigned)grid), dim3(RT), 0, h->stream, a);
+    constexpr int PIECE = decltype(form)::value;
+    if (a.per == 1) hipLaunchKernelGGL((k_rotate<decltype(t), PIECE, 1>), dim3((unsigned)grid), dim3(RT), 0, h->stream, a);
+    else hipLaunchKernelGGL((k_rotate<decltype(t), PIECE, 4>), dim3((unsigned)grid), dim3(RT), 0, h->stream, a);
   });
   DSMP_LAUNCHED(h, "rotation");
   return DSMP_OK;
@@ -473,7 +483,9 @@ extern "C" dsmp_status dsmp_qk_rotate_backward(dsmp_handle* h, const dsmp_rotate
   if (n > 0) {
     a.parts = bwd_parts(a);
     by_form(*desc, [&](auto t, auto form) {
-      hipLaunchKernelGGL((k_rotate_bwd<decltype(t), decltype(form)::value>), dim3(a.parts), dim3(RT), 0, h->stream, a);
+      constexpr int PIECE = decltype(form)::value;
+      if (a.per == 1) hipLaunchKernelGGL((k_rotate_bwd<decltype(t), PIECE, 1>), dim3(a.parts), dim3(RT), 0, h->stream, a);
+      else hipLaunchKernelGGL((k_rotate_bwd<decltype(t), PIECE, 2>), dim3(a.parts), dim3(RT), 0, h->stream, a);
     });
   }
   if (sums) hipLaunchKernelGGL(k_rotate_columns, dim3(a.hd / 8), dim3(RT), 0, h->stream, a);
