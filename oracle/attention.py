@@ -14,6 +14,9 @@ import numpy as np
 
 HALF, INTERLEAVED = 0, 1
 U = 2.0 ** -24
+# float32 results below this may be 0 instead (the hardware's powers have no subnormal results): weights
+# e^(z - lse) of keys that score 88 below the row's sum, and products with them
+TINY = 2.0 ** -126
 
 
 def pairs_of(rot, layout):
@@ -117,7 +120,7 @@ def attention(q, k, v, q_bounds, k_bounds, scale, cap=0.0, pos_q=None, pos_k=Non
             # a weight and the sum of weights: the score's error, the power's and its argument's difference (8 u of
             # it is in the score's), n additions each in numerator and sum, joined parts
             rel = 2 * ez + (2 * n + 32) * U + err.half
-            e_out[a, h] = rel * (P @ np.abs(v[b, h // G])) + 1.01 * err.half * np.abs(out[a, h])
+            e_out[a, h] = rel * (P @ np.abs(v[b, h // G])) + TINY * np.abs(v[b, h // G]).sum(0) + 1.01 * err.half * np.abs(out[a, h])
             e_lse[a, h] = (ez + (n + 32) * U)[:, 0] + 4 * U * np.abs(lse[a, h]) + 4 * U
     return out, lse, e_out, e_lse
 
@@ -148,8 +151,9 @@ def attention_backward(q, k, v, do, q_bounds, k_bounds, scale, cap=0.0, pos_q=No
             e_D = (np.abs(g) * e_out[a, h]).sum(1, keepdims=True) + (hd + 4) * U * (np.abs(g) * np.abs(o)).sum(1, keepdims=True)
             e_fall = (4 * err.cap_abs + 8 * U + 2 * ez / cap) if cap else 0.0
             e_dS = np.abs(dS) * (eP + 8 * U + err.half) + P * fall * (e_dP + e_D) + P * np.abs(dP - D) * e_fall
+            e_dS = e_dS + TINY * (1.0 + np.abs(dP - D))
             dv[b, j] += P.T @ g
-            ev[b, j] += (P * (eP + err.half + (m + 16) * U)).T @ np.abs(g)
+            ev[b, j] += (P * (eP + err.half + (m + 16) * U) + 2 * TINY).T @ np.abs(g)
             dq[a, h] = scale * (dS @ K)
             eq[a, h] = abs(scale) * (e_dS + (n + 16) * U * np.abs(dS)) @ np.abs(K)
             dk[b, j] += scale * (dS.T @ Q)

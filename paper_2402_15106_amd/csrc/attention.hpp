@@ -104,14 +104,6 @@ __device__ __forceinline__ typename Frag<T>::type lds_rows(lds_u8* X, int pitch,
 template <typename T>
 __device__ __forceinline__ typename Frag<T>::type lds_columns(lds_u8* X, int pitch, int r0, int c0);
 template <>
-__device__ __forceinline__ bf16x8 lds_columns<__bf16>(lds_u8* X, int pitch, int r0, int c0) {
-  const int l = threadIdx.x & 63, g = l >> 4, j = (l >> 2) & 3, q = l & 3;
-  lds_u8* p = X + (r0 + 4 * (g >> 1) + j) * pitch + (c0 + 16 * (g & 1) + 4 * q) * 2;
-  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * pitch));
-  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-template <>
 __device__ __forceinline__ f32x8 lds_columns<float>(lds_u8* X, int pitch, int r0, int c0) {
   const int l = threadIdx.x & 63;
   uint32_t at = (uint32_t)(uintptr_t)(X + (r0 + 4 * (l >> 5)) * pitch + (c0 + (l & 31)) * 4);
@@ -137,7 +129,7 @@ constexpr int pitch_of() {
 }
 
 // ------------------------------------------------------------- guarded global reads
-// Buffer reads of 16 bytes: what begins at or behind `bytes` comes back as zero.
+// Buffer reads: what begins at or behind `bytes` comes back as zero, in LDS too.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr uint32_t NOWHERE = 0x80000000u;   // an offset behind every tile
 
@@ -146,6 +138,66 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* base, ui
 }
 __device__ __forceinline__ u32x4 buffer_read(__amdgpu_buffer_rsrc_t r, uint32_t offset) {
   return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)offset, 0, 0));
+}
+
+// ------------------------------------------------------ tiles of bfloat16 rows in LDS
+// Rows of D values without room between them, copied from memory directly (64 lanes write 1,024
+// bytes in a row; no registers on the way).  The 16-byte units of row r are permuted by
+// XOR with swizzle(r), so that both kinds of reads are free of bank conflicts: eight rows at the
+// same unit (lds_rows), and four rows over four units (lds_columns).  LDS has 64 banks of 4 bytes: a
+// row has 16, 32 or 64 of them, so among eight rows 2, 4 or 8 begin at the same bank.
+template <int D>
+__device__ __forceinline__ int swizzle(int r) {
+  if (D == 32) return (r >> 2) & 1;
+  if (D == 64) return ((r >> 1) & 1) * 4 + ((r >> 2) & 1);
+  return (r & 3) * 4 + ((r >> 2) & 1);
+}
+
+template <int D, int ROWS>
+struct TileCopy {
+  static constexpr int RB = 2 * D, UPR = RB / 16, PER = ROWS * UPR / 256, STEP = 256 / UPR;
+  static_assert(ROWS * UPR % 256 == 0 && STEP % 8 == 0, "whole loads of a workgroup, rows of one permutation to a lane");
+  // a lane's row in its first load, and the unit that it copies there, in bytes
+  static __device__ __forceinline__ int row0() { return (int)threadIdx.x / UPR; }
+  static __device__ __forceinline__ int unit0() { return ((int)threadIdx.x % UPR ^ swizzle<D>(row0())) * 16; }
+  // load i: rows row0 + i STEP, from byte `offset` of the buffer
+  static __device__ __forceinline__ void copy(__amdgpu_buffer_rsrc_t from, lds_u8* to, int i, uint32_t offset) {
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + (i * 4 + wave) * 1024), 16,
+                                             (int)offset, 0, 0, 0);
+  }
+};
+
+// ------------------------------------------------------------- operands from tiles
+// As lds_rows and lds_columns; bfloat16 tiles as above, float32 ones with a pitch of 16 bytes more than a row.
+// A lane's place in a bfloat16 tile's first 32 rows: reads of other columns flip bits of it.
+struct LanePlace {
+  uint32_t rows, columns;
+};
+template <int D>
+__device__ __forceinline__ LanePlace lane_place() {
+  const int l = (int)threadIdx.x & 63, g = l >> 4, j = (l >> 2) & 3, q = l & 3, r = l & 31, c = 4 * (g >> 1) + j;
+  return {(uint32_t)(r * 2 * D + ((l >> 5) ^ swizzle<D>(r)) * 16),
+          (uint32_t)(c * 2 * D + ((2 * (g & 1) + (q >> 1)) ^ swizzle<D>(c)) * 16 + 8 * (q & 1))};
+}
+// The flipped places are formed where they are used: kept over a loop they would take a register each.
+__device__ __forceinline__ void formed_here(LanePlace& p) { asm volatile("" : "+v"(p.rows), "+v"(p.columns)); }
+
+template <typename T, int D>
+__device__ __forceinline__ typename Frag<T>::type tile_rows(lds_u8* X, const LanePlace& at, int r0, int t) {
+  if constexpr (sizeof(T) == 4) return lds_rows<T>(X, pitch_of<T, D, true>(), r0, 16 * t);
+  else return *(__attribute__((address_space(3))) bf16x8*)(X + r0 * 2 * D + (at.rows ^ (uint32_t)(32 * t)));
+}
+template <typename T, int D>
+__device__ __forceinline__ typename Frag<T>::type tile_columns(lds_u8* X, const LanePlace& at, int r0, int c0) {
+  if constexpr (sizeof(T) == 4) {
+    return lds_columns<T>(X, pitch_of<T, D, true>(), r0, c0);
+  } else {
+    lds_u8* p = X + r0 * 2 * D + (at.columns ^ (uint32_t)(2 * c0));
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * 2 * D));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
 }
 
 // A lane's eight values at p (16-byte aligned), or zeros.
@@ -157,6 +209,8 @@ __device__ __forceinline__ typename Frag<T>::type read_frag(const T* p, bool the
   if (there) f = *(const typename Frag<T>::type*)p;
   return f;
 }
+
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 
 // Four values of a row of results, rounded.
 template <typename T>
@@ -256,6 +310,24 @@ __device__ __forceinline__ Place place_of(const float* pos, int dim, int64_t row
   return p;
 }
 
+// Coordinates of BN rows from `row` on (those that there are: `rem`), copied to `to`, one array of BN to each
+// coordinate: one wave to each.  Arrays that are not there are cleared once instead.
+template <int BN>
+__device__ __forceinline__ void copy_places(const float* pos, int dim, int64_t row, int rem, float* to) {
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = (int)threadIdx.x & 63;
+  if (wave >= dim) return;
+  const auto from = buffer_of(pos + row * dim, (uint32_t)(rem * dim * 4));
+#pragma unroll
+  for (int i = 0; i < BN / 64; ++i)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(lds_u8*)(to + wave * BN + 64 * i), 4,
+                                             ((64 * i + l) * dim + wave) * 4, 0, 0, 0);
+}
+template <int BN>
+__device__ __forceinline__ void clear_places(int there, int dim, float* to) {
+  for (int c = there; c < dim; ++c)
+    if ((int)threadIdx.x < BN) to[c * BN + threadIdx.x] = 0.0f;
+}
+
 __device__ __forceinline__ float distance(int dim, const Place& a, float x, float y, float z) {
   const float dx = a.x - x, dy = a.y - y;
   float d = fmaf(dy, dy, dx * dx);
@@ -311,12 +383,14 @@ struct Score {
   }
 };
 
-// An operand of x with the score's sign.
-template <typename F>
-__device__ __forceinline__ void apply_sign(F& f, float sign) {
+// N operands of x with the score's sign.
+template <int N, typename F>
+__device__ __forceinline__ void apply_sign(F* f, float sign) {
   if (sign == 1.0f) return;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) f[e] = sign == 0.0f ? 0.0f : -(float)f[e];
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[k][e] = sign == 0.0f ? 0.0f : -(float)f[k][e];
 }
 
 inline AttnArgs attn_args(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks) {

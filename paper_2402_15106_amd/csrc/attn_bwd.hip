@@ -8,12 +8,14 @@ namespace {
 // Both gradients in one launch, for tiles of 32 rows or keys: the first dkv_groups workgroups
 // take those of the keys, which are the longer ones and form D_i of their rows
 // themselves and so wait for nobody; the others those of the queries.
-template <typename T, int D, typename M>
+// ROLE 1 and 2: the one or the other alone (wide heads in float32: both together leave the scalar
+// registers no room).
+template <typename T, int D, int ROLE, typename M>
 __global__ __launch_bounds__(BT, D == 128 || (D == 64 && sizeof(T) == 4) ? 1 : 2) void k_attn_bwd_few(AttnArgs a) {
-  constexpr int LQ = Bwd<T, D, true, false>::LDS, LK = Bwd<T, D, true, true>::LDS;
-  __shared__ __align__(16) unsigned char smem[LQ > LK ? LQ : LK];
-  if (blockIdx.x < a.dkv_groups) dkv_tile<T, D, true, M>(a, smem, blockIdx.x);
-  else dq_tile<T, D, true, M>(a, smem, blockIdx.x - a.dkv_groups);
+  using C = Bwd<T, D, true, true>;   // the larger of both
+  DSMP_BWD_LDS(C, lds);
+  if (ROLE == 1 || (ROLE == 0 && blockIdx.x < a.dkv_groups)) dkv_tile<T, D, true, false, M>(a, lds, blockIdx.x);
+  else dq_tile<T, D, true, M>(a, lds, blockIdx.x - (ROLE == 0 ? a.dkv_groups : 0));
 }
 
 // The splits of the gradients added up in their order, four values to a thread: those of dq, then
@@ -134,9 +136,14 @@ extern "C" dsmp_status dsmp_attention_backward(dsmp_handle* h, const dsmp_attent
   const int64_t joined = ((p.splits_q > 1 ? qs->n * wq : 0) + (p.splits_k > 1 ? 2 * ks->n * wk : 0)) / 4;
   by_attention(*desc, [&](auto t, auto width, auto mode) {
     using T = decltype(t);
-    if (few_q + few_k)
-      hipLaunchKernelGGL((k_attn_bwd_few<T, decltype(width)::value, decltype(mode)>), dim3((unsigned)(few_q + few_k)), dim3(BT), 0,
-                         h->stream, a);
+    constexpr int D = decltype(width)::value;
+    using M = decltype(mode);
+    if constexpr (sizeof(T) == 4 && D == 128) {
+      if (few_k) hipLaunchKernelGGL((k_attn_bwd_few<T, D, 1, M>), dim3((unsigned)few_k), dim3(BT), 0, h->stream, a);
+      if (few_q) hipLaunchKernelGGL((k_attn_bwd_few<T, D, 2, M>), dim3((unsigned)few_q), dim3(BT), 0, h->stream, a);
+    } else if (few_q + few_k) {
+      hipLaunchKernelGGL((k_attn_bwd_few<T, D, 0, M>), dim3((unsigned)(few_q + few_k)), dim3(BT), 0, h->stream, a);
+    }
     if (joined) hipLaunchKernelGGL((k_attn_bwd_join<T>), dim3(ceil_div(joined, BT)), dim3(BT), 0, h->stream, a);
   });
   if (p.wide_k && p.grid_k) launch_attention_dkv(h, *desc, a, p.grid_k);

@@ -18,25 +18,35 @@ constexpr int BT = 256, BW = 4;   // threads and waves of a workgroup
 
 // WIDE: 32 rows (or keys) to a wave, 128 to a workgroup, all keys (rows) of a tile to every wave.
 // FEW: 32 to a workgroup, a quarter of a tile's keys (rows) to each wave; joined at the end.
-// KEYS_OWNED: dkv_tile, whose two streamed matrices are both read both ways.
+// KEYS_OWNED: dkv_tile.  bfloat16 tiles are copied into two buffers in turn, one barrier to a tile; float32
+// ones wait in registers.
 template <typename T, int D, bool FEW, bool KEYS_OWNED>
 struct Bwd {
+  static constexpr bool DMA = sizeof(T) == 2;
   static constexpr int OWN = FEW ? 32 : 32 * BW;
-  static constexpr int BN = FEW ? 32 * BW : sizeof(T) == 2 ? 64 : 32;
+  static constexpr int BN = FEW ? 32 * BW : DMA ? 64 : 32;
   static constexpr int SUB = FEW ? 1 : BN / 32;
-  static constexpr int P0 = pitch_of<T, D, false>(), P1 = pitch_of<T, D, !KEYS_OWNED>();
+  static constexpr int PITCH = DMA ? 2 * D : pitch_of<T, D, true>(), MATRIX = BN * PITCH;
+  static constexpr int EXTRA = (KEYS_OWNED ? 6 : 3) * BN;   // float32 of the rows that go along
+  // float32: 16-byte units to a thread; the next tile waits in registers, but for FEW's large ones: those come one at a time
   static constexpr int PER = BN * D * (int)sizeof(T) / 16 / BT, STEP = BT * 16 / (D * (int)sizeof(T));
-  // the next tile waits in registers, but for FEW's large ones in float32: those come two units at a time
-  static constexpr bool AHEAD = !(FEW && sizeof(T) == 4 && D == 128);
-  static constexpr int HELD = AHEAD || PER < 2 ? PER : 2;
-  static constexpr int EXTRA = KEYS_OWNED ? 6 : 3;   // float32 of a row that go along
-  static constexpr int TILE = BN * (P0 + P1) + EXTRA * BN * 4;
-  static constexpr int JOIN = FEW ? BW * 32 * D * 4 : 0;
-  static constexpr int LDS = TILE > JOIN ? TILE : JOIN;
+  static constexpr bool AHEAD = !(FEW && D == 128);
+  static constexpr int HELD = AHEAD ? PER : 1;
+  static_assert(!FEW || MATRIX >= 2 * 32 * D * 4, "two waves' parts fit into a matrix");
   static_assert(PER >= 1 && PER * BT * 16 == BN * D * (int)sizeof(T), "whole units for every thread");
 };
 
-typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+// A workgroup's LDS: two buffers of two matrices and what goes along.  They are arrays of their own
+// in the kernels, so that a copy into one buffer is not waited for by reads of the other.
+struct BwdLds {
+  unsigned char *a0, *b0, *a1, *b1;
+  float *extra0, *extra1;
+};
+#define DSMP_BWD_LDS(C, name)                                                                                     \
+  __shared__ __align__(1024) unsigned char name##a0[C::MATRIX], name##b0[C::MATRIX], name##a1[C::DMA ? C::MATRIX : 16], \
+      name##b1[C::DMA ? C::MATRIX : 16];                                                                          \
+  __shared__ __align__(16) float name##x0[C::EXTRA], name##x1[C::DMA ? C::EXTRA : 4];                             \
+  const BwdLds name{name##a0, name##b0, name##a1, name##b1, name##x0, name##x1}
 
 // A wave's 32 rows of results (D values each, a lane's column), scaled: to `out`, or in float32 to `part`.
 template <typename T, int D>
@@ -54,16 +64,17 @@ __device__ __forceinline__ void write_rows(const f32x16* acc, float scale, T* ou
     }
 }
 
-// The four waves' results of the same 32 rows added up in LDS ([wave][value][row]) and written:
-// 256 threads with a row and four values in 32 each.
+// The four waves' results of the same 32 rows added up in LDS ([value][row], two waves' in each of a buffer's
+// matrices) and written: 256 threads with a row and four values in 32 each.
 template <typename T, int D>
-__device__ __forceinline__ void join_rows(const f32x16* acc, float* join, float scale, T* out, float* part, int hd, bool there) {
+__device__ __forceinline__ void join_rows(const f32x16* acc, const BwdLds& lds, float scale, T* out, float* part, int hd, bool there) {
   const int tid = (int)threadIdx.x, l = tid & 63, w = tid >> 6;
+  auto part_of = [&](int wave) { return (float*)(wave < 2 ? lds.a0 : lds.b0) + (wave & 1) * 32 * D; };
   __syncthreads();
 #pragma unroll
   for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) join[(w * D + 32 * d + result_row(i)) * 32 + (l & 31)] = acc[d][i];
+    for (int i = 0; i < 16; ++i) part_of(w)[(32 * d + result_row(i)) * 32 + (l & 31)] = acc[d][i];
   __syncthreads();
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) {
@@ -74,7 +85,7 @@ __device__ __forceinline__ void join_rows(const f32x16* acc, float* join, float 
     for (int e = 0; e < 4; ++e) {
       v[e] = 0.0f;
 #pragma unroll
-      for (int k = 0; k < BW; ++k) v[e] += join[(k * D + c + e) * 32 + (l & 31)];
+      for (int k = 0; k < BW; ++k) v[e] += part_of(k)[(c + e) * 32 + (l & 31)];
       v[e] *= scale;
     }
     if (part) *(float4*)(part + c) = make_float4(v[0], v[1], v[2], v[3]);
@@ -83,13 +94,10 @@ __device__ __forceinline__ void join_rows(const f32x16* acc, float* join, float 
 }
 
 template <typename T, int D, bool FEW, typename M>
-__device__ __forceinline__ void dq_tile(const AttnArgs& a, unsigned char* smem, unsigned group) {
+__device__ __forceinline__ void dq_tile(const AttnArgs& a, const BwdLds& lds, unsigned group) {
   using C = Bwd<T, D, FEW, false>;
   constexpr int ES = sizeof(T), KS = D / 16, DB = D / 32;
   typedef typename Frag<T>::type frag;
-  lds_u8* ldsK = (lds_u8*)smem;
-  lds_u8* ldsV = ldsK + C::BN * C::P0;
-  float* places = (float*)(smem + C::BN * (C::P0 + C::P1));
 
   const int tid = (int)threadIdx.x, l = tid & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = (int)(group % (unsigned)a.Hk);
@@ -121,8 +129,8 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, unsigned char* smem, 
     const frag of = read_frag<T>((const T*)a.o + row.query * a.ldo + row.head * a.hd + c, in);
 #pragma unroll
     for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[t][e], (float)of[e], delta);
-    apply_sign(qf[t], sc.sign);
   }
+  apply_sign<KS>(qf, sc.sign);
   delta += other_half(delta);
   if (row.there && h == 0 && split == 0 && (!FEW || w == 0)) a.delta[slot] = delta;
   // the exponent of a weight is A u + shift; a row without keys has the weights 0
@@ -131,49 +139,16 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, unsigned char* smem, 
   float slope = 0.0f;
   if (dim && a.dim && row.there) me = place_of(a.pos_q, a.dim, row.query), slope = a.slopes[row.head] * sc.per_slope;
 
-  const int row0 = tid / (D * ES / 16), c0 = tid % (D * ES / 16) * 16;
-  const bool in = c0 < a.hd * ES;
-  const uint32_t offK = in ? (uint32_t)(row0 * a.ldk * ES + c0) : NOWHERE, stepK = (uint32_t)(C::STEP * a.ldk * ES);
-  const uint32_t offV = in ? (uint32_t)(row0 * a.ldv * ES + c0) : NOWHERE, stepV = (uint32_t)(C::STEP * a.ldv * ES);
-  u32x4 regK[C::HELD], regV[C::HELD];
-  Place key{0.0f, 0.0f, 0.0f};
-  auto fetch = [&](int t, int i0) {
-    const int64_t j0 = k0 + (int64_t)t * C::BN;
-    const int rem = (int)min((int64_t)C::BN, klen - (int64_t)t * C::BN);
-    const auto bk = buffer_of((const T*)a.k + j0 * a.ldk + kvh * a.hd, (uint32_t)(rem * a.ldk * ES));
-    const auto bv = buffer_of((const T*)a.v + j0 * a.ldv + kvh * a.hd, (uint32_t)(rem * a.ldv * ES));
-#pragma unroll
-    for (int i = 0; i < C::HELD; ++i)
-      regK[i] = buffer_read(bk, offK + (i0 + i) * stepK), regV[i] = buffer_read(bv, offV + (i0 + i) * stepV);
-    if (dim && a.dim && i0 == 0 && tid < rem) key = place_of(a.pos_k, a.dim, j0 + tid);
-  };
-  auto put = [&](int i0) {
-#pragma unroll
-    for (int i = 0; i < C::HELD; ++i) {
-      const int r = row0 + (i0 + i) * C::STEP;
-      *(lds_u32x4*)(ldsK + r * C::P0 + c0) = regK[i];
-      *(lds_u32x4*)(ldsV + r * C::P1 + c0) = regV[i];
-    }
-    if (dim && i0 == 0 && tid < C::BN) places[tid] = key.x, places[C::BN + tid] = key.y, places[2 * C::BN + tid] = key.z;
-  };
-
   f32x16 acc[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) acc[d] = f32x16{};
 
-  if (C::AHEAD && t_begin < t_end) fetch(t_begin, 0);
-  for (int t = t_begin; t < t_end; ++t) {
-    __syncthreads();
-    if (C::AHEAD) {
-      put(0);
-    } else {
-#pragma unroll 1
-      for (int i0 = 0; i0 < C::PER; i0 += C::HELD) fetch(t, i0), put(i0);
-    }
-    __syncthreads();
-    if (C::AHEAD && t + 1 < t_end) fetch(t + 1, 0);
+  const LanePlace place = lane_place<D>();
+  auto step = [&](lds_u8* ldsK, lds_u8* ldsV, const float* places, int t) {
     const int rem = (int)min((int64_t)C::BN, klen - (int64_t)t * C::BN);
-    if (FEW && 32 * w >= rem) continue;
+    if (FEW && 32 * w >= rem) return;
+    LanePlace lane = place;
+    formed_here(lane);
 #pragma unroll
     for (int b = 0; b < C::SUB; ++b) {
       const int at = 32 * ((FEW ? w : 0) + b);
@@ -182,11 +157,11 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, unsigned char* smem, 
 #pragma unroll
       for (int i = 0; i < 16; ++i) dp[i] = -delta;
       frag kf[2], vf[2];
-      kf[0] = lds_rows<T>(ldsK, C::P0, at, 0), vf[0] = lds_rows<T>(ldsV, C::P1, at, 0);
+      kf[0] = tile_rows<T, D>(ldsK, lane, at, 0), vf[0] = tile_rows<T, D>(ldsV, lane, at, 0);
 #pragma unroll
       for (int t2 = 0; t2 < KS; ++t2) {
         if (t2 + 1 < KS)
-          kf[(t2 + 1) & 1] = lds_rows<T>(ldsK, C::P0, at, 16 * (t2 + 1)), vf[(t2 + 1) & 1] = lds_rows<T>(ldsV, C::P1, at, 16 * (t2 + 1));
+          kf[(t2 + 1) & 1] = tile_rows<T, D>(ldsK, lane, at, t2 + 1), vf[(t2 + 1) & 1] = tile_rows<T, D>(ldsV, lane, at, t2 + 1);
         x = mma(kf[t2 & 1], qf[t2], x);
         dp = mma(vf[t2 & 1], gf[t2], dp);
         __builtin_amdgcn_sched_barrier(0);
@@ -208,28 +183,106 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, unsigned char* smem, 
           x[i] = exp2_of(fmaf(u, sc.A, shift)) * dp[i];
           if (cap) x[i] *= fall;
         }
+        if (dim) __builtin_amdgcn_sched_barrier(0);
       }
       if (at + 32 > rem) {   // behind the last key
+        int left = rem - at - 4 * h;
+        asm volatile("" : "+v"(left));   // compared with constants, not with sixteen row numbers kept over the loop
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (at + result_row(i) >= rem) x[i] = 0.0f;
+          if (8 * (i >> 2) + (i & 3) >= left) x[i] = 0.0f;
       }
       __builtin_amdgcn_sched_barrier(0);
-      frag cf[2][DB];
+      frag cf[2], f{};
+      cf[0] = tile_columns<T, D>(ldsK, lane, at, 0);
 #pragma unroll
-      for (int d = 0; d < DB; ++d) cf[0][d] = lds_columns<T>(ldsK, C::P0, at, 32 * d);
+      for (int k = 0; k < 2 * DB; ++k) {
+        const int t2 = k / DB, d = k % DB;
+        if (d == 0) {
+          float v[8];
 #pragma unroll
-      for (int t2 = 0; t2 < 2; ++t2) {
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = x[8 * t2 + i];
-        const frag f = to_frag<T>(v);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          if (t2 == 0) cf[1][d] = lds_columns<T>(ldsK, C::P0, at + 16, 32 * d);
-          acc[d] = mma(cf[t2][d], f, acc[d]);
+          for (int i = 0; i < 8; ++i) v[i] = x[8 * t2 + i];
+          f = to_frag<T>(v);
         }
+        if (k + 1 < 2 * DB) cf[(k + 1) & 1] = tile_columns<T, D>(ldsK, lane, at + 16 * ((k + 1) / DB), 32 * ((k + 1) % DB));
+        acc[d] = mma(cf[k & 1], f, acc[d]);
+        if (d & 1 || DB == 1) __builtin_amdgcn_sched_barrier(0);
       }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int d = 0; d < DB; ++d) asm volatile("" : "+v"(acc[d]));   // one place for the sums after either buffer's tile
+  };
+
+  const T* keys = (const T*)a.k + k0 * a.ldk + kvh * a.hd;
+  const T* values = (const T*)a.v + k0 * a.ldv + kvh * a.hd;
+  if constexpr (C::DMA) {
+    using TC = TileCopy<D, C::BN>;
+    const bool in = TC::unit0() < a.hd * ES;
+    const uint32_t offK = in ? (uint32_t)(TC::row0() * a.ldk * ES + TC::unit0()) : NOWHERE, stepK = (uint32_t)(TC::STEP * a.ldk * ES);
+    const uint32_t offV = in ? (uint32_t)(TC::row0() * a.ldv * ES + TC::unit0()) : NOWHERE, stepV = (uint32_t)(TC::STEP * a.ldv * ES);
+    auto copy = [&](int t, lds_u8* toK, lds_u8* toV, float* places) {
+      const int64_t j = (int64_t)t * C::BN;
+      const int rem = (int)min((int64_t)C::BN, klen - j);
+      const auto bk = buffer_of(keys + j * a.ldk, (uint32_t)(rem * a.ldk * ES));
+      const auto bv = buffer_of(values + j * a.ldv, (uint32_t)(rem * a.ldv * ES));
+#pragma unroll
+      for (int i = 0; i < TC::PER; ++i) TC::copy(bk, toK, i, offK + i * stepK), TC::copy(bv, toV, i, offV + i * stepV);
+      if (dim) copy_places<C::BN>(a.pos_k, a.dim, k0 + j, rem, places);
+    };
+    if (dim) clear_places<C::BN>(a.dim, dim, lds.extra0), clear_places<C::BN>(a.dim, dim, lds.extra1);
+    if (t_begin < t_end) copy(t_begin, (lds_u8*)lds.a0, (lds_u8*)lds.b0, lds.extra0);
+    for (int t = t_begin; t < t_end; t += 2) {
+      stage_wait();
+      __syncthreads();   // the tile is there, and all waves have left the other buffer
+      if (t + 1 < t_end) copy(t + 1, (lds_u8*)lds.a1, (lds_u8*)lds.b1, lds.extra1);
+      step((lds_u8*)lds.a0, (lds_u8*)lds.b0, lds.extra0, t);
+      if (t + 1 < t_end) {   // no second way out of the loop: the sums would have a second place for it
+        stage_wait();
+        __syncthreads();
+        if (t + 2 < t_end) copy(t + 2, (lds_u8*)lds.a0, (lds_u8*)lds.b0, lds.extra0);
+        step((lds_u8*)lds.a1, (lds_u8*)lds.b1, lds.extra1, t + 1);
+      }
+    }
+  } else {
+    const int row0 = tid / (D * ES / 16), c0 = tid % (D * ES / 16) * 16;
+    const bool in = c0 < a.hd * ES;
+    const uint32_t offK = in ? (uint32_t)(row0 * a.ldk * ES + c0) : NOWHERE, stepK = (uint32_t)(C::STEP * a.ldk * ES);
+    const uint32_t offV = in ? (uint32_t)(row0 * a.ldv * ES + c0) : NOWHERE, stepV = (uint32_t)(C::STEP * a.ldv * ES);
+    u32x4 regK[C::HELD], regV[C::HELD];
+    Place key{0.0f, 0.0f, 0.0f};
+    auto fetch = [&](int t, int i0) {
+      const int64_t j = (int64_t)t * C::BN;
+      const int rem = (int)min((int64_t)C::BN, klen - j);
+      const auto bk = buffer_of(keys + j * a.ldk, (uint32_t)(rem * a.ldk * ES));
+      const auto bv = buffer_of(values + j * a.ldv, (uint32_t)(rem * a.ldv * ES));
+#pragma unroll
+      for (int i = 0; i < C::HELD; ++i)
+        regK[i] = buffer_read(bk, offK + (i0 + i) * stepK), regV[i] = buffer_read(bv, offV + (i0 + i) * stepV);
+      if (dim && a.dim && i0 == 0 && tid < rem) key = place_of(a.pos_k, a.dim, k0 + j + tid);
+    };
+    auto put = [&](int i0) {
+#pragma unroll
+      for (int i = 0; i < C::HELD; ++i) {
+        const int at = (row0 + (i0 + i) * C::STEP) * C::PITCH + c0;
+        *(lds_u32x4*)((lds_u8*)lds.a0 + at) = regK[i];
+        *(lds_u32x4*)((lds_u8*)lds.b0 + at) = regV[i];
+      }
+      float* places = lds.extra0;
+      if (dim && i0 == 0 && tid < C::BN) places[tid] = key.x, places[C::BN + tid] = key.y, places[2 * C::BN + tid] = key.z;
+    };
+    if (C::AHEAD && t_begin < t_end) fetch(t_begin, 0);
+    for (int t = t_begin; t < t_end; ++t) {
+      __syncthreads();
+      if (C::AHEAD) {
+        put(0);
+      } else {
+#pragma unroll 1
+        for (int i0 = 0; i0 < C::PER; i0 += C::HELD) fetch(t, i0), put(i0);
+      }
+      __syncthreads();
+      if (C::AHEAD && t + 1 < t_end) fetch(t + 1, 0);
+      step((lds_u8*)lds.a0, (lds_u8*)lds.b0, lds.extra0, t);
     }
   }
 
@@ -238,18 +291,17 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, unsigned char* smem, 
   const RowOf mine = row_of(a, q0, r0, R, kvh, FEW, again);
   T* out = (T*)a.gq + mine.query * a.ldgq + mine.head * a.hd;
   float* part = FEW && a.splits > 1 ? a.part + ((int64_t)split * a.nq * a.H + mine.query * a.H + mine.head) * a.hd : nullptr;
-  if (FEW) join_rows<T, D>(acc, (float*)smem, a.scale, out, part, a.hd, mine.there);
+  if (FEW) join_rows<T, D>(acc, lds, a.scale, out, part, a.hd, mine.there);
   else if (mine.there) write_rows<T, D>(acc, a.scale, out, nullptr, a.hd);
 }
 
-template <typename T, int D, bool FEW, typename M>
-__device__ __forceinline__ void dkv_tile(const AttnArgs& a, unsigned char* smem, unsigned group) {
+// PAIRED: an even number of heads share their keys, so that rows two by two have the same query, and the
+// same distance.
+template <typename T, int D, bool FEW, bool PAIRED, typename M>
+__device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, unsigned group) {
   using C = Bwd<T, D, FEW, true>;
   constexpr int ES = sizeof(T), KS = D / 16, DB = D / 32, UNITS = D * ES / 16;
   typedef typename Frag<T>::type frag;
-  lds_u8* ldsQ = (lds_u8*)smem;
-  lds_u8* ldsG = ldsQ + C::BN * C::P0;
-  float* rows = (float*)(smem + C::BN * (C::P0 + C::P1));   // shift, -D, slope, x, y, z of the tile's rows
 
   const int tid = (int)threadIdx.x, l = tid & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = (int)(group % (unsigned)a.Hk);
@@ -279,90 +331,21 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, unsigned char* smem,
       const int c = 16 * t + 8 * h;
       kf[t] = read_frag<T>((const T*)a.k + key * a.ldk + kvh * a.hd + c, there && c < a.hd);
       vf[t] = read_frag<T>((const T*)a.v + key * a.ldv + kvh * a.hd + c, there && c < a.hd);
-      apply_sign(kf[t], sc.sign);
     }
+    apply_sign<KS>(kf, sc.sign);
     if (dim && a.dim && there) me = place_of(a.pos_k, a.dim, key);
   }
-
-  const int row0 = tid / UNITS, c0 = tid % UNITS * 16;
-  const bool in = c0 < a.hd * ES;
-  u32x4 regQ[C::HELD], regG[C::HELD];
-  float dots[C::HELD];   // FEW: this unit's part of dO . o
-  float rl = -INFINITY, rd = 0.0f, rs = 0.0f;
-  Place rp{0.0f, 0.0f, 0.0f};
-  auto fetch = [&](int t, int i0) {
-    const unsigned base = (unsigned)t * C::BN;   // rows before this tile
-    const unsigned f0 = base / (unsigned)a.G, g0 = base - f0 * a.G;
-    const int64_t left = queries - f0, at = q0 + f0;
-    const int rem = (int)min((int64_t)C::BN + 1, left);
-    const int64_t side = (int64_t)kvh * a.G * a.hd;
-    const auto bq = buffer_of((const T*)a.q + at * a.ldq + side, (uint32_t)(rem * a.ldq * ES));
-    const auto bg = buffer_of((const T*)a.go + at * a.ldgo + side, (uint32_t)(rem * a.ldgo * ES));
-    const auto bo = buffer_of((const T*)a.o + at * a.ldo + side, (uint32_t)(rem * a.ldo * ES));
-#pragma unroll
-    for (int i = 0; i < C::HELD; ++i) {
-      const uint32_t x = g0 + row0 + (i0 + i) * C::STEP, qi = (x * a.g_inv) >> 20, g = x - qi * a.G;
-      const uint32_t off = g * (uint32_t)(a.hd * ES) + c0;
-      const bool got = in && (int)qi < rem;
-      regQ[i] = buffer_read(bq, got ? qi * (uint32_t)(a.ldq * ES) + off : NOWHERE);
-      regG[i] = buffer_read(bg, got ? qi * (uint32_t)(a.ldgo * ES) + off : NOWHERE);
-      if (FEW) {
-        const u32x4 regO = buffer_read(bo, got ? qi * (uint32_t)(a.ldo * ES) + off : NOWHERE);
-        typedef T unit __attribute__((ext_vector_type(16 / ES)));
-        const unit gv = __builtin_bit_cast(unit, regG[i]), ov = __builtin_bit_cast(unit, regO);
-        dots[i] = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 16 / ES; ++e) dots[i] = fmaf((float)gv[e], (float)ov[e], dots[i]);
-      }
-    }
-    if (i0 == 0 && tid < C::BN) {
-      const uint32_t x = g0 + tid, qi = (x * a.g_inv) >> 20, g = x - qi * a.G;
-      rl = -INFINITY, rd = 0.0f, rs = 0.0f, rp = Place{0.0f, 0.0f, 0.0f};
-      if ((int64_t)qi < left) {
-        const int64_t query = at + qi, slot = query * a.H + kvh * a.G + g;
-        const float lse = a.lse_in[slot];
-        rl = lse == -INFINITY ? -INFINITY : sc.C - lse * LOG2E;
-        if (!FEW) rd = -a.delta[slot];
-        if (dim && a.dim) rp = place_of(a.pos_q, a.dim, query), rs = a.slopes[kvh * a.G + g] * sc.per_slope;
-      }
-    }
-  };
-  auto put = [&](int i0) {
-#pragma unroll
-    for (int i = 0; i < C::HELD; ++i) {
-      const int r = row0 + (i0 + i) * C::STEP;
-      *(lds_u32x4*)(ldsQ + r * C::P0 + c0) = regQ[i];
-      *(lds_u32x4*)(ldsG + r * C::P1 + c0) = regG[i];
-      if (FEW) {   // the units of a row are a row of lanes
-        float d = dots[i];
-#pragma unroll
-        for (int o = 1; o < UNITS; o <<= 1) d += __shfl_xor(d, o, 64);
-        if (c0 == 0) rows[C::BN + r] = -d;
-      }
-    }
-    if (i0 == 0 && tid < C::BN) {
-      rows[tid] = rl;
-      if (!FEW) rows[C::BN + tid] = rd;
-      if (dim) rows[2 * C::BN + tid] = rs, rows[3 * C::BN + tid] = rp.x, rows[4 * C::BN + tid] = rp.y, rows[5 * C::BN + tid] = rp.z;
-    }
-  };
 
   f32x16 dk[DB], dv[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) dk[d] = f32x16{}, dv[d] = f32x16{};
 
-  if (C::AHEAD && t_begin < t_end) fetch(t_begin, 0);
-  for (int t = t_begin; t < t_end; ++t) {
-    __syncthreads();
-    if (C::AHEAD) {
-      put(0);
-    } else {
-#pragma unroll 1
-      for (int i0 = 0; i0 < C::PER; i0 += C::HELD) fetch(t, i0), put(i0);
-    }
-    __syncthreads();
-    if (C::AHEAD && t + 1 < t_end) fetch(t + 1, 0);
-    if (FEW && (int64_t)t * C::BN + 32 * w >= R) continue;
+  const LanePlace place = lane_place<D>();
+  // rows: shift, -D, slope, x, y, z of the tile's rows
+  auto step = [&](lds_u8* ldsQ, lds_u8* ldsG, const float* rows, int t) {
+    if (FEW && (int64_t)t * C::BN + 32 * w >= R) return;
+    LanePlace lane = place;
+    formed_here(lane);
 #pragma unroll
     for (int b = 0; b < C::SUB; ++b) {
       const int at = 32 * ((FEW ? w : 0) + b);
@@ -374,11 +357,12 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, unsigned char* smem,
         for (int e = 0; e < 4; ++e) dp[4 * i4 + e] = (&d.x)[e];
       }
       frag rq[2], rg[2];
-      rq[0] = lds_rows<T>(ldsQ, C::P0, at, 0), rg[0] = lds_rows<T>(ldsG, C::P1, at, 0);
+      rq[0] = tile_rows<T, D>(ldsQ, lane, at, 0), rg[0] = tile_rows<T, D>(ldsG, lane, at, 0);
 #pragma unroll
       for (int t2 = 0; t2 < KS; ++t2) {
-        if (t2 + 1 < KS)
-          rq[(t2 + 1) & 1] = lds_rows<T>(ldsQ, C::P0, at, 16 * (t2 + 1)), rg[(t2 + 1) & 1] = lds_rows<T>(ldsG, C::P1, at, 16 * (t2 + 1));
+        if (ES == 4 && D == 128 && t2 > 0) rq[t2 & 1] = tile_rows<T, D>(ldsQ, lane, at, t2), rg[t2 & 1] = tile_rows<T, D>(ldsG, lane, at, t2);
+        if (!(ES == 4 && D == 128) && t2 + 1 < KS)
+          rq[(t2 + 1) & 1] = tile_rows<T, D>(ldsQ, lane, at, t2 + 1), rg[(t2 + 1) & 1] = tile_rows<T, D>(ldsG, lane, at, t2 + 1);
         x = mma(rq[t2 & 1], kf[t2], x);
         dp = mma(rg[t2 & 1], vf[t2], dp);
         __builtin_amdgcn_sched_barrier(0);
@@ -387,43 +371,195 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, unsigned char* smem,
       for (int i4 = 0; i4 < 4; ++i4) {
         const float* row = rows + at + 8 * i4 + 4 * h;
         const float4 shift = *(const float4*)row;
-        float4 sl{}, px{}, py{}, pz{};
+        float4 sl{}, far{};
         if (dim) {
-          sl = *(const float4*)(row + 2 * C::BN), px = *(const float4*)(row + 3 * C::BN), py = *(const float4*)(row + 4 * C::BN);
+          sl = *(const float4*)(row + 2 * C::BN);
+          const float4 px = *(const float4*)(row + 3 * C::BN), py = *(const float4*)(row + 4 * C::BN);
+          float4 pz{};
           if (dim > 2) pz = *(const float4*)(row + 5 * C::BN);
+          far.x = distance(dim, me, px.x, py.x, pz.x), far.z = distance(dim, me, px.z, py.z, pz.z);
+          far.y = far.x, far.w = far.z;
+          if (!PAIRED) far.y = distance(dim, me, px.y, py.y, pz.y), far.w = distance(dim, me, px.w, py.w, pz.w);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = 4 * i4 + e;
           float fall;
           float u = sc.template u<true>(x[i], cap, &fall);
-          if (dim) u = fmaf(-(&sl.x)[e], distance(dim, me, (&px.x)[e], (&py.x)[e], (&pz.x)[e]), u);
+          if (dim) u = fmaf(-(&sl.x)[e], (&far.x)[e], u);
           x[i] = exp2_of(fmaf(u, sc.A, (&shift.x)[e]));
           dp[i] *= x[i];
           if (cap) dp[i] *= fall;
         }
+        if (dim) __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_sched_barrier(0);
+      frag cg[2], cq[2], pf{}, sf{};
+      cg[0] = tile_columns<T, D>(ldsG, lane, at, 0), cq[0] = tile_columns<T, D>(ldsQ, lane, at, 0);
 #pragma unroll
-      for (int t2 = 0; t2 < 2; ++t2) {
-        float p[8], ds[8];
+      for (int k = 0; k < 2 * DB; ++k) {
+        const int t2 = k / DB, d = k % DB;
+        if (d == 0) {
+          float p[8], ds[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = x[8 * t2 + i], ds[i] = dp[8 * t2 + i];
-        const frag pf = to_frag<T>(p), sf = to_frag<T>(ds);
-        frag cg[DB], cq[DB];
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          cg[d] = lds_columns<T>(ldsG, C::P1, at + 16 * t2, 32 * d), cq[d] = lds_columns<T>(ldsQ, C::P0, at + 16 * t2, 32 * d);
-          if (ES == 4) {   // float32 fragments are large: not all of them at once
-            dv[d] = mma(cg[d], pf, dv[d]), dk[d] = mma(cq[d], sf, dk[d]);
-            __builtin_amdgcn_sched_barrier(0);
-          }
+          for (int i = 0; i < 8; ++i) p[i] = x[8 * t2 + i], ds[i] = dp[8 * t2 + i];
+          pf = to_frag<T>(p), sf = to_frag<T>(ds);
         }
-        if (ES != 4) {
+        if (ES == 4 && k > 0)   // large fragments, long products: none ahead (nor above for wide heads)
+          cg[k & 1] = tile_columns<T, D>(ldsG, lane, at + 16 * t2, 32 * d), cq[k & 1] = tile_columns<T, D>(ldsQ, lane, at + 16 * t2, 32 * d);
+        if (ES != 4 && k + 1 < 2 * DB) {
+          const int r = at + 16 * ((k + 1) / DB), c = 32 * ((k + 1) % DB);
+          cg[(k + 1) & 1] = tile_columns<T, D>(ldsG, lane, r, c), cq[(k + 1) & 1] = tile_columns<T, D>(ldsQ, lane, r, c);
+        }
+        dv[d] = mma(cg[k & 1], pf, dv[d]), dk[d] = mma(cq[k & 1], sf, dk[d]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
 #pragma unroll
-          for (int d = 0; d < DB; ++d) dv[d] = mma(cg[d], pf, dv[d]), dk[d] = mma(cq[d], sf, dk[d]);
+    for (int d = 0; d < DB; ++d)
+      if (D <= 64) asm volatile("" : "+v"(dk[d]), "+v"(dv[d]));   // one place for the sums after either buffer's tile
+  };
+
+  // what belongs to a row, one row to a thread
+  float rl = -INFINITY, rd = 0.0f, rs = 0.0f;
+  Place rp{0.0f, 0.0f, 0.0f};
+  // a tile's first query, the head that it begins with, and the queries from it on
+  struct First {
+    int64_t at, left;
+    unsigned head;
+  };
+  auto first_of = [&](int t) {
+    const unsigned base = (unsigned)t * C::BN, f = base / (unsigned)a.G;
+    return First{q0 + f, queries - f, base - f * (unsigned)a.G};
+  };
+  auto fetch_row = [&](const First& f) {
+    if (tid >= C::BN) return;
+    const uint32_t x = f.head + tid, qi = (x * a.g_inv) >> 20, g = x - qi * a.G;
+    rl = -INFINITY, rd = 0.0f, rs = 0.0f, rp = Place{0.0f, 0.0f, 0.0f};
+    if ((int64_t)qi < f.left) {
+      const int64_t query = f.at + qi, slot = query * a.H + kvh * a.G + g;
+      const float lse = a.lse_in[slot];
+      rl = lse == -INFINITY ? -INFINITY : sc.C - lse * LOG2E;
+      if (!FEW) rd = -a.delta[slot];
+      if (dim && a.dim) rp = place_of(a.pos_q, a.dim, query), rs = a.slopes[kvh * a.G + g] * sc.per_slope;
+    }
+  };
+  auto put_row = [&](float* rows) {
+    if (tid >= C::BN) return;
+    rows[tid] = rl;
+    if (!FEW) rows[C::BN + tid] = rd;
+    if (dim) rows[2 * C::BN + tid] = rs, rows[3 * C::BN + tid] = rp.x, rows[4 * C::BN + tid] = rp.y, rows[5 * C::BN + tid] = rp.z;
+  };
+  // FEW: dO . o of the tile's rows, from the units of a row, which are a row of lanes
+  typedef T unit __attribute__((ext_vector_type(16 / ES)));
+  auto dot_of = [&](const u32x4& g, const u32x4& o) {
+    const unit gv = __builtin_bit_cast(unit, g), ov = __builtin_bit_cast(unit, o);
+    float d = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16 / ES; ++e) d = fmaf((float)gv[e], (float)ov[e], d);
+#pragma unroll
+    for (int o2 = 1; o2 < UNITS; o2 <<= 1) d += __shfl_xor(d, o2, 64);
+    return d;
+  };
+  const int64_t side = (int64_t)kvh * a.G * a.hd;
+  // where a row's unit is, from the tile's first query on
+  auto offset_of = [&](const First& f, int rem, int row, int byte, bool in, int64_t ld) {
+    const uint32_t x = f.head + row, qi = (x * a.g_inv) >> 20, g = x - qi * a.G;
+    return in && (int)qi < rem ? qi * (uint32_t)(ld * ES) + g * (uint32_t)(a.hd * ES) + byte : NOWHERE;
+  };
+  if constexpr (C::DMA) {
+    using TC = TileCopy<D, C::BN>;
+    constexpr int DOTS = FEW ? TC::PER : 1;
+    const int row0 = TC::row0(), byte = TC::unit0();
+    const bool in = byte < a.hd * ES;
+    u32x4 regG[DOTS], regO[DOTS];
+    auto copy = [&](int t, lds_u8* toQ, lds_u8* toG) {
+      const First f = first_of(t);
+      const int rem = (int)min((int64_t)C::BN + 1, f.left);
+      const auto bq = buffer_of((const T*)a.q + f.at * a.ldq + side, (uint32_t)(rem * a.ldq * ES));
+      const auto bg = buffer_of((const T*)a.go + f.at * a.ldgo + side, (uint32_t)(rem * a.ldgo * ES));
+#pragma unroll
+      for (int i = 0; i < TC::PER; ++i) {
+        TC::copy(bq, toQ, i, offset_of(f, rem, row0 + i * TC::STEP, byte, in, a.ldq));
+        TC::copy(bg, toG, i, offset_of(f, rem, row0 + i * TC::STEP, byte, in, a.ldgo));
+      }
+      if (FEW) {
+        const auto bo = buffer_of((const T*)a.o + f.at * a.ldo + side, (uint32_t)(rem * a.ldo * ES));
+#pragma unroll
+        for (int i = 0; i < DOTS; ++i) {
+          regG[i] = buffer_read(bg, offset_of(f, rem, row0 + i * TC::STEP, byte, in, a.ldgo));
+          regO[i] = buffer_read(bo, offset_of(f, rem, row0 + i * TC::STEP, byte, in, a.ldo));
         }
       }
+      fetch_row(f);
+    };
+    auto put = [&](float* rows) {
+      put_row(rows);
+      if (FEW) {
+#pragma unroll
+        for (int i = 0; i < DOTS; ++i) {
+          const float d = dot_of(regG[i], regO[i]);
+          if (tid % UNITS == 0) rows[C::BN + row0 + i * TC::STEP] = -d;
+        }
+      }
+    };
+    if (t_begin < t_end) copy(t_begin, (lds_u8*)lds.a0, (lds_u8*)lds.b0), put(lds.extra0);
+    for (int t = t_begin; t < t_end; t += 2) {
+      stage_wait();
+      __syncthreads();   // the tile is there, and all waves have left the other buffer
+      if (t + 1 < t_end) copy(t + 1, (lds_u8*)lds.a1, (lds_u8*)lds.b1);
+      step((lds_u8*)lds.a0, (lds_u8*)lds.b0, lds.extra0, t);
+      if (t + 1 < t_end) {   // no second way out of the loop: the sums would have a second place for it
+        put(lds.extra1);
+        stage_wait();
+        __syncthreads();
+        if (t + 2 < t_end) copy(t + 2, (lds_u8*)lds.a0, (lds_u8*)lds.b0);
+        step((lds_u8*)lds.a1, (lds_u8*)lds.b1, lds.extra1, t + 1);
+        if (t + 2 < t_end) put(lds.extra0);
+      }
+    }
+  } else {
+    const int row0 = tid / UNITS, c0 = tid % UNITS * 16;
+    const bool in = c0 < a.hd * ES;
+    u32x4 regQ[C::HELD], regG[C::HELD];
+    float dots[C::HELD];
+    auto fetch = [&](int t, int i0) {
+      const First f = first_of(t);
+      const int rem = (int)min((int64_t)C::BN + 1, f.left);
+      const auto bq = buffer_of((const T*)a.q + f.at * a.ldq + side, (uint32_t)(rem * a.ldq * ES));
+      const auto bg = buffer_of((const T*)a.go + f.at * a.ldgo + side, (uint32_t)(rem * a.ldgo * ES));
+      const auto bo = buffer_of((const T*)a.o + f.at * a.ldo + side, (uint32_t)(rem * a.ldo * ES));
+#pragma unroll
+      for (int i = 0; i < C::HELD; ++i) {
+        const int row = row0 + (i0 + i) * C::STEP;
+        regQ[i] = buffer_read(bq, offset_of(f, rem, row, c0, in, a.ldq));
+        regG[i] = buffer_read(bg, offset_of(f, rem, row, c0, in, a.ldgo));
+        if (FEW) dots[i] = dot_of(regG[i], buffer_read(bo, offset_of(f, rem, row, c0, in, a.ldo)));
+      }
+      if (i0 == 0) fetch_row(f);
+    };
+    auto put = [&](int i0) {
+#pragma unroll
+      for (int i = 0; i < C::HELD; ++i) {
+        const int row = row0 + (i0 + i) * C::STEP;
+        *(lds_u32x4*)((lds_u8*)lds.a0 + row * C::PITCH + c0) = regQ[i];
+        *(lds_u32x4*)((lds_u8*)lds.b0 + row * C::PITCH + c0) = regG[i];
+        if (FEW && c0 == 0) lds.extra0[C::BN + row] = -dots[i];
+      }
+      if (i0 == 0) put_row(lds.extra0);
+    };
+    if (C::AHEAD && t_begin < t_end) fetch(t_begin, 0);
+    for (int t = t_begin; t < t_end; ++t) {
+      __syncthreads();
+      if (C::AHEAD) {
+        put(0);
+      } else {
+#pragma unroll 1
+        for (int i0 = 0; i0 < C::PER; i0 += C::HELD) fetch(t, i0), put(i0);
+      }
+      __syncthreads();
+      if (C::AHEAD && t + 1 < t_end) fetch(t + 1, 0);
+      step((lds_u8*)lds.a0, (lds_u8*)lds.b0, lds.extra0, t);
     }
   }
 
@@ -435,8 +571,8 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, unsigned char* smem,
   T* gv = (T*)a.gv + key * a.ldgv + kvh * a.hd;
   if (FEW) {
     const int64_t at = (((int64_t)split * a.nk + key) * a.Hk + kvh) * a.hd;
-    join_rows<T, D>(dk, (float*)smem, a.scale, gk, a.splits_k > 1 ? a.part_k + at : nullptr, a.hd, there);
-    join_rows<T, D>(dv, (float*)smem, 1.0f, gv, a.splits_k > 1 ? a.part_v + at : nullptr, a.hd, there);
+    join_rows<T, D>(dk, lds, a.scale, gk, a.splits_k > 1 ? a.part_k + at : nullptr, a.hd, there);
+    join_rows<T, D>(dv, lds, 1.0f, gv, a.splits_k > 1 ? a.part_v + at : nullptr, a.hd, there);
   } else if (there) {
     write_rows<T, D>(dk, a.scale, gk, nullptr, a.hd);
     write_rows<T, D>(dv, 1.0f, gv, nullptr, a.hd);

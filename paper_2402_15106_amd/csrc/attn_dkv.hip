@@ -6,10 +6,15 @@ using namespace dsmp;
 
 namespace {
 
+// waves to a SIMD that the registers are cut to
 template <typename T, int D, typename M>
-__global__ __launch_bounds__(BT, D == 128 || (D == 64 && sizeof(T) == 4) ? 1 : 2) void k_attn_dkv(AttnArgs a) {
-  __shared__ __align__(16) unsigned char smem[Bwd<T, D, false, true>::LDS];
-  dkv_tile<T, D, false, M>(a, smem, blockIdx.x);
+constexpr int WAVES = D == 128 || (D == 64 && sizeof(T) == 4) ? 1 : sizeof(T) == 4 || D == 64 ? 2 : M::DIM > 0 ? 3 : 4;
+
+template <typename T, int D, bool PAIRED, typename M>
+__global__ __launch_bounds__(BT, (WAVES<T, D, M>)) void k_attn_dkv(AttnArgs a) {
+  using C = Bwd<T, D, false, true>;
+  DSMP_BWD_LDS(C, lds);
+  dkv_tile<T, D, false, PAIRED, M>(a, lds, blockIdx.x);
 }
 
 }  // namespace
@@ -18,8 +23,12 @@ namespace dsmp {
 
 void launch_attention_dkv(dsmp_handle* h, const dsmp_attention_desc& d, const AttnArgs& a, int64_t grid) {
   by_attention(d, [&](auto t, auto width, auto mode) {
-    hipLaunchKernelGGL((k_attn_dkv<decltype(t), decltype(width)::value, decltype(mode)>), dim3((unsigned)grid), dim3(BT), 0,
-                       h->stream, a);
+    using T = decltype(t);
+    constexpr int D = decltype(width)::value;
+    using M = decltype(mode);
+    constexpr bool PAIRS = sizeof(T) == 2 && M::DIM > 0;   // something to gain
+    if (PAIRS && a.G % 2 == 0) hipLaunchKernelGGL((k_attn_dkv<T, D, PAIRS, M>), dim3((unsigned)grid), dim3(BT), 0, h->stream, a);
+    else hipLaunchKernelGGL((k_attn_dkv<T, D, false, M>), dim3((unsigned)grid), dim3(BT), 0, h->stream, a);
   });
 }
 

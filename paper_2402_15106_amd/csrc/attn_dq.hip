@@ -6,9 +6,10 @@ using namespace dsmp;
 namespace {
 
 template <typename T, int D, typename M>
-__global__ __launch_bounds__(BT, D == 128 && (sizeof(T) == 4 || M::DIM > 2) ? 1 : 2) void k_attn_dq(AttnArgs a) {
-  __shared__ __align__(16) unsigned char smem[Bwd<T, D, false, false>::LDS];
-  dq_tile<T, D, false, M>(a, smem, blockIdx.x);
+__global__ __launch_bounds__(BT, sizeof(T) == 4 ? (D == 128 ? 1 : 2) : D == 128 ? 2 : D == 64 ? 3 : 4) void k_attn_dq(AttnArgs a) {
+  using C = Bwd<T, D, false, false>;
+  DSMP_BWD_LDS(C, lds);
+  dq_tile<T, D, false, M>(a, lds, blockIdx.x);
 }
 
 }  // namespace

@@ -16,27 +16,23 @@ constexpr int NT = 256, NW = 4;   // threads and waves of a workgroup
 
 // WIDE: 32 rows to a wave, 128 to a workgroup, every wave takes every key of a tile.
 // FEW: all waves have the same 32 rows and a quarter of a tile's keys each; they are joined at the end.
+// bfloat16 tiles are copied into two buffers in turn, one barrier to a tile; float32 ones wait in registers.
 template <typename T, int D, bool FEW>
 struct Fwd {
+  static constexpr bool DMA = sizeof(T) == 2;
   static constexpr int ROWS = FEW ? 32 : 32 * NW;
-  static constexpr int BN = FEW ? 32 * NW : sizeof(T) == 2 ? 64 : 32;
+  static constexpr int BN = FEW ? 32 * NW : DMA ? 64 : 32;
   static constexpr int SUB = FEW ? 1 : BN / 32;   // blocks of 32 keys that a wave takes of a tile
-  static constexpr int PK = pitch_of<T, D, true>(), PV = pitch_of<T, D, false>();
+  static constexpr int PITCH = DMA ? 2 * D : pitch_of<T, D, true>(), MATRIX = BN * PITCH, PLACES = 3 * BN;
+  // float32: 16-byte units to a thread; the next tile waits in registers, but for FEW's large ones: those come four at a time
   static constexpr int PER = BN * D * (int)sizeof(T) / 16 / NT, STEP = NT * 16 / (D * (int)sizeof(T));
-  // the next tile waits in registers, but for FEW's large ones in float32: those come four units at a time
-  static constexpr bool AHEAD = !(FEW && sizeof(T) == 4 && D == 128);
+  static constexpr bool AHEAD = !(FEW && D == 128);
   static constexpr int HELD = AHEAD || PER < 4 ? PER : 4;
-  static constexpr int TILE = BN * (PK + PV) + 3 * BN * 4;
-  static constexpr int BUFS = AHEAD && !FEW && D <= 64 ? 2 : 1;   // two tiles in LDS: one barrier to a tile
-  static constexpr int JOIN = FEW ? NW * 32 * (D + 2) * 4 : 0;
-  static constexpr int LDS = BUFS * TILE > JOIN ? BUFS * TILE : JOIN;
-  // waves to a SIMD that the registers are cut to
-  static constexpr int waves(int cap, int dim) {
-    if (D == 128) return FEW || sizeof(T) == 4 || dim > 2 ? 1 : 2;
-    if (FEW || sizeof(T) == 4) return 2;
-    return (D == 64 ? 3 : 4) - (cap || dim);
-  }
+  static_assert(!FEW || MATRIX >= 2 * 32 * D * 4, "two waves' parts fit into a matrix");
   static_assert(PER >= 1 && PER * NT * 16 == BN * D * (int)sizeof(T), "whole units for every thread");
+  // waves to a SIMD that the registers are cut to
+  template <typename M>
+  static constexpr int WAVES = D == 128 ? (FEW || !DMA ? 1 : 2) : FEW || !DMA ? 2 : D == 64 && M::DIM > 0 ? 3 : 4;
 };
 
 // How far the scores of a tile may pass the maximum that a row's sums refer to, in powers of two,
@@ -45,11 +41,13 @@ struct Fwd {
 constexpr float SLACK = 8.0f;
 
 template <typename T, int D, bool FEW, typename M>
-__global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::waves(M::CAP, M::DIM))) void k_attn_fwd(AttnArgs a) {
+__global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::template WAVES<M>)) void k_attn_fwd(AttnArgs a) {
   using C = Fwd<T, D, FEW>;
   constexpr int ES = sizeof(T), KS = D / 16, DB = D / 32;
   typedef typename Frag<T>::type frag;
-  __shared__ __align__(16) unsigned char smem[C::LDS];
+  // the buffers are arrays of their own, so that a copy into one is not waited for by reads of the other
+  __shared__ __align__(1024) unsigned char mK0[C::MATRIX], mV0[C::MATRIX], mK1[C::DMA ? C::MATRIX : 16], mV1[C::DMA ? C::MATRIX : 16];
+  __shared__ __align__(16) float mP0[C::PLACES], mP1[C::DMA ? C::PLACES : 4];
 
   const int tid = (int)threadIdx.x, l = tid & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = (int)(blockIdx.x % (unsigned)a.Hk);
@@ -77,42 +75,11 @@ __global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::waves(M::CAP, M::DIM))) void k
 #pragma unroll
   for (int t = 0; t < KS; ++t) {
     qf[t] = read_frag<T>((const T*)a.q + query * a.ldq + head * a.hd + 16 * t + 8 * h, there && 16 * t + 8 * h < a.hd);
-    apply_sign(qf[t], sc.sign);
   }
+  apply_sign<KS>(qf, sc.sign);
   Place me{0.0f, 0.0f, 0.0f};
   float slope = 0.0f;
   if (dim && a.dim && there) me = place_of(a.pos_q, a.dim, query), slope = a.slopes[head] * sc.per_slope;
-
-  // a thread's 16-byte units of a tile: one place in every STEP-th row
-  const int row0 = tid / (D * ES / 16), c0 = tid % (D * ES / 16) * 16;
-  const bool in = c0 < a.hd * ES;
-  const uint32_t offK = in ? (uint32_t)(row0 * a.ldk * ES + c0) : NOWHERE, stepK = (uint32_t)(C::STEP * a.ldk * ES);
-  const uint32_t offV = in ? (uint32_t)(row0 * a.ldv * ES + c0) : NOWHERE, stepV = (uint32_t)(C::STEP * a.ldv * ES);
-  u32x4 regK[C::HELD], regV[C::HELD];
-  Place key{0.0f, 0.0f, 0.0f};
-  auto fetch = [&](int t, int i0) {
-    const int64_t j0 = k0 + (int64_t)t * C::BN;
-    const int rem = (int)min((int64_t)C::BN, klen - (int64_t)t * C::BN);
-    const auto bk = buffer_of((const T*)a.k + j0 * a.ldk + kvh * a.hd, (uint32_t)(rem * a.ldk * ES));
-    const auto bv = buffer_of((const T*)a.v + j0 * a.ldv + kvh * a.hd, (uint32_t)(rem * a.ldv * ES));
-#pragma unroll
-    for (int i = 0; i < C::HELD; ++i)
-      regK[i] = buffer_read(bk, offK + (i0 + i) * stepK), regV[i] = buffer_read(bv, offV + (i0 + i) * stepV);
-    if (dim && a.dim && i0 == 0 && tid < rem) key = place_of(a.pos_k, a.dim, j0 + tid);
-  };
-  auto put = [&](int buf, int i0) {
-    lds_u8* to = (lds_u8*)smem + buf * C::TILE;
-#pragma unroll
-    for (int i = 0; i < C::HELD; ++i) {
-      const int row = row0 + (i0 + i) * C::STEP;
-      *(__attribute__((address_space(3))) u32x4*)(to + row * C::PK + c0) = regK[i];
-      *(__attribute__((address_space(3))) u32x4*)(to + C::BN * C::PK + row * C::PV + c0) = regV[i];
-    }
-    if (dim && i0 == 0 && tid < C::BN) {
-      float* places = (float*)(smem + buf * C::TILE + C::BN * (C::PK + C::PV));
-      places[tid] = key.x, places[C::BN + tid] = key.y, places[2 * C::BN + tid] = key.z;
-    }
-  };
 
   f32x16 o[DB];
 #pragma unroll
@@ -121,24 +88,26 @@ __global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::waves(M::CAP, M::DIM))) void k
     for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
   float m = -INFINITY, sum = 0.0f;   // the u that this lane's row refers to; the sum over this half's keys
 
+  const LanePlace place = lane_place<D>();
   // one tile: scores, then weights and their products with the values
-  auto step = [&](int buf, int rem) {
-    lds_u8* ldsK = (lds_u8*)smem + buf * C::TILE;
-    lds_u8* ldsV = ldsK + C::BN * C::PK;
-    const float* places = (const float*)(smem + buf * C::TILE + C::BN * (C::PK + C::PV));
+  auto step = [&](lds_u8* ldsK, lds_u8* ldsV, const float* places, int t) {
+    const int rem = (int)min((int64_t)C::BN, klen - (int64_t)t * C::BN);
+    if (FEW && 32 * w >= rem) return;
     const int sub0 = FEW ? w : 0;
+    LanePlace lane = place;
+    formed_here(lane);
     // Fragments are read one step ahead of their products and no further (the scheduler would
     // read all of them at once and run out of registers); the products run while the
     // next step's powers are formed.
     f32x16 x[C::SUB];
     frag kf[2][C::SUB];
 #pragma unroll
-    for (int b = 0; b < C::SUB; ++b) kf[0][b] = lds_rows<T>(ldsK, C::PK, 32 * (sub0 + b), 0), x[b] = f32x16{};
+    for (int b = 0; b < C::SUB; ++b) kf[0][b] = tile_rows<T, D>(ldsK, lane, 32 * (sub0 + b), 0), x[b] = f32x16{};
 #pragma unroll
     for (int t2 = 0; t2 < KS; ++t2) {
 #pragma unroll
       for (int b = 0; b < C::SUB; ++b)
-        if (t2 + 1 < KS) kf[(t2 + 1) & 1][b] = lds_rows<T>(ldsK, C::PK, 32 * (sub0 + b), 16 * (t2 + 1));
+        if (t2 + 1 < KS) kf[(t2 + 1) & 1][b] = tile_rows<T, D>(ldsK, lane, 32 * (sub0 + b), t2 + 1);
 #pragma unroll
       for (int b = 0; b < C::SUB; ++b) x[b] = mma(kf[t2 & 1][b], qf[t2], x[b]);
       __builtin_amdgcn_sched_barrier(0);
@@ -164,9 +133,11 @@ __global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::waves(M::CAP, M::DIM))) void k
         }
       }
       if (at + 32 > rem) {   // behind the last key
+        int left = rem - at - 4 * h;
+        asm volatile("" : "+v"(left));   // compared with constants, not with sixteen row numbers kept over the loop
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (at + result_row(i) >= rem) x[b][i] = -INFINITY;
+          if (8 * (i >> 2) + (i & 3) >= left) x[b][i] = -INFINITY;
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, x[b][i]);
@@ -174,7 +145,7 @@ __global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::waves(M::CAP, M::DIM))) void k
     }
     frag vf[2][DB];
 #pragma unroll
-    for (int d = 0; d < DB; ++d) vf[0][d] = lds_columns<T>(ldsV, C::PV, 32 * sub0, 32 * d);
+    for (int d = 0; d < DB; ++d) vf[0][d] = tile_columns<T, D>(ldsV, lane, 32 * sub0, 32 * d);
     top = fmaxf(top, other_half(top));
     if (__any((top - m) * sc.A > SLACK)) {   // also where m is -infinity
       const float now = fmaxf(m, top), shrink = m == -INFINITY ? 0.0f : exp2_of((m - now) * sc.A);
@@ -196,44 +167,86 @@ __global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::waves(M::CAP, M::DIM))) void k
       const frag pf = to_frag<T>(p);
 #pragma unroll
       for (int d = 0; d < DB; ++d)
-        if (k + 1 < 2 * C::SUB) vf[(k + 1) & 1][d] = lds_columns<T>(ldsV, C::PV, 32 * sub0 + 16 * (k + 1), 32 * d);
+        if (k + 1 < 2 * C::SUB) vf[(k + 1) & 1][d] = tile_columns<T, D>(ldsV, lane, 32 * sub0 + 16 * (k + 1), 32 * d);
 #pragma unroll
       for (int d = 0; d < DB; ++d) o[d] = mma(vf[k & 1][d], pf, o[d]);
       __builtin_amdgcn_sched_barrier(0);
     }
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+      if (C::template WAVES<M> > 1) asm volatile("" : "+v"(o[d]));   // one place for the sums after either buffer's tile
     sum += add;
   };
-  auto rem_of = [&](int t) { return (int)min((int64_t)C::BN, klen - (int64_t)t * C::BN); };
-  auto take = [&](int buf, int t) {
-    const int rem = rem_of(t);
-    if (FEW && 32 * w >= rem) return;
-    step(buf, rem);
-  };
 
-  if (C::BUFS == 2) {
-    if (t_begin < t_end) fetch(t_begin, 0), put(0, 0);
-    if (t_begin + 1 < t_end) fetch(t_begin + 1, 0);
-    __syncthreads();
-    for (int t = t_begin; t < t_end; ++t) {
-      const int buf = (t - t_begin) & 1;
-      take(buf, t);
-      if (t + 1 < t_end) put(buf ^ 1, 0);   // all waves have left that tile at the barrier before
-      if (t + 2 < t_end) fetch(t + 2, 0);
-      __syncthreads();
+  const T* keys = (const T*)a.k + k0 * a.ldk + kvh * a.hd;
+  const T* values = (const T*)a.v + k0 * a.ldv + kvh * a.hd;
+  if constexpr (C::DMA) {
+    using TC = TileCopy<D, C::BN>;
+    const bool in = TC::unit0() < a.hd * ES;
+    const uint32_t offK = in ? (uint32_t)(TC::row0() * a.ldk * ES + TC::unit0()) : NOWHERE, stepK = (uint32_t)(TC::STEP * a.ldk * ES);
+    const uint32_t offV = in ? (uint32_t)(TC::row0() * a.ldv * ES + TC::unit0()) : NOWHERE, stepV = (uint32_t)(TC::STEP * a.ldv * ES);
+    auto copy = [&](int t, lds_u8* toK, lds_u8* toV, float* places) {
+      const int64_t j = (int64_t)t * C::BN;
+      const int rem = (int)min((int64_t)C::BN, klen - j);
+      const auto bk = buffer_of(keys + j * a.ldk, (uint32_t)(rem * a.ldk * ES));
+      const auto bv = buffer_of(values + j * a.ldv, (uint32_t)(rem * a.ldv * ES));
+#pragma unroll
+      for (int i = 0; i < TC::PER; ++i) TC::copy(bk, toK, i, offK + i * stepK), TC::copy(bv, toV, i, offV + i * stepV);
+      if (dim) copy_places<C::BN>(a.pos_k, a.dim, k0 + j, rem, places);
+    };
+    if (dim) clear_places<C::BN>(a.dim, dim, mP0), clear_places<C::BN>(a.dim, dim, mP1);
+    if (t_begin < t_end) copy(t_begin, (lds_u8*)mK0, (lds_u8*)mV0, mP0);
+    for (int t = t_begin; t < t_end; t += 2) {
+      stage_wait();
+      __syncthreads();   // the tile is there, and all waves have left the other buffer
+      if (t + 1 < t_end) copy(t + 1, (lds_u8*)mK1, (lds_u8*)mV1, mP1);
+      step((lds_u8*)mK0, (lds_u8*)mV0, mP0, t);
+      if (t + 1 < t_end) {   // no second way out of the loop: the sums would have a second place for it
+        stage_wait();
+        __syncthreads();
+        if (t + 2 < t_end) copy(t + 2, (lds_u8*)mK0, (lds_u8*)mV0, mP0);
+        step((lds_u8*)mK1, (lds_u8*)mV1, mP1, t + 1);
+      }
     }
   } else {
+    // a thread's 16-byte units of a tile: one place in every STEP-th row
+    const int row0 = tid / (D * ES / 16), c0 = tid % (D * ES / 16) * 16;
+    const bool in = c0 < a.hd * ES;
+    const uint32_t offK = in ? (uint32_t)(row0 * a.ldk * ES + c0) : NOWHERE, stepK = (uint32_t)(C::STEP * a.ldk * ES);
+    const uint32_t offV = in ? (uint32_t)(row0 * a.ldv * ES + c0) : NOWHERE, stepV = (uint32_t)(C::STEP * a.ldv * ES);
+    u32x4 regK[C::HELD], regV[C::HELD];
+    Place key{0.0f, 0.0f, 0.0f};
+    auto fetch = [&](int t, int i0) {
+      const int64_t j = (int64_t)t * C::BN;
+      const int rem = (int)min((int64_t)C::BN, klen - j);
+      const auto bk = buffer_of(keys + j * a.ldk, (uint32_t)(rem * a.ldk * ES));
+      const auto bv = buffer_of(values + j * a.ldv, (uint32_t)(rem * a.ldv * ES));
+#pragma unroll
+      for (int i = 0; i < C::HELD; ++i)
+        regK[i] = buffer_read(bk, offK + (i0 + i) * stepK), regV[i] = buffer_read(bv, offV + (i0 + i) * stepV);
+      if (dim && a.dim && i0 == 0 && tid < rem) key = place_of(a.pos_k, a.dim, k0 + j + tid);
+    };
+    auto put = [&](int i0) {
+#pragma unroll
+      for (int i = 0; i < C::HELD; ++i) {
+        const int at = (row0 + (i0 + i) * C::STEP) * C::PITCH + c0;
+        *(lds_u32x4*)((lds_u8*)mK0 + at) = regK[i];
+        *(lds_u32x4*)((lds_u8*)mV0 + at) = regV[i];
+      }
+      if (dim && i0 == 0 && tid < C::BN) mP0[tid] = key.x, mP0[C::BN + tid] = key.y, mP0[2 * C::BN + tid] = key.z;
+    };
     if (C::AHEAD && t_begin < t_end) fetch(t_begin, 0);
     for (int t = t_begin; t < t_end; ++t) {
       __syncthreads();
       if (C::AHEAD) {
-        put(0, 0);
+        put(0);
       } else {
 #pragma unroll 1
-        for (int i0 = 0; i0 < C::PER; i0 += C::HELD) fetch(t, i0), put(0, i0);
+        for (int i0 = 0; i0 < C::PER; i0 += C::HELD) fetch(t, i0), put(i0);
       }
       __syncthreads();
       if (C::AHEAD && t + 1 < t_end) fetch(t + 1, 0);
-      take(0, t);
+      step((lds_u8*)mK0, (lds_u8*)mV0, mP0, t);
     }
   }
   sum += other_half(sum);
@@ -257,14 +270,16 @@ __global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::waves(M::CAP, M::DIM))) void k
       }
     return;
   }
-  // the waves' parts, [wave][value][row], joined by 256 threads: a row and four values in 32 each
+  // the waves' parts, [value][row], two in each of a buffer's matrices, joined by 256 threads: a row and
+  // four values in 32 each
   m = fmaf(m, sc.A, sc.C);   // in powers of two from here on
-  float *jo = (float*)smem, *jm = jo + NW * D * 32, *js = jm + NW * 32;
+  float *jm = mP0, *js = mP0 + NW * 32;
+  auto part_of = [&](int wave) { return (float*)(wave < 2 ? mK0 : mV0) + (wave & 1) * 32 * D; };
   __syncthreads();
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) jo[(w * D + 32 * d + result_row(i)) * 32 + (l & 31)] = o[d][i];
+    for (int i = 0; i < 16; ++i) part_of(w)[(32 * d + result_row(i)) * 32 + (l & 31)] = o[d][i];
   if (h == 0) jm[w * 32 + l] = m, js[w * 32 + l] = sum;
   __syncthreads();
   if (!mine.there) return;
@@ -297,7 +312,7 @@ __global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::waves(M::CAP, M::DIM))) void k
     for (int e = 0; e < 4; ++e) {
       v[e] = 0.0f;
 #pragma unroll
-      for (int k = 0; k < NW; ++k) v[e] = fmaf(weight[k], jo[(k * D + c + e) * 32 + (l & 31)], v[e]);
+      for (int k = 0; k < NW; ++k) v[e] = fmaf(weight[k], part_of(k)[(c + e) * 32 + (l & 31)], v[e]);
       v[e] *= inv;
     }
     if (whole) store4((T*)a.out + mine.query * a.ldout + mine.head * a.hd + c, v[0], v[1], v[2], v[3]);

@@ -172,12 +172,16 @@ def test_many_rows_and_few_keys_and_the_other_way(env, nq, nk, H, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_scores_that_rise_from_tile_to_tile(env, dtype):
-    """Each later key scores higher: the running maximum is passed by more than its slack again and again."""
+    """Each later key scores higher: the running maximum is passed by more than its slack again and again, and
+    the first keys' weights are below the smallest float32 (88 and more below the sum)."""
     c = Case(env, [0, 40], [0, 1000], 2, 2, 16, dtype, scale=1.0)
     c.k.copy_((c.torch.arange(1000, device="cuda")[:, None] * 0.06).expand(1000, 32))
-    c.q.copy_(c.torch.rand(40, 32, device="cuda") * 0.2)
+    g = c.torch.Generator(device="cuda")
+    g.manual_seed(11)
+    c.q.copy_(c.torch.rand(40, 32, generator=g, device="cuda") * 0.2)
     announce(dtype)
     c.check()
+    assert float(c.forward()[1].max()) > 92.0
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
