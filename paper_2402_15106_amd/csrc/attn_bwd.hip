@@ -72,7 +72,7 @@ BwdPlan bwd_plan(const dsmp_attention_desc& d, const dsmp_segments& qs, const ds
 }
 
 struct BwdWs {
-  float *delta, *q, *k, *v;
+  float *shift, *minus_d, *q, *k, *v;
   size_t total;
 };
 
@@ -80,7 +80,7 @@ BwdWs bwd_ws(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_s
   const BwdPlan p = bwd_plan(d, qs, ks);
   Carve cv(ws);
   BwdWs w{};
-  w.delta = cv.take<float>((size_t)qs.n * d.heads);
+  w.shift = cv.take<float>((size_t)qs.n * d.heads), w.minus_d = cv.take<float>((size_t)qs.n * d.heads);
   const size_t of_q = p.splits_q > 1 ? (size_t)p.splits_q * qs.n * d.heads * d.head_dim : 0;
   const size_t of_k = p.splits_k > 1 ? (size_t)p.splits_k * ks.n * d.kv_heads * d.head_dim : 0;
   w.q = cv.take<float>(of_q), w.k = cv.take<float>(of_k), w.v = cv.take<float>(of_k);
@@ -124,7 +124,7 @@ extern "C" dsmp_status dsmp_attention_backward(dsmp_handle* h, const dsmp_attent
   AttnArgs a = attn_args(*desc, *qs, *ks);
   a.q = q, a.ldq = ldq, a.k = k, a.ldk = ldk, a.v = v, a.ldv = ldv, a.o = out, a.ldo = ldo, a.go = grad_out, a.ldgo = ldgo;
   a.gq = grad_q, a.ldgq = ldgq, a.gk = grad_k, a.ldgk = ldgk, a.gv = grad_v, a.ldgv = ldgv;
-  a.lse_in = lse, a.delta = w.delta, a.part = w.q, a.part_k = w.k, a.part_v = w.v;
+  a.lse_in = lse, a.shift = w.shift, a.minus_d = w.minus_d, a.part = w.q, a.part_k = w.k, a.part_v = w.v;
   a.splits = p.splits_q, a.splits_k = p.splits_k;
   a.pos_q = pos_q, a.pos_k = pos_k, a.slopes = slopes;
   DeviceScope dev(h);

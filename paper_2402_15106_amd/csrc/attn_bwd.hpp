@@ -105,7 +105,8 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, const BwdLds& lds, un
   const int split = FEW ? (int)(rest % (unsigned)a.splits) : 0;
   const int64_t tile = FEW ? rest / (unsigned)a.splits : rest;
   int64_t first;
-  const int seg = find_segment(a.qb, a.n_seg, a.G, C::OWN, tile, &first);
+  const int seg = FEW ? find_segment(a.qb, a.n_seg, a.G, C::OWN, tile, &first)
+                      : find_segment_longest_first(a.qb, a.kb, a.n_seg, a.G, C::OWN, tile, &first);
   const int64_t q0 = a.qb.at(seg), R = (a.qb.at(seg + 1) - q0) * a.G, r0 = (tile - first) * C::OWN;
   if (tile < first || r0 >= R) return;
   const int64_t k0 = a.kb.at(seg), klen = a.kb.at(seg + 1) - k0;
@@ -132,9 +133,9 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, const BwdLds& lds, un
   }
   apply_sign<KS>(qf, sc.sign);
   delta += other_half(delta);
-  if (row.there && h == 0 && split == 0 && (!FEW || w == 0)) a.delta[slot] = delta;
   // the exponent of a weight is A u + shift; a row without keys has the weights 0
   const float lse = row.there ? a.lse_in[slot] : INFINITY, shift = lse == -INFINITY ? -INFINITY : sc.C - lse * LOG2E;
+  if (row.there && h == 0 && split == 0 && (!FEW || w == 0)) a.shift[slot] = shift, a.minus_d[slot] = -delta;
   Place me{0.0f, 0.0f, 0.0f};
   float slope = 0.0f;
   if (dim && a.dim && row.there) me = place_of(a.pos_q, a.dim, row.query), slope = a.slopes[row.head] * sc.per_slope;
@@ -309,7 +310,8 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
   const int split = FEW ? (int)(rest % (unsigned)a.splits_k) : 0;
   const int64_t tile = FEW ? rest / (unsigned)a.splits_k : rest;
   int64_t first;
-  const int seg = find_segment(a.kb, a.n_seg, 1, C::OWN, tile, &first);
+  const int seg = FEW ? find_segment(a.kb, a.n_seg, 1, C::OWN, tile, &first)
+                      : find_segment_longest_first(a.kb, a.qb, a.n_seg, 1, C::OWN, tile, &first);
   const int64_t k0 = a.kb.at(seg), klen = a.kb.at(seg + 1) - k0, j0 = (tile - first) * C::OWN;
   if (tile < first || j0 >= klen) return;
   const int64_t q0 = a.qb.at(seg), queries = a.qb.at(seg + 1) - q0, R = queries > 0 ? queries * a.G : 0;
@@ -370,17 +372,19 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) {
         const float* row = rows + at + 8 * i4 + 4 * h;
-        const float4 shift = *(const float4*)row;
-        float4 sl{}, far{};
+        float4 far{};
         if (dim) {
-          sl = *(const float4*)(row + 2 * C::BN);
           const float4 px = *(const float4*)(row + 3 * C::BN), py = *(const float4*)(row + 4 * C::BN);
           float4 pz{};
           if (dim > 2) pz = *(const float4*)(row + 5 * C::BN);
           far.x = distance(dim, me, px.x, py.x, pz.x), far.z = distance(dim, me, px.z, py.z, pz.z);
           far.y = far.x, far.w = far.z;
           if (!PAIRED) far.y = distance(dim, me, px.y, py.y, pz.y), far.w = distance(dim, me, px.w, py.w, pz.w);
+          __builtin_amdgcn_sched_barrier(0);   // not all of a row's numbers in registers at once
         }
+        const float4 shift = *(const float4*)row;
+        float4 sl{};
+        if (dim) sl = *(const float4*)(row + 2 * C::BN);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = 4 * i4 + e;
@@ -420,8 +424,10 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
       if (D <= 64) asm volatile("" : "+v"(dk[d]), "+v"(dv[d]));   // one place for the sums after either buffer's tile
   };
 
-  // what belongs to a row, one row to a thread
-  float rl = -INFINITY, rd = 0.0f, rs = 0.0f;
+  // what belongs to a row, one row to a thread: the shift is formed here (FEW) or was by the launch for the
+  // queries, and so was -D, but for FEW, which forms it from its rows' units.  A row behind the last has zeros: its
+  // weights, whatever they are, meet gradients of 0.
+  float rl = 0.0f, rd = 0.0f, rs = 0.0f;
   Place rp{0.0f, 0.0f, 0.0f};
   // a tile's first query, the head that it begins with, and the queries from it on
   struct First {
@@ -435,19 +441,22 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
   auto fetch_row = [&](const First& f) {
     if (tid >= C::BN) return;
     const uint32_t x = f.head + tid, qi = (x * a.g_inv) >> 20, g = x - qi * a.G;
-    rl = -INFINITY, rd = 0.0f, rs = 0.0f, rp = Place{0.0f, 0.0f, 0.0f};
+    rl = rd = rs = 0.0f, rp = Place{0.0f, 0.0f, 0.0f};
     if ((int64_t)qi < f.left) {
       const int64_t query = f.at + qi, slot = query * a.H + kvh * a.G + g;
-      const float lse = a.lse_in[slot];
-      rl = lse == -INFINITY ? -INFINITY : sc.C - lse * LOG2E;
-      if (!FEW) rd = -a.delta[slot];
+      if (FEW) {
+        const float lse = a.lse_in[slot];
+        rl = lse == -INFINITY ? -INFINITY : sc.C - lse * LOG2E;
+      } else if (!C::DMA) {
+        rl = a.shift[slot], rd = a.minus_d[slot];
+      }
       if (dim && a.dim) rp = place_of(a.pos_q, a.dim, query), rs = a.slopes[kvh * a.G + g] * sc.per_slope;
     }
   };
   auto put_row = [&](float* rows) {
     if (tid >= C::BN) return;
-    rows[tid] = rl;
-    if (!FEW) rows[C::BN + tid] = rd;
+    if (FEW || !C::DMA) rows[tid] = rl;
+    if (!FEW && !C::DMA) rows[C::BN + tid] = rd;
     if (dim) rows[2 * C::BN + tid] = rs, rows[3 * C::BN + tid] = rp.x, rows[4 * C::BN + tid] = rp.y, rows[5 * C::BN + tid] = rp.z;
   };
   // FEW: dO . o of the tile's rows, from the units of a row, which are a row of lanes
@@ -473,7 +482,7 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
     const int row0 = TC::row0(), byte = TC::unit0();
     const bool in = byte < a.hd * ES;
     u32x4 regG[DOTS], regO[DOTS];
-    auto copy = [&](int t, lds_u8* toQ, lds_u8* toG) {
+    auto copy = [&](int t, lds_u8* toQ, lds_u8* toG, float* rows) {
       const First f = first_of(t);
       const int rem = (int)min((int64_t)C::BN + 1, f.left);
       const auto bq = buffer_of((const T*)a.q + f.at * a.ldq + side, (uint32_t)(rem * a.ldq * ES));
@@ -491,7 +500,14 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
           regO[i] = buffer_read(bo, offset_of(f, rem, row0 + i * TC::STEP, byte, in, a.ldo));
         }
       }
-      fetch_row(f);
+      if (!FEW && w < 2) {   // a wave for the shifts, one for -D
+        static_assert(FEW || C::BN == 64, "a row to a lane");
+        const auto from = buffer_of((w ? a.minus_d : a.shift) + f.at * a.H, (uint32_t)(rem * a.H * 4));
+        const uint32_t x = f.head + l, qi = (x * a.g_inv) >> 20, g = x - qi * a.G;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(lds_u8*)(rows + w * C::BN), 4,
+                                                 (int)((int)qi < rem ? (qi * a.H + kvh * a.G + g) * 4 : NOWHERE), 0, 0, 0);
+      }
+      if (FEW || dim) fetch_row(f);
     };
     auto put = [&](float* rows) {
       put_row(rows);
@@ -503,17 +519,17 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
         }
       }
     };
-    if (t_begin < t_end) copy(t_begin, (lds_u8*)lds.a0, (lds_u8*)lds.b0), put(lds.extra0);
+    if (t_begin < t_end) copy(t_begin, (lds_u8*)lds.a0, (lds_u8*)lds.b0, lds.extra0), put(lds.extra0);
     for (int t = t_begin; t < t_end; t += 2) {
       stage_wait();
       __syncthreads();   // the tile is there, and all waves have left the other buffer
-      if (t + 1 < t_end) copy(t + 1, (lds_u8*)lds.a1, (lds_u8*)lds.b1);
+      if (t + 1 < t_end) copy(t + 1, (lds_u8*)lds.a1, (lds_u8*)lds.b1, lds.extra1);
       step((lds_u8*)lds.a0, (lds_u8*)lds.b0, lds.extra0, t);
       if (t + 1 < t_end) {   // no second way out of the loop: the sums would have a second place for it
         put(lds.extra1);
         stage_wait();
         __syncthreads();
-        if (t + 2 < t_end) copy(t + 2, (lds_u8*)lds.a0, (lds_u8*)lds.b0);
+        if (t + 2 < t_end) copy(t + 2, (lds_u8*)lds.a0, (lds_u8*)lds.b0, lds.extra0);
         step((lds_u8*)lds.a1, (lds_u8*)lds.b1, lds.extra1, t + 1);
         if (t + 2 < t_end) put(lds.extra0);
       }

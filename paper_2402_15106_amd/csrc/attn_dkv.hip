@@ -1,5 +1,5 @@
 // Attention backward, the gradients of the keys and values, for tiles of 128 keys that fill the
-// card.  D_i comes from the launch for the queries.
+// card.  D_i and lse_i come from the launch for the queries.
 #include "attn_bwd.hpp"
 
 using namespace dsmp;
@@ -8,7 +8,7 @@ namespace {
 
 // waves to a SIMD that the registers are cut to
 template <typename T, int D, typename M>
-constexpr int WAVES = D == 128 || (D == 64 && sizeof(T) == 4) ? 1 : sizeof(T) == 4 || D == 64 ? 2 : M::DIM > 0 ? 3 : 4;
+constexpr int WAVES = D == 128 || (D == 64 && sizeof(T) == 4) ? 1 : sizeof(T) == 4 ? 2 : D == 64 ? 3 - (M::DIM > 0 || M::CAP > 0) : 4 - (M::DIM > 0);
 
 template <typename T, int D, bool PAIRED, typename M>
 __global__ __launch_bounds__(BT, (WAVES<T, D, M>)) void k_attn_dkv(AttnArgs a) {

@@ -55,7 +55,8 @@ __global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::template WAVES<M>)) void k_att
   const int split = (int)(rest % (unsigned)a.splits);
   const int64_t tile = rest / (unsigned)a.splits;
   int64_t first;
-  const int seg = find_segment(a.qb, a.n_seg, a.G, C::ROWS, tile, &first);
+  const int seg = FEW ? find_segment(a.qb, a.n_seg, a.G, C::ROWS, tile, &first)
+                      : find_segment_longest_first(a.qb, a.kb, a.n_seg, a.G, C::ROWS, tile, &first);
   const int64_t q0 = a.qb.at(seg), R = (a.qb.at(seg + 1) - q0) * a.G, r0 = (tile - first) * C::ROWS;
   if (tile < first || r0 >= R) return;
   const int64_t k0 = a.kb.at(seg), klen = a.kb.at(seg + 1) - k0;

@@ -24,12 +24,12 @@ def attention_ws(lib, desc, q, k):
 
 def test_attention_workspace(lib):
     d = dm.attention_desc(8, 2, 64, dm.BF16)
-    st, f, b = attention_ws(lib, d, (16384, 1, None), (16384, 1, None))
-    assert st == dm.OK and f == 0 and b == 16384 * 8 * 4                 # the tiles fill the card: no parts to join
+    st, f, b = attention_ws(lib, dm.attention_desc(8, 8, 64, dm.BF16), (16384, 1, None), (16384, 1, None))
+    assert st == dm.OK and f == 0 and b == 2 * 16384 * 8 * 4                 # the tiles fill the card: no parts to join
     st, f, b = attention_ws(lib, d, (5, 1, None), (262144, 1, None))
     assert st == dm.OK and f >= 2 * 5 * 8 * 66 * 4 and b >= 2 * 5 * 8 * 64 * 4    # two parts at least
     st, f, b = attention_ws(lib, d, (5, 1, None), (100, 1, None))
-    assert st == dm.OK and f == 0 and 5 * 8 * 4 <= b <= 256
+    assert st == dm.OK and f == 0 and 2 * 5 * 8 * 4 <= b <= 512
     assert attention_ws(lib, d, (0, 3, None), (0, 3, None)) == (dm.OK, 0, 0)
 
 
