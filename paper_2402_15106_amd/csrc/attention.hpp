@@ -221,6 +221,22 @@ __device__ __forceinline__ void store4(T* p, float a, float b, float c, float d)
   *(t4*)p = v;
 }
 
+// A wave's 32 rows of results (D values each, a lane's column), scaled: to `out`, or in float32 to `part`.
+template <typename T, int D>
+__device__ __forceinline__ void write_rows(const f32x16* acc, float scale, T* out, float* part, int hd) {
+  const int h = ((int)threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      const int c = 32 * d + 8 * i4 + 4 * h;
+      if (c >= hd) continue;
+      const float v[4] = {acc[d][4 * i4] * scale, acc[d][4 * i4 + 1] * scale, acc[d][4 * i4 + 2] * scale, acc[d][4 * i4 + 3] * scale};
+      if (part) *(float4*)(part + c) = make_float4(v[0], v[1], v[2], v[3]);
+      else store4(out + c, v[0], v[1], v[2], v[3]);
+    }
+}
+
 // ------------------------------------------------------------------ segments
 struct Bounds {
   const int32_t* ptr;   // NULL: equal segments of `len` rows
@@ -452,29 +468,54 @@ void by_attention(const dsmp_attention_desc& d, F f) {
   else width(__bf16{}, Mode<0, 3>{});
 }
 
-// Workgroups of 256 threads that fill the card (256 CUs) twice; a launch has fewer than 2^32 threads.
-constexpr int64_t FILL = 512, MAX_GROUPS = ((int64_t)1 << 24) - 1;
+constexpr int64_t MAX_GROUPS = ((int64_t)1 << 24) - 1;   // a launch has fewer than 2^32 threads
 
-// How far FEW's workgroups are cut over the other side.  Each of one or two kinds of them, `groups`
-// with `steps` tiles to go over, is cut so that a workgroup has about the same amount of work, and as
-// far as the shortest estimated time asks: the tiles dealt to the card's `slots`, half of
-// a workgroup's for the uneven end, and the launch that adds up the parts (3 us, and their
-// bytes written and read at 4 TB/s).  1,000 nodes, 4 heads of 32 in float32: forward uncut
-// 31 us, now 18; backward 51, now 39; bfloat16 heads gain less (backward 22, now 17).
+// ------------------------------------------------- which tiles, and how far they are cut
+// A call takes tiles of 128 rows (WIDE) or of 32 (FEW), whichever its estimated time is shorter for, and
+// either may be cut over the other side into parts that are added up afterwards.
+//
+// CU microseconds of a tile where the card is full, as measured (8,192 scores of a WIDE bfloat16 tile, 4,096 of the
+// others; heads of up to 32, 64 and 128): forward 4.3 G scores of heads of 64 in 1,180 us WIDE; FEW tiles have four
+// times the copies to LDS for a score, which bounds the keys' gradients (16,384 x 8 heads, two of keys: 3,356 us with
+// FEW, CHANGED with WIDE cut).  A distance and a cap are float32 work for each score.
+enum Pass { FORWARD, GRAD_Q, GRAD_K };
+inline double tile_us(const dsmp_attention_desc& d, Pass pass, bool wide) {
+  static const double bf16[3][2][3] = {{{0.40, 0.58, 1.04}, {0.25, 0.36, 0.65}},
+                                       {{0.50, 0.74, 1.40}, {0.33, 0.48, 0.90}},
+                                       {{0.75, 1.04, 2.10}, {0.80, 1.26, 2.50}}};
+  static const double f32[3][3] = {{2.2, 3.3, 6.0}, {3.0, 4.5, 9.0}, {4.0, 6.0, 12.0}};
+  const int w = d.head_dim <= 32 ? 0 : d.head_dim <= 64 ? 1 : 2;
+  if (d.dtype == DSMP_F32) return f32[pass][w] + (d.dim ? 0.5 : 0.0) + (d.cap != 0.0f ? 0.5 : 0.0);
+  const double more = (d.dim ? 0.50 : 0.0) + (d.cap != 0.0f ? 0.25 : 0.0);
+  return bf16[pass][wide ? 0 : 1][w] + (wide ? more : 0.5 * more);
+}
+// whether a CU's registers or LDS hold one workgroup only
+inline bool one_to_a_cu(const dsmp_attention_desc& d, Pass pass, bool wide) {
+  if (d.dtype == DSMP_F32) return d.head_dim > 64 || (pass != FORWARD && !wide && d.head_dim > 32) || (pass == GRAD_K && d.head_dim > 32);
+  return d.head_dim > 64 && (!wide || pass == GRAD_K);
+}
+
+// One or two kinds of workgroups in a launch, `groups` with `steps` tiles of `us` to go over, and the bytes
+// of the parts of one split.  They are cut so that a workgroup has about the same amount of work,
+// as far as the shortest estimated time asks: the work dealt to 256 CUs, of which one workgroup takes about
+// 0.55 and two 0.8, a third of a workgroup's for the uneven end, and the launch that adds up the parts
+// (3 us, and their bytes written and read at 4 TB/s).
 struct Cut {
   int64_t groups, steps;
-  double us, bytes;   // of a tile; of the parts of one split
+  double us, bytes;
   int splits;
 };
-inline void cut_evenly(Cut* c, int n, int64_t slots, int most) {
+inline double cut_evenly(Cut* c, int n, bool one, int most) {
+  constexpr double CUS = 256;
   double total = 0, best = 0;
   for (int i = 0; i < n; ++i) total += c[i].groups * c[i].steps * c[i].us;
   int now[2] = {1, 1};
-  for (int k = 0; k <= 4; ++k) {   // k = 0: uncut
+  static const int targets[] = {0, 1, 2, 3, 4, 6, 8};   // workgroups to a CU; 0: uncut
+  for (const int k : targets) {
     double sum = 0, longest = 0, join = 0;
     int64_t groups = 0;
     for (int i = 0; i < n; ++i) {
-      const int64_t per = k ? std::max<int64_t>(1, (int64_t)std::ceil(total / (k * slots * c[i].us))) : std::max<int64_t>(1, c[i].steps);
+      const int64_t per = k ? std::max<int64_t>(1, (int64_t)std::ceil(total / (k * CUS * c[i].us))) : std::max<int64_t>(1, c[i].steps);
       now[i] = (int)std::min<int64_t>(most, std::max<int64_t>(1, (c[i].steps + per - 1) / per));
       const double time = c[i].groups ? (double)((c[i].steps + now[i] - 1) / now[i]) * c[i].us : 0.0;
       sum += c[i].groups * now[i] * time;
@@ -483,12 +524,19 @@ inline void cut_evenly(Cut* c, int n, int64_t slots, int most) {
       if (now[i] > 1) join += 2 * now[i] * c[i].bytes / 4e6;
     }
     if (now[0] > 1 || (n > 1 && now[1] > 1)) join += 3.0;
-    const double time = (groups <= slots ? longest : sum / slots + 0.5 * longest) + join;
+    const double each = groups / CUS;
+    const double part = one ? 0.7 : each <= 1 ? 0.55 : each <= 2 ? 0.55 + 0.25 * (each - 1) : std::min(1.0, 0.8 + 0.2 * (each - 2));
+    const double time = (each <= 1 ? longest / part : sum / (CUS * part) + 0.3 * longest) + join;
     if (k == 0 || time < best) {
       best = time;
       for (int i = 0; i < n; ++i) c[i].splits = now[i];
     }
   }
+  return best;
+}
+// tiles of `size` rows that there are, for an estimate (a launch has tiles_of)
+inline int64_t about_tiles(int64_t n, int64_t n_seg, int M, int size) {
+  return (n * M + size - 1) / size + (n_seg > 1 ? std::min<int64_t>(n, n_seg / 2) : 0);
 }
 
 size_t attention_bwd_bytes(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks);

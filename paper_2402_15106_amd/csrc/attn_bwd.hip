@@ -48,26 +48,35 @@ struct BwdPlan {
   int64_t grid_q, grid_k;
 };
 
-// Rows and keys each in tiles of 128 where these fill the card, else of 32, and where these are
-// few as well cut over the other side.
+// The gradients of the queries and of the keys each WIDE or FEW, cut each for itself; or both FEW, in one launch.
 BwdPlan bwd_plan(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks) {
-  const int G = d.heads / d.kv_heads;
-  BwdPlan p{false, false, 1, 1, tiles_of(qs.n, qs.n_seg, G, 32 * BW) * d.kv_heads, tiles_of(ks.n, ks.n_seg, 1, 32 * BW) * d.kv_heads};
-  p.wide_q = p.grid_q >= FILL, p.wide_k = p.grid_k >= FILL;
-  if (!p.wide_q) p.grid_q = tiles_of(qs.n, qs.n_seg, G, 32) * d.kv_heads;
-  if (!p.wide_k) p.grid_k = tiles_of(ks.n, ks.n_seg, 1, 32) * d.kv_heads;
-  // microseconds of a tile, as measured: three products against four; float32 heads over 32 and
-  // bfloat16 ones over 64 leave a SIMD's registers to one wave
-  const bool f32 = d.dtype == DSMP_F32, one = d.head_dim > (f32 ? 32 : 64);
-  const double tile = (f32 ? 6.0 : 1.2) * (d.head_dim <= 32 ? 1 : d.head_dim <= 64 ? (f32 ? 1.2 : 2) : (f32 ? 2.5 : 4));
-  Cut c[2] = {{p.wide_q || !qs.n ? 0 : p.grid_q, (ks.n / ks.n_seg + 127) / 128, 0.75 * tile, 4.0 * qs.n * d.heads * d.head_dim, 1},
-              {p.wide_k || !ks.n ? 0 : p.grid_k, (qs.n / qs.n_seg * G + 127) / 128, tile, 8.0 * ks.n * d.kv_heads * d.head_dim, 1}};
-  cut_evenly(c, 2, one ? FILL / 2 : FILL, 64);
-  if (c[0].groups) p.splits_q = c[0].splits;
-  if (c[1].groups) p.splits_k = c[1].splits;
+  const int G = d.heads / d.kv_heads, per_wide = d.dtype == DSMP_F32 ? 32 : 64;
+  const int64_t keys = ks.n / ks.n_seg, rows = qs.n / qs.n_seg * G;
+  const double bq = 4.0 * qs.n * d.heads * d.head_dim, bk = 8.0 * ks.n * d.kv_heads * d.head_dim;
+  Cut q[2], k[2], both[2];
+  double tq[2], tk[2];
+  for (int wide = 0; wide < 2; ++wide) {
+    const int own = wide ? 32 * BW : 32, along = wide ? per_wide : 128;
+    q[wide] = {qs.n ? about_tiles(qs.n, qs.n_seg, G, own) * d.kv_heads : 0, (keys + along - 1) / along, tile_us(d, GRAD_Q, wide), bq, 1};
+    k[wide] = {ks.n ? about_tiles(ks.n, ks.n_seg, 1, own) * d.kv_heads : 0, (rows + along - 1) / along, tile_us(d, GRAD_K, wide), bk, 1};
+  }
+  both[0] = q[0], both[1] = k[0];
+  const double together = cut_evenly(both, 2, one_to_a_cu(d, GRAD_K, false), 64);
+  for (int wide = 0; wide < 2; ++wide) {
+    tq[wide] = cut_evenly(&q[wide], 1, one_to_a_cu(d, GRAD_Q, wide), 64);
+    tk[wide] = cut_evenly(&k[wide], 1, one_to_a_cu(d, GRAD_K, wide), 64);
+  }
+  BwdPlan p{};
+  p.wide_q = tq[1] < tq[0], p.wide_k = tk[1] < tk[0];
+  p.splits_q = q[p.wide_q].splits, p.splits_k = k[p.wide_k].splits;
+  if (together < std::min(tq[0], tq[1]) + std::min(tk[0], tk[1]) + 3.0) {
+    p.wide_q = p.wide_k = false;
+    p.splits_q = both[0].splits, p.splits_k = both[1].splits;
+  }
+  p.grid_q = qs.n ? tiles_of(qs.n, qs.n_seg, G, p.wide_q ? 32 * BW : 32) * d.kv_heads : 0;
+  p.grid_k = ks.n ? tiles_of(ks.n, ks.n_seg, 1, p.wide_k ? 32 * BW : 32) * d.kv_heads : 0;
+  if (p.grid_q * p.splits_q + p.grid_k * p.splits_k > MAX_GROUPS) p.splits_q = p.splits_k = 1;
   p.grid_q *= p.splits_q, p.grid_k *= p.splits_k;
-  if (qs.n == 0) p.grid_q = 0;
-  if (ks.n == 0) p.grid_k = 0;
   return p;
 }
 
@@ -144,9 +153,13 @@ extern "C" dsmp_status dsmp_attention_backward(dsmp_handle* h, const dsmp_attent
     } else if (few_q + few_k) {
       hipLaunchKernelGGL((k_attn_bwd_few<T, D, 0, M>), dim3((unsigned)(few_q + few_k)), dim3(BT), 0, h->stream, a);
     }
-    if (joined) hipLaunchKernelGGL((k_attn_bwd_join<T>), dim3(ceil_div(joined, BT)), dim3(BT), 0, h->stream, a);
   });
   if (p.wide_k && p.grid_k) launch_attention_dkv(h, *desc, a, p.grid_k);
+  if (joined) {
+    const dim3 grid(ceil_div(joined, BT));
+    if (desc->dtype == DSMP_BF16) hipLaunchKernelGGL((k_attn_bwd_join<__bf16>), grid, dim3(BT), 0, h->stream, a);
+    else hipLaunchKernelGGL((k_attn_bwd_join<float>), grid, dim3(BT), 0, h->stream, a);
+  }
   DSMP_LAUNCHED(h, "attention backward");
   return DSMP_OK;
 }

@@ -48,22 +48,6 @@ struct BwdLds {
   __shared__ __align__(16) float name##x0[C::EXTRA], name##x1[C::DMA ? C::EXTRA : 4];                             \
   const BwdLds name{name##a0, name##b0, name##a1, name##b1, name##x0, name##x1}
 
-// A wave's 32 rows of results (D values each, a lane's column), scaled: to `out`, or in float32 to `part`.
-template <typename T, int D>
-__device__ __forceinline__ void write_rows(const f32x16* acc, float scale, T* out, float* part, int hd) {
-  const int h = ((int)threadIdx.x & 63) >> 5;
-#pragma unroll
-  for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-    for (int i4 = 0; i4 < 4; ++i4) {
-      const int c = 32 * d + 8 * i4 + 4 * h;
-      if (c >= hd) continue;
-      const float v[4] = {acc[d][4 * i4] * scale, acc[d][4 * i4 + 1] * scale, acc[d][4 * i4 + 2] * scale, acc[d][4 * i4 + 3] * scale};
-      if (part) *(float4*)(part + c) = make_float4(v[0], v[1], v[2], v[3]);
-      else store4(out + c, v[0], v[1], v[2], v[3]);
-    }
-}
-
 // The four waves' results of the same 32 rows added up in LDS ([value][row], two waves' in each of a buffer's
 // matrices) and written: 256 threads with a row and four values in 32 each.
 template <typename T, int D>
@@ -102,8 +86,8 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, const BwdLds& lds, un
   const int tid = (int)threadIdx.x, l = tid & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = (int)(group % (unsigned)a.Hk);
   const unsigned rest = group / (unsigned)a.Hk;
-  const int split = FEW ? (int)(rest % (unsigned)a.splits) : 0;
-  const int64_t tile = FEW ? rest / (unsigned)a.splits : rest;
+  const int split = (int)(rest % (unsigned)a.splits);
+  const int64_t tile = rest / (unsigned)a.splits;
   int64_t first;
   const int seg = FEW ? find_segment(a.qb, a.n_seg, a.G, C::OWN, tile, &first)
                       : find_segment_longest_first(a.qb, a.kb, a.n_seg, a.G, C::OWN, tile, &first);
@@ -111,7 +95,7 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, const BwdLds& lds, un
   if (tile < first || r0 >= R) return;
   const int64_t k0 = a.kb.at(seg), klen = a.kb.at(seg + 1) - k0;
   const int tiles = klen > 0 ? (int)((klen + C::BN - 1) / C::BN) : 0;
-  const int per = FEW ? (tiles + a.splits - 1) / a.splits : tiles;
+  const int per = (tiles + a.splits - 1) / a.splits;
   const int t_begin = min(split * per, tiles), t_end = min(t_begin + per, tiles);
 
   const bool cap = M::cap(a);
@@ -291,9 +275,9 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, const BwdLds& lds, un
   asm volatile("" : "+v"(again));
   const RowOf mine = row_of(a, q0, r0, R, kvh, FEW, again);
   T* out = (T*)a.gq + mine.query * a.ldgq + mine.head * a.hd;
-  float* part = FEW && a.splits > 1 ? a.part + ((int64_t)split * a.nq * a.H + mine.query * a.H + mine.head) * a.hd : nullptr;
+  float* part = a.splits > 1 ? a.part + ((int64_t)split * a.nq * a.H + mine.query * a.H + mine.head) * a.hd : nullptr;
   if (FEW) join_rows<T, D>(acc, lds, a.scale, out, part, a.hd, mine.there);
-  else if (mine.there) write_rows<T, D>(acc, a.scale, out, nullptr, a.hd);
+  else if (mine.there) write_rows<T, D>(acc, a.scale, out, part, a.hd);
 }
 
 // PAIRED: an even number of heads share their keys, so that rows two by two have the same query, and the
@@ -307,8 +291,8 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
   const int tid = (int)threadIdx.x, l = tid & 63, h = l >> 5, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = (int)(group % (unsigned)a.Hk);
   const unsigned rest = group / (unsigned)a.Hk;
-  const int split = FEW ? (int)(rest % (unsigned)a.splits_k) : 0;
-  const int64_t tile = FEW ? rest / (unsigned)a.splits_k : rest;
+  const int split = (int)(rest % (unsigned)a.splits_k);
+  const int64_t tile = rest / (unsigned)a.splits_k;
   int64_t first;
   const int seg = FEW ? find_segment(a.kb, a.n_seg, 1, C::OWN, tile, &first)
                       : find_segment_longest_first(a.kb, a.qb, a.n_seg, 1, C::OWN, tile, &first);
@@ -316,7 +300,7 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
   if (tile < first || j0 >= klen) return;
   const int64_t q0 = a.qb.at(seg), queries = a.qb.at(seg + 1) - q0, R = queries > 0 ? queries * a.G : 0;
   const int tiles = (int)((R + C::BN - 1) / C::BN);
-  const int per = FEW ? (tiles + a.splits_k - 1) / a.splits_k : tiles;
+  const int per = (tiles + a.splits_k - 1) / a.splits_k;
   const int t_begin = min(split * per, tiles), t_end = min(t_begin + per, tiles);
 
   const bool cap = M::cap(a);
@@ -585,13 +569,14 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
   const bool there = j < klen;
   T* gk = (T*)a.gk + key * a.ldgk + kvh * a.hd;
   T* gv = (T*)a.gv + key * a.ldgv + kvh * a.hd;
+  const int64_t at = (((int64_t)split * a.nk + key) * a.Hk + kvh) * a.hd;
+  float *pk = a.splits_k > 1 ? a.part_k + at : nullptr, *pv = a.splits_k > 1 ? a.part_v + at : nullptr;
   if (FEW) {
-    const int64_t at = (((int64_t)split * a.nk + key) * a.Hk + kvh) * a.hd;
-    join_rows<T, D>(dk, lds, a.scale, gk, a.splits_k > 1 ? a.part_k + at : nullptr, a.hd, there);
-    join_rows<T, D>(dv, lds, 1.0f, gv, a.splits_k > 1 ? a.part_v + at : nullptr, a.hd, there);
+    join_rows<T, D>(dk, lds, a.scale, gk, pk, a.hd, there);
+    join_rows<T, D>(dv, lds, 1.0f, gv, pv, a.hd, there);
   } else if (there) {
-    write_rows<T, D>(dk, a.scale, gk, nullptr, a.hd);
-    write_rows<T, D>(dv, 1.0f, gv, nullptr, a.hd);
+    write_rows<T, D>(dk, a.scale, gk, pk, a.hd);
+    write_rows<T, D>(dv, 1.0f, gv, pv, a.hd);
   }
 }
 

@@ -256,19 +256,18 @@ __global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::template WAVES<M>)) void k_att
   asm volatile("" : "+v"(again));
   const RowOf mine = row_of(a, q0, r0, R, kvh, FEW, again);
   const int64_t slot = mine.query * a.H + mine.head;   // this row's among all queries and heads
+  const int64_t part = (int64_t)split * a.nq * a.H + slot;
+  float* const ml = a.part + (int64_t)a.splits * a.nq * a.H * a.hd + 2 * part;
   if (!FEW) {
     if (!mine.there) return;
+    if (a.splits > 1) {
+      if (h == 0) ml[0] = fmaf(m, sc.A, sc.C), ml[1] = sum;
+      write_rows<T, D>(o, 1.0f, (T*)nullptr, a.part + part * a.hd, a.hd);
+      return;
+    }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     if (a.lse && h == 0) a.lse[slot] = (fmaf(m, sc.A, sc.C) + __log2f(sum)) * LN2;
-    T* out = (T*)a.out + mine.query * a.ldout + mine.head * a.hd;
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) {
-        const int c = 32 * d + 8 * i4 + 4 * h;
-        if (c < a.hd)
-          store4(out + c, o[d][4 * i4] * inv, o[d][4 * i4 + 1] * inv, o[d][4 * i4 + 2] * inv, o[d][4 * i4 + 3] * inv);
-      }
+    write_rows<T, D>(o, inv, (T*)a.out + mine.query * a.ldout + mine.head * a.hd, nullptr, a.hd);
     return;
   }
   // the waves' parts, [value][row], two in each of a buffer's matrices, joined by 256 threads: a row and
@@ -295,10 +294,8 @@ __global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::template WAVES<M>)) void k_att
   const int g4 = 4 * (tid >> 5);
   const bool whole = a.splits == 1;
   const float inv = !whole ? 1.0f : total == 0.0f ? 0.0f : 1.0f / total;
-  const int64_t part = (int64_t)split * a.nq * a.H + slot;
   if (tid < 32) {
     if (!whole) {
-      float* ml = a.part + (int64_t)a.splits * a.nq * a.H * a.hd + 2 * part;
       ml[0] = top, ml[1] = total;
     } else if (a.lse) {
       a.lse[slot] = (top + __log2f(total)) * LN2;
@@ -426,19 +423,22 @@ struct FwdPlan {
   int64_t grid;
 };
 
-// Rows in tiles of 128 where these fill the card, else of 32, whose keys are dealt to
-// the waves, and where these are few as well to several workgroups.
 FwdPlan fwd_plan(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks) {
   const int G = d.heads / d.kv_heads;
-  FwdPlan p{false, 1, tiles_of(qs.n, qs.n_seg, G, 32 * NW) * d.kv_heads};
-  if (p.grid >= FILL) return p;
-  p.few = true;
-  p.grid = tiles_of(qs.n, qs.n_seg, G, 32) * d.kv_heads;
-  // microseconds of a tile, as measured; heads over 64 leave a SIMD's registers to one wave
-  const double tile = (d.dtype == DSMP_F32 ? 3.5 : 0.5) * (d.head_dim <= 32 ? 1 : d.head_dim <= 64 ? 2 : 4);
-  Cut c{p.grid, (ks.n / ks.n_seg + 127) / 128, tile, 4.0 * qs.n * d.heads * d.head_dim, 1};
-  cut_evenly(&c, 1, d.head_dim > 64 ? FILL / 2 : FILL, MAX_SPLITS);
-  p.splits = c.splits;
+  const int64_t keys = ks.n / ks.n_seg;
+  const double bytes = 4.0 * qs.n * d.heads * d.head_dim;
+  const int per_wide = d.dtype == DSMP_F32 ? 32 : 64;
+  Cut wide{about_tiles(qs.n, qs.n_seg, G, 32 * NW) * d.kv_heads, (keys + per_wide - 1) / per_wide, tile_us(d, FORWARD, true), bytes, 1};
+  Cut few{about_tiles(qs.n, qs.n_seg, G, 32) * d.kv_heads, (keys + 127) / 128, tile_us(d, FORWARD, false), bytes, 1};
+  // one tile of rows to a segment: keys and values come from memory, once, at 5 TB/s
+  if (qs.n * G <= 32 * qs.n_seg) few.us = std::max(few.us, 128.0 * d.head_dim * (d.dtype == DSMP_F32 ? 8 : 4) * 256 / 5e6);
+  const double tw = cut_evenly(&wide, 1, one_to_a_cu(d, FORWARD, true), 64);
+  const double tf = cut_evenly(&few, 1, one_to_a_cu(d, FORWARD, false), MAX_SPLITS);
+  FwdPlan p{};
+  p.few = tf <= tw;
+  p.splits = p.few ? few.splits : wide.splits;
+  p.grid = tiles_of(qs.n, qs.n_seg, G, p.few ? 32 : 32 * NW) * d.kv_heads;
+  if (p.grid * p.splits > MAX_GROUPS) p.splits = 1;
   p.grid *= p.splits;
   return p;
 }
