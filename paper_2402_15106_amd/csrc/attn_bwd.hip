@@ -61,10 +61,10 @@ BwdPlan bwd_plan(const dsmp_attention_desc& d, const dsmp_segments& qs, const ds
     k[wide] = {ks.n ? about_tiles(ks.n, ks.n_seg, 1, own) * d.kv_heads : 0, (rows + along - 1) / along, tile_us(d, GRAD_K, wide), bk, 1};
   }
   both[0] = q[0], both[1] = k[0];
-  const double together = cut_evenly(both, 2, one_to_a_cu(d, GRAD_K, false), 64);
+  const double together = cut_evenly(both, 2, held(d, GRAD_K, false), 64, uneven_end(ks));
   for (int wide = 0; wide < 2; ++wide) {
-    tq[wide] = cut_evenly(&q[wide], 1, one_to_a_cu(d, GRAD_Q, wide), 64);
-    tk[wide] = cut_evenly(&k[wide], 1, one_to_a_cu(d, GRAD_K, wide), 64);
+    tq[wide] = cut_evenly(&q[wide], 1, held(d, GRAD_Q, wide), 64, uneven_end(ks));
+    tk[wide] = cut_evenly(&k[wide], 1, held(d, GRAD_K, wide), 64, uneven_end(ks));
   }
   BwdPlan p{};
   p.wide_q = tq[1] < tq[0], p.wide_k = tk[1] < tk[0];

@@ -379,11 +379,20 @@ __global__ __launch_bounds__(1024) void k_attn_join(AttnArgs a) {
   const int tid = (int)threadIdx.x, c = 4 * (tid & 31), slice = tid >> 5;
   const float2 x = tid < a.splits ? ((const float2*)(a.part + (int64_t)a.splits * all * a.hd))[tid * all + slot]
                                   : make_float2(-INFINITY, 0.0f);
+  // the first parts are on their way while the weights are formed
+  constexpr int AHEAD = 8;
+  const float* from = a.part + slot * a.hd + c;
+  const int64_t step = all * a.hd;
+  float4 p[AHEAD];
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k)
+    if (c < a.hd && slice + 32 * k < a.splits) p[k] = *(const float4*)(from + (slice + 32 * k) * step);
   float top = x.x;
   for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
   if ((tid & 63) == 0) wave[0][tid >> 6] = top;
   __syncthreads();
   top = wave[0][0];
+#pragma unroll
   for (int k = 1; k < 16; ++k) top = fmaxf(top, wave[0][k]);
   const float mine = x.y == 0.0f ? 0.0f : exp2_of(x.x - (top == -INFINITY ? 0.0f : top));
   weight[tid] = mine;
@@ -392,18 +401,20 @@ __global__ __launch_bounds__(1024) void k_attn_join(AttnArgs a) {
   if ((tid & 63) == 0) wave[1][tid >> 6] = total;
   __syncthreads();
   total = 0.0f;
+#pragma unroll
   for (int k = 0; k < 16; ++k) total += wave[1][k];
   float v[4] = {};
-  if (c < a.hd) {
-    const float* from = a.part + slot * a.hd + c;
-    const int64_t step = all * a.hd;
-#pragma unroll 8
-    for (int s = slice; s < a.splits; s += 32) {
-      const float w = weight[s];
-      const float4 p = *(const float4*)(from + s * step);
+  auto add = [&](int s, const float4& q) {
+    const float w = weight[s];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = w == 0.0f ? v[e] : fmaf(w, (&p.x)[e], v[e]);
-    }
+    for (int e = 0; e < 4; ++e) v[e] = w == 0.0f ? v[e] : fmaf(w, (&q.x)[e], v[e]);
+  };
+  if (c < a.hd) {
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (slice + 32 * k < a.splits) add(slice + 32 * k, p[k]);
+#pragma unroll 4
+    for (int s = slice + 32 * AHEAD; s < a.splits; s += 32) add(s, *(const float4*)(from + s * step));
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) red[slice][c + e] = v[e];
@@ -412,6 +423,7 @@ __global__ __launch_bounds__(1024) void k_attn_join(AttnArgs a) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     v[e] = 0.0f;
+#pragma unroll
     for (int s = 0; s < 32; ++s) v[e] += red[s][c + e];
   }
   write_joined<T>(a, slot, query, c, v, top, total);
@@ -430,12 +442,14 @@ FwdPlan fwd_plan(const dsmp_attention_desc& d, const dsmp_segments& qs, const ds
   const int per_wide = d.dtype == DSMP_F32 ? 32 : 64;
   Cut wide{about_tiles(qs.n, qs.n_seg, G, 32 * NW) * d.kv_heads, (keys + per_wide - 1) / per_wide, tile_us(d, FORWARD, true), bytes, 1};
   Cut few{about_tiles(qs.n, qs.n_seg, G, 32) * d.kv_heads, (keys + 127) / 128, tile_us(d, FORWARD, false), bytes, 1};
+  double end = uneven_end(ks);
   // one tile of rows to a segment: keys and values come from memory, once, at 5 TB/s
-  if (qs.n * G <= 32 * qs.n_seg) few.us = std::max(few.us, 128.0 * d.head_dim * (d.dtype == DSMP_F32 ? 8 : 4) * 256 / 5e6);
-  const double tw = cut_evenly(&wide, 1, one_to_a_cu(d, FORWARD, true), 64);
-  const double tf = cut_evenly(&few, 1, one_to_a_cu(d, FORWARD, false), MAX_SPLITS);
+  const bool once = qs.n * G <= 32 * qs.n_seg;
+  if (once) end *= 2, few.us = std::max(few.us, 128 * d.head_dim * (d.dtype == DSMP_F32 ? 8.0 : 4.0) * 256 / 5e6);
+  const double tw = cut_evenly(&wide, 1, held(d, FORWARD, true), 64, end);
+  const double tf = cut_evenly(&few, 1, held(d, FORWARD, false), MAX_SPLITS, end);
   FwdPlan p{};
-  p.few = tf <= tw;
+  p.few = once || tf <= tw;
   p.splits = p.few ? few.splits : wide.splits;
   p.grid = tiles_of(qs.n, qs.n_seg, G, p.few ? 32 : 32 * NW) * d.kv_heads;
   if (p.grid * p.splits > MAX_GROUPS) p.splits = 1;
