@@ -143,20 +143,23 @@ __device__ __forceinline__ u32x4 buffer_read(__amdgpu_buffer_rsrc_t r, uint32_t 
 // ------------------------------------------------------ tiles of bfloat16 rows in LDS
 // Rows of D values without room between them, copied from memory directly (64 lanes write 1,024
 // bytes in a row; no registers on the way).  The 16-byte units of row r are permuted by
-// XOR with swizzle(r), so that both kinds of reads are free of bank conflicts: eight rows at the
-// same unit (lds_rows), and four rows over four units (lds_columns).  LDS has 64 banks of 4 bytes: a
-// row has 16, 32 or 64 of them, so among eight rows 2, 4 or 8 begin at the same bank.
+// XOR with swizzle(r), so that both kinds of reads are free of bank conflicts: 16 rows at the
+// same unit at once (tile_rows), and four rows over four units (tile_columns).  LDS has 64 banks of 4
+// bytes: a row has 16, 32 or 64 of them, so among 16 rows 4, 8 or all begin at the same bank.
 template <int D>
 __device__ __forceinline__ int swizzle(int r) {
-  if (D == 32) return (r >> 2) & 1;
-  if (D == 64) return ((r >> 1) & 1) * 4 + ((r >> 2) & 1);
-  return (r & 3) * 4 + ((r >> 2) & 1);
+  if (D == 32) return (r >> 2) & 3;
+  if (D == 64) return ((r >> 1) & 1) * 4 + ((r >> 2) & 1) * 2 + ((r >> 3) & 1);
+  return (r & 3) * 4 + ((r >> 2) & 3);
 }
+// what eight rows further on flip in a unit's place
+template <int D>
+constexpr uint32_t EIGHT_ROWS = 16 * (D == 64 ? 1 : 2);
 
 template <int D, int ROWS>
 struct TileCopy {
   static constexpr int RB = 2 * D, UPR = RB / 16, PER = ROWS * UPR / 256, STEP = 256 / UPR;
-  static_assert(ROWS * UPR % 256 == 0 && STEP % 8 == 0, "whole loads of a workgroup, rows of one permutation to a lane");
+  static_assert(ROWS * UPR % 256 == 0 && STEP % 16 == 0, "whole loads of a workgroup, rows of one permutation to a lane");
   // a lane's row in its first load, and the unit that it copies there, in bytes
   static __device__ __forceinline__ int row0() { return (int)threadIdx.x / UPR; }
   static __device__ __forceinline__ int unit0() { return ((int)threadIdx.x % UPR ^ swizzle<D>(row0())) * 16; }
@@ -194,8 +197,9 @@ __device__ __forceinline__ typename Frag<T>::type tile_columns(lds_u8* X, const 
     return lds_columns<T>(X, pitch_of<T, D, true>(), r0, c0);
   } else {
     lds_u8* p = X + r0 * 2 * D + (at.columns ^ (uint32_t)(2 * c0));
+    lds_u8* p8 = X + (r0 + 8) * 2 * D + (at.columns ^ ((uint32_t)(2 * c0) ^ EIGHT_ROWS<D>));
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * 2 * D));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p8);
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   }
 }
@@ -224,7 +228,9 @@ __device__ __forceinline__ void store4(T* p, float a, float b, float c, float d)
 // A wave's 32 rows of results (D values each, a lane's column), scaled: to `out`, or in float32 to `part`.
 template <typename T, int D>
 __device__ __forceinline__ void write_rows(const f32x16* acc, float scale, T* out, float* part, int hd) {
-  const int h = ((int)threadIdx.x & 63) >> 5;
+  int tid = (int)threadIdx.x;
+  asm volatile("" : "+v"(tid));   // what follows from it is formed here, not kept in registers over the caller's loop
+  const int h = (tid & 63) >> 5;
 #pragma unroll
   for (int d = 0; d < D / 32; ++d)
 #pragma unroll

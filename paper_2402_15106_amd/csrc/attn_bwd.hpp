@@ -379,28 +379,29 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
           dp[i] *= x[i];
           if (cap) dp[i] *= fall;
         }
-        if (dim) __builtin_amdgcn_sched_barrier(0);
+        if (dim || i4 == 1) __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_sched_barrier(0);
-      frag cg[2], cq[2], pf{}, sf{};
-      cg[0] = tile_columns<T, D>(ldsG, lane, at, 0), cq[0] = tile_columns<T, D>(ldsQ, lane, at, 0);
+      // the products for dv and dk in turn, fragments one ahead (none in float32, whose are large and products long)
+      frag cf[2], pf{}, sf{};
+      auto columns = [&](int n) {
+        return tile_columns<T, D>(n & 1 ? ldsQ : ldsG, lane, at + 16 * (n / 2 / DB), 32 * (n / 2 % DB));
+      };
+      cf[0] = columns(0);
 #pragma unroll
-      for (int k = 0; k < 2 * DB; ++k) {
-        const int t2 = k / DB, d = k % DB;
-        if (d == 0) {
+      for (int n = 0; n < 4 * DB; ++n) {
+        const int t2 = n / 2 / DB, d = n / 2 % DB;
+        if (d == 0 && n % 2 == 0) {
           float p[8], ds[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) p[i] = x[8 * t2 + i], ds[i] = dp[8 * t2 + i];
           pf = to_frag<T>(p), sf = to_frag<T>(ds);
         }
-        if (ES == 4 && k > 0)   // large fragments, long products: none ahead (nor above for wide heads)
-          cg[k & 1] = tile_columns<T, D>(ldsG, lane, at + 16 * t2, 32 * d), cq[k & 1] = tile_columns<T, D>(ldsQ, lane, at + 16 * t2, 32 * d);
-        if (ES != 4 && k + 1 < 2 * DB) {
-          const int r = at + 16 * ((k + 1) / DB), c = 32 * ((k + 1) % DB);
-          cg[(k + 1) & 1] = tile_columns<T, D>(ldsG, lane, r, c), cq[(k + 1) & 1] = tile_columns<T, D>(ldsQ, lane, r, c);
-        }
-        dv[d] = mma(cg[k & 1], pf, dv[d]), dk[d] = mma(cq[k & 1], sf, dk[d]);
-        __builtin_amdgcn_sched_barrier(0);
+        if (ES == 4 && n > 0) cf[n & 1] = columns(n);
+        if (ES != 4 && n + 1 < 4 * DB) cf[(n + 1) & 1] = columns(n + 1);
+        if (n & 1) dk[d] = mma(cf[n & 1], sf, dk[d]);
+        else dv[d] = mma(cf[n & 1], pf, dv[d]);
+        if (n & 1) __builtin_amdgcn_sched_barrier(0);
       }
     }
 #pragma unroll
