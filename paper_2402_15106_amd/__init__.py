@@ -2,8 +2,9 @@
 
 Node sampling, radius-graph construction, the edge-conditioned
 message-passing layer (forward and backward), the encoder, decoder and loss of
-the hop loop, group norms and 8-bit activation checkpoints as hand-written HIP
-kernels behind a C ABI (include/dsmpnn.h); this package is the thin Python binding.
+the hop loop, group norms, 8-bit activation checkpoints and attention within
+packed sub-graphs as hand-written HIP kernels behind a C ABI (include/dsmpnn.h);
+this package is the thin Python binding.
 """
 
 from ._lib import (  # noqa: F401
@@ -15,3 +16,4 @@ from ._lib import (  # noqa: F401
 from .hop import HopShapes, HopStep  # noqa: F401,E402
 from .infer import SubdomainInference  # noqa: F401,E402
 from .stack import CheckpointedStack, StackShapes  # noqa: F401,E402
+from .attention import AttentionLayer, AttentionShapes  # noqa: F401,E402

@@ -1,0 +1,110 @@
+"""Attention within packed sub-graphs as a layer, composed from library calls (call
+order and buffers only; the projections are plain matrix products of torch).
+
+    [q k v] = u Wqkv^T, q and k normed for each head and rotated by the nodes' coordinates
+    out = softmax(c(q.k / sqrt(head_dim)) - slope |p_i - p_j|) v  over the nodes of a sub-graph
+    f = out Wo^T
+
+Message passing reaches the neighbours within the radius; here every node of a sub-graph
+sees every other one.  u is what a norm hands to a layer (dsmp_group_norm_forward), f is
+float32, the addend of the next norm, as a message-passing layer's output is.
+"""
+
+from dataclasses import dataclass
+
+import torch
+
+from . import _lib as L
+
+
+@dataclass
+class AttentionShapes:
+    n: int                 # nodes
+    d: int                 # width of u and f
+    heads: int
+    kv_heads: int          # divides heads
+    head_dim: int          # a multiple of 8, at most 128
+    dtype: int             # F32 or BF16: u and the weights
+    dim: int               # coordinates (1..3): of the rotation and of the distance
+    rot: int = 0           # rotated values of each head
+    layout: int = L.ROTATE_HALF
+    norm: bool = True      # queries and keys normed
+    cap: float = 0.0
+    distance: bool = True  # whether scores fall with the distance
+    eps: float = 1e-6
+
+
+class AttentionLayer:
+    """Buffers for n nodes; ``forward`` gives f, ``backward`` the gradients of the forward
+    call that came last, with its arguments as they were.  ``read`` is for evaluation: few points
+    that read the field of many nodes.
+
+    params: Wqkv [(heads + 2 kv_heads) head_dim, d], Wo [d, heads head_dim] (of the layer's type),
+    gamma_q, gamma_k (float32 [head_dim], with norm), freq (float32 [rot / 2], with rot),
+    slopes (float32 [heads], with distance)."""
+
+    def __init__(self, lib: "L.Dsmp", s: AttentionShapes):
+        self.lib, self.s = lib, s
+        self.rotate = L.rotate_desc(s.heads, s.kv_heads, s.head_dim, s.dtype, s.rot, axes=s.dim, layout=s.layout,
+                                    norm=s.norm, eps=s.eps)
+        self.attend = L.attention_desc(s.heads, s.kv_heads, s.head_dim, s.dtype, dim=s.dim if s.distance else 0, cap=s.cap)
+        self.wq, self.wk = s.heads * s.head_dim, s.kv_heads * s.head_dim
+        self._kept = None
+
+    def _project(self, u, W, what):
+        if u.dim() != 2 or u.shape[1] != self.s.d or u.dtype is not L._TORCH.get(self.s.dtype):
+            raise L.DsmpError(L.INVALID_ARG, "%s: a %s matrix of %d columns is needed" % (what, L._TORCH.get(self.s.dtype), self.s.d))
+        return torch.mm(u, W.t())
+
+    @staticmethod
+    def _buffer(like, segments):
+        """Rows of no segment stay as they are: zero."""
+        return torch.zeros_like(like) if isinstance(segments, torch.Tensor) else torch.empty_like(like)
+
+    def _attention(self, p, q, k, v, pos, k_pos, segments, k_segments):
+        place = dict(pos=pos, k_pos=k_pos, slopes=p["slopes"]) if self.s.distance else {}
+        return place, self.lib.dsmp_attention_forward(self.attend, q, k, v, segments=segments, k_segments=k_segments,
+                                                      out=self._buffer(q, segments), **place)
+
+    def forward(self, params: dict, u: torch.Tensor, pos: torch.Tensor, segments=None) -> torch.Tensor:
+        """f [n, d] (float32) of u [n, d] at pos (float32 [n, dim]); segments as for the norms."""
+        lib, p, wq, wk = self.lib, params, self.wq, self.wk
+        self._kept = None
+        if u.shape[0] != self.s.n:
+            raise L.DsmpError(L.INVALID_ARG, "u: %d rows are needed" % self.s.n)
+        qkv = self._project(u, p["Wqkv"], "u")
+        q, k, v = qkv[:, :wq], qkv[:, wq:wq + wk], qkv[:, wq + wk:]
+        qr, kr = lib.dsmp_qk_rotate_forward(self.rotate, q, k, p.get("gamma_q"), p.get("gamma_k"), pos, p.get("freq"))
+        place, (out, lse) = self._attention(p, qr, kr, v, pos, None, segments, None)
+        f = torch.mm(out, p["Wo"].t()).float()
+        self._kept = (p, u, pos, segments, place, qkv, qr, kr, out, lse)
+        return f
+
+    def backward(self, grad_f: torch.Tensor):
+        """(grad_u float32, {"dWqkv", "dWo"[, "dgamma_q", "dgamma_k"]}) of sum(grad_f * f)."""
+        if self._kept is None:
+            raise L.DsmpError(L.INVALID_ARG, "no forward call that came to its end")
+        lib, wq, wk = self.lib, self.wq, self.wk
+        p, u, pos, segments, place, qkv, qr, kr, out, lse = self._kept
+        q, k, v = qkv[:, :wq], qkv[:, wq:wq + wk], qkv[:, wq + wk:]
+        g = grad_f.to(u.dtype)
+        dqkv = self._buffer(qkv, segments)
+        dq, dk, dv = dqkv[:, :wq], dqkv[:, wq:wq + wk], dqkv[:, wq + wk:]
+        lib.dsmp_attention_backward(self.attend, qr, kr, v, out, lse, torch.mm(g, p["Wo"]), segments=segments,
+                                    grad_q=dq, grad_k=dk, grad_v=dv, **place)
+        _, _, grads = lib.dsmp_qk_rotate_backward(self.rotate, q, k, p.get("gamma_q"), p.get("gamma_k"), pos, p.get("freq"),
+                                                  dq, dk, grad_q=dq, grad_k=dk)
+        grads["dWqkv"], grads["dWo"] = torch.mm(dqkv.t(), u).float(), torch.mm(g.t(), out).float()
+        return torch.mm(dqkv, p["Wqkv"]).float(), grads
+
+    def read(self, params: dict, u, pos, u_keys, pos_keys, segments=None, k_segments=None) -> torch.Tensor:
+        """f [m, d] (float32) at m points with features u and coordinates pos, from the nodes u_keys,
+        pos_keys of the same segments.  Nothing is kept."""
+        lib, p, wq, wk = self.lib, params, self.wq, self.wk
+        q = self._project(u, p["Wqkv"][:wq], "u")
+        kv = self._project(u_keys, p["Wqkv"][wq:], "u_keys")
+        lib.dsmp_qk_rotate_forward(self.rotate, q, None, p.get("gamma_q"), None, pos, p.get("freq"), q_out=q)
+        k = kv[:, :wk]
+        lib.dsmp_qk_rotate_forward(self.rotate, None, k, None, p.get("gamma_k"), pos_keys, p.get("freq"), k_out=k)
+        _, (out, _) = self._attention(p, q, k, kv[:, wk:], pos, pos_keys, segments, k_segments)
+        return torch.mm(out, p["Wo"].t()).float()
