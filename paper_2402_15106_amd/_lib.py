@@ -880,7 +880,7 @@ class Dsmp:
         return grad_q, grad_k, out
 
     def _attn_size(self, desc, qs, ks):
-        key = (desc.heads, desc.kv_heads, desc.head_dim, qs.n, qs.n_seg, ks.n, ks.n_seg)
+        key = (bytes(desc), qs.n, qs.n_seg, ks.n, ks.n_seg)   # the cuts depend on type, distance and cap too
         sizes = self._attn_sizes.get(key)
         if sizes is None:
             f, b = ctypes.c_size_t(), ctypes.c_size_t()

@@ -145,3 +145,20 @@ def test_scratch_of_captured_calls_is_their_own(monkeypatch):
     assert all(p not in (shared[0][0], shared[2][0]) and size >= 9000 for p, size in calls(9)) and h._ws == held
     ws = torch.empty(9000, dtype=torch.uint8)
     assert calls(9, ws=ws) == [(ws.data_ptr(), 9000)] * 3
+
+
+def test_scratch_of_calls_that_differ_in_type_or_scores_alone():
+    """The way a call is cut depends on how long its products and scores take, so its scratch does too."""
+    h = _lib.Dsmp.__new__(_lib.Dsmp)
+    h.lib, h.h, h._index, h._attn_sizes = dm.load_library(), None, -1, {}
+    differ = 0
+    for n, nk in ((5, 262144), (600, 9000), (4096, 4096), (3000, 40000)):
+        seen = set()
+        for dtype in (dm.F32, dm.BF16):
+            for dim, cap in ((0, 0.0), (3, 0.0), (2, 9.0)):
+                d = dm.attention_desc(8, 2, 64, dtype, dim=dim, cap=cap)
+                st, f, b = attention_ws(h.lib, d, (n, 1, None), (nk, 1, None))
+                assert st == dm.OK and h.dsmp_attention_workspace(d, n, nk) == (f, b), (n, nk, dtype, dim, cap)
+                seen.add((f, b))
+        differ += len(seen) > 1
+    assert differ        # else this test shows nothing
