@@ -151,7 +151,11 @@ extern "C" dsmp_status dsmp_attention_backward(dsmp_handle* h, const dsmp_attent
       if (few_k) hipLaunchKernelGGL((k_attn_bwd_few<T, D, 1, M>), dim3((unsigned)few_k), dim3(BT), 0, h->stream, a);
       if (few_q) hipLaunchKernelGGL((k_attn_bwd_few<T, D, 2, M>), dim3((unsigned)few_q), dim3(BT), 0, h->stream, a);
     } else if (few_q + few_k) {
-      hipLaunchKernelGGL((k_attn_bwd_few<T, D, 0, M>), dim3((unsigned)(few_q + few_k)), dim3(BT), 0, h->stream, a);
+      const int64_t first = few_q + few_k > MAX_GROUPS ? few_k : few_q + few_k;   // what one launch takes
+      hipLaunchKernelGGL((k_attn_bwd_few<T, D, 0, M>), dim3((unsigned)first), dim3(BT), 0, h->stream, a);
+      a.dkv_groups = 0;
+      if (first < few_q + few_k)
+        hipLaunchKernelGGL((k_attn_bwd_few<T, D, 0, M>), dim3((unsigned)few_q), dim3(BT), 0, h->stream, a);
     }
   });
   if (p.wide_k && p.grid_k) launch_attention_dkv(h, *desc, a, p.grid_k);
