@@ -517,9 +517,10 @@ dsmp_status dsmp_qk_rotate_forward(dsmp_handle* h, const dsmp_rotate_desc* desc,
 
 /* Backward from the forward's inputs: grad_q, grad_k (of dtype, as the gradients
  * that come in: operands of the projection's own gradients) receive the gradients
- * with respect to q and k, and may be grad_q_out, grad_k_out themselves.  dgamma_q, dgamma_k: device float32 [head_dim]
- * (NULL when the gamma is), summed over rows and heads, overwritten, or added to when
- * flags has DSMP_GRAD_ACCUMULATE.  Coordinates and frequencies get no gradient. */
+ * with respect to q and k, and may be grad_q_out, grad_k_out themselves (with their
+ * row distance).  dgamma_q, dgamma_k: device float32 [head_dim] (NULL when the gamma
+ * is), summed over rows and heads, overwritten, or added to when flags has
+ * DSMP_GRAD_ACCUMULATE.  Coordinates and frequencies get no gradient. */
 dsmp_status dsmp_qk_rotate_workspace(const dsmp_rotate_desc* desc, int64_t n, size_t* bwd_ws_bytes);
 dsmp_status dsmp_qk_rotate_backward(dsmp_handle* h, const dsmp_rotate_desc* desc, int64_t n, const void* q, int64_t ldq,
                                     const void* k, int64_t ldk, const float* gamma_q, const float* gamma_k,
@@ -540,16 +541,17 @@ dsmp_status dsmp_qk_rotate_backward(dsmp_handle* h, const dsmp_rotate_desc* desc
  *
  * Matrices as above: q, out [nq, heads * head_dim], k, v [nk, kv_heads * head_dim].
  * Coordinates: device float32 [rows, dim], slopes: device float32 [heads]; both
- * constants (no gradient), NULL when dim == 0; the squares of the differences have to
- * be finite in float32. */
+ * constants (no gradient), NULL when dim == 0; the squares of the coordinates and of
+ * their differences have to be finite in float32.  Scores z have to stay within 2^24,
+ * where float32 has no digit behind the point left.  Outputs overlap no other array. */
 typedef struct dsmp_attention_desc {
   int32_t heads;     /* 1..256 */
   int32_t kv_heads;  /* divides heads */
   int32_t head_dim;  /* a multiple of 8, at most 128; others give UNSUPPORTED */
   int32_t dtype;     /* of all matrices: DSMP_F32 or DSMP_BF16 */
   int32_t dim;       /* coordinates of the distance, 0..3; 0: none */
-  float scale;       /* finite */
-  float cap;         /* >= 0, finite; 0: none */
+  float scale;       /* 0, or of a magnitude within 2^-60 and 2^60 */
+  float cap;         /* 0: none, or within 2^-60 and 2^60, with DSMP_BF16 up to 1024; others give UNSUPPORTED */
 } dsmp_attention_desc;
 
 /* Segments: queries and keys have the same number of segments.  The bounds of

@@ -477,11 +477,13 @@ dsmp_status check_attention(dsmp_handle* h, const dsmp_attention_desc* d, const 
   DSMP_CHECK(h, d->dim >= 0 && d->dim <= 3, DSMP_INVALID_ARG, "0 to 3 coordinates");
   DSMP_CHECK(h, std::isfinite(d->scale), DSMP_INVALID_ARG, "the scale must be finite");
   DSMP_CHECK(h, std::isfinite(d->cap) && d->cap >= 0.0f, DSMP_INVALID_ARG, "the cap must be finite and not negative");
-  const float least = 0x1p-64f, most = 0x1p64f;   // slopes are divided by them
+  const float least = 0x1p-60f, most = 0x1p60f;   // slopes are divided by them, and one by the other: finite in float32
   DSMP_CHECK(h, d->scale == 0.0f || (std::fabs(d->scale) >= least && std::fabs(d->scale) <= most), DSMP_UNSUPPORTED,
-             "a scale must be 0 or within 2^-64 and 2^64");
+             "a scale must be 0 or within 2^-60 and 2^60");
   DSMP_CHECK(h, d->cap == 0.0f || (d->cap >= least && d->cap <= most), DSMP_UNSUPPORTED,
-             "a cap must be 0 or within 2^-64 and 2^64");
+             "a cap must be 0 or within 2^-60 and 2^60");
+  // tanh is within 2^-22 there (see Score): 2^-12 of a score at 2^10, an eighth of what rounds its weight
+  DSMP_CHECK(h, d->dtype == DSMP_F32 || d->cap <= 1024.0f, DSMP_UNSUPPORTED, "a cap over 1024 needs float32");
   const int G = d->heads / d->kv_heads;
   for (const dsmp_segments* s : {qs, ks}) {
     DSMP_CHECK(h, s->n >= 0 && s->n_seg >= 1, DSMP_INVALID_ARG, "negative rows or no segment");

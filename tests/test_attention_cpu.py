@@ -38,7 +38,8 @@ def test_attention_workspace(lib):
     (dict(head_dim=12), dm.UNSUPPORTED), (dict(head_dim=136), dm.UNSUPPORTED), (dict(head_dim=0), dm.INVALID_ARG),
     (dict(dtype=2), dm.INVALID_ARG), (dict(dim=4), dm.INVALID_ARG), (dict(dim=-1), dm.INVALID_ARG),
     (dict(scale=float("nan")), dm.INVALID_ARG), (dict(scale=1e-30), dm.UNSUPPORTED), (dict(scale=-1e30), dm.UNSUPPORTED),
-    (dict(cap=1e-30), dm.UNSUPPORTED), (dict(scale=0.0), dm.OK), (dict(scale=-0.1), dm.OK), (dict(cap=-1.0), dm.INVALID_ARG), (dict(cap=float("inf")), dm.INVALID_ARG)])
+    (dict(cap=1e-30), dm.UNSUPPORTED), (dict(cap=1025.0), dm.UNSUPPORTED), (dict(cap=1024.0), dm.OK), (dict(cap=1e6, dtype=dm.F32), dm.OK),
+    (dict(scale=2.0 ** 62, cap=2.0 ** -62), dm.UNSUPPORTED), (dict(scale=2.0 ** 60, cap=2.0 ** -60), dm.OK), (dict(scale=0.0), dm.OK), (dict(scale=-0.1), dm.OK), (dict(cap=-1.0), dm.INVALID_ARG), (dict(cap=float("inf")), dm.INVALID_ARG)])
 def test_attention_refuses_descriptors(lib, change, status):
     args = {**dict(heads=4, kv_heads=2, head_dim=64, dtype=dm.BF16, dim=2, scale=0.1, cap=0.0), **change}
     assert attention_ws(lib, dm.attention_desc(**args), (10, 1, None), (10, 1, None))[0] == status

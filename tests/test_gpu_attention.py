@@ -135,7 +135,7 @@ def test_heads(env, H, Hk, hd, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("hd", [32, 64, 128])
-@pytest.mark.parametrize("dim,cap", [(0, 5.0), (1, 0.0), (1, 2.0), (2, 3.0), (3, 0.0), (3, 20.0)])
+@pytest.mark.parametrize("dim,cap", [(0, 5.0), (0, 1024.0), (1, 0.0), (1, 2.0), (2, 3.0), (3, 0.0), (3, 20.0)])
 def test_scores(env, dim, cap, hd, dtype):
     announce(dtype, dim, cap, hd)
     Case(env, [0, 70], [0, 100], 4, 2, hd, dtype, dim=dim, cap=cap, scale=0.3).check()
@@ -384,3 +384,59 @@ def test_refusals(env):
     with pytest.raises(dm.DsmpError) as e:
         lib.dsmp_attention_backward(c.desc, c.q, c.k, c.v, out, lse, c.do, ws=torch.empty(8, dtype=torch.uint8, device="cuda"), **c.at)
     assert e.value.status == dm.WORKSPACE_TOO_SMALL
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_tiles_of_many_segments(env, dtype):
+    """More segments than are ordered by their length, in tiles of 128 rows."""
+    g = np.random.default_rng(8)
+    qb, kb = (np.concatenate([[0], np.cumsum(g.integers(90, 200, 70))]).tolist() for _ in range(2))
+    announce(dtype, qb[-1], kb[-1])
+    Case(env, qb, kb, 16, 16, 32, dtype, dim=3).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("H,Hk", [(256, 1), (255, 51)])
+def test_most_heads(env, H, Hk, dtype):
+    """More rows to a query than a tile has, and heads whose number is no power of two."""
+    announce(dtype, H, Hk)
+    Case(env, [0, 3, 10], [0, 90, 151], H, Hk, 16, dtype, dim=2).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("H,n", [(1, 200), (128, 200)])
+def test_wrong_bounds_leave_other_memory_alone(env, H, n, dtype):
+    """Bounds that descend, are negative or past the end: the kernels hold them to the arrays."""
+    dm, lib, torch = env
+    c = Case(env, [0, n], [0, n], H, H, 32, dtype, dim=2)
+    bounds = torch.tensor([-7, 60, 20, 99999, 2 ** 31 - 1, -(2 ** 31), 150], dtype=torch.int32, device="cuda")
+    at = {**c.at, "segments": bounds, "k_segments": bounds.flip(0).contiguous()}
+    announce(dtype, H)
+    outs = [torch.full((3 * n, 32 * H), 7.0, dtype=c.q.dtype, device="cuda") for _ in range(4)]
+    lse = torch.full((3 * n, H), 7.0, device="cuda")
+    mid = slice(n, 2 * n)
+    lib.dsmp_attention_forward(c.desc, c.q, c.k, c.v, out=outs[0][mid], lse=lse[mid], **at)
+    lib.dsmp_attention_backward(c.desc, c.q, c.k, c.v, outs[0][mid], lse[mid], c.do, grad_q=outs[1][mid], grad_k=outs[2][mid],
+                                grad_v=outs[3][mid], **at)
+    torch.cuda.synchronize()
+    for t in (*outs, lse):
+        assert (t[:n] == 7).all() and (t[2 * n:] == 7).all()
+
+
+def test_captured_call_takes_the_bounds_of_its_replay(env):
+    dm, lib, torch = env
+    a, b = (Case(env, [0, x, 90], [0, y, 150], 2, 1, 32, "bf16", dim=2, seed=4) for x, y in ((30, 100), (71, 9)))
+    a.backward(*a.forward())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        out, lse = lib.dsmp_attention_forward(a.desc, a.q, a.k, a.v, **a.at)
+        grads = lib.dsmp_attention_backward(a.desc, a.q, a.k, a.v, out, lse, a.do, **a.at)
+    for name in ("segments", "k_segments"):
+        a.at[name].copy_(b.at[name])
+    for _ in range(3):
+        graph.replay()
+        o, l = a.forward()
+        want = [o, l, *a.backward(o, l)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip((out, lse, *grads), want))
