@@ -537,7 +537,8 @@ dsmp_status dsmp_qk_rotate_backward(dsmp_handle* h, const dsmp_rotate_desc* desc
  *     P = softmax of z over the keys of s,  out_i = sum_j P v_j,  lse_i = log sum_j e^z
  * A query whose segment has no keys gets out 0 and lse -infinity.  Scores, sums and
  * the softmax are float32; with DSMP_BF16 the operands of the products are bfloat16
- * (P and the scores' gradients are rounded to it), accumulated in float32.
+ * (P and the scores' gradients are rounded to it, or to sums of two such values in
+ * small calls), accumulated in float32.
  *
  * Matrices as above: q, out [nq, heads * head_dim], k, v [nk, kv_heads * head_dim].
  * Coordinates: device float32 [rows, dim], slopes: device float32 [heads]; both

@@ -178,7 +178,7 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, const BwdLds& lds, un
           if (8 * (i >> 2) + (i & 3) >= left) x[i] = 0.0f;
       }
       __builtin_amdgcn_sched_barrier(0);
-      frag cf[2], f{};
+      frag cf[2], f{}, rest[2]{};
       cf[0] = tile_columns<T, D>(ldsK, lane, at, 0);
 #pragma unroll
       for (int k = 0; k < 2 * DB; ++k) {
@@ -188,12 +188,21 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, const BwdLds& lds, un
 #pragma unroll
           for (int i = 0; i < 8; ++i) v[i] = x[8 * t2 + i];
           f = to_frag<T>(v);
+          if constexpr (FEW && C::DMA) rest[t2] = rest_frag(v, f);
         }
         if (k + 1 < 2 * DB) cf[(k + 1) & 1] = tile_columns<T, D>(ldsK, lane, at + 16 * ((k + 1) / DB), 32 * ((k + 1) % DB));
         acc[d] = mma(cf[k & 1], f, acc[d]);
         if (d & 1 || DB == 1) __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_sched_barrier(0);
+      if constexpr (FEW && C::DMA)
+        if (a.fine) {
+#pragma unroll
+          for (int k = 0; k < 2 * DB; ++k) {
+            acc[k % DB] = mma(tile_columns<T, D>(ldsK, lane, at + 16 * (k / DB), 32 * (k % DB)), rest[k / DB], acc[k % DB]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
     }
 #pragma unroll
     for (int d = 0; d < DB; ++d) asm volatile("" : "+v"(acc[d]));   // one place for the sums after either buffer's tile
@@ -383,7 +392,7 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
       }
       __builtin_amdgcn_sched_barrier(0);
       // the products for dv and dk in turn, fragments one ahead (none in float32, whose are large and products long)
-      frag cf[2], pf{}, sf{};
+      frag cf[2], pf{}, sf{}, rest[4]{};
       auto columns = [&](int n) {
         return tile_columns<T, D>(n & 1 ? ldsQ : ldsG, lane, at + 16 * (n / 2 / DB), 32 * (n / 2 % DB));
       };
@@ -396,6 +405,7 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
 #pragma unroll
           for (int i = 0; i < 8; ++i) p[i] = x[8 * t2 + i], ds[i] = dp[8 * t2 + i];
           pf = to_frag<T>(p), sf = to_frag<T>(ds);
+          if constexpr (FEW && C::DMA) rest[2 * t2] = rest_frag(p, pf), rest[2 * t2 + 1] = rest_frag(ds, sf);
         }
         if (ES == 4 && n > 0) cf[n & 1] = columns(n);
         if (ES != 4 && n + 1 < 4 * DB) cf[(n + 1) & 1] = columns(n + 1);
@@ -403,6 +413,17 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
         else dv[d] = mma(cf[n & 1], pf, dv[d]);
         if (n & 1) __builtin_amdgcn_sched_barrier(0);
       }
+      if constexpr (FEW && C::DMA)
+        if (a.fine) {
+#pragma unroll
+          for (int n = 0; n < 4 * DB; ++n) {
+            const int d = n / 2 % DB;
+            const frag f = columns(n);
+            if (n & 1) dk[d] = mma(f, rest[2 * (n / 2 / DB) + 1], dk[d]);
+            else dv[d] = mma(f, rest[2 * (n / 2 / DB)], dv[d]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
     }
 #pragma unroll
     for (int d = 0; d < DB; ++d)

@@ -171,6 +171,12 @@ __global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::template WAVES<M>)) void k_att
         if (k + 1 < 2 * C::SUB) vf[(k + 1) & 1][d] = tile_columns<T, D>(ldsV, lane, 32 * sub0 + 16 * (k + 1), 32 * d);
 #pragma unroll
       for (int d = 0; d < DB; ++d) o[d] = mma(vf[k & 1][d], pf, o[d]);
+      if constexpr (FEW && C::DMA)
+        if (a.fine) {
+          const frag rest = rest_frag(p, pf);
+#pragma unroll
+          for (int d = 0; d < DB; ++d) o[d] = mma(vf[k & 1][d], rest, o[d]);
+        }
       __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll

@@ -440,3 +440,28 @@ def test_captured_call_takes_the_bounds_of_its_replay(env):
         want = [o, l, *a.backward(o, l)]
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip((out, lse, *grads), want))
+
+
+@pytest.mark.parametrize("nq,nk", [(50, 90), (3, 2000)])
+def test_weights_of_small_calls_keep_sixteen_bits(env, nq, nk):
+    """bfloat16: P is a sum of two values, within 2^-16 of it (what is left after the first rounding, 2^-8, is rounded
+    to 2^-8 of that).  A score is exact products added in float32, 34 roundings of 2^-24 of sum |q k| scale < 16: below
+    2^-14.9 of P; power, sum and logarithm stay below 2^-20.  So out and dv are within 2^-14 sum P |v| and half a step of
+    their own, 2^-8."""
+    c = Case(env, [0, nq], [0, nk], 4, 2, 32, "bf16")
+    announce(nq, nk)
+    out, lse = c.forward()
+    _, _, dv = c.backward(out, lse)
+    q, k, v, do = (c.heads(t, h) for t, h in ((c.q, 4), (c.k, 2), (c.v, 2), (c.do, 4)))
+    want_dv, room = np.zeros_like(v), np.zeros_like(v)
+    for a in range(4):
+        z = c.scale * q[:, a] @ k[:, a // 2].T
+        assert (c.scale * np.abs(q[:, a]) @ np.abs(k[:, a // 2]).T).max() < 16
+        P = np.exp(z - z.max(1, keepdims=True))
+        P /= P.sum(1, keepdims=True)
+        o = P @ v[:, a // 2]
+        near = 2.0 ** -14 * (P @ np.abs(v[:, a // 2]))
+        assert (np.abs(c.heads(out, 4)[:, a] - o) <= 2.0 ** -8 * (np.abs(o) + near) + near).all()
+        want_dv[:, a // 2] += P.T @ do[:, a]
+        room[:, a // 2] += 2.0 ** -14 * (P.T @ np.abs(do[:, a]))
+    assert (np.abs(c.heads(dv, 2) - want_dv) <= 2.0 ** -8 * (np.abs(want_dv) + room) + room).all()
