@@ -412,28 +412,31 @@ __device__ __forceinline__ float tanh_of(float x) {
 
 // A score is formed as u with z log2(e) = A u + C, so that e^(z - b) is one fma and one power:
 //   no cap              u = x - (slope / scale) d,      A = scale log2(e),    C = 0
-//   cap, bfloat16       u = -r - (slope / 2 cap) d,     A = 2 cap log2(e),    C = cap log2(e)
-//   cap, float32        u = tanh - (slope / cap) d,     A = cap log2(e),      C = 0
-// x = q.k, d the distance, r = 1 / (1 + e^(2 scale x / cap)): tanh = 1 - 2 r, whose absolute error of about
-// 2^-23 bfloat16 operands hide, and 1 - tanh^2 = 4 r (1 - r).  A is positive: a negative scale goes into
-// the sign of one operand of x, and a scale of 0 makes that operand 0 (`sign`).
-template <typename T>
+//   cap                 u = -r - (slope / 2 cap) d,     A = 2 cap log2(e),    C = cap log2(e)
+//   cap, to its digits  u = tanh - (slope / cap) d,     A = cap log2(e),      C = 0     (float32, and the forward's fine FEW tiles)
+// x = q.k, d the distance, r = 1 / (1 + e^(2 scale x / cap)): tanh = 1 - 2 r, whose absolute error of about 2^-23
+// bfloat16 operands hide, but not in the lse of few keys, which may be near zero; and 1 - tanh^2 = 4 r (1 - r).
+// A is positive: a negative scale goes into the sign of one operand of x, and a scale of 0 makes that operand 0 (`sign`).
+template <typename T, bool FEW>
 struct Score {
   float A, C, turn, per_slope, sign;
+  static constexpr bool EITHER = sizeof(T) == 2 && FEW;
+  std::conditional_t<EITHER, int, std::integral_constant<int, sizeof(T) == 4>> digits;
   __device__ __forceinline__ Score(const AttnArgs& a, bool cap) {
+    if constexpr (EITHER) digits = a.fine;
     sign = a.scale > 0.0f ? 1.0f : a.scale < 0.0f ? -1.0f : 0.0f;
     const float scale = a.scale == 0.0f ? 1.0f : fabsf(a.scale);
-    const float unit = !cap ? scale : sizeof(T) == 4 ? a.cap : 2.0f * a.cap;
+    const float unit = !cap ? scale : digits ? a.cap : 2.0f * a.cap;
     A = unit * LOG2E;
     per_slope = 1.0f / unit;
-    C = cap && sizeof(T) == 2 ? a.cap * LOG2E : 0.0f;
-    turn = !cap ? 0.0f : sizeof(T) == 4 ? scale / a.cap : 2.0f * LOG2E * scale / a.cap;
+    C = cap && !digits ? a.cap * LOG2E : 0.0f;
+    turn = !cap ? 0.0f : digits ? scale / a.cap : 2.0f * LOG2E * scale / a.cap;
   }
   // u without its bias; `fall` receives 1 - tanh^2
   template <bool SLOPE>
   __device__ __forceinline__ float u(float x, bool cap, float* fall) const {
     if (!cap) return x;
-    if (sizeof(T) == 4) {
+    if (digits) {
       const float t = tanh_of(x * turn);
       if (SLOPE) *fall = 1.0f - t * t;
       return t;
@@ -467,7 +470,7 @@ inline AttnArgs attn_args(const dsmp_attention_desc& d, const dsmp_segments& qs,
   // Rounded weights put the results, which are rounded too, 1.4 times as far off as float32 products would, and
   // up to 1.6 times with few keys, whose roundings do not average out; as sums of two values no further than those
   // (0.0017 for 0.0023 to 0.0026).  Forward and backward of 300 x 300, 4 heads of 32: 25.9 us without, 26.0 with them;
-  // 500 x 500, 8 heads of 128: 52.8 and 56.3; 2,048 x 2,048, 4 heads of 64, which take them no more: 82 and 92.
+  // 500 x 500, 8 heads of 128: 52.8 and 56.3; 2,048 x 2,048, 8 heads of 64, which take them no more: 83 and 93.
   a.fine = ks.n <= 512 * ks.n_seg || (double)qs.n * ks.n <= 0x1p18 * qs.n_seg * ks.n_seg;   // 512 keys, or 2^18 scores to a segment
   return a;
 }

@@ -6,7 +6,10 @@
 //
 // Neither has atomics: a workgroup owns its rows or its keys and keeps their sums in registers.
 // P and dS are so formed in both (two products of seven), which sums over workgroups in a
-// fixed order would cost in memory instead.  The gradients of shared key heads add up in the
+// fixed order would cost in memory instead.  D comes from the rounded out in bfloat16, an error of up to
+// 2^-8 |dO| |out| that all keys of a row share: with many keys it is lost in their own
+// roundings, with few it is the largest (4 to 12 keys: dq 0.0026 to 0.0032 off).  Where a segment's keys are in one block of 32
+// FEW tiles take D from the weights instead, D = sum_j P_ij dP_ij (dq and dk 0.0017 off).  The gradients of shared key heads add up in the
 // accumulators: the rows of a key head are the queries times the G heads that share it.
 #pragma once
 
@@ -77,6 +80,13 @@ __device__ __forceinline__ void join_rows(const f32x16* acc, const BwdLds& lds, 
   }
 }
 
+// Of a wave's 32 lanes.
+__device__ __forceinline__ float sum_of_half(float v) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
 template <typename T, int D, bool FEW, typename M>
 __device__ __forceinline__ void dq_tile(const AttnArgs& a, const BwdLds& lds, unsigned group) {
   using C = Bwd<T, D, FEW, false>;
@@ -100,7 +110,7 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, const BwdLds& lds, un
 
   const bool cap = M::cap(a);
   const int dim = M::dim(a);
-  const Score<T> sc(a, cap);
+  const Score<T, false> sc(a, cap);
   const RowOf row = row_of(a, q0, r0, R, kvh, FEW, tid);
   const int64_t slot = row.query * a.H + row.head;
   frag qf[KS], gf[KS];
@@ -151,6 +161,9 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, const BwdLds& lds, un
         dp = mma(vf[t2 & 1], gf[t2], dp);
         __builtin_amdgcn_sched_barrier(0);
       }
+      int left = rem - at - 4 * h;
+      asm volatile("" : "+v"(left));   // compared with constants, not with sixteen row numbers kept over the loop
+      float more = 0.0f;   // sum of P (dP - D) over the keys: what D lacks, where all of them are here
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) {
         float4 px{}, py{}, pz{};
@@ -165,14 +178,23 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, const BwdLds& lds, un
           float fall;
           float u = sc.template u<true>(x[i], cap, &fall);
           if (dim) u = fmaf(-slope, distance(dim, me, (&px.x)[e], (&py.x)[e], (&pz.x)[e]), u);
-          x[i] = exp2_of(fmaf(u, sc.A, shift)) * dp[i];
+          const float p = exp2_of(fmaf(u, sc.A, shift));
+          if constexpr (FEW && C::DMA) {
+            x[i] = 8 * i4 + e < left ? p : 0.0f;
+            more = fmaf(x[i], dp[i], more);
+          } else {
+            x[i] = p * dp[i];
+          }
           if (cap) x[i] *= fall;
         }
         if (dim) __builtin_amdgcn_sched_barrier(0);
       }
-      if (at + 32 > rem) {   // behind the last key
-        int left = rem - at - 4 * h;
-        asm volatile("" : "+v"(left));   // compared with constants, not with sixteen row numbers kept over the loop
+      if constexpr (FEW && C::DMA) {
+        more = klen <= 32 ? more + other_half(more) : 0.0f;
+        if (klen <= 32 && row.there && h == 0) a.minus_d[slot] = -delta - more;   // for a launch for keys in wide tiles
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] *= dp[i] - more;
+      } else if (at + 32 > rem) {   // behind the last key
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (8 * (i >> 2) + (i & 3) >= left) x[i] = 0.0f;
@@ -314,7 +336,7 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
 
   const bool cap = M::cap(a);
   const int dim = M::dim(a);
-  const Score<T> sc(a, cap);
+  const Score<T, false> sc(a, cap);
   frag kf[KS], vf[KS];
   Place me{0.0f, 0.0f, 0.0f};
   {
@@ -385,6 +407,8 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const BwdLds& lds, u
           float u = sc.template u<true>(x[i], cap, &fall);
           if (dim) u = fmaf(-(&sl.x)[e], (&far.x)[e], u);
           x[i] = exp2_of(fmaf(u, sc.A, (&shift.x)[e]));
+          if constexpr (FEW && C::DMA)
+            if (klen <= 32) dp[i] -= sum_of_half((l & 31) < klen ? x[i] * dp[i] : 0.0f);
           dp[i] *= x[i];
           if (cap) dp[i] *= fall;
         }

@@ -67,7 +67,7 @@ __global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::template WAVES<M>)) void k_att
   // this lane's row
   const bool cap = M::cap(a);
   const int dim = M::dim(a);
-  const Score<T> sc(a, cap);
+  const Score<T, FEW> sc(a, cap);
   const RowOf row = row_of(a, q0, r0, R, kvh, FEW, tid);
   const bool there = row.there;
   const int64_t query = row.query;
