@@ -485,7 +485,9 @@ dsmp_status dsmp_group_norm_backward(dsmp_handle* h, const dsmp_norm_desc* desc,
  * for the pairs p < rot / 2; DSMP_ROTATE_HALF: (a, b) = (p, p + rot / 2),
  * DSMP_ROTATE_INTERLEAVED: (a, b) = (2 p, 2 p + 1).  The values from rot on are u.
  * The angle is formed and brought into one turn in float64, so far positions keep
- * their digits; norms and products are float32.
+ * their digits; norms and products are float32: mean x^2 + eps of a head has to be a normal
+ * float32 value (with eps = 0 a head of zeros has no norm, and its results and the gammas'
+ * gradients are NaN).
  *
  * Matrices: device [n, heads * head_dim] of dtype, rows ld elements apart
  * (heads * head_dim <= ld <= 2^16), 16-byte aligned, as every one of their rows:

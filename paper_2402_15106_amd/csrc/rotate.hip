@@ -276,7 +276,9 @@ __global__ __launch_bounds__(RT) void k_rotate_bwd(RotArgs a) {
           float q = 0.0f, m = 0.0f;
 #pragma unroll
           for (int i = 0; i < N; ++i) q = fmaf(x[i], x[i], q);
-          const float r = __builtin_amdgcn_rsqf(fmaf(sum_lanes(q, a.lg), mean, a.eps));
+          q = sum_lanes(q, a.lg);
+          // a slot without a head has nothing to add to the sums: without eps its zeros would have an infinite 1 / rms
+          const float r = on && hh < c1 ? __builtin_amdgcn_rsqf(fmaf(q, mean, a.eps)) : 0.0f;
 #pragma unroll
           for (int i = 0; i < N; ++i) {
             x[i] *= r;
