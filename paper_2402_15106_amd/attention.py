@@ -7,7 +7,9 @@ order and buffers only; the projections are plain matrix products of torch).
 
 Message passing reaches the neighbours within the radius; here every node of a sub-graph
 sees every other one.  u is what a norm hands to a layer (dsmp_group_norm_forward), f is
-float32, the addend of the next norm, as a message-passing layer's output is.
+float32, the addend of the next norm, as a message-passing layer's output is; f, the
+gradient of u and those of the weights are float32 sums in either type, while q, k, v and
+what grad_f hands back to them are operands of the next products and have the layer's type.
 """
 
 from dataclasses import dataclass
@@ -32,6 +34,11 @@ class AttentionShapes:
     cap: float = 0.0
     distance: bool = True  # whether scores fall with the distance
     eps: float = 1e-6
+
+
+def _sums(a, b):
+    """a @ b as float32 sums, whatever the operands' type (rounded to bfloat16 and back they would keep 8 bits)."""
+    return torch.mm(a, b) if a.dtype == torch.float32 else torch.mm(a, b, out_dtype=torch.float32)
 
 
 class AttentionLayer:
@@ -76,7 +83,7 @@ class AttentionLayer:
         q, k, v = qkv[:, :wq], qkv[:, wq:wq + wk], qkv[:, wq + wk:]
         qr, kr = lib.dsmp_qk_rotate_forward(self.rotate, q, k, p.get("gamma_q"), p.get("gamma_k"), pos, p.get("freq"))
         place, (out, lse) = self._attention(p, qr, kr, v, pos, None, segments, None)
-        f = torch.mm(out, p["Wo"].t()).float()
+        f = _sums(out, p["Wo"].t())
         self._kept = (p, u, pos, segments, place, qkv, qr, kr, out, lse)
         return f
 
@@ -94,8 +101,8 @@ class AttentionLayer:
                                     grad_q=dq, grad_k=dk, grad_v=dv, **place)
         _, _, grads = lib.dsmp_qk_rotate_backward(self.rotate, q, k, p.get("gamma_q"), p.get("gamma_k"), pos, p.get("freq"),
                                                   dq, dk, grad_q=dq, grad_k=dk)
-        grads["dWqkv"], grads["dWo"] = torch.mm(dqkv.t(), u).float(), torch.mm(g.t(), out).float()
-        return torch.mm(dqkv, p["Wqkv"]).float(), grads
+        grads["dWqkv"], grads["dWo"] = _sums(dqkv.t(), u), _sums(g.t(), out)
+        return _sums(dqkv, p["Wqkv"]), grads
 
     def read(self, params: dict, u, pos, u_keys, pos_keys, segments=None, k_segments=None) -> torch.Tensor:
         """f [m, d] (float32) at m points with features u and coordinates pos, from the nodes u_keys,
@@ -107,4 +114,4 @@ class AttentionLayer:
         k = kv[:, :wk]
         lib.dsmp_qk_rotate_forward(self.rotate, None, k, None, p.get("gamma_k"), pos_keys, p.get("freq"), k_out=k)
         _, (out, _) = self._attention(p, q, k, kv[:, wk:], pos, pos_keys, segments, k_segments)
-        return torch.mm(out, p["Wo"].t()).float()
+        return _sums(out, p["Wo"].t())
