@@ -56,17 +56,31 @@ class AttentionLayer:
                                     norm=s.norm, eps=s.eps)
         self.attend = L.attention_desc(s.heads, s.kv_heads, s.head_dim, s.dtype, dim=s.dim if s.distance else 0, cap=s.cap)
         self.wq, self.wk = s.heads * s.head_dim, s.kv_heads * s.head_dim
+        self._rows = torch.arange(s.n, dtype=torch.int32, device=lib.device)[:, None]
         self._kept = None
 
-    def _project(self, u, W, what):
+    def _checked(self, u, what):
         if u.dim() != 2 or u.shape[1] != self.s.d or u.dtype is not L._TORCH.get(self.s.dtype):
             raise L.DsmpError(L.INVALID_ARG, "%s: a %s matrix of %d columns is needed" % (what, L._TORCH.get(self.s.dtype), self.s.d))
-        return torch.mm(u, W.t())
+        return u
 
     @staticmethod
     def _buffer(like, segments):
         """Rows of no segment stay as they are: zero."""
         return torch.zeros_like(like) if isinstance(segments, torch.Tensor) else torch.empty_like(like)
+
+    def _room(self, segments):
+        """Which rows belong to no segment, [n, 1], by the bounds on the device (None: there are none)."""
+        self.lib._segments(self.s.n, segments)   # refused here, or they are bounds on the device
+        if not isinstance(segments, torch.Tensor):
+            return None
+        below = self._rows < segments[::segments.numel() - 1]   # the first bound and the last one
+        return below[:, :1] == below[:, 1:]
+
+    @staticmethod
+    def _cleared(t, room):
+        """t without what it holds in those rows (what is no matrix is refused by the calls that take it)."""
+        return t if room is None or t is None or t.dim() != 2 else torch.where(room, 0.0, t)
 
     def _attention(self, p, q, k, v, pos, k_pos, segments, k_segments):
         place = dict(pos=pos, k_pos=k_pos, slopes=p["slopes"]) if self.s.distance else {}
@@ -74,17 +88,23 @@ class AttentionLayer:
                                                       out=self._buffer(q, segments), **place)
 
     def forward(self, params: dict, u: torch.Tensor, pos: torch.Tensor, segments=None) -> torch.Tensor:
-        """f [n, d] (float32) of u [n, d] at pos (float32 [n, dim]); segments as for the norms."""
+        """f [n, d] (float32) of u [n, d] at pos (float32 [n, dim]); segments as for dsmp_attention_forward: whatever
+        u, pos and later grad_f hold in rows in front of the first bound and behind the last one (room
+        for further sub-graphs), f and the gradient of u are 0 there, and the other gradients know nothing of them."""
         lib, p, wq, wk = self.lib, params, self.wq, self.wk
         self._kept = None
-        if u.shape[0] != self.s.n:
+        if self._checked(u, "u").shape[0] != self.s.n:
             raise L.DsmpError(L.INVALID_ARG, "u: %d rows are needed" % self.s.n)
-        qkv = self._project(u, p["Wqkv"], "u")
+        room = self._room(segments)
+        u, pos = self._cleared(u, room), self._cleared(pos, room)
+        qkv = torch.mm(u, p["Wqkv"].t())
+        if room is not None and self.s.norm and self.s.eps == 0.0:
+            qkv.masked_fill_(room, 1.0)   # rows of zeros have no norm without eps; their gradients are 0 times what there is
         q, k, v = qkv[:, :wq], qkv[:, wq:wq + wk], qkv[:, wq + wk:]
         qr, kr = lib.dsmp_qk_rotate_forward(self.rotate, q, k, p.get("gamma_q"), p.get("gamma_k"), pos, p.get("freq"))
         place, (out, lse) = self._attention(p, qr, kr, v, pos, None, segments, None)
         f = _sums(out, p["Wo"].t())
-        self._kept = (p, u, pos, segments, place, qkv, qr, kr, out, lse)
+        self._kept = (p, u, pos, segments, room, place, qkv, qr, kr, out, lse)
         return f
 
     def backward(self, grad_f: torch.Tensor):
@@ -92,9 +112,11 @@ class AttentionLayer:
         if self._kept is None:
             raise L.DsmpError(L.INVALID_ARG, "no forward call that came to its end")
         lib, wq, wk = self.lib, self.wq, self.wk
-        p, u, pos, segments, place, qkv, qr, kr, out, lse = self._kept
+        p, u, pos, segments, room, place, qkv, qr, kr, out, lse = self._kept
         q, k, v = qkv[:, :wq], qkv[:, wq:wq + wk], qkv[:, wq + wk:]
-        g = grad_f.to(u.dtype)
+        if grad_f.shape != (self.s.n, self.s.d):
+            raise L.DsmpError(L.INVALID_ARG, "grad_f: a matrix of %d rows and %d columns is needed" % (self.s.n, self.s.d))
+        g = self._cleared(grad_f.to(u.dtype), room)
         dqkv = self._buffer(qkv, segments)
         dq, dk, dv = dqkv[:, :wq], dqkv[:, wq:wq + wk], dqkv[:, wq + wk:]
         lib.dsmp_attention_backward(self.attend, qr, kr, v, out, lse, torch.mm(g, p["Wo"]), segments=segments,
@@ -108,8 +130,8 @@ class AttentionLayer:
         """f [m, d] (float32) at m points with features u and coordinates pos, from the nodes u_keys,
         pos_keys of the same segments.  Nothing is kept."""
         lib, p, wq, wk = self.lib, params, self.wq, self.wk
-        q = self._project(u, p["Wqkv"][:wq], "u")
-        kv = self._project(u_keys, p["Wqkv"][wq:], "u_keys")
+        q = torch.mm(self._checked(u, "u"), p["Wqkv"][:wq].t())
+        kv = torch.mm(self._checked(u_keys, "u_keys"), p["Wqkv"][wq:].t())
         lib.dsmp_qk_rotate_forward(self.rotate, q, None, p.get("gamma_q"), None, pos, p.get("freq"), q_out=q)
         k = kv[:, :wk]
         lib.dsmp_qk_rotate_forward(self.rotate, None, k, None, p.get("gamma_k"), pos_keys, p.get("freq"), k_out=k)

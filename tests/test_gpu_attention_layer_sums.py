@@ -21,6 +21,8 @@ class Watched:
 
     def __getattr__(self, name):
         call = getattr(self.lib, name)
+        if not name.startswith("dsmp_"):
+            return call
 
         def watched(*args, **kw):
             got = call(*args, **kw)
