@@ -3,6 +3,7 @@
 // score of a query and a key.
 #pragma once
 
+#include "attn_plan.hpp"
 #include "nnconv.hpp"
 
 #include <cmath>
@@ -310,8 +311,6 @@ __device__ __forceinline__ int find_segment_longest_first(const Bounds& b, const
   return seg;
 }
 
-inline int64_t tiles_of(int64_t n, int64_t n_seg, int M, int size) { return n * M / size + n_seg; }
-
 // ------------------------------------------------------------------ arguments
 struct AttnArgs {
   const void *q, *k, *v, *go, *o;
@@ -489,85 +488,6 @@ void by_attention(const dsmp_attention_desc& d, F f) {
   else if (d.cap != 0.0f) width(__bf16{}, Mode<1, 3>{});
   else if (d.dim <= 2) width(__bf16{}, Mode<0, 2>{});
   else width(__bf16{}, Mode<0, 3>{});
-}
-
-constexpr int64_t MAX_GROUPS = ((int64_t)1 << 24) - 1;   // a launch has fewer than 2^32 threads
-
-// ------------------------------------------------- which tiles, and how far they are cut
-// A call takes tiles of 128 rows (WIDE) or of 32 (FEW), whichever its estimated time is shorter for, and
-// either may be cut over the other side into parts that are added up afterwards.
-//
-// CU microseconds of a tile where the CUs are full, as measured (8,192 scores of a WIDE bfloat16 tile, 4,096 of the
-// others; heads of up to 32, 64 and 128).  FEW tiles have four times the copies to LDS for a score, which
-// bounds the keys' gradients: 16,384 x 8 heads of 64, two of keys, backward 3,346 us with FEW for the keys, 1,785 with
-// WIDE, cut.  A distance and a cap are float32 work for each score.
-enum Pass { FORWARD, GRAD_Q, GRAD_K };
-inline int width_of(const dsmp_attention_desc& d) { return d.head_dim <= 32 ? 0 : d.head_dim <= 64 ? 1 : 2; }
-inline double tile_us(const dsmp_attention_desc& d, Pass pass, bool wide) {
-  static const double bf16[3][2][3] = {{{0.40, 0.58, 1.04}, {0.25, 0.36, 0.80}},
-                                       {{0.50, 0.74, 1.40}, {0.33, 0.48, 1.20}},
-                                       {{0.75, 1.04, 2.10}, {0.80, 1.26, 3.60}}};
-  static const double f32[3][3] = {{1.9, 2.6, 9.0}, {2.8, 6.0, 14.0}, {3.7, 8.0, 18.0}};
-  const int w = width_of(d);
-  if (d.dtype == DSMP_F32) return f32[pass][w] + (d.dim ? 0.5 : 0.0) + (d.cap != 0.0f ? 0.5 : 0.0);
-  const double more = (d.dim ? 0.50 : 0.0) + (d.cap != 0.0f ? 0.25 : 0.0);
-  return bf16[pass][wide ? 0 : 1][w] + (wide ? more : 0.5 * more);
-}
-// workgroups that a CU's registers and LDS hold
-inline int held(const dsmp_attention_desc& d, Pass pass, bool wide) {
-  const int w = width_of(d);
-  if (d.dtype == DSMP_F32) return w == 0 || (w == 1 && pass == FORWARD) ? 2 : 1;
-  if (w == 2) return wide && pass != GRAD_K ? 2 : 1;
-  return wide ? (w == 1 && pass == GRAD_K ? 2 : 3) : w == 1 ? 2 : 3;
-}
-
-// One or two kinds of workgroups in a launch, `groups` with `steps` tiles of `us` to go over, and the bytes
-// of the parts of one split.  They are cut so that a workgroup has about the same amount of work,
-// as far as the shortest estimated time asks: the work dealt to 256 CUs, which are full with `held`
-// workgroups each, START for each workgroup, `end` of the longest workgroup for the uneven end (more with
-// segments, whose lengths differ), and the launch that adds up the parts (5 us, and their bytes written and read at
-// 4 TB/s).
-struct Cut {
-  int64_t groups, steps;
-  double us, bytes;
-  int splits;
-};
-inline double cut_evenly(Cut* c, int n, int held, int most, double end) {
-  constexpr double CUS = 256, START = 1.2;
-  double total = 0, best = 0;
-  for (int i = 0; i < n; ++i) total += c[i].groups * c[i].steps * c[i].us;
-  int now[2] = {1, 1};
-  static const int targets[] = {0, 1, 2, 3, 4, 6, 8};   // workgroups to a CU; 0: uncut
-  for (const int k : targets) {
-    double sum = 0, longest = 0, join = 0;
-    int64_t groups = 0;
-    for (int i = 0; i < n; ++i) {
-      const int64_t per = k ? std::max<int64_t>(1, (int64_t)std::ceil(total / (k * CUS * c[i].us))) : std::max<int64_t>(1, c[i].steps);
-      now[i] = (int)std::min<int64_t>(most, std::max<int64_t>(1, (c[i].steps + per - 1) / per));
-      const double time = c[i].groups ? (double)((c[i].steps + now[i] - 1) / now[i]) * c[i].us : 0.0;
-      sum += c[i].groups * now[i] * time;
-      longest = std::max(longest, time);
-      groups += c[i].groups * now[i];
-      if (now[i] > 1) join += 2 * now[i] * c[i].bytes / 4e6;
-    }
-    if (now[0] > 1 || (n > 1 && now[1] > 1)) join += 5.0;
-    // what a CU does of its full rate with one workgroup, and with as many as there are for each
-    const double each = groups / CUS, alone = held == 1 ? 1.0 : held == 2 ? 0.65 : 0.55;
-    const double part = each >= held || held == 1 ? 1.0 : each <= 1 ? alone : alone + (1.0 - alone) * (each - 1) / (held - 1);
-    const double time = (each <= 1 ? longest / part : sum / (CUS * part) + end * longest) + START * each + join;
-    if (k == 0 || time < 0.98 * best) {
-      best = time;
-      for (int i = 0; i < n; ++i) c[i].splits = now[i];
-    }
-  }
-  return best;
-}
-inline double uneven_end(const dsmp_segments& s) { return s.n_seg == 1 ? 0.3 : 1.0; }
-
-// tiles of `size` rows that there are, for an estimate (a launch has tiles_of)
-inline int64_t about_tiles(int64_t n, int64_t n_seg, int M, int size) {
-  if (n * M <= n_seg * size) return std::min(n * M, n_seg);
-  return (n * M + size - 1) / size + (n_seg > 1 ? n_seg / 2 : 0);
 }
 
 size_t attention_bwd_bytes(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks);

@@ -42,46 +42,6 @@ __global__ __launch_bounds__(BT) void k_attn_bwd_join(AttnArgs a) {
   store4(out + (4 * i - row * width), v.x, v.y, v.z, v.w);
 }
 
-struct BwdPlan {
-  bool wide_q, wide_k;
-  int splits_q, splits_k;
-  int64_t grid_q, grid_k;
-};
-
-// The gradients of the queries and of the keys each WIDE or FEW, cut each for itself; or both FEW, in one launch.
-BwdPlan bwd_plan(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks) {
-  const int G = d.heads / d.kv_heads, per_wide = d.dtype == DSMP_F32 ? 32 : 64;
-  const int64_t keys = ks.n / ks.n_seg, rows = qs.n / qs.n_seg * G;
-  const double bq = 4.0 * qs.n * d.heads * d.head_dim, bk = 8.0 * ks.n * d.kv_heads * d.head_dim;
-  Cut q[2], k[2], both[2];
-  double tq[2], tk[2];
-  for (int wide = 0; wide < 2; ++wide) {
-    const int own = wide ? 32 * BW : 32, along = wide ? per_wide : 128;
-    q[wide] = {qs.n ? about_tiles(qs.n, qs.n_seg, G, own) * d.kv_heads : 0, (keys + along - 1) / along, tile_us(d, GRAD_Q, wide), bq, 1};
-    k[wide] = {ks.n ? about_tiles(ks.n, ks.n_seg, 1, own) * d.kv_heads : 0, (rows + along - 1) / along, tile_us(d, GRAD_K, wide), bk, 1};
-  }
-  both[0] = q[0], both[1] = k[0];
-  const double together = cut_evenly(both, 2, held(d, GRAD_K, false), 64, uneven_end(ks));
-  for (int wide = 0; wide < 2; ++wide) {
-    tq[wide] = cut_evenly(&q[wide], 1, held(d, GRAD_Q, wide), 64, uneven_end(ks));
-    tk[wide] = cut_evenly(&k[wide], 1, held(d, GRAD_K, wide), 64, uneven_end(ks));
-  }
-  // few keys to a segment: FEW tiles of queries take D from the weights
-  if (d.dtype == DSMP_BF16 && ks.n <= 32 * ks.n_seg) tq[1] = 2 * tq[0] + tq[1];
-  BwdPlan p{};
-  p.wide_q = tq[1] < tq[0], p.wide_k = tk[1] < tk[0];
-  p.splits_q = q[p.wide_q].splits, p.splits_k = k[p.wide_k].splits;
-  if (together < std::min(tq[0], tq[1]) + std::min(tk[0], tk[1]) + 3.0) {
-    p.wide_q = p.wide_k = false;
-    p.splits_q = both[0].splits, p.splits_k = both[1].splits;
-  }
-  p.grid_q = qs.n ? tiles_of(qs.n, qs.n_seg, G, p.wide_q ? 32 * BW : 32) * d.kv_heads : 0;
-  p.grid_k = ks.n ? tiles_of(ks.n, ks.n_seg, 1, p.wide_k ? 32 * BW : 32) * d.kv_heads : 0;
-  if (p.grid_q * p.splits_q + p.grid_k * p.splits_k > MAX_GROUPS) p.splits_q = p.splits_k = 1;
-  p.grid_q *= p.splits_q, p.grid_k *= p.splits_k;
-  return p;
-}
-
 struct BwdWs {
   float *shift, *minus_d, *q, *k, *v;
   size_t total;

@@ -26,7 +26,7 @@ constexpr int BT = 256, BW = 4;   // threads and waves of a workgroup
 template <typename T, int D, bool FEW, bool KEYS_OWNED>
 struct Bwd {
   static constexpr bool DMA = sizeof(T) == 2;
-  static constexpr int OWN = FEW ? 32 : 32 * BW;
+  static constexpr int OWN = FEW ? FEW_ROWS : WIDE_ROWS;
   static constexpr int BN = FEW ? 32 * BW : DMA ? 64 : 32;
   static constexpr int SUB = FEW ? 1 : BN / 32;
   static constexpr int PITCH = DMA ? 2 * D : pitch_of<T, D, true>(), MATRIX = BN * PITCH;
@@ -35,6 +35,7 @@ struct Bwd {
   static constexpr int PER = BN * D * (int)sizeof(T) / 16 / BT, STEP = BT * 16 / (D * (int)sizeof(T));
   static constexpr bool AHEAD = !(FEW && D == 128);
   static constexpr int HELD = AHEAD ? PER : 1;
+  static_assert(FEW_ROWS == 32 && WIDE_ROWS == 32 * BW, "32 rows or keys to a wave");
   static_assert(!FEW || MATRIX >= 2 * 32 * D * 4, "two waves' parts fit into a matrix");
   static_assert(PER >= 1 && PER * BT * 16 == BN * D * (int)sizeof(T), "whole units for every thread");
 };

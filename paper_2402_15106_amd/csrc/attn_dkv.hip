@@ -27,7 +27,7 @@ void launch_attention_dkv(dsmp_handle* h, const dsmp_attention_desc& d, const At
     constexpr int D = decltype(width)::value;
     using M = decltype(mode);
     constexpr bool PAIRS = sizeof(T) == 2 && M::DIM > 0;   // something to gain
-    if (PAIRS && a.G % 2 == 0) hipLaunchKernelGGL((k_attn_dkv<T, D, PAIRS, M>), dim3((unsigned)grid), dim3(BT), 0, h->stream, a);
+    if (PAIRS && rows_paired(d)) hipLaunchKernelGGL((k_attn_dkv<T, D, PAIRS, M>), dim3((unsigned)grid), dim3(BT), 0, h->stream, a);
     else hipLaunchKernelGGL((k_attn_dkv<T, D, false, M>), dim3((unsigned)grid), dim3(BT), 0, h->stream, a);
   });
 }

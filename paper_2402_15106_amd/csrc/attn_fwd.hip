@@ -20,7 +20,7 @@ constexpr int NT = 256, NW = 4;   // threads and waves of a workgroup
 template <typename T, int D, bool FEW>
 struct Fwd {
   static constexpr bool DMA = sizeof(T) == 2;
-  static constexpr int ROWS = FEW ? 32 : 32 * NW;
+  static constexpr int ROWS = FEW ? FEW_ROWS : WIDE_ROWS;
   static constexpr int BN = FEW ? 32 * NW : DMA ? 64 : 32;
   static constexpr int SUB = FEW ? 1 : BN / 32;   // blocks of 32 keys that a wave takes of a tile
   static constexpr int PITCH = DMA ? 2 * D : pitch_of<T, D, true>(), MATRIX = BN * PITCH, PLACES = 3 * BN;
@@ -28,6 +28,7 @@ struct Fwd {
   static constexpr int PER = BN * D * (int)sizeof(T) / 16 / NT, STEP = NT * 16 / (D * (int)sizeof(T));
   static constexpr bool AHEAD = !(FEW && D == 128);
   static constexpr int HELD = AHEAD || PER < 4 ? PER : 4;
+  static_assert(FEW_ROWS == 32 && WIDE_ROWS == 32 * NW, "32 rows to a wave");
   static_assert(!FEW || MATRIX >= 2 * 32 * D * 4, "two waves' parts fit into a matrix");
   static_assert(PER >= 1 && PER * NT * 16 == BN * D * (int)sizeof(T), "whole units for every thread");
   // waves to a SIMD that the registers are cut to
@@ -327,7 +328,6 @@ __global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::template WAVES<M>)) void k_att
 // The splits of a query's head, joined in their order.  A split without keys has the sum 0
 // and has written no values.  FEW_SPLITS: 32 lanes to each; otherwise a workgroup of 1,024, whose
 // 32 slices of the splits are added up.
-constexpr int FEW_SPLITS = 8, MAX_SPLITS = 1024;
 
 __device__ __forceinline__ bool in_segments(const AttnArgs& a, int64_t query) {
   return query >= a.qb.at(0) && query < a.qb.at(a.n_seg);
@@ -433,34 +433,6 @@ __global__ __launch_bounds__(1024) void k_attn_join(AttnArgs a) {
     for (int s = 0; s < 32; ++s) v[e] += red[s][c + e];
   }
   write_joined<T>(a, slot, query, c, v, top, total);
-}
-
-struct FwdPlan {
-  bool few;
-  int splits;
-  int64_t grid;
-};
-
-FwdPlan fwd_plan(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks) {
-  const int G = d.heads / d.kv_heads;
-  const int64_t keys = ks.n / ks.n_seg;
-  const double bytes = 4.0 * qs.n * d.heads * d.head_dim;
-  const int per_wide = d.dtype == DSMP_F32 ? 32 : 64;
-  Cut wide{about_tiles(qs.n, qs.n_seg, G, 32 * NW) * d.kv_heads, (keys + per_wide - 1) / per_wide, tile_us(d, FORWARD, true), bytes, 1};
-  Cut few{about_tiles(qs.n, qs.n_seg, G, 32) * d.kv_heads, (keys + 127) / 128, tile_us(d, FORWARD, false), bytes, 1};
-  double end = uneven_end(ks);
-  // one tile of rows to a segment: keys and values come from memory, once, at 5 TB/s
-  const bool once = qs.n * G <= 32 * qs.n_seg;
-  if (once) end *= 2, few.us = std::max(few.us, 128 * d.head_dim * (d.dtype == DSMP_F32 ? 8.0 : 4.0) * 256 / 5e6);
-  const double tw = cut_evenly(&wide, 1, held(d, FORWARD, true), 64, end);
-  const double tf = cut_evenly(&few, 1, held(d, FORWARD, false), MAX_SPLITS, end);
-  FwdPlan p{};
-  p.few = once || tf <= tw;
-  p.splits = p.few ? few.splits : wide.splits;
-  p.grid = tiles_of(qs.n, qs.n_seg, G, p.few ? 32 : 32 * NW) * d.kv_heads;
-  if (p.grid * p.splits > MAX_GROUPS) p.splits = 1;
-  p.grid *= p.splits;
-  return p;
 }
 
 size_t fwd_bytes(const dsmp_attention_desc& d, const dsmp_segments& qs, const dsmp_segments& ks) {
