@@ -56,7 +56,6 @@ class AttentionLayer:
                                     norm=s.norm, eps=s.eps)
         self.attend = L.attention_desc(s.heads, s.kv_heads, s.head_dim, s.dtype, dim=s.dim if s.distance else 0, cap=s.cap)
         self.wq, self.wk = s.heads * s.head_dim, s.kv_heads * s.head_dim
-        self._rows = torch.arange(s.n, dtype=torch.int32, device=lib.device)[:, None]
         self._kept = None
 
     def _checked(self, u, what):
@@ -74,7 +73,8 @@ class AttentionLayer:
         self.lib._segments(self.s.n, segments)   # refused here, or they are bounds on the device
         if not isinstance(segments, torch.Tensor):
             return None
-        below = self._rows < segments[::segments.numel() - 1]   # the first bound and the last one
+        rows = torch.arange(self.s.n, dtype=torch.int32, device=segments.device)[:, None]   # on the call's own stream
+        below = rows < segments[::segments.numel() - 1]   # the first bound and the last one
         return below[:, :1] == below[:, 1:]
 
     @staticmethod

@@ -98,3 +98,23 @@ def test_refusals(env):  # noqa: F811
         with pytest.raises(dm.DsmpError) as e:
             layer.backward(g)
         assert e.value.status == dm.INVALID_ARG
+
+
+def test_on_a_stream_of_its_own(env):  # noqa: F811
+    """A layer made on one stream and run on another at once: nothing of it waits on the first."""
+    dm, lib, torch = env
+    c = Setup(env, "f32", n=300, bounds=[5, 100, 250])
+    c.u[250:], c.gf[:5] = float("nan"), float("inf")
+    layer = dm.AttentionLayer(lib, c.s)
+    want = layer.forward(c.p, c.u, c.pos, c.seg), *layer.backward(c.gf)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    busy = torch.randn(4096, 4096, device="cuda")
+    for _ in range(20):
+        busy = torch.mm(busy, busy).clamp_(-1, 1)
+    other = dm.AttentionLayer(lib, c.s)
+    with torch.cuda.stream(side):
+        got = other.forward(c.p, c.u, c.pos, c.seg), *other.backward(c.gf)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert all(torch.equal(got[2][k], want[2][k]) for k in want[2])
