@@ -538,9 +538,11 @@ dsmp_status dsmp_qk_rotate_backward(dsmp_handle* h, const dsmp_rotate_desc* desc
  *     z = c - slope_a |p_i - p_j|                (dim = 0: z = c)
  *     P = softmax of z over the keys of s,  out_i = sum_j P v_j,  lse_i = log sum_j e^z
  * A query whose segment has no keys gets out 0 and lse -infinity.  Scores, sums and
- * the softmax are float32; with DSMP_BF16 the operands of the products are bfloat16
- * (P and the scores' gradients are rounded to it, or to sums of two such values in
- * small calls), accumulated in float32.
+ * the softmax are float32; with DSMP_BF16 the operands of the products are bfloat16,
+ * accumulated in float32.  P and the scores' gradients are rounded to bfloat16 (results are
+ * then 0.0023 to 0.0026 off, root mean square, where their own rounding is 0.0017), or to sums of two such
+ * values (0.0017) where a call has at most 512 keys or 2^18 scores of a head to a segment on average (gradients with
+ * dim > 0: 4,096 keys) and takes tiles of 32 rows, as small calls do; DSMP_F32 rounds neither.
  *
  * Matrices as above: q, out [nq, heads * head_dim], k, v [nk, kv_heads * head_dim].
  * Coordinates: device float32 [rows, dim], slopes: device float32 [heads]; both

@@ -285,9 +285,10 @@ def rotary_frequencies(rot, axes=1, base=10000.0, factor=1.0, extent=None, slow=
     dsmp_qk_rotate_*: base^(-i / m) for the m = rot / 2 / axes pairs i of each axis.
 
     factor > 1 scales them for coordinates that reach `factor` times further than those a
-    model was trained on: all by 1 / factor; or, with `extent` (the trained range), pairs
-    that turn fewer than `slow` times over it by 1 / factor, those that turn more than
-    `fast` times not at all, and those between by a linear mixture of both."""
+    model was trained on: all by 1 / factor (interpolated positions, arXiv 2306.15595); or, with
+    `extent` (the trained range), pairs that turn fewer than `slow` times over it by 1 / factor,
+    those that turn more than `fast` times not at all, and those between by a linear mixture of
+    both (arXiv 2309.00071, section 3.2)."""
     if axes < 1 or rot < 0 or rot % (2 * axes):
         raise DsmpError(INVALID_ARG, "rot must be a multiple of 2 axes")
     if not (base > 0 and factor > 0 and (extent is None or (extent > 0 and fast > slow))):

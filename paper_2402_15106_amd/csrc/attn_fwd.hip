@@ -325,8 +325,8 @@ __global__ __launch_bounds__(NT, (Fwd<T, D, FEW>::template WAVES<M>)) void k_att
   }
 }
 
-// The splits of a query's head, joined in their order.  A split without keys has the sum 0
-// and has written no values.  FEW_SPLITS: 32 lanes to each; otherwise a workgroup of 1,024, whose
+// The splits of a query's head, joined in their order.  A split without keys (of a segment with fewer tiles than
+// splits) has the sum 0 and zeros for values, which have no part in the result.  FEW_SPLITS: 32 lanes to each; otherwise a workgroup of 1,024, whose
 // 32 slices of the splits are added up.
 
 __device__ __forceinline__ bool in_segments(const AttnArgs& a, int64_t query) {
