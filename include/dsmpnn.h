@@ -522,7 +522,9 @@ dsmp_status dsmp_qk_rotate_forward(dsmp_handle* h, const dsmp_rotate_desc* desc,
  * with respect to q and k, and may be grad_q_out, grad_k_out themselves (with their
  * row distance).  dgamma_q, dgamma_k: device float32 [head_dim] (NULL when the gamma
  * is), summed over rows and heads, overwritten, or added to when flags has
- * DSMP_GRAD_ACCUMULATE.  Coordinates and frequencies get no gradient. */
+ * DSMP_GRAD_ACCUMULATE.  Coordinates and frequencies get no gradient.  All n rows count:
+ * where attention leaves rows out (room around the segments), its gradients there have to be
+ * 0 and q, k and pos finite, or dgamma is of what they hold. */
 dsmp_status dsmp_qk_rotate_workspace(const dsmp_rotate_desc* desc, int64_t n, size_t* bwd_ws_bytes);
 dsmp_status dsmp_qk_rotate_backward(dsmp_handle* h, const dsmp_rotate_desc* desc, int64_t n, const void* q, int64_t ldq,
                                     const void* k, int64_t ldk, const float* gamma_q, const float* gamma_k,

@@ -932,7 +932,8 @@ class Dsmp:
     def dsmp_attention_backward(self, desc: AttentionDesc, q, k, v, out, lse, grad_out, segments=None, k_segments=None,
                                 pos=None, k_pos=None, slopes=None, grad_q=None, grad_k=None, grad_v=None, ws=None):
         """Gradients with respect to q, k and v of the forward call that returned out and lse; returns
-        (grad_q, grad_k, grad_v), of the matrices' own type."""
+        (grad_q, grad_k, grad_v), of the matrices' own type.  Rows of no segment are left alone here too: in
+        a tensor that the call makes they are not set."""
         nq, dt, qshape, kshape, qs, ks, args = self._attn_inputs(desc, q, k, v, segments, k_segments, pos, k_pos, slopes)
         args += [*self._rows(out, "out", qshape, dt), self._flat(lse, "lse", (nq, desc.heads)),
                  *self._rows(grad_out, "grad_out", qshape, dt)]
